@@ -460,6 +460,46 @@ jp_status jp_budget_lambda_static(const float* logp_actor, const float* logp_pol
                                   const uint8_t* mask, int64_t T, float budget, float* out_lambda,
                                   void* cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * The model's last layers around the token pass.  These calls keep nothing in the context: it gives
+ * them the device, the stream, the error text and the launch count, and any scratch is the caller's
+ * (a workspace of the stated size, 256-byte aligned, its content of no meaning before or after).  So they may be captured into CUDA
+ * graphs, and calls with different workspaces and outputs may run at the same time on different
+ * streams.  The calling thread's current device is left as it was.
+ *
+ * Layer norm and RMS norm of each row of x [T, H] (DEVICE, rows ld elements apart, 0 = H):
+ *   mu = mean(x), or 0 with JP_NORM_RMS;  r = 1 / sqrt(mean((x - mu)^2) + eps);
+ *   y = (x - mu) r weight + bias
+ * and backward, from dy = dL/dy and what the forward left in out_mean / out_rstd:
+ *   dx = r (g - mean(g) - xhat mean(g xhat)), g = dy weight, xhat = (x - mu) r  (no mean(g) with JP_NORM_RMS)
+ *   dweight = sum over rows of dy xhat,  dbias = sum over rows of dy.
+ * Sums and statistics are fp32; y and dx are rounded once.  The sums over rows are taken in a fixed
+ * order: the same call gives the same bits. */
+enum { JP_NORM_RMS = 1 };
+typedef struct {
+  int64_t T;             /* rows; 0 is legal (a backward then writes zero dweight and dbias) */
+  int64_t H;             /* width, 1 .. 2^30-1 (pitches too)                                  */
+  int64_t ld_x, ld_y;    /* row pitches in elements, 0 = H (ld_y: of y)                      */
+  int64_t ld_dy, ld_dx;  /* backward                                                         */
+  int32_t dtype;         /* jp_dtype of x, y, dy, dx; pointers aligned to the element; 16-byte aligned
+                            pointers and pitches are faster                                  */
+  int32_t param_dtype;   /* jp_dtype of weight and bias                                      */
+  int32_t flags;         /* 0 or JP_NORM_RMS                                                 */
+  float eps;             /* >= 0, finite                                                     */
+} jp_norm_desc;
+/* weight [H], bias [H] or NULL; out_mean, out_rstd [T] fp32 or NULL (out_mean reads 0 with
+ * JP_NORM_RMS).  y may be x itself (same pointer and pitch); no other overlap. */
+jp_status jp_layer_norm_forward(jp_ctx* ctx, const jp_norm_desc* desc, const void* x, const void* weight,
+                                const void* bias, void* y, float* out_mean, float* out_rstd);
+/* Bytes of workspace jp_layer_norm_backward needs for these sizes on the context's device (0: bad
+ * arguments, or T == 0). */
+size_t jp_layer_norm_workspace_bytes(jp_ctx* ctx, int64_t T, int64_t H, int32_t dtype);
+/* mean (NULL with JP_NORM_RMS), rstd: [T] fp32.  dweight [H] fp32, dbias [H] fp32 or NULL: written, not added to.  dx may
+ * be dy or x itself (same pointer and pitch); no other overlap. */
+jp_status jp_layer_norm_backward(jp_ctx* ctx, const jp_norm_desc* desc, const void* dy, const void* x,
+                                 const void* weight, const float* mean, const float* rstd, void* dx,
+                                 float* dweight, float* dbias, void* workspace, size_t workspace_bytes);
+
 /* Self-test of the bounded waits (the paper has no counterpart).  Every wait inside the kernels
  * of this library (on a shared-memory barrier that the copy engine, another warp or the tensor
  * cores complete) gives up after a fixed number of SM clock cycles, sets JP_ERR_TIMEOUT in a

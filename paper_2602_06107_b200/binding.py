@@ -22,12 +22,14 @@ JP_STATIC_MAX_ROWS = 131072
 JP_ERR_TOO_LARGE = -8
 JP_DESC_KL = 1
 JP_DESC_SPARSE_CAP = 2
+JP_NORM_RMS = 1
 
 EXPORTS = (
     "jp_create", "jp_destroy", "jp_set_stream", "jp_obrs_workspace_bytes", "jp_reserve",
     "jp_obrs_forward", "jp_obrs_forward_sparse_actor", "jp_lmhead_lse_topk", "jp_obrs_forward_lmhead", "jp_obrs_backward", "jp_batch_begin", "jp_batch_chunk", "jp_batch_finalize",
     "jp_obrs_forward_host", "jp_selftest_bounded_wait", "jp_obrs_apply_kappa", "jp_batch_totals", "jp_obrs_apply_totals", "jp_batch_logprobs", "jp_obrs_row_lambda", "jp_vshard_record_floats", "jp_vshard_local", "jp_vshard_local_push", "jp_vshard_merge", "jp_vshard_backward", "jp_budget_lambda_static", "jp_probe_stream", "jp_status_string", "jp_last_error", "jp_launch_count",
     "jp_enable_kernel_timing", "jp_stream_kernel_times",
+    "jp_layer_norm_forward", "jp_layer_norm_workspace_bytes", "jp_layer_norm_backward",
 )
 
 
@@ -75,6 +77,14 @@ class jp_obrs_bwd_desc(ctypes.Structure):
         ("eps_lo", ctypes.c_float), ("eps_hi", ctypes.c_float), ("c2", ctypes.c_float), ("tis_cap", ctypes.c_float),
         ("out_obj_policy", ctypes.c_void_p), ("out_obj_actor", ctypes.c_void_p), ("out_kl", ctypes.c_void_p),
         ("out_loss", ctypes.c_void_p),
+    ]
+
+
+class jp_norm_desc(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int64), ("H", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64),
+        ("ld_dy", ctypes.c_int64), ("ld_dx", ctypes.c_int64), ("dtype", ctypes.c_int32),
+        ("param_dtype", ctypes.c_int32), ("flags", ctypes.c_int32), ("eps", ctypes.c_float),
     ]
 
 
@@ -136,6 +146,11 @@ def load():
     lib.jp_enable_kernel_timing.argtypes = [vp, ctypes.c_int]
     lib.jp_stream_kernel_times.argtypes = [vp, ctypes.POINTER(ctypes.c_float), i64]
     lib.jp_stream_kernel_times.restype = i64
+    lib.jp_layer_norm_forward.argtypes = [vp, ctypes.POINTER(jp_norm_desc), vp, vp, vp, vp, vp, vp]
+    lib.jp_layer_norm_workspace_bytes.argtypes = [vp, i64, i64, i32]
+    lib.jp_layer_norm_workspace_bytes.restype = ctypes.c_size_t
+    lib.jp_layer_norm_backward.argtypes = [vp, ctypes.POINTER(jp_norm_desc), vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                           ctypes.c_size_t]
     for name in EXPORTS:
         getattr(lib, name)          # raises AttributeError if the library lacks an entry point
     _lib = lib
@@ -171,6 +186,20 @@ class Context:
         if st != 0:
             raise JackpotError(f"jp_create failed: {self.lib.jp_status_string(st).decode()}")
         self.h = h
+        self.stream = int(stream)
+
+    def call_on_current_stream(self, fn, *args):
+        """For the entry points that keep nothing in the context: enqueues on torch's current stream of the
+        context's device, so that outputs and scratch from torch's allocator are used on the stream they belong to."""
+        cur = torch.cuda.current_stream(self.device).cuda_stream
+        if cur == self.stream:
+            self.check(fn(self.h, *args))
+            return
+        self.lib.jp_set_stream(self.h, cur)
+        try:
+            self.check(fn(self.h, *args))
+        finally:
+            self.lib.jp_set_stream(self.h, self.stream)
 
     def close(self):
         if getattr(self, "h", None):
@@ -393,6 +422,34 @@ def make_bwd_desc(advantages=None, lambda_distill=0.0, grad_out=1.0, n_valid=0, 
         setattr(b, name, t.data_ptr() if t is not None else None)
     b.eps_lo, b.eps_hi, b.c2, b.tis_cap = eps_lo, eps_hi, c2, tis_cap
     return b
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _check_device(ctx: Context, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != ctx.device:
+            raise JackpotError(f"tensor on {t.device}, but the context is on cuda:{ctx.device}")
+
+
+def jp_layer_norm_forward(ctx: Context, desc: jp_norm_desc, x, weight, bias, y, out_mean, out_rstd):
+    _check_device(ctx, x, weight, bias, y, out_mean, out_rstd)
+    ctx.call_on_current_stream(ctx.lib.jp_layer_norm_forward, ctypes.byref(desc), _addr(x), _addr(weight), _addr(bias),
+                               _addr(y), _addr(out_mean), _addr(out_rstd))
+
+
+def jp_layer_norm_workspace_bytes(ctx: Context, T: int, H: int, dtype: int) -> int:
+    return int(ctx.lib.jp_layer_norm_workspace_bytes(ctx.h, T, H, dtype))
+
+
+def jp_layer_norm_backward(ctx: Context, desc: jp_norm_desc, dy, x, weight, mean, rstd, dx, dweight, dbias, workspace):
+    """``workspace``: a uint8 CUDA tensor of at least jp_layer_norm_workspace_bytes bytes, or None when T is 0."""
+    _check_device(ctx, dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
+    ctx.call_on_current_stream(ctx.lib.jp_layer_norm_backward, ctypes.byref(desc), _addr(dy), _addr(x), _addr(weight),
+                               _addr(mean), _addr(rstd), _addr(dx), _addr(dweight), _addr(dbias), _addr(workspace),
+                               0 if workspace is None else workspace.numel())
 
 
 def jp_enable_kernel_timing(ctx: Context, on: bool):

@@ -94,6 +94,21 @@ jp_status cuda_fail(jp_ctx* c, cudaError_t e, const char* what) {
   return fail(c, JP_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
 }
 
+// Sets the context's device for one call and restores the caller's.
+struct DeviceScope {
+  int prev = -1;
+  bool ok = true;
+  explicit DeviceScope(int device) {
+    int cur = 0;
+    if (cudaGetDevice(&cur) != cudaSuccess) { ok = false; return; }
+    if (cur != device) {
+      ok = cudaSetDevice(device) == cudaSuccess;
+      prev = cur;
+    }
+  }
+  ~DeviceScope() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 jp_status ensure_workspace(jp_ctx* c, int64_t rows, int k) {
@@ -778,6 +793,90 @@ jp_status jp_batch_logprobs(jp_ctx* c, float* out_logp_actor, float* out_logp_po
   cudaError_t e = launch_logprobs(c->rec_rows, c->rec, out_logp_actor, out_logp_policy, out_valid, c->stream);
   if (e != cudaSuccess) return cuda_fail(c, e, "log-prob copy launch");
   if (c->rec_rows > 0) c->launches += 1;
+  return JP_OK;
+}
+
+namespace {
+
+bool element_aligned(const void* p, int32_t dtype) { return ((uintptr_t)p & (dtype == JP_BF16 ? 1u : 3u)) == 0; }
+
+jp_status norm_args(jp_ctx* c, const jp_norm_desc* d, NormArgs* a) {
+  if (!d) return fail(c, JP_ERR_INVALID_ARG, "desc is NULL");
+  if (d->T < 0 || d->T > (int64_t)0x7fffffff || d->H < 1 || d->H > (int64_t)0x3fffffff)
+    return fail(c, JP_ERR_INVALID_ARG, "T or H out of range");
+  if ((d->dtype != JP_BF16 && d->dtype != JP_F32) || (d->param_dtype != JP_BF16 && d->param_dtype != JP_F32))
+    return fail(c, JP_ERR_INVALID_ARG, "unknown dtype");
+  if (d->flags & ~JP_NORM_RMS) return fail(c, JP_ERR_INVALID_ARG, "unknown flag");
+  if (!(d->eps >= 0.f) || !(d->eps < 3.0e38f)) return fail(c, JP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  a->T = d->T; a->H = d->H;
+  a->ld_x = d->ld_x ? d->ld_x : d->H;
+  a->ld_y = d->ld_y ? d->ld_y : d->H;
+  a->ld_dy = d->ld_dy ? d->ld_dy : d->H;
+  a->ld_dx = d->ld_dx ? d->ld_dx : d->H;
+  for (const int64_t ld : {a->ld_x, a->ld_y, a->ld_dy, a->ld_dx})     // (T < 2^31, so row * pitch stays within 63 bits)
+    if (ld < d->H || ld > (int64_t)0x3fffffff) return fail(c, JP_ERR_INVALID_ARG, "leading dimension < H or out of range");
+  a->dtype = d->dtype;
+  a->param_bf16 = d->param_dtype == JP_BF16;
+  a->rms = (d->flags & JP_NORM_RMS) != 0;
+  a->eps = d->eps;
+  return JP_OK;
+}
+
+}  // namespace
+
+jp_status jp_layer_norm_forward(jp_ctx* c, const jp_norm_desc* d, const void* x, const void* weight, const void* bias,
+                                void* y, float* out_mean, float* out_rstd) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  NormArgs a{};
+  jp_status st = norm_args(c, d, &a);
+  if (st != JP_OK) return st;
+  if (a.T == 0) return JP_OK;
+  if (!x || !weight || !y) return fail(c, JP_ERR_INVALID_ARG, "x, weight or y is NULL");
+  if (!element_aligned(x, d->dtype) || !element_aligned(y, d->dtype) || !element_aligned(weight, d->param_dtype) ||
+      !element_aligned(bias, d->param_dtype))
+    return fail(c, JP_ERR_ALIGNMENT, "x, y, weight and bias must be aligned to their elements");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  a.x = x; a.weight = weight; a.bias = bias; a.y = y; a.out_mean = out_mean; a.out_rstd = out_rstd;
+  const cudaError_t e = launch_norm_forward(a, c->stream, c->sms);
+  if (e != cudaSuccess) return cuda_fail(c, e, "layer norm launch");
+  c->launches += 1;
+  return JP_OK;
+}
+
+size_t jp_layer_norm_workspace_bytes(jp_ctx* c, int64_t T, int64_t H, int32_t dtype) {
+  if (!c || T < 1 || T > (int64_t)0x7fffffff || H < 1 || H > (int64_t)0x3fffffff || (dtype != JP_BF16 && dtype != JP_F32)) return 0;
+  return (size_t)norm_backward_groups(T, H, dtype, c->sms) * 2 * (size_t)H * sizeof(float);
+}
+
+jp_status jp_layer_norm_backward(jp_ctx* c, const jp_norm_desc* d, const void* dy, const void* x, const void* weight,
+                                 const float* mean, const float* rstd, void* dx, float* dweight, float* dbias,
+                                 void* workspace, size_t workspace_bytes) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  NormArgs a{};
+  jp_status st = norm_args(c, d, &a);
+  if (st != JP_OK) return st;
+  if (!dweight) return fail(c, JP_ERR_INVALID_ARG, "dweight is NULL");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  if (a.T == 0) {
+    cudaError_t e = cudaMemsetAsync(dweight, 0, (size_t)a.H * sizeof(float), c->stream);
+    if (e == cudaSuccess && dbias) e = cudaMemsetAsync(dbias, 0, (size_t)a.H * sizeof(float), c->stream);
+    return e == cudaSuccess ? JP_OK : cuda_fail(c, e, "cudaMemsetAsync");
+  }
+  if (!dy || !x || !weight || !rstd || !dx || (!mean && !a.rms))
+    return fail(c, JP_ERR_INVALID_ARG, "dy, x, weight, dx, rstd or mean is NULL");
+  if (!element_aligned(x, d->dtype) || !element_aligned(dy, d->dtype) || !element_aligned(dx, d->dtype) ||
+      !element_aligned(weight, d->param_dtype))
+    return fail(c, JP_ERR_ALIGNMENT, "x, dy, dx and weight must be aligned to their elements");
+  if (!workspace || workspace_bytes < jp_layer_norm_workspace_bytes(c, a.T, a.H, a.dtype))
+    return fail(c, JP_ERR_WORKSPACE, "workspace is NULL or smaller than jp_layer_norm_workspace_bytes");
+  if (((uintptr_t)workspace & 255u) != 0) return fail(c, JP_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  a.dy = dy; a.x = x; a.weight = weight; a.mean = mean; a.rstd = rstd; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
+  a.partial = (float*)workspace;
+  const cudaError_t e = launch_norm_backward(a, c->stream, c->sms);
+  if (e != cudaSuccess) return cuda_fail(c, e, "layer norm backward launch");
+  c->launches += 2;
   return JP_OK;
 }
 

@@ -247,4 +247,28 @@ cudaError_t launch_lmhead(const void* hidden, int64_t ldh, const void* weight, i
                           int32_t* status, float* out_lse, float* out_logp, int32_t* out_idx, float* out_val,
                           cudaStream_t s);
 
+// Layer norm and RMS norm (jp_norm.cu).
+struct NormArgs {
+  const void* x;           // [T, ld_x]
+  const void* dy;          // backward: [T, ld_dy]
+  const void* weight;      // [H]
+  const void* bias;        // [H] or null
+  void* y;                 // forward: [T, ld_y]
+  void* dx;                // backward: [T, ld_dx]
+  int64_t T, H, ld_x, ld_y, ld_dy, ld_dx;
+  int32_t dtype;
+  bool param_bf16, rms;
+  float eps;
+  const float* mean;       // backward: [T] (unused for RMS norm)
+  const float* rstd;       // backward: [T]
+  float* out_mean;         // forward: [T] or null
+  float* out_rstd;         // forward: [T] or null
+  float* partial;          // backward: [groups, 2, H] workspace
+  float* dweight;          // [H]
+  float* dbias;            // [H] or null
+};
+cudaError_t launch_norm_forward(const NormArgs& a, cudaStream_t s, int sms);
+int64_t norm_backward_groups(int64_t T, int64_t H, int dtype, int sms);
+cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s, int sms);
+
 }  // namespace jp

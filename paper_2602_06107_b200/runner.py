@@ -120,10 +120,28 @@ def forward_sparse_actor(ctx: B.Context, zp, tokens, mask, logp_inf_token, topk_
     return out
 
 
+def _final_norm(ctx, h, norm):
+    """The model's last norm on its hidden states, ready for the context's stream."""
+    weight, bias, eps, rms = norm
+    y, _, _ = layer_norm(ctx, h, weight, bias, eps=eps, rms=rms)
+    current = torch.cuda.current_stream(ctx.device)
+    if current.cuda_stream != ctx.stream:
+        own = torch.cuda.ExternalStream(ctx.stream, device=ctx.device)
+        own.wait_stream(current)
+        y.record_stream(own)
+    return y
+
+
 def forward_lmhead(ctx: B.Context, h_actor, w_actor, h_policy, w_policy, tokens, mask=None, *, lam=None, budget=None, k=20,
-                   seed=0, token_offset=0, c1=0.0):
-    """One jp_obrs_forward_lmhead call; returns a dict of device tensors plus ``stats``."""
+                   seed=0, token_offset=0, c1=0.0, norm_actor=None, norm_policy=None):
+    """One jp_obrs_forward_lmhead call; returns a dict of device tensors plus ``stats``.  ``norm_actor`` /
+    ``norm_policy``: a model's last norm, ``(weight, bias or None, eps, rms)``, when ``h_*`` are the hidden states in
+    front of it (jp_layer_norm_forward runs first)."""
     assert (lam is None) != (budget is None)
+    if norm_actor is not None:
+        h_actor = _final_norm(ctx, h_actor, norm_actor)
+    if norm_policy is not None:
+        h_policy = _final_norm(ctx, h_policy, norm_policy)
     T, V = h_actor.shape[0], w_actor.shape[0]
     dev = h_actor.device
     out = _alloc_outputs(T, dev)
@@ -141,3 +159,68 @@ def forward_lmhead(ctx: B.Context, h_actor, w_actor, h_policy, w_policy, tokens,
     torch.cuda.synchronize(dev)
     out["stats"] = B.read_stats(out["stats_buf"])
     return out
+
+
+def _rows(t, name):
+    """[T, H] matrix with contiguous rows -> its row pitch in elements."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise B.JackpotError(f"{name} must be a matrix with contiguous rows")
+    if t.shape[0] <= 1:
+        return t.shape[1]
+    if t.stride(0) < t.shape[1]:
+        raise B.JackpotError(f"{name}: rows overlap")
+    return t.stride(0)
+
+
+def _vector(t, n, name, dtype=None):
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise B.JackpotError(f"{name} must be a contiguous vector of {n} elements")
+    if dtype is not None and t.dtype != dtype:
+        raise B.JackpotError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _norm_desc(x, weight, bias, eps, rms):
+    d = B.jp_norm_desc()
+    d.T, d.H = x.shape
+    _vector(weight, d.H, "weight")
+    if bias is not None:
+        _vector(bias, d.H, "bias", weight.dtype)
+    d.dtype, d.param_dtype = B._dtype_code(x), B._dtype_code(weight)
+    d.flags = B.JP_NORM_RMS if rms else 0
+    d.eps = eps
+    return d
+
+
+def layer_norm(ctx: B.Context, x, weight, bias=None, *, eps=1e-6, rms=False, out=None):
+    """One jp_layer_norm_forward call on torch's current stream: ``(y, mean, rstd)`` (mean None with ``rms``).
+    ``out``: where y goes (may be ``x``)."""
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    ld_x, ld_y = _rows(x, "x"), _rows(y, "out")
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise B.JackpotError("out must have x's shape and dtype")
+    d = _norm_desc(x, weight, bias, eps, rms)
+    d.ld_x, d.ld_y = ld_x, ld_y
+    mean = None if rms else torch.empty(d.T, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(d.T, dtype=torch.float32, device=x.device)
+    B.jp_layer_norm_forward(ctx, d, x, weight, bias, y, mean, rstd)
+    return y, mean, rstd
+
+
+def layer_norm_backward(ctx: B.Context, dy, x, weight, mean, rstd, *, rms=False, bias=True, dx=None):
+    """One jp_layer_norm_backward call on torch's current stream: ``(dx, dweight, dbias)`` with fp32 dweight and dbias
+    (dbias None without ``bias``).  ``mean`` and ``rstd`` are the forward's; ``dx``: where dx goes (may be ``dy`` or ``x``)."""
+    if dx is None:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    lds = _rows(x, "x"), _rows(dy, "dy"), _rows(dx, "dx")
+    if dy.shape != x.shape or dx.shape != x.shape or dy.dtype != x.dtype or dx.dtype != x.dtype:
+        raise B.JackpotError("dy and dx must have x's shape and dtype")
+    d = _norm_desc(x, weight, None, 0.0, rms)
+    d.ld_x, d.ld_dy, d.ld_dx = lds
+    if not rms:
+        _vector(mean, d.T, "mean", torch.float32)
+    _vector(rstd, d.T, "rstd", torch.float32)
+    sums = torch.empty((2 if bias else 1, d.H), dtype=torch.float32, device=x.device)
+    need = B.jp_layer_norm_workspace_bytes(ctx, d.T, d.H, d.dtype)
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    B.jp_layer_norm_backward(ctx, d, dy, x, weight, None if rms else mean, rstd, dx, sums[0], sums[1] if bias else None, ws)
+    return dx, sums[0], sums[1] if bias else None
