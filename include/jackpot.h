@@ -50,7 +50,7 @@ typedef enum {
   JP_ERR_TOO_LARGE = -8
 } jp_status;
 
-typedef enum { JP_BF16 = 0, JP_F32 = 1 } jp_dtype;
+typedef enum { JP_BF16 = 0, JP_F32 = 1, JP_F16 = 2 /* scales of 4-bit weights only */ } jp_dtype;
 typedef enum { JP_LAMBDA_FIXED = 0, JP_LAMBDA_FROM_BUDGET = 1 } jp_lambda_mode;
 
 enum { JP_MAX_TOPK = 128 };
@@ -499,6 +499,36 @@ size_t jp_layer_norm_workspace_bytes(jp_ctx* ctx, int64_t T, int64_t H, int32_t 
 jp_status jp_layer_norm_backward(jp_ctx* ctx, const jp_norm_desc* desc, const void* dy, const void* x,
                                  const void* weight, const float* mean, const float* rstd, void* dx,
                                  float* dweight, float* dbias, void* workspace, size_t workspace_bytes);
+
+/* Linear layer with 4-bit weights for a few tokens, such as the output layer of a quantised rollout
+ * model while it decodes (nothing is kept in the context, as above):
+ *   out[m, n] = sum_k x[m, k] (q[n, k] - z[n, k / group]) s[n, k / group]
+ * x [M, K] bf16, q in 0..15, group 32, 64 or 128 (the last group of a row may be short).  q - z is
+ * exact, each group's sum of exact products is fp32, and so are its scaling and the sum over groups; out is rounded once.
+ *
+ * jp_w4_pack lays the weights out once, when they are loaded:
+ *   q      : [N, ld_q] bytes (DEVICE), two values a byte, the lower k in the low half; ld_q in bytes,
+ *            0 = (K + 1) / 2
+ *   scales : [N, ld_scales] of scale_dtype JP_BF16 or JP_F16, 0 = ceil(K / group)
+ *   zeros  : [N, ld_zeros] uint8, values 0..15 (the low four bits are used), or NULL: 8 everywhere
+ *   packed : jp_w4_packed_bytes(N, K, group) bytes (DEVICE, 16-byte aligned), to be passed with the
+ *            same N, K and group to jp_w4_linear.  The layout is this library's own. */
+enum { JP_W4_MAX_TOKENS = 32 };
+typedef struct {
+  int64_t N;             /* output features, 1 .. 2^31-1            */
+  int64_t K;             /* input features, 1 .. 65536              */
+  int32_t group;         /* 32, 64 or 128                           */
+  int32_t scale_dtype;   /* jp_w4_pack: JP_BF16 or JP_F16           */
+  int64_t ld_q, ld_scales, ld_zeros;   /* jp_w4_pack                */
+} jp_w4_desc;
+/* 0: bad arguments */
+size_t jp_w4_packed_bytes(int64_t N, int64_t K, int32_t group);
+jp_status jp_w4_pack(jp_ctx* ctx, const jp_w4_desc* desc, const uint8_t* q, const void* scales,
+                     const uint8_t* zeros, void* packed);
+/* x [M, ld_x] bf16 and out [M, ld_out] of out_dtype (JP_BF16 or JP_F32), pointers aligned to their
+ * elements, 0 <= M <= JP_W4_MAX_TOKENS (more: JP_ERR_TOO_LARGE), ld = 0 means K and N. */
+jp_status jp_w4_linear(jp_ctx* ctx, const jp_w4_desc* desc, const void* packed, const void* x, int64_t ld_x,
+                       int64_t M, void* out, int64_t ld_out, int32_t out_dtype);
 
 /* Self-test of the bounded waits (the paper has no counterpart).  Every wait inside the kernels
  * of this library (on a shared-memory barrier that the copy engine, another warp or the tensor

@@ -15,7 +15,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libjackpot.so")
 
-JP_BF16, JP_F32 = 0, 1
+JP_BF16, JP_F32, JP_F16 = 0, 1, 2
 JP_LAMBDA_FIXED, JP_LAMBDA_FROM_BUDGET = 0, 1
 JP_MAX_TOPK = 128
 JP_STATIC_MAX_ROWS = 131072
@@ -23,6 +23,7 @@ JP_ERR_TOO_LARGE = -8
 JP_DESC_KL = 1
 JP_DESC_SPARSE_CAP = 2
 JP_NORM_RMS = 1
+JP_W4_MAX_TOKENS = 32
 
 EXPORTS = (
     "jp_create", "jp_destroy", "jp_set_stream", "jp_obrs_workspace_bytes", "jp_reserve",
@@ -30,6 +31,7 @@ EXPORTS = (
     "jp_obrs_forward_host", "jp_selftest_bounded_wait", "jp_obrs_apply_kappa", "jp_batch_totals", "jp_obrs_apply_totals", "jp_batch_logprobs", "jp_obrs_row_lambda", "jp_vshard_record_floats", "jp_vshard_local", "jp_vshard_local_push", "jp_vshard_merge", "jp_vshard_backward", "jp_budget_lambda_static", "jp_probe_stream", "jp_status_string", "jp_last_error", "jp_launch_count",
     "jp_enable_kernel_timing", "jp_stream_kernel_times",
     "jp_layer_norm_forward", "jp_layer_norm_workspace_bytes", "jp_layer_norm_backward",
+    "jp_w4_packed_bytes", "jp_w4_pack", "jp_w4_linear",
 )
 
 
@@ -85,6 +87,13 @@ class jp_norm_desc(ctypes.Structure):
         ("T", ctypes.c_int64), ("H", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64),
         ("ld_dy", ctypes.c_int64), ("ld_dx", ctypes.c_int64), ("dtype", ctypes.c_int32),
         ("param_dtype", ctypes.c_int32), ("flags", ctypes.c_int32), ("eps", ctypes.c_float),
+    ]
+
+
+class jp_w4_desc(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("group", ctypes.c_int32), ("scale_dtype", ctypes.c_int32),
+        ("ld_q", ctypes.c_int64), ("ld_scales", ctypes.c_int64), ("ld_zeros", ctypes.c_int64),
     ]
 
 
@@ -151,6 +160,10 @@ def load():
     lib.jp_layer_norm_workspace_bytes.restype = ctypes.c_size_t
     lib.jp_layer_norm_backward.argtypes = [vp, ctypes.POINTER(jp_norm_desc), vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                            ctypes.c_size_t]
+    lib.jp_w4_packed_bytes.argtypes = [i64, i64, i32]
+    lib.jp_w4_packed_bytes.restype = ctypes.c_size_t
+    lib.jp_w4_pack.argtypes = [vp, ctypes.POINTER(jp_w4_desc), vp, vp, vp, vp]
+    lib.jp_w4_linear.argtypes = [vp, ctypes.POINTER(jp_w4_desc), vp, vp, i64, i64, vp, i64, i32]
     for name in EXPORTS:
         getattr(lib, name)          # raises AttributeError if the library lacks an entry point
     _lib = lib
@@ -450,6 +463,21 @@ def jp_layer_norm_backward(ctx: Context, desc: jp_norm_desc, dy, x, weight, mean
     ctx.call_on_current_stream(ctx.lib.jp_layer_norm_backward, ctypes.byref(desc), _addr(dy), _addr(x), _addr(weight),
                                _addr(mean), _addr(rstd), _addr(dx), _addr(dweight), _addr(dbias), _addr(workspace),
                                0 if workspace is None else workspace.numel())
+
+
+def jp_w4_packed_bytes(N: int, K: int, group: int) -> int:
+    return int(load().jp_w4_packed_bytes(N, K, group))
+
+
+def jp_w4_pack(ctx: Context, desc: jp_w4_desc, q, scales, zeros, packed):
+    _check_device(ctx, q, scales, zeros, packed)
+    ctx.call_on_current_stream(ctx.lib.jp_w4_pack, ctypes.byref(desc), _addr(q), _addr(scales), _addr(zeros), _addr(packed))
+
+
+def jp_w4_linear(ctx: Context, desc: jp_w4_desc, packed, x, ld_x: int, M: int, out, ld_out: int, out_dtype: int):
+    _check_device(ctx, packed, x, out)
+    ctx.call_on_current_stream(ctx.lib.jp_w4_linear, ctypes.byref(desc), _addr(packed), _addr(x), ld_x, M, _addr(out),
+                               ld_out, out_dtype)
 
 
 def jp_enable_kernel_timing(ctx: Context, on: bool):

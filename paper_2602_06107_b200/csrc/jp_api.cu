@@ -880,6 +880,84 @@ jp_status jp_layer_norm_backward(jp_ctx* c, const jp_norm_desc* d, const void* d
   return JP_OK;
 }
 
+namespace {
+
+jp_status w4_shape(jp_ctx* c, const jp_w4_desc* d) {
+  if (!d) return fail(c, JP_ERR_INVALID_ARG, "desc is NULL");
+  if (d->N < 1 || d->N > (int64_t)0x7fffffff) return fail(c, JP_ERR_INVALID_ARG, "N out of range");
+  if (d->K < 1 || d->K > kW4MaxK) return fail(c, JP_ERR_INVALID_ARG, "K out of range (1 .. 65536)");
+  if (d->group != 32 && d->group != 64 && d->group != 128) return fail(c, JP_ERR_UNSUPPORTED, "group must be 32, 64 or 128");
+  return JP_OK;
+}
+
+}  // namespace
+
+size_t jp_w4_packed_bytes(int64_t N, int64_t K, int32_t group) {
+  if (N < 1 || N > (int64_t)0x7fffffff || K < 1 || K > kW4MaxK || (group != 32 && group != 64 && group != 128)) return 0;
+  return w4_packed_bytes(N, K, group);
+}
+
+jp_status jp_w4_pack(jp_ctx* c, const jp_w4_desc* d, const uint8_t* q, const void* scales, const uint8_t* zeros,
+                     void* packed) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  const jp_status st = w4_shape(c, d);
+  if (st != JP_OK) return st;
+  if (d->scale_dtype != JP_BF16 && d->scale_dtype != JP_F16) return fail(c, JP_ERR_INVALID_ARG, "scales must be JP_BF16 or JP_F16");
+  if (!q || !scales || !packed) return fail(c, JP_ERR_INVALID_ARG, "q, scales or packed is NULL");
+  if (!aligned16(packed)) return fail(c, JP_ERR_ALIGNMENT, "packed must be 16-byte aligned");
+  if ((uintptr_t)scales & 1u) return fail(c, JP_ERR_ALIGNMENT, "scales must be aligned to their elements");
+  const int64_t bytes = (d->K + 1) / 2, groups = (d->K + d->group - 1) / d->group, most = (int64_t)1 << 31;
+  W4PackArgs a{};
+  a.q = q; a.scales = scales; a.zeros = zeros; a.packed = packed;
+  a.N = d->N; a.K = d->K; a.group = d->group; a.scales_bf16 = d->scale_dtype == JP_BF16;
+  a.ld_q = d->ld_q ? d->ld_q : bytes;
+  a.ld_scales = d->ld_scales ? d->ld_scales : groups;
+  a.ld_zeros = d->ld_zeros ? d->ld_zeros : groups;
+  if (a.ld_q < bytes || a.ld_scales < groups || (zeros && a.ld_zeros < groups) || a.ld_q > most || a.ld_scales > most ||
+      a.ld_zeros > most)
+    return fail(c, JP_ERR_INVALID_ARG, "a leading dimension is smaller than a row or out of range");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  const cudaError_t e = launch_w4_pack(a, c->stream, c->sms);
+  if (e != cudaSuccess) return cuda_fail(c, e, "4-bit layout launch");
+  c->launches += 1;
+  return JP_OK;
+}
+
+jp_status jp_w4_linear(jp_ctx* c, const jp_w4_desc* d, const void* packed, const void* x, int64_t ld_x, int64_t M,
+                       void* out, int64_t ld_out, int32_t out_dtype) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  const jp_status st = w4_shape(c, d);
+  if (st != JP_OK) return st;
+  if (M < 0) return fail(c, JP_ERR_INVALID_ARG, "M < 0");
+  if (M > JP_W4_MAX_TOKENS) return fail(c, JP_ERR_TOO_LARGE, "more than JP_W4_MAX_TOKENS tokens");
+  if (out_dtype != JP_BF16 && out_dtype != JP_F32) return fail(c, JP_ERR_INVALID_ARG, "out must be JP_BF16 or JP_F32");
+  if (ld_x == 0) ld_x = d->K;
+  if (ld_out == 0) ld_out = d->N;
+  const int64_t most = (int64_t)1 << 40;
+  if (ld_x < d->K || ld_out < d->N || ld_x > most || ld_out > most)
+    return fail(c, JP_ERR_INVALID_ARG, "a leading dimension is smaller than a row or out of range");
+  if (M == 0) return JP_OK;
+  if (!packed || !x || !out) return fail(c, JP_ERR_INVALID_ARG, "packed, x or out is NULL");
+  if (!aligned16(packed)) return fail(c, JP_ERR_ALIGNMENT, "packed must be 16-byte aligned");
+  if (((uintptr_t)x & 1u) || !element_aligned(out, out_dtype))
+    return fail(c, JP_ERR_ALIGNMENT, "x and out must be aligned to their elements");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  W4Args a{};
+  a.packed = packed; a.N = d->N; a.K = d->K; a.ld_x = ld_x; a.ld_out = ld_out; a.out_bf16 = out_dtype == JP_BF16;
+  const int per = w4_tokens_per_launch(d->K);
+  for (int64_t m = 0; m < M; m += per) {
+    a.x = (const char*)x + m * ld_x * 2;
+    a.out = (char*)out + m * ld_out * (a.out_bf16 ? 2 : 4);
+    a.M = (int32_t)(M - m < per ? M - m : per);
+    const cudaError_t e = launch_w4(a, d->group, c->stream, c->sms);
+    if (e != cudaSuccess) return cuda_fail(c, e, "4-bit linear layer launch");
+    c->launches += 1;
+  }
+  return JP_OK;
+}
+
 jp_status jp_selftest_bounded_wait(jp_ctx* c, int64_t limit_cycles, int32_t* out_status) {
   if (!c) return JP_ERR_INVALID_ARG;
   if (limit_cycles < 1 || limit_cycles > 2000000000ll) return fail(c, JP_ERR_INVALID_ARG, "limit_cycles must lie in [1, 2e9] (about a second at most)");

@@ -271,4 +271,31 @@ cudaError_t launch_norm_forward(const NormArgs& a, cudaStream_t s, int sms);
 int64_t norm_backward_groups(int64_t T, int64_t H, int dtype, int sms);
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s, int sms);
 
+// Linear layers with 4-bit weights (jp_w4.cu).
+constexpr int kW4MaxTokens = 32;
+constexpr int64_t kW4MaxK = 65536;       // x of one token fits the kernel's shared memory
+struct W4PackArgs {
+  const uint8_t* q;        // [N, ld_q] bytes, two values each
+  const void* scales;      // [N, ld_scales]
+  const uint8_t* zeros;    // [N, ld_zeros] or null: 8
+  void* packed;
+  int64_t N, K, ld_q, ld_scales, ld_zeros;
+  int32_t group;
+  bool scales_bf16;        // else fp16
+  int64_t tiles, kblocks;  // set by the launch
+};
+struct W4Args {
+  const void* packed;
+  const void* x;           // [M, ld_x] bf16
+  void* out;               // [M, ld_out]
+  int64_t N, K, ld_x, ld_out;
+  int32_t M;
+  bool out_bf16;           // else fp32
+  int64_t tiles, kblocks;  // set by the launch
+};
+size_t w4_packed_bytes(int64_t N, int64_t K, int group);
+int w4_tokens_per_launch(int64_t K);
+cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms);
+cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms);
+
 }  // namespace jp

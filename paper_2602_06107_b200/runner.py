@@ -224,3 +224,72 @@ def layer_norm_backward(ctx: B.Context, dy, x, weight, mean, rstd, *, rms=False,
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     B.jp_layer_norm_backward(ctx, d, dy, x, weight, None if rms else mean, rstd, dx, sums[0], sums[1] if bias else None, ws)
     return dx, sums[0], sums[1] if bias else None
+
+
+class W4Weight:
+    """4-bit weights laid out by jp_w4_pack: what jp_w4_linear takes."""
+
+    def __init__(self, packed, N, K, group):
+        self.packed = packed
+        self.desc = B.jp_w4_desc(N=N, K=K, group=group)
+        self.N, self.K, self.group = N, K, group
+
+
+def quantize_w4(weight, group=128, *, symmetric=True, scale_dtype=torch.bfloat16):
+    """Rounds a [N, K] weight to 4 bits, each ``group`` of a row by its own largest magnitude (``symmetric``) or range:
+    ``(q [N, (K + 1) // 2] uint8, scales [N, groups], zeros [N, groups] uint8 or None)`` for :func:`pack_w4`."""
+    N, K = weight.shape
+    G = (K + group - 1) // group
+    w = torch.nn.functional.pad(weight.float(), (0, G * group - K)).view(N, G, group)
+    if symmetric:
+        scales = (w.abs().amax(2) / 7.0).to(scale_dtype)
+        zeros, z = None, 8.0
+    else:
+        lo, hi = w.amin(2).clamp(max=0.0), w.amax(2).clamp(min=0.0)
+        scales = ((hi - lo) / 15.0).to(scale_dtype)
+        s = scales.float()
+        z = torch.where(s > 0, -lo / s, torch.zeros_like(s)).round().clamp(0, 15)
+        zeros, z = z.to(torch.uint8), z[..., None]
+    s = scales.float()[..., None]
+    v = torch.where(s > 0, w / s, torch.zeros_like(w)).round()
+    v = (v + z).clamp(0, 15).to(torch.uint8).view(N, G * group)
+    v = v[:, :K + K % 2] if G * group >= K + K % 2 else torch.nn.functional.pad(v, (0, 1))
+    return (v[:, 0::2] | v[:, 1::2] << 4).contiguous(), scales, zeros
+
+
+def pack_w4(ctx: B.Context, q, scales, zeros=None, *, K, group=128):
+    """One jp_w4_pack call on torch's current stream: lays ``q`` [N, (K + 1) // 2] uint8 (two values a byte, the lower
+    index in the low half), ``scales`` [N, groups] bf16 or fp16 and ``zeros`` [N, groups] uint8 (None: 8) out once."""
+    N, bytes_, G = q.shape[0], (K + 1) // 2, (K + group - 1) // group
+    d = B.jp_w4_desc(N=N, K=K, group=group)
+    need = B.jp_w4_packed_bytes(N, K, group)
+    if need == 0:
+        raise B.JackpotError(f"no layout for N = {N}, K = {K}, group = {group} (1 <= K <= 65536; group 32, 64 or 128)")
+    codes = {torch.bfloat16: B.JP_BF16, torch.float16: B.JP_F16}
+    if q.dtype != torch.uint8 or scales.dtype not in codes or (zeros is not None and zeros.dtype != torch.uint8):
+        raise B.JackpotError("q and zeros must be uint8, scales bfloat16 or float16")
+    if q.shape != (N, bytes_) or scales.shape != (N, G) or (zeros is not None and zeros.shape != (N, G)):
+        raise B.JackpotError(f"for K = {K} and group = {group}: q must be [N, {bytes_}], scales and zeros [N, {G}]")
+    d.scale_dtype = codes[scales.dtype]
+    d.ld_q, d.ld_scales = _rows(q, "q"), _rows(scales, "scales")
+    if zeros is not None:
+        d.ld_zeros = _rows(zeros, "zeros")
+    packed = torch.empty(need, dtype=torch.uint8, device=q.device)
+    B.jp_w4_pack(ctx, d, q, scales, zeros, packed)
+    return W4Weight(packed, N, K, group)
+
+
+def linear_w4(ctx: B.Context, x, w: W4Weight, *, out_dtype=torch.bfloat16, out=None):
+    """One jp_w4_linear call on torch's current stream: x [M, K] bf16, M <= 32, times the packed weight: [M, N]."""
+    if x.dtype != torch.bfloat16:
+        raise B.JackpotError(f"x must be bfloat16, got {x.dtype}")
+    ld_x = _rows(x, "x")
+    M = x.shape[0]
+    if x.shape[1] != w.K:
+        raise B.JackpotError(f"x has {x.shape[1]} columns, the weight {w.K}")
+    if out is None:
+        out = torch.empty((M, w.N), dtype=out_dtype, device=x.device)
+    elif out.shape != (M, w.N):
+        raise B.JackpotError(f"out must be [{M}, {w.N}]")
+    B.jp_w4_linear(ctx, w.desc, w.packed, x, ld_x, M, out, _rows(out, "out"), B._dtype_code(out))
+    return out
