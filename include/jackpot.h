@@ -500,6 +500,47 @@ jp_status jp_layer_norm_backward(jp_ctx* ctx, const jp_norm_desc* desc, const vo
                                  const void* weight, const float* mean, const float* rstd, void* dx,
                                  float* dweight, float* dbias, void* workspace, size_t workspace_bytes);
 
+/* Verification of drafted tokens against the target model (speculative decoding of a rollout), from
+ * given random numbers: lossless rejection sampling, the emitted tokens are distributed as the
+ * target's own.  For each of B sequences with n <= N drafted tokens x_0 .. x_{n-1}, and p_i, q_i the
+ * softmax of target row i and draft row i over V entries at the sequence's temperature:
+ *   x_i is accepted while u_accept[i] < p_i(x_i) / q_i(x_i);
+ *   at the first rejection, position m, one token is drawn from max(p_m - q_m, 0) (normalised; from
+ *   p_m, should nothing be left above zero); when all are accepted (m = n), from p_n.
+ *   A draw is the first v whose cumulative mass, in the order of v, exceeds u_sample times the whole.
+ * The decisions and draws are those of the definition in 64 bits.  With draft_logits NULL the draft
+ * had no distribution (a lookup): q_i is 1 at x_i.  Temperature 0: x_i must be the target row's
+ * largest entry (the lowest index of several) and the emitted token is the largest entry.
+ * n = 0, or N = 0, samples one token from target row 0.
+ *   target_logits [B, N + 1, V], draft_logits [B, N, V] of desc->dtype, 16-byte aligned, pitches
+ *     multiples of 16 bytes; rows past a sequence's n drafts (n + 1 for the target) are not read
+ *   draft_tokens [B, N] int32 (an id outside [0, V) is a rejected draft), n_draft [B] int32 or NULL
+ *     (N everywhere; values are clamped to 0 .. N), temperature [B] fp32 or NULL (1 everywhere)
+ *   u_accept [B, N], u_sample [B] fp32 in [0, 1)
+ *   out_n_accepted [B] int32: m;  out_tokens [B, N + 1] int32: the m accepted drafts, the drawn token, then -1
+ *   out_accept_prob [B, N] fp32 or NULL: min(1, p_i(x_i) / q_i(x_i)) up to and with the first rejected draft, 0 after
+ *   out_logp [B, N + 1] fp32 or NULL: log p_i of each emitted token at the sequence's temperature (at 1 where it is
+ *     0), 0 elsewhere: what a rollout stores as log p_inf(a_t)
+ * -inf logits have probability 0.  A row that is needed and holds NaN or +inf, or nothing above -inf,
+ * rejects its draft, and the token that would be drawn from it is -1; so does a sequence whose
+ * temperature is neither 0 nor within 1e-4 .. 1e4 (with n_accepted 0).  Sequences do not affect one another. */
+enum { JP_VERIFY_MAX_DRAFT = 32 };
+typedef struct {
+  int64_t B;             /* sequences, 0 .. 65535                                       */
+  int64_t V;             /* vocabulary                                                  */
+  int64_t ld_target, seq_target;   /* pitches of rows and sequences in elements; 0: V, (N + 1) ld */
+  int64_t ld_draft, seq_draft;     /* 0: V, N ld                                        */
+  int32_t N;             /* draft places of a sequence, 0 .. JP_VERIFY_MAX_DRAFT        */
+  int32_t dtype;         /* jp_dtype of both tensors                                    */
+} jp_verify_desc;
+/* Bytes of workspace for these sizes on the context's device (0: bad arguments or B == 0). */
+size_t jp_verify_workspace_bytes(jp_ctx* ctx, int64_t B, int32_t N, int64_t V, int32_t dtype, int with_draft_logits);
+jp_status jp_verify_draft(jp_ctx* ctx, const jp_verify_desc* desc, const void* target_logits, const void* draft_logits,
+                          const int32_t* draft_tokens, const int32_t* n_draft, const float* temperature,
+                          const float* u_accept, const float* u_sample, int32_t* out_n_accepted,
+                          int32_t* out_tokens, float* out_accept_prob, float* out_logp, void* workspace,
+                          size_t workspace_bytes);
+
 /* Linear layer with 4-bit weights for a few tokens, such as the output layer of a quantised rollout
  * model while it decodes (nothing is kept in the context, as above):
  *   out[m, n] = sum_k x[m, k] (q[n, k] - z[n, k / group]) s[n, k / group]

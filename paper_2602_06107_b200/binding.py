@@ -24,6 +24,7 @@ JP_DESC_KL = 1
 JP_DESC_SPARSE_CAP = 2
 JP_NORM_RMS = 1
 JP_W4_MAX_TOKENS = 32
+JP_VERIFY_MAX_DRAFT = 32
 
 EXPORTS = (
     "jp_create", "jp_destroy", "jp_set_stream", "jp_obrs_workspace_bytes", "jp_reserve",
@@ -32,6 +33,7 @@ EXPORTS = (
     "jp_enable_kernel_timing", "jp_stream_kernel_times",
     "jp_layer_norm_forward", "jp_layer_norm_workspace_bytes", "jp_layer_norm_backward",
     "jp_w4_packed_bytes", "jp_w4_pack", "jp_w4_linear",
+    "jp_verify_workspace_bytes", "jp_verify_draft",
 )
 
 
@@ -94,6 +96,13 @@ class jp_w4_desc(ctypes.Structure):
     _fields_ = [
         ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("group", ctypes.c_int32), ("scale_dtype", ctypes.c_int32),
         ("ld_q", ctypes.c_int64), ("ld_scales", ctypes.c_int64), ("ld_zeros", ctypes.c_int64),
+    ]
+
+
+class jp_verify_desc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int64), ("V", ctypes.c_int64), ("ld_target", ctypes.c_int64), ("seq_target", ctypes.c_int64),
+        ("ld_draft", ctypes.c_int64), ("seq_draft", ctypes.c_int64), ("N", ctypes.c_int32), ("dtype", ctypes.c_int32),
     ]
 
 
@@ -164,6 +173,9 @@ def load():
     lib.jp_w4_packed_bytes.restype = ctypes.c_size_t
     lib.jp_w4_pack.argtypes = [vp, ctypes.POINTER(jp_w4_desc), vp, vp, vp, vp]
     lib.jp_w4_linear.argtypes = [vp, ctypes.POINTER(jp_w4_desc), vp, vp, i64, i64, vp, i64, i32]
+    lib.jp_verify_workspace_bytes.argtypes = [vp, i64, i32, i64, i32, ctypes.c_int]
+    lib.jp_verify_workspace_bytes.restype = ctypes.c_size_t
+    lib.jp_verify_draft.argtypes = [vp, ctypes.POINTER(jp_verify_desc)] + [vp] * 12 + [ctypes.c_size_t]
     for name in EXPORTS:
         getattr(lib, name)          # raises AttributeError if the library lacks an entry point
     _lib = lib
@@ -478,6 +490,21 @@ def jp_w4_linear(ctx: Context, desc: jp_w4_desc, packed, x, ld_x: int, M: int, o
     _check_device(ctx, packed, x, out)
     ctx.call_on_current_stream(ctx.lib.jp_w4_linear, ctypes.byref(desc), _addr(packed), _addr(x), ld_x, M, _addr(out),
                                ld_out, out_dtype)
+
+
+def jp_verify_workspace_bytes(ctx: Context, B: int, N: int, V: int, dtype: int, with_draft_logits: bool) -> int:
+    return int(ctx.lib.jp_verify_workspace_bytes(ctx.h, B, N, V, dtype, 1 if with_draft_logits else 0))
+
+
+def jp_verify_draft(ctx: Context, desc: jp_verify_desc, target_logits, draft_logits, draft_tokens, n_draft, temperature,
+                    u_accept, u_sample, out_n_accepted, out_tokens, out_accept_prob, out_logp, workspace):
+    """``workspace``: a uint8 CUDA tensor of at least jp_verify_workspace_bytes bytes, or None when B is 0."""
+    _check_device(ctx, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept, u_sample,
+                  out_n_accepted, out_tokens, out_accept_prob, out_logp, workspace)
+    ctx.call_on_current_stream(ctx.lib.jp_verify_draft, ctypes.byref(desc), _addr(target_logits), _addr(draft_logits),
+                               _addr(draft_tokens), _addr(n_draft), _addr(temperature), _addr(u_accept), _addr(u_sample),
+                               _addr(out_n_accepted), _addr(out_tokens), _addr(out_accept_prob), _addr(out_logp),
+                               _addr(workspace), 0 if workspace is None else workspace.numel())
 
 
 def jp_enable_kernel_timing(ctx: Context, on: bool):

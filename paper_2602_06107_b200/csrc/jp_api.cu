@@ -958,6 +958,69 @@ jp_status jp_w4_linear(jp_ctx* c, const jp_w4_desc* d, const void* packed, const
   return JP_OK;
 }
 
+namespace {
+
+// Sizes of a verification call; blocks of the row pass are counted in 31 bits.
+const char* verify_sizes(int64_t B, int32_t N, int64_t V, int32_t dtype, bool with_draft, int sms, VerifyPlan* p) {
+  if (B < 0 || B > 65535) return "B out of range (0 .. 65535)";
+  if (N < 0 || N > JP_VERIFY_MAX_DRAFT) return "N out of range (0 .. JP_VERIFY_MAX_DRAFT)";
+  if (V < 1 || V > (int64_t)0x7fffffff) return "V out of range";
+  if (dtype != JP_BF16 && dtype != JP_F32) return "unknown dtype";
+  *p = verify_plan(B > 0 ? B : 1, N, V, dtype, with_draft, sms);
+  return nullptr;
+}
+
+}  // namespace
+
+size_t jp_verify_workspace_bytes(jp_ctx* c, int64_t B, int32_t N, int64_t V, int32_t dtype, int with_draft_logits) {
+  VerifyPlan p{};
+  if (!c || B == 0 || verify_sizes(B, N, V, dtype, with_draft_logits != 0, c->sms, &p)) return 0;
+  return p.bytes;
+}
+
+jp_status jp_verify_draft(jp_ctx* c, const jp_verify_desc* d, const void* target_logits, const void* draft_logits,
+                          const int32_t* draft_tokens, const int32_t* n_draft, const float* temperature,
+                          const float* u_accept, const float* u_sample, int32_t* out_n_accepted, int32_t* out_tokens,
+                          float* out_accept_prob, float* out_logp, void* workspace, size_t workspace_bytes) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  if (!d) return fail(c, JP_ERR_INVALID_ARG, "desc is NULL");
+  if (d->N == 0) draft_logits = nullptr;
+  VerifyPlan p{};
+  if (const char* why = verify_sizes(d->B, d->N, d->V, d->dtype, draft_logits != nullptr, c->sms, &p))
+    return fail(c, JP_ERR_INVALID_ARG, why);
+  if (d->B == 0) return JP_OK;
+  const int64_t es = d->dtype == JP_BF16 ? 2 : 4, most = (int64_t)1 << 40;
+  VerifyArgs a{};
+  a.ld_target = d->ld_target ? d->ld_target : d->V;
+  a.seq_target = d->seq_target ? d->seq_target : (d->N + 1) * a.ld_target;
+  a.ld_draft = d->ld_draft ? d->ld_draft : d->V;
+  a.seq_draft = d->seq_draft ? d->seq_draft : d->N * a.ld_draft;
+  if (a.ld_target < d->V || a.ld_target > most || a.seq_target < 0 || a.seq_target > most ||
+      (draft_logits && (a.ld_draft < d->V || a.ld_draft > most || a.seq_draft < 0 || a.seq_draft > most)))
+    return fail(c, JP_ERR_INVALID_ARG, "a row pitch is smaller than V, or a pitch is out of range");
+  if (a.ld_target * es % 16 || a.seq_target * es % 16 || (draft_logits && (a.ld_draft * es % 16 || a.seq_draft * es % 16)))
+    return fail(c, JP_ERR_ALIGNMENT, "pitches of rows and sequences must be multiples of 16 bytes");
+  if (!target_logits || !u_sample || !out_n_accepted || !out_tokens || (d->N > 0 && (!draft_tokens || !u_accept)))
+    return fail(c, JP_ERR_INVALID_ARG, "a required pointer is NULL");
+  if (!aligned16(target_logits) || !aligned16(draft_logits)) return fail(c, JP_ERR_ALIGNMENT, "logits must be 16-byte aligned");
+  if (!workspace || workspace_bytes < p.bytes)
+    return fail(c, JP_ERR_WORKSPACE, "workspace is NULL or smaller than jp_verify_workspace_bytes");
+  if ((uintptr_t)workspace & 255u) return fail(c, JP_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  a.target = target_logits; a.draft = draft_logits; a.B = d->B; a.V = d->V; a.N = d->N;
+  a.tokens = draft_tokens; a.n_draft = n_draft; a.temperature = temperature; a.u_accept = u_accept; a.u_sample = u_sample;
+  a.out_n_accepted = out_n_accepted; a.out_tokens = out_tokens; a.out_accept_prob = out_accept_prob; a.out_logp = out_logp;
+  a.rows_per_seq = p.rows_per_seq; a.splits = p.splits; a.draw_splits = p.draw_splits;
+  a.ticket = (int32_t*)workspace;
+  a.parts = (char*)workspace + p.parts_off;
+  a.segs = (char*)workspace + p.segs_off;
+  const cudaError_t e = launch_verify(a, d->dtype, c->stream);
+  if (e != cudaSuccess) return cuda_fail(c, e, "draft verification launch");
+  c->launches += 2;
+  return JP_OK;
+}
+
 jp_status jp_selftest_bounded_wait(jp_ctx* c, int64_t limit_cycles, int32_t* out_status) {
   if (!c) return JP_ERR_INVALID_ARG;
   if (limit_cycles < 1 || limit_cycles > 2000000000ll) return fail(c, JP_ERR_INVALID_ARG, "limit_cycles must lie in [1, 2e9] (about a second at most)");

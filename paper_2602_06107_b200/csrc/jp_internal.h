@@ -298,4 +298,33 @@ int w4_tokens_per_launch(int64_t K);
 cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms);
 cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms);
 
+// Verification of drafted tokens (jp_verify.cu).
+constexpr int kVerifyMaxDraft = 32;
+struct VerifyPlan {
+  int rows_per_seq, splits, draw_splits;
+  size_t parts_off, segs_off, bytes;
+};
+VerifyPlan verify_plan(int64_t B, int N, int64_t V, int dtype, bool with_draft, int sms);
+struct VerifyArgs {
+  const void* target;      // [B, N + 1, V], rows ld_target apart, sequences seq_target (elements)
+  const void* draft;       // [B, N, V] or null
+  int64_t ld_target, seq_target, ld_draft, seq_draft;
+  int64_t B, V;
+  int32_t N;
+  const int32_t* tokens;   // [B, N]
+  const int32_t* n_draft;  // [B] or null
+  const float* temperature;   // [B] or null
+  const float* u_accept;   // [B, N]
+  const float* u_sample;   // [B]
+  int32_t* out_n_accepted; // [B]
+  int32_t* out_tokens;     // [B, N + 1]
+  float* out_accept_prob;  // [B, N] or null
+  float* out_logp;         // [B, N + 1] or null
+  int rows_per_seq, splits, draw_splits;
+  int32_t* ticket;         // [B]
+  void* parts;
+  void* segs;
+};
+cudaError_t launch_verify(VerifyArgs a, int dtype, cudaStream_t s);
+
 }  // namespace jp

@@ -293,3 +293,56 @@ def linear_w4(ctx: B.Context, x, w: W4Weight, *, out_dtype=torch.bfloat16, out=N
         raise B.JackpotError(f"out must be [{M}, {w.N}]")
     B.jp_w4_linear(ctx, w.desc, w.packed, x, ld_x, M, out, _rows(out, "out"), B._dtype_code(out))
     return out
+
+
+def _positions(t, B_, rows, V, name):
+    """[B, rows, V] logits with contiguous rows -> the pitches of rows and sequences in elements."""
+    if t.dim() != 3 or tuple(t.shape) != (B_, rows, V) or (V > 1 and t.stride(2) != 1):
+        raise B.JackpotError(f"{name} must be [{B_}, {rows}, {V}] with contiguous rows")
+    up = (V + 7) // 8 * 8                        # places with a single row have no pitch of their own: any that is allowed
+    ld = t.stride(1) if rows > 1 else up
+    seq = t.stride(0) if B_ > 1 else rows * ld
+    if ld < V or seq < (rows - 1) * ld + V:
+        raise B.JackpotError(f"{name}: rows or sequences overlap")
+    return ld, seq
+
+
+def _dense(t, shape, dtype, name):
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        raise B.JackpotError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)}")
+
+
+def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_accept, u_sample, *, n_draft=None,
+                 temperature=None, accept_prob=True, logp=True):
+    """One jp_verify_draft call on torch's current stream.  target_logits [B, N + 1, V], draft_logits [B, N, V] or None
+    (drafts without a distribution), draft_tokens [B, N] int32, u_accept [B, N] and u_sample [B] fp32, n_draft [B] int32
+    or None, temperature [B] fp32 or None.  Returns ``n_accepted`` [B], ``tokens`` [B, N + 1] and, unless turned off,
+    ``accept_prob`` [B, N] and ``logp`` [B, N + 1]."""
+    if target_logits.dim() != 3 or target_logits.shape[1] < 1:
+        raise B.JackpotError("target_logits must be [B, N + 1, V]")
+    n_seq, rows, V = target_logits.shape
+    N, dev = rows - 1, target_logits.device
+    d = B.jp_verify_desc(B=n_seq, V=V, N=N, dtype=B._dtype_code(target_logits))
+    d.ld_target, d.seq_target = _positions(target_logits, n_seq, rows, V, "target_logits")
+    if draft_logits is not None:
+        if draft_logits.dtype != target_logits.dtype:
+            raise B.JackpotError("draft_logits must have target_logits' dtype")
+        d.ld_draft, d.seq_draft = _positions(draft_logits, n_seq, N, V, "draft_logits")
+    _dense(draft_tokens, (n_seq, N), torch.int32, "draft_tokens")
+    _dense(u_accept, (n_seq, N), torch.float32, "u_accept")
+    _dense(u_sample, (n_seq,), torch.float32, "u_sample")
+    if n_draft is not None:
+        _dense(n_draft, (n_seq,), torch.int32, "n_draft")
+    if temperature is not None:
+        _dense(temperature, (n_seq,), torch.float32, "temperature")
+    out = dict(n_accepted=torch.empty(n_seq, dtype=torch.int32, device=dev),
+               tokens=torch.empty((n_seq, rows), dtype=torch.int32, device=dev))
+    if accept_prob:
+        out["accept_prob"] = torch.empty((n_seq, N), dtype=torch.float32, device=dev)
+    if logp:
+        out["logp"] = torch.empty((n_seq, rows), dtype=torch.float32, device=dev)
+    need = B.jp_verify_workspace_bytes(ctx, n_seq, N, V, d.dtype, draft_logits is not None and N > 0)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    B.jp_verify_draft(ctx, d, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept, u_sample,
+                      out["n_accepted"], out["tokens"], out.get("accept_prob"), out.get("logp"), ws)
+    return out
