@@ -521,7 +521,8 @@ jp_status jp_layer_norm_backward(jp_ctx* ctx, const jp_norm_desc* desc, const vo
  *   out_accept_prob [B, N] fp32 or NULL: min(1, p_i(x_i) / q_i(x_i)) up to and with the first rejected draft, 0 after
  *   out_logp [B, N + 1] fp32 or NULL: log p_i of each emitted token at the sequence's temperature (at 1 where it is
  *     0), 0 elsewhere: what a rollout stores as log p_inf(a_t)
- * -inf logits have probability 0.  A row that is needed and holds NaN or +inf, or nothing above -inf,
+ * -inf logits have probability 0, and so has what lies below 2^-840 (logits masked by the type's lowest
+ * value): such a draft is rejected whatever its q, and such an entry is not drawn.  A row that is needed and holds NaN or +inf, or nothing above -inf,
  * rejects its draft, and the token that would be drawn from it is -1; so does a sequence whose
  * temperature is neither 0 nor within 1e-4 .. 1e4 (with n_accepted 0).  Sequences do not affect one another. */
 enum { JP_VERIFY_MAX_DRAFT = 32 };

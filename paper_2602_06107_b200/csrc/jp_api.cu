@@ -1012,6 +1012,7 @@ jp_status jp_verify_draft(jp_ctx* c, const jp_verify_desc* d, const void* target
   a.tokens = draft_tokens; a.n_draft = n_draft; a.temperature = temperature; a.u_accept = u_accept; a.u_sample = u_sample;
   a.out_n_accepted = out_n_accepted; a.out_tokens = out_tokens; a.out_accept_prob = out_accept_prob; a.out_logp = out_logp;
   a.rows_per_seq = p.rows_per_seq; a.splits = p.splits; a.draw_splits = p.draw_splits;
+  a.split_vecs = p.split_vecs; a.seg_vecs = p.seg_vecs; a.n_segs = p.n_segs; a.block_segs = p.block_segs;
   a.ticket = (int32_t*)workspace;
   a.parts = (char*)workspace + p.parts_off;
   a.segs = (char*)workspace + p.segs_off;

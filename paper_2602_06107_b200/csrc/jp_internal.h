@@ -300,8 +300,11 @@ cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms);
 
 // Verification of drafted tokens (jp_verify.cu).
 constexpr int kVerifyMaxDraft = 32;
+constexpr int kVerifyMaxSplits = 64;     // slices of a row
+constexpr int kVerifyMaxSegs = 1024;     // segments of a draw
 struct VerifyPlan {
-  int rows_per_seq, splits, draw_splits;
+  int rows_per_seq, splits, draw_splits, n_segs, block_segs;
+  int64_t split_vecs, seg_vecs;   // 16-byte vectors of a slice, of a warp's segment
   size_t parts_off, segs_off, bytes;
 };
 VerifyPlan verify_plan(int64_t B, int N, int64_t V, int dtype, bool with_draft, int sms);
@@ -320,7 +323,8 @@ struct VerifyArgs {
   int32_t* out_tokens;     // [B, N + 1]
   float* out_accept_prob;  // [B, N] or null
   float* out_logp;         // [B, N + 1] or null
-  int rows_per_seq, splits, draw_splits;
+  int rows_per_seq, splits, draw_splits, n_segs, block_segs;
+  int64_t split_vecs, seg_vecs;
   int32_t* ticket;         // [B]
   void* parts;
   void* segs;

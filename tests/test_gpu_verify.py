@@ -75,7 +75,7 @@ def one_sequence(zt, zd, tok, u, us, n, t):
         if lp is not None and not draft_bad and 0 <= x < V:
             if t == 0:
                 a = float(x == int(np.argmax(zt[m])))
-            elif lp[x] > -np.inf:
+            elif lp[x] > -840 * math.log(2):                  # (below: probability 0)
                 a = math.exp(lp[x]) if lq is None else (np.inf if lq[x] == -np.inf else math.exp(min(lp[x] - lq[x], 700)))
         probs[m] = min(a, 1.0)
         if float(u[m]) < a:
