@@ -212,13 +212,16 @@ class Context:
             raise JackpotError(f"jp_create failed: {self.lib.jp_status_string(st).decode()}")
         self.h = h
         self.stream = int(stream)
+        self._sizes = {}                # workspace bytes by entry point and sizes
 
     def call_on_current_stream(self, fn, *args):
         """For the entry points that keep nothing in the context: enqueues on torch's current stream of the
         context's device, so that outputs and scratch from torch's allocator are used on the stream they belong to."""
-        cur = torch.cuda.current_stream(self.device).cuda_stream
+        cur = torch._C._cuda_getCurrentRawStream(self.device)
         if cur == self.stream:
-            self.check(fn(self.h, *args))
+            st = fn(self.h, *args)
+            if st:
+                self.check(st)
             return
         self.lib.jp_set_stream(self.h, cur)
         try:
@@ -449,31 +452,42 @@ def make_bwd_desc(advantages=None, lambda_distill=0.0, grad_out=1.0, n_valid=0, 
     return b
 
 
-def _addr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _check_device(ctx: Context, *tensors):
+def _on_device(ctx: Context, *tensors):
+    """Addresses of the tensors (None stays None), all of which must be on the context's device."""
+    device, out = ctx.device, []
     for t in tensors:
-        if t is not None and t.get_device() != ctx.device:
-            raise JackpotError(f"tensor on {t.device}, but the context is on cuda:{ctx.device}")
+        if t is None:
+            out.append(None)
+        elif t.get_device() == device:
+            out.append(t.data_ptr())
+        else:
+            raise JackpotError(f"tensor on {t.device}, but the context is on cuda:{device}")
+    return out
+
+
+def _workspace_bytes(ctx: Context, fn, *sizes) -> int:
+    key = (fn.__name__, sizes)
+    n = ctx._sizes.get(key)
+    if n is None:
+        n = ctx._sizes[key] = int(fn(ctx.h, *sizes))
+        if len(ctx._sizes) > 4096:
+            ctx._sizes.clear()
+    return n
 
 
 def jp_layer_norm_forward(ctx: Context, desc: jp_norm_desc, x, weight, bias, y, out_mean, out_rstd):
-    _check_device(ctx, x, weight, bias, y, out_mean, out_rstd)
-    ctx.call_on_current_stream(ctx.lib.jp_layer_norm_forward, ctypes.byref(desc), _addr(x), _addr(weight), _addr(bias),
-                               _addr(y), _addr(out_mean), _addr(out_rstd))
+    ctx.call_on_current_stream(ctx.lib.jp_layer_norm_forward, ctypes.byref(desc),
+                               *_on_device(ctx, x, weight, bias, y, out_mean, out_rstd))
 
 
 def jp_layer_norm_workspace_bytes(ctx: Context, T: int, H: int, dtype: int) -> int:
-    return int(ctx.lib.jp_layer_norm_workspace_bytes(ctx.h, T, H, dtype))
+    return _workspace_bytes(ctx, ctx.lib.jp_layer_norm_workspace_bytes, T, H, dtype)
 
 
 def jp_layer_norm_backward(ctx: Context, desc: jp_norm_desc, dy, x, weight, mean, rstd, dx, dweight, dbias, workspace):
     """``workspace``: a uint8 CUDA tensor of at least jp_layer_norm_workspace_bytes bytes, or None when T is 0."""
-    _check_device(ctx, dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
-    ctx.call_on_current_stream(ctx.lib.jp_layer_norm_backward, ctypes.byref(desc), _addr(dy), _addr(x), _addr(weight),
-                               _addr(mean), _addr(rstd), _addr(dx), _addr(dweight), _addr(dbias), _addr(workspace),
+    ctx.call_on_current_stream(ctx.lib.jp_layer_norm_backward, ctypes.byref(desc),
+                               *_on_device(ctx, dy, x, weight, mean, rstd, dx, dweight, dbias, workspace),
                                0 if workspace is None else workspace.numel())
 
 
@@ -482,29 +496,25 @@ def jp_w4_packed_bytes(N: int, K: int, group: int) -> int:
 
 
 def jp_w4_pack(ctx: Context, desc: jp_w4_desc, q, scales, zeros, packed):
-    _check_device(ctx, q, scales, zeros, packed)
-    ctx.call_on_current_stream(ctx.lib.jp_w4_pack, ctypes.byref(desc), _addr(q), _addr(scales), _addr(zeros), _addr(packed))
+    ctx.call_on_current_stream(ctx.lib.jp_w4_pack, ctypes.byref(desc), *_on_device(ctx, q, scales, zeros, packed))
 
 
 def jp_w4_linear(ctx: Context, desc: jp_w4_desc, packed, x, ld_x: int, M: int, out, ld_out: int, out_dtype: int):
-    _check_device(ctx, packed, x, out)
-    ctx.call_on_current_stream(ctx.lib.jp_w4_linear, ctypes.byref(desc), _addr(packed), _addr(x), ld_x, M, _addr(out),
-                               ld_out, out_dtype)
+    p, xa, oa = _on_device(ctx, packed, x, out)
+    ctx.call_on_current_stream(ctx.lib.jp_w4_linear, ctypes.byref(desc), p, xa, ld_x, M, oa, ld_out, out_dtype)
 
 
 def jp_verify_workspace_bytes(ctx: Context, B: int, N: int, V: int, dtype: int, with_draft_logits: bool) -> int:
-    return int(ctx.lib.jp_verify_workspace_bytes(ctx.h, B, N, V, dtype, 1 if with_draft_logits else 0))
+    return _workspace_bytes(ctx, ctx.lib.jp_verify_workspace_bytes, B, N, V, dtype, 1 if with_draft_logits else 0)
 
 
 def jp_verify_draft(ctx: Context, desc: jp_verify_desc, target_logits, draft_logits, draft_tokens, n_draft, temperature,
                     u_accept, u_sample, out_n_accepted, out_tokens, out_accept_prob, out_logp, workspace):
     """``workspace``: a uint8 CUDA tensor of at least jp_verify_workspace_bytes bytes, or None when B is 0."""
-    _check_device(ctx, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept, u_sample,
-                  out_n_accepted, out_tokens, out_accept_prob, out_logp, workspace)
-    ctx.call_on_current_stream(ctx.lib.jp_verify_draft, ctypes.byref(desc), _addr(target_logits), _addr(draft_logits),
-                               _addr(draft_tokens), _addr(n_draft), _addr(temperature), _addr(u_accept), _addr(u_sample),
-                               _addr(out_n_accepted), _addr(out_tokens), _addr(out_accept_prob), _addr(out_logp),
-                               _addr(workspace), 0 if workspace is None else workspace.numel())
+    ctx.call_on_current_stream(ctx.lib.jp_verify_draft, ctypes.byref(desc),
+                               *_on_device(ctx, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept,
+                                           u_sample, out_n_accepted, out_tokens, out_accept_prob, out_logp, workspace),
+                               0 if workspace is None else workspace.numel())
 
 
 def jp_enable_kernel_timing(ctx: Context, on: bool):

@@ -194,7 +194,7 @@ __device__ __noinline__ double exact_terms(uint4 v0, uint4 v1, float zref, doubl
 }
 
 constexpr int kGroup = 4;       // vectors a thread takes at a time
-constexpr int kGroups = 3;      // groups in flight: 48 KB a block
+constexpr int kGroups = 2;      // groups in flight: 32 KB a block (three were no faster)
 template <int DT> __device__ __forceinline__ uint4 neg_inf() { return Vec<DT>::neg_inf(); }
 
 // A thread's vectors p[tid], p[tid + kThreads], ... below n through its own places in shared memory, kGroups groups ahead (asynchronous
@@ -785,10 +785,9 @@ cudaError_t launch_verify(VerifyArgs a, int dtype, cudaStream_t s) {
   const dim3 g1((unsigned)a.splits, (unsigned)a.rows_per_seq, (unsigned)a.B), g2((unsigned)a.draw_splits, (unsigned)a.B);
   constexpr int kPlaces = kGroups * kGroup * kThreads * 16;
   auto* rows = dtype == JP_BF16 ? verify_rows_kernel<JP_BF16> : verify_rows_kernel<JP_F32>;
-  cudaError_t e = cudaFuncSetAttribute(rows, cudaFuncAttributeMaxDynamicSharedMemorySize, kPlaces);
-  if (e != cudaSuccess) return e;
   rows<<<g1, kThreads, kPlaces, s>>>(a);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = g2;
   cfg.blockDim = dim3(kThreads);

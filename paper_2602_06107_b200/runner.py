@@ -163,45 +163,48 @@ def forward_lmhead(ctx: B.Context, h_actor, w_actor, h_policy, w_policy, tokens,
 
 def _rows(t, name):
     """[T, H] matrix with contiguous rows -> its row pitch in elements."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise B.JackpotError(f"{name} must be a matrix with contiguous rows")
-    if t.shape[0] <= 1:
-        return t.shape[1]
-    if t.stride(0) < t.shape[1]:
+    if shape[0] <= 1:
+        return shape[1]
+    if stride[0] < shape[1]:
         raise B.JackpotError(f"{name}: rows overlap")
-    return t.stride(0)
+    return stride[0]
 
 
-def _vector(t, n, name, dtype=None):
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise B.JackpotError(f"{name} must be a contiguous vector of {n} elements")
-    if dtype is not None and t.dtype != dtype:
-        raise B.JackpotError(f"{name} must be {dtype}, got {t.dtype}")
+def _dense(t, shape, dtype, name):
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        raise B.JackpotError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)}")
 
 
-def _norm_desc(x, weight, bias, eps, rms):
-    d = B.jp_norm_desc()
-    d.T, d.H = x.shape
-    _vector(weight, d.H, "weight")
+def _norm_desc(x, weight, bias, eps, rms, out, name, dy=None):
+    """Checks and fills what both passes share; ``out`` is y or dx."""
+    d = B.jp_norm_desc(dtype=B._dtype_code(x), param_dtype=B._dtype_code(weight), flags=B.JP_NORM_RMS if rms else 0, eps=eps,
+                       ld_x=_rows(x, "x"))
+    shape = x.shape
+    d.T, d.H = shape
+    _dense(weight, shape[1:], weight.dtype, "weight")
     if bias is not None:
-        _vector(bias, d.H, "bias", weight.dtype)
-    d.dtype, d.param_dtype = B._dtype_code(x), B._dtype_code(weight)
-    d.flags = B.JP_NORM_RMS if rms else 0
-    d.eps = eps
+        _dense(bias, shape[1:], weight.dtype, "bias")
+    if out.shape != shape or out.dtype is not x.dtype:
+        raise B.JackpotError(f"{name} must have x's shape and dtype")
+    if dy is None:
+        d.ld_y = _rows(out, name)
+    else:
+        if dy.shape != shape or dy.dtype is not x.dtype:
+            raise B.JackpotError("dy must have x's shape and dtype")
+        d.ld_dx, d.ld_dy = _rows(out, name), _rows(dy, "dy")
     return d
 
 
 def layer_norm(ctx: B.Context, x, weight, bias=None, *, eps=1e-6, rms=False, out=None):
     """One jp_layer_norm_forward call on torch's current stream: ``(y, mean, rstd)`` (mean None with ``rms``).
     ``out``: where y goes (may be ``x``)."""
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    ld_x, ld_y = _rows(x, "x"), _rows(y, "out")
-    if y.shape != x.shape or y.dtype != x.dtype:
-        raise B.JackpotError("out must have x's shape and dtype")
-    d = _norm_desc(x, weight, bias, eps, rms)
-    d.ld_x, d.ld_y = ld_x, ld_y
-    mean = None if rms else torch.empty(d.T, dtype=torch.float32, device=x.device)
-    rstd = torch.empty(d.T, dtype=torch.float32, device=x.device)
+    y = x.new_empty(x.shape) if out is None else out
+    d = _norm_desc(x, weight, bias, eps, rms, y, "out")
+    mean = None if rms else x.new_empty(d.T, dtype=torch.float32)
+    rstd = x.new_empty(d.T, dtype=torch.float32)
     B.jp_layer_norm_forward(ctx, d, x, weight, bias, y, mean, rstd)
     return y, mean, rstd
 
@@ -210,20 +213,18 @@ def layer_norm_backward(ctx: B.Context, dy, x, weight, mean, rstd, *, rms=False,
     """One jp_layer_norm_backward call on torch's current stream: ``(dx, dweight, dbias)`` with fp32 dweight and dbias
     (dbias None without ``bias``).  ``mean`` and ``rstd`` are the forward's; ``dx``: where dx goes (may be ``dy`` or ``x``)."""
     if dx is None:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    lds = _rows(x, "x"), _rows(dy, "dy"), _rows(dx, "dx")
-    if dy.shape != x.shape or dx.shape != x.shape or dy.dtype != x.dtype or dx.dtype != x.dtype:
-        raise B.JackpotError("dy and dx must have x's shape and dtype")
-    d = _norm_desc(x, weight, None, 0.0, rms)
-    d.ld_x, d.ld_dy, d.ld_dx = lds
+        dx = x.new_empty(x.shape)
+    d = _norm_desc(x, weight, None, 0.0, rms, dx, "dx", dy)
+    T, H = x.shape
     if not rms:
-        _vector(mean, d.T, "mean", torch.float32)
-    _vector(rstd, d.T, "rstd", torch.float32)
-    sums = torch.empty((2 if bias else 1, d.H), dtype=torch.float32, device=x.device)
-    need = B.jp_layer_norm_workspace_bytes(ctx, d.T, d.H, d.dtype)
-    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-    B.jp_layer_norm_backward(ctx, d, dy, x, weight, None if rms else mean, rstd, dx, sums[0], sums[1] if bias else None, ws)
-    return dx, sums[0], sums[1] if bias else None
+        _dense(mean, (T,), torch.float32, "mean")
+    _dense(rstd, (T,), torch.float32, "rstd")
+    dweight = x.new_empty(H, dtype=torch.float32)
+    dbias = x.new_empty(H, dtype=torch.float32) if bias else None
+    need = B.jp_layer_norm_workspace_bytes(ctx, T, H, d.dtype)
+    ws = x.new_empty(need, dtype=torch.uint8) if need else None
+    B.jp_layer_norm_backward(ctx, d, dy, x, weight, None if rms else mean, rstd, dx, dweight, dbias, ws)
+    return dx, dweight, dbias
 
 
 class W4Weight:
@@ -288,28 +289,24 @@ def linear_w4(ctx: B.Context, x, w: W4Weight, *, out_dtype=torch.bfloat16, out=N
     if x.shape[1] != w.K:
         raise B.JackpotError(f"x has {x.shape[1]} columns, the weight {w.K}")
     if out is None:
-        out = torch.empty((M, w.N), dtype=out_dtype, device=x.device)
+        out = x.new_empty((M, w.N), dtype=out_dtype)
     elif out.shape != (M, w.N):
         raise B.JackpotError(f"out must be [{M}, {w.N}]")
     B.jp_w4_linear(ctx, w.desc, w.packed, x, ld_x, M, out, _rows(out, "out"), B._dtype_code(out))
     return out
 
 
-def _positions(t, B_, rows, V, name):
+def _positions(t, shape, name):
     """[B, rows, V] logits with contiguous rows -> the pitches of rows and sequences in elements."""
-    if t.dim() != 3 or tuple(t.shape) != (B_, rows, V) or (V > 1 and t.stride(2) != 1):
-        raise B.JackpotError(f"{name} must be [{B_}, {rows}, {V}] with contiguous rows")
-    up = (V + 7) // 8 * 8                        # places with a single row have no pitch of their own: any that is allowed
-    ld = t.stride(1) if rows > 1 else up
-    seq = t.stride(0) if B_ > 1 else rows * ld
+    stride = t.stride()
+    if t.shape != shape or (stride[2] != 1 and shape[2] > 1):
+        raise B.JackpotError(f"{name} must be {list(shape)} with contiguous rows")
+    n_seq, rows, V = shape
+    ld = stride[1] if rows > 1 else (V + 7) // 8 * 8         # a single row has no pitch of its own: any that is allowed
+    seq = stride[0] if n_seq > 1 else rows * ld
     if ld < V or seq < (rows - 1) * ld + V:
         raise B.JackpotError(f"{name}: rows or sequences overlap")
     return ld, seq
-
-
-def _dense(t, shape, dtype, name):
-    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
-        raise B.JackpotError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)}")
 
 
 def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_accept, u_sample, *, n_draft=None,
@@ -321,13 +318,15 @@ def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_ac
     if target_logits.dim() != 3 or target_logits.shape[1] < 1:
         raise B.JackpotError("target_logits must be [B, N + 1, V]")
     n_seq, rows, V = target_logits.shape
-    N, dev = rows - 1, target_logits.device
-    d = B.jp_verify_desc(B=n_seq, V=V, N=N, dtype=B._dtype_code(target_logits))
-    d.ld_target, d.seq_target = _positions(target_logits, n_seq, rows, V, "target_logits")
+    N = rows - 1
+    ld, seq = _positions(target_logits, (n_seq, rows, V), "target_logits")
+    d = B.jp_verify_desc(B=n_seq, V=V, N=N, dtype=B._dtype_code(target_logits), ld_target=ld, seq_target=seq)
     if draft_logits is not None:
-        if draft_logits.dtype != target_logits.dtype:
+        if draft_logits.dtype is not target_logits.dtype:
             raise B.JackpotError("draft_logits must have target_logits' dtype")
-        d.ld_draft, d.seq_draft = _positions(draft_logits, n_seq, N, V, "draft_logits")
+        if draft_logits.dim() != 3:
+            raise B.JackpotError("draft_logits must be [B, N, V]")
+        d.ld_draft, d.seq_draft = _positions(draft_logits, (n_seq, N, V), "draft_logits")
     _dense(draft_tokens, (n_seq, N), torch.int32, "draft_tokens")
     _dense(u_accept, (n_seq, N), torch.float32, "u_accept")
     _dense(u_sample, (n_seq,), torch.float32, "u_sample")
@@ -335,14 +334,14 @@ def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_ac
         _dense(n_draft, (n_seq,), torch.int32, "n_draft")
     if temperature is not None:
         _dense(temperature, (n_seq,), torch.float32, "temperature")
-    out = dict(n_accepted=torch.empty(n_seq, dtype=torch.int32, device=dev),
-               tokens=torch.empty((n_seq, rows), dtype=torch.int32, device=dev))
+    new = u_sample.new_empty
+    out = dict(n_accepted=new(n_seq, dtype=torch.int32), tokens=new((n_seq, rows), dtype=torch.int32))
     if accept_prob:
-        out["accept_prob"] = torch.empty((n_seq, N), dtype=torch.float32, device=dev)
+        out["accept_prob"] = torch.empty_like(u_accept)
     if logp:
-        out["logp"] = torch.empty((n_seq, rows), dtype=torch.float32, device=dev)
+        out["logp"] = new((n_seq, rows))
     need = B.jp_verify_workspace_bytes(ctx, n_seq, N, V, d.dtype, draft_logits is not None and N > 0)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    ws = new(need, dtype=torch.uint8) if need else None
     B.jp_verify_draft(ctx, d, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept, u_sample,
                       out["n_accepted"], out["tokens"], out.get("accept_prob"), out.get("logp"), ws)
     return out
