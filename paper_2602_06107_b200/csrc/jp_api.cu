@@ -946,12 +946,11 @@ jp_status jp_w4_linear(jp_ctx* c, const jp_w4_desc* d, const void* packed, const
   if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
   W4Args a{};
   a.packed = packed; a.N = d->N; a.K = d->K; a.ld_x = ld_x; a.ld_out = ld_out; a.out_bf16 = out_dtype == JP_BF16;
-  const int per = w4_tokens_per_launch(d->K);
-  for (int64_t m = 0; m < M; m += per) {
+  for (int64_t m = 0; m < M; m += a.M) {
     a.x = (const char*)x + m * ld_x * 2;
     a.out = (char*)out + m * ld_out * (a.out_bf16 ? 2 : 4);
-    a.M = (int32_t)(M - m < per ? M - m : per);
-    const cudaError_t e = launch_w4(a, d->group, c->stream, c->sms);
+    a.M = w4_tokens_per_launch(d->K, d->group, M - m);
+    const cudaError_t e = launch_w4(a, d->group, c->stream, c->sms, c->device);
     if (e != cudaSuccess) return cuda_fail(c, e, "4-bit linear layer launch");
     c->launches += 1;
   }

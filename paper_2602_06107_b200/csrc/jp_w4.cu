@@ -19,6 +19,8 @@
 // summed in shared memory in the warps' order (deterministic).  x is staged in shared memory once per CTA in B-fragment order.
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -28,8 +30,13 @@ namespace {
 constexpr int kTileRows = 16;
 constexpr int kBlockK = 128;
 constexpr int kWarps = 16;
-constexpr int kDepth = 4;             // blocks a warp has in flight
-constexpr int kXBytes = 128 * 1024;   // shared memory for x
+constexpr int kSharedBytes = 232448;  // of one block
+// Blocks a warp has in flight; what the ring and the warps' parts of shared tiles leave is for x.
+__host__ __device__ constexpr int depth_of(int groups) { return groups == 4 ? 4 : 5; }
+__host__ __device__ constexpr int block_bytes(int groups) { return 1024 + kTileRows * 4 * groups; }
+__host__ __device__ constexpr int part_bytes(int nt) { return kWarps * nt * 32 * 16; }
+__host__ __device__ constexpr int ring_bytes(int groups) { return kWarps * depth_of(groups) * block_bytes(groups); }
+constexpr int x_bytes(int nt, int groups) { return kSharedBytes - ring_bytes(groups) - part_bytes(nt); }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -45,27 +52,11 @@ __device__ __forceinline__ uint32_t dequant2(uint32_t w, int shift, uint32_t z12
   return *(const uint32_t*)&d;
 }
 
-template <int GROUPS> struct ScaleWords;      // a row's scale words of one block
-template <> struct ScaleWords<1> { uint32_t w[1]; };
-template <> struct alignas(8) ScaleWords<2> { uint32_t w[2]; };
-template <> struct alignas(16) ScaleWords<4> { uint32_t w[4]; };
-
-template <int GROUPS>
-struct Block {
-  uint4 q[2];
-  ScaleWords<GROUPS> s[2];                    // rows lane / 4 and lane / 4 + 8
-};
-
-template <int GROUPS>
-__device__ __forceinline__ void load_block(Block<GROUPS>& b, const char* p, int lane) {
-  b.q[0] = ldg_stream((const uint4*)p + lane);
-  b.q[1] = ldg_stream((const uint4*)p + 32 + lane);
-  const ScaleWords<GROUPS>* s = (const ScaleWords<GROUPS>*)(p + 1024);
-  b.s[0] = s[lane >> 2];
-  b.s[1] = s[(lane >> 2) + 8];
+__device__ __forceinline__ void copy16(void* smem, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global) : "memory");
 }
 
-template <int NT, int GROUPS>
+template <int NT>
 __device__ __forceinline__ void store_tile(const W4Args& A, const float (&acc)[NT][4], int64_t tile, int lane) {
   const int64_t n = tile * kTileRows + (lane >> 2);
 #pragma unroll
@@ -83,34 +74,49 @@ __device__ __forceinline__ void store_tile(const W4Args& A, const float (&acc)[N
 
 template <int NT, int GROUPS>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
-  constexpr int kBytes = 1024 + kTileRows * 4 * GROUPS;
+  constexpr int kBytes = block_bytes(GROUPS), kDepth = depth_of(GROUPS);
   extern __shared__ __align__(16) char smem[];
-  float4* slots = (float4*)smem;                                        // [warp][head, tail][NT][lane]
-  uint4* xs = (uint4*)(smem + kWarps * 2 * NT * 32 * 16);               // [block][step pair][token][lane % 4]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  char* ring = smem + warp * kDepth * kBytes;
+  float4* parts = (float4*)(smem + ring_bytes(GROUPS));                 // [warp][NT][lane]: of a tile that an earlier warp begins
+  uint4* xs = (uint4*)(smem + ring_bytes(GROUPS) + part_bytes(NT));     // [block][step pair][token][lane % 4]
+  const int kblocks = (int)A.kblocks;
   const int64_t tile0 = A.tiles * blockIdx.x / gridDim.x, tile1 = A.tiles * (blockIdx.x + 1) / gridDim.x;
-  const int64_t blocks = (tile1 - tile0) * A.kblocks;
+  const int64_t blocks = (tile1 - tile0) * kblocks;
   const int64_t b0 = blocks * warp / kWarps, b1 = blocks * (warp + 1) / kWarps;
-  const char* base = (const char*)A.packed + tile0 * A.kblocks * kBytes;
-  Block<GROUPS> ring[kDepth];
+  const int count = (int)(b1 - b0);
+  const char* src = (const char*)A.packed + (tile0 * kblocks + b0) * kBytes + lane * 16;
+  int issued = 0, slot_in = 0, slot_out = 0;
+  auto fetch = [&]() {
+    if (issued < count) {
+      copy16(ring + slot_in + lane * 16, src);
+      copy16(ring + slot_in + 512 + lane * 16, src + 512);
+      if (lane < 4 * GROUPS) copy16(ring + slot_in + 1024 + lane * 16, src + 1024);
+      src += kBytes;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    ++issued;
+    slot_in = slot_in == (kDepth - 1) * kBytes ? 0 : slot_in + kBytes;
+  };
 #pragma unroll
-  for (int j = 0; j < kDepth; ++j)
-    if (b0 + j < b1) load_block(ring[j], base + (b0 + j) * kBytes, lane);
+  for (int j = 0; j < kDepth; ++j) fetch();
 
   // x in B-fragment order: word w of unit (block, step pair, token, t) is columns 128 block + 32 pair + 16 (w / 2)
-  // + 8 (w % 2) + 2 t and the next
-  const int units = (int)A.kblocks * 4 * A.M * 4;
-  for (int u = tid; u < units; u += kWarps * 32) {
-    const int t = u & 3, m = (u >> 2) % A.M, pair = (u >> 2) / A.M;
-    const uint16_t* xr = (const uint16_t*)A.x + (int64_t)m * A.ld_x;
-    uint32_t w[4];
+  // + 8 (w % 2) + 2 t and the next.  A warp takes (token, block) by (token, block), a lane two pairs of columns of each.
+  {
+    const int tasks = A.M * kblocks;
+    for (int u = warp; u < tasks; u += kWarps) {
+      const int m = u % A.M, kb = u / A.M;
+      const uint16_t* xr = (const uint16_t*)A.x + (int64_t)m * A.ld_x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t k = (int64_t)pair * 32 + (i >> 1) * 16 + (i & 1) * 8 + t * 2;
-      const uint32_t lo = k < A.K ? xr[k] : 0, hi = k + 1 < A.K ? xr[k + 1] : 0;
-      w[i] = lo | hi << 16;
+      for (int h = 0; h < 2; ++h) {
+        const int in = lane * 2 + h * 64;                   // column within the block
+        const int64_t k = (int64_t)kb * kBlockK + in;
+        const uint32_t lo = k < A.K ? xr[k] : 0, hi = k + 1 < A.K ? xr[k + 1] : 0;
+        const int pair = in >> 5, w = (in >> 3) & 3, t = (in >> 1) & 3;
+        ((uint32_t*)(xs + ((kb * 4 + pair) * A.M + m) * 4 + t))[w] = lo | hi << 16;
+      }
     }
-    xs[u] = make_uint4(w[0], w[1], w[2], w[3]);
   }
   __syncthreads();
 
@@ -119,42 +125,62 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
-  int64_t tile = b0 / A.kblocks;                    // within the CTA's run
-  int kb = (int)(b0 - tile * A.kblocks);
+  int64_t tile = b0 / kblocks;                      // within the CTA's run
+  int kb = (int)(b0 - tile * kblocks);
   bool whole = kb == 0;                             // this warp has the tile from its first block on
-  for (int64_t b = b0; b < b1; b += kDepth) {
+  const int row = lane >> 2;
+  // (a column of B makes the same column of the result alone: places without a token take the last token's, and are not stored)
+  const uint4* xt[NT];
 #pragma unroll
-    for (int j = 0; j < kDepth; ++j) {
-      if (b + j < b1) {
-        const uint4* xb = xs + (int64_t)kb * 16 * A.M;
-        float part[NT][4];
+  for (int t = 0; t < NT; ++t) xt[t] = xs + min(t * 8 + row, A.M - 1) * 4 + (lane & 3);
+  const int x_pair = A.M * 4;
+  int x_at = kb * 4 * x_pair;
+  for (int b = 0; b < count; ++b) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    __syncwarp();
+    const char* blk = ring + slot_out;
+    uint32_t sw[2][GROUPS];
+    if constexpr (GROUPS == 1) {
+      sw[0][0] = ((const uint32_t*)(blk + 1024))[row];
+      sw[1][0] = ((const uint32_t*)(blk + 1024))[row + 8];
+    } else if constexpr (GROUPS == 2) {
+      *(uint2*)sw[0] = ((const uint2*)(blk + 1024))[row];
+      *(uint2*)sw[1] = ((const uint2*)(blk + 1024))[row + 8];
+    } else {
+      *(uint4*)sw[0] = ((const uint4*)(blk + 1024))[row];
+      *(uint4*)sw[1] = ((const uint4*)(blk + 1024))[row + 8];
+    }
+    float part[NT][4];
 #pragma unroll
-        for (int step = 0; step < 8; ++step) {
-          const int grp = step * GROUPS / 8;
+    for (int half = 0; half < 2; ++half) {
+      const uint4 v = ((const uint4*)blk)[half * 32 + lane];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int pair = half * 2 + p;
+        uint4 f[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) f[t] = xt[t][x_at + pair * x_pair];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int step = pair * 2 + h, grp = step * GROUPS / 8;
           if (step % (8 / GROUPS) == 0) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
               for (int e = 0; e < 4; ++e) part[t][e] = 0.f;
           }
-          const uint32_t z0 = (ring[j].s[0].w[grp] & 15u) * 0x00010001u | 0x43004300u;
-          const uint32_t z1 = (ring[j].s[1].w[grp] & 15u) * 0x00010001u | 0x43004300u;
-          const uint4& v = ring[j].q[step >> 2];
-          const uint32_t w = (step & 3) == 0 ? v.x : (step & 3) == 1 ? v.y : (step & 3) == 2 ? v.z : v.w;
+          const uint32_t z0 = (sw[0][grp] & 15u) * 0x00010001u + 0x43004300u;
+          const uint32_t z1 = (sw[1][grp] & 15u) * 0x00010001u + 0x43004300u;
+          const uint32_t w = p == 0 ? (h == 0 ? v.x : v.y) : (h == 0 ? v.z : v.w);
           uint32_t a[4];
           a[0] = dequant2(w, 0, z0);
           a[1] = dequant2(w, 4, z1);
           a[2] = dequant2(w, 8, z0);
           a[3] = dequant2(w, 12, z1);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const int m = t * 8 + (lane >> 2);
-            uint2 f = make_uint2(0u, 0u);
-            if (m < A.M) f = ((const uint2*)(xb + ((step >> 1) * A.M + m) * 4 + (lane & 3)))[step & 1];
-            mma_bf16(part[t], a, f.x, f.y);
-          }
+          for (int t = 0; t < NT; ++t) mma_bf16(part[t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
           if ((step + 1) % (8 / GROUPS) == 0) {
-            const float s0 = __uint_as_float(ring[j].s[0].w[grp] & ~15u), s1 = __uint_as_float(ring[j].s[1].w[grp] & ~15u);
+            const float s0 = __uint_as_float(sw[0][grp] & ~15u), s1 = __uint_as_float(sw[1][grp] & ~15u);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
               acc[t][0] = fmaf(part[t][0], s0, acc[t][0]);
@@ -164,52 +190,50 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
             }
           }
         }
-        if (b + j + kDepth < b1) load_block(ring[j], base + (b + j + kDepth) * kBytes, lane);
-        ++kb;
-        const bool tile_end = kb == A.kblocks;
-        if (tile_end || b + j + 1 == b1) {
-          if (tile_end && whole) {
-            store_tile<NT, GROUPS>(A, acc, tile0 + tile, lane);
-          } else {
-            // slot 0: the part of a tile that an earlier warp began; slot 1: of one that this warp begins
-            float4* s = slots + ((warp * 2 + (whole ? 1 : 0)) * NT) * 32 + lane;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) s[t * 32] = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
-          }
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
-          if (tile_end) { kb = 0; ++tile; whole = true; }
-        }
       }
+    }
+    __syncwarp();                                   // (every lane has read the scales: the place may be filled again)
+    fetch();
+    slot_out = slot_out == (kDepth - 1) * kBytes ? 0 : slot_out + kBytes;
+    x_at += 4 * x_pair;
+    if (++kb == kblocks) {
+      if (whole) {
+        store_tile<NT>(A, acc, tile0 + tile, lane);
+      } else {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          parts[(warp * NT + t) * 32 + lane] = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
+      kb = 0;
+      x_at = 0;
+      ++tile;
+      whole = true;
     }
   }
+  // A tile that is not finished: its first warp keeps its part and adds those of the warps after it, in their order.
+  const bool open = count > 0 && kb != 0;
+  if (open && !whole) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) parts[(warp * NT + t) * 32 + lane] = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
+  }
   __syncthreads();
-  // The warp that has a shared tile's first block adds the parts of the warps after it.
-  if (b1 > b0) {
-    const int64_t last = (b1 - 1) / A.kblocks, end = (last + 1) * A.kblocks;
-    if (b1 < end && last * A.kblocks >= b0) {
-      float sum[NT][4];
-      const float4* s = slots + ((warp * 2 + 1) * NT) * 32 + lane;
+  if (open && whole) {
+    const int64_t end = (tile + 1) * kblocks;
+    for (int o = warp + 1; o < kWarps; ++o) {
+      const int64_t o0 = blocks * o / kWarps, o1 = blocks * (o + 1) / kWarps;
+      if (o0 >= end) break;
+      if (o1 == o0) continue;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const float4 v = s[t * 32];
-        sum[t][0] = v.x; sum[t][1] = v.y; sum[t][2] = v.z; sum[t][3] = v.w;
+        const float4 v = parts[(o * NT + t) * 32 + lane];
+        acc[t][0] += v.x; acc[t][1] += v.y; acc[t][2] += v.z; acc[t][3] += v.w;
       }
-      for (int o = warp + 1; o < kWarps; ++o) {
-        const int64_t o0 = blocks * o / kWarps, o1 = blocks * (o + 1) / kWarps;
-        if (o0 >= end) break;
-        if (o1 == o0) continue;
-        const float4* q = slots + ((o * 2) * NT) * 32 + lane;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const float4 v = q[t * 32];
-          sum[t][0] += v.x; sum[t][1] += v.y; sum[t][2] += v.z; sum[t][3] += v.w;
-        }
-      }
-      store_tile<NT, GROUPS>(A, sum, tile0 + last, lane);
     }
+    store_tile<NT>(A, acc, tile0 + tile, lane);
   }
 }
 
@@ -252,21 +276,24 @@ __global__ void __launch_bounds__(256) w4_pack_kernel(W4PackArgs A) {
 }
 
 template <int NT, int GROUPS>
-cudaError_t run(const W4Args& a, cudaStream_t s, int sms) {
-  const int bytes = kWarps * 2 * NT * 32 * 16 + (int)a.kblocks * 4 * a.M * 4 * 16;
-  cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       kWarps * 2 * NT * 32 * 16 + kXBytes);
-  if (e != cudaSuccess) return e;
+cudaError_t run(const W4Args& a, cudaStream_t s, int sms, int device) {
+  static std::atomic<bool> ready[64];               // per device: the kernel may use this much shared memory
+  if (device < 0 || device >= 64 || !ready[device].load(std::memory_order_acquire)) {
+    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+    if (e != cudaSuccess) return e;
+    if (device >= 0 && device < 64) ready[device].store(true, std::memory_order_release);
+  }
+  const int bytes = ring_bytes(GROUPS) + part_bytes(NT) + (int)a.kblocks * kBlockK * 2 * a.M;
   const int grid = (int)(a.tiles < sms ? a.tiles : sms);
   w4_kernel<NT, GROUPS><<<grid, kWarps * 32, bytes, s>>>(a);
   return cudaGetLastError();
 }
 
 template <int NT>
-cudaError_t run_groups(const W4Args& a, int group, cudaStream_t s, int sms) {
-  if (group == 128) return run<NT, 1>(a, s, sms);
-  if (group == 64) return run<NT, 2>(a, s, sms);
-  return run<NT, 4>(a, s, sms);
+cudaError_t run_groups(const W4Args& a, int group, cudaStream_t s, int sms, int device) {
+  if (group == 128) return run<NT, 1>(a, s, sms, device);
+  if (group == 64) return run<NT, 2>(a, s, sms, device);
+  return run<NT, 4>(a, s, sms, device);
 }
 
 }  // namespace
@@ -283,19 +310,22 @@ cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms) {
   return cudaGetLastError();
 }
 
-// Tokens of one launch: as many as shared memory holds of x.
-int w4_tokens_per_launch(int64_t K) {
+// Tokens of one launch, of M that are left: as many as shared memory holds of x (one always fits).
+int w4_tokens_per_launch(int64_t K, int group, int64_t M) {
   const int64_t kblocks = (K + kBlockK - 1) / kBlockK;
-  const int64_t m = kXBytes / (kblocks * kBlockK * 2);
-  return (int)(m < kW4MaxTokens ? m : kW4MaxTokens);
+  const int groups = kBlockK / group;
+  int64_t m = M < kW4MaxTokens ? M : kW4MaxTokens;
+  while (m > 1 && m * kblocks * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, groups)) --m;
+  return (int)m;
 }
 
-cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms) {
+cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms, int device) {
   a.tiles = (a.N + kTileRows - 1) / kTileRows;
   a.kblocks = (a.K + kBlockK - 1) / kBlockK;
-  if (a.M <= 8) return run_groups<1>(a, group, s, sms);
-  if (a.M <= 16) return run_groups<2>(a, group, s, sms);
-  return run_groups<4>(a, group, s, sms);
+  static_assert(kW4MaxK * 2 <= x_bytes(1, 1) && kW4MaxK * 2 <= x_bytes(1, 2) && kW4MaxK * 2 <= x_bytes(1, 4), "one token fits");
+  if (a.M <= 8) return run_groups<1>(a, group, s, sms, device);
+  if (a.M <= 16) return run_groups<2>(a, group, s, sms, device);
+  return run_groups<4>(a, group, s, sms, device);
 }
 
 }  // namespace jp
