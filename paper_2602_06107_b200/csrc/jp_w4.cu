@@ -9,8 +9,7 @@
 //
 // Weights are laid out once (pack_kernel) in the order the MMA's A fragments want them: tiles of 16 rows, blocks of 128
 // columns, per block 8 steps of k = 16.  A lane's 8 weights of a step are one 32-bit word whose nibbles j and j + 4 are the
-// two halves of fragment register j, so (word >> 4j) & 0x000f000f | 0x43004300 is that register plus 128 (bf16 128 + q), and
-// one packed subtraction of 128 + z gives the exact value.  A block is 1024 bytes of words, then one 32-bit word per
+// two halves of fragment register j: four masks, one shift and four packed multiply-adds (scaled2) make the fragment.  A block is 1024 bytes of words, then one 32-bit word per
 // (row, group): the scale as fp32 with its low 4 bits replaced by z (scales come in bf16 or fp16: those bits are zero).
 // Blocks of a tile follow one another, tiles too: what a warp reads is one contiguous run of memory.
 //
@@ -44,12 +43,26 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// (w >> shift) & 0x000f000f | 0x43004300, minus 128 + z in both halves: two exact bf16 integers
-__device__ __forceinline__ uint32_t dequant2(uint32_t w, int shift, uint32_t z128) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(r) : "r"(w >> shift));
-  const __nv_bfloat162 d = __hsub2(*(const __nv_bfloat162*)&r, *(const __nv_bfloat162*)&z128);
-  return *(const uint32_t*)&d;
+// d = a b: the first step of a group
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+// Bits 0 .. 7 of a bf16 are the number bits 2^-133, over the subnormals and the first normal binade alike.  So a nibble that is
+// masked out in place, at bits 0 or 4 of each half, is q 2^-133 or q 2^-129, and one fused multiply-add by 2^127 with -z / 64 or
+// -z / 4 makes it (q - z) / 64 or / 4, exactly: no shift, no exponent to set.  (The scale takes the 64 or the 4 back.)
+constexpr uint32_t k2To127 = 0x7f007f00u, kMinus2To127 = 0xff00ff00u;
+__device__ __forceinline__ uint32_t scaled2(uint32_t bits, uint32_t minus_z) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(bits), "r"(k2To127), "r"(minus_z));
+  return d;
+}
+__device__ __forceinline__ uint32_t minus_scaled2(uint32_t bits) {      // -z / 64 (z at bits 0) or -z / 4 (at bits 4)
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(bits), "r"(kMinus2To127), "r"(0u));
+  return d;
 }
 
 __device__ __forceinline__ void copy16(void* smem, const void* global) {
@@ -151,6 +164,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
       *(uint4*)sw[1] = ((const uint4*)(blk + 1024))[row + 8];
     }
     float part[NT][4];
+    uint32_t z0 = 0, z1 = 0;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const uint4 v = ((const uint4*)blk)[half * 32 + lane];
@@ -163,24 +177,25 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int step = pair * 2 + h, grp = step * GROUPS / 8;
-          if (step % (8 / GROUPS) == 0) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) part[t][e] = 0.f;
+          const bool first = step % (8 / GROUPS) == 0;
+          if (first) {
+            z0 = minus_scaled2((sw[0][grp] & 15u) * 0x00010001u);
+            z1 = minus_scaled2((sw[1][grp] & 15u) * 0x00100010u);
           }
-          const uint32_t z0 = (sw[0][grp] & 15u) * 0x00010001u + 0x43004300u;
-          const uint32_t z1 = (sw[1][grp] & 15u) * 0x00010001u + 0x43004300u;
           const uint32_t w = p == 0 ? (h == 0 ? v.x : v.y) : (h == 0 ? v.z : v.w);
           uint32_t a[4];
-          a[0] = dequant2(w, 0, z0);
-          a[1] = dequant2(w, 4, z1);
-          a[2] = dequant2(w, 8, z0);
-          a[3] = dequant2(w, 12, z1);
+          const uint32_t w8 = w >> 8;
+          a[0] = scaled2(w & 0x000f000fu, z0);
+          a[1] = scaled2(w & 0x00f000f0u, z1);
+          a[2] = scaled2(w8 & 0x000f000fu, z0);
+          a[3] = scaled2(w8 & 0x00f000f0u, z1);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) mma_bf16(part[t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
+          for (int t = 0; t < NT; ++t) {
+            if (first) mma_bf16_first(part[t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
+            else mma_bf16(part[t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
+          }
           if ((step + 1) % (8 / GROUPS) == 0) {
-            const float s0 = __uint_as_float(sw[0][grp] & ~15u), s1 = __uint_as_float(sw[1][grp] & ~15u);
+            const float s0 = __uint_as_float(sw[0][grp] & ~15u) * 64.f, s1 = __uint_as_float(sw[1][grp] & ~15u) * 4.f;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
               acc[t][0] = fmaf(part[t][0], s0, acc[t][0]);
