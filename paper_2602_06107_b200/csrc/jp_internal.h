@@ -294,7 +294,7 @@ struct W4Args {
   int64_t tiles, kblocks;  // set by the launch
 };
 size_t w4_packed_bytes(int64_t N, int64_t K, int group);
-int w4_tokens_per_launch(int64_t K, int group, int64_t M);
+int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M);
 cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms);
 cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms, int device);
 

@@ -30,12 +30,13 @@ constexpr int kTileRows = 16;
 constexpr int kBlockK = 128;
 constexpr int kWarps = 16;
 constexpr int kSharedBytes = 232448;  // of one block
-// Blocks a warp has in flight; what the ring and the warps' parts of shared tiles leave is for x.
-__host__ __device__ constexpr int depth_of(int groups) { return groups == 4 ? 4 : 5; }
+// A warp takes `unit` blocks at a time (two where there are enough: less to do per block around the products, 36 -> 33 us at
+// 151,936 x 2048 and one token) and has `depth` units in flight: 3 of two, or 5 (4) of one, or 3 of one where x needs the room.
+// What the ring and the warps' parts of shared tiles leave is for x.
 __host__ __device__ constexpr int block_bytes(int groups) { return 1024 + kTileRows * 4 * groups; }
 __host__ __device__ constexpr int part_bytes(int nt) { return kWarps * nt * 32 * 16; }
-__host__ __device__ constexpr int ring_bytes(int groups) { return kWarps * depth_of(groups) * block_bytes(groups); }
-constexpr int x_bytes(int nt, int groups) { return kSharedBytes - ring_bytes(groups) - part_bytes(nt); }
+__host__ __device__ constexpr int ring_bytes(int unit, int depth, int groups) { return kWarps * depth * unit * block_bytes(groups); }
+constexpr int x_bytes(int nt, int unit, int depth, int groups) { return kSharedBytes - ring_bytes(unit, depth, groups) - part_bytes(nt); }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -85,52 +86,60 @@ __device__ __forceinline__ void store_tile(const W4Args& A, const float (&acc)[N
     }
 }
 
-template <int NT, int GROUPS>
+template <int NT, int GROUPS, int UNIT, int DEPTH>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
-  constexpr int kBytes = block_bytes(GROUPS), kDepth = depth_of(GROUPS);
+  constexpr int kBlock = block_bytes(GROUPS), kBytes = UNIT * kBlock, kDepth = DEPTH;
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   char* ring = smem + warp * kDepth * kBytes;
-  float4* parts = (float4*)(smem + ring_bytes(GROUPS));                 // [warp][NT][lane]: of a tile that an earlier warp begins
-  uint4* xs = (uint4*)(smem + ring_bytes(GROUPS) + part_bytes(NT));     // [block][step pair][token][lane % 4]
+  float4* parts = (float4*)(smem + ring_bytes(UNIT, DEPTH, GROUPS));                 // [warp][NT][lane]: of a tile that an earlier warp begins
+  uint4* xs = (uint4*)(smem + ring_bytes(UNIT, DEPTH, GROUPS) + part_bytes(NT));     // [block][step pair][token][lane % 4]
   const int kblocks = (int)A.kblocks;
   const int64_t tile0 = A.tiles * blockIdx.x / gridDim.x, tile1 = A.tiles * (blockIdx.x + 1) / gridDim.x;
-  const int64_t blocks = (tile1 - tile0) * kblocks;
+  const int tile_units = kblocks / UNIT;
+  const int64_t blocks = (tile1 - tile0) * tile_units;      // (units)
   const int64_t b0 = blocks * warp / kWarps, b1 = blocks * (warp + 1) / kWarps;
   const int count = (int)(b1 - b0);
-  const char* src = (const char*)A.packed + (tile0 * kblocks + b0) * kBytes + lane * 16;
+  const char* src = (const char*)A.packed + (tile0 * tile_units + b0) * kBytes + lane * 16;
+  asm volatile("griddepcontrol.wait;" ::: "memory");                // launched as a programmatic dependent of whatever is before it
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int issued = 0, slot_in = 0, slot_out = 0;
   auto fetch = [&]() {
     if (issued < count) {
-      copy16(ring + slot_in + lane * 16, src);
-      copy16(ring + slot_in + 512 + lane * 16, src + 512);
-      if (lane < 4 * GROUPS) copy16(ring + slot_in + 1024 + lane * 16, src + 1024);
+#pragma unroll
+      for (int c = 0; c < kBytes; c += 512)
+        if (c + 512 <= kBytes || lane * 16 < kBytes - c) copy16(ring + slot_in + c + lane * 16, src + c);
       src += kBytes;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     ++issued;
     slot_in = slot_in == (kDepth - 1) * kBytes ? 0 : slot_in + kBytes;
   };
-#pragma unroll
-  for (int j = 0; j < kDepth; ++j) fetch();
-
+  fetch();
+  fetch();
   // x in B-fragment order: word w of unit (block, step pair, token, t) is columns 128 block + 32 pair + 16 (w / 2)
-  // + 8 (w % 2) + 2 t and the next.  A warp takes (token, block) by (token, block), a lane two pairs of columns of each.
-  {
-    const int tasks = A.M * kblocks;
-    for (int u = warp; u < tasks; u += kWarps) {
-      const int m = u % A.M, kb = u / A.M;
-      const uint16_t* xr = (const uint16_t*)A.x + (int64_t)m * A.ld_x;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int in = lane * 2 + h * 64;                   // column within the block
-        const int64_t k = (int64_t)kb * kBlockK + in;
-        const uint32_t lo = k < A.K ? xr[k] : 0, hi = k + 1 < A.K ? xr[k + 1] : 0;
-        const int pair = in >> 5, w = (in >> 3) & 3, t = (in >> 1) & 3;
-        ((uint32_t*)(xs + ((kb * 4 + pair) * A.M + m) * 4 + t))[w] = lo | hi << 16;
-      }
+  // + 8 (w % 2) + 2 t and the next.  A warp takes half a block's columns of all tokens, a lane a pair of columns.  Asynchronous copies
+  // and little code: in the smallest calls fetching instructions is part of the time (the loop unrolled by eight cost 4 us).
+  const bool pairs = (((uintptr_t)A.x | (uintptr_t)(A.ld_x * 2)) & 3) == 0;
+  for (int half = warp; half < 2 * kblocks; half += kWarps) {
+    const int in = (half & 1) * 64 + lane * 2, k = (half >> 1) * kBlockK + in;       // column within the block, in the row
+    const int valid = k + 1 < A.K ? 4 : k < A.K ? 2 : 0;    // bytes; the rest is filled with zeros
+    const uint16_t* xr = (const uint16_t*)A.x + (valid ? k : 0);
+    uint32_t* to = (uint32_t*)(xs + ((half >> 1) * 4 + (in >> 5)) * A.M * 4 + ((in >> 1) & 3)) + ((in >> 3) & 3);
+    if (pairs) {
+#pragma unroll 1
+      for (int m = 0; m < A.M; ++m, xr += A.ld_x, to += 16)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(xr), "r"(valid) : "memory");
+    } else {                                                // rows that start on odd elements
+#pragma unroll 4
+      for (int m = 0; m < A.M; ++m)
+        to[m * 16] = (valid ? __ldg(xr + m * A.ld_x) : 0u) | (valid == 4 ? (uint32_t)__ldg(xr + m * A.ld_x + 1) << 16 : 0u);
     }
   }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll
+  for (int j = 2; j < kDepth; ++j) fetch();
+  asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 2) : "memory");
   __syncthreads();
 
   float acc[NT][4];
@@ -138,8 +147,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
-  int64_t tile = b0 / kblocks;                      // within the CTA's run
-  int kb = (int)(b0 - tile * kblocks);
+  int64_t tile = b0 / tile_units;                   // within the CTA's run
+  int kb = (int)(b0 - tile * tile_units);
   bool whole = kb == 0;                             // this warp has the tile from its first block on
   const int row = lane >> 2;
   // (a column of B makes the same column of the result alone: places without a token take the last token's, and are not stored)
@@ -147,11 +156,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) xt[t] = xs + min(t * 8 + row, A.M - 1) * 4 + (lane & 3);
   const int x_pair = A.M * 4;
-  int x_at = kb * 4 * x_pair;
+  int x_at = kb * UNIT * 4 * x_pair;
   for (int b = 0; b < count; ++b) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
     __syncwarp();
-    const char* blk = ring + slot_out;
+#pragma unroll
+    for (int u = 0; u < UNIT; ++u) {
+    const char* blk = ring + slot_out + u * kBlock;
     uint32_t sw[2][GROUPS];
     if constexpr (GROUPS == 1) {
       sw[0][0] = ((const uint32_t*)(blk + 1024))[row];
@@ -173,7 +184,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
         const int pair = half * 2 + p;
         uint4 f[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) f[t] = xt[t][x_at + pair * x_pair];
+        for (int t = 0; t < NT; ++t) f[t] = xt[t][x_at + (u * 4 + pair) * x_pair];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int step = pair * 2 + h, grp = step * GROUPS / 8;
@@ -207,11 +218,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
         }
       }
     }
+    }
     __syncwarp();                                   // (every lane has read the scales: the place may be filled again)
     fetch();
     slot_out = slot_out == (kDepth - 1) * kBytes ? 0 : slot_out + kBytes;
-    x_at += 4 * x_pair;
-    if (++kb == kblocks) {
+    x_at += UNIT * 4 * x_pair;
+    if (++kb == tile_units) {
       if (whole) {
         store_tile<NT>(A, acc, tile0 + tile, lane);
       } else {
@@ -237,7 +249,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   }
   __syncthreads();
   if (open && whole) {
-    const int64_t end = (tile + 1) * kblocks;
+    const int64_t end = (tile + 1) * tile_units;
     for (int o = warp + 1; o < kWarps; ++o) {
       const int64_t o0 = blocks * o / kWarps, o1 = blocks * (o + 1) / kWarps;
       if (o0 >= end) break;
@@ -290,54 +302,80 @@ __global__ void __launch_bounds__(256) w4_pack_kernel(W4PackArgs A) {
   }
 }
 
-template <int NT, int GROUPS>
+template <int NT, int GROUPS, int UNIT, int DEPTH>
 cudaError_t run(const W4Args& a, cudaStream_t s, int sms, int device) {
   static std::atomic<bool> ready[64];               // per device: the kernel may use this much shared memory
   if (device < 0 || device >= 64 || !ready[device].load(std::memory_order_acquire)) {
-    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS, UNIT, DEPTH>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
     if (e != cudaSuccess) return e;
     if (device >= 0 && device < 64) ready[device].store(true, std::memory_order_release);
   }
-  const int bytes = ring_bytes(GROUPS) + part_bytes(NT) + (int)a.kblocks * kBlockK * 2 * a.M;
+  const int bytes = ring_bytes(UNIT, DEPTH, GROUPS) + part_bytes(NT) + (int)a.kblocks * kBlockK * 2 * a.M;
   const int grid = (int)(a.tiles < sms ? a.tiles : sms);
-  w4_kernel<NT, GROUPS><<<grid, kWarps * 32, bytes, s>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;     // set up while the kernel before it ends: 0.5 us a call
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, w4_kernel<NT, GROUPS, UNIT, DEPTH>, a);
+}
+
+template <int NT, int GROUPS>
+cudaError_t run_unit(const W4Args& a, cudaStream_t s, int sms, int device) {
+  // units of two where a warp gets several of them (with fewer, half of the warps would be idle)
+  const int64_t grid = a.tiles < sms ? a.tiles : sms, x = a.kblocks * kBlockK * 2 * a.M;
+  constexpr int kFull = GROUPS == 4 ? 4 : 5;
+  if (a.kblocks % 2 == 0 && a.tiles * a.kblocks >= 4 * kWarps * grid && x <= x_bytes(NT, 2, 3, GROUPS))
+    return run<NT, GROUPS, 2, 3>(a, s, sms, device);
+  if (x <= x_bytes(NT, 1, kFull, GROUPS)) return run<NT, GROUPS, 1, kFull>(a, s, sms, device);
+  return run<NT, GROUPS, 1, 3>(a, s, sms, device);
 }
 
 template <int NT>
 cudaError_t run_groups(const W4Args& a, int group, cudaStream_t s, int sms, int device) {
-  if (group == 128) return run<NT, 1>(a, s, sms, device);
-  if (group == 64) return run<NT, 2>(a, s, sms, device);
-  return run<NT, 4>(a, s, sms, device);
+  if (group == 128) return run_unit<NT, 1>(a, s, sms, device);
+  if (group == 64) return run_unit<NT, 2>(a, s, sms, device);
+  return run_unit<NT, 4>(a, s, sms, device);
+}
+
+// Blocks of 128 columns a row has in the layout: an even number (the last one zeros) for weights large enough to be taken by two.
+int64_t blocks_of(int64_t N, int64_t K) {
+  const int64_t n = (K + kBlockK - 1) / kBlockK, tiles = (N + kTileRows - 1) / kTileRows;
+  return n >= 8 && tiles * n >= 8192 ? (n + 1) / 2 * 2 : n;
 }
 
 }  // namespace
 
 size_t w4_packed_bytes(int64_t N, int64_t K, int group) {
-  const int64_t tiles = (N + kTileRows - 1) / kTileRows, kblocks = (K + kBlockK - 1) / kBlockK;
-  return (size_t)(tiles * kblocks) * (size_t)(1024 + kTileRows * 4 * (kBlockK / group));
+  const int64_t tiles = (N + kTileRows - 1) / kTileRows;
+  return (size_t)(tiles * blocks_of(N, K)) * (size_t)block_bytes(kBlockK / group);
 }
 
 cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms) {
   a.tiles = (a.N + kTileRows - 1) / kTileRows;
-  a.kblocks = (a.K + kBlockK - 1) / kBlockK;
+  a.kblocks = blocks_of(a.N, a.K);
   w4_pack_kernel<<<sms * 8, 256, 0, s>>>(a);
   return cudaGetLastError();
 }
 
-// Tokens of one launch, of M that are left: as many as shared memory holds of x (one always fits).
-int w4_tokens_per_launch(int64_t K, int group, int64_t M) {
-  const int64_t kblocks = (K + kBlockK - 1) / kBlockK;
+// Tokens of one launch, of M that are left: as many as shared memory holds of x (one always fits), the launches even.
+int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M) {
   const int groups = kBlockK / group;
   int64_t m = M < kW4MaxTokens ? M : kW4MaxTokens;
-  while (m > 1 && m * kblocks * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, groups)) --m;
-  return (int)m;
+  while (m > 1 && m * blocks_of(N, K) * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, 1, 3, groups)) --m;
+  const int64_t launches = (M + m - 1) / m;
+  return (int)((M + launches - 1) / launches);
 }
 
 cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms, int device) {
   a.tiles = (a.N + kTileRows - 1) / kTileRows;
-  a.kblocks = (a.K + kBlockK - 1) / kBlockK;
-  static_assert(kW4MaxK * 2 <= x_bytes(1, 1) && kW4MaxK * 2 <= x_bytes(1, 2) && kW4MaxK * 2 <= x_bytes(1, 4), "one token fits");
+  a.kblocks = blocks_of(a.N, a.K);
+  static_assert(kW4MaxK * 2 <= x_bytes(1, 1, 3, 4), "one token fits");
   if (a.M <= 8) return run_groups<1>(a, group, s, sms, device);
   if (a.M <= 16) return run_groups<2>(a, group, s, sms, device);
   return run_groups<4>(a, group, s, sms, device);
