@@ -9,8 +9,9 @@
 // Both passes are bound by HBM: forward reads x and writes y, backward reads x and dy and writes dx.  A row
 // stays in the registers of one group of threads between its reduction and its output, so nothing is read
 // twice; the squares are taken of x - mu (a second reduction over registers) because E x^2 - mu^2 cancels.
-// A group walks rows with the fixed stride of the grid and loads the next row before it reduces the present
-// one.  Each thread owns fixed columns, so dw and db add up in its registers over all rows of its group; the
+// Groups walk rows with the fixed stride of the grid, weight and bias in registers.  Where rows start on 16 bytes the next rows come
+// through asynchronous copies, each thread into places of its own (kStages rows ahead, no barriers); else the next row is in registers.
+// Each thread owns fixed columns, so dw and db add up in its registers over all rows of its group; the
 // groups' sums go to the workspace and a second kernel adds them in a fixed order: no atomics, the same bits
 // every time.
 #include "jp_common.cuh"
@@ -89,36 +90,144 @@ __device__ __forceinline__ float2 group_sum(float a, float b, float2 (*sh)[kMaxW
   slot ^= 1;
   if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float2(a, b);
   __syncthreads();
-  const int lane = threadIdx.x & 31;
-  const float2 v = lane < warps ? s[lane] : make_float2(0.f, 0.f);
-  return make_float2(warp_sum(v.x), warp_sum(v.y));
+  float2 t = s[0];
+  for (int w = 1; w < warps; ++w) {
+    t.x += s[w].x;
+    t.y += s[w].y;
+  }
+  return t;
 }
 
-template <int DT, int W, int NV>
-__global__ void __launch_bounds__((W == 1 ? NV > 8 : NV > 1) ? 512 : 256) norm_fwd_kernel(NormArgs A) {
-  using Ac = Access<DT, W>;
-  constexpr int ES = Vec<DT>::ESIZE;
-  __shared__ float2 sh[2][kMaxWarps];
-  int slot = 0;
-  const int n = blockDim.x;
-  const float inv_h = 1.f / (float)A.H;
-  typename Ac::raw next[NV];
-  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  auto fetch = [&](int64_t r) {
-    const char* x = (const char*)A.x + r * A.ld_x * ES;
+// Columns of this thread: access i covers columns (threadIdx.x + i * blockDim.x) * W and the next W - 1.
+template <int W> __device__ __forceinline__ int64_t column(int i) { return (int64_t)(threadIdx.x + i * (int)blockDim.x) * W; }
+
+// Weight or bias at the thread's columns, loaded once: bf16 pairs as they are, the rest as fp32.
+template <int W, int NV, bool BF16>
+struct Params {
+  static constexpr int N = W == 1 ? NV : BF16 ? NV * W / 2 : NV * W;
+  uint32_t r[N];
+  __device__ __forceinline__ void load(const void* p, int64_t H) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(threadIdx.x + i * n) * W;
-      next[i] = c < A.H ? Ac::load(x + c * ES) : Ac::zero();
+      const int64_t c = column<W>(i);
+      if constexpr (W == 1) {
+        r[i] = p && c < H ? (BF16 ? (uint32_t)((const uint16_t*)p)[c] << 16 : ((const uint32_t*)p)[c]) : 0u;
+      } else {
+        constexpr int words = N / NV;
+#pragma unroll
+        for (int q = 0; q < words; q += 2) {
+          const uint2 v = p && c < H ? *(const uint2*)((const char*)p + c * (BF16 ? 2 : 4) + q * 4) : make_uint2(0u, 0u);
+          r[i * words + q] = v.x;
+          r[i * words + q + 1] = v.y;
+        }
+      }
     }
-  };
-  if (row < A.T) fetch(row);
+  }
+  __device__ __forceinline__ float get(int i, int e) const {
+    if constexpr (W == 1) return __uint_as_float(r[i]);
+    else if constexpr (BF16) {
+      const uint32_t w = r[(i * W + e) / 2];
+      return __uint_as_float((e & 1) ? (w & 0xffff0000u) : (w << 16));
+    } else return __uint_as_float(r[i * W + e]);
+  }
+};
+
+// The group's rows of NT matrices one after the other: row `first`, then every `step`-th.
+constexpr int kStages = 3;
+template <int DT, int W, int NV, int NT>
+struct Rows {
+  using Ac = Access<DT, W>;
+  static constexpr int ES = Vec<DT>::ESIZE;
+  static constexpr bool kAsync = W > 1;
+  const char* base[NT];
+  int64_t pitch[NT];
+  int64_t next_row, step, T, H;
+  uint4* places;                // [kStages][NT][NV][threads of the block], this thread's column
+  int threads, in, out;
+  typename Ac::raw ahead[kAsync ? 1 : NT][kAsync ? 1 : NV];
+  __device__ __forceinline__ void fetch() {
+    if (next_row < T) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const char* r = base[t] + next_row * pitch[t];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int64_t c = column<W>(i);
+          if (c < H) {
+            if constexpr (kAsync)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(
+                               places + ((in * NT + t) * NV + i) * threads)), "l"(r + c * ES) : "memory");
+            else ahead[t][i] = Ac::load(r + c * ES);
+          }
+        }
+      }
+    }
+    next_row += step;
+    if constexpr (kAsync) {
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      in = in == kStages - 1 ? 0 : in + 1;
+    }
+  }
+  __device__ __forceinline__ void start(int64_t first) {
+    next_row = first;
+    in = out = 0;
+    if constexpr (kAsync) {
+#pragma unroll
+      for (int s = 0; s < kStages; ++s) fetch();
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) ahead[t][i] = Ac::zero();
+      fetch();
+    }
+  }
+  // the oldest row; columns past the end read 0
+  __device__ __forceinline__ void take(typename Ac::raw (&v)[NT][NV]) {
+    if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if constexpr (kAsync) v[t][i] = column<W>(i) < H ? places[((out * NT + t) * NV + i) * threads] : Ac::zero();
+        else v[t][i] = ahead[t][i];
+      }
+    if constexpr (kAsync) out = out == kStages - 1 ? 0 : out + 1;
+  }
+};
+
+// Threads and blocks an SM holds of the kernels below
+constexpr int group_threads(int w, int nv) { return (w == 1 ? nv > 8 : nv > 1) ? 512 : 256; }
+
+template <int DT, int W, int NV, bool PB>
+__global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs A) {
+  using Ac = Access<DT, W>;
+  constexpr int ES = Vec<DT>::ESIZE;
+  extern __shared__ uint4 places[];
+  __shared__ float2 sh[2][kMaxWarps];
+  asm volatile("griddepcontrol.wait;" ::: "memory");        // launched as a programmatic dependent of whatever is before it
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  int slot = 0;
+  const float inv_h = 1.f / (float)A.H;
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  Rows<DT, W, NV, 1> in;
+  in.base[0] = (const char*)A.x;
+  in.pitch[0] = A.ld_x * ES;
+  in.step = step; in.T = A.T; in.H = A.H;
+  in.threads = blockDim.x * blockDim.y;
+  in.places = places + threadIdx.y * blockDim.x + threadIdx.x;
+  in.start(row);
+  Params<W, NV, PB> w, b;
+  w.load(A.weight, A.H);
+  b.load(A.bias, A.H);
   for (; row < A.T; row += step) {
     float v[NV][W];
+    typename Ac::raw raw[1][NV];
+    in.take(raw);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) Ac::unpack(next[i], v[i]);
-    if (row + step < A.T) fetch(row + step);
+    for (int i = 0; i < NV; ++i) Ac::unpack(raw[0][i], v[i]);
+    in.fetch();
     float mean = 0.f;
     if (!A.rms) {
       float s = 0.f;
@@ -131,8 +240,7 @@ __global__ void __launch_bounds__((W == 1 ? NV > 8 : NV > 1) ? 512 : 256) norm_f
     float s2 = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(threadIdx.x + i * n) * W;
-      if (c < A.H) {
+      if (column<W>(i) < A.H) {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
           v[i][e] -= mean;
@@ -148,14 +256,11 @@ __global__ void __launch_bounds__((W == 1 ? NV > 8 : NV > 1) ? 512 : 256) norm_f
     char* y = (char*)A.y + row * A.ld_y * ES;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(threadIdx.x + i * n) * W;
+      const int64_t c = column<W>(i);
       if (c < A.H) {
         float o[W];
 #pragma unroll
-        for (int e = 0; e < W; ++e) {
-          o[e] = v[i][e] * rstd * load_elem(A.weight, c + e, A.param_bf16);
-          if (A.bias) o[e] += load_elem(A.bias, c + e, A.param_bf16);
-        }
+        for (int e = 0; e < W; ++e) o[e] = fmaf(v[i][e] * rstd, w.get(i, e), b.get(i, e));
         Ac::store(y + c * ES, o);
       }
     }
@@ -197,55 +302,63 @@ __global__ void __launch_bounds__(1024) norm_fwd_wide_kernel(NormArgs A) {
   }
 }
 
-template <int DT, int W, int NV>
-__global__ void __launch_bounds__((W == 1 ? NV > 8 : NV > 1) ? 512 : 256) norm_bwd_kernel(NormArgs A) {
+template <int DT, int W, int NV, bool PB, bool BIAS>
+__global__ void __launch_bounds__(group_threads(W, NV)) norm_bwd_kernel(NormArgs A) {
   using Ac = Access<DT, W>;
   constexpr int ES = Vec<DT>::ESIZE;
+  extern __shared__ uint4 places[];
   __shared__ float2 sh[2][kMaxWarps];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   int slot = 0;
-  const int n = blockDim.x;
   const float inv_h = 1.f / (float)A.H;
-  float dw[NV][W], db[NV][W];
+  float dw[NV][W], db[BIAS ? NV : 1][W];
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int e = 0; e < W; ++e) dw[i][e] = db[i][e] = 0.f;
-  typename Ac::raw nx[NV], ny[NV];
+    for (int e = 0; e < W; ++e) {
+      dw[i][e] = 0.f;
+      if (BIAS) db[i][e] = 0.f;
+    }
   const int64_t group = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  auto fetch = [&](int64_t r) {
-    const char* x = (const char*)A.x + r * A.ld_x * ES;
-    const char* dy = (const char*)A.dy + r * A.ld_dy * ES;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(threadIdx.x + i * n) * W;
-      nx[i] = c < A.H ? Ac::load(x + c * ES) : Ac::zero();
-      ny[i] = c < A.H ? Ac::load(dy + c * ES) : Ac::zero();
-    }
-  };
-  if (group < A.T) fetch(group);
+  Rows<DT, W, NV, 2> in;
+  in.base[0] = (const char*)A.x;
+  in.base[1] = (const char*)A.dy;
+  in.pitch[0] = A.ld_x * ES;
+  in.pitch[1] = A.ld_dy * ES;
+  in.step = step; in.T = A.T; in.H = A.H;
+  in.threads = blockDim.x * blockDim.y;
+  in.places = places + threadIdx.y * blockDim.x + threadIdx.x;
+  in.start(group);
+  Params<W, NV, PB> w;
+  w.load(A.weight, A.H);
+  float mean = 0.f, rstd = 0.f;
+  if (group < A.T) {
+    mean = A.rms ? 0.f : A.mean[group];
+    rstd = A.rstd[group];
+  }
   for (int64_t row = group; row < A.T; row += step) {
-    typename Ac::raw cx[NV], cy[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) { cx[i] = nx[i]; cy[i] = ny[i]; }
-    if (row + step < A.T) fetch(row + step);
-    const float mean = A.rms ? 0.f : A.mean[row], rstd = A.rstd[row];
+    typename Ac::raw raw[2][NV];
+    in.take(raw);
+    in.fetch();
+    float mean_next = 0.f, rstd_next = 0.f;
+    if (row + step < A.T) {
+      mean_next = A.rms ? 0.f : A.mean[row + step];
+      rstd_next = A.rstd[row + step];
+    }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(threadIdx.x + i * n) * W;
-      if (c < A.H) {
-        float x[W], dy[W];
-        Ac::unpack(cx[i], x);
-        Ac::unpack(cy[i], dy);
+      float x[W], dy[W];
+      Ac::unpack(raw[0][i], x);
+      Ac::unpack(raw[1][i], dy);                            // (0 past the end, and so is everything below)
 #pragma unroll
-        for (int e = 0; e < W; ++e) {
-          const float xh = (x[e] - mean) * rstd, g = dy[e] * load_elem(A.weight, c + e, A.param_bf16);
-          s1 += g;
-          s2 = fmaf(g, xh, s2);
-          dw[i][e] = fmaf(dy[e], xh, dw[i][e]);
-          db[i][e] += dy[e];
-        }
+      for (int e = 0; e < W; ++e) {
+        const float xh = (x[e] - mean) * rstd, g = dy[e] * w.get(i, e);
+        s1 += g;
+        s2 = fmaf(g, xh, s2);
+        dw[i][e] = fmaf(dy[e], xh, dw[i][e]);
+        if (BIAS) db[i][e] += dy[e];
       }
     }
     const float2 s = group_sum(s1, s2, sh, slot);
@@ -253,29 +366,32 @@ __global__ void __launch_bounds__((W == 1 ? NV > 8 : NV > 1) ? 512 : 256) norm_b
     char* dx = (char*)A.dx + row * A.ld_dx * ES;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(threadIdx.x + i * n) * W;
+      const int64_t c = column<W>(i);
       if (c < A.H) {
         float x[W], dy[W], o[W];
-        Ac::unpack(cx[i], x);
-        Ac::unpack(cy[i], dy);
+        Ac::unpack(raw[0][i], x);
+        Ac::unpack(raw[1][i], dy);
 #pragma unroll
         for (int e = 0; e < W; ++e) {
-          const float xh = (x[e] - mean) * rstd, g = dy[e] * load_elem(A.weight, c + e, A.param_bf16);
+          const float xh = (x[e] - mean) * rstd, g = dy[e] * w.get(i, e);
           o[e] = (g - m1 - xh * m2) * rstd;
         }
         Ac::store(dx + c * ES, o);
       }
     }
+    mean = mean_next;
+    rstd = rstd_next;
   }
-  float* pw = A.partial + group * 2 * A.H;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the kernel that adds the lines may set up
+  float* pw = A.partial + group * (BIAS ? 2 : 1) * A.H;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int64_t c = (int64_t)(threadIdx.x + i * n) * W;
+    const int64_t c = column<W>(i);
     if (c < A.H) {
 #pragma unroll
       for (int e = 0; e < W; ++e) {
         pw[c + e] = dw[i][e];
-        if (A.dbias) pw[A.H + c + e] = db[i][e];
+        if (BIAS) pw[A.H + c + e] = db[i][e];
       }
     }
   }
@@ -289,8 +405,9 @@ __global__ void __launch_bounds__(1024) norm_bwd_wide_kernel(NormArgs A) {
   __shared__ float2 sh[2][kMaxWarps];
   int slot = 0;
   const float inv_h = 1.f / (float)A.H;
-  float* pw = A.partial + (int64_t)blockIdx.x * 2 * A.H;
-  for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x) pw[c] = pw[A.H + c] = 0.f;
+  const int per_group = A.dbias ? 2 : 1;
+  float* pw = A.partial + (int64_t)blockIdx.x * per_group * A.H;
+  for (int64_t c = threadIdx.x; c < per_group * A.H; c += blockDim.x) pw[c] = 0.f;
   for (int64_t row = blockIdx.x; row < A.T; row += gridDim.x) {
     const char* x = (const char*)A.x + row * A.ld_x * ES;
     const char* dy = (const char*)A.dy + row * A.ld_dy * ES;
@@ -303,7 +420,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_wide_kernel(NormArgs A) {
       s1 += g;
       s2 = fmaf(g, xh, s2);
       pw[c] = fmaf(d, xh, pw[c]);
-      pw[A.H + c] += d;
+      if (A.dbias) pw[A.H + c] += d;
     }
     const float2 s = group_sum(s1, s2, sh, slot);
     const float m1 = A.rms ? 0.f : s.x * inv_h, m2 = s.y * inv_h;
@@ -316,23 +433,25 @@ __global__ void __launch_bounds__(1024) norm_bwd_wide_kernel(NormArgs A) {
   }
 }
 
-// dw[c] = sum over the groups' lines, in a fixed order: 8 threads a column, each every 8th line, then their sums.
-__global__ void __launch_bounds__(256) norm_sum_kernel(const float* partial, int64_t groups, int64_t H, float* dw,
-                                                       float* db) {
-  __shared__ float sh[8][33];
-  const bool second = blockIdx.y == 1;
-  float* out = second ? db : dw;
+// dw[c] = sum over the groups' lines, in a fixed order: 32 threads a column, each every 32nd line, then their sums.
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, int64_t groups, int64_t H, int per_group,
+                                                        float* dw, float* db) {
+  __shared__ float sh[32][33];
+  const int which = blockIdx.y;
+  float* out = which ? db : dw;
   const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   float s = 0.f;
-  if (c < H)
-    for (int64_t g = threadIdx.y; g < groups; g += 8) s += partial[(g * 2 + second) * H + c];
+  if (c < H) {
+    const float* p = partial + ((int64_t)threadIdx.y * per_group + which) * H + c;
+#pragma unroll 8
+    for (int64_t g = threadIdx.y; g < groups; g += 32, p += 32 * per_group * H) s += *p;
+  }
   sh[threadIdx.y][threadIdx.x] = s;
   __syncthreads();
-  if (threadIdx.y == 0 && c < H) {
-#pragma unroll
-    for (int i = 1; i < 8; ++i) s += sh[i][threadIdx.x];
-    out[c] = s;
-  }
+  const float v = warp_sum(sh[threadIdx.x][threadIdx.y]);   // warp y has column y of the block
+  const int64_t o = (int64_t)blockIdx.x * 32 + threadIdx.y;
+  if (threadIdx.x == 0 && o < H) out[o] = v;
 }
 
 struct Plan {
@@ -344,18 +463,20 @@ struct Plan {
 
 bool vector_rows(const NormArgs& a, bool backward) {
   const int64_t es = a.dtype == JP_BF16 ? 2 : 4;
-  auto ok = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * es % 16 == 0; };
-  if (a.H * es % 16) return false;
+  auto on16 = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
+  auto ok = [&](const void* p, int64_t ld) { return on16(p) && ld * es % 16 == 0; };
+  if (a.H * es % 16 || !on16(a.weight) || !on16(a.bias)) return false;
   return backward ? ok(a.x, a.ld_x) && ok(a.dy, a.ld_dy) && ok(a.dx, a.ld_dx) : ok(a.x, a.ld_x) && ok(a.y, a.ld_y);
 }
 
 // Threads and registers of a row.  16-byte accesses where rows start on 16 bytes, else single elements; 1, 2 or 4 vectors
-// (8 or 16 elements) a thread so that rows up to 16384 bf16 (8192 fp32, or 8192 unaligned) stay in registers.
-Plan plan_for(int64_t H, int dtype, bool vec) {
+// (8 or 16 elements) a thread so that rows up to 16384 bf16 (8192 fp32, or 8192 unaligned) stay in registers; the sums of a backward
+// pass take as much again, so 8192 there.
+Plan plan_for(int64_t H, int dtype, bool vec, bool backward) {
   Plan p{};
   p.w = vec ? (dtype == JP_BF16 ? 8 : 4) : 1;
   const int64_t n = (H + p.w - 1) / p.w;
-  if (vec) p.nv = n <= 256 ? 1 : n <= 1024 ? 2 : n <= 2048 ? 4 : 0;
+  if (vec) p.nv = n <= 256 ? 1 : n <= 1024 ? 2 : n <= (backward ? 8192 / p.w : 2048) ? 4 : 0;
   else p.nv = n <= 2048 ? 8 : n <= 8192 ? 16 : 0;
   if (p.nv == 0) { p.threads = 1024; p.rows = 1; p.w = 1; return p; }
   const int64_t per = (n + p.nv - 1) / p.nv;
@@ -372,45 +493,64 @@ int grid_for(int64_t T, const Plan& p, int sms) {
   return (int)(need < cap ? need : cap);
 }
 
-template <int DT>
-void fwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
-  constexpr int VW = Vec<DT>::N;
-  const dim3 b(p.threads, p.rows);
-  if (p.nv == 0) norm_fwd_wide_kernel<DT><<<grid, b, 0, s>>>(a);
-  else if (p.w == 1 && p.nv == 8) norm_fwd_kernel<DT, 1, 8><<<grid, b, 0, s>>>(a);
-  else if (p.w == 1) norm_fwd_kernel<DT, 1, 16><<<grid, b, 0, s>>>(a);
-  else if (p.nv == 1) norm_fwd_kernel<DT, VW, 1><<<grid, b, 0, s>>>(a);
-  else if (p.nv == 2) norm_fwd_kernel<DT, VW, 2><<<grid, b, 0, s>>>(a);
-  else norm_fwd_kernel<DT, VW, 4><<<grid, b, 0, s>>>(a);
+template <class K>
+cudaError_t launch(K* kernel, const NormArgs& a, dim3 grid, dim3 block, int smem, cudaStream_t s) {
+  if (smem > 47 * 1024) {                                   // (with the static part beyond what a kernel has without asking)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <int DT>
-void bwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
+template <int DT, bool PB>
+cudaError_t fwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
   constexpr int VW = Vec<DT>::N;
   const dim3 b(p.threads, p.rows);
-  if (p.nv == 0) norm_bwd_wide_kernel<DT><<<grid, b, 0, s>>>(a);
-  else if (p.w == 1 && p.nv == 8) norm_bwd_kernel<DT, 1, 8><<<grid, b, 0, s>>>(a);
-  else if (p.w == 1) norm_bwd_kernel<DT, 1, 16><<<grid, b, 0, s>>>(a);
-  else if (p.nv == 1) norm_bwd_kernel<DT, VW, 1><<<grid, b, 0, s>>>(a);
-  else if (p.nv == 2) norm_bwd_kernel<DT, VW, 2><<<grid, b, 0, s>>>(a);
-  else norm_bwd_kernel<DT, VW, 4><<<grid, b, 0, s>>>(a);
+  const int smem = p.w > 1 ? kStages * p.nv * p.threads * p.rows * 16 : 0;
+  if (p.nv == 0) { norm_fwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
+  if (p.w == 1) return p.nv == 8 ? launch(norm_fwd_kernel<DT, 1, 8, PB>, a, grid, b, smem, s) : launch(norm_fwd_kernel<DT, 1, 16, PB>, a, grid, b, smem, s);
+  if (p.nv == 1) return launch(norm_fwd_kernel<DT, VW, 1, PB>, a, grid, b, smem, s);
+  if (p.nv == 2) return launch(norm_fwd_kernel<DT, VW, 2, PB>, a, grid, b, smem, s);
+  return launch(norm_fwd_kernel<DT, VW, 4, PB>, a, grid, b, smem, s);
+}
+
+template <int DT, bool PB, bool BIAS>
+cudaError_t bwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
+  constexpr int VW = Vec<DT>::N;
+  const dim3 b(p.threads, p.rows);
+  const int smem = p.w > 1 ? 2 * kStages * p.nv * p.threads * p.rows * 16 : 0;
+  if (p.nv == 0) { norm_bwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
+  if (p.w == 1) return p.nv == 8 ? launch(norm_bwd_kernel<DT, 1, 8, PB, BIAS>, a, grid, b, smem, s) : launch(norm_bwd_kernel<DT, 1, 16, PB, BIAS>, a, grid, b, smem, s);
+  if (p.nv == 1) return launch(norm_bwd_kernel<DT, VW, 1, PB, BIAS>, a, grid, b, smem, s);
+  if (p.nv == 2) return launch(norm_bwd_kernel<DT, VW, 2, PB, BIAS>, a, grid, b, smem, s);
+  if constexpr (DT == JP_F32) return launch(norm_bwd_kernel<DT, VW, 4, PB, BIAS>, a, grid, b, smem, s);
+  return cudaErrorInvalidConfiguration;
 }
 
 }  // namespace
 
 cudaError_t launch_norm_forward(const NormArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a.H, a.dtype, vector_rows(a, false));
+  const Plan p = plan_for(a.H, a.dtype, vector_rows(a, false), false);
   const int grid = grid_for(a.T, p, sms);
-  if (a.dtype == JP_BF16) fwd<JP_BF16>(a, p, grid, s);
-  else fwd<JP_F32>(a, p, grid, s);
-  return cudaGetLastError();
+  if (a.dtype == JP_BF16) return a.param_bf16 ? fwd<JP_BF16, true>(a, p, grid, s) : fwd<JP_BF16, false>(a, p, grid, s);
+  return a.param_bf16 ? fwd<JP_F32, true>(a, p, grid, s) : fwd<JP_F32, false>(a, p, grid, s);
 }
 
 // Lines of partial sums a backward call can need, whatever the alignment of its pointers.
 int64_t norm_backward_groups(int64_t T, int64_t H, int dtype, int sms) {
   int64_t most = 0;
   for (int vec = 0; vec < 2; ++vec) {
-    const Plan p = plan_for(H, dtype, vec != 0);
+    const Plan p = plan_for(H, dtype, vec != 0, true);
     const int64_t g = (int64_t)grid_for(T, p, sms) * p.rows;
     most = g > most ? g : most;
   }
@@ -418,15 +558,23 @@ int64_t norm_backward_groups(int64_t T, int64_t H, int dtype, int sms) {
 }
 
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a.H, a.dtype, vector_rows(a, true));
+  const Plan p = plan_for(a.H, a.dtype, vector_rows(a, true), true);
   const int grid = grid_for(a.T, p, sms);
-  if (a.dtype == JP_BF16) bwd<JP_BF16>(a, p, grid, s);
-  else bwd<JP_F32>(a, p, grid, s);
-  cudaError_t e = cudaGetLastError();
+  auto run = [&](auto* with, auto* without) { return a.dbias ? with(a, p, grid, s) : without(a, p, grid, s); };
+  cudaError_t e;
+  if (a.dtype == JP_BF16) e = a.param_bf16 ? run(bwd<JP_BF16, true, true>, bwd<JP_BF16, true, false>) : run(bwd<JP_BF16, false, true>, bwd<JP_BF16, false, false>);
+  else e = a.param_bf16 ? run(bwd<JP_F32, true, true>, bwd<JP_F32, true, false>) : run(bwd<JP_F32, false, true>, bwd<JP_F32, false, false>);
   if (e != cudaSuccess) return e;
-  norm_sum_kernel<<<dim3((unsigned)((a.H + 31) / 32), a.dbias ? 2 : 1), dim3(32, 8), 0, s>>>(
-      a.partial, (int64_t)grid * p.rows, a.H, a.dweight, a.dbias);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)((a.H + 31) / 32), a.dbias ? 2 : 1);
+  cfg.blockDim = dim3(32, 32);
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, norm_sum_kernel, (const float*)a.partial, (int64_t)grid * p.rows, a.H, a.dbias ? 2 : 1, a.dweight, a.dbias);
 }
 
 }  // namespace jp
