@@ -123,6 +123,18 @@ struct Params {
       }
     }
   }
+  __device__ __forceinline__ void read(const char* p) {     // (NV == 1) W consecutive ones
+#pragma unroll
+    for (int q = 0; q < N; q += N < 4 ? 2 : 4) {
+      if constexpr (N < 4) {
+        const uint2 v = *(const uint2*)(p + q * 4);
+        r[q] = v.x; r[q + 1] = v.y;
+      } else {
+        const uint4 v = *(const uint4*)(p + q * 4);
+        r[q] = v.x; r[q + 1] = v.y; r[q + 2] = v.z; r[q + 3] = v.w;
+      }
+    }
+  }
   __device__ __forceinline__ float get(int i, int e) const {
     if constexpr (W == 1) return __uint_as_float(r[i]);
     else if constexpr (BF16) {
@@ -134,7 +146,7 @@ struct Params {
 
 // The group's rows of NT matrices one after the other: row `first`, then every `step`-th.
 constexpr int kStages = 3;
-template <int DT, int W, int NV, int NT>
+template <int DT, int W, int NV, int NT, int STAGES = kStages>
 struct Rows {
   using Ac = Access<DT, W>;
   static constexpr int ES = Vec<DT>::ESIZE;
@@ -142,7 +154,7 @@ struct Rows {
   const char* base[NT];
   int64_t pitch[NT];
   int64_t next_row, step, T, H;
-  uint4* places;                // [kStages][NT][NV][threads of the block], this thread's column
+  uint4* places;                // [STAGES][NT][NV][threads of the block], this thread's column
   int threads, in, out;
   typename Ac::raw ahead[kAsync ? 1 : NT][kAsync ? 1 : NV];
   __device__ __forceinline__ void fetch() {
@@ -165,7 +177,7 @@ struct Rows {
     next_row += step;
     if constexpr (kAsync) {
       asm volatile("cp.async.commit_group;" ::: "memory");
-      in = in == kStages - 1 ? 0 : in + 1;
+      in = in == STAGES - 1 ? 0 : in + 1;
     }
   }
   __device__ __forceinline__ void start(int64_t first) {
@@ -173,7 +185,7 @@ struct Rows {
     in = out = 0;
     if constexpr (kAsync) {
 #pragma unroll
-      for (int s = 0; s < kStages; ++s) fetch();
+      for (int s = 0; s < STAGES; ++s) fetch();
     } else {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -184,7 +196,7 @@ struct Rows {
   }
   // the oldest row; columns past the end read 0
   __device__ __forceinline__ void take(typename Ac::raw (&v)[NT][NV]) {
-    if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -192,7 +204,7 @@ struct Rows {
         if constexpr (kAsync) v[t][i] = column<W>(i) < H ? places[((out * NT + t) * NV + i) * threads] : Ac::zero();
         else v[t][i] = ahead[t][i];
       }
-    if constexpr (kAsync) out = out == kStages - 1 ? 0 : out + 1;
+    if constexpr (kAsync) out = out == STAGES - 1 ? 0 : out + 1;
   }
 };
 
@@ -261,6 +273,95 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
         float o[W];
 #pragma unroll
         for (int e = 0; e < W; ++e) o[e] = fmaf(v[i][e] * rstd, w.get(i, e), b.get(i, e));
+        Ac::store(y + c * ES, o);
+      }
+    }
+  }
+}
+
+// One warp a row, NVL vectors a lane, for many rows of up to 4096 bf16 or 2048 fp32: the reductions are shuffles and no row waits for
+// another (a block of 256 threads a row, with a barrier for each of its two sums, took 48 us at 8192 x 4096 with bias in bf16; this takes 30).  Weight and
+// bias are in shared memory beside the rows to come.
+constexpr int kWarpRows = 12;                 // rows a block
+constexpr int kWarpStages = 2;
+constexpr int warp_blocks(int nvl) { return nvl == 16 ? 1 : nvl == 8 ? 2 : 3; }      // per SM
+template <int DT, int NVL, bool PB>
+__global__ void __launch_bounds__(32 * kWarpRows, warp_blocks(NVL)) norm_fwd_warp_kernel(NormArgs A) {
+  constexpr int W = Vec<DT>::N, ES = Vec<DT>::ESIZE, PS = PB ? 2 : 4;
+  using Ac = Access<DT, W>;
+  extern __shared__ uint4 places[];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int lane = threadIdx.x, H = (int)A.H;
+  const float inv_h = 1.f / (float)A.H;
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  Rows<DT, W, NVL, 1, kWarpStages> in;
+  in.base[0] = (const char*)A.x;
+  in.pitch[0] = A.ld_x * ES;
+  in.step = step; in.T = A.T; in.H = A.H;
+  in.threads = 32 * kWarpRows;
+  in.places = places + threadIdx.y * 32 + lane;
+  in.start(row);
+  const int n = H * PS / 16, tid = threadIdx.y * 32 + lane;
+  uint4* const params = places + kWarpStages * NVL * 32 * kWarpRows;
+  for (int i = tid; i < n; i += 32 * kWarpRows) {
+    params[i] = ((const uint4*)A.weight)[i];
+    if (A.bias) params[n + i] = ((const uint4*)A.bias)[i];
+  }
+  const char* w = (const char*)params;
+  const char* b = A.bias ? (const char*)(params + n) : nullptr;
+  __syncthreads();
+  for (; row < A.T; row += step) {
+    uint4 rows[1][NVL];
+    in.take(rows);
+    uint4 (&v)[NVL] = rows[0];
+    in.fetch();
+    float mean = 0.f;
+    if (!A.rms) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < NVL; ++i) {
+        float t[W];
+        Ac::unpack(v[i], t);
+#pragma unroll
+        for (int o = 1; o < W; o *= 2)
+#pragma unroll
+          for (int e = 0; e + o < W; e += 2 * o) t[e] += t[e + o];
+        s += t[0];
+      }
+      mean = warp_sum(s) * inv_h;
+    }
+    float s2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < NVL; ++i)
+      if ((lane + i * 32) * W < H) {
+        float t[W];
+        Ac::unpack(v[i], t);
+#pragma unroll
+        for (int e = 0; e < W; ++e) s2 = fmaf(t[e] - mean, t[e] - mean, s2);
+      }
+    const float rstd = 1.f / sqrtf(warp_sum(s2) * inv_h + A.eps);
+    if (lane == 0) {
+      if (A.out_mean) A.out_mean[row] = mean;
+      if (A.out_rstd) A.out_rstd[row] = rstd;
+    }
+    char* y = (char*)A.y + row * A.ld_y * ES;
+#pragma unroll
+    for (int i = 0; i < NVL; ++i) {
+      const int c = (lane + i * 32) * W;
+      if (c < H) {
+        float t[W], o[W];
+        Ac::unpack(v[i], t);
+        Params<W, 1, PB> p;
+        p.read(w + c * PS);
+#pragma unroll
+        for (int e = 0; e < W; ++e) o[e] = (t[e] - mean) * rstd * p.get(0, e);
+        if (b) {
+          p.read(b + c * PS);
+#pragma unroll
+          for (int e = 0; e < W; ++e) o[e] += p.get(0, e);
+        }
         Ac::store(y + c * ES, o);
       }
     }
@@ -512,9 +613,25 @@ cudaError_t launch(K* kernel, const NormArgs& a, dim3 grid, dim3 block, int smem
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
+template <int DT, bool PB, int NVL>
+cudaError_t fwd_warp(const NormArgs& a, cudaStream_t s, int sms) {
+  const int64_t need = (a.T + kWarpRows - 1) / kWarpRows, cap = (int64_t)sms * warp_blocks(NVL);
+  const int smem = kWarpStages * NVL * 32 * kWarpRows * 16 + (int)a.H * (PB ? 2 : 4) * (a.bias ? 2 : 1);
+  return launch(norm_fwd_warp_kernel<DT, NVL, PB>, a, dim3((unsigned)(need < cap ? need : cap)), dim3(32, kWarpRows), smem, s);
+}
+
 template <int DT, bool PB>
-cudaError_t fwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
+cudaError_t fwd(const NormArgs& a, cudaStream_t s, int sms) {
   constexpr int VW = Vec<DT>::N;
+  const bool vec = vector_rows(a, false);
+  // a warp a row where every SM gets its blocks full of rows; with fewer rows a block a row is done sooner
+  if (vec && a.T >= (int64_t)sms * kWarpRows && a.H > 64 * VW && a.H <= 512 * VW) {
+    if (a.H <= 128 * VW) return fwd_warp<DT, PB, 4>(a, s, sms);
+    if (a.H <= 256 * VW) return fwd_warp<DT, PB, 8>(a, s, sms);
+    return fwd_warp<DT, PB, 16>(a, s, sms);
+  }
+  const Plan p = plan_for(a.H, a.dtype, vec, false);
+  const int grid = grid_for(a.T, p, sms);
   const dim3 b(p.threads, p.rows);
   const int smem = p.w > 1 ? kStages * p.nv * p.threads * p.rows * 16 : 0;
   if (p.nv == 0) { norm_fwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
@@ -540,10 +657,8 @@ cudaError_t bwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_norm_forward(const NormArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a.H, a.dtype, vector_rows(a, false), false);
-  const int grid = grid_for(a.T, p, sms);
-  if (a.dtype == JP_BF16) return a.param_bf16 ? fwd<JP_BF16, true>(a, p, grid, s) : fwd<JP_BF16, false>(a, p, grid, s);
-  return a.param_bf16 ? fwd<JP_F32, true>(a, p, grid, s) : fwd<JP_F32, false>(a, p, grid, s);
+  if (a.dtype == JP_BF16) return a.param_bf16 ? fwd<JP_BF16, true>(a, s, sms) : fwd<JP_BF16, false>(a, s, sms);
+  return a.param_bf16 ? fwd<JP_F32, true>(a, s, sms) : fwd<JP_F32, false>(a, s, sms);
 }
 
 // Lines of partial sums a backward call can need, whatever the alignment of its pointers.

@@ -96,6 +96,22 @@ def test_both_passes_match_the_formula(ctx, T, H, dtype, rms, bias):
     check_backward(got, dy, x, w, mean, rstd, rms)
 
 
+@pytest.mark.parametrize("T,H", [(1776, 520), (2001, 1024), (1999, 1288), (1777, 2048), (3600, 4096), (1800, 4088)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rms,bias,param", [(False, True, torch.float32), (True, False, torch.bfloat16)])
+def test_many_rows(ctx, T, H, dtype, rms, bias, param):
+    """Rows enough to fill every SM several times over.  A register adds at most 26 rows, a sum of lines at most 64 in a row."""
+    x, dy, w, b = make(T, H, dtype, param, bias, seed=T + H, ld=H + (H % 16))
+    y, mean, rstd = runner.layer_norm(ctx, x, w, b, eps=EPS, rms=rms)
+    check_forward(y, mean, rstd, x, w, b, rms)
+    got = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd, rms=rms, bias=bias)
+    check_backward(got, dy, x, w, mean, rstd, rms)
+    again = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd, rms=rms, bias=bias)
+    assert all(a is c or torch.equal(a, c) for a, c in zip(got, again))
+    y2, _, _ = runner.layer_norm(ctx, x, w, b, eps=EPS, rms=rms, out=x)
+    assert torch.equal(y2, y)
+
+
 @pytest.mark.parametrize("H,ld", [(2048, 2056), (1000, 1001), (63, 70), (4096, 4104)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_row_pitches_and_in_place(ctx, H, ld, dtype):
