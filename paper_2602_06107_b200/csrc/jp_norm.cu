@@ -151,38 +151,50 @@ struct Rows {
   using Ac = Access<DT, W>;
   static constexpr int ES = Vec<DT>::ESIZE;
   static constexpr bool kAsync = W > 1;
-  const char* base[NT];
-  int64_t pitch[NT];
-  int64_t next_row, step, T, H;
-  uint4* places;                // [STAGES][NT][NV][threads of the block], this thread's column
+  const char* next[NT];         // the next row to fetch, from this thread's first column on
+  int64_t stride[NT];           // bytes from one row of the group to the next
+  int64_t left;                 // rows not fetched yet
+  const uint4* read;            // this thread's column of places [STAGES][NT][NV][threads of the block]
+  uint32_t write;
   int threads, in, out;
+  bool have[NV];                // the access is within the row
   typename Ac::raw ahead[kAsync ? 1 : NT][kAsync ? 1 : NV];
   __device__ __forceinline__ void fetch() {
-    if (next_row < T) {
+    if (left > 0) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const char* r = base[t] + next_row * pitch[t];
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int64_t c = column<W>(i);
-          if (c < H) {
+        for (int i = 0; i < NV; ++i)
+          if (have[i]) {
+            const char* p = next[t] + (int64_t)i * (int)blockDim.x * W * ES;
             if constexpr (kAsync)
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(
-                               places + ((in * NT + t) * NV + i) * threads)), "l"(r + c * ES) : "memory");
-            else ahead[t][i] = Ac::load(r + c * ES);
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(write + ((in + t) * NV + i) * threads * 16), "l"(p) : "memory");
+            else ahead[t][i] = Ac::load(p);
           }
-        }
-      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) next[t] += stride[t];
+      --left;
     }
-    next_row += step;
     if constexpr (kAsync) {
       asm volatile("cp.async.commit_group;" ::: "memory");
-      in = in == STAGES - 1 ? 0 : in + 1;
+      in = in == (STAGES - 1) * NT ? 0 : in + NT;
     }
   }
-  __device__ __forceinline__ void start(int64_t first) {
-    next_row = first;
+  // rows first, first + step, ... below T of the NT matrices
+  __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T,
+                                        int64_t H, uint4* smem) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      next[t] = (const char*)base[t] + (first * ld[t] + (int64_t)threadIdx.x * W) * ES;
+      stride[t] = step * ld[t] * ES;
+    }
+    left = first < T ? (T - first + step - 1) / step : 0;
+    threads = blockDim.x * blockDim.y;
+    read = smem + threadIdx.y * blockDim.x + threadIdx.x;
+    write = (uint32_t)__cvta_generic_to_shared(read);
     in = out = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) have[i] = column<W>(i) < H;
     if constexpr (kAsync) {
 #pragma unroll
       for (int s = 0; s < STAGES; ++s) fetch();
@@ -201,10 +213,10 @@ struct Rows {
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        if constexpr (kAsync) v[t][i] = column<W>(i) < H ? places[((out * NT + t) * NV + i) * threads] : Ac::zero();
+        if constexpr (kAsync) v[t][i] = have[i] ? read[((out + t) * NV + i) * threads] : Ac::zero();
         else v[t][i] = ahead[t][i];
       }
-    if constexpr (kAsync) out = out == STAGES - 1 ? 0 : out + 1;
+    if constexpr (kAsync) out = out == (STAGES - 1) * NT ? 0 : out + NT;
   }
 };
 
@@ -224,12 +236,7 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
   int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   Rows<DT, W, NV, 1> in;
-  in.base[0] = (const char*)A.x;
-  in.pitch[0] = A.ld_x * ES;
-  in.step = step; in.T = A.T; in.H = A.H;
-  in.threads = blockDim.x * blockDim.y;
-  in.places = places + threadIdx.y * blockDim.x + threadIdx.x;
-  in.start(row);
+  in.start({A.x}, {A.ld_x}, row, step, A.T, A.H, places);
   Params<W, NV, PB> w, b;
   w.load(A.weight, A.H);
   b.load(A.bias, A.H);
@@ -297,12 +304,7 @@ __global__ void __launch_bounds__(32 * kWarpRows, warp_blocks(NVL)) norm_fwd_war
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   Rows<DT, W, NVL, 1, kWarpStages> in;
-  in.base[0] = (const char*)A.x;
-  in.pitch[0] = A.ld_x * ES;
-  in.step = step; in.T = A.T; in.H = A.H;
-  in.threads = 32 * kWarpRows;
-  in.places = places + threadIdx.y * 32 + lane;
-  in.start(row);
+  in.start({A.x}, {A.ld_x}, row, step, A.T, A.H, places);
   const int n = H * PS / 16, tid = threadIdx.y * 32 + lane;
   uint4* const params = places + kWarpStages * NVL * 32 * kWarpRows;
   for (int i = tid; i < n; i += 32 * kWarpRows) {
@@ -403,12 +405,56 @@ __global__ void __launch_bounds__(1024) norm_fwd_wide_kernel(NormArgs A) {
   }
 }
 
+// N sums at once over the threads of a row's group (N a power of two up to 8), every thread getting all of them: N - 1 + log2(32 / N)
+// shuffles instead of 5 N, one barrier, and each warp adds the warps' parts by itself.
+template <int N>
+__device__ __forceinline__ void group_sums(float (&v)[N], float (*sh)[N][kMaxWarps], int& slot) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int n = N, o = 16; o > 0; o >>= 1) {
+    if (n > 1) {                                            // half of the values go to the lanes that differ in bit o
+      n /= 2;
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i)
+        if (i < n) {
+          const float keep = (lane & o) ? v[i + n] : v[i], send = (lane & o) ? v[i] : v[i + n];
+          v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        }
+    } else {
+      v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    }
+  }
+  constexpr int kLanes = 32 / N;                            // lane / kLanes is the number of the sum it holds
+  const int mine = lane / kLanes;
+  float s = v[0];
+  if (blockDim.x > 32) {
+    const int warps = blockDim.x >> 5;
+    float (*part)[kMaxWarps] = sh[slot];
+    slot ^= 1;
+    if (lane % kLanes == 0) part[mine][threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.f;
+    for (int w = lane % kLanes; w < warps; w += kLanes) s += part[mine][w];
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, s, i * kLanes);
+}
+
+__device__ __forceinline__ void keep_packed(uint4& v) { asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)); }
+__device__ __forceinline__ void keep_packed(uint32_t& v) { asm volatile("" : "+r"(v)); }
+
+// Rows a group takes at a time, so that their sums share a barrier: at 8192 x 4096 (RMS norm, bf16) one at a time takes 55 us, two 41;
+// four do not fit the registers (67).
+__host__ __device__ constexpr int bwd_rows(int w, int nv) { return w == 1 || nv == 4 ? 1 : 2; }
+
 template <int DT, int W, int NV, bool PB, bool BIAS>
-__global__ void __launch_bounds__(group_threads(W, NV)) norm_bwd_kernel(NormArgs A) {
+__global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
   using Ac = Access<DT, W>;
-  constexpr int ES = Vec<DT>::ESIZE;
+  constexpr int ES = Vec<DT>::ESIZE, R = bwd_rows(W, NV);
   extern __shared__ uint4 places[];
-  __shared__ float2 sh[2][kMaxWarps];
+  __shared__ float sh[2][2 * R][kMaxWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   int slot = 0;
   const float inv_h = 1.f / (float)A.H;
@@ -422,66 +468,93 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_bwd_kernel(NormArgs
     }
   const int64_t group = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  Rows<DT, W, NV, 2> in;
-  in.base[0] = (const char*)A.x;
-  in.base[1] = (const char*)A.dy;
-  in.pitch[0] = A.ld_x * ES;
-  in.pitch[1] = A.ld_dy * ES;
-  in.step = step; in.T = A.T; in.H = A.H;
-  in.threads = blockDim.x * blockDim.y;
-  in.places = places + threadIdx.y * blockDim.x + threadIdx.x;
-  in.start(group);
-  Params<W, NV, PB> w;
-  w.load(A.weight, A.H);
-  float mean = 0.f, rstd = 0.f;
-  if (group < A.T) {
-    mean = A.rms ? 0.f : A.mean[group];
-    rstd = A.rstd[group];
+  Rows<DT, W, NV, 2, 2 * R> in;
+  in.start({A.x, A.dy}, {A.ld_x, A.ld_dy}, group, step, A.T, A.H, places);
+  float w[NV][W];
+  {
+    Params<W, NV, PB> p;
+    p.load(A.weight, A.H);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < W; ++e) w[i][e] = p.get(i, e);
   }
-  for (int64_t row = group; row < A.T; row += step) {
-    typename Ac::raw raw[2][NV];
-    in.take(raw);
-    in.fetch();
-    float mean_next = 0.f, rstd_next = 0.f;
-    if (row + step < A.T) {
-      mean_next = A.rms ? 0.f : A.mean[row + step];
-      rstd_next = A.rstd[row + step];
+  char* out = (char*)A.dx + (group * A.ld_dx + (int64_t)threadIdx.x * W) * ES;
+  const int64_t out_stride = step * A.ld_dx * ES;
+  float mean_next[R], rstd_next[R];
+  auto fetch_stats = [&](int64_t row) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool have = row + r * step < A.T;
+      mean_next[r] = have && !A.rms ? A.mean[row + r * step] : 0.f;
+      rstd_next[r] = have ? A.rstd[row + r * step] : 0.f;
     }
-    float s1 = 0.f, s2 = 0.f;
+  };
+  fetch_stats(group);
+  for (int64_t row = group; row < A.T; row += R * step) {
+    typename Ac::raw raw[R][2][NV];
+    float mean[R], rstd[R], s[2 * R];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float x[W], dy[W];
-      Ac::unpack(raw[0][i], x);
-      Ac::unpack(raw[1][i], dy);                            // (0 past the end, and so is everything below)
+    for (int r = 0; r < R; ++r) {
+      mean[r] = mean_next[r];
+      rstd[r] = rstd_next[r];
+      in.take(raw[r]);
+      if (r > 0 && row + r * step >= A.T) {                 // past the last row: 0, and so is everything below
 #pragma unroll
-      for (int e = 0; e < W; ++e) {
-        const float xh = (x[e] - mean) * rstd, g = dy[e] * w.get(i, e);
-        s1 += g;
-        s2 = fmaf(g, xh, s2);
-        dw[i][e] = fmaf(dy[e], xh, dw[i][e]);
-        if (BIAS) db[i][e] += dy[e];
+        for (int i = 0; i < NV; ++i) raw[r][0][i] = raw[r][1][i] = Ac::zero();
       }
+      in.fetch();
     }
-    const float2 s = group_sum(s1, s2, sh, slot);
-    const float m1 = A.rms ? 0.f : s.x * inv_h, m2 = s.y * inv_h;
-    char* dx = (char*)A.dx + row * A.ld_dx * ES;
+    fetch_stats(row + R * step);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      if (c < A.H) {
-        float x[W], dy[W], o[W];
-        Ac::unpack(raw[0][i], x);
-        Ac::unpack(raw[1][i], dy);
+    for (int r = 0; r < R; ++r) {
+      float s1 = 0.f, s2 = 0.f;
+      const float shift = -mean[r] * rstd[r];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        float x[W], dy[W];
+        Ac::unpack(raw[r][0][i], x);
+        Ac::unpack(raw[r][1][i], dy);                       // (0 past the end, and so is everything below)
 #pragma unroll
         for (int e = 0; e < W; ++e) {
-          const float xh = (x[e] - mean) * rstd, g = dy[e] * w.get(i, e);
-          o[e] = (g - m1 - xh * m2) * rstd;
+          const float xh = fmaf(x[e], rstd[r], shift), g = dy[e] * w[i][e];
+          s1 += g;
+          s2 = fmaf(g, xh, s2);
+          dw[i][e] = fmaf(dy[e], xh, dw[i][e]);
+          if (BIAS) db[i][e] += dy[e];
         }
-        Ac::store(dx + c * ES, o);
       }
+      s[2 * r] = s1;
+      s[2 * r + 1] = s2;
     }
-    mean = mean_next;
-    rstd = rstd_next;
+    group_sums<2 * R>(s, sh, slot);
+    // (unpacked again below instead of being kept over the sums: as fp32 a row takes twice the registers)
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        keep_packed(raw[r][0][i]);
+        keep_packed(raw[r][1][i]);
+      }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r * step >= A.T) break;
+      // dx = r (g - m1 - xhat m2) = r g + (x c1 + c0)
+      const float m1 = A.rms ? 0.f : s[2 * r] * inv_h, m2 = s[2 * r + 1] * inv_h;
+      const float c1 = -rstd[r] * rstd[r] * m2, c0 = rstd[r] * (mean[r] * rstd[r] * m2 - m1);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (in.have[i]) {
+          float x[W], dy[W], o[W];
+          Ac::unpack(raw[r][0][i], x);
+          Ac::unpack(raw[r][1][i], dy);
+#pragma unroll
+          for (int e = 0; e < W; ++e) o[e] = fmaf(dy[e] * w[i][e], rstd[r], fmaf(x[e], c1, c0));
+          Ac::store(out + (int64_t)i * (int)blockDim.x * W * ES, o);
+        }
+      }
+      out += out_stride;
+    }
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the kernel that adds the lines may set up
   float* pw = A.partial + group * (BIAS ? 2 : 1) * A.H;
@@ -586,11 +659,11 @@ Plan plan_for(int64_t H, int dtype, bool vec, bool backward) {
   return p;
 }
 
-// Blocks: all rows at once where there are few, else what the SMs hold.
-int grid_for(int64_t T, const Plan& p, int sms) {
+// Blocks: all rows at once where there are few, else what the SMs hold (a backward pass: 128 registers a thread).
+int grid_for(int64_t T, const Plan& p, int sms, bool backward) {
   const int64_t need = (T + p.rows - 1) / p.rows;
-  const int per_sm = 1024 / (p.threads * p.rows);
-  const int64_t cap = (int64_t)sms * (per_sm > 8 ? 8 : per_sm);
+  const int per_sm = (backward ? 512 : 1024) / (p.threads * p.rows);
+  const int64_t cap = (int64_t)sms * (per_sm > 8 ? 8 : per_sm < 1 ? 1 : per_sm);
   return (int)(need < cap ? need : cap);
 }
 
@@ -631,7 +704,7 @@ cudaError_t fwd(const NormArgs& a, cudaStream_t s, int sms) {
     return fwd_warp<DT, PB, 16>(a, s, sms);
   }
   const Plan p = plan_for(a.H, a.dtype, vec, false);
-  const int grid = grid_for(a.T, p, sms);
+  const int grid = grid_for(a.T, p, sms, false);
   const dim3 b(p.threads, p.rows);
   const int smem = p.w > 1 ? kStages * p.nv * p.threads * p.rows * 16 : 0;
   if (p.nv == 0) { norm_fwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
@@ -645,7 +718,7 @@ template <int DT, bool PB, bool BIAS>
 cudaError_t bwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
   constexpr int VW = Vec<DT>::N;
   const dim3 b(p.threads, p.rows);
-  const int smem = p.w > 1 ? 2 * kStages * p.nv * p.threads * p.rows * 16 : 0;
+  const int smem = p.w > 1 ? 2 * (2 * bwd_rows(p.w, p.nv)) * p.nv * p.threads * p.rows * 16 : 0;
   if (p.nv == 0) { norm_bwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
   if (p.w == 1) return p.nv == 8 ? launch(norm_bwd_kernel<DT, 1, 8, PB, BIAS>, a, grid, b, smem, s) : launch(norm_bwd_kernel<DT, 1, 16, PB, BIAS>, a, grid, b, smem, s);
   if (p.nv == 1) return launch(norm_bwd_kernel<DT, VW, 1, PB, BIAS>, a, grid, b, smem, s);
@@ -666,7 +739,7 @@ int64_t norm_backward_groups(int64_t T, int64_t H, int dtype, int sms) {
   int64_t most = 0;
   for (int vec = 0; vec < 2; ++vec) {
     const Plan p = plan_for(H, dtype, vec != 0, true);
-    const int64_t g = (int64_t)grid_for(T, p, sms) * p.rows;
+    const int64_t g = (int64_t)grid_for(T, p, sms, true) * p.rows;
     most = g > most ? g : most;
   }
   return most;
@@ -674,7 +747,7 @@ int64_t norm_backward_groups(int64_t T, int64_t H, int dtype, int sms) {
 
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s, int sms) {
   const Plan p = plan_for(a.H, a.dtype, vector_rows(a, true), true);
-  const int grid = grid_for(a.T, p, sms);
+  const int grid = grid_for(a.T, p, sms, true);
   auto run = [&](auto* with, auto* without) { return a.dbias ? with(a, p, grid, s) : without(a, p, grid, s); };
   cudaError_t e;
   if (a.dtype == JP_BF16) e = a.param_bf16 ? run(bwd<JP_BF16, true, true>, bwd<JP_BF16, true, false>) : run(bwd<JP_BF16, false, true>, bwd<JP_BF16, false, false>);
