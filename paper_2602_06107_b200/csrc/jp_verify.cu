@@ -29,7 +29,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kDrawBlocks = 3;       // blocks of the draw per SM
+constexpr int kDrawBlocks = 2;       // blocks of the draw per SM (three get 80 registers a thread and were 5 % slower)
 constexpr unsigned kAll = 0xffffffffu;
 constexpr double kLog2eD = 1.4426950408889634074;
 constexpr double kLn2D = 0.69314718055994530942;
@@ -122,21 +122,24 @@ __device__ __forceinline__ double block_scan_d(double v, double* sh, double* tot
 
 // 2^x times what tab is scaled by, |x| <= 1000, to about 2e-12 relative.  tab[j] is scale 2^(j / 32) with j << 15 taken from its
 // high word, so that adding k << 15 for k = round(32 x) gives scale 2^(k / 32) in one addition.
-__device__ __forceinline__ double exp2_table(double x, const double* tab) {
+// Constants whose low word is 0 are part of an instruction; the two that need all their bits come in registers (c1 = ln 2,
+// c2 = ln^2 2 / 2), since the compiler would otherwise move them there again for every element.
+__device__ __forceinline__ double exp2_table(double x, const double* tab, double c1, double c2) {
   constexpr double kMagic = 211106232532992.0;            // 1.5 * 2^47: adding it leaves k in the low word
   const double m = x + kMagic;
   const int k = __double2loint(m);
   const double t = tab[k & 31];
   const double r = x - (m - kMagic);                      // |r| <= 1/64; terms of exp(r ln 2) up to r^4
-  double y = 0.0096181291076284771619;
-  y = fma(y, r, 0.055504108664821579953);
-  y = fma(y, r, 0.24022650695910071233);
-  y = fma(y, r, 0.69314718055994530942);
+  double y = 0.009618125855922699;                        // ln^4 2 / 24 and ln^3 2 / 6 to 2^-21: r^3 makes 1e-13 of that
+  y = fma(y, r, 0.05550411343574524);
+  y = fma(y, r, c2);
+  y = fma(y, r, c1);
   y = fma(y, r, 1.0);
   return y * __hiloint2double(__double2hiint(t) + (k << 15), __double2loint(t));
 }
+constexpr double kLn2Square = 0.24022650695910071233;     // ln^2 2 / 2
 __device__ __forceinline__ double exp2_clamped(double x, const double* tab) {     // 0 below -1000, 2^1000 above
-  return x < -1000.0 ? 0.0 : exp2_table(x < 1000.0 ? x : 1000.0, tab);
+  return x < -1000.0 ? 0.0 : exp2_table(x < 1000.0 ? x : 1000.0, tab, kLn2D, kLn2Square);
 }
 __device__ __forceinline__ double table_entry(int j, double scale) {
   const double t = kPow2[j] * scale;
@@ -249,13 +252,13 @@ struct RowLoop {
   const double* tab;
   RowSums r;
   __device__ __forceinline__ void two(const uint4& v0, const uint4& v1, int i0, int i1) {
-    float t[2 * W];
+    float t[4];
 #pragma unroll
-    for (int e = 0; e < 2 * W; ++e) t[e] = ex2_approx(fmaf(Vec<DT>::get(e < W ? v0 : v1, e % W), cf, -ref));
-#pragma unroll
-    for (int o = 1; o < 2 * W; o *= 2)
-#pragma unroll
-      for (int e = 0; e + o < 2 * W; e += 2 * o) t[e] += t[e + o];
+    for (int e = 0; e < 2 * W; ++e) {
+      const float x = ex2_approx(fmaf(Vec<DT>::get(e < W ? v0 : v1, e % W), cf, -ref));
+      t[e & 3] = e < 4 ? x : t[e & 3] + x;
+    }
+    t[0] = (t[0] + t[1]) + (t[2] + t[3]);
     if (t[0] > 32.f) r.exact += exact_terms<DT>(v0, v1, zref, c, tab);     // rare: logits well above the sample that gave the reference
     else r.fast += (double)t[0];
     if (GREEDY) {
@@ -398,40 +401,51 @@ __device__ __forceinline__ double row_sum(const RowPart* p, int splits, double c
 struct DrawRow {
   const char* z;
   double c, ref, off;        // off = -ref c
+  double c1, c2;             // of exp2_table
   float cut;                 // smaller logits count as this one: 2^kClamp
   const double* tab;
   // FAR: references so large that off would lose too much, and that cut may be the reference itself
   template <bool FAR>
   __device__ __forceinline__ double prob(float v) const {
     if (FAR) {
-      const double y = exp2_table(((double)v - ref) * c, tab);
+      const double y = exp2_table(((double)v - ref) * c, tab, c1, c2);
       return v < cut ? 0.0 : y;
     }
-    return exp2_table(fma((double)fmaxf(v, cut), c, off), tab);
+    return exp2_table(fma((double)fmaxf(v, cut), c, off), tab, c1, c2);
   }
 };
 
-// Sums of the segments first, first + step, ... (count of them) of seg_vecs vectors each, by one warp, into out[segment].
+// Sums of the segments first, first + step, ... (count of them) of seg_vecs vectors each (a multiple of 32), by one warp, into
+// out[segment].
 template <int DT, bool Q, bool FAR>
 __device__ __forceinline__ void segments(const DrawRow& T, const DrawRow& D, int64_t skip, int first, int step, int count,
                                          int64_t seg_vecs, int64_t nv, int64_t V, SegPart* out) {
   constexpr int W = Vec<DT>::N;
   const int lane = threadIdx.x & 31;
-  const int steps = (int)((seg_vecs + 31) / 32);
-  const int64_t skip_vec = skip >= 0 ? skip / W : -1;
+  const int steps = (int)seg_vecs / 32, full = (int)(V / W);
+  const int skip_vec = skip >= 0 ? (int)(skip / W) : -1;
   // Two vectors are in flight while one is computed.  (They move through registers: a loop unrolled by three does not fit the
   // instruction cache and ran a quarter slower.)
   uint4 t0, t1, q0, q1;
-  int in_seg = 0, in_step = 0;                              // the next vector to load
+  int in_left = count, in_step = 0, at_vec = first * (int)seg_vecs + lane;         // the next vector to load
   auto fetch = [&](uint4& vt, uint4& vq) {
     vt = vq = Vec<DT>::neg_inf();
-    const int64_t o = (int64_t)in_step * 32 + lane, i = (int64_t)(first + in_seg * step) * seg_vecs + o;
-    if (in_seg < count && o < seg_vecs && i < nv) {
-      vt = row_vec<DT>(T.z, i, V);
-      if (Q) vq = row_vec<DT>(D.z, i, V);
-      if (!Q && i == skip_vec) Vec<DT>::set(vt, (int)(skip - skip_vec * W), JP_NEG_INF);
+    if (in_left > 0) {
+      if (at_vec < full) {
+        vt = ldg_stream((const uint4*)T.z + at_vec);
+        if (Q) vq = ldg_stream((const uint4*)D.z + at_vec);
+      } else if (at_vec < (int)nv) {
+        vt = row_vec<DT>(T.z, at_vec, V);
+        if (Q) vq = row_vec<DT>(D.z, at_vec, V);
+      }
+      if (!Q && at_vec == skip_vec) Vec<DT>::set(vt, (int)(skip - (int64_t)skip_vec * W), JP_NEG_INF);
+      at_vec += 32;
+      if (++in_step == steps) {
+        in_step = 0;
+        --in_left;
+        at_vec += (step - 1) * (int)seg_vecs;
+      }
     }
-    if (++in_step == steps) { in_step = 0; ++in_seg; }
   };
   fetch(t0, q0);
   fetch(t1, q1);
@@ -612,6 +626,8 @@ __global__ void __launch_bounds__(kThreads, kDrawBlocks) verify_draw_kernel(Veri
   if (kind != 1 || !usable) return;
 
   // masses of the row to draw from: this block's slice, a contiguous run of vectors a warp
+  double c1 = kLn2D, c2 = kLn2Square;
+  asm volatile("" : "+d"(c1), "+d"(c2));                    // (values to keep in registers, not constants)
   auto row_of = [&](const char* z, int r, double* table) {
     DrawRow d;
     d.z = z;
@@ -619,6 +635,8 @@ __global__ void __launch_bounds__(kThreads, kDrawBlocks) verify_draw_kernel(Veri
     d.ref = (double)s_ref[r];
     d.off = -d.ref * c;
     d.cut = __double2float_ru(d.ref + kClamp / c);
+    d.c1 = c1;
+    d.c2 = c2;
     d.tab = table;
     if (tid < 32) table[tid] = table_entry(tid, s_inv[r]);
     return d;
@@ -707,7 +725,8 @@ __global__ void __launch_bounds__(kThreads, kDrawBlocks) verify_draw_kernel(Veri
       if (mass_of[k] > 0 && before <= want) pick = Pick{tid * per + k, before};
       before += mass_of[k];
     }
-    const Pick seg = block_last(pick.place, pick.before, s_pick);
+    Pick seg = block_last(pick.place, pick.before, s_pick);
+    if (seg.place < 0) seg = Pick{0, 0.0};                  // (cannot be: the first segment with mass has nothing before it)
     const int64_t e0 = seg.place * A.seg_vecs * W, e1 = e0 + A.seg_vecs * W < A.V ? e0 + A.seg_vecs * W : A.V;
     const int64_t each = (A.seg_vecs * W + kThreads - 1) / kThreads;
     const int64_t f0 = e0 + each * tid, f1 = f0 + each < e1 ? f0 + each : e1;
@@ -745,10 +764,11 @@ __global__ void __launch_bounds__(kThreads, kDrawBlocks) verify_draw_kernel(Veri
     token = e0 + (at.place < 0 ? 0 : at.place);
   }
   if (tid == 0) {
-    A.out_tokens[b * (N + 1) + m] = (int32_t)token;
+    const bool have = token >= 0 && token < A.V;
+    A.out_tokens[b * (N + 1) + m] = have ? (int32_t)token : -1;
     if (A.out_logp)
       A.out_logp[b * (N + 1) + m] =
-          (float)((((double)Vec<DT>::load_scalar(T.z, token) - T.ref) * c - log2(sum_t * P)) * kLn2D);
+          have ? (float)((((double)Vec<DT>::load_scalar(T.z, token) - T.ref) * c - log2(sum_t * P)) * kLn2D) : 0.f;
   }
 }
 
@@ -769,10 +789,10 @@ VerifyPlan verify_plan(int64_t B, int N, int64_t V, int dtype, bool with_draft, 
   // Segments of the draw: short ones where there are few sequences, longer ones (fewer reductions) where they fill the SMs; blocks:
   // one wave of kDrawBlocks per SM.
   const int64_t warps = (int64_t)sms * kDrawBlocks * kWarps;
-  p.seg_vecs = B * ((nv + 63) / 64) >= warps ? 64 : 32;
-  if (p.seg_vecs * kVerifyMaxSegs < nv) p.seg_vecs = (nv + kVerifyMaxSegs - 1) / kVerifyMaxSegs;
+  p.seg_vecs = B * ((nv + 127) / 128) >= 2 * warps ? 128 : B * ((nv + 63) / 64) >= warps ? 64 : 32;
+  if (p.seg_vecs * kVerifyMaxSegs < nv) p.seg_vecs = ((nv + kVerifyMaxSegs - 1) / kVerifyMaxSegs + 31) / 32 * 32;
   p.n_segs = (int)((nv + p.seg_vecs - 1) / p.seg_vecs);
-  p.draw_splits = pick(sms * kDrawBlocks / (B > 0 ? B : 1), (p.n_segs + kWarps - 1) / kWarps);
+  p.draw_splits = pick(sms * kDrawBlocks / B, (p.n_segs + kWarps - 1) / kWarps);
   p.block_segs = (p.n_segs + p.draw_splits - 1) / p.draw_splits;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   p.parts_off = up((size_t)B * 4);
