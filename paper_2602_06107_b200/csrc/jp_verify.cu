@@ -10,9 +10,9 @@
 // Bound by HBM: (2 n + 1) rows of the vocabulary are read once, one pair of rows a sequence once more.
 //
 // verify_rows_kernel sums 2^((z - R) c) over slices of rows (c = log2 e / temperature).  The reference R need not be the maximum: fp32
-// has 2^+-126 of room.  So it is the largest of the slice's first 16 KB, and the loop has no running maximum: one unpack, one
-// FMA, one ex2 and one add an element; 16 terms (fp32 input: 8) are added in fp32, the rest in fp64.  Terms that reach 32 together (a
-// peak outside the sample, where the exponent's rounding would count) are taken again in fp64, and a slice whose sum leaves
+// has 2^+-126 of room.  So it is the largest of the slice's first 8 KB, and the loop has no running maximum: one unpack, one
+// FMA, one ex2 and one add an element; 16 terms (fp32 input: 8) are added in fp32, the rest in fp64.  Terms that reach
+// 256 together (a peak outside the sample: exponents of 8 and more are rounded by more than 2^-22) are taken again in fp64, and a slice whose sum leaves
 // 2^-60 .. 2^60 from its own maximum.
 //
 // verify_draw_kernel takes the decisions of a sequence (again in every block: cheaper than a launch of its own) and then the
@@ -196,8 +196,8 @@ __device__ __noinline__ double exact_terms(uint4 v0, uint4 v1, float zref, doubl
   return s;
 }
 
-constexpr int kGroup = 4;       // vectors a thread takes at a time
-constexpr int kGroups = 2;      // groups in flight: 32 KB a block (three were no faster)
+constexpr int kGroup = 2;       // vectors a thread takes at a time
+constexpr int kGroups = 3;      // groups in flight: 24 KB a block (more were no faster)
 template <int DT> __device__ __forceinline__ uint4 neg_inf() { return Vec<DT>::neg_inf(); }
 
 // A thread's vectors p[tid], p[tid + kThreads], ... below n through its own places in shared memory, kGroups groups ahead (asynchronous
@@ -259,7 +259,7 @@ struct RowLoop {
       t[e & 3] = e < 4 ? x : t[e & 3] + x;
     }
     t[0] = (t[0] + t[1]) + (t[2] + t[3]);
-    if (t[0] > 32.f) r.exact += exact_terms<DT>(v0, v1, zref, c, tab);     // rare: logits well above the sample that gave the reference
+    if (t[0] > 256.f) r.exact += exact_terms<DT>(v0, v1, zref, c, tab);    // rare: logits well above the sample that gave the reference
     else r.fast += (double)t[0];
     if (GREEDY) {
       const float m0 = Vec<DT>::vmax(v0), m1 = Vec<DT>::vmax(v1);
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_rows_kernel(VerifyArgs A) 
   in.next(v, neg_inf<DT>());
   const double c = log2e_over(kind == 0 ? 1.f : temp);
   const float cf = (float)c;
-  float zref = fmaxf(Vec<DT>::vmax(last), fmaxf(Vec<DT>::vmax2(v[0], v[1]), Vec<DT>::vmax2(v[2], v[3])));
+  float zref = fmaxf(Vec<DT>::vmax(last), Vec<DT>::vmax2(v[0], v[1]));
   zref = block_max_f(zref, (float*)sh);
   if (!(fabsf(zref) < 1e30f)) zref = 0.f;                   // (such a slice leaves the range below and is taken exactly)
   const float ref = zref * cf;
