@@ -454,15 +454,12 @@ def make_bwd_desc(advantages=None, lambda_distill=0.0, grad_out=1.0, n_valid=0, 
 
 def _on_device(ctx: Context, *tensors):
     """Addresses of the tensors (None stays None), all of which must be on the context's device."""
-    device, out = ctx.device, []
-    for t in tensors:
-        if t is None:
-            out.append(None)
-        elif t.get_device() == device:
-            out.append(t.data_ptr())
-        else:
-            raise JackpotError(f"tensor on {t.device}, but the context is on cuda:{device}")
-    return out
+    device = ctx.device
+    return [None if t is None else t.data_ptr() if t.get_device() == device else _wrong_device(t, device) for t in tensors]
+
+
+def _wrong_device(t, device):
+    raise JackpotError(f"tensor on {t.device}, but the context is on cuda:{device}")
 
 
 def _workspace_bytes(ctx: Context, fn, *sizes) -> int:

@@ -178,6 +178,10 @@ def _dense(t, shape, dtype, name):
         raise B.JackpotError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)}")
 
 
+def _like(x):
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
 def _norm_desc(x, weight, bias, eps, rms, out, name, dy=None):
     """Checks and fills what both passes share; ``out`` is y or dx."""
     d = B.jp_norm_desc(dtype=B._dtype_code(x), param_dtype=B._dtype_code(weight), flags=B.JP_NORM_RMS if rms else 0, eps=eps,
@@ -201,7 +205,7 @@ def _norm_desc(x, weight, bias, eps, rms, out, name, dy=None):
 def layer_norm(ctx: B.Context, x, weight, bias=None, *, eps=1e-6, rms=False, out=None):
     """One jp_layer_norm_forward call on torch's current stream: ``(y, mean, rstd)`` (mean None with ``rms``).
     ``out``: where y goes (may be ``x``)."""
-    y = x.new_empty(x.shape) if out is None else out
+    y = _like(x) if out is None else out
     d = _norm_desc(x, weight, bias, eps, rms, y, "out")
     mean = None if rms else x.new_empty(d.T, dtype=torch.float32)
     rstd = x.new_empty(d.T, dtype=torch.float32)
@@ -213,7 +217,7 @@ def layer_norm_backward(ctx: B.Context, dy, x, weight, mean, rstd, *, rms=False,
     """One jp_layer_norm_backward call on torch's current stream: ``(dx, dweight, dbias)`` with fp32 dweight and dbias
     (dbias None without ``bias``).  ``mean`` and ``rstd`` are the forward's; ``dx``: where dx goes (may be ``dy`` or ``x``)."""
     if dx is None:
-        dx = x.new_empty(x.shape)
+        dx = _like(x)
     d = _norm_desc(x, weight, None, 0.0, rms, dx, "dx", dy)
     T, H = x.shape
     if not rms:
@@ -334,12 +338,13 @@ def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_ac
         _dense(n_draft, (n_seq,), torch.int32, "n_draft")
     if temperature is not None:
         _dense(temperature, (n_seq,), torch.float32, "temperature")
-    new = u_sample.new_empty
-    out = dict(n_accepted=new(n_seq, dtype=torch.int32), tokens=new((n_seq, rows), dtype=torch.int32))
+    new, dev = u_sample.new_empty, u_sample.device           # (empty_strided: the cheapest call that makes a matrix)
+    out = dict(n_accepted=new(n_seq, dtype=torch.int32),
+               tokens=torch.empty_strided((n_seq, rows), (rows, 1), dtype=torch.int32, device=dev))
     if accept_prob:
         out["accept_prob"] = torch.empty_like(u_accept)
     if logp:
-        out["logp"] = new((n_seq, rows))
+        out["logp"] = torch.empty_strided((n_seq, rows), (rows, 1), dtype=torch.float32, device=dev)
     need = B.jp_verify_workspace_bytes(ctx, n_seq, N, V, d.dtype, draft_logits is not None and N > 0)
     ws = new(need, dtype=torch.uint8) if need else None
     B.jp_verify_draft(ctx, d, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept, u_sample,
