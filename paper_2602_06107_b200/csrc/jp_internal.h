@@ -263,7 +263,7 @@ struct NormArgs {
   const float* rstd;       // backward: [T]
   float* out_mean;         // forward: [T] or null
   float* out_rstd;         // forward: [T] or null
-  float* partial;          // backward: [groups, 2, H] workspace
+  float* partial;          // backward: [blocks, 1 or 2, H] workspace
   float* dweight;          // [H]
   float* dbias;            // [H] or null
 };

@@ -10,7 +10,7 @@
 // stays in the registers of one group of threads between its reduction and its output, so nothing is read
 // twice; the squares are taken of x - mu (a second reduction over registers) because E x^2 - mu^2 cancels.
 // Groups walk rows with the fixed stride of the grid, weight and bias in registers.  Where rows start on 16 bytes the next rows come
-// through asynchronous copies, each thread into places of its own (kStages rows ahead, no barriers); else the next row is in registers.
+// through asynchronous copies, each thread into places of its own (kStages rows ahead, no barriers); else the group copies together.
 // Each thread owns fixed columns, so dw and db add up in its registers over all rows of its group; the
 // groups' sums go to the workspace and a second kernel adds them in a fixed order: no atomics, the same bits
 // every time.
@@ -150,7 +150,6 @@ template <int DT, int W, int NV, int NT, int STAGES = kStages>
 struct Rows {
   using Ac = Access<DT, W>;
   static constexpr int ES = Vec<DT>::ESIZE;
-  static constexpr bool kAsync = W > 1;
   const char* next[NT];         // the next row to fetch, from this thread's first column on
   int64_t stride[NT];           // bytes from one row of the group to the next
   int64_t left;                 // rows not fetched yet
@@ -158,7 +157,6 @@ struct Rows {
   uint32_t write;
   int threads, in, out;
   bool have[NV];                // the access is within the row
-  typename Ac::raw ahead[kAsync ? 1 : NT][kAsync ? 1 : NV];
   __device__ __forceinline__ void fetch() {
     if (left > 0) {
 #pragma unroll
@@ -167,18 +165,14 @@ struct Rows {
         for (int i = 0; i < NV; ++i)
           if (have[i]) {
             const char* p = next[t] + (int64_t)i * (int)blockDim.x * W * ES;
-            if constexpr (kAsync)
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(write + ((in + t) * NV + i) * threads * 16), "l"(p) : "memory");
-            else ahead[t][i] = Ac::load(p);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(write + ((in + t) * NV + i) * threads * 16), "l"(p) : "memory");
           }
 #pragma unroll
       for (int t = 0; t < NT; ++t) next[t] += stride[t];
       --left;
     }
-    if constexpr (kAsync) {
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      in = in == (STAGES - 1) * NT ? 0 : in + NT;
-    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    in = in == (STAGES - 1) * NT ? 0 : in + NT;
   }
   // rows first, first + step, ... below T of the NT matrices
   __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T,
@@ -195,28 +189,99 @@ struct Rows {
     in = out = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) have[i] = column<W>(i) < H;
-    if constexpr (kAsync) {
 #pragma unroll
-      for (int s = 0; s < STAGES; ++s) fetch();
-    } else {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) ahead[t][i] = Ac::zero();
-      fetch();
-    }
+    for (int s = 0; s < STAGES; ++s) fetch();
   }
   // the oldest row; columns past the end read 0
   __device__ __forceinline__ void take(typename Ac::raw (&v)[NT][NV]) {
-    if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if constexpr (kAsync) v[t][i] = have[i] ? read[((out + t) * NV + i) * threads] : Ac::zero();
-        else v[t][i] = ahead[t][i];
+      for (int i = 0; i < NV; ++i) v[t][i] = have[i] ? read[((out + t) * NV + i) * threads] : Ac::zero();
+    out = out == (STAGES - 1) * NT ? 0 : out + NT;
+  }
+};
+
+// The same for rows that start anywhere: the group copies the 16-byte vectors that cover a row (a row's place begins at the row's own
+// offset to 16 bytes), and every thread reads its elements once all have arrived.  Vectors that reach beyond the matrix, in its first
+// and last row, are copied element by element.  The place is free again after the barrier of the row's first sum.  (With element loads
+// into registers, one row ahead, 8192 x 4095 bf16 took 147 us forward and 225 us backward; this 70 and 93.)
+__host__ __device__ inline int span_bytes(int64_t H, int es) { return (int)((H * es + 15) / 16 + 1) * 16; }
+template <int DT, int NV, int NT, int STAGES>
+struct Rows<DT, 1, NV, NT, STAGES> {
+  static constexpr int ES = Vec<DT>::ESIZE;
+  const char* next[NT];         // the next row to fetch
+  const char* taken[NT];        // the next row to take
+  const char* lo[NT];
+  const char* hi[NT];           // the matrix
+  int64_t stride[NT], left;
+  char* place;                  // [STAGES][NT][span]
+  int span, bytes, in, out;
+  bool have[NV];
+  __device__ __forceinline__ void fetch() {
+    if (left > 0) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const char* const p = next[t];
+        const int head = (int)((uintptr_t)p & 15);
+        const char* from = p - head + threadIdx.x * 16;
+        char* to = place + (in + t) * span + threadIdx.x * 16;
+        for (int i = threadIdx.x * 16; i < head + bytes; i += blockDim.x * 16, from += blockDim.x * 16, to += blockDim.x * 16) {
+          if (from >= lo[t] && from + 16 <= hi[t]) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+          } else {
+            for (int q = 0; q < 16; q += ES)
+              if (from + q >= p && from + q < p + bytes) {
+                if constexpr (ES == 2) *(uint16_t*)(to + q) = *(const volatile uint16_t*)(from + q);
+                else *(uint32_t*)(to + q) = *(const volatile uint32_t*)(from + q);
+              }
+          }
+        }
+        next[t] += stride[t];
       }
-    if constexpr (kAsync) out = out == (STAGES - 1) * NT ? 0 : out + NT;
+      --left;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    in = in == (STAGES - 1) * NT ? 0 : in + NT;
+  }
+  __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T,
+                                        int64_t H, uint4* smem) {
+    bytes = (int)H * ES;
+    span = span_bytes(H, ES);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      lo[t] = (const char*)base[t];
+      hi[t] = lo[t] + ((T - 1) * ld[t] + H) * ES;
+      next[t] = taken[t] = lo[t] + first * ld[t] * ES;
+      stride[t] = step * ld[t] * ES;
+    }
+    left = first < T ? (T - first + step - 1) / step : 0;
+    place = (char*)smem + threadIdx.y * STAGES * NT * span;
+    in = out = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) have[i] = column<1>(i) < H;
+#pragma unroll 1
+    for (int s = 0; s < STAGES; ++s) fetch();
+  }
+  __device__ __forceinline__ void take(uint32_t (&v)[NT][NV]) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+    if (blockDim.x == 32) __syncwarp();
+    else __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const char* row = place + (out + t) * span + ((uintptr_t)taken[t] & 15);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        v[t][i] = 0u;
+        if (have[i]) {
+          if constexpr (ES == 2) v[t][i] = (uint32_t)((const uint16_t*)row)[threadIdx.x + i * blockDim.x] << 16;
+          else v[t][i] = ((const uint32_t*)row)[threadIdx.x + i * blockDim.x];
+        }
+      }
+      taken[t] += stride[t];
+    }
+    out = out == (STAGES - 1) * NT ? 0 : out + NT;
   }
 };
 
@@ -246,7 +311,7 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
     in.take(raw);
 #pragma unroll
     for (int i = 0; i < NV; ++i) Ac::unpack(raw[0][i], v[i]);
-    in.fetch();
+    if (W > 1) in.fetch();
     float mean = 0.f;
     if (!A.rms) {
       float s = 0.f;
@@ -268,6 +333,10 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
       }
     }
     const float rstd = 1.f / sqrtf(group_sum(s2, 0.f, sh, slot).x * inv_h + A.eps);
+    if (W == 1) {
+      __syncwarp();                                         // (every thread of the group has read the row)
+      in.fetch();
+    }
     if (threadIdx.x == 0) {
       if (A.out_mean) A.out_mean[row] = mean;
       if (A.out_rstd) A.out_rstd[row] = rstd;
@@ -286,14 +355,16 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
   }
 }
 
-// One warp a row, NVL vectors a lane, for many rows of up to 4096 bf16 or 2048 fp32: the reductions are shuffles and no row waits for
-// another (a block of 256 threads a row, with a barrier for each of its two sums, took 48 us at 8192 x 4096 with bias in bf16; this takes 30).  Weight and
-// bias are in shared memory beside the rows to come.
-constexpr int kWarpRows = 12;                 // rows a block
+// One warp a row, NVL vectors a lane, for many rows of up to 5120 bf16 or 2560 fp32: the reductions are shuffles and no row waits for
+// another (a block a row, with a barrier for each of its two sums, took 48 us at 8192 x 4096 with bias in bf16 and 52 at 6553 x 5120; this
+// takes 30 and 36).  Weight and bias are in shared memory beside the rows to come; wider rows leave too few warps an SM (at 4096 x 8192,
+// five of them, RMS norm, 42 us; a block a row 40).
 constexpr int kWarpStages = 2;
-constexpr int warp_blocks(int nvl) { return nvl == 16 ? 1 : nvl == 8 ? 2 : 3; }      // per SM
+__host__ __device__ constexpr int warp_rows(int nvl) { return nvl == 20 ? 9 : 12; }   // rows a block
+__host__ __device__ constexpr int warp_blocks(int nvl) { return nvl >= 16 ? 1 : nvl == 8 ? 2 : 3; }      // per SM
 template <int DT, int NVL, bool PB>
-__global__ void __launch_bounds__(32 * kWarpRows, warp_blocks(NVL)) norm_fwd_warp_kernel(NormArgs A) {
+__global__ void __launch_bounds__(32 * warp_rows(NVL), warp_blocks(NVL)) norm_fwd_warp_kernel(NormArgs A) {
+  constexpr int kWarpRows = warp_rows(NVL);
   constexpr int W = Vec<DT>::N, ES = Vec<DT>::ESIZE, PS = PB ? 2 : 4;
   using Ac = Access<DT, W>;
   extern __shared__ uint4 places[];
@@ -468,7 +539,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
     }
   const int64_t group = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  Rows<DT, W, NV, 2, 2 * R> in;
+  Rows<DT, W, NV, 2, W == 1 ? kStages : 2 * R> in;
   in.start({A.x, A.dy}, {A.ld_x, A.ld_dy}, group, step, A.T, A.H, places);
   float w[NV][W];
   {
@@ -503,7 +574,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) raw[r][0][i] = raw[r][1][i] = Ac::zero();
       }
-      in.fetch();
+      if (W > 1) in.fetch();
     }
     fetch_stats(row + R * step);
 #pragma unroll
@@ -528,6 +599,10 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
       s[2 * r + 1] = s2;
     }
     group_sums<2 * R>(s, sh, slot);
+    if (W == 1) {
+      __syncwarp();                                         // (every thread of the group has read the rows)
+      in.fetch();
+    }
     // (unpacked again below instead of being kept over the sums: as fp32 a row takes twice the registers)
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -557,7 +632,32 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
     }
   }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the kernel that adds the lines may set up
-  float* pw = A.partial + group * (BIAS ? 2 : 1) * A.H;
+  constexpr int kPer = BIAS ? 2 : 1;
+  if (blockDim.y > 1) {     // short rows: the block's groups are added first, in their order (30000 x 63 bf16: 29 -> 18 us)
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    float* all = (float*)places;                            // [groups][kPer][H]: less than the rows took
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t c = column<W>(i);
+      if (c < A.H) {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          all[threadIdx.y * kPer * A.H + c + e] = dw[i][e];
+          if (BIAS) all[(threadIdx.y * kPer + 1) * A.H + c + e] = db[i][e];
+        }
+      }
+    }
+    __syncthreads();
+    float* line = A.partial + (int64_t)blockIdx.x * kPer * A.H;
+    for (int c = threadIdx.y * 32 + threadIdx.x; c < kPer * (int)A.H; c += 32 * blockDim.y) {
+      float t = all[c];
+      for (int y = 1; y < blockDim.y; ++y) t += all[y * kPer * (int)A.H + c];
+      line[c] = t;
+    }
+    return;
+  }
+  float* pw = A.partial + group * kPer * A.H;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int64_t c = column<W>(i);
@@ -644,14 +744,14 @@ bool vector_rows(const NormArgs& a, bool backward) {
 }
 
 // Threads and registers of a row.  16-byte accesses where rows start on 16 bytes, else single elements; 1, 2 or 4 vectors
-// (8 or 16 elements) a thread so that rows up to 16384 bf16 (8192 fp32, or 8192 unaligned) stay in registers; the sums of a backward
+// (2, 8 or 16 elements) a thread so that rows up to 16384 bf16 (8192 fp32, or 8192 unaligned) stay in registers; the sums of a backward
 // pass take as much again, so 8192 there.
 Plan plan_for(int64_t H, int dtype, bool vec, bool backward) {
   Plan p{};
   p.w = vec ? (dtype == JP_BF16 ? 8 : 4) : 1;
   const int64_t n = (H + p.w - 1) / p.w;
   if (vec) p.nv = n <= 256 ? 1 : n <= 1024 ? 2 : n <= (backward ? 8192 / p.w : 2048) ? 4 : 0;
-  else p.nv = n <= 2048 ? 8 : n <= 8192 ? 16 : 0;
+  else p.nv = n <= 64 ? 2 : n <= 2048 ? 8 : n <= 8192 ? 16 : 0;
   if (p.nv == 0) { p.threads = 1024; p.rows = 1; p.w = 1; return p; }
   const int64_t per = (n + p.nv - 1) / p.nv;
   p.threads = (int)((per + 31) / 32 * 32);
@@ -659,10 +759,11 @@ Plan plan_for(int64_t H, int dtype, bool vec, bool backward) {
   return p;
 }
 
-// Blocks: all rows at once where there are few, else what the SMs hold (a backward pass: 128 registers a thread).
+// Blocks: all rows at once where there are few, else what the registers of an SM hold: 512 threads of a backward pass and of 16 elements
+// a thread, 768 of 8 single elements, 1024 of the rest.
 int grid_for(int64_t T, const Plan& p, int sms, bool backward) {
   const int64_t need = (T + p.rows - 1) / p.rows;
-  const int per_sm = (backward ? 512 : 1024) / (p.threads * p.rows);
+  const int per_sm = (p.w == 1 && p.nv == 2 ? 1024 : backward || p.nv == 16 ? 512 : p.w == 1 ? 768 : 1024) / (p.threads * p.rows);
   const int64_t cap = (int64_t)sms * (per_sm > 8 ? 8 : per_sm < 1 ? 1 : per_sm);
   return (int)(need < cap ? need : cap);
 }
@@ -688,6 +789,7 @@ cudaError_t launch(K* kernel, const NormArgs& a, dim3 grid, dim3 block, int smem
 
 template <int DT, bool PB, int NVL>
 cudaError_t fwd_warp(const NormArgs& a, cudaStream_t s, int sms) {
+  constexpr int kWarpRows = warp_rows(NVL);
   const int64_t need = (a.T + kWarpRows - 1) / kWarpRows, cap = (int64_t)sms * warp_blocks(NVL);
   const int smem = kWarpStages * NVL * 32 * kWarpRows * 16 + (int)a.H * (PB ? 2 : 4) * (a.bias ? 2 : 1);
   return launch(norm_fwd_warp_kernel<DT, NVL, PB>, a, dim3((unsigned)(need < cap ? need : cap)), dim3(32, kWarpRows), smem, s);
@@ -698,17 +800,19 @@ cudaError_t fwd(const NormArgs& a, cudaStream_t s, int sms) {
   constexpr int VW = Vec<DT>::N;
   const bool vec = vector_rows(a, false);
   // a warp a row where every SM gets its blocks full of rows; with fewer rows a block a row is done sooner
-  if (vec && a.T >= (int64_t)sms * kWarpRows && a.H > 64 * VW && a.H <= 512 * VW) {
+  if (vec && a.T >= (int64_t)sms * 12 && a.H > 64 * VW && a.H <= 640 * VW) {
     if (a.H <= 128 * VW) return fwd_warp<DT, PB, 4>(a, s, sms);
     if (a.H <= 256 * VW) return fwd_warp<DT, PB, 8>(a, s, sms);
-    return fwd_warp<DT, PB, 16>(a, s, sms);
+    if (a.H <= 512 * VW) return fwd_warp<DT, PB, 16>(a, s, sms);
+    return fwd_warp<DT, PB, 20>(a, s, sms);
   }
   const Plan p = plan_for(a.H, a.dtype, vec, false);
   const int grid = grid_for(a.T, p, sms, false);
   const dim3 b(p.threads, p.rows);
-  const int smem = p.w > 1 ? kStages * p.nv * p.threads * p.rows * 16 : 0;
+  const int smem = kStages * p.rows * (p.w > 1 ? p.nv * p.threads * 16 : span_bytes(a.H, Vec<DT>::ESIZE));
   if (p.nv == 0) { norm_fwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
-  if (p.w == 1) return p.nv == 8 ? launch(norm_fwd_kernel<DT, 1, 8, PB>, a, grid, b, smem, s) : launch(norm_fwd_kernel<DT, 1, 16, PB>, a, grid, b, smem, s);
+  if (p.w == 1)
+    return p.nv == 2 ? launch(norm_fwd_kernel<DT, 1, 2, PB>, a, grid, b, smem, s) : p.nv == 8 ? launch(norm_fwd_kernel<DT, 1, 8, PB>, a, grid, b, smem, s) : launch(norm_fwd_kernel<DT, 1, 16, PB>, a, grid, b, smem, s);
   if (p.nv == 1) return launch(norm_fwd_kernel<DT, VW, 1, PB>, a, grid, b, smem, s);
   if (p.nv == 2) return launch(norm_fwd_kernel<DT, VW, 2, PB>, a, grid, b, smem, s);
   return launch(norm_fwd_kernel<DT, VW, 4, PB>, a, grid, b, smem, s);
@@ -718,9 +822,10 @@ template <int DT, bool PB, bool BIAS>
 cudaError_t bwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
   constexpr int VW = Vec<DT>::N;
   const dim3 b(p.threads, p.rows);
-  const int smem = p.w > 1 ? 2 * (2 * bwd_rows(p.w, p.nv)) * p.nv * p.threads * p.rows * 16 : 0;
+  const int smem = 2 * p.rows * (p.w > 1 ? 2 * bwd_rows(p.w, p.nv) * p.nv * p.threads * 16 : kStages * span_bytes(a.H, Vec<DT>::ESIZE));
   if (p.nv == 0) { norm_bwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
-  if (p.w == 1) return p.nv == 8 ? launch(norm_bwd_kernel<DT, 1, 8, PB, BIAS>, a, grid, b, smem, s) : launch(norm_bwd_kernel<DT, 1, 16, PB, BIAS>, a, grid, b, smem, s);
+  if (p.w == 1)
+    return p.nv == 2 ? launch(norm_bwd_kernel<DT, 1, 2, PB, BIAS>, a, grid, b, smem, s) : p.nv == 8 ? launch(norm_bwd_kernel<DT, 1, 8, PB, BIAS>, a, grid, b, smem, s) : launch(norm_bwd_kernel<DT, 1, 16, PB, BIAS>, a, grid, b, smem, s);
   if (p.nv == 1) return launch(norm_bwd_kernel<DT, VW, 1, PB, BIAS>, a, grid, b, smem, s);
   if (p.nv == 2) return launch(norm_bwd_kernel<DT, VW, 2, PB, BIAS>, a, grid, b, smem, s);
   if constexpr (DT == JP_F32) return launch(norm_bwd_kernel<DT, VW, 4, PB, BIAS>, a, grid, b, smem, s);
@@ -739,7 +844,7 @@ int64_t norm_backward_groups(int64_t T, int64_t H, int dtype, int sms) {
   int64_t most = 0;
   for (int vec = 0; vec < 2; ++vec) {
     const Plan p = plan_for(H, dtype, vec != 0, true);
-    const int64_t g = (int64_t)grid_for(T, p, sms, true) * p.rows;
+    const int64_t g = grid_for(T, p, sms, true);
     most = g > most ? g : most;
   }
   return most;
@@ -762,7 +867,7 @@ cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s, int sms) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, norm_sum_kernel, (const float*)a.partial, (int64_t)grid * p.rows, a.H, a.dbias ? 2 : 1, a.dweight, a.dbias);
+  return cudaLaunchKernelEx(&cfg, norm_sum_kernel, (const float*)a.partial, (int64_t)grid, a.H, a.dbias ? 2 : 1, a.dweight, a.dbias);
 }
 
 }  // namespace jp

@@ -1,11 +1,13 @@
 """Layer norm and RMS norm (jp_layer_norm_forward, jp_layer_norm_backward) against a plain implementation in 64 bits.
 
-Bars.  u = 2^-24.  A sum over a row adds at most 16 terms a thread, then 10 levels of a tree, so mean and mean square
-are within 32 u of the sums of magnitudes; the handful of operations on each element adds a few u more.  64 u times the
+Bars.  u = 2^-24.  A sum over a row adds at most 160 squares in a lane (20 vectors; the sums of x themselves are a tree
+of 3 levels, then 20 terms), then a tree of at most 10 levels.  An addition errs by u of the sum so far, which grows from
+0 to the whole for terms of one distribution, so 160 of them make 80 u and rstd, which takes half of it, 40 u; mean is
+within 32 u of the sum of magnitudes.  The handful of operations on each element adds a few u more.  64 u times the
 magnitudes that enter an output (not the output itself, which may cancel) bounds the fp32 arithmetic; the rounding of
 the output adds half a step of its type, 2^-8 relative for bf16.  rstd of the backward is an input there.  The sums over
-rows add ceil(T / groups) rows in a register, then groups / 8 lines, then 8: below 100 terms in a row for the sizes here,
-so 128 u times the sum of magnitudes.  Rows wider than what registers hold add H / 1024 terms a thread instead of 16."""
+rows add ceil(T / groups) rows in a register, then 8 groups of a block, then every 32nd line, then a tree of 5 levels:
+below 100 terms in a row for the sizes here, so 128 u times the sum of magnitudes.  Rows wider than what registers hold add H / 1024 terms a thread instead of 16."""
 import pytest
 import torch
 
@@ -96,11 +98,13 @@ def test_both_passes_match_the_formula(ctx, T, H, dtype, rms, bias):
     check_backward(got, dy, x, w, mean, rstd, rms)
 
 
-@pytest.mark.parametrize("T,H", [(1776, 520), (2001, 1024), (1999, 1288), (1777, 2048), (3600, 4096), (1800, 4088)])
+@pytest.mark.parametrize("T,H", [(1776, 520), (2001, 1024), (1999, 1288), (1777, 2048), (3600, 4096), (1800, 4088), (1790, 8192), (1900, 6152),
+                                 (30011, 63), (2500, 4095)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("rms,bias,param", [(False, True, torch.float32), (True, False, torch.bfloat16)])
 def test_many_rows(ctx, T, H, dtype, rms, bias, param):
-    """Rows enough to fill every SM several times over.  A register adds at most 26 rows, a sum of lines at most 64 in a row."""
+    """Rows enough to fill every SM several times over.  A register adds at most 26 rows, a sum of lines at most
+    19 (592 blocks, every 32nd)."""
     x, dy, w, b = make(T, H, dtype, param, bias, seed=T + H, ld=H + (H % 16))
     y, mean, rstd = runner.layer_norm(ctx, x, w, b, eps=EPS, rms=rms)
     check_forward(y, mean, rstd, x, w, b, rms)
