@@ -53,7 +53,8 @@ __device__ __forceinline__ void mma_bf16_first(float (&d)[4], const uint32_t (&a
 
 // Bits 0 .. 7 of a bf16 are the number bits 2^-133, over the subnormals and the first normal binade alike.  So a nibble that is
 // masked out in place, at bits 0 or 4 of each half, is q 2^-133 or q 2^-129, and one fused multiply-add by 2^127 with -z / 64 or
-// -z / 4 makes it (q - z) / 64 or / 4, exactly: no shift, no exponent to set.  (The scale takes the 64 or the 4 back.)
+// -z / 4 makes it (q - z) / 64 or / 4, exactly: no shift, no exponent to set.  (The
+// finished sum takes the 64 or the 4 back: a large scale would leave fp32 by it.)
 constexpr uint32_t k2To127 = 0x7f007f00u, kMinus2To127 = 0xff00ff00u;
 __device__ __forceinline__ uint32_t scaled2(uint32_t bits, uint32_t minus_z) {
   uint32_t d;
@@ -80,8 +81,9 @@ __device__ __forceinline__ void store_tile(const W4Args& A, const float (&acc)[N
       const int64_t row = n + (e >> 1) * 8;
       const int m = t * 8 + (lane & 3) * 2 + (e & 1);
       if (m < A.M && row < A.N) {
-        if (A.out_bf16) ((__nv_bfloat16*)A.out)[m * A.ld_out + row] = __float2bfloat16_rn(acc[t][e]);
-        else ((float*)A.out)[m * A.ld_out + row] = acc[t][e];
+        const float sum = acc[t][e] * (e < 2 ? 64.f : 4.f);
+        if (A.out_bf16) ((__nv_bfloat16*)A.out)[m * A.ld_out + row] = __float2bfloat16_rn(sum);
+        else ((float*)A.out)[m * A.ld_out + row] = sum;
       }
     }
 }
@@ -206,7 +208,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
             else mma_bf16(part[t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
           }
           if ((step + 1) % (8 / GROUPS) == 0) {
-            const float s0 = __uint_as_float(sw[0][grp] & ~15u) * 64.f, s1 = __uint_as_float(sw[1][grp] & ~15u) * 4.f;
+            const float s0 = __uint_as_float(sw[0][grp] & ~15u), s1 = __uint_as_float(sw[1][grp] & ~15u);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
               acc[t][0] = fmaf(part[t][0], s0, acc[t][0]);

@@ -216,3 +216,16 @@ def test_quantised_weights_are_within_half_a_step(K, group, symmetric):
     # rounded zero point of an uneven range by another half
     assert ((back - w.double()).abs() <= step * (0.5 + 15 / 256 + (0 if symmetric else 0.5)) + 1e-12).all()
     assert (back[2] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("power,x_power", [(124, -20), (-120, 0)])
+def test_scales_near_the_ends_of_bf16(ctx, power, x_power):
+    """Weights up to 8 x 2^125 with small x, and down to 2^-121: neither the sums nor the scaled parts leave fp32.  (What a
+    subnormal part loses is 2^-150 a group, far below the bar of 48 x 2^-24 of sums near 2^-112.)"""
+    N, K, group = 70, 600, 32
+    q, s, z = make(N, K, group, True, torch.bfloat16, seed=12)
+    s = (s.double().sign() * (1 + s.double().abs()) * 2.0 ** power).to(torch.bfloat16)
+    w = runner.pack_w4(ctx, q, s, z, K=K, group=group)
+    x = (tokens(6, K, seed=3).float() * 2.0 ** x_power).to(torch.bfloat16)
+    check(runner.linear_w4(ctx, x, w, out_dtype=torch.float32), x, unpacked(q, s, z, K, group), group)
