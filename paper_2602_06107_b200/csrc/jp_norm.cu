@@ -9,11 +9,14 @@
 // Both passes are bound by HBM: forward reads x and writes y, backward reads x and dy and writes dx.  A row
 // stays in the registers of one group of threads between its reduction and its output, so nothing is read
 // twice; the squares are taken of x - mu (a second reduction over registers) because E x^2 - mu^2 cancels.
-// Groups walk rows with the fixed stride of the grid, weight and bias in registers.  Where rows start on 16 bytes the next rows come
-// through asynchronous copies, each thread into places of its own (kStages rows ahead, no barriers); else the group copies together.
+// Groups walk rows with the fixed stride of the grid, weight and bias in registers.  The next rows come through asynchronous copies, each
+// thread into places of its own (kStages rows ahead, no barriers); what lies before and behind a row's aligned vectors is one element a
+// thread (Span).  Where x and y (or x, dy and dx) differ in their offsets to 16 bytes the group copies together (Rows of width 1).
 // Each thread owns fixed columns, so dw and db add up in its registers over all rows of its group; the
 // groups' sums go to the workspace and a second kernel adds them in a fixed order: no atomics, the same bits
 // every time.
+#include <type_traits>
+
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -101,6 +104,28 @@ __device__ __forceinline__ float2 group_sum(float a, float b, float2 (*sh)[kMaxW
 // Columns of this thread: access i covers columns (threadIdx.x + i * blockDim.x) * W and the next W - 1.
 template <int W> __device__ __forceinline__ int64_t column(int i) { return (int64_t)(threadIdx.x + i * (int)blockDim.x) * W; }
 
+// A row that does not start on 16 bytes: the elements before the first boundary, the vectors between, and the elements behind the last
+// boundary.  The vectors are dealt out like those of an aligned row, and the edges (below two vectors) one a thread, so that nothing of
+// a neighbouring row is read or masked.  A group's rows are a multiple of the period apart after which starts repeat: threads keep their
+// columns.
+struct Span {
+  int head, tail;
+  int64_t body;                 // elements of each
+  int64_t edge;                 // this thread's column of the edges, or -1
+};
+template <int W> __device__ __forceinline__ Span span_of(bool off, const void* base, int64_t row, int64_t ld, int es, int64_t H) {
+  Span s{0, 0, H, -1};
+  if (off) {
+    const int64_t first = (int64_t)((16 - ((uintptr_t)base + (uintptr_t)(row * ld * es))) & 15) / es;
+    s.head = (int)(first < H ? first : H);
+    s.tail = (int)(H - s.head) % W;
+    s.body = H - s.head - s.tail;
+    const int t = threadIdx.x;
+    s.edge = t < s.head ? t : t >= W && t - W < s.tail ? s.head + s.body + (t - W) : -1;
+  }
+  return s;
+}
+
 // Weight or bias at the thread's columns, loaded once: bf16 pairs as they are, the rest as fp32.
 template <int W, int NV, bool BF16>
 struct Params {
@@ -122,6 +147,20 @@ struct Params {
         }
       }
     }
+  }
+  __device__ __forceinline__ void load(const void* p, const Span& sp) {      // of a span's vectors
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (p && column<W>(i) < sp.body) {
+        const int64_t c = sp.head + column<W>(i);
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          if constexpr (BF16) r[(i * W + e) / 2] |= (uint32_t)((const uint16_t*)p)[c + e] << (16 * (e & 1));
+          else r[i * W + e] = ((const uint32_t*)p)[c + e];
+        }
+      }
   }
   __device__ __forceinline__ void read(const char* p) {     // (NV == 1) W consecutive ones
 #pragma unroll
@@ -146,7 +185,7 @@ struct Params {
 
 // The group's rows of NT matrices one after the other: row `first`, then every `step`-th.
 constexpr int kStages = 3;
-template <int DT, int W, int NV, int NT, int STAGES = kStages>
+template <int DT, int W, int NV, int NT, bool OFF = false, int STAGES = kStages>
 struct Rows {
   using Ac = Access<DT, W>;
   static constexpr int ES = Vec<DT>::ESIZE;
@@ -157,6 +196,20 @@ struct Rows {
   uint32_t write;
   int threads, in, out;
   bool have[NV];                // the access is within the row
+  // (OFF) the thread's element of the edges: of the next two rows, loaded two rows ahead
+  const char* edge[NT];
+  int64_t edges_left;
+  uint32_t edge0[NT], edge1[NT];
+  __device__ __forceinline__ void next_edge() {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      edge0[t] = edge1[t];
+      edge1[t] = 0u;
+      if (edges_left > 0) edge1[t] = Access<DT, 1>::load(edge[t]);
+      edge[t] += stride[t];
+    }
+    --edges_left;
+  }
   __device__ __forceinline__ void fetch() {
     if (left > 0) {
 #pragma unroll
@@ -176,10 +229,11 @@ struct Rows {
   }
   // rows first, first + step, ... below T of the NT matrices
   __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T,
-                                        int64_t H, uint4* smem) {
+                                        const Span& sp, uint4* smem) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      next[t] = (const char*)base[t] + (first * ld[t] + (int64_t)threadIdx.x * W) * ES;
+      next[t] = (const char*)base[t] + (first * ld[t] + sp.head + (int64_t)threadIdx.x * W) * ES;
+      if (OFF) edge[t] = (const char*)base[t] + (first * ld[t] + sp.edge) * ES;
       stride[t] = step * ld[t] * ES;
     }
     left = first < T ? (T - first + step - 1) / step : 0;
@@ -188,12 +242,22 @@ struct Rows {
     write = (uint32_t)__cvta_generic_to_shared(read);
     in = out = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) have[i] = column<W>(i) < H;
+    for (int i = 0; i < NV; ++i) have[i] = column<W>(i) < sp.body;
 #pragma unroll
     for (int s = 0; s < STAGES; ++s) fetch();
+    if (OFF) {
+      edges_left = sp.edge >= 0 && first < T ? (T - first + step - 1) / step : 0;
+      next_edge();
+      next_edge();
+    }
   }
   // the oldest row; columns past the end read 0
-  __device__ __forceinline__ void take(typename Ac::raw (&v)[NT][NV]) {
+  __device__ __forceinline__ void take(typename Ac::raw (&v)[NT][NV], float (&ve)[NT]) {
+    if (OFF) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) ve[t] = __uint_as_float(edge0[t]);
+      next_edge();
+    }
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -203,13 +267,14 @@ struct Rows {
   }
 };
 
-// The same for rows that start anywhere: the group copies the 16-byte vectors that cover a row (a row's place begins at the row's own
+// The same for matrices whose rows start at different offsets to 16 bytes: the group copies the 16-byte vectors that cover a row (a row's place begins at the row's own
 // offset to 16 bytes), and every thread reads its elements once all have arrived.  Vectors that reach beyond the matrix, in its first
 // and last row, are copied element by element.  The place is free again after the barrier of the row's first sum.  (With element loads
-// into registers, one row ahead, 8192 x 4095 bf16 took 147 us forward and 225 us backward; this 70 and 93.)
+// into registers, one row ahead, 8192 x 4095 bf16 took 147 us forward and 225 us backward; this 70 and 93, rows of one offset as spans
+// 34 and 69.)
 __host__ __device__ inline int span_bytes(int64_t H, int es) { return (int)((H * es + 15) / 16 + 1) * 16; }
 template <int DT, int NV, int NT, int STAGES>
-struct Rows<DT, 1, NV, NT, STAGES> {
+struct Rows<DT, 1, NV, NT, false, STAGES> {
   static constexpr int ES = Vec<DT>::ESIZE;
   const char* next[NT];         // the next row to fetch
   const char* taken[NT];        // the next row to take
@@ -246,7 +311,8 @@ struct Rows<DT, 1, NV, NT, STAGES> {
     in = in == (STAGES - 1) * NT ? 0 : in + NT;
   }
   __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T,
-                                        int64_t H, uint4* smem) {
+                                        const Span& sp, uint4* smem) {
+    const int64_t H = sp.body;
     bytes = (int)H * ES;
     span = span_bytes(H, ES);
 #pragma unroll
@@ -264,7 +330,7 @@ struct Rows<DT, 1, NV, NT, STAGES> {
 #pragma unroll 1
     for (int s = 0; s < STAGES; ++s) fetch();
   }
-  __device__ __forceinline__ void take(uint32_t (&v)[NT][NV]) {
+  __device__ __forceinline__ void take(uint32_t (&v)[NT][NV], float (&)[NT]) {
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
     if (blockDim.x == 32) __syncwarp();
     else __syncthreads();
@@ -288,7 +354,7 @@ struct Rows<DT, 1, NV, NT, STAGES> {
 // Threads and blocks an SM holds of the kernels below
 constexpr int group_threads(int w, int nv) { return (w == 1 ? nv > 8 : nv > 1) ? 512 : 256; }
 
-template <int DT, int W, int NV, bool PB>
+template <int DT, int W, int NV, bool PB, bool OFF>
 __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs A) {
   using Ac = Access<DT, W>;
   constexpr int ES = Vec<DT>::ESIZE;
@@ -300,15 +366,27 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
   const float inv_h = 1.f / (float)A.H;
   int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  Rows<DT, W, NV, 1> in;
-  in.start({A.x}, {A.ld_x}, row, step, A.T, A.H, places);
+  const Span span = span_of<W>(OFF, A.x, row, A.ld_x, ES, A.H);
+  Rows<DT, W, NV, 1, OFF> in;
+  in.start({A.x}, {A.ld_x}, row, step, A.T, span, places);
   Params<W, NV, PB> w, b;
-  w.load(A.weight, A.H);
-  b.load(A.bias, A.H);
+  float we = 0.f, be = 0.f;     // of the edge
+  if constexpr (OFF) {
+    w.load(A.weight, span);
+    b.load(A.bias, span);
+    if (span.edge >= 0) {
+      we = load_elem(A.weight, span.edge, PB);
+      if (A.bias) be = load_elem(A.bias, span.edge, PB);
+    }
+  } else {
+    w.load(A.weight, A.H);
+    b.load(A.bias, A.H);
+  }
   for (; row < A.T; row += step) {
     float v[NV][W];
     typename Ac::raw raw[1][NV];
-    in.take(raw);
+    float ve[1] = {0.f};
+    in.take(raw, ve);
 #pragma unroll
     for (int i = 0; i < NV; ++i) Ac::unpack(raw[0][i], v[i]);
     if (W > 1) in.fetch();
@@ -319,18 +397,23 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
       for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < W; ++e) s += v[i][e];
+      if (OFF) s += ve[0];
       mean = group_sum(s, 0.f, sh, slot).x * inv_h;
     }
     float s2 = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (column<W>(i) < A.H) {
+      if (column<W>(i) < span.body) {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
           v[i][e] -= mean;
           s2 = fmaf(v[i][e], v[i][e], s2);
         }
       }
+    }
+    if (OFF && span.edge >= 0) {
+      ve[0] -= mean;
+      s2 = fmaf(ve[0], ve[0], s2);
     }
     const float rstd = 1.f / sqrtf(group_sum(s2, 0.f, sh, slot).x * inv_h + A.eps);
     if (W == 1) {
@@ -341,11 +424,15 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
       if (A.out_mean) A.out_mean[row] = mean;
       if (A.out_rstd) A.out_rstd[row] = rstd;
     }
-    char* y = (char*)A.y + row * A.ld_y * ES;
+    if (OFF && span.edge >= 0) {
+      const float o = fmaf(ve[0] * rstd, we, be);
+      Access<DT, 1>::store((char*)A.y + (row * A.ld_y + span.edge) * ES, &o);
+    }
+    char* y = (char*)A.y + (row * A.ld_y + span.head) * ES;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int64_t c = column<W>(i);
-      if (c < A.H) {
+      if (c < span.body) {
         float o[W];
 #pragma unroll
         for (int e = 0; e < W; ++e) o[e] = fmaf(v[i][e] * rstd, w.get(i, e), b.get(i, e));
@@ -362,7 +449,8 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
 constexpr int kWarpStages = 2;
 __host__ __device__ constexpr int warp_rows(int nvl) { return nvl == 20 ? 9 : 12; }   // rows a block
 __host__ __device__ constexpr int warp_blocks(int nvl) { return nvl >= 16 ? 1 : nvl == 8 ? 2 : 3; }      // per SM
-template <int DT, int NVL, bool PB>
+__host__ __device__ inline int param_bytes(int64_t H, int ps) { return ((int)H * ps + 15) / 16 * 16; }      // of one of them
+template <int DT, int NVL, bool PB, bool OFF>
 __global__ void __launch_bounds__(32 * warp_rows(NVL), warp_blocks(NVL)) norm_fwd_warp_kernel(NormArgs A) {
   constexpr int kWarpRows = warp_rows(NVL);
   constexpr int W = Vec<DT>::N, ES = Vec<DT>::ESIZE, PS = PB ? 2 : 4;
@@ -370,24 +458,41 @@ __global__ void __launch_bounds__(32 * warp_rows(NVL), warp_blocks(NVL)) norm_fw
   extern __shared__ uint4 places[];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int lane = threadIdx.x, H = (int)A.H;
+  const int lane = threadIdx.x;
   const float inv_h = 1.f / (float)A.H;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  Rows<DT, W, NVL, 1, kWarpStages> in;
-  in.start({A.x}, {A.ld_x}, row, step, A.T, A.H, places);
-  const int n = H * PS / 16, tid = threadIdx.y * 32 + lane;
+  // (OFF: the rows of a block are the grid apart, which is a multiple of the period: they share weight and bias in shared memory)
+  int64_t row = OFF ? blockIdx.x + (int64_t)gridDim.x * threadIdx.y : (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const Span span = span_of<W>(OFF, A.x, blockIdx.x, A.ld_x, ES, A.H);
+  const int end = (int)span.body;
+  Rows<DT, W, NVL, 1, OFF, kWarpStages> in;
+  in.start({A.x}, {A.ld_x}, row, step, A.T, span, places);
+  const int n = param_bytes(A.H, PS) / 16, tid = threadIdx.y * 32 + lane;
   uint4* const params = places + kWarpStages * NVL * 32 * kWarpRows;
-  for (int i = tid; i < n; i += 32 * kWarpRows) {
-    params[i] = ((const uint4*)A.weight)[i];
-    if (A.bias) params[n + i] = ((const uint4*)A.bias)[i];
+  float we = 0.f, be = 0.f;
+  if constexpr (OFF) {
+    using P = std::conditional_t<PB, uint16_t, uint32_t>;
+    for (int c = tid; c < end; c += 32 * kWarpRows) {
+      ((P*)params)[c] = ((const P*)A.weight)[span.head + c];
+      if (A.bias) ((P*)(params + n))[c] = ((const P*)A.bias)[span.head + c];
+    }
+    if (span.edge >= 0) {
+      we = load_elem(A.weight, span.edge, PB);
+      if (A.bias) be = load_elem(A.bias, span.edge, PB);
+    }
+  } else {
+    for (int i = tid; i < end * PS / 8; i += 32 * kWarpRows) {        // (four bf16 are the least a row has)
+      ((uint2*)params)[i] = ((const uint2*)A.weight)[i];
+      if (A.bias) ((uint2*)(params + n))[i] = ((const uint2*)A.bias)[i];
+    }
   }
   const char* w = (const char*)params;
   const char* b = A.bias ? (const char*)(params + n) : nullptr;
   __syncthreads();
   for (; row < A.T; row += step) {
     uint4 rows[1][NVL];
-    in.take(rows);
+    float ve[1] = {0.f};
+    in.take(rows, ve);
     uint4 (&v)[NVL] = rows[0];
     in.fetch();
     float mean = 0.f;
@@ -403,27 +508,33 @@ __global__ void __launch_bounds__(32 * warp_rows(NVL), warp_blocks(NVL)) norm_fw
           for (int e = 0; e + o < W; e += 2 * o) t[e] += t[e + o];
         s += t[0];
       }
+      if (OFF) s += ve[0];
       mean = warp_sum(s) * inv_h;
     }
     float s2 = 0.f;
 #pragma unroll
     for (int i = 0; i < NVL; ++i)
-      if ((lane + i * 32) * W < H) {
+      if ((lane + i * 32) * W < end) {
         float t[W];
         Ac::unpack(v[i], t);
 #pragma unroll
         for (int e = 0; e < W; ++e) s2 = fmaf(t[e] - mean, t[e] - mean, s2);
       }
+    if (OFF && span.edge >= 0) s2 = fmaf(ve[0] - mean, ve[0] - mean, s2);
     const float rstd = 1.f / sqrtf(warp_sum(s2) * inv_h + A.eps);
     if (lane == 0) {
       if (A.out_mean) A.out_mean[row] = mean;
       if (A.out_rstd) A.out_rstd[row] = rstd;
     }
-    char* y = (char*)A.y + row * A.ld_y * ES;
+    if (OFF && span.edge >= 0) {
+      const float o = (ve[0] - mean) * rstd * we + be;
+      Access<DT, 1>::store((char*)A.y + (row * A.ld_y + span.edge) * ES, &o);
+    }
+    char* y = (char*)A.y + (row * A.ld_y + span.head) * ES;
 #pragma unroll
     for (int i = 0; i < NVL; ++i) {
       const int c = (lane + i * 32) * W;
-      if (c < H) {
+      if (c < end) {
         float t[W], o[W];
         Ac::unpack(v[i], t);
         Params<W, 1, PB> p;
@@ -517,13 +628,14 @@ __device__ __forceinline__ void keep_packed(uint4& v) { asm volatile("" : "+r"(v
 __device__ __forceinline__ void keep_packed(uint32_t& v) { asm volatile("" : "+r"(v)); }
 
 // Rows a group takes at a time, so that their sums share a barrier: at 8192 x 4096 (RMS norm, bf16) one at a time takes 55 us, two 41;
-// four do not fit the registers (67).
-__host__ __device__ constexpr int bwd_rows(int w, int nv) { return w == 1 || nv == 4 ? 1 : 2; }
+// four do not fit the registers (67), but for 4 fp32 a thread (16000 x 768: two 37 us, four 28).  With their edges rows of 2 x 8 bf16 a
+// thread fit one at a time (8192 x 4095: two 89 us, one 69).
+__host__ __device__ constexpr int bwd_rows(int w, int nv, bool off) { return w == 1 || nv == 4 || (off && w == 8 && nv == 2) ? 1 : w == 4 && nv == 1 ? 4 : 2; }
 
-template <int DT, int W, int NV, bool PB, bool BIAS>
+template <int DT, int W, int NV, bool PB, bool BIAS, bool OFF>
 __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
   using Ac = Access<DT, W>;
-  constexpr int ES = Vec<DT>::ESIZE, R = bwd_rows(W, NV);
+  constexpr int ES = Vec<DT>::ESIZE, R = bwd_rows(W, NV, OFF);
   extern __shared__ uint4 places[];
   __shared__ float sh[2][2 * R][kMaxWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -539,18 +651,23 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
     }
   const int64_t group = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
-  Rows<DT, W, NV, 2, W == 1 ? kStages : 2 * R> in;
-  in.start({A.x, A.dy}, {A.ld_x, A.ld_dy}, group, step, A.T, A.H, places);
+  const Span span = span_of<W>(OFF, A.x, group, A.ld_x, ES, A.H);
+  Rows<DT, W, NV, 2, OFF, W == 1 ? kStages : 2 * R> in;
+  in.start({A.x, A.dy}, {A.ld_x, A.ld_dy}, group, step, A.T, span, places);
   float w[NV][W];
+  const float we = OFF && span.edge >= 0 ? load_elem(A.weight, span.edge, PB) : 0.f;
+  float dwe = 0.f, dbe = 0.f;   // of the edge
   {
     Params<W, NV, PB> p;
-    p.load(A.weight, A.H);
+    if constexpr (OFF) p.load(A.weight, span);
+    else p.load(A.weight, A.H);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < W; ++e) w[i][e] = p.get(i, e);
   }
-  char* out = (char*)A.dx + (group * A.ld_dx + (int64_t)threadIdx.x * W) * ES;
+  char* out = (char*)A.dx + (group * A.ld_dx + span.head + (int64_t)threadIdx.x * W) * ES;
+  const int64_t out_edge = (span.edge - span.head - (int64_t)threadIdx.x * W) * ES;
   const int64_t out_stride = step * A.ld_dx * ES;
   float mean_next[R], rstd_next[R];
   auto fetch_stats = [&](int64_t row) {
@@ -564,15 +681,17 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
   fetch_stats(group);
   for (int64_t row = group; row < A.T; row += R * step) {
     typename Ac::raw raw[R][2][NV];
-    float mean[R], rstd[R], s[2 * R];
+    float mean[R], rstd[R], s[2 * R], edge[R][2];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       mean[r] = mean_next[r];
       rstd[r] = rstd_next[r];
-      in.take(raw[r]);
+      edge[r][0] = edge[r][1] = 0.f;
+      in.take(raw[r], edge[r]);
       if (r > 0 && row + r * step >= A.T) {                 // past the last row: 0, and so is everything below
 #pragma unroll
         for (int i = 0; i < NV; ++i) raw[r][0][i] = raw[r][1][i] = Ac::zero();
+        edge[r][0] = edge[r][1] = 0.f;
       }
       if (W > 1) in.fetch();
     }
@@ -594,6 +713,13 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
           dw[i][e] = fmaf(dy[e], xh, dw[i][e]);
           if (BIAS) db[i][e] += dy[e];
         }
+      }
+      if (OFF) {
+        const float xh = fmaf(edge[r][0], rstd[r], shift), g = edge[r][1] * we;
+        s1 += g;
+        s2 = fmaf(g, xh, s2);
+        dwe = fmaf(edge[r][1], xh, dwe);
+        dbe += edge[r][1];
       }
       s[2 * r] = s1;
       s[2 * r + 1] = s2;
@@ -628,6 +754,10 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
           Ac::store(out + (int64_t)i * (int)blockDim.x * W * ES, o);
         }
       }
+      if (OFF && span.edge >= 0) {
+        const float o = fmaf(edge[r][1] * we, rstd[r], fmaf(edge[r][0], c1, c0));
+        Access<DT, 1>::store(out + out_edge, &o);
+      }
       out += out_stride;
     }
   }
@@ -640,14 +770,18 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
     float* all = (float*)places;                            // [groups][kPer][H]: less than the rows took
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      if (c < A.H) {
+      const int64_t c = span.head + column<W>(i);
+      if (column<W>(i) < span.body) {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
           all[threadIdx.y * kPer * A.H + c + e] = dw[i][e];
           if (BIAS) all[(threadIdx.y * kPer + 1) * A.H + c + e] = db[i][e];
         }
       }
+    }
+    if (OFF && span.edge >= 0) {
+      all[threadIdx.y * kPer * A.H + span.edge] = dwe;
+      if (BIAS) all[(threadIdx.y * kPer + 1) * A.H + span.edge] = dbe;
     }
     __syncthreads();
     float* line = A.partial + (int64_t)blockIdx.x * kPer * A.H;
@@ -661,14 +795,18 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
   float* pw = A.partial + group * kPer * A.H;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int64_t c = column<W>(i);
-    if (c < A.H) {
+    const int64_t c = span.head + column<W>(i);
+    if (column<W>(i) < span.body) {
 #pragma unroll
       for (int e = 0; e < W; ++e) {
         pw[c + e] = dw[i][e];
         if (BIAS) pw[A.H + c + e] = db[i][e];
       }
     }
+  }
+  if (OFF && span.edge >= 0) {
+    pw[span.edge] = dwe;
+    if (BIAS) pw[A.H + span.edge] = dbe;
   }
 }
 
@@ -736,22 +874,32 @@ struct Plan {
   int rows;       // groups a block
 };
 
-bool vector_rows(const NormArgs& a, bool backward) {
+enum RowKind { kAligned, kSpans, kElements };        // rows on 16 bytes; all matrices' rows at the same offsets to 16 bytes; neither
+struct RowsAt { RowKind kind; int period; };          // rows after which the offsets repeat
+RowsAt rows_at(const NormArgs& a, bool backward) {
   const int64_t es = a.dtype == JP_BF16 ? 2 : 4;
-  auto on16 = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
-  auto ok = [&](const void* p, int64_t ld) { return on16(p) && ld * es % 16 == 0; };
-  if (a.H * es % 16 || !on16(a.weight) || !on16(a.bias)) return false;
-  return backward ? ok(a.x, a.ld_x) && ok(a.dy, a.ld_dy) && ok(a.dx, a.ld_dx) : ok(a.x, a.ld_x) && ok(a.y, a.ld_y);
+  const void* p[3] = {a.x, backward ? a.dx : a.y, backward ? a.dy : a.x};
+  const int64_t ld[3] = {a.ld_x, backward ? a.ld_dx : a.ld_y, backward ? a.ld_dy : a.ld_x};
+  bool aligned = a.H * es % 16 == 0 && ((uintptr_t)a.weight & 15) == 0 && ((uintptr_t)a.bias & 15) == 0;
+  for (int i = 0; i < 3; ++i) {
+    if ((((uintptr_t)p[i] ^ (uintptr_t)p[0]) & 15) != 0 || (ld[i] - ld[0]) * es % 16 != 0) return {kElements, 1};
+    aligned = aligned && ((uintptr_t)p[i] & 15) == 0 && ld[i] * es % 16 == 0;
+  }
+  int period = 1;
+  while (a.ld_x * es * period % 16 != 0) period *= 2;
+  return {aligned ? kAligned : kSpans, period};
 }
 
-// Threads and registers of a row.  16-byte accesses where rows start on 16 bytes, else single elements; 1, 2 or 4 vectors
-// (2, 8 or 16 elements) a thread so that rows up to 16384 bf16 (8192 fp32, or 8192 unaligned) stay in registers; the sums of a backward
-// pass take as much again, so 8192 there.
-Plan plan_for(int64_t H, int dtype, bool vec, bool backward) {
+// Threads and registers of a row.  16-byte accesses, or single elements where the matrices' rows differ in their offsets; 1, 2 or 4
+// vectors (2, 8 or 16 elements) a thread so that rows up to 16384 bf16 (8192 fp32, or 8192 single elements) stay in registers; the sums
+// of a backward pass take as much again, so 8192 there (and two aligned vectors from 192 on: 12000 x 2048 bf16 46 us with
+// one, 42; of 12000 x 2047, where two take one row at a time, 48 with one, 53).
+Plan plan_for(int64_t H, int dtype, RowKind kind, bool backward) {
   Plan p{};
-  p.w = vec ? (dtype == JP_BF16 ? 8 : 4) : 1;
+  const int vw = dtype == JP_BF16 ? 8 : 4;
+  p.w = kind == kElements ? 1 : vw;
   const int64_t n = (H + p.w - 1) / p.w;
-  if (vec) p.nv = n <= 256 ? 1 : n <= 1024 ? 2 : n <= (backward ? 8192 / p.w : 2048) ? 4 : 0;
+  if (p.w > 1) p.nv = n <= (backward && kind == kAligned ? 192 : 256) ? 1 : n <= 1024 ? 2 : n <= (backward ? 8192 / p.w : 2048) ? 4 : 0;
   else p.nv = n <= 64 ? 2 : n <= 2048 ? 8 : n <= 8192 ? 16 : 0;
   if (p.nv == 0) { p.threads = 1024; p.rows = 1; p.w = 1; return p; }
   const int64_t per = (n + p.nv - 1) / p.nv;
@@ -761,12 +909,14 @@ Plan plan_for(int64_t H, int dtype, bool vec, bool backward) {
 }
 
 // Blocks: all rows at once where there are few, else what the registers of an SM hold: 512 threads of a backward pass and of 16 elements
-// a thread, 768 of 8 single elements, 1024 of the rest.
-int grid_for(int64_t T, const Plan& p, int sms, bool backward) {
+// a thread, 768 of 8 single elements, 1024 of the rest; a multiple of the period.
+int grid_for(int64_t T, const Plan& p, int sms, bool backward, int period) {
   const int64_t need = (T + p.rows - 1) / p.rows;
   const int per_sm = (p.w == 1 && p.nv == 2 ? 1024 : backward || p.nv == 16 ? 512 : p.w == 1 ? 768 : 1024) / (p.threads * p.rows);
   const int64_t cap = (int64_t)sms * (per_sm > 8 ? 8 : per_sm < 1 ? 1 : per_sm);
-  return (int)(need < cap ? need : cap);
+  if (need <= cap) return (int)need;
+  if (p.rows % period == 0) return (int)cap;
+  return (int)(cap < period ? period : cap / period * period);
 }
 
 template <class K>
@@ -789,47 +939,68 @@ cudaError_t launch(K* kernel, const NormArgs& a, dim3 grid, dim3 block, int smem
 }
 
 template <int DT, bool PB, int NVL>
-cudaError_t fwd_warp(const NormArgs& a, cudaStream_t s, int sms) {
+cudaError_t fwd_warp(const NormArgs& a, const RowsAt& at, cudaStream_t s, int sms) {
   constexpr int kWarpRows = warp_rows(NVL);
-  const int64_t need = (a.T + kWarpRows - 1) / kWarpRows, cap = (int64_t)sms * warp_blocks(NVL);
-  const int smem = kWarpStages * NVL * 32 * kWarpRows * 16 + (int)a.H * (PB ? 2 : 4) * (a.bias ? 2 : 1);
-  return launch(norm_fwd_warp_kernel<DT, NVL, PB>, a, dim3((unsigned)(need < cap ? need : cap)), dim3(32, kWarpRows), smem, s);
+  const int64_t most = (int64_t)sms * warp_blocks(NVL), cap = most < at.period ? at.period : most / at.period * at.period;
+  const bool off = at.kind == kSpans;
+  const int64_t need = off ? cap : (a.T + kWarpRows - 1) / kWarpRows;
+  const int smem = kWarpStages * NVL * 32 * kWarpRows * 16 +
+                   param_bytes(a.H, PB ? 2 : 4) * (a.bias ? 2 : 1);
+  const dim3 g((unsigned)(need < cap ? need : cap)), b(32, kWarpRows);
+  return off ? launch(norm_fwd_warp_kernel<DT, NVL, PB, true>, a, g, b, smem, s) : launch(norm_fwd_warp_kernel<DT, NVL, PB, false>, a, g, b, smem, s);
 }
 
 template <int DT, bool PB>
 cudaError_t fwd(const NormArgs& a, cudaStream_t s, int sms) {
   constexpr int VW = Vec<DT>::N;
-  const bool vec = vector_rows(a, false);
+  const RowsAt at = rows_at(a, false);
+  const RowKind kind = at.kind == kSpans && a.H <= 64 ? kElements : at.kind;
   // a warp a row where every SM gets its blocks full of rows; with fewer rows a block a row is done sooner
-  if (vec && a.T >= (int64_t)sms * 12 && a.H > 64 * VW && a.H <= 640 * VW) {
-    if (a.H <= 128 * VW) return fwd_warp<DT, PB, 4>(a, s, sms);
-    if (a.H <= 256 * VW) return fwd_warp<DT, PB, 8>(a, s, sms);
-    if (a.H <= 512 * VW) return fwd_warp<DT, PB, 16>(a, s, sms);
-    return fwd_warp<DT, PB, 20>(a, s, sms);
+  const int64_t n = (a.H + VW - 1) / VW;
+  if (at.kind != kElements && a.T >= (int64_t)sms * 12 && n > 64 && n <= 640) {
+    if (n <= 128) return fwd_warp<DT, PB, 4>(a, at, s, sms);
+    if (n <= 256) return fwd_warp<DT, PB, 8>(a, at, s, sms);
+    if (n <= 512) return fwd_warp<DT, PB, 16>(a, at, s, sms);
+    return fwd_warp<DT, PB, 20>(a, at, s, sms);
   }
-  const Plan p = plan_for(a.H, a.dtype, vec, false);
-  const int grid = grid_for(a.T, p, sms, false);
+  // (short rows: vectors would leave most lanes idle, 14 us at 30,000 x 63 bf16 against 11)
+  const Plan p = plan_for(a.H, a.dtype, kind, false);
+  const int grid = grid_for(a.T, p, sms, false, at.period);
   const dim3 b(p.threads, p.rows);
   const int smem = kStages * p.rows * (p.w > 1 ? p.nv * p.threads * 16 : span_bytes(a.H, Vec<DT>::ESIZE));
   if (p.nv == 0) { norm_fwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
   if (p.w == 1)
-    return p.nv == 2 ? launch(norm_fwd_kernel<DT, 1, 2, PB>, a, grid, b, smem, s) : p.nv == 8 ? launch(norm_fwd_kernel<DT, 1, 8, PB>, a, grid, b, smem, s) : launch(norm_fwd_kernel<DT, 1, 16, PB>, a, grid, b, smem, s);
-  if (p.nv == 1) return launch(norm_fwd_kernel<DT, VW, 1, PB>, a, grid, b, smem, s);
-  if (p.nv == 2) return launch(norm_fwd_kernel<DT, VW, 2, PB>, a, grid, b, smem, s);
-  return launch(norm_fwd_kernel<DT, VW, 4, PB>, a, grid, b, smem, s);
+    return p.nv == 2   ? launch(norm_fwd_kernel<DT, 1, 2, PB, false>, a, grid, b, smem, s)
+           : p.nv == 8 ? launch(norm_fwd_kernel<DT, 1, 8, PB, false>, a, grid, b, smem, s)
+                       : launch(norm_fwd_kernel<DT, 1, 16, PB, false>, a, grid, b, smem, s);
+  if (kind == kSpans)
+    return p.nv == 1   ? launch(norm_fwd_kernel<DT, VW, 1, PB, true>, a, grid, b, smem, s)
+           : p.nv == 2 ? launch(norm_fwd_kernel<DT, VW, 2, PB, true>, a, grid, b, smem, s)
+                       : launch(norm_fwd_kernel<DT, VW, 4, PB, true>, a, grid, b, smem, s);
+  if (p.nv == 1) return launch(norm_fwd_kernel<DT, VW, 1, PB, false>, a, grid, b, smem, s);
+  if (p.nv == 2) return launch(norm_fwd_kernel<DT, VW, 2, PB, false>, a, grid, b, smem, s);
+  return launch(norm_fwd_kernel<DT, VW, 4, PB, false>, a, grid, b, smem, s);
 }
 
 template <int DT, bool PB, bool BIAS>
-cudaError_t bwd(const NormArgs& a, const Plan& p, int grid, cudaStream_t s) {
+cudaError_t bwd(const NormArgs& a, const Plan& p, bool off, int grid, cudaStream_t s) {
   constexpr int VW = Vec<DT>::N;
   const dim3 b(p.threads, p.rows);
-  const int smem = 2 * p.rows * (p.w > 1 ? 2 * bwd_rows(p.w, p.nv) * p.nv * p.threads * 16 : kStages * span_bytes(a.H, Vec<DT>::ESIZE));
+  const int smem = 2 * p.rows * (p.w > 1 ? 2 * bwd_rows(p.w, p.nv, off) * p.nv * p.threads * 16 : kStages * span_bytes(a.H, Vec<DT>::ESIZE));
   if (p.nv == 0) { norm_bwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
   if (p.w == 1)
-    return p.nv == 2 ? launch(norm_bwd_kernel<DT, 1, 2, PB, BIAS>, a, grid, b, smem, s) : p.nv == 8 ? launch(norm_bwd_kernel<DT, 1, 8, PB, BIAS>, a, grid, b, smem, s) : launch(norm_bwd_kernel<DT, 1, 16, PB, BIAS>, a, grid, b, smem, s);
-  if (p.nv == 1) return launch(norm_bwd_kernel<DT, VW, 1, PB, BIAS>, a, grid, b, smem, s);
-  if (p.nv == 2) return launch(norm_bwd_kernel<DT, VW, 2, PB, BIAS>, a, grid, b, smem, s);
-  if constexpr (DT == JP_F32) return launch(norm_bwd_kernel<DT, VW, 4, PB, BIAS>, a, grid, b, smem, s);
+    return p.nv == 2   ? launch(norm_bwd_kernel<DT, 1, 2, PB, BIAS, false>, a, grid, b, smem, s)
+           : p.nv == 8 ? launch(norm_bwd_kernel<DT, 1, 8, PB, BIAS, false>, a, grid, b, smem, s)
+                       : launch(norm_bwd_kernel<DT, 1, 16, PB, BIAS, false>, a, grid, b, smem, s);
+  if (off) {
+    if (p.nv == 1) return launch(norm_bwd_kernel<DT, VW, 1, PB, BIAS, true>, a, grid, b, smem, s);
+    if (p.nv == 2) return launch(norm_bwd_kernel<DT, VW, 2, PB, BIAS, true>, a, grid, b, smem, s);
+    if constexpr (DT == JP_F32) return launch(norm_bwd_kernel<DT, VW, 4, PB, BIAS, true>, a, grid, b, smem, s);
+    return cudaErrorInvalidConfiguration;
+  }
+  if (p.nv == 1) return launch(norm_bwd_kernel<DT, VW, 1, PB, BIAS, false>, a, grid, b, smem, s);
+  if (p.nv == 2) return launch(norm_bwd_kernel<DT, VW, 2, PB, BIAS, false>, a, grid, b, smem, s);
+  if constexpr (DT == JP_F32) return launch(norm_bwd_kernel<DT, VW, 4, PB, BIAS, false>, a, grid, b, smem, s);
   return cudaErrorInvalidConfiguration;
 }
 
@@ -843,18 +1014,21 @@ cudaError_t launch_norm_forward(const NormArgs& a, cudaStream_t s, int sms) {
 // Lines of partial sums a backward call can need, whatever the alignment of its pointers.
 int64_t norm_backward_groups(int64_t T, int64_t H, int dtype, int sms) {
   int64_t most = 0;
-  for (int vec = 0; vec < 2; ++vec) {
-    const Plan p = plan_for(H, dtype, vec != 0, true);
-    const int64_t g = grid_for(T, p, sms, true);
-    most = g > most ? g : most;
-  }
+  for (const RowKind kind : {kAligned, kSpans, kElements})
+    for (const int period : {1, 8}) {
+      const int64_t g = grid_for(T, plan_for(H, dtype, kind, true), sms, true, period);
+      most = g > most ? g : most;
+    }
   return most;
 }
 
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a.H, a.dtype, vector_rows(a, true), true);
-  const int grid = grid_for(a.T, p, sms, true);
-  auto run = [&](auto* with, auto* without) { return a.dbias ? with(a, p, grid, s) : without(a, p, grid, s); };
+  const RowsAt at = rows_at(a, true);
+  const Plan p = plan_for(a.H, a.dtype, at.kind, true);
+  const int grid = grid_for(a.T, p, sms, true, at.period);
+  auto run = [&](auto* with, auto* without) {
+    return a.dbias ? with(a, p, at.kind == kSpans, grid, s) : without(a, p, at.kind == kSpans, grid, s);
+  };
   cudaError_t e;
   if (a.dtype == JP_BF16) e = a.param_bf16 ? run(bwd<JP_BF16, true, true>, bwd<JP_BF16, true, false>) : run(bwd<JP_BF16, false, true>, bwd<JP_BF16, false, false>);
   else e = a.param_bf16 ? run(bwd<JP_F32, true, true>, bwd<JP_F32, true, false>) : run(bwd<JP_F32, false, true>, bwd<JP_F32, false, false>);

@@ -112,8 +112,39 @@ def test_many_rows(ctx, T, H, dtype, rms, bias, param):
     check_backward(got, dy, x, w, mean, rstd, rms)
     again = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd, rms=rms, bias=bias)
     assert all(a is c or torch.equal(a, c) for a, c in zip(got, again))
+    # in place as out of place, with rows at the same pitch (which decides the order of a row's sums)
+    beside, _, _ = runner.layer_norm(ctx, x, w, b, eps=EPS, rms=rms, out=torch.empty_strided(x.shape, x.stride(), dtype=dtype, device="cuda"))
+    check_forward(beside, mean, rstd, x, w, b, rms)
     y2, _, _ = runner.layer_norm(ctx, x, w, b, eps=EPS, rms=rms, out=x)
-    assert torch.equal(y2, y)
+    assert torch.equal(y2, beside)
+
+
+@pytest.mark.parametrize("T,H", [(3, 5), (1, 1023), (40, 255), (5000, 7), (30011, 63), (1790, 519), (2001, 1283), (1999, 2047), (3600, 4095),
+                                 (1801, 5113), (1777, 2558), (600, 4089), (400, 8185), (300, 8191), (9, 16377), (1900, 1028)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rms,param,start", [(False, torch.float32, 0), (True, torch.bfloat16, 0), (False, torch.bfloat16, 3)])
+def test_rows_that_share_vectors(ctx, T, H, dtype, rms, param, start):
+    """Packed rows of odd width, all matrices at the same offset: NaN around the inputs, and what is around the outputs stays."""
+    x0, dy0, w, b = make(T, H, dtype, param, not rms, seed=T + H)
+
+    def placed(src):
+        flat = torch.full((start + T * H + 9,), float("nan"), device="cuda", dtype=dtype)
+        view = flat[start:start + T * H].view(T, H)
+        if src is not None:
+            view.copy_(src)
+        return flat, view
+
+    (_, x), (_, dy), (fy, y), (fdx, dx) = placed(x0), placed(dy0), placed(None), placed(None)
+    _, mean, rstd = runner.layer_norm(ctx, x, w, b, eps=EPS, rms=rms, out=y)
+    check_forward(y, mean, rstd, x0, w, b, rms)
+    got = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd, rms=rms, bias=not rms, dx=dx)
+    check_backward(got, dy0, x0, w, mean, rstd, rms)
+    for flat in (fy, fdx):
+        assert flat[:start].isnan().all() and flat[start + T * H:].isnan().all()
+    same = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd, rms=rms, bias=not rms, dx=dy)
+    assert all(a is c or torch.equal(a, c) for a, c in zip(got, same))
+    same, _, _ = runner.layer_norm(ctx, x, w, b, eps=EPS, rms=rms, out=x)
+    assert torch.equal(same, y)
 
 
 @pytest.mark.parametrize("H,ld", [(2048, 2056), (1000, 1001), (63, 70), (4096, 4104)])
@@ -126,12 +157,17 @@ def test_row_pitches_and_in_place(ctx, H, ld, dtype):
     y, mean, rstd = runner.layer_norm(ctx, x, w, b, eps=EPS, out=big[1:T + 1, :H])
     check_forward(y, mean, rstd, keep_x, w, b, False)
     assert (big[0] == 5).all() and (big[-1] == 5).all() and (big[:, H:] == 5).all()    # nothing beside the rows is written
-    got = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd)
+    # (bits are compared between rows of the same pitch and offset, which decide the order of a row's sums)
+    beside = torch.empty_strided(x.shape, x.stride(), dtype=dtype, device="cuda")
+    check_backward(runner.layer_norm_backward(ctx, dy, x, w, mean, rstd), keep_dy, x, w, mean, rstd, False)
+    got = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd, dx=torch.empty_strided(x.shape, x.stride(), dtype=dtype, device="cuda"))
     same = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd, dx=dy)                # dx in dy's place
     assert all(torch.equal(a, c) for a, c in zip(got, same)) and same[0].data_ptr() == dy.data_ptr()
     check_backward(same, keep_dy, x, w, mean, rstd, False)
+    y3, _, _ = runner.layer_norm(ctx, x, w, b, eps=EPS, out=beside)
+    check_forward(y3, mean, rstd, keep_x, w, b, False)
     y2, _, _ = runner.layer_norm(ctx, x, w, b, eps=EPS, out=x)                         # y in x's place
-    assert torch.equal(y2, y) and y2.data_ptr() == x.data_ptr()
+    assert torch.equal(y2, y3) and y2.data_ptr() == x.data_ptr()
     assert (x.storage_offset() == 0) and (torch.as_strided(x, (T, ld - H), (ld, 1), H) == 7).all()
 
 
