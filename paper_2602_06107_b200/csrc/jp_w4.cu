@@ -8,7 +8,8 @@
 // clock that shared memory moves, and a TMEM read per group for the scales; with 1 to 32 tokens its rate is of no use.)
 //
 // Weights are laid out once (pack_kernel) in the order the MMA's A fragments want them: tiles of 16 rows, blocks of 128
-// columns, per block 8 steps of k = 16.  A lane's 8 weights of a step are one 32-bit word whose nibbles j and j + 4 are the
+// columns, per block 8 steps of k = 16.  Which of a group's columns make a step is free as long as A and B agree: two steps take 32
+// columns, lane t of a row's four 8 t .. 8 t + 7, so that a lane's x of two steps are 16 bytes of memory.  A lane's 8 weights of a step are one 32-bit word whose nibbles j and j + 4 are the
 // two halves of fragment register j: four masks, one shift and four packed multiply-adds (scaled2) make the fragment.  A block is 1024 bytes of words, then one 32-bit word per
 // (row, group): the scale as fp32 with its low 4 bits replaced by z (scales come in bf16 or fp16: those bits are zero).
 // Blocks of a tile follow one another, tiles too: what a warp reads is one contiguous run of memory.
@@ -119,23 +120,50 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   };
   fetch();
   fetch();
-  // x in B-fragment order: word w of unit (block, step pair, token, t) is columns 128 block + 32 pair + 16 (w / 2)
-  // + 8 (w % 2) + 2 t and the next.  A warp takes half a block's columns of all tokens, a lane a pair of columns.  Asynchronous copies
-  // and little code: in the smallest calls fetching instructions is part of the time (the loop unrolled by eight cost 4 us).
-  const bool pairs = (((uintptr_t)A.x | (uintptr_t)(A.ld_x * 2)) & 3) == 0;
-  for (int half = warp; half < 2 * kblocks; half += kWarps) {
-    const int in = (half & 1) * 64 + lane * 2, k = (half >> 1) * kBlockK + in;       // column within the block, in the row
-    const int valid = k + 1 < A.K ? 4 : k < A.K ? 2 : 0;    // bytes; the rest is filled with zeros
-    const uint16_t* xr = (const uint16_t*)A.x + (valid ? k : 0);
-    uint32_t* to = (uint32_t*)(xs + ((half >> 1) * 4 + (in >> 5)) * A.M * 4 + ((in >> 1) & 3)) + ((in >> 3) & 3);
-    if (pairs) {
+  // x in B-fragment order: unit (block, step pair, token, t) of 16 bytes is columns 128 block + 32 pair + 8 t and the next seven.
+  // Asynchronous copies and little code: in the smallest calls fetching instructions is part of the time (the loops unrolled by eight
+  // cost 4 us).
+  const uintptr_t starts = (uintptr_t)A.x | (uintptr_t)(A.ld_x * 2);
+  if ((starts & 15) == 0) {                                 // a lane takes units, a warp eight step pairs of one token to one of eight
+    const int some = A.M > 4 ? 3 : A.M > 2 ? 2 : A.M - 1, r = lane >> 2, pairs = 8 >> some;
+    for (int sp = warp * pairs + (r >> some); sp < 4 * kblocks; sp += kWarps * pairs) {
+      const int k = sp * 32 + (lane & 3) * 8, bytes = k < A.K ? (A.K - k < 8 ? (int)(A.K - k) * 2 : 16) : 0;        // the rest is zeros
+      const uint16_t* xr = (const uint16_t*)A.x + (bytes ? k : 0);
+      uint4* to = xs + sp * A.M * 4 + (lane & 3);
 #pragma unroll 1
-      for (int m = 0; m < A.M; ++m, xr += A.ld_x, to += 16)
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(xr), "r"(valid) : "memory");
-    } else {                                                // rows that start on odd elements
+      for (int m = r & ((1 << some) - 1); m < A.M; m += 8)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to + m * 4)),
+                     "l"(xr + m * A.ld_x), "r"(bytes) : "memory");
+    }
+  } else {                                                  // a lane takes two columns, a warp half a block's, token after token
+    for (int half = warp; half < 2 * kblocks; half += kWarps) {
+      const int k = half * 64 + lane * 2;
+      const int valid = k + 1 < A.K ? 4 : k < A.K ? 2 : 0;  // bytes; the rest is filled with zeros
+      const uint16_t* xr = (const uint16_t*)A.x + (valid ? k : 0);
+      uint32_t* to = (uint32_t*)(xs + (half * 2 + (lane >> 4)) * A.M * 4) + (lane & 15);
+      if ((starts & 3) == 0) {
+#pragma unroll 1
+        for (int m = 0; m < A.M; ++m, xr += A.ld_x, to += 16)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(xr), "r"(valid) : "memory");
+      } else if (A.M > 4) {             // rows that start on odd elements, eight tokens together (15 x 84091 x 3347: 53 us by four, 45)
+#pragma unroll 1
+        for (int m = 0; m < A.M; m += 8) {
+          uint32_t lo[8], hi[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint16_t* const from = xr + (m + i < A.M ? (m + i) * A.ld_x : 0);
+            lo[i] = valid ? __ldg(from) : 0u;
+            hi[i] = valid == 4 ? __ldg(from + 1) : 0u;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (m + i < A.M) to[(m + i) * 16] = lo[i] | hi[i] << 16;
+        }
+      } else {
 #pragma unroll 4
-      for (int m = 0; m < A.M; ++m)
-        to[m * 16] = (valid ? __ldg(xr + m * A.ld_x) : 0u) | (valid == 4 ? (uint32_t)__ldg(xr + m * A.ld_x + 1) << 16 : 0u);
+        for (int m = 0; m < A.M; ++m)
+          to[m * 16] = (valid ? __ldg(xr + m * A.ld_x) : 0u) | (valid == 4 ? (uint32_t)__ldg(xr + m * A.ld_x + 1) << 16 : 0u);
+      }
     }
   }
   asm volatile("cp.async.commit_group;" ::: "memory");
@@ -283,7 +311,7 @@ __global__ void __launch_bounds__(256) w4_pack_kernel(W4PackArgs A) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int64_t n = tile * kTileRows + (lane >> 2) + (j & 1) * 8;
-        const int64_t k = k0 + step * 16 + (j >> 1) * 8 + (lane & 3) * 2;
+        const int64_t k = k0 + (step >> 1) * 32 + (lane & 3) * 8 + (step & 1) * 4 + (j >> 1) * 2;
         const uint32_t z = zero_of(n, k);                 // past the end: q = z, which contributes nothing
         const uint32_t byte = n < A.N && k < A.K ? A.q[n * A.ld_q + k / 2] : z | z << 4;
         v |= (byte & 15u) << (4 * j);
