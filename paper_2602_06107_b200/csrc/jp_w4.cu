@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   // x in B-fragment order: unit (block, step pair, token, t) of 16 bytes is columns 128 block + 32 pair + 8 t and the next seven.
   // Asynchronous copies and little code: in the smallest calls fetching instructions is part of the time (the loops unrolled by eight
   // cost 4 us).
-  const uintptr_t starts = (uintptr_t)A.x | (uintptr_t)(A.ld_x * 2);
+  const uintptr_t starts = (uintptr_t)A.x | (uintptr_t)(A.M > 1 ? A.ld_x * 2 : 0);
   if ((starts & 15) == 0) {                                 // a lane takes units, a warp eight step pairs of one token to one of eight
     const int some = A.M > 4 ? 3 : A.M > 2 ? 2 : A.M - 1, r = lane >> 2, pairs = 8 >> some;
     for (int sp = warp * pairs + (r >> some); sp < 4 * kblocks; sp += kWarps * pairs) {

@@ -229,3 +229,18 @@ def test_scales_near_the_ends_of_bf16(ctx, power, x_power):
     w = runner.pack_w4(ctx, q, s, z, K=K, group=group)
     x = (tokens(6, K, seed=3).float() * 2.0 ** x_power).to(torch.bfloat16)
     check(runner.linear_w4(ctx, x, w, out_dtype=torch.float32), x, unpacked(q, s, z, K, group), group)
+
+
+@gpu
+@pytest.mark.parametrize("start", [0, 1, 2, 4, 8])
+@pytest.mark.parametrize("M,ld", [(1, 0), (1, 601), (2, 600), (3, 601), (4, 604), (6, 601), (9, 608), (32, 603)])
+def test_where_tokens_start(ctx, start, M, ld):
+    """Rows of x on 16 bytes, 8, 4 and 2, alone and at any pitch; what is around them is NaN and is not read."""
+    N, K, group = 50, 599, 64
+    q, s, z = make(N, K, group, True, torch.bfloat16, seed=4)
+    w = runner.pack_w4(ctx, q, s, z, K=K, group=group)
+    ld = ld or K
+    flat = torch.full((start + M * ld,), float("nan"), device="cuda", dtype=torch.bfloat16)
+    x = flat[start:].as_strided((M, K), (ld, 1), start)
+    x.copy_(tokens(M, K, seed=M))
+    check(runner.linear_w4(ctx, x, w, out_dtype=torch.float32), x, unpacked(q, s, z, K, group), group)
