@@ -190,12 +190,14 @@ def _ptr(t):
     return ctypes.c_void_p(int(t))
 
 
+_DTYPE_CODES = {torch.bfloat16: JP_BF16, torch.float32: JP_F32}
+
+
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
-        return JP_BF16
-    if t.dtype == torch.float32:
-        return JP_F32
-    raise JackpotError(f"logits must be bfloat16 or float32, got {t.dtype}")
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise JackpotError(f"logits must be bfloat16 or float32, got {t.dtype}")
+    return code
 
 
 class Context:
@@ -213,6 +215,7 @@ class Context:
         self.h = h
         self.stream = int(stream)
         self._sizes = {}                # workspace bytes by entry point and sizes
+        self._descs = {}                # descriptors by their fields: an entry point only reads them
 
     def call_on_current_stream(self, fn, *args):
         """For the entry points that keep nothing in the context: enqueues on torch's current stream of the
@@ -462,11 +465,22 @@ def _wrong_device(t, device):
     raise JackpotError(f"tensor on {t.device}, but the context is on cuda:{device}")
 
 
-def _workspace_bytes(ctx: Context, fn, *sizes) -> int:
-    key = (fn.__name__, sizes)
+def _desc(ctx: Context, cls, *fields):
+    """The descriptor ``cls(*fields)``, built once for the same fields (not to be written to)."""
+    key = (cls, fields)
+    d = ctx._descs.get(key)
+    if d is None:
+        if len(ctx._descs) >= 4096:
+            ctx._descs.clear()
+        d = ctx._descs[key] = cls(*fields)
+    return d
+
+
+def _workspace_bytes(ctx: Context, name, *sizes) -> int:
+    key = (name, sizes)
     n = ctx._sizes.get(key)
     if n is None:
-        n = ctx._sizes[key] = int(fn(ctx.h, *sizes))
+        n = ctx._sizes[key] = int(getattr(ctx.lib, name)(ctx.h, *sizes))
         if len(ctx._sizes) > 4096:
             ctx._sizes.clear()
     return n
@@ -478,7 +492,7 @@ def jp_layer_norm_forward(ctx: Context, desc: jp_norm_desc, x, weight, bias, y, 
 
 
 def jp_layer_norm_workspace_bytes(ctx: Context, T: int, H: int, dtype: int) -> int:
-    return _workspace_bytes(ctx, ctx.lib.jp_layer_norm_workspace_bytes, T, H, dtype)
+    return _workspace_bytes(ctx, "jp_layer_norm_workspace_bytes", T, H, dtype)
 
 
 def jp_layer_norm_backward(ctx: Context, desc: jp_norm_desc, dy, x, weight, mean, rstd, dx, dweight, dbias, workspace):
@@ -502,7 +516,7 @@ def jp_w4_linear(ctx: Context, desc: jp_w4_desc, packed, x, ld_x: int, M: int, o
 
 
 def jp_verify_workspace_bytes(ctx: Context, B: int, N: int, V: int, dtype: int, with_draft_logits: bool) -> int:
-    return _workspace_bytes(ctx, ctx.lib.jp_verify_workspace_bytes, B, N, V, dtype, 1 if with_draft_logits else 0)
+    return _workspace_bytes(ctx, "jp_verify_workspace_bytes", B, N, V, dtype, 1 if with_draft_logits else 0)
 
 
 def jp_verify_draft(ctx: Context, desc: jp_verify_desc, target_logits, draft_logits, draft_tokens, n_draft, temperature,

@@ -163,14 +163,16 @@ def forward_lmhead(ctx: B.Context, h_actor, w_actor, h_policy, w_policy, tokens,
 
 def _rows(t, name):
     """[T, H] matrix with contiguous rows -> its row pitch in elements."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
-        raise B.JackpotError(f"{name} must be a matrix with contiguous rows")
-    if shape[0] <= 1:
-        return shape[1]
-    if stride[0] < shape[1]:
-        raise B.JackpotError(f"{name}: rows overlap")
-    return stride[0]
+    shape = t.shape
+    if len(shape) == 2:
+        if t.is_contiguous() or shape[0] <= 1 and (shape[1] <= 1 or t.stride(1) == 1):
+            return shape[1]
+        pitch, one = t.stride()
+        if one == 1 or shape[1] <= 1:
+            if pitch < shape[1]:
+                raise B.JackpotError(f"{name}: rows overlap")
+            return pitch
+    raise B.JackpotError(f"{name} must be a matrix with contiguous rows")
 
 
 def _dense(t, shape, dtype, name):
@@ -182,31 +184,30 @@ def _like(x):
     return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
 
 
-def _norm_desc(x, weight, bias, eps, rms, out, name, dy=None):
+def _norm_desc(ctx, x, weight, bias, eps, rms, out, name, dy=None):
     """Checks and fills what both passes share; ``out`` is y or dx."""
-    d = B.jp_norm_desc(dtype=B._dtype_code(x), param_dtype=B._dtype_code(weight), flags=B.JP_NORM_RMS if rms else 0, eps=eps,
-                       ld_x=_rows(x, "x"))
-    shape = x.shape
-    d.T, d.H = shape
-    _dense(weight, shape[1:], weight.dtype, "weight")
+    ld_x, shape, dtype, param = _rows(x, "x"), x.shape, x.dtype, weight.dtype
+    _dense(weight, shape[1:], param, "weight")
     if bias is not None:
-        _dense(bias, shape[1:], weight.dtype, "bias")
-    if out.shape != shape or out.dtype is not x.dtype:
+        _dense(bias, shape[1:], param, "bias")
+    if out.shape != shape or out.dtype is not dtype:
         raise B.JackpotError(f"{name} must have x's shape and dtype")
+    ld_out, ld_y, ld_dy, ld_dx = _rows(out, name), 0, 0, 0
     if dy is None:
-        d.ld_y = _rows(out, name)
+        ld_y = ld_out
     else:
-        if dy.shape != shape or dy.dtype is not x.dtype:
+        if dy.shape != shape or dy.dtype is not dtype:
             raise B.JackpotError("dy must have x's shape and dtype")
-        d.ld_dx, d.ld_dy = _rows(out, name), _rows(dy, "dy")
-    return d
+        ld_dx, ld_dy = ld_out, _rows(dy, "dy")
+    return B._desc(ctx, B.jp_norm_desc, shape[0], shape[1], ld_x, ld_y, ld_dy, ld_dx, B._dtype_code(x), B._dtype_code(weight),
+                   B.JP_NORM_RMS if rms else 0, float(eps))
 
 
 def layer_norm(ctx: B.Context, x, weight, bias=None, *, eps=1e-6, rms=False, out=None):
     """One jp_layer_norm_forward call on torch's current stream: ``(y, mean, rstd)`` (mean None with ``rms``).
     ``out``: where y goes (may be ``x``)."""
     y = _like(x) if out is None else out
-    d = _norm_desc(x, weight, bias, eps, rms, y, "out")
+    d = _norm_desc(ctx, x, weight, bias, eps, rms, y, "out")
     mean = None if rms else x.new_empty(d.T, dtype=torch.float32)
     rstd = x.new_empty(d.T, dtype=torch.float32)
     B.jp_layer_norm_forward(ctx, d, x, weight, bias, y, mean, rstd)
@@ -218,7 +219,7 @@ def layer_norm_backward(ctx: B.Context, dy, x, weight, mean, rstd, *, rms=False,
     (dbias None without ``bias``).  ``mean`` and ``rstd`` are the forward's; ``dx``: where dx goes (may be ``dy`` or ``x``)."""
     if dx is None:
         dx = _like(x)
-    d = _norm_desc(x, weight, None, 0.0, rms, dx, "dx", dy)
+    d = _norm_desc(ctx, x, weight, None, 0.0, rms, dx, "dx", dy)
     T, H = x.shape
     if not rms:
         _dense(mean, (T,), torch.float32, "mean")
@@ -324,13 +325,14 @@ def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_ac
     n_seq, rows, V = target_logits.shape
     N = rows - 1
     ld, seq = _positions(target_logits, (n_seq, rows, V), "target_logits")
-    d = B.jp_verify_desc(B=n_seq, V=V, N=N, dtype=B._dtype_code(target_logits), ld_target=ld, seq_target=seq)
+    ld_d = seq_d = 0
     if draft_logits is not None:
         if draft_logits.dtype is not target_logits.dtype:
             raise B.JackpotError("draft_logits must have target_logits' dtype")
         if draft_logits.dim() != 3:
             raise B.JackpotError("draft_logits must be [B, N, V]")
-        d.ld_draft, d.seq_draft = _positions(draft_logits, (n_seq, N, V), "draft_logits")
+        ld_d, seq_d = _positions(draft_logits, (n_seq, N, V), "draft_logits")
+    d = B._desc(ctx, B.jp_verify_desc, n_seq, V, ld, seq, ld_d, seq_d, N, B._dtype_code(target_logits))
     _dense(draft_tokens, (n_seq, N), torch.int32, "draft_tokens")
     _dense(u_accept, (n_seq, N), torch.float32, "u_accept")
     _dense(u_sample, (n_seq,), torch.float32, "u_sample")
@@ -338,15 +340,15 @@ def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_ac
         _dense(n_draft, (n_seq,), torch.int32, "n_draft")
     if temperature is not None:
         _dense(temperature, (n_seq,), torch.float32, "temperature")
-    new, dev = u_sample.new_empty, u_sample.device           # (empty_strided: the cheapest call that makes a matrix)
-    out = dict(n_accepted=new(n_seq, dtype=torch.int32),
+    dev = u_sample.device                                    # (empty_strided: the cheapest call that makes a matrix)
+    out = dict(n_accepted=torch.empty_like(u_sample, dtype=torch.int32),
                tokens=torch.empty_strided((n_seq, rows), (rows, 1), dtype=torch.int32, device=dev))
     if accept_prob:
         out["accept_prob"] = torch.empty_like(u_accept)
     if logp:
         out["logp"] = torch.empty_strided((n_seq, rows), (rows, 1), dtype=torch.float32, device=dev)
     need = B.jp_verify_workspace_bytes(ctx, n_seq, N, V, d.dtype, draft_logits is not None and N > 0)
-    ws = new(need, dtype=torch.uint8) if need else None
+    ws = u_sample.new_empty(need, dtype=torch.uint8) if need else None
     B.jp_verify_draft(ctx, d, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept, u_sample,
                       out["n_accepted"], out["tokens"], out.get("accept_prob"), out.get("logp"), ws)
     return out
