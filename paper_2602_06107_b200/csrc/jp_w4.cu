@@ -31,13 +31,17 @@ constexpr int kTileRows = 16;
 constexpr int kBlockK = 128;
 constexpr int kWarps = 16;
 constexpr int kSharedBytes = 232448;  // of one block
-// A warp takes `unit` blocks at a time (two where there are enough: less to do per block around the products, 36 -> 33 us at
-// 151,936 x 2048 and one token) and has `depth` units in flight: 3 of two, or 5 (4) of one, or 3 of one where x needs the room.
+// A warp takes a unit at a time and has DEPTH of them in flight.  A unit is two blocks where there are enough (less to do per block around
+// the products): two of one tile, or for many tiles the same block of two tiles, which then share what is read of x (151,936 x 2048 and
+// one token: one block 34.8 us, two of a tile 32.2, of two tiles 30.5; x 4096 and eight: 68.7, 62.2, 60.9; at 11008 x 4096 pairs of
+// tiles come out uneven, 6.9 us with two blocks of one tile, 7.7).  Above eight tokens the products take longer than either saves.
 // What the ring and the warps' parts of shared tiles leave is for x.
 __host__ __device__ constexpr int block_bytes(int groups) { return 1024 + kTileRows * 4 * groups; }
-__host__ __device__ constexpr int part_bytes(int nt) { return kWarps * nt * 32 * 16; }
-__host__ __device__ constexpr int ring_bytes(int unit, int depth, int groups) { return kWarps * depth * unit * block_bytes(groups); }
-constexpr int x_bytes(int nt, int unit, int depth, int groups) { return kSharedBytes - ring_bytes(unit, depth, groups) - part_bytes(nt); }
+__host__ __device__ constexpr int part_bytes(int tiles, int nt) { return kWarps * tiles * nt * 32 * 16; }
+__host__ __device__ constexpr int ring_bytes(int blocks, int depth, int groups) { return kWarps * depth * blocks * block_bytes(groups); }
+constexpr int x_bytes(int nt, int tiles, int unit, int depth, int groups) {
+  return kSharedBytes - ring_bytes(tiles * unit, depth, groups) - part_bytes(tiles, nt);
+}
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -89,30 +93,57 @@ __device__ __forceinline__ void store_tile(const W4Args& A, const float (&acc)[N
     }
 }
 
-template <int NT, int GROUPS, int UNIT, int DEPTH>
+template <int NT, int GROUPS, int TILES, int UNIT, int DEPTH>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
-  constexpr int kBlock = block_bytes(GROUPS), kBytes = UNIT * kBlock, kDepth = DEPTH;
+  static_assert(TILES == 1 || UNIT == 1, "a unit is blocks of one tile, or a block of two");
+  constexpr int kBlock = block_bytes(GROUPS), kBytes = UNIT * TILES * kBlock, kDepth = DEPTH;
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   char* ring = smem + warp * kDepth * kBytes;
-  float4* parts = (float4*)(smem + ring_bytes(UNIT, DEPTH, GROUPS));                 // [warp][NT][lane]: of a tile that an earlier warp begins
-  uint4* xs = (uint4*)(smem + ring_bytes(UNIT, DEPTH, GROUPS) + part_bytes(NT));     // [block][step pair][token][lane % 4]
+  float4* parts = (float4*)(smem + ring_bytes(TILES * UNIT, DEPTH, GROUPS));                 // [warp][TILES][NT][lane]: of a tile that an earlier warp begins
+  uint4* xs = (uint4*)(smem + ring_bytes(TILES * UNIT, DEPTH, GROUPS) + part_bytes(TILES, NT));     // [block][step pair][token][lane % 4]
   const int kblocks = (int)A.kblocks;
-  const int64_t tile0 = A.tiles * blockIdx.x / gridDim.x, tile1 = A.tiles * (blockIdx.x + 1) / gridDim.x;
+  const int64_t runs = TILES == 1 ? A.tiles : (A.tiles + 1) / 2;        // (below, a tile is a pair of them)
+  const int64_t tile0 = runs * blockIdx.x / gridDim.x, tile1 = runs * (blockIdx.x + 1) / gridDim.x;
   const int tile_units = kblocks / UNIT;
   const int64_t blocks = (tile1 - tile0) * tile_units;      // (units)
   const int64_t b0 = blocks * warp / kWarps, b1 = blocks * (warp + 1) / kWarps;
   const int count = (int)(b1 - b0);
-  const char* src = (const char*)A.packed + (tile0 * tile_units + b0) * kBytes + lane * 16;
+  const char* src;
+  int in_kb = 0;                                            // (pairs) block of the next unit to load, and where the second tile's is
+  int64_t in_tile = 0, second = 0;
+  if constexpr (TILES == 1) {
+    src = (const char*)A.packed + (tile0 * tile_units + b0) * kBytes + lane * 16;
+  } else {
+    in_tile = tile0 + b0 / tile_units;
+    in_kb = (int)(b0 % tile_units);
+    src = (const char*)A.packed + (in_tile * 2 * kblocks + in_kb) * kBlock + lane * 16;
+    second = 2 * in_tile + 1 < A.tiles ? (int64_t)kblocks * kBlock : 0;        // (the last pair may have one tile: its rows come twice)
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");                // launched as a programmatic dependent of whatever is before it
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int issued = 0, slot_in = 0, slot_out = 0;
   auto fetch = [&]() {
     if (issued < count) {
+      if constexpr (TILES == 1) {
 #pragma unroll
-      for (int c = 0; c < kBytes; c += 512)
-        if (c + 512 <= kBytes || lane * 16 < kBytes - c) copy16(ring + slot_in + c + lane * 16, src + c);
-      src += kBytes;
+        for (int c = 0; c < kBytes; c += 512)
+          if (c + 512 <= kBytes || lane * 16 < kBytes - c) copy16(ring + slot_in + c + lane * 16, src + c);
+        src += kBytes;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int c = 0; c < kBlock; c += 512)
+            if (c + 512 <= kBlock || lane * 16 < kBlock - c)
+              copy16(ring + slot_in + j * kBlock + c + lane * 16, src + (j ? second : 0) + c);
+        src += kBlock;
+        if (++in_kb == kblocks) {
+          in_kb = 0;
+          src += (int64_t)kblocks * kBlock;
+          second = 2 * ++in_tile + 1 < A.tiles ? (int64_t)kblocks * kBlock : 0;
+        }
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     ++issued;
@@ -172,11 +203,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 2) : "memory");
   __syncthreads();
 
-  float acc[NT][4];
+  float acc[TILES][NT][4];
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+  for (int j = 0; j < TILES; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[j][t][e] = 0.f;
+  auto keep_part = [&]() {
+#pragma unroll
+    for (int j = 0; j < TILES; ++j)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        parts[((warp * TILES + j) * NT + t) * 32 + lane] = make_float4(acc[j][t][0], acc[j][t][1], acc[j][t][2], acc[j][t][3]);
+  };
   int64_t tile = b0 / tile_units;                   // within the CTA's run
   int kb = (int)(b0 - tile * tile_units);
   bool whole = kb == 0;                             // this warp has the tile from its first block on
@@ -192,62 +232,70 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
     __syncwarp();
 #pragma unroll
     for (int u = 0; u < UNIT; ++u) {
-    const char* blk = ring + slot_out + u * kBlock;
-    uint32_t sw[2][GROUPS];
-    if constexpr (GROUPS == 1) {
-      sw[0][0] = ((const uint32_t*)(blk + 1024))[row];
-      sw[1][0] = ((const uint32_t*)(blk + 1024))[row + 8];
-    } else if constexpr (GROUPS == 2) {
-      *(uint2*)sw[0] = ((const uint2*)(blk + 1024))[row];
-      *(uint2*)sw[1] = ((const uint2*)(blk + 1024))[row + 8];
-    } else {
-      *(uint4*)sw[0] = ((const uint4*)(blk + 1024))[row];
-      *(uint4*)sw[1] = ((const uint4*)(blk + 1024))[row + 8];
-    }
-    float part[NT][4];
-    uint32_t z0 = 0, z1 = 0;
+      uint32_t sw[TILES][2][GROUPS];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const uint4 v = ((const uint4*)blk)[half * 32 + lane];
+      for (int j = 0; j < TILES; ++j) {
+        const char* const words = ring + slot_out + (u + j) * kBlock + 1024;
+        if constexpr (GROUPS == 1) {
+          sw[j][0][0] = ((const uint32_t*)words)[row];
+          sw[j][1][0] = ((const uint32_t*)words)[row + 8];
+        } else if constexpr (GROUPS == 2) {
+          *(uint2*)sw[j][0] = ((const uint2*)words)[row];
+          *(uint2*)sw[j][1] = ((const uint2*)words)[row + 8];
+        } else {
+          *(uint4*)sw[j][0] = ((const uint4*)words)[row];
+          *(uint4*)sw[j][1] = ((const uint4*)words)[row + 8];
+        }
+      }
+      float part[TILES][NT][4];
+      uint32_t z0[TILES], z1[TILES];
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int pair = half * 2 + p;
-        uint4 f[NT];
+      for (int half = 0; half < 2; ++half) {
+        uint4 v[TILES];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) f[t] = xt[t][x_at + (u * 4 + pair) * x_pair];
+        for (int j = 0; j < TILES; ++j) v[j] = ((const uint4*)(ring + slot_out + (u + j) * kBlock))[half * 32 + lane];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int step = pair * 2 + h, grp = step * GROUPS / 8;
-          const bool first = step % (8 / GROUPS) == 0;
-          if (first) {
-            z0 = minus_scaled2((sw[0][grp] & 15u) * 0x00010001u);
-            z1 = minus_scaled2((sw[1][grp] & 15u) * 0x00100010u);
-          }
-          const uint32_t w = p == 0 ? (h == 0 ? v.x : v.y) : (h == 0 ? v.z : v.w);
-          uint32_t a[4];
-          const uint32_t w8 = w >> 8;
-          a[0] = scaled2(w & 0x000f000fu, z0);
-          a[1] = scaled2(w & 0x00f000f0u, z1);
-          a[2] = scaled2(w8 & 0x000f000fu, z0);
-          a[3] = scaled2(w8 & 0x00f000f0u, z1);
+        for (int p = 0; p < 2; ++p) {
+          const int pair = half * 2 + p;
+          uint4 f[NT];
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            if (first) mma_bf16_first(part[t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
-            else mma_bf16(part[t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
-          }
-          if ((step + 1) % (8 / GROUPS) == 0) {
-            const float s0 = __uint_as_float(sw[0][grp] & ~15u), s1 = __uint_as_float(sw[1][grp] & ~15u);
+          for (int t = 0; t < NT; ++t) f[t] = xt[t][x_at + (u * 4 + pair) * x_pair];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              acc[t][0] = fmaf(part[t][0], s0, acc[t][0]);
-              acc[t][1] = fmaf(part[t][1], s0, acc[t][1]);
-              acc[t][2] = fmaf(part[t][2], s1, acc[t][2]);
-              acc[t][3] = fmaf(part[t][3], s1, acc[t][3]);
+          for (int h = 0; h < 2; ++h) {
+            const int step = pair * 2 + h, grp = step * GROUPS / 8;
+            const bool first = step % (8 / GROUPS) == 0;
+#pragma unroll
+            for (int j = 0; j < TILES; ++j) {
+              if (first) {
+                z0[j] = minus_scaled2((sw[j][0][grp] & 15u) * 0x00010001u);
+                z1[j] = minus_scaled2((sw[j][1][grp] & 15u) * 0x00100010u);
+              }
+              const uint32_t w = p == 0 ? (h == 0 ? v[j].x : v[j].y) : (h == 0 ? v[j].z : v[j].w);
+              uint32_t a[4];
+              const uint32_t w8 = w >> 8;
+              a[0] = scaled2(w & 0x000f000fu, z0[j]);
+              a[1] = scaled2(w & 0x00f000f0u, z1[j]);
+              a[2] = scaled2(w8 & 0x000f000fu, z0[j]);
+              a[3] = scaled2(w8 & 0x00f000f0u, z1[j]);
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                if (first) mma_bf16_first(part[j][t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
+                else mma_bf16(part[j][t], a, h == 0 ? f[t].x : f[t].z, h == 0 ? f[t].y : f[t].w);
+              }
+              if ((step + 1) % (8 / GROUPS) == 0) {
+                const float s0 = __uint_as_float(sw[j][0][grp] & ~15u), s1 = __uint_as_float(sw[j][1][grp] & ~15u);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                  acc[j][t][0] = fmaf(part[j][t][0], s0, acc[j][t][0]);
+                  acc[j][t][1] = fmaf(part[j][t][1], s0, acc[j][t][1]);
+                  acc[j][t][2] = fmaf(part[j][t][2], s1, acc[j][t][2]);
+                  acc[j][t][3] = fmaf(part[j][t][3], s1, acc[j][t][3]);
+                }
+              }
             }
           }
         }
       }
-    }
     }
     __syncwarp();                                   // (every lane has read the scales: the place may be filled again)
     fetch();
@@ -255,16 +303,17 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
     x_at += UNIT * 4 * x_pair;
     if (++kb == tile_units) {
       if (whole) {
-        store_tile<NT>(A, acc, tile0 + tile, lane);
-      } else {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-          parts[(warp * NT + t) * 32 + lane] = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
+        for (int j = 0; j < TILES; ++j) store_tile<NT>(A, acc[j], (tile0 + tile) * TILES + j, lane);
+      } else {
+        keep_part();
       }
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int j = 0; j < TILES; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[j][t][e] = 0.f;
       kb = 0;
       x_at = 0;
       ++tile;
@@ -273,10 +322,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   }
   // A tile that is not finished: its first warp keeps its part and adds those of the warps after it, in their order.
   const bool open = count > 0 && kb != 0;
-  if (open && !whole) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) parts[(warp * NT + t) * 32 + lane] = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
-  }
+  if (open && !whole) keep_part();
   __syncthreads();
   if (open && whole) {
     const int64_t end = (tile + 1) * tile_units;
@@ -285,12 +331,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
       if (o0 >= end) break;
       if (o1 == o0) continue;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const float4 v = parts[(o * NT + t) * 32 + lane];
-        acc[t][0] += v.x; acc[t][1] += v.y; acc[t][2] += v.z; acc[t][3] += v.w;
-      }
+      for (int j = 0; j < TILES; ++j)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float4 v = parts[((o * TILES + j) * NT + t) * 32 + lane];
+          acc[j][t][0] += v.x; acc[j][t][1] += v.y; acc[j][t][2] += v.z; acc[j][t][3] += v.w;
+        }
     }
-    store_tile<NT>(A, acc, tile0 + tile, lane);
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) store_tile<NT>(A, acc[j], (tile0 + tile) * TILES + j, lane);
   }
 }
 
@@ -332,16 +381,17 @@ __global__ void __launch_bounds__(256) w4_pack_kernel(W4PackArgs A) {
   }
 }
 
-template <int NT, int GROUPS, int UNIT, int DEPTH>
+template <int NT, int GROUPS, int TILES, int UNIT, int DEPTH>
 cudaError_t run(const W4Args& a, cudaStream_t s, int sms, int device) {
   static std::atomic<bool> ready[64];               // per device: the kernel may use this much shared memory
   if (device < 0 || device >= 64 || !ready[device].load(std::memory_order_acquire)) {
-    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS, UNIT, DEPTH>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS, TILES, UNIT, DEPTH>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
     if (e != cudaSuccess) return e;
     if (device >= 0 && device < 64) ready[device].store(true, std::memory_order_release);
   }
-  const int bytes = ring_bytes(UNIT, DEPTH, GROUPS) + part_bytes(NT) + (int)a.kblocks * kBlockK * 2 * a.M;
-  const int grid = (int)(a.tiles < sms ? a.tiles : sms);
+  const int bytes = ring_bytes(TILES * UNIT, DEPTH, GROUPS) + part_bytes(TILES, NT) + (int)a.kblocks * kBlockK * 2 * a.M;
+  const int64_t runs = (a.tiles + TILES - 1) / TILES;
+  const int grid = (int)(runs < sms ? runs : sms);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kWarps * 32);
@@ -352,18 +402,21 @@ cudaError_t run(const W4Args& a, cudaStream_t s, int sms, int device) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, w4_kernel<NT, GROUPS, UNIT, DEPTH>, a);
+  return cudaLaunchKernelEx(&cfg, w4_kernel<NT, GROUPS, TILES, UNIT, DEPTH>, a);
 }
 
 template <int NT, int GROUPS>
 cudaError_t run_unit(const W4Args& a, cudaStream_t s, int sms, int device) {
-  // units of two where a warp gets several of them (with fewer, half of the warps would be idle)
   const int64_t grid = a.tiles < sms ? a.tiles : sms, x = a.kblocks * kBlockK * 2 * a.M;
   constexpr int kFull = GROUPS == 4 ? 4 : 5;
-  if (a.kblocks % 2 == 0 && a.tiles * a.kblocks >= 4 * kWarps * grid && x <= x_bytes(NT, 2, 3, GROUPS))
-    return run<NT, GROUPS, 2, 3>(a, s, sms, device);
-  if (x <= x_bytes(NT, 1, kFull, GROUPS)) return run<NT, GROUPS, 1, kFull>(a, s, sms, device);
-  return run<NT, GROUPS, 1, 3>(a, s, sms, device);
+  if constexpr (NT == 1) {
+    if (a.tiles >= 8 * sms && x <= x_bytes(1, 2, 1, 3, GROUPS)) return run<1, GROUPS, 2, 1, 3>(a, s, sms, device);
+    // (with fewer units than these half of the warps would be idle)
+    if (a.kblocks % 2 == 0 && a.tiles * a.kblocks >= 4 * kWarps * grid && x <= x_bytes(1, 1, 2, 3, GROUPS))
+      return run<1, GROUPS, 1, 2, 3>(a, s, sms, device);
+  }
+  if (x <= x_bytes(NT, 1, 1, kFull, GROUPS)) return run<NT, GROUPS, 1, 1, kFull>(a, s, sms, device);
+  return run<NT, GROUPS, 1, 1, 3>(a, s, sms, device);
 }
 
 template <int NT>
@@ -397,7 +450,7 @@ cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms) {
 int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M) {
   const int groups = kBlockK / group;
   int64_t m = M < kW4MaxTokens ? M : kW4MaxTokens;
-  while (m > 1 && m * blocks_of(N, K) * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, 1, 3, groups)) --m;
+  while (m > 1 && m * blocks_of(N, K) * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, 1, 1, 3, groups)) --m;
   const int64_t launches = (M + m - 1) / m;
   return (int)((M + launches - 1) / launches);
 }
@@ -405,7 +458,7 @@ int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M) {
 cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms, int device) {
   a.tiles = (a.N + kTileRows - 1) / kTileRows;
   a.kblocks = blocks_of(a.N, a.K);
-  static_assert(kW4MaxK * 2 <= x_bytes(1, 1, 3, 4), "one token fits");
+  static_assert(kW4MaxK * 2 <= x_bytes(1, 1, 1, 3, 4), "one token fits");
   if (a.M <= 8) return run_groups<1>(a, group, s, sms, device);
   if (a.M <= 16) return run_groups<2>(a, group, s, sms, device);
   return run_groups<4>(a, group, s, sms, device);

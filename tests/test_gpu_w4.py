@@ -244,3 +244,20 @@ def test_where_tokens_start(ctx, start, M, ld):
     x = flat[start:].as_strided((M, K), (ld, 1), start)
     x.copy_(tokens(M, K, seed=M))
     check(runner.linear_w4(ctx, x, w, out_dtype=torch.float32), x, unpacked(q, s, z, K, group), group)
+
+
+@gpu
+@pytest.mark.parametrize("N,K", [(19000, 200), (18960, 1024), (18961, 129), (37900, 385)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_pairs_of_tiles(ctx, N, K, group):
+    """Enough tiles that they are taken in pairs, an even and an odd number of them, with a short last one."""
+    q, s, z = make(N, K, group, True, torch.float16, seed=N)
+    w = runner.pack_w4(ctx, q, s, z, K=K, group=group)
+    ref = unpacked(q, s, z, K, group)
+    for M in (1, 5, 8, 11):
+        big = torch.full((M + 2, N + 3), 7.0, device="cuda")
+        x = tokens(M, K, seed=M)
+        out = runner.linear_w4(ctx, x, w, out=big[1:M + 1, :N])
+        check(out, x, ref, group)
+        assert (big[0] == 7).all() and (big[-1] == 7).all() and (big[:, N:] == 7).all()
+        assert torch.equal(runner.linear_w4(ctx, x, w, out_dtype=torch.float32), out)
