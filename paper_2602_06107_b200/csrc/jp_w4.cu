@@ -30,17 +30,18 @@ namespace {
 constexpr int kTileRows = 16;
 constexpr int kBlockK = 128;
 constexpr int kWarps = 16;
+constexpr int kDepth = 3;
 constexpr int kSharedBytes = 232448;  // of one block
-// A warp takes a unit at a time and has DEPTH of them in flight.  A unit is two blocks where there are enough (less to do per block around
+// A warp takes a unit at a time and has three of them in flight (five were no faster).  A unit is two blocks where there are enough (less to do per block around
 // the products): two of one tile, or for many tiles the same block of two tiles, which then share what is read of x (151,936 x 2048 and
 // one token: one block 34.8 us, two of a tile 32.2, of two tiles 30.5; x 4096 and eight: 68.7, 62.2, 60.9; at 11008 x 4096 pairs of
 // tiles come out uneven, 6.9 us with two blocks of one tile, 7.7).  Above eight tokens the products take longer than either saves.
 // What the ring and the warps' parts of shared tiles leave is for x.
 __host__ __device__ constexpr int block_bytes(int groups) { return 1024 + kTileRows * 4 * groups; }
 __host__ __device__ constexpr int part_bytes(int tiles, int nt) { return kWarps * tiles * nt * 32 * 16; }
-__host__ __device__ constexpr int ring_bytes(int blocks, int depth, int groups) { return kWarps * depth * blocks * block_bytes(groups); }
-constexpr int x_bytes(int nt, int tiles, int unit, int depth, int groups) {
-  return kSharedBytes - ring_bytes(tiles * unit, depth, groups) - part_bytes(tiles, nt);
+__host__ __device__ constexpr int ring_bytes(int blocks, int groups) { return kWarps * kDepth * blocks * block_bytes(groups); }
+constexpr int x_bytes(int nt, int tiles, int unit, int groups) {
+  return kSharedBytes - ring_bytes(tiles * unit, groups) - part_bytes(tiles, nt);
 }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -93,15 +94,15 @@ __device__ __forceinline__ void store_tile(const W4Args& A, const float (&acc)[N
     }
 }
 
-template <int NT, int GROUPS, int TILES, int UNIT, int DEPTH>
+template <int NT, int GROUPS, int TILES, int UNIT>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   static_assert(TILES == 1 || UNIT == 1, "a unit is blocks of one tile, or a block of two");
-  constexpr int kBlock = block_bytes(GROUPS), kBytes = UNIT * TILES * kBlock, kDepth = DEPTH;
+  constexpr int kBlock = block_bytes(GROUPS), kBytes = UNIT * TILES * kBlock;
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   char* ring = smem + warp * kDepth * kBytes;
-  float4* parts = (float4*)(smem + ring_bytes(TILES * UNIT, DEPTH, GROUPS));                 // [warp][TILES][NT][lane]: of a tile that an earlier warp begins
-  uint4* xs = (uint4*)(smem + ring_bytes(TILES * UNIT, DEPTH, GROUPS) + part_bytes(TILES, NT));     // [block][step pair][token][lane % 4]
+  float4* parts = (float4*)(smem + ring_bytes(TILES * UNIT, GROUPS));                 // [warp][TILES][NT][lane]: of a tile that an earlier warp begins
+  uint4* xs = (uint4*)(smem + ring_bytes(TILES * UNIT, GROUPS) + part_bytes(TILES, NT));     // [block][step pair][token][lane % 4]
   const int kblocks = (int)A.kblocks;
   const int64_t runs = TILES == 1 ? A.tiles : (A.tiles + 1) / 2;        // (below, a tile is a pair of them)
   const int64_t tile0 = runs * blockIdx.x / gridDim.x, tile1 = runs * (blockIdx.x + 1) / gridDim.x;
@@ -381,15 +382,15 @@ __global__ void __launch_bounds__(256) w4_pack_kernel(W4PackArgs A) {
   }
 }
 
-template <int NT, int GROUPS, int TILES, int UNIT, int DEPTH>
+template <int NT, int GROUPS, int TILES, int UNIT>
 cudaError_t run(const W4Args& a, cudaStream_t s, int sms, int device) {
   static std::atomic<bool> ready[64];               // per device: the kernel may use this much shared memory
   if (device < 0 || device >= 64 || !ready[device].load(std::memory_order_acquire)) {
-    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS, TILES, UNIT, DEPTH>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS, TILES, UNIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
     if (e != cudaSuccess) return e;
     if (device >= 0 && device < 64) ready[device].store(true, std::memory_order_release);
   }
-  const int bytes = ring_bytes(TILES * UNIT, DEPTH, GROUPS) + part_bytes(TILES, NT) + (int)a.kblocks * kBlockK * 2 * a.M;
+  const int bytes = ring_bytes(TILES * UNIT, GROUPS) + part_bytes(TILES, NT) + (int)a.kblocks * kBlockK * 2 * a.M;
   const int64_t runs = (a.tiles + TILES - 1) / TILES;
   const int grid = (int)(runs < sms ? runs : sms);
   cudaLaunchConfig_t cfg{};
@@ -402,21 +403,19 @@ cudaError_t run(const W4Args& a, cudaStream_t s, int sms, int device) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, w4_kernel<NT, GROUPS, TILES, UNIT, DEPTH>, a);
+  return cudaLaunchKernelEx(&cfg, w4_kernel<NT, GROUPS, TILES, UNIT>, a);
 }
 
 template <int NT, int GROUPS>
 cudaError_t run_unit(const W4Args& a, cudaStream_t s, int sms, int device) {
   const int64_t grid = a.tiles < sms ? a.tiles : sms, x = a.kblocks * kBlockK * 2 * a.M;
-  constexpr int kFull = GROUPS == 4 ? 4 : 5;
   if constexpr (NT == 1) {
-    if (a.tiles >= 8 * sms && x <= x_bytes(1, 2, 1, 3, GROUPS)) return run<1, GROUPS, 2, 1, 3>(a, s, sms, device);
+    if (a.tiles >= 8 * sms && x <= x_bytes(1, 2, 1, GROUPS)) return run<1, GROUPS, 2, 1>(a, s, sms, device);
     // (with fewer units than these half of the warps would be idle)
-    if (a.kblocks % 2 == 0 && a.tiles * a.kblocks >= 4 * kWarps * grid && x <= x_bytes(1, 1, 2, 3, GROUPS))
-      return run<1, GROUPS, 1, 2, 3>(a, s, sms, device);
+    if (a.kblocks % 2 == 0 && a.tiles * a.kblocks >= 4 * kWarps * grid && x <= x_bytes(1, 1, 2, GROUPS))
+      return run<1, GROUPS, 1, 2>(a, s, sms, device);
   }
-  if (x <= x_bytes(NT, 1, 1, kFull, GROUPS)) return run<NT, GROUPS, 1, 1, kFull>(a, s, sms, device);
-  return run<NT, GROUPS, 1, 1, 3>(a, s, sms, device);
+  return run<NT, GROUPS, 1, 1>(a, s, sms, device);
 }
 
 template <int NT>
@@ -450,7 +449,7 @@ cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms) {
 int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M) {
   const int groups = kBlockK / group;
   int64_t m = M < kW4MaxTokens ? M : kW4MaxTokens;
-  while (m > 1 && m * blocks_of(N, K) * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, 1, 1, 3, groups)) --m;
+  while (m > 1 && m * blocks_of(N, K) * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, 1, 1, groups)) --m;
   const int64_t launches = (M + m - 1) / m;
   return (int)((M + launches - 1) / launches);
 }
@@ -458,7 +457,7 @@ int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M) {
 cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms, int device) {
   a.tiles = (a.N + kTileRows - 1) / kTileRows;
   a.kblocks = blocks_of(a.N, a.K);
-  static_assert(kW4MaxK * 2 <= x_bytes(1, 1, 1, 3, 4), "one token fits");
+  static_assert(kW4MaxK * 2 <= x_bytes(1, 1, 1, 4), "one token fits");
   if (a.M <= 8) return run_groups<1>(a, group, s, sms, device);
   if (a.M <= 16) return run_groups<2>(a, group, s, sms, device);
   return run_groups<4>(a, group, s, sms, device);
