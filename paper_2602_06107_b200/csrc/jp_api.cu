@@ -949,7 +949,7 @@ jp_status jp_w4_linear(jp_ctx* c, const jp_w4_desc* d, const void* packed, const
   for (int64_t m = 0; m < M; m += a.M) {
     a.x = (const char*)x + m * ld_x * 2;
     a.out = (char*)out + m * ld_out * (a.out_bf16 ? 2 : 4);
-    a.M = w4_tokens_per_launch(d->N, d->K, d->group, M - m);
+    a.M = w4_tokens_per_launch(d->N, d->K, d->group, M - m, c->sms);
     const cudaError_t e = launch_w4(a, d->group, c->stream, c->sms, c->device);
     if (e != cudaSuccess) return cuda_fail(c, e, "4-bit linear layer launch");
     c->launches += 1;

@@ -292,9 +292,10 @@ struct W4Args {
   int32_t M;
   bool out_bf16;           // else fp32
   int64_t tiles, kblocks;  // set by the launch
+  int32_t split;           // CTAs that share the columns of a tile
 };
 size_t w4_packed_bytes(int64_t N, int64_t K, int group);
-int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M);
+int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M, int sms);
 cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms);
 cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms, int device);
 

@@ -94,26 +94,48 @@ __device__ __forceinline__ void store_tile(const W4Args& A, const float (&acc)[N
     }
 }
 
-template <int NT, int GROUPS, int TILES, int UNIT>
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// 16 bytes at this place in the shared memory of another CTA of the cluster
+__device__ __forceinline__ float4 load_cluster(const float4* p, int cta) {
+  uint32_t at;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+// SPLIT: the CTAs of a cluster share a run of tiles and take a part of the columns each; the tiles' sums stay in shared memory, and
+// at the end every CTA adds those of some tiles, in the cluster's order.
+template <int NT, int GROUPS, int TILES, int UNIT, bool SPLIT>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   static_assert(TILES == 1 || UNIT == 1, "a unit is blocks of one tile, or a block of two");
+  static_assert(!SPLIT || TILES * UNIT == 1, "units of one block");
   constexpr int kBlock = block_bytes(GROUPS), kBytes = UNIT * TILES * kBlock;
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   char* ring = smem + warp * kDepth * kBytes;
   float4* parts = (float4*)(smem + ring_bytes(TILES * UNIT, GROUPS));                 // [warp][TILES][NT][lane]: of a tile that an earlier warp begins
-  uint4* xs = (uint4*)(smem + ring_bytes(TILES * UNIT, GROUPS) + part_bytes(TILES, NT));     // [block][step pair][token][lane % 4]
-  const int kblocks = (int)A.kblocks;
+  const int row_blocks = (int)A.kblocks;
   const int64_t runs = TILES == 1 ? A.tiles : (A.tiles + 1) / 2;        // (below, a tile is a pair of them)
-  const int64_t tile0 = runs * blockIdx.x / gridDim.x, tile1 = runs * (blockIdx.x + 1) / gridDim.x;
+  const int ctas = SPLIT ? A.split : 1, rank = SPLIT ? blockIdx.x % ctas : 0;
+  const int64_t run = blockIdx.x / ctas, all_runs = gridDim.x / ctas;
+  const int64_t tile0 = runs * run / all_runs, tile1 = runs * (run + 1) / all_runs;
+  const int kb0 = SPLIT ? row_blocks * rank / ctas : 0, kblocks = SPLIT ? row_blocks * (rank + 1) / ctas - kb0 : row_blocks;       // this CTA's
+  float4* sums = (float4*)(smem + ring_bytes(TILES * UNIT, GROUPS) + part_bytes(TILES, NT));     // (SPLIT) [tile][NT][lane]
+  uint4* xs = (uint4*)sums + (SPLIT ? (tile1 - tile0) * NT * 32 : 0);        // [block][step pair][token][lane % 4]
   const int tile_units = kblocks / UNIT;
   const int64_t blocks = (tile1 - tile0) * tile_units;      // (units)
   const int64_t b0 = blocks * warp / kWarps, b1 = blocks * (warp + 1) / kWarps;
   const int count = (int)(b1 - b0);
   const char* src;
-  int in_kb = 0;                                            // (pairs) block of the next unit to load, and where the second tile's is
+  int in_kb = 0;                                            // (SPLIT, pairs) block of the next unit to load, and where the second tile's is
   int64_t in_tile = 0, second = 0;
-  if constexpr (TILES == 1) {
+  if constexpr (SPLIT) {
+    in_kb = (int)(b0 % kblocks);
+    src = (const char*)A.packed + ((tile0 + b0 / kblocks) * row_blocks + kb0 + in_kb) * kBlock + lane * 16;
+  } else if constexpr (TILES == 1) {
     src = (const char*)A.packed + (tile0 * tile_units + b0) * kBytes + lane * 16;
   } else {
     in_tile = tile0 + b0 / tile_units;
@@ -131,6 +153,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
         for (int c = 0; c < kBytes; c += 512)
           if (c + 512 <= kBytes || lane * 16 < kBytes - c) copy16(ring + slot_in + c + lane * 16, src + c);
         src += kBytes;
+        if (SPLIT && ++in_kb == kblocks) {
+          in_kb = 0;
+          src += (int64_t)(row_blocks - kblocks) * kBlock;
+        }
       } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -159,7 +185,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
   if ((starts & 15) == 0) {                                 // a lane takes units, a warp eight step pairs of one token to one of eight
     const int some = A.M > 4 ? 3 : A.M > 2 ? 2 : A.M - 1, r = lane >> 2, pairs = 8 >> some;
     for (int sp = warp * pairs + (r >> some); sp < 4 * kblocks; sp += kWarps * pairs) {
-      const int k = sp * 32 + (lane & 3) * 8, bytes = k < A.K ? (A.K - k < 8 ? (int)(A.K - k) * 2 : 16) : 0;        // the rest is zeros
+      const int k = kb0 * kBlockK + sp * 32 + (lane & 3) * 8, bytes = k < A.K ? (A.K - k < 8 ? (int)(A.K - k) * 2 : 16) : 0;        // the rest is zeros
       const uint16_t* xr = (const uint16_t*)A.x + (bytes ? k : 0);
       uint4* to = xs + sp * A.M * 4 + (lane & 3);
 #pragma unroll 1
@@ -169,7 +195,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
     }
   } else {                                                  // a lane takes two columns, a warp half a block's, token after token
     for (int half = warp; half < 2 * kblocks; half += kWarps) {
-      const int k = half * 64 + lane * 2;
+      const int k = kb0 * kBlockK + half * 64 + lane * 2;
       const int valid = k + 1 < A.K ? 4 : k < A.K ? 2 : 0;  // bytes; the rest is filled with zeros
       const uint16_t* xr = (const uint16_t*)A.x + (valid ? k : 0);
       uint32_t* to = (uint32_t*)(xs + (half * 2 + (lane >> 4)) * A.M * 4) + (lane & 15);
@@ -219,6 +245,17 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
         parts[((warp * TILES + j) * NT + t) * 32 + lane] = make_float4(acc[j][t][0], acc[j][t][1], acc[j][t][2], acc[j][t][3]);
   };
   int64_t tile = b0 / tile_units;                   // within the CTA's run
+  auto put_tile = [&]() {
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) {
+      if constexpr (SPLIT) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sums[(tile * NT + t) * 32 + lane] = make_float4(acc[j][t][0], acc[j][t][1], acc[j][t][2], acc[j][t][3]);
+      } else {
+        store_tile<NT>(A, acc[j], (tile0 + tile) * TILES + j, lane);
+      }
+    }
+  };
   int kb = (int)(b0 - tile * tile_units);
   bool whole = kb == 0;                             // this warp has the tile from its first block on
   const int row = lane >> 2;
@@ -304,8 +341,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
     x_at += UNIT * 4 * x_pair;
     if (++kb == tile_units) {
       if (whole) {
-#pragma unroll
-        for (int j = 0; j < TILES; ++j) store_tile<NT>(A, acc[j], (tile0 + tile) * TILES + j, lane);
+        put_tile();
       } else {
         keep_part();
       }
@@ -339,8 +375,25 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(W4Args A) {
           acc[j][t][0] += v.x; acc[j][t][1] += v.y; acc[j][t][2] += v.z; acc[j][t][3] += v.w;
         }
     }
+    put_tile();
+  }
+  if constexpr (SPLIT) {
+    cluster_sync();
+    for (int64_t i = rank + (int64_t)warp * ctas; i < tile1 - tile0; i += (int64_t)kWarps * ctas) {
+      float sum[NT][4];
 #pragma unroll
-    for (int j = 0; j < TILES; ++j) store_tile<NT>(A, acc[j], (tile0 + tile) * TILES + j, lane);
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[t][e] = 0.f;
+      for (int o = 0; o < ctas; ++o)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float4 v = load_cluster(sums + (i * NT + t) * 32 + lane, o);
+          sum[t][0] += v.x; sum[t][1] += v.y; sum[t][2] += v.z; sum[t][3] += v.w;
+        }
+      store_tile<NT>(A, sum, tile0 + i, lane);
+    }
+    cluster_sync();                                 // (no CTA leaves while its sums are read)
   }
 }
 
@@ -382,33 +435,72 @@ __global__ void __launch_bounds__(256) w4_pack_kernel(W4PackArgs A) {
   }
 }
 
-template <int NT, int GROUPS, int TILES, int UNIT>
+// Clusters of `split` CTAs that are resident at once, or fewer (a cluster is within one of the groups that the SMs form, and each of these
+// has some left over: 74, 33 and 15 of 2, 4 and 8), and the shared memory a CTA needs for its part of x and its run's sums.
+int split_runs(int64_t tiles, int split, int sms) {
+  const int64_t most = sms > 6 * split ? (sms - 5 * (split - 1)) / split : 1;
+  return (int)(tiles < most ? tiles : most);
+}
+int64_t split_bytes(int64_t tiles, int64_t kblocks, int64_t M, int nt, int split, int sms) {
+  const int runs = split_runs(tiles, split, sms);
+  return (tiles + runs - 1) / runs * nt * 512 + (kblocks + split - 1) / split * kBlockK * 2 * M;
+}
+constexpr int kMaxSplit = 8;
+// CTAs that share the columns of a tile, 1: none.  Two or more where the tokens' x does not fit beside the ring (it would take a launch
+// for each part of the tokens, each reading the weights again), as few as fit with the run's sums (30 tokens, 9217 x 8192: 51 us in
+// launches, 29 in clusters of eight); and where tiles are few, so that more SMs work (28 tokens, 109 x 6274: 26 us, 7.8; one token,
+// 256 x 8192: 5.3, 4.1).
+int split_of(int64_t tiles, int64_t kblocks, int groups, int64_t M, int sms) {
+  const int nt = M <= 8 ? 1 : M <= 16 ? 2 : 4;
+  const int64_t room = x_bytes(nt, 1, 1, groups);
+  const bool fits = M * kblocks * kBlockK * 2 <= room;
+  int best = 1;
+  for (int split = 2; split <= kMaxSplit && split <= kblocks; split *= 2) {
+    if (split_bytes(tiles, kblocks, M, nt, split, sms) > room) continue;
+    if (fits && !(tiles * split * 2 <= sms && kblocks >= 8 * split)) break;
+    best = split;
+    if (!fits) break;
+  }
+  return best;
+}
+
+template <int NT, int GROUPS, int TILES, int UNIT, bool SPLIT = false>
 cudaError_t run(const W4Args& a, cudaStream_t s, int sms, int device) {
   static std::atomic<bool> ready[64];               // per device: the kernel may use this much shared memory
   if (device < 0 || device >= 64 || !ready[device].load(std::memory_order_acquire)) {
-    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS, TILES, UNIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+    const cudaError_t e = cudaFuncSetAttribute(w4_kernel<NT, GROUPS, TILES, UNIT, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
     if (e != cudaSuccess) return e;
     if (device >= 0 && device < 64) ready[device].store(true, std::memory_order_release);
   }
-  const int bytes = ring_bytes(TILES * UNIT, GROUPS) + part_bytes(TILES, NT) + (int)a.kblocks * kBlockK * 2 * a.M;
   const int64_t runs = (a.tiles + TILES - 1) / TILES;
-  const int grid = (int)(runs < sms ? runs : sms);
+  int bytes, grid;
+  if constexpr (SPLIT) {
+    grid = split_runs(a.tiles, a.split, sms) * a.split;
+    bytes = kSharedBytes - x_bytes(NT, 1, 1, GROUPS) + (int)split_bytes(a.tiles, a.kblocks, a.M, NT, a.split, sms);
+  } else {
+    grid = (int)(runs < sms ? runs : sms);
+    bytes = ring_bytes(TILES * UNIT, GROUPS) + part_bytes(TILES, NT) + (int)a.kblocks * kBlockK * 2 * a.M;
+  }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kWarps * 32);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = s;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;     // set up while the kernel before it ends: 0.5 us a call
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, w4_kernel<NT, GROUPS, TILES, UNIT>, a);
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // set up while the kernel before it ends: 0.5 us a call
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = SPLIT ? a.split : 1;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = SPLIT ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, w4_kernel<NT, GROUPS, TILES, UNIT, SPLIT>, a);
 }
 
 template <int NT, int GROUPS>
 cudaError_t run_unit(const W4Args& a, cudaStream_t s, int sms, int device) {
   const int64_t grid = a.tiles < sms ? a.tiles : sms, x = a.kblocks * kBlockK * 2 * a.M;
+  if (a.split > 1) return run<NT, GROUPS, 1, 1, true>(a, s, sms, device);
   if constexpr (NT == 1) {
     if (a.tiles >= 8 * sms && x <= x_bytes(1, 2, 1, GROUPS)) return run<1, GROUPS, 2, 1>(a, s, sms, device);
     // (with fewer units than these half of the warps would be idle)
@@ -446,8 +538,9 @@ cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms) {
 }
 
 // Tokens of one launch, of M that are left: as many as shared memory holds of x (one always fits), the launches even.
-int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M) {
+int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M, int sms) {
   const int groups = kBlockK / group;
+  if (split_of((N + kTileRows - 1) / kTileRows, blocks_of(N, K), groups, M, sms) > 1) return (int)M;
   int64_t m = M < kW4MaxTokens ? M : kW4MaxTokens;
   while (m > 1 && m * blocks_of(N, K) * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, 1, 1, groups)) --m;
   const int64_t launches = (M + m - 1) / m;
@@ -457,6 +550,7 @@ int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M) {
 cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms, int device) {
   a.tiles = (a.N + kTileRows - 1) / kTileRows;
   a.kblocks = blocks_of(a.N, a.K);
+  a.split = split_of(a.tiles, a.kblocks, kBlockK / group, a.M, sms);
   static_assert(kW4MaxK * 2 <= x_bytes(1, 1, 1, 4), "one token fits");
   if (a.M <= 8) return run_groups<1>(a, group, s, sms, device);
   if (a.M <= 16) return run_groups<2>(a, group, s, sms, device);

@@ -261,3 +261,19 @@ def test_pairs_of_tiles(ctx, N, K, group):
         check(out, x, ref, group)
         assert (big[0] == 7).all() and (big[-1] == 7).all() and (big[:, N:] == 7).all()
         assert torch.equal(runner.linear_w4(ctx, x, w, out_dtype=torch.float32), out)
+
+
+@gpu
+@pytest.mark.parametrize("N,K,M", [(109, 6274, 28), (292, 2447, 32), (9217, 8126, 30), (1, 40000, 2), (16, 65536, 9), (700, 1100, 1),
+                                   (4000, 8192, 13), (33, 3000, 7)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_columns_split_over_a_cluster(ctx, N, K, M, group):
+    """Few rows with many columns, and more tokens than one block's shared memory holds; the same call gives the same bits."""
+    q, s, z = make(N, K, group, True, torch.bfloat16, seed=K)
+    w = runner.pack_w4(ctx, q, s, z, K=K, group=group)
+    big = torch.full((M + 2, N + 3), 7.0, device="cuda")
+    x = tokens(M, K, seed=M)
+    out = runner.linear_w4(ctx, x, w, out=big[1:M + 1, :N])
+    check(out, x, unpacked(q, s, z, K, group), group)
+    assert (big[0] == 7).all() and (big[-1] == 7).all() and (big[:, N:] == 7).all()
+    assert torch.equal(runner.linear_w4(ctx, x, w, out_dtype=torch.float32), out)
