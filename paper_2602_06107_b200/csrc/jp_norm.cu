@@ -267,11 +267,11 @@ struct Rows {
   }
 };
 
-// The same for matrices whose rows start at different offsets to 16 bytes: the group copies the 16-byte vectors that cover a row (a row's place begins at the row's own
-// offset to 16 bytes), and every thread reads its elements once all have arrived.  Vectors that reach beyond the matrix, in its first
-// and last row, are copied element by element.  The place is free again after the barrier of the row's first sum.  (With element loads
-// into registers, one row ahead, 8192 x 4095 bf16 took 147 us forward and 225 us backward; this 70 and 93, rows of one offset as spans
-// 34 and 69.)
+// The same for matrices whose rows start at different offsets to 16 bytes: the group copies the 16-byte vectors that cover a row (a row's
+// place begins at the row's own offset), and every thread reads its elements once all have arrived.  Vectors that reach beyond the
+// matrix, in its first and last row, are copied element by element.  The place is free again after the barrier of the row's first sum.
+// (With element loads into registers, one row ahead, 8192 x 4095 bf16 took 147 us forward and 225 us backward; this 70 and 93, rows of
+// one offset as spans 34 and 69.)
 __host__ __device__ inline int span_bytes(int64_t H, int es) { return (int)((H * es + 15) / 16 + 1) * 16; }
 template <int DT, int NV, int NT, int STAGES>
 struct Rows<DT, 1, NV, NT, false, STAGES> {

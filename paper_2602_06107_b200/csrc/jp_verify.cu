@@ -12,8 +12,8 @@
 // verify_rows_kernel sums 2^((z - R) c) over slices of rows (c = log2 e / temperature).  The reference R need not be the maximum: fp32
 // has 2^+-126 of room.  So it is the largest of the slice's first 8 KB, and the loop has no running maximum: one unpack, one
 // FMA, one ex2 and one add an element; 16 terms (fp32 input: 8) are added in fp32, the rest in fp64.  Terms that reach
-// 256 together (a peak outside the sample: exponents of 8 and more are rounded by more than 2^-22) are taken again in fp64, and a slice whose sum leaves
-// 2^-60 .. 2^60 from its own maximum.
+// 256 together (a peak outside the sample: exponents of 8 and more are rounded by more than 2^-22) are taken again in fp64, and a slice
+// whose sum leaves 2^-60 .. 2^60 from its own maximum.
 //
 // verify_draw_kernel takes the decisions of a sequence (again in every block: cheaper than a launch of its own) and then the
 // masses of the row to draw from, by segments.  Which token a draw hits depends on sums over the vocabulary next to a

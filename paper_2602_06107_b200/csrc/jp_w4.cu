@@ -7,12 +7,13 @@
 // fp32 sum.  (tcgen05 would need the 16-bit weights written to shared memory or TMEM first, 92 of the 128 bytes a
 // clock that shared memory moves, and a TMEM read per group for the scales; with 1 to 32 tokens its rate is of no use.)
 //
-// Weights are laid out once (pack_kernel) in the order the MMA's A fragments want them: tiles of 16 rows, blocks of 128
-// columns, per block 8 steps of k = 16.  Which of a group's columns make a step is free as long as A and B agree: two steps take 32
-// columns, lane t of a row's four 8 t .. 8 t + 7, so that a lane's x of two steps are 16 bytes of memory.  A lane's 8 weights of a step are one 32-bit word whose nibbles j and j + 4 are the
-// two halves of fragment register j: four masks, one shift and four packed multiply-adds (scaled2) make the fragment.  A block is 1024 bytes of words, then one 32-bit word per
-// (row, group): the scale as fp32 with its low 4 bits replaced by z (scales come in bf16 or fp16: those bits are zero).
-// Blocks of a tile follow one another, tiles too: what a warp reads is one contiguous run of memory.
+// Weights are laid out once (pack_kernel) in the order the MMA's A fragments want them: tiles of 16 rows, blocks of 128 columns, per
+// block 8 steps of k = 16.  Which of a group's columns make a step is free as long as A and B agree: two steps take 32 columns, lane t of
+// a row's four 8 t .. 8 t + 7, so that a lane's x of two steps are 16 bytes of memory.  A lane's 8 weights of a step are one 32-bit word
+// whose nibbles j and j + 4 are the two halves of fragment register j: four masks, one shift and four packed multiply-adds (scaled2) make
+// the fragment.  A block is 1024 bytes of words, then one 32-bit word per (row, group): the scale as fp32 with its low 4 bits replaced by
+// z (scales come in bf16 or fp16: those bits are zero).  Blocks of a tile follow one another, tiles too: what a warp reads is one
+// contiguous run of memory, or a few.
 //
 // Work split: a CTA takes a contiguous run of tiles, and its 16 warps take equal contiguous runs of the CTA's blocks,
 // whatever the tile boundaries.  So every size keeps all warps busy to within one block; a tile that two or more warps share is

@@ -277,3 +277,30 @@ def test_columns_split_over_a_cluster(ctx, N, K, M, group):
     check(out, x, unpacked(q, s, z, K, group), group)
     assert (big[0] == 7).all() and (big[-1] == 7).all() and (big[:, N:] == 7).all()
     assert torch.equal(runner.linear_w4(ctx, x, w, out_dtype=torch.float32), out)
+
+
+@gpu
+@pytest.mark.parametrize("N,K,M", [(109, 6274, 28), (19000, 300, 3), (9217, 4100, 32)])
+def test_every_kind_of_launch_in_graphs_on_two_streams(ctx, N, K, M):
+    """A captured call reads its inputs anew, and two of them may run at the same time."""
+    q, s, z = make(N, K, 64, True, torch.bfloat16, seed=N)
+    w = runner.pack_w4(ctx, q, s, z, K=K, group=64)
+    xs, outs, graphs, streams = [], [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i in range(2):
+        xs.append(tokens(M, K, seed=i).clone())
+        runner.linear_w4(ctx, xs[i], w)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(runner.linear_w4(ctx, xs[i], w, out_dtype=torch.float32))
+        graphs.append(g)
+    for again in range(3):
+        for i in range(2):
+            xs[i].copy_(tokens(M, K, seed=10 * again + i))
+        torch.cuda.synchronize()
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(outs[i], runner.linear_w4(ctx, xs[i], w, out_dtype=torch.float32))
