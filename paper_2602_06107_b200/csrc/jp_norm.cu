@@ -76,6 +76,22 @@ template <int DT> struct Access<DT, 1> {
   }
 };
 
+// Two fp32 operations in one instruction: at 8192 x 4096 both passes are as much bound by issue as by HBM (forward with bias 31 us
+// without, 28.5; backward of RMS norm 41, 39.5).  x r - mu r is one of them: off by 2^-24 (|x| + |mu|) r, as mu itself is.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  asm("{.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;}" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
+  return a;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  asm("{.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;}" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
+  return a;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  asm("{.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%0, %1};\n\tfma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;}"
+      : "+f"(c.x), "+f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -271,7 +287,7 @@ struct Rows {
 // place begins at the row's own offset), and every thread reads its elements once all have arrived.  Vectors that reach beyond the
 // matrix, in its first and last row, are copied element by element.  The place is free again after the barrier of the row's first sum.
 // (With element loads into registers, one row ahead, 8192 x 4095 bf16 took 147 us forward and 225 us backward; this 70 and 93, rows of
-// one offset as spans 34 and 69.)
+// one offset as spans 34 and 62.)
 __host__ __device__ inline int span_bytes(int64_t H, int es) { return (int)((H * es + 15) / 16 + 1) * 16; }
 template <int DT, int NV, int NT, int STAGES>
 struct Rows<DT, 1, NV, NT, false, STAGES> {
@@ -442,21 +458,9 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
   }
 }
 
-// Two fp32 operations in one instruction: at 8192 x 4096 with bias the forward is as much bound by issue as by HBM (31 us without, 28.5).
-// x r - mu r is one of them: off by 2^-24 (|x| + |mu|) r, as mu itself is.
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  asm("{.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;}" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
-  return a;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  asm("{.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%0, %1};\n\tfma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;}"
-      : "+f"(c.x), "+f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return c;
-}
-
 // One warp a row, NVL vectors a lane, for many rows of up to 5120 bf16 or 2560 fp32: the reductions are shuffles and no row waits for
 // another (a block a row, with a barrier for each of its two sums, took 48 us at 8192 x 4096 with bias in bf16 and 52 at 6553 x 5120; this
-// takes 30 and 36).  Weight and bias are in shared memory beside the rows to come; wider rows leave too few warps an SM (at 4096 x 8192,
+// takes 28 and 31).  Weight and bias are in shared memory beside the rows to come; wider rows leave too few warps an SM (at 4096 x 8192,
 // five of them, RMS norm, 42 us; a block a row 40).
 constexpr int kWarpStages = 2;
 __host__ __device__ constexpr int warp_rows(int nvl) { return nvl == 20 ? 9 : 12; }   // rows a block
@@ -647,9 +651,9 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float (*sh)[N][kMaxWar
 __device__ __forceinline__ void keep_packed(uint4& v) { asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)); }
 __device__ __forceinline__ void keep_packed(uint32_t& v) { asm volatile("" : "+r"(v)); }
 
-// Rows a group takes at a time, so that their sums share a barrier: at 8192 x 4096 (RMS norm, bf16) one at a time takes 55 us, two 41;
-// four do not fit the registers (67), but for 4 fp32 a thread (16000 x 768: two 37 us, four 28).  With their edges rows of 2 x 8 bf16 a
-// thread fit one at a time (8192 x 4095: two 89 us, one 69).
+// Rows a group takes at a time, so that their sums share a barrier: at 8192 x 4096 (RMS norm, bf16) two take three quarters of
+// the time of one; four do not fit the registers (1.2 times), but for 4 fp32 a thread (16000 x 768: two 37 us, four 28).  With their edges rows of 2 x 8 bf16 a
+// thread fit one at a time (8192 x 4095: two 89 us, one 62).
 __host__ __device__ constexpr int bwd_rows(int w, int nv, bool off) { return w == 1 || nv == 4 || (off && w == 8 && nv == 2) ? 1 : w == 4 && nv == 1 ? 4 : 2; }
 
 template <int DT, int W, int NV, bool PB, bool BIAS, bool OFF>
@@ -718,22 +722,39 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
     fetch_stats(row + R * step);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      float s1 = 0.f, s2 = 0.f;
+      float2 s1v = make_float2(0.f, 0.f), s2v = make_float2(0.f, 0.f);
       const float shift = -mean[r] * rstd[r];
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         float x[W], dy[W];
         Ac::unpack(raw[r][0][i], x);
         Ac::unpack(raw[r][1][i], dy);                       // (0 past the end, and so is everything below)
+        if constexpr (W > 1) {
 #pragma unroll
-        for (int e = 0; e < W; ++e) {
-          const float xh = fmaf(x[e], rstd[r], shift), g = dy[e] * w[i][e];
-          s1 += g;
-          s2 = fmaf(g, xh, s2);
-          dw[i][e] = fmaf(dy[e], xh, dw[i][e]);
-          if (BIAS) db[i][e] += dy[e];
+          for (int e = 0; e < W; e += 2) {
+            const float2 d = make_float2(dy[e], dy[e + 1]);
+            const float2 xh = fma2(make_float2(x[e], x[e + 1]), make_float2(rstd[r], rstd[r]), make_float2(shift, shift));
+            const float2 g = mul2(d, make_float2(w[i][e], w[i][e + 1]));
+            s1v = add2(s1v, g);
+            s2v = fma2(g, xh, s2v);
+            const float2 dwe2 = fma2(d, xh, make_float2(dw[i][e], dw[i][e + 1]));
+            dw[i][e] = dwe2.x;
+            dw[i][e + 1] = dwe2.y;
+            if (BIAS) {
+              const float2 dbe2 = add2(make_float2(db[i][e], db[i][e + 1]), d);
+              db[i][e] = dbe2.x;
+              db[i][e + 1] = dbe2.y;
+            }
+          }
+        } else {
+          const float xh = fmaf(x[0], rstd[r], shift), g = dy[0] * w[i][0];
+          s1v.x += g;
+          s2v.x = fmaf(g, xh, s2v.x);
+          dw[i][0] = fmaf(dy[0], xh, dw[i][0]);
+          if (BIAS) db[i][0] += dy[0];
         }
       }
+      float s1 = s1v.x + s1v.y, s2 = s2v.x + s2v.y;
       if (OFF) {
         const float xh = fmaf(edge[r][0], rstd[r], shift), g = edge[r][1] * we;
         s1 += g;
@@ -770,7 +791,17 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
           Ac::unpack(raw[r][0][i], x);
           Ac::unpack(raw[r][1][i], dy);
 #pragma unroll
-          for (int e = 0; e < W; ++e) o[e] = fmaf(dy[e] * w[i][e], rstd[r], fmaf(x[e], c1, c0));
+          for (int e = 0; e < W; e += 2) {
+            if constexpr (W > 1) {
+              const float2 g = mul2(make_float2(dy[e], dy[e + 1]), make_float2(w[i][e], w[i][e + 1]));
+              const float2 rest = fma2(make_float2(x[e], x[e + 1]), make_float2(c1, c1), make_float2(c0, c0));
+              const float2 d = fma2(g, make_float2(rstd[r], rstd[r]), rest);
+              o[e] = d.x;
+              o[e + 1] = d.y;
+            } else {
+              o[e] = fmaf(dy[e] * w[i][e], rstd[r], fmaf(x[e], c1, c0));
+            }
+          }
           Ac::store(out + (int64_t)i * (int)blockDim.x * W * ES, o);
         }
       }
