@@ -652,8 +652,8 @@ __device__ __forceinline__ void keep_packed(uint4& v) { asm volatile("" : "+r"(v
 __device__ __forceinline__ void keep_packed(uint32_t& v) { asm volatile("" : "+r"(v)); }
 
 // Rows a group takes at a time, so that their sums share a barrier: at 8192 x 4096 (RMS norm, bf16) two take three quarters of
-// the time of one; four do not fit the registers (1.2 times), but for 4 fp32 a thread (16000 x 768: two 37 us, four 28).  With their edges rows of 2 x 8 bf16 a
-// thread fit one at a time (8192 x 4095: two 89 us, one 62).
+// the time of one; four do not fit the registers (1.2 times), but for 4 fp32 a thread (16000 x 768: two 37 us, four 28).  With their edges
+// rows of 2 x 8 bf16 a thread fit one at a time (8192 x 4095: two 89 us, one 62).
 __host__ __device__ constexpr int bwd_rows(int w, int nv, bool off) { return w == 1 || nv == 4 || (off && w == 8 && nv == 2) ? 1 : w == 4 && nv == 1 ? 4 : 2; }
 
 template <int DT, int W, int NV, bool PB, bool BIAS, bool OFF>

@@ -325,14 +325,14 @@ def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_ac
     n_seq, rows, V = target_logits.shape
     N = rows - 1
     ld, seq = _positions(target_logits, (n_seq, rows, V), "target_logits")
-    ld_d = seq_d = 0
+    dtype, ld_d, seq_d = B._dtype_code(target_logits), 0, 0
     if draft_logits is not None:
         if draft_logits.dtype is not target_logits.dtype:
             raise B.JackpotError("draft_logits must have target_logits' dtype")
         if draft_logits.dim() != 3:
             raise B.JackpotError("draft_logits must be [B, N, V]")
         ld_d, seq_d = _positions(draft_logits, (n_seq, N, V), "draft_logits")
-    d = B._desc(ctx, B.jp_verify_desc, n_seq, V, ld, seq, ld_d, seq_d, N, B._dtype_code(target_logits))
+    d = B._desc(ctx, B.jp_verify_desc, n_seq, V, ld, seq, ld_d, seq_d, N, dtype)
     _dense(draft_tokens, (n_seq, N), torch.int32, "draft_tokens")
     _dense(u_accept, (n_seq, N), torch.float32, "u_accept")
     _dense(u_sample, (n_seq,), torch.float32, "u_sample")
