@@ -871,7 +871,10 @@ __global__ void __launch_bounds__(1024) norm_bwd_wide_kernel(NormArgs A) {
   const float inv_h = 1.f / (float)A.H;
   const int per_group = A.dbias ? 2 : 1;
   float* pw = A.partial + (int64_t)blockIdx.x * per_group * A.H;
-  for (int64_t c = threadIdx.x; c < per_group * A.H; c += blockDim.x) pw[c] = 0.f;
+  for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x) {             // (the thread that adds to a place empties it: no barrier)
+    pw[c] = 0.f;
+    if (A.dbias) pw[A.H + c] = 0.f;
+  }
   for (int64_t row = blockIdx.x; row < A.T; row += gridDim.x) {
     const char* x = (const char*)A.x + row * A.ld_x * ES;
     const char* dy = (const char*)A.dy + row * A.ld_dy * ES;

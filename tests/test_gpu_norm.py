@@ -320,3 +320,24 @@ def test_refusals(ctx):
             B.jp_layer_norm_forward(ctx, e, x, w, b, y, None, None)
     B.jp_layer_norm_forward(ctx, d, x, w, b, y, None, None)            # the context works as before
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,H", [(5, 8200), (300, 13824), (160, 20011), (3, 8191 * 3)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_wide_backward_does_not_depend_on_what_the_workspace_held(ctx, T, H, dtype):
+    """Widths beyond the registers that are no multiple of the block's 1024 threads: the place of dbias[c] is emptied by the thread that
+    adds to it.  Every call, on a workspace of NaN or of large numbers, gives the same bits."""
+    x, dy, w, b = make(T, H, dtype, torch.float32, True, seed=T + H)
+    _, mean, rstd = runner.layer_norm(ctx, x, w, b, eps=EPS)
+    d = B.jp_norm_desc(T=T, H=H, dtype=B._dtype_code(x), param_dtype=B.JP_F32)
+    need = B.jp_layer_norm_workspace_bytes(ctx, T, H, d.dtype)
+    ws = torch.empty(need // 4, device="cuda")
+    first = None
+    for i in range(40):
+        ws.fill_(float("nan") if i % 2 else 1e30)
+        dx, dw, db = torch.empty_like(x), torch.empty(H, device="cuda"), torch.empty(H, device="cuda")
+        B.jp_layer_norm_backward(ctx, d, dy, x, w, mean, rstd, dx, dw, db, ws.view(torch.uint8))
+        if first is None:
+            first = (dx, dw, db)
+            check_backward(first, dy, x, w, mean, rstd, False)
+        assert all(torch.equal(a, c) for a, c in zip(first, (dx, dw, db)))
