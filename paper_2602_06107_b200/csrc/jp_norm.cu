@@ -973,10 +973,14 @@ int grid_for(int64_t T, const Plan& p, int sms, bool backward, int period) {
   return (int)(cap < period ? period : cap / period * period);
 }
 
-template <class K>
-cudaError_t launch(K* kernel, const NormArgs& a, dim3 grid, dim3 block, int smem, cudaStream_t s) {
+// The limit of dynamic shared memory belongs to the kernel on the device, for all contexts and threads: every call sets it to the same
+// amount, whatever its width, so that none lowers it under another between its setting and its launch.
+constexpr int kSharedBytes = 232448 - 2048;                 // of one block, less the static part of the widest kernel
+static_assert(kWarpStages * 16 * 32 * warp_rows(16) * 16 + 2 * 4096 * 4 <= kSharedBytes && kWarpStages * 20 * 32 * warp_rows(20) * 16 + 2 * 5120 * 4 <= kSharedBytes, "");
+template <auto kernel>
+cudaError_t launch(const NormArgs& a, dim3 grid, dim3 block, int smem, cudaStream_t s) {
   if (smem > 47 * 1024) {                                   // (with the static part beyond what a kernel has without asking)
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg{};
@@ -1001,7 +1005,7 @@ cudaError_t fwd_warp(const NormArgs& a, const RowsAt& at, cudaStream_t s, int sm
   const int smem = kWarpStages * NVL * 32 * kWarpRows * 16 +
                    param_bytes(a.H, PB ? 2 : 4) * (a.bias ? 2 : 1);
   const dim3 g((unsigned)(need < cap ? need : cap)), b(32, kWarpRows);
-  return off ? launch(norm_fwd_warp_kernel<DT, NVL, PB, true>, a, g, b, smem, s) : launch(norm_fwd_warp_kernel<DT, NVL, PB, false>, a, g, b, smem, s);
+  return off ? launch<norm_fwd_warp_kernel<DT, NVL, PB, true>>(a, g, b, smem, s) : launch<norm_fwd_warp_kernel<DT, NVL, PB, false>>(a, g, b, smem, s);
 }
 
 template <int DT, bool PB>
@@ -1024,16 +1028,16 @@ cudaError_t fwd(const NormArgs& a, cudaStream_t s, int sms) {
   const int smem = kStages * p.rows * (p.w > 1 ? p.nv * p.threads * 16 : span_bytes(a.H, Vec<DT>::ESIZE));
   if (p.nv == 0) { norm_fwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
   if (p.w == 1)
-    return p.nv == 2   ? launch(norm_fwd_kernel<DT, 1, 2, PB, false>, a, grid, b, smem, s)
-           : p.nv == 8 ? launch(norm_fwd_kernel<DT, 1, 8, PB, false>, a, grid, b, smem, s)
-                       : launch(norm_fwd_kernel<DT, 1, 16, PB, false>, a, grid, b, smem, s);
+    return p.nv == 2   ? launch<norm_fwd_kernel<DT, 1, 2, PB, false>>(a, grid, b, smem, s)
+           : p.nv == 8 ? launch<norm_fwd_kernel<DT, 1, 8, PB, false>>(a, grid, b, smem, s)
+                       : launch<norm_fwd_kernel<DT, 1, 16, PB, false>>(a, grid, b, smem, s);
   if (kind == kSpans)
-    return p.nv == 1   ? launch(norm_fwd_kernel<DT, VW, 1, PB, true>, a, grid, b, smem, s)
-           : p.nv == 2 ? launch(norm_fwd_kernel<DT, VW, 2, PB, true>, a, grid, b, smem, s)
-                       : launch(norm_fwd_kernel<DT, VW, 4, PB, true>, a, grid, b, smem, s);
-  if (p.nv == 1) return launch(norm_fwd_kernel<DT, VW, 1, PB, false>, a, grid, b, smem, s);
-  if (p.nv == 2) return launch(norm_fwd_kernel<DT, VW, 2, PB, false>, a, grid, b, smem, s);
-  return launch(norm_fwd_kernel<DT, VW, 4, PB, false>, a, grid, b, smem, s);
+    return p.nv == 1   ? launch<norm_fwd_kernel<DT, VW, 1, PB, true>>(a, grid, b, smem, s)
+           : p.nv == 2 ? launch<norm_fwd_kernel<DT, VW, 2, PB, true>>(a, grid, b, smem, s)
+                       : launch<norm_fwd_kernel<DT, VW, 4, PB, true>>(a, grid, b, smem, s);
+  if (p.nv == 1) return launch<norm_fwd_kernel<DT, VW, 1, PB, false>>(a, grid, b, smem, s);
+  if (p.nv == 2) return launch<norm_fwd_kernel<DT, VW, 2, PB, false>>(a, grid, b, smem, s);
+  return launch<norm_fwd_kernel<DT, VW, 4, PB, false>>(a, grid, b, smem, s);
 }
 
 template <int DT, bool PB, bool BIAS>
@@ -1043,18 +1047,18 @@ cudaError_t bwd(const NormArgs& a, const Plan& p, bool off, int grid, cudaStream
   const int smem = 2 * p.rows * (p.w > 1 ? 2 * bwd_rows(p.w, p.nv, off) * p.nv * p.threads * 16 : kStages * span_bytes(a.H, Vec<DT>::ESIZE));
   if (p.nv == 0) { norm_bwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
   if (p.w == 1)
-    return p.nv == 2   ? launch(norm_bwd_kernel<DT, 1, 2, PB, BIAS, false>, a, grid, b, smem, s)
-           : p.nv == 8 ? launch(norm_bwd_kernel<DT, 1, 8, PB, BIAS, false>, a, grid, b, smem, s)
-                       : launch(norm_bwd_kernel<DT, 1, 16, PB, BIAS, false>, a, grid, b, smem, s);
+    return p.nv == 2   ? launch<norm_bwd_kernel<DT, 1, 2, PB, BIAS, false>>(a, grid, b, smem, s)
+           : p.nv == 8 ? launch<norm_bwd_kernel<DT, 1, 8, PB, BIAS, false>>(a, grid, b, smem, s)
+                       : launch<norm_bwd_kernel<DT, 1, 16, PB, BIAS, false>>(a, grid, b, smem, s);
   if (off) {
-    if (p.nv == 1) return launch(norm_bwd_kernel<DT, VW, 1, PB, BIAS, true>, a, grid, b, smem, s);
-    if (p.nv == 2) return launch(norm_bwd_kernel<DT, VW, 2, PB, BIAS, true>, a, grid, b, smem, s);
-    if constexpr (DT == JP_F32) return launch(norm_bwd_kernel<DT, VW, 4, PB, BIAS, true>, a, grid, b, smem, s);
+    if (p.nv == 1) return launch<norm_bwd_kernel<DT, VW, 1, PB, BIAS, true>>(a, grid, b, smem, s);
+    if (p.nv == 2) return launch<norm_bwd_kernel<DT, VW, 2, PB, BIAS, true>>(a, grid, b, smem, s);
+    if constexpr (DT == JP_F32) return launch<norm_bwd_kernel<DT, VW, 4, PB, BIAS, true>>(a, grid, b, smem, s);
     return cudaErrorInvalidConfiguration;
   }
-  if (p.nv == 1) return launch(norm_bwd_kernel<DT, VW, 1, PB, BIAS, false>, a, grid, b, smem, s);
-  if (p.nv == 2) return launch(norm_bwd_kernel<DT, VW, 2, PB, BIAS, false>, a, grid, b, smem, s);
-  if constexpr (DT == JP_F32) return launch(norm_bwd_kernel<DT, VW, 4, PB, BIAS, false>, a, grid, b, smem, s);
+  if (p.nv == 1) return launch<norm_bwd_kernel<DT, VW, 1, PB, BIAS, false>>(a, grid, b, smem, s);
+  if (p.nv == 2) return launch<norm_bwd_kernel<DT, VW, 2, PB, BIAS, false>>(a, grid, b, smem, s);
+  if constexpr (DT == JP_F32) return launch<norm_bwd_kernel<DT, VW, 4, PB, BIAS, false>>(a, grid, b, smem, s);
   return cudaErrorInvalidConfiguration;
 }
 
