@@ -77,7 +77,8 @@ template <int DT> struct Access<DT, 1> {
 };
 
 // Two fp32 operations in one instruction: at 8192 x 4096 both passes are as much bound by issue as by HBM (forward with bias 31 us
-// without, 28.5; backward of RMS norm 41, 39.5).  x r - mu r is one of them: off by 2^-24 (|x| + |mu|) r, as mu itself is.
+// without, 28.5; backward of RMS norm 41, 39.5).  xhat is (x - mu) r in two of them, not x r + (-mu r) in one: rounding mu r would leave
+// 2^-24 |mu| r in every xhat, a thousand times its own rounding in a row whose mean is a thousand standard deviations.
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   asm("{.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;}" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
   return a;
@@ -466,7 +467,7 @@ constexpr int kWarpStages = 2;
 __host__ __device__ constexpr int warp_rows(int nvl) { return nvl == 20 ? 9 : 12; }   // rows a block
 __host__ __device__ constexpr int warp_blocks(int nvl) { return nvl >= 16 ? 1 : nvl == 8 ? 2 : 3; }      // per SM
 __host__ __device__ inline int param_bytes(int64_t H, int ps) { return ((int)H * ps + 15) / 16 * 16; }      // of one of them
-template <int DT, int NVL, bool PB, bool OFF>
+template <int DT, int NVL, bool PB, bool OFF, bool CENTER>
 __global__ void __launch_bounds__(32 * warp_rows(NVL), warp_blocks(NVL)) norm_fwd_warp_kernel(NormArgs A) {
   constexpr int kWarpRows = warp_rows(NVL);
   constexpr int W = Vec<DT>::N, ES = Vec<DT>::ESIZE, PS = PB ? 2 : 4;
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(32 * warp_rows(NVL), warp_blocks(NVL)) norm_fw
     uint4 (&v)[NVL] = rows[0];
     in.fetch();
     float mean = 0.f;
-    if (!A.rms) {
+    if (!A.rms) {                                           // (CENTER; as a branch, or the row stays unpacked from here on and spills)
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < NVL; ++i) {
@@ -536,20 +537,20 @@ __global__ void __launch_bounds__(32 * warp_rows(NVL), warp_blocks(NVL)) norm_fw
         Ac::unpack(v[i], t);
 #pragma unroll
         for (int e = 0; e < W; e += 2) {
-          const float2 d = add2(make_float2(t[e], t[e + 1]), less);
+          const float2 x = make_float2(t[e], t[e + 1]), d = CENTER ? add2(x, less) : x;
           sq = fma2(d, d, sq);
         }
       }
     float s2 = sq.x + sq.y;
     if (OFF && span.edge >= 0) s2 = fmaf(ve[0] - mean, ve[0] - mean, s2);
     const float rstd = 1.f / sqrtf(warp_sum(s2) * inv_h + A.eps);
-    const float2 scale = make_float2(rstd, rstd), shift = make_float2(-mean * rstd, -mean * rstd);
+    const float2 scale = make_float2(rstd, rstd);
     if (lane == 0) {
       if (A.out_mean) A.out_mean[row] = mean;
       if (A.out_rstd) A.out_rstd[row] = rstd;
     }
     if (OFF && span.edge >= 0) {
-      const float o = fmaf(fmaf(ve[0], rstd, shift.x), we, be);
+      const float o = fmaf((ve[0] - mean) * rstd, we, be);
       Access<DT, 1>::store((char*)A.y + (row * A.ld_y + span.edge) * ES, &o);
     }
     char* y = (char*)A.y + (row * A.ld_y + span.head) * ES;
@@ -564,7 +565,7 @@ __global__ void __launch_bounds__(32 * warp_rows(NVL), warp_blocks(NVL)) norm_fw
         if (b) q.read(b + c * PS);
 #pragma unroll
         for (int e = 0; e < W; e += 2) {
-          const float2 xh = fma2(make_float2(t[e], t[e + 1]), scale, shift);
+          const float2 x = make_float2(t[e], t[e + 1]), xh = mul2(CENTER ? add2(x, less) : x, scale);
           const float2 add = b ? make_float2(q.get(0, e), q.get(0, e + 1)) : make_float2(0.f, 0.f);
           const float2 r = fma2(xh, make_float2(p.get(0, e), p.get(0, e + 1)), add);
           o[e] = r.x;
@@ -653,13 +654,16 @@ __device__ __forceinline__ void keep_packed(uint32_t& v) { asm volatile("" : "+r
 
 // Rows a group takes at a time, so that their sums share a barrier: at 8192 x 4096 (RMS norm, bf16) two take three quarters of
 // the time of one; four do not fit the registers (1.2 times), but for 4 fp32 a thread (16000 x 768: two 37 us, four 28).  With their edges
-// rows of 2 x 8 bf16 a thread fit one at a time (8192 x 4095: two 89 us, one 62).
-__host__ __device__ constexpr int bwd_rows(int w, int nv, bool off) { return w == 1 || nv == 4 || (off && w == 8 && nv == 2) ? 1 : w == 4 && nv == 1 ? 4 : 2; }
+// rows of 2 x 8 bf16 a thread fit one at a time (8192 x 4095: two 89 us, one 66), and so do those of a layer norm with the bias's
+// gradient (sums: 8192 x 4096, two 58.6 us, one 51.9).
+__host__ __device__ constexpr int bwd_rows(int w, int nv, bool off, bool sums) {
+  return w == 1 || nv == 4 || ((off || sums) && w == 8 && nv == 2) ? 1 : w == 4 && nv == 1 ? 4 : 2;
+}
 
-template <int DT, int W, int NV, bool PB, bool BIAS, bool OFF>
+template <int DT, int W, int NV, bool PB, bool BIAS, bool OFF, bool CENTER>
 __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
   using Ac = Access<DT, W>;
-  constexpr int ES = Vec<DT>::ESIZE, R = bwd_rows(W, NV, OFF);
+  constexpr int ES = Vec<DT>::ESIZE, R = bwd_rows(W, NV, OFF, BIAS && CENTER);
   extern __shared__ uint4 places[];
   __shared__ float sh[2][2 * R][kMaxWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -698,7 +702,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const bool have = row + r * step < A.T;
-      mean_next[r] = have && !A.rms ? A.mean[row + r * step] : 0.f;
+      mean_next[r] = CENTER && have ? A.mean[row + r * step] : 0.f;
       rstd_next[r] = have ? A.rstd[row + r * step] : 0.f;
     }
   };
@@ -723,7 +727,6 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float2 s1v = make_float2(0.f, 0.f), s2v = make_float2(0.f, 0.f);
-      const float shift = -mean[r] * rstd[r];
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         float x[W], dy[W];
@@ -733,7 +736,8 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
 #pragma unroll
           for (int e = 0; e < W; e += 2) {
             const float2 d = make_float2(dy[e], dy[e + 1]);
-            const float2 xh = fma2(make_float2(x[e], x[e + 1]), make_float2(rstd[r], rstd[r]), make_float2(shift, shift));
+            const float2 xe = make_float2(x[e], x[e + 1]);
+            const float2 xh = mul2(CENTER ? add2(xe, make_float2(-mean[r], -mean[r])) : xe, make_float2(rstd[r], rstd[r]));
             const float2 g = mul2(d, make_float2(w[i][e], w[i][e + 1]));
             s1v = add2(s1v, g);
             s2v = fma2(g, xh, s2v);
@@ -747,7 +751,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
             }
           }
         } else {
-          const float xh = fmaf(x[0], rstd[r], shift), g = dy[0] * w[i][0];
+          const float xh = (CENTER ? x[0] - mean[r] : x[0]) * rstd[r], g = dy[0] * w[i][0];
           s1v.x += g;
           s2v.x = fmaf(g, xh, s2v.x);
           dw[i][0] = fmaf(dy[0], xh, dw[i][0]);
@@ -756,7 +760,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
       }
       float s1 = s1v.x + s1v.y, s2 = s2v.x + s2v.y;
       if (OFF) {
-        const float xh = fmaf(edge[r][0], rstd[r], shift), g = edge[r][1] * we;
+        const float xh = (CENTER ? edge[r][0] - mean[r] : edge[r][0]) * rstd[r], g = edge[r][1] * we;
         s1 += g;
         s2 = fmaf(g, xh, s2);
         dwe = fmaf(edge[r][1], xh, dwe);
@@ -781,9 +785,9 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (row + r * step >= A.T) break;
-      // dx = r (g - m1 - xhat m2) = r g + (x c1 + c0)
-      const float m1 = A.rms ? 0.f : s[2 * r] * inv_h, m2 = s[2 * r + 1] * inv_h;
-      const float c1 = -rstd[r] * rstd[r] * m2, c0 = rstd[r] * (mean[r] * rstd[r] * m2 - m1);
+      // dx = r (g - m1 - xhat m2) = r g + ((x - mu) c1 + c0)
+      const float m1 = CENTER ? s[2 * r] * inv_h : 0.f, m2 = s[2 * r + 1] * inv_h;
+      const float c1 = -rstd[r] * rstd[r] * m2, c0 = -rstd[r] * m1;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         if (in.have[i]) {
@@ -794,19 +798,20 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
           for (int e = 0; e < W; e += 2) {
             if constexpr (W > 1) {
               const float2 g = mul2(make_float2(dy[e], dy[e + 1]), make_float2(w[i][e], w[i][e + 1]));
-              const float2 rest = fma2(make_float2(x[e], x[e + 1]), make_float2(c1, c1), make_float2(c0, c0));
+              const float2 xe = make_float2(x[e], x[e + 1]);
+              const float2 rest = fma2(CENTER ? add2(xe, make_float2(-mean[r], -mean[r])) : xe, make_float2(c1, c1), make_float2(c0, c0));
               const float2 d = fma2(g, make_float2(rstd[r], rstd[r]), rest);
               o[e] = d.x;
               o[e + 1] = d.y;
             } else {
-              o[e] = fmaf(dy[e] * w[i][e], rstd[r], fmaf(x[e], c1, c0));
+              o[e] = fmaf(dy[e] * w[i][e], rstd[r], fmaf(CENTER ? x[e] - mean[r] : x[e], c1, c0));
             }
           }
           Ac::store(out + (int64_t)i * (int)blockDim.x * W * ES, o);
         }
       }
       if (OFF && span.edge >= 0) {
-        const float o = fmaf(edge[r][1] * we, rstd[r], fmaf(edge[r][0], c1, c0));
+        const float o = fmaf(edge[r][1] * we, rstd[r], fmaf(CENTER ? edge[r][0] - mean[r] : edge[r][0], c1, c0));
         Access<DT, 1>::store(out + out_edge, &o);
       }
       out += out_stride;
@@ -1005,7 +1010,8 @@ cudaError_t fwd_warp(const NormArgs& a, const RowsAt& at, cudaStream_t s, int sm
   const int smem = kWarpStages * NVL * 32 * kWarpRows * 16 +
                    param_bytes(a.H, PB ? 2 : 4) * (a.bias ? 2 : 1);
   const dim3 g((unsigned)(need < cap ? need : cap)), b(32, kWarpRows);
-  return off ? launch<norm_fwd_warp_kernel<DT, NVL, PB, true>>(a, g, b, smem, s) : launch<norm_fwd_warp_kernel<DT, NVL, PB, false>>(a, g, b, smem, s);
+  if (a.rms) return off ? launch<norm_fwd_warp_kernel<DT, NVL, PB, true, false>>(a, g, b, smem, s) : launch<norm_fwd_warp_kernel<DT, NVL, PB, false, false>>(a, g, b, smem, s);
+  return off ? launch<norm_fwd_warp_kernel<DT, NVL, PB, true, true>>(a, g, b, smem, s) : launch<norm_fwd_warp_kernel<DT, NVL, PB, false, true>>(a, g, b, smem, s);
 }
 
 template <int DT, bool PB>
@@ -1040,26 +1046,32 @@ cudaError_t fwd(const NormArgs& a, cudaStream_t s, int sms) {
   return launch<norm_fwd_kernel<DT, VW, 4, PB, false>>(a, grid, b, smem, s);
 }
 
-template <int DT, bool PB, bool BIAS>
+template <int DT, bool PB, bool BIAS, bool CENTER>
 cudaError_t bwd(const NormArgs& a, const Plan& p, bool off, int grid, cudaStream_t s) {
   constexpr int VW = Vec<DT>::N;
   const dim3 b(p.threads, p.rows);
-  const int smem = 2 * p.rows * (p.w > 1 ? 2 * bwd_rows(p.w, p.nv, off) * p.nv * p.threads * 16 : kStages * span_bytes(a.H, Vec<DT>::ESIZE));
+  const int smem = 2 * p.rows * (p.w > 1 ? 2 * bwd_rows(p.w, p.nv, off, BIAS && CENTER) * p.nv * p.threads * 16 : kStages * span_bytes(a.H, Vec<DT>::ESIZE));
   if (p.nv == 0) { norm_bwd_wide_kernel<DT><<<grid, b, 0, s>>>(a); return cudaGetLastError(); }
   if (p.w == 1)
-    return p.nv == 2   ? launch<norm_bwd_kernel<DT, 1, 2, PB, BIAS, false>>(a, grid, b, smem, s)
-           : p.nv == 8 ? launch<norm_bwd_kernel<DT, 1, 8, PB, BIAS, false>>(a, grid, b, smem, s)
-                       : launch<norm_bwd_kernel<DT, 1, 16, PB, BIAS, false>>(a, grid, b, smem, s);
+    return p.nv == 2   ? launch<norm_bwd_kernel<DT, 1, 2, PB, BIAS, false, CENTER>>(a, grid, b, smem, s)
+           : p.nv == 8 ? launch<norm_bwd_kernel<DT, 1, 8, PB, BIAS, false, CENTER>>(a, grid, b, smem, s)
+                       : launch<norm_bwd_kernel<DT, 1, 16, PB, BIAS, false, CENTER>>(a, grid, b, smem, s);
   if (off) {
-    if (p.nv == 1) return launch<norm_bwd_kernel<DT, VW, 1, PB, BIAS, true>>(a, grid, b, smem, s);
-    if (p.nv == 2) return launch<norm_bwd_kernel<DT, VW, 2, PB, BIAS, true>>(a, grid, b, smem, s);
-    if constexpr (DT == JP_F32) return launch<norm_bwd_kernel<DT, VW, 4, PB, BIAS, true>>(a, grid, b, smem, s);
+    if (p.nv == 1) return launch<norm_bwd_kernel<DT, VW, 1, PB, BIAS, true, CENTER>>(a, grid, b, smem, s);
+    if (p.nv == 2) return launch<norm_bwd_kernel<DT, VW, 2, PB, BIAS, true, CENTER>>(a, grid, b, smem, s);
+    if constexpr (DT == JP_F32) return launch<norm_bwd_kernel<DT, VW, 4, PB, BIAS, true, CENTER>>(a, grid, b, smem, s);
     return cudaErrorInvalidConfiguration;
   }
-  if (p.nv == 1) return launch<norm_bwd_kernel<DT, VW, 1, PB, BIAS, false>>(a, grid, b, smem, s);
-  if (p.nv == 2) return launch<norm_bwd_kernel<DT, VW, 2, PB, BIAS, false>>(a, grid, b, smem, s);
-  if constexpr (DT == JP_F32) return launch<norm_bwd_kernel<DT, VW, 4, PB, BIAS, false>>(a, grid, b, smem, s);
+  if (p.nv == 1) return launch<norm_bwd_kernel<DT, VW, 1, PB, BIAS, false, CENTER>>(a, grid, b, smem, s);
+  if (p.nv == 2) return launch<norm_bwd_kernel<DT, VW, 2, PB, BIAS, false, CENTER>>(a, grid, b, smem, s);
+  if constexpr (DT == JP_F32) return launch<norm_bwd_kernel<DT, VW, 4, PB, BIAS, false, CENTER>>(a, grid, b, smem, s);
   return cudaErrorInvalidConfiguration;
+}
+
+template <int DT, bool PB>
+cudaError_t bwd(const NormArgs& a, const Plan& p, bool off, int grid, cudaStream_t s) {
+  if (a.rms) return a.dbias ? bwd<DT, PB, true, false>(a, p, off, grid, s) : bwd<DT, PB, false, false>(a, p, off, grid, s);
+  return a.dbias ? bwd<DT, PB, true, true>(a, p, off, grid, s) : bwd<DT, PB, false, true>(a, p, off, grid, s);
 }
 
 }  // namespace
@@ -1084,12 +1096,10 @@ cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t s, int sms) {
   const RowsAt at = rows_at(a, true);
   const Plan p = plan_for(a.H, a.dtype, at.kind, true);
   const int grid = grid_for(a.T, p, sms, true, at.period);
-  auto run = [&](auto* with, auto* without) {
-    return a.dbias ? with(a, p, at.kind == kSpans, grid, s) : without(a, p, at.kind == kSpans, grid, s);
-  };
+  const bool off = at.kind == kSpans;
   cudaError_t e;
-  if (a.dtype == JP_BF16) e = a.param_bf16 ? run(bwd<JP_BF16, true, true>, bwd<JP_BF16, true, false>) : run(bwd<JP_BF16, false, true>, bwd<JP_BF16, false, false>);
-  else e = a.param_bf16 ? run(bwd<JP_F32, true, true>, bwd<JP_F32, true, false>) : run(bwd<JP_F32, false, true>, bwd<JP_F32, false, false>);
+  if (a.dtype == JP_BF16) e = a.param_bf16 ? bwd<JP_BF16, true>(a, p, off, grid, s) : bwd<JP_BF16, false>(a, p, off, grid, s);
+  else e = a.param_bf16 ? bwd<JP_F32, true>(a, p, off, grid, s) : bwd<JP_F32, false>(a, p, off, grid, s);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)((a.H + 31) / 32), a.dbias ? 2 : 1);

@@ -341,3 +341,53 @@ def test_wide_backward_does_not_depend_on_what_the_workspace_held(ctx, T, H, dty
             first = (dx, dw, db)
             check_backward(first, dy, x, w, mean, rstd, False)
         assert all(torch.equal(a, c) for a, c in zip(first, (dx, dw, db)))
+
+
+def far_rows(T, H, dtype, seed):
+    """Rows whose mean is 1000 (fp32) or 50 (bf16, which holds no more of their spread) standard deviations from zero."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    at, sigma = (2000.0, 2.0) if dtype is torch.float32 else (1000.0, 20.0)
+    x = (torch.randn((T, H), generator=g, device="cuda") * sigma + at).to(dtype)
+    dy = torch.randn((T, H), generator=g, device="cuda").to(dtype)
+    w = 1 + 0.3 * torch.randn(H, generator=g, device="cuda")
+    b = 0.2 * torch.randn(H, generator=g, device="cuda")
+    return x, dy, w, b
+
+
+@pytest.mark.parametrize("T", [40, 2000])
+@pytest.mark.parametrize("H", [63, 768, 1283, 2047, 2048, 4096, 5112, 8192, 8200])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("apart", [False, True])
+def test_rows_far_from_zero_keep_their_spread(ctx, T, H, dtype, apart):
+    """xhat = (x - mean) rstd with the difference taken first, whichever kernel the row count and the width choose (``apart``: matrices
+    at different offsets to 16 bytes).  From the mean and rstd of the call itself, xhat is off by 2 u (difference and product) and y by u of
+    each of its two terms more: below 4 u of their magnitudes.  In the backward, mean and rstd are inputs: nothing in a bar grows with
+    |mean|; a weight's sum of up to 124 terms (8200: 14 rows in memory, then the lines; fewer elsewhere) and its xhat stay below 128 u."""
+    x, dy, w, b = far_rows(T, H, dtype, seed=T + H)
+    if apart:
+        flat = torch.empty(T * H + 1, device="cuda", dtype=dtype)
+        xo = flat[1:].view(T, H)
+        x = xo.copy_(x)
+    y, mean, rstd = runner.layer_norm(ctx, x, w, b, eps=EPS)
+    xh = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    ref = xh * w.double() + b.double()
+    mag = (xh * w.double()).abs() + b.double().abs()
+    assert ((y.double() - ref).abs() <= HALF[dtype] * ref.abs() * (1 + 2.0 ** -8) + 4 * U * mag).all()
+    dx, dw, db = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd)
+    rdx, rdw, rdb, mag, magw, magb = plain_backward(dy, x, w, mean, rstd, False)
+    assert ((dx.double() - rdx).abs() <= HALF[dtype] * rdx.abs() * (1 + 2.0 ** -8) + 64 * U * mag).all()
+    assert ((dw.double() - rdw).abs() <= 128 * U * magw).all()
+    assert ((db.double() - rdb).abs() <= 128 * U * magb).all()
+
+
+@pytest.mark.parametrize("T", [40, 2000])
+@pytest.mark.parametrize("H", [1024, 2048, 4096, 8192, 16384])
+def test_rows_of_one_value_give_the_bias(ctx, T, H):
+    """Sums of 2000 over a power of two of columns, and their mean, are exact; so x - mean is 0 whatever rstd is (1000 here)."""
+    w, b = torch.rand(H, device="cuda") + 0.5, torch.rand(H, device="cuda")
+    x = torch.full((T, H), 2000.0, device="cuda")
+    y, mean, rstd = runner.layer_norm(ctx, x, w, b, eps=EPS)
+    assert (mean == 2000).all() and torch.equal(y, b.expand(T, H))
+    dy = torch.randn((T, H), device="cuda")
+    dx, dw, db = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd)
+    assert (dw == 0).all()
