@@ -787,7 +787,7 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(NormArgs A) {
       if (row + r * step >= A.T) break;
       // dx = r (g - m1 - xhat m2) = r g + ((x - mu) c1 + c0)
       const float m1 = CENTER ? s[2 * r] * inv_h : 0.f, m2 = s[2 * r + 1] * inv_h;
-      const float c1 = -rstd[r] * rstd[r] * m2, c0 = -rstd[r] * m1;
+      const float c1 = -rstd[r] * (rstd[r] * m2), c0 = -rstd[r] * m1;      // (r r alone may leave fp32: tiny rows, eps 0)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         if (in.have[i]) {

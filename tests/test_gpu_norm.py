@@ -391,3 +391,16 @@ def test_rows_of_one_value_give_the_bias(ctx, T, H):
     dy = torch.randn((T, H), device="cuda")
     dx, dw, db = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd)
     assert (dw == 0).all()
+
+
+def test_tiny_rows_without_eps(ctx):
+    """Rows of 2^-66 with eps 0: rstd is 2^66, whose square is beyond fp32; dx is rstd times numbers near 1 all the same."""
+    T, H = 6, 1024
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.where(torch.rand((T, H), generator=g, device="cuda") < 0.5, -1.0, 1.0) * 2.0 ** -66
+    dy, w = torch.randn((T, H), generator=g, device="cuda"), 1 + 0.3 * torch.randn(H, generator=g, device="cuda")
+    for rms in (True, False):
+        rstd = torch.full((T,), 2.0 ** 66, device="cuda")
+        mean = None if rms else torch.zeros(T, device="cuda")
+        got = runner.layer_norm_backward(ctx, dy, x, w, mean, rstd, rms=rms)
+        check_backward(got, dy, x, w, torch.zeros(T, device="cuda"), rstd, rms)
