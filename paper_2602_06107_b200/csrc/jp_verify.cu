@@ -20,7 +20,7 @@
 // border, so this pass is fp64: 2^x from a table of 32 entries and a polynomial of degree 4 (Tang's table-driven scheme), about 10 fp64
 // operations an element.  The row sums of the first pass are good to 1e-7 only, so they serve to decide the sign of p - q; per segment
 // sum p and sum q over p > q are kept apart, beside the full sums, and the last block of a sequence to finish scales them with the
-// exact normalisers.  A decision closer than 2e-5 to its random number takes its two row sums again in fp64.
+// exact normalisers (and, for rows so nearly equal that the sign matters, takes the segments again with these).  A decision closer than 2e-5 to its random number takes its two row sums again in fp64.
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -480,6 +480,18 @@ __device__ __forceinline__ void segments(const DrawRow& T, const DrawRow& D, int
   }
 }
 
+// A draw from max(p - q, 0) takes its segments again where that sums to less than kApart times what the first pass's sums are off by
+// (eta).  For entries whose log (p / q) spreads over s, the whole is about 0.4 s and those of the wrong sign are off by 0.2 eta^2 / s
+// together: 1e-7 of the whole at this border.
+constexpr double kApart = 1e3;
+// All segments again by one block, with p and q in their exact normalisation.
+template <int DT>
+__device__ __noinline__ void segments_again(DrawRow T, DrawRow D, bool far, int segs, int64_t seg_vecs, int64_t nv, int64_t V, SegPart* out) {
+  const int warp = threadIdx.x >> 5, count = warp < segs ? (segs - warp + kWarps - 1) / kWarps : 0;
+  if (far) segments<DT, true, true>(T, D, -1, warp, kWarps, count, seg_vecs, nv, V, out);
+  else segments<DT, true, false>(T, D, -1, warp, kWarps, count, seg_vecs, nv, V, out);
+}
+
 // Of all threads' (place, sum before it), the one with the largest place; place -1: none.
 struct Pick { int place; double before; };
 __device__ __forceinline__ Pick block_last(int place, double before, Pick* sh) {
@@ -674,36 +686,53 @@ __global__ void __launch_bounds__(kThreads, kDrawBlocks) verify_draw_kernel(Veri
   const int per = (segs + kThreads - 1) / kThreads;
   constexpr int kPer = kVerifyMaxSegs / kThreads;
   double mass_of[kPer], q_of[kPer], all_of[kPer];
-  double pa = 0, qa = 0;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    mass_of[k] = q_of[k] = all_of[k] = 0;
-    const int g = tid * per + k;
-    if (k < per && g < segs) {
-      const double2 w = __ldcg(sp + 2 * g), v = __ldcg(sp + 2 * g + 1);
-      mass_of[k] = w.x;
-      q_of[k] = w.y;
-      all_of[k] = v.x;
-      pa += v.x;
-      qa += v.y;
-    }
-  }
-  double a = 1.0, cq = 0.0, P = 1.0;
-  if (use_q) {
-    P = block_sum_d(pa, sh);
-    const double Q = block_sum_d(qa, sh);
-    a = 1.0 / P;
-    cq = 1.0 / Q;
-  }
   const double tiny = kTiny * s_inv[m];
-  double mine = 0, total, before;
+  double a = 1.0, cq = 0.0, P = 1.0, mine, total, before;
+  for (bool again = false;; again = true) {
+    double pa = 0, qa = 0;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    mass_of[k] = mass_of[k] * a - q_of[k] * cq;
-    if (!(mass_of[k] > tiny)) mass_of[k] = 0;
-    mine += mass_of[k];
+    for (int k = 0; k < kPer; ++k) {
+      mass_of[k] = q_of[k] = all_of[k] = 0;
+      const int g = tid * per + k;
+      if (k < per && g < segs) {
+        const double2 w = __ldcg(sp + 2 * g), v = __ldcg(sp + 2 * g + 1);
+        mass_of[k] = w.x;
+        q_of[k] = w.y;
+        all_of[k] = v.x;
+        pa += v.x;
+        qa += v.y;
+      }
+    }
+    double apart = 0;
+    if (again) {
+      a = cq = 1.0;
+    } else if (use_q) {
+      P = block_sum_d(pa, sh);
+      const double Q = block_sum_d(qa, sh);
+      a = 1.0 / P;
+      cq = 1.0 / Q;
+      apart = fabs(P - Q);
+    }
+    mine = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      mass_of[k] = mass_of[k] * a - q_of[k] * cq;
+      if (!(mass_of[k] > tiny)) mass_of[k] = 0;
+      mine += mass_of[k];
+    }
+    before = block_scan_d(mine, sh, &total);
+    // Where p / q lies between 1 and P / Q the first pass's sums had the sign of p - q wrong, and such an entry counts with up to
+    // |P / Q - 1| p (1e-7 p and less) more or less than it should.  Two nearly equal rows, where that may count, are taken
+    // again with the sums known now.
+    if (!(apart * kApart > total)) break;
+    if (tid < 32) {
+      tab_t[tid] = table_entry(tid, s_inv[m] * a);
+      tab_q[tid] = table_entry(tid, s_inv[N + 1 + m] * cq);
+    }
+    __syncthreads();
+    segments_again<DT>(T, D, far, segs, A.seg_vecs, nv, A.V, parts);
+    __syncthreads();
   }
-  before = block_scan_d(mine, sh, &total);
   const bool whole = use_q && !(total > 0);                 // nothing left above zero: draw from p itself
   if (whole) {
     mine = 0;

@@ -343,3 +343,41 @@ def test_refusals(ctx):
         with pytest.raises(B.JackpotError):
             B.jp_verify_draft(ctx, e, t, q, *tail, ws)
     check(ctx, s)
+
+
+def draws_inside_entries(s, rng):
+    """Sets u_sample to the middle of what an entry of more than average mass takes of the first row's max(p - q, 0), a random one a sequence."""
+    zt, zd = host(s["target_logits"]), host(s["draft_logits"])
+    for b in range(zt.shape[0]):
+        mass = np.maximum(np.exp(log_softmax(zt[b, 0], 1)) - np.exp(log_softmax(zd[b, 0], 1)), 0)
+        c = np.cumsum(mass)
+        v = rng.choice(np.nonzero(mass >= c[-1] / mass.size)[0])
+        s["u_sample"][b] = float((c[v] - mass[v] / 2) / c[-1])
+
+
+@pytest.mark.parametrize("V", [1000, 20011])
+@pytest.mark.parametrize("eps", [1e-5, 1e-6, 1e-7])
+def test_draws_between_nearly_equal_rows(ctx, V, eps):
+    """A draft that differs from the target by little more than fp32's steps: p - q is far below what the sums of the first pass are
+    good to.  The draw is half an entry's mass from its borders, at least 1 / 2 V of the whole: above 2e-5, where p and q in 64 bits, off by
+    2e-16 each, leave 2e-16 sqrt(V) / 1e-8 of a whole of 1e-8 and more."""
+    s = make(100, 1, V, torch.float32, seed=21)
+    g = torch.Generator(device="cuda").manual_seed(22)
+    s["draft_logits"].copy_(s["target_logits"][:, :1] + eps * torch.randn((100, 1, V), generator=g, device="cuda"))
+    s["draft_tokens"][:] = -1                                 # rejected
+    draws_inside_entries(s, np.random.default_rng(23))
+    check(ctx, s)
+
+
+def test_draws_where_one_entry_is_raised_by_a_step(ctx):
+    """Equal rows but for the largest entry, one fp32 step higher in the draft: everything else has p above q, by 1e-7 of itself."""
+    s = make(64, 1, 3000, torch.float32, seed=24)
+    z = s["target_logits"]
+    z[:, :, 7] = 7.5
+    z[:, :, 2999] = 11.0
+    s["draft_logits"].copy_(z[:, :1])
+    s["draft_logits"][:, :, 2999] = float(np.nextafter(np.float32(11.0), np.float32(12)))
+    s["draft_tokens"][:] = 3000                               # rejected
+    draws_inside_entries(s, np.random.default_rng(25))
+    got = check(ctx, s)
+    assert (got["tokens"][:, 0] != 2999).all()
