@@ -447,12 +447,13 @@ int64_t split_bytes(int64_t tiles, int64_t kblocks, int64_t M, int nt, int split
   return (tiles + runs - 1) / runs * nt * 512 + (kblocks + split - 1) / split * kBlockK * 2 * M;
 }
 constexpr int kMaxSplit = 8;
+constexpr int token_groups(int64_t M) { return M <= 8 ? 1 : M <= 16 ? 2 : 4; }      // of eight, that the products take
 // CTAs that share the columns of a tile, 1: none.  Two or more where the tokens' x does not fit beside the ring (it would take a launch
 // for each part of the tokens, each reading the weights again), as few as fit with the run's sums (30 tokens, 9217 x 8192: 51 us in
 // launches, 29 in clusters of eight); and where tiles are few, so that more SMs work (28 tokens, 109 x 6274: 26 us, 7.8; one token,
 // 256 x 8192: 5.3, 4.1).
 int split_of(int64_t tiles, int64_t kblocks, int groups, int64_t M, int sms) {
-  const int nt = M <= 8 ? 1 : M <= 16 ? 2 : 4;
+  const int nt = token_groups(M);
   const int64_t room = x_bytes(nt, 1, 1, groups);
   const bool fits = M * kblocks * kBlockK * 2 <= room;
   int best = 1;
@@ -538,14 +539,21 @@ cudaError_t launch_w4_pack(W4PackArgs a, cudaStream_t s, int sms) {
   return cudaGetLastError();
 }
 
-// Tokens of one launch, of M that are left: as many as shared memory holds of x (one always fits), the launches even.
+// Tokens of one launch, of M that are left (32 at most).  As few launches as shared memory allows, since each reads all weights: x of a
+// launch is in one block or in the clusters that share the columns (one token always fits).  The launches are even, or all but the last
+// whole groups of eight tokens where that makes fewer groups, which is what the products take (23 tokens, 26375 x 7955: 15 and 8 72 us, 12
+// and 11 79; 32 tokens, 4096 x 14336: 16 and 16 28 us, 26 and 6 37).
 int w4_tokens_per_launch(int64_t N, int64_t K, int group, int64_t M, int sms) {
   const int groups = kBlockK / group;
-  if (split_of((N + kTileRows - 1) / kTileRows, blocks_of(N, K), groups, M, sms) > 1) return (int)M;
+  const int64_t tiles = (N + kTileRows - 1) / kTileRows, kblocks = blocks_of(N, K);
+  auto fits = [&](int64_t m) {
+    return m * kblocks * kBlockK * 2 <= x_bytes(token_groups(m), 1, 1, groups) || split_of(tiles, kblocks, groups, m, sms) > 1;
+  };
   int64_t m = M < kW4MaxTokens ? M : kW4MaxTokens;
-  while (m > 1 && m * blocks_of(N, K) * kBlockK * 2 > x_bytes(m <= 8 ? 1 : m <= 16 ? 2 : 4, 1, 1, groups)) --m;
-  const int64_t launches = (M + m - 1) / m;
-  return (int)((M + launches - 1) / launches);
+  while (m > 1 && !fits(m)) --m;
+  const int64_t launches = (M + m - 1) / m, even = (M + launches - 1) / launches, whole = (even + 7) / 8 * 8 < m ? (even + 7) / 8 * 8 : m;
+  auto products = [&](int64_t each) { return (launches - 1) * token_groups(each) + token_groups(M - (launches - 1) * each); };
+  return (int)(products(whole) < products(even) ? whole : even);
 }
 
 cudaError_t launch_w4(W4Args a, int group, cudaStream_t s, int sms, int device) {

@@ -304,3 +304,18 @@ def test_every_kind_of_launch_in_graphs_on_two_streams(ctx, N, K, M):
         torch.cuda.synchronize()
         for i in range(2):
             assert torch.equal(outs[i], runner.linear_w4(ctx, xs[i], w, out_dtype=torch.float32))
+
+
+@gpu
+@pytest.mark.parametrize("N,K,M,launches", [(8192, 28672, 32, 2), (16, 65536, 32, 4), (18000, 8192, 32, 2), (4096, 14336, 32, 2), (2048, 2048, 32, 1),
+                                            (42785, 6806, 30, 2), (40, 65536, 1, 1)])
+def test_few_launches_where_x_does_not_fit(ctx, N, K, M, launches):
+    """Every launch reads all weights: as many tokens in each as fit one block or a cluster of blocks."""
+    q, s, z = make(N, K, 128, True, torch.bfloat16, seed=N)
+    w = runner.pack_w4(ctx, q, s, z, K=K)
+    x = tokens(M, K, seed=M)
+    before = ctx.launch_count()
+    out = runner.linear_w4(ctx, x, w, out_dtype=torch.float32)
+    assert ctx.launch_count() - before == launches
+    ref = unpacked(q, s, z, K, 128)
+    check(out, x, ref, 128)
