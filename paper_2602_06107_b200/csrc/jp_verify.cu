@@ -18,9 +18,10 @@
 // verify_draw_kernel takes the decisions of a sequence (again in every block: cheaper than a launch of its own) and then the
 // masses of the row to draw from, by segments.  Which token a draw hits depends on sums over the vocabulary next to a
 // border, so this pass is fp64: 2^x from a table of 32 entries and a polynomial of degree 4 (Tang's table-driven scheme), about 10 fp64
-// operations an element.  The row sums of the first pass are good to 1e-7 only, so they serve to decide the sign of p - q; per segment
+// operations an element.  The row sums of the first pass are good to 1e-7, in the worst case to 3e-6, so they serve to decide the sign of p - q; per segment
 // sum p and sum q over p > q are kept apart, beside the full sums, and the last block of a sequence to finish scales them with the
-// exact normalisers (and, for rows so nearly equal that the sign matters, takes the segments again with these).  A decision closer than 2e-5 to its random number takes its two row sums again in fp64.
+// exact normalisers (and, for rows so nearly equal that the sign matters, takes the segments again with these).  A decision closer
+// than kNear (2e-5) to its random number takes its two row sums again in fp64.
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -31,6 +32,7 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kDrawBlocks = 2;       // blocks of the draw per SM (three get 80 registers a thread and were 5 % slower)
 constexpr unsigned kAll = 0xffffffffu;
+constexpr double kNear = 2e-5;       // decisions closer to their random number than this have their sums taken again in fp64
 constexpr double kLog2eD = 1.4426950408889634074;
 constexpr double kLn2D = 0.69314718055994530942;
 // Logits below ref + kFloor / c have probability 0 (ref: the row's reference, 2^-60 to 2^66 of its sum).  The sums take them as
@@ -331,7 +333,9 @@ __global__ void __launch_bounds__(kThreads, 4) verify_rows_kernel(VerifyArgs A) 
   RowPart part;
   part.ref = zref;
   part.idx = 0;
-  // relative to zref (ref is rounded); what cf lacks of c counts by its product with a distance to the reference, below 1e-6
+  // relative to zref (ref is rounded).  An exponent x that counts is off by half its step and by what cf lacks of c, 2^-25 |x|: 1.1e-6 of its
+  // term where the sample gave a reference (of a slice's 2^15 terms those below 2^-20 hardly count).  Where the whole sample was masked, zref is 0 and
+  // all that counts may lie near 2^-60: 2^-19 and 60 2^-25, times ln 2, 2.6e-6.  Two rows of that stay well within the 2e-5 of kNear.
   part.s = block_sum_d(r.fast * exp2_clamped((double)ref - (double)zref * (double)cf, tab) + r.exact, sh);
   if (!(part.s > 0x1p-60 && part.s < 0x1p60)) part = exact_slice<DT>(row, i0, i1, A.V, c, tab, sh);
   if (kind == 0) {                                          // greedy: the slice's largest logit becomes its reference
@@ -578,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, kDrawBlocks) verify_draw_kernel(Veri
           scale *= sq;
         }
         ratio = ok ? exp2_clamped(d, tab) * scale : 0.0;
-        near = ok && fabs(ratio - (double)s_u[lane]) <= 2e-5 * ratio && ratio > 0;
+        near = ok && fabs(ratio - (double)s_u[lane]) <= kNear * ratio && ratio > 0;
       }
     }
     if (lane < n) s_ratio[lane] = ratio;

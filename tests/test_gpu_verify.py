@@ -381,3 +381,21 @@ def test_draws_where_one_entry_is_raised_by_a_step(ctx):
     draws_inside_entries(s, np.random.default_rng(25))
     got = check(ctx, s)
     assert (got["tokens"][:, 0] != 2999).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_borders_where_the_start_of_a_slice_is_masked(ctx, dtype):
+    """All but the last 1000 entries are masked and these lie near -40: the sums have no reference nearby and are off by up to 3e-6; u_accept
+    is one fp32 step from the border all the same."""
+    n, V = 60, 50000
+    s = make(n, 1, V, dtype, seed=27, sigma=1.0)
+    for k in ("target_logits", "draft_logits"):
+        s[k] -= 40.0
+        s[k][:, :, :V - 1000] = -math.inf
+    g = torch.Generator(device="cuda").manual_seed(28)
+    s["draft_tokens"][:] = torch.randint(V - 1000, V, (n, 1), generator=g, device="cuda", dtype=torch.int32)
+    zt, zd, tok = host(s["target_logits"]), host(s["draft_logits"]), host(s["draft_tokens"])
+    for b in range(n):
+        a = math.exp(min(0.0, log_softmax(zt[b, 0], 1)[tok[b, 0]] - log_softmax(zd[b, 0], 1)[tok[b, 0]]))
+        s["u_accept"][b, 0] = float(np.nextafter(np.float32(a), np.float32(0 if b % 2 else 1)))
+    check(ctx, s)
