@@ -568,7 +568,8 @@ size_t jp_w4_packed_bytes(int64_t N, int64_t K, int32_t group);
 jp_status jp_w4_pack(jp_ctx* ctx, const jp_w4_desc* desc, const uint8_t* q, const void* scales,
                      const uint8_t* zeros, void* packed);
 /* x [M, ld_x] bf16 and out [M, ld_out] of out_dtype (JP_BF16 or JP_F32), pointers aligned to their
- * elements, 0 <= M <= JP_W4_MAX_TOKENS (more: JP_ERR_TOO_LARGE), ld = 0 means K and N. */
+ * elements, 0 <= M <= JP_W4_MAX_TOKENS (more: JP_ERR_TOO_LARGE), ld = 0 means K and N.  (jp_verify_draft takes rows a
+ * multiple of 16 bytes apart: with an odd N give ld_out rounded up.) */
 jp_status jp_w4_linear(jp_ctx* ctx, const jp_w4_desc* desc, const void* packed, const void* x, int64_t ld_x,
                        int64_t M, void* out, int64_t ld_out, int32_t out_dtype);
 

@@ -286,7 +286,9 @@ def pack_w4(ctx: B.Context, q, scales, zeros=None, *, K, group=128):
 
 
 def linear_w4(ctx: B.Context, x, w: W4Weight, *, out_dtype=torch.bfloat16, out=None):
-    """One jp_w4_linear call on torch's current stream: x [M, K] bf16, M <= 32, times the packed weight: [M, N]."""
+    """One jp_w4_linear call on torch's current stream: x [M, K] bf16, M <= 32, times the packed weight: [M, N], contiguous or
+    in ``out``.  :func:`verify_draft` takes logits with rows a multiple of 16 bytes apart only: for an N that is no multiple of 8 (bf16)
+    or 4 (fp32), pass ``out = torch.empty((M, (N + 7) // 8 * 8), ...)[:, :N]``."""
     if x.dtype != torch.bfloat16:
         raise B.JackpotError(f"x must be bfloat16, got {x.dtype}")
     ld_x = _rows(x, "x")
@@ -318,8 +320,9 @@ def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_ac
                  temperature=None, accept_prob=True, logp=True):
     """One jp_verify_draft call on torch's current stream.  target_logits [B, N + 1, V], draft_logits [B, N, V] or None
     (drafts without a distribution), draft_tokens [B, N] int32, u_accept [B, N] and u_sample [B] fp32, n_draft [B] int32
-    or None, temperature [B] fp32 or None.  Returns ``n_accepted`` [B], ``tokens`` [B, N + 1] and, unless turned off,
-    ``accept_prob`` [B, N] and ``logp`` [B, N + 1]."""
+    or None, temperature [B] fp32 or None.  The logits start on 16 bytes and their rows and sequences are multiples of 16 bytes
+    apart: those of an odd vocabulary are a slice of wider rows.  Returns ``n_accepted`` [B], ``tokens`` [B, N + 1] and,
+    unless turned off, ``accept_prob`` [B, N] and ``logp`` [B, N + 1]."""
     if target_logits.dim() != 3 or target_logits.shape[1] < 1:
         raise B.JackpotError("target_logits must be [B, N + 1, V]")
     n_seq, rows, V = target_logits.shape

@@ -183,3 +183,30 @@ def test_w4_output_beyond_32_bit_offsets(ctx):
     out = runner.linear_w4(ctx, x, w, out=big.as_strided((M, N), (pitch, 1)))
     assert torch.equal(out, runner.linear_w4(ctx, x, w))
     assert (big[N:pitch] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_an_odd_vocabulary_from_the_output_layer_to_the_verification(ctx, dtype):
+    """Logits of 5003 entries in rows of 5008, as linear_w4 writes them on request; packed rows of 5003 are refused by name."""
+    n_seq, N, H, V, group = 4, 2, 256, 5003, 64
+    g = torch.Generator(device="cuda").manual_seed(31)
+    q, s, z = runner.quantize_w4(torch.randn((V, H), generator=g, device="cuda") * 0.2, group)
+    w = runner.pack_w4(ctx, q, s, z, K=H, group=group)
+    h = torch.randn((n_seq * (N + 1), H), generator=g, device="cuda").to(torch.bfloat16)
+    ld = (V + 7) // 8 * 8
+    wide = torch.full((n_seq * (N + 1), ld), 7.0, device="cuda", dtype=dtype)
+    logits = runner.linear_w4(ctx, h, w, out=wide[:, :V])
+    assert logits.data_ptr() == wide.data_ptr() and (wide[:, V:] == 7).all()
+    packed = runner.linear_w4(ctx, h, w, out_dtype=dtype)
+    assert packed.is_contiguous() and torch.equal(packed, logits)
+    target = wide.view(n_seq, N + 1, ld)[:, :, :V]
+    tokens = target[:, :N].argmax(2).to(torch.int32)
+    u, us = torch.rand((n_seq, N), generator=g, device="cuda") * 0.01, torch.rand(n_seq, generator=g, device="cuda")
+    out = runner.verify_draft(ctx, target, None, tokens, u, us)
+    logp = torch.log_softmax(target.double(), 2)
+    for b in range(n_seq):
+        for i in range(int(out["n_accepted"][b]) + 1):
+            want = float(logp[b, i, int(out["tokens"][b, i])])
+            assert abs(float(out["logp"][b, i]) - want) <= 6e-6 + U * abs(want)
+    with pytest.raises(B.JackpotError, match="16 bytes"):
+        runner.verify_draft(ctx, packed.view(n_seq, N + 1, V), None, tokens, u, us)
