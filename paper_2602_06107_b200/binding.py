@@ -193,10 +193,10 @@ def _ptr(t):
 _DTYPE_CODES = {torch.bfloat16: JP_BF16, torch.float32: JP_F32}
 
 
-def _dtype_code(t: torch.Tensor) -> int:
+def _dtype_code(t: torch.Tensor, what: str = "logits") -> int:
     code = _DTYPE_CODES.get(t.dtype)
     if code is None:
-        raise JackpotError(f"logits must be bfloat16 or float32, got {t.dtype}")
+        raise JackpotError(f"{what} must be bfloat16 or float32, got {t.dtype}")
     return code
 
 

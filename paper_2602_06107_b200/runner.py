@@ -199,7 +199,7 @@ def _norm_desc(ctx, x, weight, bias, eps, rms, out, name, dy=None):
         if dy.shape != shape or dy.dtype is not dtype:
             raise B.JackpotError("dy must have x's shape and dtype")
         ld_dx, ld_dy = ld_out, _rows(dy, "dy")
-    return B._desc(ctx, B.jp_norm_desc, shape[0], shape[1], ld_x, ld_y, ld_dy, ld_dx, B._dtype_code(x), B._dtype_code(weight),
+    return B._desc(ctx, B.jp_norm_desc, shape[0], shape[1], ld_x, ld_y, ld_dy, ld_dx, B._dtype_code(x, "x"), B._dtype_code(weight, "weight"),
                    B.JP_NORM_RMS if rms else 0, float(eps))
 
 
@@ -299,7 +299,7 @@ def linear_w4(ctx: B.Context, x, w: W4Weight, *, out_dtype=torch.bfloat16, out=N
         out = x.new_empty((M, w.N), dtype=out_dtype)
     elif out.shape != (M, w.N):
         raise B.JackpotError(f"out must be [{M}, {w.N}]")
-    B.jp_w4_linear(ctx, w.desc, w.packed, x, ld_x, M, out, _rows(out, "out"), B._dtype_code(out))
+    B.jp_w4_linear(ctx, w.desc, w.packed, x, ld_x, M, out, _rows(out, "out"), B._dtype_code(out, "out"))
     return out
 
 

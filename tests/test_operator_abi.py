@@ -4,8 +4,12 @@ import ctypes
 import os
 import subprocess
 
+import pytest
+import torch
+
 from paper_2602_06107_b200 import binding as B
 from paper_2602_06107_b200 import build as jp_build
+from paper_2602_06107_b200 import runner
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 STRUCTS = {"jp_norm_desc": B.jp_norm_desc, "jp_w4_desc": B.jp_w4_desc, "jp_verify_desc": B.jp_verify_desc}
@@ -46,3 +50,19 @@ def test_calls_without_a_context_are_refused():
     assert lib.jp_w4_linear(None, ctypes.byref(w), None, None, 0, 1, None, 0, 0) == -1
     assert lib.jp_verify_draft(None, ctypes.byref(v), *[None] * 12, 0) == -1
     assert lib.jp_verify_workspace_bytes(None, 1, 1, 8, 0, 1) == 0
+
+
+def test_a_wrong_dtype_is_refused_by_the_arguments_name():
+    """The checks of dtypes come before anything that needs a device."""
+    class Ctx:
+        _descs = {}
+    x, w = torch.empty((2, 8), dtype=torch.float16), torch.empty(8)
+    with pytest.raises(B.JackpotError, match="^x must be bfloat16 or float32"):
+        runner.layer_norm(Ctx(), x, w)
+    with pytest.raises(B.JackpotError, match="^weight must be bfloat16 or float32"):
+        runner.layer_norm(Ctx(), x.float(), w.half())
+    packed = runner.W4Weight(torch.empty(0, dtype=torch.uint8), 4, 8, 32)
+    with pytest.raises(B.JackpotError, match="^out must be bfloat16 or float32"):
+        runner.linear_w4(Ctx(), x.bfloat16(), packed, out_dtype=torch.float16)
+    with pytest.raises(B.JackpotError, match="^logits must be bfloat16 or float32"):
+        B._dtype_code(x)
