@@ -399,3 +399,17 @@ def test_borders_where_the_start_of_a_slice_is_masked(ctx, dtype):
         a = math.exp(min(0.0, log_softmax(zt[b, 0], 1)[tok[b, 0]] - log_softmax(zd[b, 0], 1)[tok[b, 0]]))
         s["u_accept"][b, 0] = float(np.nextafter(np.float32(a), np.float32(0 if b % 2 else 1)))
     check(ctx, s)
+
+
+def test_draws_between_nearly_equal_rows_far_from_zero(ctx):
+    """Logits near 2^21, a quarter apart: equal rows but for one entry of 1e-8, a step higher in the draft.  Everything else has p above q by
+    less than 1e-8 of itself."""
+    s = make(64, 1, 3000, torch.float32, seed=29)
+    z = s["target_logits"]
+    z.copy_((z * 4).round() / 4 + 2.0 ** 21)
+    z[:, :, 2000] = z.amax(2) - 12
+    s["draft_logits"].copy_(z[:, :1])
+    s["draft_logits"][:, :, 2000] += 0.25
+    s["draft_tokens"][:] = -5                                 # rejected
+    draws_inside_entries(s, np.random.default_rng(30))
+    check(ctx, s)
