@@ -465,7 +465,8 @@ jp_status jp_budget_lambda_static(const float* logp_actor, const float* logp_pol
  * them the device, the stream, the error text and the launch count, and any scratch is the caller's
  * (a workspace of the stated size, 256-byte aligned, its content of no meaning before or after).  So they may be captured into CUDA
  * graphs, and calls with different workspaces and outputs may run at the same time on different
- * streams.  The calling thread's current device is left as it was.
+ * streams.  The calling thread's current device is left as it was.  int32 and fp32 arrays are aligned to their
+ * elements (else JP_ERR_ALIGNMENT), and so is what states no alignment of its own.
  *
  * Layer norm and RMS norm of each row of x [T, H] (DEVICE, rows ld elements apart, 0 = H):
  *   mu = mean(x), or 0 with JP_NORM_RMS;  r = 1 / sqrt(mean((x - mu)^2) + eps);

@@ -110,6 +110,7 @@ struct DeviceScope {
 };
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+template <class... P> bool aligned4(P... p) { return (((uintptr_t)p | ...) & 3u) == 0; }      // int32 and fp32 arrays; NULL is aligned
 
 jp_status ensure_workspace(jp_ctx* c, int64_t rows, int k) {
   int kk = k > 0 ? k : 1;
@@ -835,6 +836,7 @@ jp_status jp_layer_norm_forward(jp_ctx* c, const jp_norm_desc* d, const void* x,
   if (!element_aligned(x, d->dtype) || !element_aligned(y, d->dtype) || !element_aligned(weight, d->param_dtype) ||
       !element_aligned(bias, d->param_dtype))
     return fail(c, JP_ERR_ALIGNMENT, "x, y, weight and bias must be aligned to their elements");
+  if (!aligned4(out_mean, out_rstd)) return fail(c, JP_ERR_ALIGNMENT, "out_mean and out_rstd must be aligned to their elements");
   DeviceScope dev(c->device);
   if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
   a.x = x; a.weight = weight; a.bias = bias; a.y = y; a.out_mean = out_mean; a.out_rstd = out_rstd;
@@ -857,6 +859,7 @@ jp_status jp_layer_norm_backward(jp_ctx* c, const jp_norm_desc* d, const void* d
   jp_status st = norm_args(c, d, &a);
   if (st != JP_OK) return st;
   if (!dweight) return fail(c, JP_ERR_INVALID_ARG, "dweight is NULL");
+  if (!aligned4(dweight, dbias, mean, rstd)) return fail(c, JP_ERR_ALIGNMENT, "mean, rstd, dweight and dbias must be aligned to their elements");
   DeviceScope dev(c->device);
   if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
   if (a.T == 0) {
@@ -1002,6 +1005,8 @@ jp_status jp_verify_draft(jp_ctx* c, const jp_verify_desc* d, const void* target
   if (!target_logits || !u_sample || !out_n_accepted || !out_tokens || (d->N > 0 && (!draft_tokens || !u_accept)))
     return fail(c, JP_ERR_INVALID_ARG, "a required pointer is NULL");
   if (!aligned16(target_logits) || !aligned16(draft_logits)) return fail(c, JP_ERR_ALIGNMENT, "logits must be 16-byte aligned");
+  if (!aligned4(draft_tokens, n_draft, temperature, u_accept, u_sample, out_n_accepted, out_tokens, out_accept_prob, out_logp))
+    return fail(c, JP_ERR_ALIGNMENT, "int32 and fp32 arrays must be aligned to their elements");
   if (!workspace || workspace_bytes < p.bytes)
     return fail(c, JP_ERR_WORKSPACE, "workspace is NULL or smaller than jp_verify_workspace_bytes");
   if ((uintptr_t)workspace & 255u) return fail(c, JP_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
