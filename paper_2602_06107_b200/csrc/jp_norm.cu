@@ -77,7 +77,7 @@ template <int DT> struct Access<DT, 1> {
 };
 
 // Two fp32 operations in one instruction: at 8192 x 4096 both passes are as much bound by issue as by HBM (forward with bias 31 us
-// without, 28.5; backward of RMS norm 41, 39.5).  xhat is (x - mu) r in two of them, not x r + (-mu r) in one: rounding mu r would leave
+// without, 28.9; backward of RMS norm 41, 39.4).  xhat is (x - mu) r in two of them, not x r + (-mu r) in one: rounding mu r would leave
 // 2^-24 |mu| r in every xhat, a thousand times its own rounding in a row whose mean is a thousand standard deviations.
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   asm("{.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;}" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
@@ -288,7 +288,7 @@ struct Rows {
 // place begins at the row's own offset), and every thread reads its elements once all have arrived.  Vectors that reach beyond the
 // matrix, in its first and last row, are copied element by element.  The place is free again after the barrier of the row's first sum.
 // (With element loads into registers, one row ahead, 8192 x 4095 bf16 took 147 us forward and 225 us backward; this 70 and 93, rows of
-// one offset as spans 34 and 62.)
+// one offset as spans 32 and 66.)
 __host__ __device__ inline int span_bytes(int64_t H, int es) { return (int)((H * es + 15) / 16 + 1) * 16; }
 template <int DT, int NV, int NT, int STAGES>
 struct Rows<DT, 1, NV, NT, false, STAGES> {
@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(group_threads(W, NV)) norm_fwd_kernel(NormArgs
 
 // One warp a row, NVL vectors a lane, for many rows of up to 5120 bf16 or 2560 fp32: the reductions are shuffles and no row waits for
 // another (a block a row, with a barrier for each of its two sums, took 48 us at 8192 x 4096 with bias in bf16 and 52 at 6553 x 5120; this
-// takes 28 and 31).  Weight and bias are in shared memory beside the rows to come; wider rows leave too few warps an SM (at 4096 x 8192,
+// takes 29 and 31).  Weight and bias are in shared memory beside the rows to come; wider rows leave too few warps an SM (at 4096 x 8192,
 // five of them, RMS norm, 42 us; a block a row 40).
 constexpr int kWarpStages = 2;
 __host__ __device__ constexpr int warp_rows(int nvl) { return nvl == 20 ? 9 : 12; }   // rows a block

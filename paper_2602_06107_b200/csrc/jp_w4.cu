@@ -33,10 +33,11 @@ constexpr int kBlockK = 128;
 constexpr int kWarps = 16;
 constexpr int kDepth = 3;
 constexpr int kSharedBytes = 232448;  // of one block
-// A warp takes a unit at a time and has three of them in flight (five were no faster).  A unit is two blocks where there are enough (less to do per block around
-// the products): two of one tile, or for many tiles the same block of two tiles, which then share what is read of x (151,936 x 2048 and
-// one token: one block 34.8 us, two of a tile 32.2, of two tiles 30.5; x 4096 and eight: 68.7, 62.2, 60.9; at 11008 x 4096 pairs of
-// tiles come out uneven, 6.9 us with two blocks of one tile, 7.7).  Above eight tokens the products take longer than either saves.
+// A warp takes a unit at a time and has three of them in flight (four: below, 30.8 and 63.5 us).  A unit is two blocks where there are
+// enough (less to do per block around the products): two of one tile, or for many tiles the same block of two tiles, which then share what
+// is read of x (weights from HBM at full clocks: 151,936 x 2048 and one token, one block 34.6 us, two of a tile 32.1, of two tiles 30.3; x
+// 4096 and eight, 72.2, 65.0, 60.9; at 11008 x 4096 pairs of tiles come out uneven, 10.6 us, two blocks of one tile 9.5).  Above eight
+// tokens the products take longer than either saves.
 // What the ring and the warps' parts of shared tiles leave is for x.
 __host__ __device__ constexpr int block_bytes(int groups) { return 1024 + kTileRows * 4 * groups; }
 __host__ __device__ constexpr int part_bytes(int tiles, int nt) { return kWarps * tiles * nt * 32 * 16; }
