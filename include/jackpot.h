@@ -574,6 +574,69 @@ jp_status jp_w4_pack(jp_ctx* ctx, const jp_w4_desc* desc, const uint8_t* q, cons
 jp_status jp_w4_linear(jp_ctx* ctx, const jp_w4_desc* desc, const void* packed, const void* x, int64_t ld_x,
                        int64_t M, void* out, int64_t ld_out, int32_t out_dtype);
 
+/* ---------------------------------------------------------------------------
+ * Losses of one model over its own logits, with their gradient.  Nothing is kept in the context, as above.
+ *
+ * Common to both: logits [T, ld] of dtype, d_logits [T, ld_d] of the same dtype (NULL: no gradient; it may be the logits
+ * themselves, same pointer and pitch; no other overlap), 16-byte aligned with pitches a multiple of 16 bytes; tokens [T] int32,
+ * mask [T] uint8 or NULL.  With p = softmax(z / temperature) and x the row's token:
+ *   lp = log p_x,   d_logits[v] = grad_out dL/dlp (1[v = x] - p_v) / temperature, rounded once; 0 in all V places of a row that takes no part.
+ *   out_logp [T] fp32 or NULL: lp;  out_state [T] uint8 or NULL: 0 a row with mask 0 or a token outside [0, V), 1 a row that
+ *     takes part, 2 (policy loss) one whose ratio sits on the clipped branch, 3 a row without usable numbers
+ * A row holding NaN or +inf, or nothing above -1e38 (in units of log2: masked throughout), or whose terms are not finite (a token
+ * of probability 0 with a KL term, NaN among its inputs) has state 3 and takes no part, as a masked one; the
+ * others do not depend on it.  -inf logits have probability 0 and gradient 0.
+ * Rows with mask 0 are not read.  The same call gives the same bits.
+ *
+ * Clipped policy loss with a KL term to a reference model.  r = exp(lp - logp_old), d = logp_ref - lp:
+ *   l = max(-A r, -A clip(r, 1 - eps_lo, 1 + eps_hi)),   k = exp(d) - d - 1  (>= 0; its mean estimates KL(p || p_ref))
+ *   out_loss[0] = sum over valid rows of c (l + kl_coef k),  out_loss[1] = sum of c l,  out_loss[2] = sum of c k
+ *   c = token_weight / N, N = n_valid, or the rows with mask != 0 if n_valid is 0
+ * The gradient of the clipped branch is 0 in l.  One read and one write of the logits in HBM. */
+typedef struct {
+  int64_t T, V;          /* rows (0 is legal: loss 0) and vocabulary, below 2^31        */
+  int64_t ld, ld_d;      /* pitches in elements, 0 = V                                  */
+  int64_t n_valid;       /* N of the whole batch (this call may hold a part); 0: counted from the mask */
+  int32_t dtype;         /* JP_BF16 or JP_F32                                           */
+  float temperature;     /* 1e-4 .. 1e4; 0 means 1                                      */
+  float eps_lo, eps_hi;  /* clip range [1 - eps_lo, 1 + eps_hi], eps_lo <= 1; both 0: no clipping */
+  float kl_coef;         /* finite; used with logp_ref only                             */
+  float grad_out;        /* upstream scalar of the gradient; 0 means 1                  */
+} jp_policy_desc;
+/* 0: bad arguments, or T == 0 */
+size_t jp_policy_workspace_bytes(jp_ctx* ctx, int64_t T);
+/* advantages, logp_old [T] fp32, logp_ref, token_weight [T] fp32 or NULL; out_loss [3] fp32 in DEVICE memory, out_kl [T] or NULL: k */
+jp_status jp_policy_loss(jp_ctx* ctx, const jp_policy_desc* desc, const void* logits, const int32_t* tokens,
+                         const uint8_t* mask, const float* advantages, const float* logp_old, const float* logp_ref,
+                         const float* token_weight, float* out_loss, float* out_logp, float* out_kl, uint8_t* out_state,
+                         void* d_logits, void* workspace, size_t workspace_bytes);
+
+/* Preference loss over P pairs of sequences packed one after the other: sequence s is the rows seq_start[s] .. seq_start[s + 1] - 1
+ * (ascending, [2 P + 1] int32 in DEVICE memory; rows in front of the first and behind the last one take no part), 2 i chosen
+ * and 2 i + 1 rejected.  S_s = the sum of lp over the sequence's valid rows (JP_PREFERENCE_AVERAGE: their mean; 0 without any), R_s = ref_logp[s]
+ * (the reference model's S_s; NULL: 0):
+ *   h_i = beta ((S_2i - R_2i) - (S_2i+1 - R_2i+1)) - margin
+ *   out_loss[0] = mean over pairs of -(1 - label_smoothing) log sigma(h) - label_smoothing log sigma(-h)
+ * (0 if P is 0).  temperature is 1.  A row's coefficient needs both sequences of its pair, so the logits are read twice. */
+enum { JP_PREFERENCE_AVERAGE = 1 };
+typedef struct {
+  int64_t T, V, ld, ld_d;   /* as above                                                 */
+  int64_t P;                /* pairs, 0 .. 2^24                                         */
+  int32_t dtype;
+  int32_t flags;            /* 0 or JP_PREFERENCE_AVERAGE                               */
+  float beta;               /* finite                                                   */
+  float label_smoothing;    /* 0 .. 1                                                   */
+  float margin;             /* finite                                                   */
+  float grad_out;           /* 0 means 1                                                */
+} jp_preference_desc;
+/* 0: bad arguments, or T == 0 */
+size_t jp_preference_workspace_bytes(jp_ctx* ctx, int64_t T, int64_t P);
+/* out_loss [1] fp32; out_margin [P], out_seq_logp [2 P] fp32 or NULL: h and S */
+jp_status jp_preference_loss(jp_ctx* ctx, const jp_preference_desc* desc, const void* logits, const int32_t* tokens,
+                             const uint8_t* mask, const int32_t* seq_start, const float* ref_logp, float* out_loss,
+                             float* out_margin, float* out_seq_logp, float* out_logp, uint8_t* out_state, void* d_logits,
+                             void* workspace, size_t workspace_bytes);
+
 /* Self-test of the bounded waits (the paper has no counterpart).  Every wait inside the kernels
  * of this library (on a shared-memory barrier that the copy engine, another warp or the tensor
  * cores complete) gives up after a fixed number of SM clock cycles, sets JP_ERR_TIMEOUT in a

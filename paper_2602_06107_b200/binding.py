@@ -25,6 +25,7 @@ JP_DESC_SPARSE_CAP = 2
 JP_NORM_RMS = 1
 JP_W4_MAX_TOKENS = 32
 JP_VERIFY_MAX_DRAFT = 32
+JP_PREFERENCE_AVERAGE = 1
 
 EXPORTS = (
     "jp_create", "jp_destroy", "jp_set_stream", "jp_obrs_workspace_bytes", "jp_reserve",
@@ -34,6 +35,7 @@ EXPORTS = (
     "jp_layer_norm_forward", "jp_layer_norm_workspace_bytes", "jp_layer_norm_backward",
     "jp_w4_packed_bytes", "jp_w4_pack", "jp_w4_linear",
     "jp_verify_workspace_bytes", "jp_verify_draft",
+    "jp_policy_workspace_bytes", "jp_policy_loss", "jp_preference_workspace_bytes", "jp_preference_loss",
 )
 
 
@@ -103,6 +105,22 @@ class jp_verify_desc(ctypes.Structure):
     _fields_ = [
         ("B", ctypes.c_int64), ("V", ctypes.c_int64), ("ld_target", ctypes.c_int64), ("seq_target", ctypes.c_int64),
         ("ld_draft", ctypes.c_int64), ("seq_draft", ctypes.c_int64), ("N", ctypes.c_int32), ("dtype", ctypes.c_int32),
+    ]
+
+
+class jp_policy_desc(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int64), ("V", ctypes.c_int64), ("ld", ctypes.c_int64), ("ld_d", ctypes.c_int64),
+        ("n_valid", ctypes.c_int64), ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float), ("eps_lo", ctypes.c_float),
+        ("eps_hi", ctypes.c_float), ("kl_coef", ctypes.c_float), ("grad_out", ctypes.c_float),
+    ]
+
+
+class jp_preference_desc(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int64), ("V", ctypes.c_int64), ("ld", ctypes.c_int64), ("ld_d", ctypes.c_int64), ("P", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32), ("beta", ctypes.c_float), ("label_smoothing", ctypes.c_float),
+        ("margin", ctypes.c_float), ("grad_out", ctypes.c_float),
     ]
 
 
@@ -176,6 +194,12 @@ def load():
     lib.jp_verify_workspace_bytes.argtypes = [vp, i64, i32, i64, i32, ctypes.c_int]
     lib.jp_verify_workspace_bytes.restype = ctypes.c_size_t
     lib.jp_verify_draft.argtypes = [vp, ctypes.POINTER(jp_verify_desc)] + [vp] * 12 + [ctypes.c_size_t]
+    lib.jp_policy_workspace_bytes.argtypes = [vp, i64]
+    lib.jp_policy_workspace_bytes.restype = ctypes.c_size_t
+    lib.jp_policy_loss.argtypes = [vp, ctypes.POINTER(jp_policy_desc)] + [vp] * 13 + [ctypes.c_size_t]
+    lib.jp_preference_workspace_bytes.argtypes = [vp, i64, i64]
+    lib.jp_preference_workspace_bytes.restype = ctypes.c_size_t
+    lib.jp_preference_loss.argtypes = [vp, ctypes.POINTER(jp_preference_desc)] + [vp] * 12 + [ctypes.c_size_t]
     for name in EXPORTS:
         getattr(lib, name)          # raises AttributeError if the library lacks an entry point
     _lib = lib
@@ -525,6 +549,32 @@ def jp_verify_draft(ctx: Context, desc: jp_verify_desc, target_logits, draft_log
     ctx.call_on_current_stream(ctx.lib.jp_verify_draft, ctypes.byref(desc),
                                *_on_device(ctx, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept,
                                            u_sample, out_n_accepted, out_tokens, out_accept_prob, out_logp, workspace),
+                               0 if workspace is None else workspace.numel())
+
+
+def jp_policy_workspace_bytes(ctx: Context, T: int) -> int:
+    return _workspace_bytes(ctx, "jp_policy_workspace_bytes", T)
+
+
+def jp_policy_loss(ctx: Context, desc: jp_policy_desc, logits, tokens, mask, advantages, logp_old, logp_ref, token_weight,
+                   out_loss, out_logp, out_kl, out_state, d_logits, workspace):
+    """``workspace``: a uint8 CUDA tensor of at least jp_policy_workspace_bytes bytes, or None when T is 0."""
+    ctx.call_on_current_stream(ctx.lib.jp_policy_loss, ctypes.byref(desc),
+                               *_on_device(ctx, logits, tokens, mask, advantages, logp_old, logp_ref, token_weight, out_loss,
+                                           out_logp, out_kl, out_state, d_logits, workspace),
+                               0 if workspace is None else workspace.numel())
+
+
+def jp_preference_workspace_bytes(ctx: Context, T: int, P: int) -> int:
+    return _workspace_bytes(ctx, "jp_preference_workspace_bytes", T, P)
+
+
+def jp_preference_loss(ctx: Context, desc: jp_preference_desc, logits, tokens, mask, seq_start, ref_logp, out_loss, out_margin,
+                       out_seq_logp, out_logp, out_state, d_logits, workspace):
+    """``workspace``: a uint8 CUDA tensor of at least jp_preference_workspace_bytes bytes, or None when T is 0."""
+    ctx.call_on_current_stream(ctx.lib.jp_preference_loss, ctypes.byref(desc),
+                               *_on_device(ctx, logits, tokens, mask, seq_start, ref_logp, out_loss, out_margin, out_seq_logp,
+                                           out_logp, out_state, d_logits, workspace),
                                0 if workspace is None else workspace.numel())
 
 

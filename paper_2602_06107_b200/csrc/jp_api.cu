@@ -1026,6 +1026,121 @@ jp_status jp_verify_draft(jp_ctx* c, const jp_verify_desc* d, const void* target
   return JP_OK;
 }
 
+namespace {
+
+// What both losses share: sizes, pitches, alignment.
+jp_status loss_args(jp_ctx* c, int64_t T, int64_t V, int64_t ld, int64_t ld_d, int32_t dtype, float temperature, float grad_out,
+                    const void* logits, const void* d_logits, const int32_t* tokens, LossArgs* a) {
+  if (T < 0 || T > (int64_t)0x7fffffff || V < 1 || V > (int64_t)0x7fffffff) return fail(c, JP_ERR_INVALID_ARG, "T or V out of range");
+  if (dtype != JP_BF16 && dtype != JP_F32) return fail(c, JP_ERR_INVALID_ARG, "unknown dtype");
+  const int64_t es = dtype == JP_BF16 ? 2 : 4, most = (int64_t)1 << 31;      // (T < 2^31: row * pitch stays within 63 bits)
+  a->T = T; a->V = V; a->dtype = dtype;
+  a->ld = ld ? ld : V;
+  a->ld_d = ld_d ? ld_d : V;
+  if (a->ld < V || a->ld > most || (d_logits && (a->ld_d < V || a->ld_d > most)))
+    return fail(c, JP_ERR_INVALID_ARG, "a leading dimension is smaller than V or out of range");
+  if (temperature == 0.f) temperature = 1.f;
+  if (!(temperature >= 1e-4f && temperature <= 1e4f)) return fail(c, JP_ERR_INVALID_ARG, "temperature must lie in 1e-4 .. 1e4");
+  if (grad_out == 0.f) grad_out = 1.f;
+  if (!(grad_out > -3.0e38f && grad_out < 3.0e38f)) return fail(c, JP_ERR_INVALID_ARG, "grad_out must be finite");
+  a->c = (float)(1.4426950408889634 / (double)temperature);
+  a->c_to_nat = 1.0 / ((double)temperature * (double)a->c);
+  a->grad_scale = (double)grad_out / (double)temperature;
+  if (T == 0) return JP_OK;
+  if (!logits || !tokens) return fail(c, JP_ERR_INVALID_ARG, "logits or tokens is NULL");
+  if (a->ld * es % 16 || (d_logits && a->ld_d * es % 16)) return fail(c, JP_ERR_ALIGNMENT, "pitches must be multiples of 16 bytes");
+  if (!aligned16(logits) || !aligned16(d_logits)) return fail(c, JP_ERR_ALIGNMENT, "logits and d_logits must be 16-byte aligned");
+  if (d_logits == logits && a->ld != a->ld_d) return fail(c, JP_ERR_INVALID_ARG, "d_logits in the logits' place must have their pitch");
+  a->z = logits; a->dz = const_cast<void*>(d_logits); a->tokens = tokens;
+  return JP_OK;
+}
+
+jp_status loss_workspace(jp_ctx* c, const void* workspace, size_t have, size_t need) {
+  if (!workspace || have < need) return fail(c, JP_ERR_WORKSPACE, "workspace is NULL or smaller than the call's workspace_bytes function says");
+  if ((uintptr_t)workspace & 255u) return fail(c, JP_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  return JP_OK;
+}
+
+bool is_finite(float v) { return v > -3.4e38f && v < 3.4e38f; }
+
+}  // namespace
+
+size_t jp_policy_workspace_bytes(jp_ctx* c, int64_t T) { return !c || T < 1 || T > (int64_t)0x7fffffff ? 0 : policy_workspace_bytes(T); }
+
+jp_status jp_policy_loss(jp_ctx* c, const jp_policy_desc* d, const void* logits, const int32_t* tokens, const uint8_t* mask,
+                         const float* advantages, const float* logp_old, const float* logp_ref, const float* token_weight,
+                         float* out_loss, float* out_logp, float* out_kl, uint8_t* out_state, void* d_logits, void* workspace,
+                         size_t workspace_bytes) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  if (!d) return fail(c, JP_ERR_INVALID_ARG, "desc is NULL");
+  LossArgs a{};
+  jp_status st = loss_args(c, d->T, d->V, d->ld, d->ld_d, d->dtype, d->temperature, d->grad_out, logits, d_logits, tokens, &a);
+  if (st != JP_OK) return st;
+  if (d->n_valid < 0) return fail(c, JP_ERR_INVALID_ARG, "n_valid < 0");
+  if (!(d->eps_lo >= 0.f && d->eps_lo <= 1.f) || !(d->eps_hi >= 0.f && is_finite(d->eps_hi)))
+    return fail(c, JP_ERR_INVALID_ARG, "eps_lo must lie in 0 .. 1, eps_hi be finite and >= 0");
+  if (!is_finite(d->kl_coef)) return fail(c, JP_ERR_INVALID_ARG, "kl_coef must be finite");
+  if (!out_loss) return fail(c, JP_ERR_INVALID_ARG, "out_loss is NULL");
+  if (!aligned4(tokens, advantages, logp_old, logp_ref, token_weight, out_loss, out_logp, out_kl))
+    return fail(c, JP_ERR_ALIGNMENT, "int32 and fp32 arrays must be aligned to their elements");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  if (d->T == 0) {
+    const cudaError_t e = cudaMemsetAsync(out_loss, 0, 3 * sizeof(float), c->stream);
+    return e == cudaSuccess ? JP_OK : cuda_fail(c, e, "cudaMemsetAsync");
+  }
+  if (!advantages || !logp_old) return fail(c, JP_ERR_INVALID_ARG, "advantages or logp_old is NULL");
+  st = loss_workspace(c, workspace, workspace_bytes, policy_workspace_bytes(d->T));
+  if (st != JP_OK) return st;
+  a.mask = mask; a.advantages = advantages; a.logp_old = logp_old; a.logp_ref = logp_ref; a.token_weight = token_weight;
+  a.n_valid = d->n_valid; a.clip = d->eps_lo != 0.f || d->eps_hi != 0.f; a.eps_lo = d->eps_lo; a.eps_hi = d->eps_hi;
+  a.kl_coef = d->kl_coef;
+  a.out_loss = out_loss; a.out_logp = out_logp; a.out_kl = out_kl; a.out_state = out_state;
+  const cudaError_t e = launch_policy(a, workspace, c->stream, c->sms);
+  if (e != cudaSuccess) return cuda_fail(c, e, "policy loss launch");
+  c->launches += 2;
+  return JP_OK;
+}
+
+size_t jp_preference_workspace_bytes(jp_ctx* c, int64_t T, int64_t P) {
+  return !c || T < 1 || T > (int64_t)0x7fffffff || P < 0 || P > (1 << 24) ? 0 : preference_workspace_bytes(T, P);
+}
+
+jp_status jp_preference_loss(jp_ctx* c, const jp_preference_desc* d, const void* logits, const int32_t* tokens, const uint8_t* mask,
+                             const int32_t* seq_start, const float* ref_logp, float* out_loss, float* out_margin,
+                             float* out_seq_logp, float* out_logp, uint8_t* out_state, void* d_logits, void* workspace,
+                             size_t workspace_bytes) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  if (!d) return fail(c, JP_ERR_INVALID_ARG, "desc is NULL");
+  LossArgs a{};
+  jp_status st = loss_args(c, d->T, d->V, d->ld, d->ld_d, d->dtype, 1.f, d->grad_out, logits, d_logits, tokens, &a);
+  if (st != JP_OK) return st;
+  if (d->P < 0 || d->P > (1 << 24)) return fail(c, JP_ERR_INVALID_ARG, "P out of range");
+  if (d->flags & ~JP_PREFERENCE_AVERAGE) return fail(c, JP_ERR_INVALID_ARG, "unknown flag");
+  if (!is_finite(d->beta) || !is_finite(d->margin)) return fail(c, JP_ERR_INVALID_ARG, "beta and margin must be finite");
+  if (!(d->label_smoothing >= 0.f && d->label_smoothing <= 1.f)) return fail(c, JP_ERR_INVALID_ARG, "label_smoothing must lie in 0 .. 1");
+  if (!out_loss || !seq_start) return fail(c, JP_ERR_INVALID_ARG, "out_loss or seq_start is NULL");
+  if (!aligned4(tokens, seq_start, ref_logp, out_loss, out_margin, out_seq_logp, out_logp))
+    return fail(c, JP_ERR_ALIGNMENT, "int32 and fp32 arrays must be aligned to their elements");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  if (d->T == 0 && d->P > 0) return fail(c, JP_ERR_INVALID_ARG, "pairs without rows");
+  if (d->T == 0) {
+    const cudaError_t e = cudaMemsetAsync(out_loss, 0, sizeof(float), c->stream);
+    return e == cudaSuccess ? JP_OK : cuda_fail(c, e, "cudaMemsetAsync");
+  }
+  st = loss_workspace(c, workspace, workspace_bytes, preference_workspace_bytes(d->T, d->P));
+  if (st != JP_OK) return st;
+  a.mask = mask; a.seq_start = seq_start; a.ref_logp = ref_logp; a.P = d->P; a.average = (d->flags & JP_PREFERENCE_AVERAGE) != 0;
+  a.beta = d->beta; a.label_smoothing = d->label_smoothing; a.margin = d->margin;
+  a.out_loss = out_loss; a.out_margin = out_margin; a.out_seq_logp = out_seq_logp; a.out_logp = out_logp; a.out_state = out_state;
+  int n = 0;
+  const cudaError_t e = launch_preference(a, workspace, c->stream, c->sms, &n);
+  c->launches += n;
+  if (e != cudaSuccess) return cuda_fail(c, e, "preference loss launch");
+  return JP_OK;
+}
+
 jp_status jp_selftest_bounded_wait(jp_ctx* c, int64_t limit_cycles, int32_t* out_status) {
   if (!c) return JP_ERR_INVALID_ARG;
   if (limit_cycles < 1 || limit_cycles > 2000000000ll) return fail(c, JP_ERR_INVALID_ARG, "limit_cycles must lie in [1, 2e9] (about a second at most)");

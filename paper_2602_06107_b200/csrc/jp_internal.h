@@ -332,4 +332,51 @@ struct VerifyArgs {
 };
 cudaError_t launch_verify(VerifyArgs a, int dtype, cudaStream_t s);
 
+
+// Policy and preference losses over the logits of one model (jp_loss.cu).
+struct LossArgs {
+  const void* z;           // [T, ld]
+  void* dz;                // [T, ld_d] or null: no gradient
+  const int32_t* tokens;   // [T]
+  const uint8_t* mask;     // [T] or null
+  int64_t T, V, ld, ld_d;
+  int32_t dtype;
+  float c;                 // log2(e) / temperature
+  double c_to_nat;         // 1 / (temperature c): from units of c back to natural logarithms
+  double grad_scale;       // upstream scalar / temperature
+  float* out_loss;
+  float* out_logp;         // [T] or null
+  uint8_t* out_state;      // [T] or null
+  // policy
+  const float* advantages; // [T]
+  const float* logp_old;   // [T]
+  const float* logp_ref;   // [T] or null
+  const float* token_weight;   // [T] or null
+  int64_t n_valid;         // 0: the rows with mask != 0
+  bool clip;
+  float eps_lo, eps_hi, kl_coef;
+  float* out_kl;           // [T] or null
+  double* term;            // [T] workspace
+  double* kl_term;         // [T] workspace
+  // preference
+  const int32_t* seq_start;    // [2 P + 1]
+  const float* ref_logp;   // [2 P] or null
+  int64_t P;
+  bool average;
+  float beta, label_smoothing, margin;
+  float* out_margin;       // [P] or null
+  float* out_seq_logp;     // [2 P] or null
+  double* row_lp;          // workspace [T]: log-probability of the row's token, 0 where it takes no part
+  float2* row_sum;         // [T] maximum and sum of the row
+  float* row_coef;         // [T]
+  uint8_t* row_used;       // [T]
+  double* seq_sum;         // [2 P]
+  double* seq_per;         // [2 P]
+  int32_t cluster;         // set by the launch: blocks that share a row
+};
+size_t policy_workspace_bytes(int64_t T);
+cudaError_t launch_policy(LossArgs a, void* workspace, cudaStream_t s, int sms);
+size_t preference_workspace_bytes(int64_t T, int64_t P);
+cudaError_t launch_preference(LossArgs a, void* workspace, cudaStream_t s, int sms, int* n_launch);
+
 }  // namespace jp

@@ -355,3 +355,81 @@ def verify_draft(ctx: B.Context, target_logits, draft_logits, draft_tokens, u_ac
     B.jp_verify_draft(ctx, d, target_logits, draft_logits, draft_tokens, n_draft, temperature, u_accept, u_sample,
                       out["n_accepted"], out["tokens"], out.get("accept_prob"), out.get("logp"), ws)
     return out
+
+
+def _logit_pitch(t, shape, name):
+    """[T, V] logits with contiguous rows -> their pitch in elements."""
+    stride = t.stride()
+    if t.shape != shape or (stride[1] != 1 and shape[1] > 1):
+        raise B.JackpotError(f"{name} must be {list(shape)} with contiguous rows")
+    if shape[0] <= 1:
+        return (shape[1] + 7) // 8 * 8                       # a single row has no pitch of its own: any that is allowed
+    if stride[0] < shape[1]:
+        raise B.JackpotError(f"{name}: rows overlap")
+    return stride[0]
+
+
+def _loss_rows(logits, tokens, mask, grad, d_logits):
+    """Checks what the losses share: T, V, the pitches of logits and d_logits, and d_logits itself (None without ``grad``)."""
+    if logits.dim() != 2:
+        raise B.JackpotError("logits must be [T, V]")
+    shape = logits.shape
+    ld = _logit_pitch(logits, shape, "logits")
+    _dense(tokens, shape[:1], torch.int32, "tokens")
+    if mask is not None:
+        _dense(mask, shape[:1], torch.uint8, "mask")
+    if not grad:
+        return shape[0], shape[1], ld, 0, None
+    if d_logits is None:
+        d_logits = logits.new_empty((shape[0], (shape[1] + 7) // 8 * 8))[:, :shape[1]]
+    elif d_logits.dtype is not logits.dtype:
+        raise B.JackpotError("d_logits must have logits' dtype")
+    return shape[0], shape[1], ld, _logit_pitch(d_logits, shape, "d_logits"), d_logits
+
+
+def policy_loss(ctx: B.Context, logits, tokens, advantages, logp_old, *, logp_ref=None, mask=None, token_weight=None, n_valid=0,
+                eps_lo=0.2, eps_hi=0.2, kl_coef=0.0, temperature=1.0, grad_out=1.0, grad=True, d_logits=None):
+    """One jp_policy_loss call on torch's current stream: the clipped policy loss of one model's logits [T, V] with a KL term to a
+    reference model, and its gradient.  tokens [T] int32, advantages, logp_old, logp_ref, token_weight [T] fp32, mask [T] uint8.
+    ``n_valid``: the tokens of the whole batch, where this call holds a part of it (0: counted from the mask).  ``d_logits``: where the
+    gradient goes (may be ``logits``).  Returns ``loss`` [3] (whole, clipped term, KL term), ``logp``, ``kl``, ``state`` [T] and
+    ``d_logits`` (None without ``grad``).  Rows are a multiple of 16 bytes apart: those of an odd vocabulary are a slice of wider rows."""
+    T, V, ld, ld_d, d_logits = _loss_rows(logits, tokens, mask, grad, d_logits)
+    for t, name in ((advantages, "advantages"), (logp_old, "logp_old"), (logp_ref, "logp_ref"), (token_weight, "token_weight")):
+        if t is not None or name in ("advantages", "logp_old"):
+            _dense(t, (T,), torch.float32, name)
+    d = B._desc(ctx, B.jp_policy_desc, T, V, ld, ld_d, int(n_valid), B._dtype_code(logits), float(temperature), float(eps_lo),
+                float(eps_hi), float(kl_coef), float(grad_out))
+    out = dict(loss=advantages.new_empty(3), logp=torch.empty_like(advantages), kl=torch.empty_like(advantages),
+               state=torch.empty_like(advantages, dtype=torch.uint8), d_logits=d_logits)
+    need = B.jp_policy_workspace_bytes(ctx, T)
+    ws = advantages.new_empty(need, dtype=torch.uint8) if need else None
+    B.jp_policy_loss(ctx, d, logits, tokens, mask, advantages, logp_old, logp_ref, token_weight, out["loss"], out["logp"],
+                     out["kl"], out["state"], d_logits, ws)
+    return out
+
+
+def preference_loss(ctx: B.Context, logits, tokens, seq_start, *, ref_logp=None, mask=None, beta=0.1, label_smoothing=0.0,
+                    margin=0.0, average=False, grad_out=1.0, grad=True, d_logits=None):
+    """One jp_preference_loss call on torch's current stream: the loss of P pairs of sequences packed in logits [T, V], and its
+    gradient.  seq_start [2 P + 1] int32: sequence 2 i (chosen) and 2 i + 1 (rejected) are pair i; ref_logp [2 P] fp32: the reference
+    model's sums (means with ``average``).  Returns ``loss`` [1], ``margin`` [P], ``seq_logp`` [2 P], ``logp``, ``state`` [T] and
+    ``d_logits`` (None without ``grad``; may be ``logits``)."""
+    T, V, ld, ld_d, d_logits = _loss_rows(logits, tokens, mask, grad, d_logits)
+    if seq_start.dim() != 1 or seq_start.shape[0] % 2 == 0:
+        raise B.JackpotError("seq_start must be [2 P + 1]")
+    n = seq_start.shape[0] - 1
+    _dense(seq_start, (n + 1,), torch.int32, "seq_start")
+    if ref_logp is not None:
+        _dense(ref_logp, (n,), torch.float32, "ref_logp")
+    d = B._desc(ctx, B.jp_preference_desc, T, V, ld, ld_d, n // 2, B._dtype_code(logits),
+                B.JP_PREFERENCE_AVERAGE if average else 0, float(beta), float(label_smoothing), float(margin), float(grad_out))
+    f32 = torch.float32
+    out = dict(loss=seq_start.new_empty(1, dtype=f32), margin=seq_start.new_empty(n // 2, dtype=f32),
+               seq_logp=seq_start.new_empty(n, dtype=f32), logp=torch.empty_like(tokens, dtype=f32),
+               state=torch.empty_like(tokens, dtype=torch.uint8), d_logits=d_logits)
+    need = B.jp_preference_workspace_bytes(ctx, T, n // 2)
+    ws = seq_start.new_empty(need, dtype=torch.uint8) if need else None
+    B.jp_preference_loss(ctx, d, logits, tokens, mask, seq_start, ref_logp, out["loss"], out["margin"], out["seq_logp"],
+                         out["logp"], out["state"], d_logits, ws)
+    return out
