@@ -637,6 +637,47 @@ jp_status jp_preference_loss(jp_ctx* ctx, const jp_preference_desc* desc, const 
                              float* out_margin, float* out_seq_logp, float* out_logp, uint8_t* out_state, void* d_logits,
                              void* workspace, size_t workspace_bytes);
 
+/* The norms before and after a block of a model, fused with its gate and the residual stream (nothing is kept in the context, as
+ * above).  x is the block's output, rows of [T, H]:
+ *   u = norm(x) post_weight + post_bias   (the norm behind the block; u = x if post_weight is NULL)
+ *   sum = residual + scale token_gate[t] gate[h] u, rounded to its type   (a gate that is NULL is 1)
+ *   y = norm(sum) weight + bias           (the norm in front of the next block, of sum as stored)
+ * with norm(v) = (v - mu) r, mu and r as in jp_layer_norm_forward, JP_NORM_RMS for both norms alike.  Backward, from dy = dL/dy and dsum = what arrives
+ * at sum from elsewhere (NULL: nothing):
+ *   dresidual = dsum + the gradient of y's norm,   dx = the gradient through gate and first norm
+ *   dweight, dbias, dpost_weight, dpost_bias, dgate: sums over rows, dtoken_gate [T]: over a row; fp32, written, not added to.
+ * Statistics and sums are fp32; sum, y, dresidual and dx are rounded once (dx comes from the unrounded dresidual).  The same call
+ * gives the same bits. */
+typedef struct {
+  int64_t T, H;                              /* rows (0 is legal) and width, 1 .. 2^30-1        */
+  int64_t ld_x, ld_residual, ld_sum, ld_y;   /* row pitches in elements, 0 = H                  */
+  int64_t ld_dy, ld_dsum, ld_dx, ld_dresidual;
+  int32_t dtype;                             /* jp_dtype of all matrices; pointers aligned to the element, faster on 16 bytes */
+  int32_t param_dtype;                       /* jp_dtype of weights, biases and gate            */
+  int32_t flags;                             /* 0 or JP_NORM_RMS                                */
+  float eps;                                 /* >= 0, finite                                    */
+  float scale;                               /* of the residual branch, finite                  */
+} jp_block_norm_desc;
+/* weight [H]; bias, post_weight, post_bias (with post_weight only), gate [H] and token_gate [T] fp32 or NULL.  out_* [T] fp32 or NULL (means
+ * read 0 with JP_NORM_RMS; out_post_* are not written without post_weight).  sum may be residual or x, y may be x (or residual where
+ * sum is not): same pointer and pitch; no other overlap. */
+jp_status jp_block_norm_forward(jp_ctx* ctx, const jp_block_norm_desc* desc, const void* x, const void* residual,
+                                const void* weight, const void* bias, const void* post_weight, const void* post_bias,
+                                const void* gate, const float* token_gate, void* sum, void* y, float* out_mean,
+                                float* out_rstd, float* out_post_mean, float* out_post_rstd);
+/* 0: bad arguments, or T == 0 */
+size_t jp_block_norm_workspace_bytes(jp_ctx* ctx, int64_t T, int64_t H, int32_t dtype);
+/* mean, rstd, post_mean, post_rstd: the forward's (means NULL with JP_NORM_RMS, post_* without post_weight).  x may be NULL without
+ * post_weight and gates.  dbias NULL: neither dbias nor dpost_bias is wanted; else dpost_bias goes with post_weight.  dpost_weight,
+ * dgate, dtoken_gate go with post_weight, gate, token_gate.  dx and dresidual may each be one of dy, dsum, x, sum (same pointer and
+ * pitch; not both the same); no other overlap. */
+jp_status jp_block_norm_backward(jp_ctx* ctx, const jp_block_norm_desc* desc, const void* dy, const void* dsum,
+                                 const void* x, const void* sum, const void* weight, const void* post_weight,
+                                 const void* post_bias, const void* gate, const float* token_gate, const float* mean,
+                                 const float* rstd, const float* post_mean, const float* post_rstd, void* dx,
+                                 void* dresidual, float* dweight, float* dbias, float* dpost_weight, float* dpost_bias,
+                                 float* dgate, float* dtoken_gate, void* workspace, size_t workspace_bytes);
+
 /* Self-test of the bounded waits (the paper has no counterpart).  Every wait inside the kernels
  * of this library (on a shared-memory barrier that the copy engine, another warp or the tensor
  * cores complete) gives up after a fixed number of SM clock cycles, sets JP_ERR_TIMEOUT in a

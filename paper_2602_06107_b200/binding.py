@@ -36,6 +36,7 @@ EXPORTS = (
     "jp_w4_packed_bytes", "jp_w4_pack", "jp_w4_linear",
     "jp_verify_workspace_bytes", "jp_verify_draft",
     "jp_policy_workspace_bytes", "jp_policy_loss", "jp_preference_workspace_bytes", "jp_preference_loss",
+    "jp_block_norm_forward", "jp_block_norm_workspace_bytes", "jp_block_norm_backward",
 )
 
 
@@ -124,6 +125,15 @@ class jp_preference_desc(ctypes.Structure):
     ]
 
 
+class jp_block_norm_desc(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int64), ("H", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_residual", ctypes.c_int64),
+        ("ld_sum", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("ld_dy", ctypes.c_int64), ("ld_dsum", ctypes.c_int64),
+        ("ld_dx", ctypes.c_int64), ("ld_dresidual", ctypes.c_int64), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+        ("flags", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float),
+    ]
+
+
 STATS_BYTES = ctypes.sizeof(jp_stats)
 _lib = None
 
@@ -200,6 +210,10 @@ def load():
     lib.jp_preference_workspace_bytes.argtypes = [vp, i64, i64]
     lib.jp_preference_workspace_bytes.restype = ctypes.c_size_t
     lib.jp_preference_loss.argtypes = [vp, ctypes.POINTER(jp_preference_desc)] + [vp] * 12 + [ctypes.c_size_t]
+    lib.jp_block_norm_forward.argtypes = [vp, ctypes.POINTER(jp_block_norm_desc)] + [vp] * 14
+    lib.jp_block_norm_workspace_bytes.argtypes = [vp, i64, i64, i32]
+    lib.jp_block_norm_workspace_bytes.restype = ctypes.c_size_t
+    lib.jp_block_norm_backward.argtypes = [vp, ctypes.POINTER(jp_block_norm_desc)] + [vp] * 22 + [ctypes.c_size_t]
     for name in EXPORTS:
         getattr(lib, name)          # raises AttributeError if the library lacks an entry point
     _lib = lib
@@ -575,6 +589,28 @@ def jp_preference_loss(ctx: Context, desc: jp_preference_desc, logits, tokens, m
     ctx.call_on_current_stream(ctx.lib.jp_preference_loss, ctypes.byref(desc),
                                *_on_device(ctx, logits, tokens, mask, seq_start, ref_logp, out_loss, out_margin, out_seq_logp,
                                            out_logp, out_state, d_logits, workspace),
+                               0 if workspace is None else workspace.numel())
+
+
+def jp_block_norm_forward(ctx: Context, desc: jp_block_norm_desc, x, residual, weight, bias, post_weight, post_bias, gate, token_gate,
+                          sum, y, out_mean, out_rstd, out_post_mean, out_post_rstd):
+    ctx.call_on_current_stream(ctx.lib.jp_block_norm_forward, ctypes.byref(desc),
+                               *_on_device(ctx, x, residual, weight, bias, post_weight, post_bias, gate, token_gate, sum, y,
+                                           out_mean, out_rstd, out_post_mean, out_post_rstd))
+
+
+def jp_block_norm_workspace_bytes(ctx: Context, T: int, H: int, dtype: int) -> int:
+    return _workspace_bytes(ctx, "jp_block_norm_workspace_bytes", T, H, dtype)
+
+
+def jp_block_norm_backward(ctx: Context, desc: jp_block_norm_desc, dy, dsum, x, sum, weight, post_weight, post_bias, gate, token_gate,
+                           mean, rstd, post_mean, post_rstd, dx, dresidual, dweight, dbias, dpost_weight, dpost_bias, dgate,
+                           dtoken_gate, workspace):
+    """``workspace``: a uint8 CUDA tensor of at least jp_block_norm_workspace_bytes bytes, or None when T is 0."""
+    ctx.call_on_current_stream(ctx.lib.jp_block_norm_backward, ctypes.byref(desc),
+                               *_on_device(ctx, dy, dsum, x, sum, weight, post_weight, post_bias, gate, token_gate, mean, rstd,
+                                           post_mean, post_rstd, dx, dresidual, dweight, dbias, dpost_weight, dpost_bias, dgate,
+                                           dtoken_gate, workspace),
                                0 if workspace is None else workspace.numel())
 
 

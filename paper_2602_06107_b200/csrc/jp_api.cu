@@ -110,6 +110,7 @@ struct DeviceScope {
 };
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+template <class... P> bool elements_aligned(int32_t dtype, P... p) { return (((uintptr_t)p | ...) & (dtype == JP_BF16 ? 1u : 3u)) == 0; }      // NULL is aligned
 template <class... P> bool aligned4(P... p) { return (((uintptr_t)p | ...) & 3u) == 0; }      // int32 and fp32 arrays; NULL is aligned
 
 jp_status ensure_workspace(jp_ctx* c, int64_t rows, int k) {
@@ -1138,6 +1139,111 @@ jp_status jp_preference_loss(jp_ctx* c, const jp_preference_desc* d, const void*
   const cudaError_t e = launch_preference(a, workspace, c->stream, c->sms, &n);
   c->launches += n;
   if (e != cudaSuccess) return cuda_fail(c, e, "preference loss launch");
+  return JP_OK;
+}
+
+namespace {
+
+jp_status block_args(jp_ctx* c, const jp_block_norm_desc* d, BlockArgs* a) {
+  if (!d) return fail(c, JP_ERR_INVALID_ARG, "desc is NULL");
+  if (d->T < 0 || d->T > (int64_t)0x7fffffff || d->H < 1 || d->H > (int64_t)0x3fffffff)
+    return fail(c, JP_ERR_INVALID_ARG, "T or H out of range");
+  if ((d->dtype != JP_BF16 && d->dtype != JP_F32) || (d->param_dtype != JP_BF16 && d->param_dtype != JP_F32))
+    return fail(c, JP_ERR_INVALID_ARG, "unknown dtype");
+  if (d->flags & ~JP_NORM_RMS) return fail(c, JP_ERR_INVALID_ARG, "unknown flag");
+  if (!(d->eps >= 0.f) || !(d->eps < 3.0e38f)) return fail(c, JP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (!is_finite(d->scale)) return fail(c, JP_ERR_INVALID_ARG, "scale must be finite");
+  a->T = d->T; a->H = d->H;
+  const int64_t from[8] = {d->ld_x, d->ld_residual, d->ld_sum, d->ld_y, d->ld_dy, d->ld_dsum, d->ld_dx, d->ld_dresidual};
+  int64_t* const to[8] = {&a->ld_x, &a->ld_residual, &a->ld_sum, &a->ld_y, &a->ld_dy, &a->ld_dsum, &a->ld_dx, &a->ld_dresidual};
+  for (int i = 0; i < 8; ++i) {
+    *to[i] = from[i] ? from[i] : d->H;
+    if (*to[i] < d->H || *to[i] > (int64_t)0x3fffffff) return fail(c, JP_ERR_INVALID_ARG, "leading dimension < H or out of range");
+  }
+  a->dtype = d->dtype; a->param_bf16 = d->param_dtype == JP_BF16; a->rms = (d->flags & JP_NORM_RMS) != 0;
+  a->eps = d->eps; a->scale = d->scale;
+  return JP_OK;
+}
+
+}  // namespace
+
+jp_status jp_block_norm_forward(jp_ctx* c, const jp_block_norm_desc* d, const void* x, const void* residual, const void* weight,
+                                const void* bias, const void* post_weight, const void* post_bias, const void* gate,
+                                const float* token_gate, void* sum, void* y, float* out_mean, float* out_rstd, float* out_post_mean,
+                                float* out_post_rstd) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  BlockArgs a{};
+  const jp_status st = block_args(c, d, &a);
+  if (st != JP_OK) return st;
+  if (post_bias && !post_weight) return fail(c, JP_ERR_INVALID_ARG, "post_bias without post_weight");
+  if (a.T == 0) return JP_OK;
+  if (!x || !residual || !weight || !sum || !y) return fail(c, JP_ERR_INVALID_ARG, "x, residual, weight, sum or y is NULL");
+  if (sum == y) return fail(c, JP_ERR_INVALID_ARG, "sum and y are the same matrix");
+  if (!elements_aligned(d->dtype, x, residual, (const void*)sum, (const void*)y) ||
+      !elements_aligned(d->param_dtype, weight, bias, post_weight, post_bias, gate) ||
+      !aligned4(token_gate, out_mean, out_rstd, out_post_mean, out_post_rstd))
+    return fail(c, JP_ERR_ALIGNMENT, "matrices, parameters and fp32 arrays must be aligned to their elements");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  a.x = x; a.residual = residual; a.weight = weight; a.bias = bias; a.post_weight = post_weight; a.post_bias = post_bias;
+  a.gate = gate; a.token_gate = token_gate; a.sum = sum; a.y = y;
+  a.out_mean = out_mean; a.out_rstd = out_rstd; a.out_post_mean = out_post_mean; a.out_post_rstd = out_post_rstd;
+  const cudaError_t e = launch_block_forward(a, c->stream, c->sms);
+  if (e != cudaSuccess) return cuda_fail(c, e, "block norm launch");
+  c->launches += 1;
+  return JP_OK;
+}
+
+size_t jp_block_norm_workspace_bytes(jp_ctx* c, int64_t T, int64_t H, int32_t dtype) {
+  if (!c || T < 1 || T > (int64_t)0x7fffffff || H < 1 || H > (int64_t)0x3fffffff || (dtype != JP_BF16 && dtype != JP_F32)) return 0;
+  return block_workspace_bytes(T, H, dtype, c->sms);
+}
+
+jp_status jp_block_norm_backward(jp_ctx* c, const jp_block_norm_desc* d, const void* dy, const void* dsum, const void* x, const void* sum,
+                                 const void* weight, const void* post_weight, const void* post_bias, const void* gate,
+                                 const float* token_gate, const float* mean, const float* rstd, const float* post_mean,
+                                 const float* post_rstd, void* dx, void* dresidual, float* dweight, float* dbias, float* dpost_weight,
+                                 float* dpost_bias, float* dgate, float* dtoken_gate, void* workspace, size_t workspace_bytes) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  BlockArgs a{};
+  const jp_status st = block_args(c, d, &a);
+  if (st != JP_OK) return st;
+  if (post_bias && !post_weight) return fail(c, JP_ERR_INVALID_ARG, "post_bias without post_weight");
+  if (!dweight || (post_weight && (!dpost_weight || (dbias && !dpost_bias))) || (gate && !dgate))
+    return fail(c, JP_ERR_INVALID_ARG, "dweight, dpost_weight, dpost_bias or dgate is NULL");
+  if (!aligned4(token_gate, mean, rstd, post_mean, post_rstd, dweight, dbias, dpost_weight, dpost_bias, dgate, dtoken_gate))
+    return fail(c, JP_ERR_ALIGNMENT, "fp32 arrays must be aligned to their elements");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  if (a.T == 0) {
+    float* const sums[5] = {dweight, dbias, post_weight ? dpost_weight : nullptr, post_weight && dbias ? dpost_bias : nullptr, gate ? dgate : nullptr};
+    for (float* p : sums)
+      if (p) {
+        const cudaError_t e = cudaMemsetAsync(p, 0, (size_t)a.H * sizeof(float), c->stream);
+        if (e != cudaSuccess) return cuda_fail(c, e, "cudaMemsetAsync");
+      }
+    return JP_OK;
+  }
+  if (!dy || !sum || !weight || !rstd || !dx || !dresidual || (!mean && !a.rms))
+    return fail(c, JP_ERR_INVALID_ARG, "dy, sum, weight, rstd, mean, dx or dresidual is NULL");
+  if (post_weight && (!post_rstd || (!post_mean && !a.rms))) return fail(c, JP_ERR_INVALID_ARG, "post_rstd or post_mean is NULL");
+  if (!x && (post_weight || gate || token_gate)) return fail(c, JP_ERR_INVALID_ARG, "x is NULL");
+  if (token_gate && !dtoken_gate) return fail(c, JP_ERR_INVALID_ARG, "dtoken_gate is NULL");
+  if (dx == dresidual) return fail(c, JP_ERR_INVALID_ARG, "dx and dresidual are the same matrix");
+  if (!elements_aligned(d->dtype, dy, dsum, x, sum, (const void*)dx, (const void*)dresidual) ||
+      !elements_aligned(d->param_dtype, weight, post_weight, post_bias, gate))
+    return fail(c, JP_ERR_ALIGNMENT, "matrices and parameters must be aligned to their elements");
+  if (!workspace || workspace_bytes < block_workspace_bytes(a.T, a.H, a.dtype, c->sms))
+    return fail(c, JP_ERR_WORKSPACE, "workspace is NULL or smaller than jp_block_norm_workspace_bytes");
+  if ((uintptr_t)workspace & 255u) return fail(c, JP_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  a.dy = dy; a.dsum = dsum; a.x = x; a.sum = const_cast<void*>(sum); a.weight = weight; a.post_weight = post_weight;
+  a.post_bias = post_bias; a.gate = gate; a.token_gate = token_gate; a.mean = mean; a.rstd = rstd; a.post_mean = post_mean;
+  a.post_rstd = post_rstd; a.dx = dx; a.dresidual = dresidual; a.with_bias = dbias != nullptr;
+  a.dweight = dweight; a.dbias = dbias; a.dpost_weight = dpost_weight; a.dpost_bias = dpost_bias; a.dgate = dgate; a.dtoken_gate = dtoken_gate;
+  a.partial = (float*)workspace;
+  const cudaError_t e = launch_block_backward(a, c->stream, c->sms);
+  if (e != cudaSuccess) return cuda_fail(c, e, "block norm backward launch");
+  c->launches += 2;
   return JP_OK;
 }
 

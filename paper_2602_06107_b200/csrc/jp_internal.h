@@ -379,4 +379,45 @@ cudaError_t launch_policy(LossArgs a, void* workspace, cudaStream_t s, int sms);
 size_t preference_workspace_bytes(int64_t T, int64_t P);
 cudaError_t launch_preference(LossArgs a, void* workspace, cudaStream_t s, int sms, int* n_launch);
 
+// The norms around a block with gate and residual (jp_block.cu).
+struct BlockArgs {
+  const void* x;           // [T, ld_x] the block's output
+  const void* residual;    // forward: [T, ld_residual]
+  void* sum;               // [T, ld_sum] (backward: read)
+  void* y;                 // forward: [T, ld_y]
+  const void* dy;          // backward: [T, ld_dy]
+  const void* dsum;        // backward: [T, ld_dsum] or null
+  void* dx;                // backward: [T, ld_dx]
+  void* dresidual;         // backward: [T, ld_dresidual]
+  int64_t T, H, ld_x, ld_residual, ld_sum, ld_y, ld_dy, ld_dsum, ld_dx, ld_dresidual;
+  int32_t dtype;
+  bool param_bf16, rms;
+  float eps, scale;
+  const void* weight;      // [H] of the norm in front of the next block
+  const void* bias;        // [H] or null
+  const void* post_weight; // [H] of the norm behind this block, or null: none
+  const void* post_bias;   // [H] or null
+  const void* gate;        // [H] or null
+  const float* token_gate; // [T] or null
+  float* out_post_mean;    // forward: [T] or null each
+  float* out_post_rstd;
+  float* out_mean;
+  float* out_rstd;
+  const float* post_mean;  // backward: [T]
+  const float* post_rstd;
+  const float* mean;
+  const float* rstd;
+  bool with_bias;          // backward: dbias, and dpost_bias with a norm behind the block
+  float* dweight;          // [H]
+  float* dbias;
+  float* dpost_weight;
+  float* dpost_bias;
+  float* dgate;
+  float* dtoken_gate;      // [T]
+  float* partial;          // backward: [blocks, sums, H] workspace
+};
+cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms);
+size_t block_workspace_bytes(int64_t T, int64_t H, int dtype, int sms);
+cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms);
+
 }  // namespace jp

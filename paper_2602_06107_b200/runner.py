@@ -433,3 +433,73 @@ def preference_loss(ctx: B.Context, logits, tokens, seq_start, *, ref_logp=None,
     B.jp_preference_loss(ctx, d, logits, tokens, mask, seq_start, ref_logp, out["loss"], out["margin"], out["seq_logp"],
                          out["logp"], out["state"], d_logits, ws)
     return out
+
+
+def _block_params(x, weight, **vectors):
+    """Checks weight and what else of [H] there is; the dtype code of all of them."""
+    shape, param = x.shape[1:], weight.dtype
+    _dense(weight, shape, param, "weight")
+    for name, t in vectors.items():
+        if t is not None:
+            _dense(t, shape, param, name)
+    return B._dtype_code(weight, "weight")
+
+
+def _same(t, x, name):
+    if t.shape != x.shape or t.dtype is not x.dtype:
+        raise B.JackpotError(f"{name} must have x's shape and dtype")
+    return _rows(t, name)
+
+
+def block_norm(ctx: B.Context, x, residual, weight, bias=None, *, post_weight=None, post_bias=None, gate=None, token_gate=None,
+               scale=1.0, eps=1e-6, rms=False, out_sum=None, out=None):
+    """One jp_block_norm_forward call on torch's current stream: ``sum = residual + scale gate norm(x)`` and ``y = norm(sum)``, x [T, H]
+    being a block's output.  weight, bias: of the norm in front of the next block; post_weight, post_bias: of the norm behind this one
+    (None: x as it is); gate [H] of their dtype, token_gate [T] fp32.  ``out_sum`` and ``out``: where sum and y go (may be ``residual``
+    and ``x``).  Returns ``sum``, ``y``, ``mean``, ``rstd``, ``post_mean``, ``post_rstd`` (means None with ``rms``, post_* without a norm)."""
+    ld_x, ld_r = _rows(x, "x"), _same(residual, x, "residual")
+    param = _block_params(x, weight, bias=bias, post_weight=post_weight, post_bias=post_bias, gate=gate)
+    T, H = x.shape
+    if token_gate is not None:
+        _dense(token_gate, (T,), torch.float32, "token_gate")
+    total = _like(x) if out_sum is None else out_sum
+    y = _like(x) if out is None else out
+    d = B._desc(ctx, B.jp_block_norm_desc, T, H, ld_x, ld_r, _same(total, x, "out_sum"), _same(y, x, "out"), 0, 0, 0, 0,
+                B._dtype_code(x, "x"), param, B.JP_NORM_RMS if rms else 0, float(eps), float(scale))
+    post = post_weight is not None
+    mean, pmean = None if rms else x.new_empty(T, dtype=torch.float32), x.new_empty(T, dtype=torch.float32) if post and not rms else None
+    rstd, prstd = x.new_empty(T, dtype=torch.float32), x.new_empty(T, dtype=torch.float32) if post else None
+    B.jp_block_norm_forward(ctx, d, x, residual, weight, bias, post_weight, post_bias, gate, token_gate, total, y, mean, rstd, pmean, prstd)
+    return dict(sum=total, y=y, mean=mean, rstd=rstd, post_mean=pmean, post_rstd=prstd)
+
+
+def block_norm_backward(ctx: B.Context, dy, dsum, x, sum, weight, mean, rstd, *, post_weight=None, post_bias=None, post_mean=None,
+                        post_rstd=None, gate=None, token_gate=None, scale=1.0, rms=False, bias=True, dx=None, dresidual=None):
+    """One jp_block_norm_backward call on torch's current stream.  dsum: the gradient that arrives at ``sum`` from elsewhere (None:
+    nothing); mean, rstd, post_mean, post_rstd: the forward's.  ``bias``: whether dbias (and dpost_bias) are wanted; ``dx``, ``dresidual``: where
+    they go (may be ``dy`` and ``dsum``).  Returns ``dx``, ``dresidual`` and, fp32, ``dweight``, ``dbias``, ``dpost_weight``, ``dpost_bias``, ``dgate``,
+    ``dtoken_gate``; None for what there is not."""
+    ld_x, ld_s, ld_dy = _rows(x, "x"), _same(sum, x, "sum"), _same(dy, x, "dy")
+    ld_ds = 0 if dsum is None else _same(dsum, x, "dsum")
+    param = _block_params(x, weight, post_weight=post_weight, post_bias=post_bias, gate=gate)
+    T, H = x.shape
+    post = post_weight is not None
+    for t, name, need in ((mean, "mean", not rms), (rstd, "rstd", True), (post_mean, "post_mean", post and not rms),
+                          (post_rstd, "post_rstd", post), (token_gate, "token_gate", token_gate is not None)):
+        if need:
+            if t is None:
+                raise B.JackpotError(f"{name} is missing")
+            _dense(t, (T,), torch.float32, name)
+    dx = _like(x) if dx is None else dx
+    dresidual = _like(x) if dresidual is None else dresidual
+    d = B._desc(ctx, B.jp_block_norm_desc, T, H, ld_x, 0, ld_s, 0, ld_dy, ld_ds, _same(dx, x, "dx"), _same(dresidual, x, "dresidual"),
+                B._dtype_code(x, "x"), param, B.JP_NORM_RMS if rms else 0, 0.0, float(scale))
+    vec = lambda wanted, n=H: x.new_empty(n, dtype=torch.float32) if wanted else None
+    out = dict(dx=dx, dresidual=dresidual, dweight=vec(True), dbias=vec(bias), dpost_weight=vec(post), dpost_bias=vec(bias and post),
+               dgate=vec(gate is not None), dtoken_gate=vec(token_gate is not None, T))
+    need = B.jp_block_norm_workspace_bytes(ctx, T, H, d.dtype)
+    ws = x.new_empty(need, dtype=torch.uint8) if need else None
+    B.jp_block_norm_backward(ctx, d, dy, dsum, x, sum, weight, post_weight, post_bias, gate, token_gate, None if rms else mean, rstd,
+                             post_mean if post and not rms else None, post_rstd if post else None, dx, dresidual, out["dweight"],
+                             out["dbias"], out["dpost_weight"], out["dpost_bias"], out["dgate"], out["dtoken_gate"], ws)
+    return out
