@@ -678,6 +678,33 @@ jp_status jp_block_norm_backward(jp_ctx* ctx, const jp_block_norm_desc* desc, co
                                  void* dresidual, float* dweight, float* dbias, float* dpost_weight, float* dpost_bias,
                                  float* dgate, float* dtoken_gate, void* workspace, size_t workspace_bytes);
 
+/* Linear layer in 8-bit integers with a scale for each token and each output channel, such as a projection or the output layer of a
+ * quantised model over a prompt, or while it decodes more tokens than jp_w4_linear takes (nothing is kept in the context, as above):
+ *   sx[m] = max_k |x[m, k]| / 127,  xq[m, k] = 127 x[m, k] / max_k |x[m, k]| rounded to the nearest integer (halves to even, exactly; 0 in a row of zeros)
+ *   out[m, n] = sx[m] scales[n] sum_k xq[m, k] q[n, k]
+ * Sums are exact (int32), out is rounded from fp32 once.  A token that holds NaN or an infinity gives NaN, the others do not depend on it.
+ *
+ * jp_i8_pack lays the weights out once: q [N, ld_q] int8 (DEVICE, any value), scales [N] fp32, packed of jp_i8_packed_bytes(N, K)
+ * bytes (16-byte aligned).  jp_i8_linear takes the same N and K. */
+enum { JP_I8_MAX_K = 65536 };
+typedef struct {
+  int64_t N;             /* output features, 1 .. 2^31-1                 */
+  int64_t K;             /* input features, 1 .. JP_I8_MAX_K             */
+  int64_t ld_q;          /* jp_i8_pack: pitch of q, 0 = K                */
+} jp_i8_desc;
+/* 0: bad arguments */
+size_t jp_i8_packed_bytes(int64_t N, int64_t K);
+jp_status jp_i8_pack(jp_ctx* ctx, const jp_i8_desc* desc, const int8_t* q, const float* scales, void* packed);
+/* Bytes of M tokens of K features once they are quantised (0: bad arguments, or M == 0); 0 <= M < 2^24. */
+size_t jp_i8_token_bytes(int64_t M, int64_t K);
+/* Quantises x [M, ld_x] bf16 (0 = K, aligned to its elements) into tokens (16-byte aligned), for several layers that read the same x. */
+jp_status jp_i8_quantize(jp_ctx* ctx, const void* x, int64_t ld_x, int64_t M, int64_t K, void* tokens, size_t token_bytes);
+/* out [M, ld_out] of out_dtype (JP_BF16 or JP_F32, 0 = N).  x [M, ld_x] bf16 is quantised into tokens first; x NULL: tokens are as
+ * jp_i8_quantize left them.  out_status: one int32 in DEVICE memory or NULL: 0, or JP_ERR_TIMEOUT if a wait inside the kernel
+ * ran out (out is then unspecified). */
+jp_status jp_i8_linear(jp_ctx* ctx, const jp_i8_desc* desc, const void* packed, const void* x, int64_t ld_x, int64_t M,
+                       void* tokens, size_t token_bytes, void* out, int64_t ld_out, int32_t out_dtype, int32_t* out_status);
+
 /* Self-test of the bounded waits (the paper has no counterpart).  Every wait inside the kernels
  * of this library (on a shared-memory barrier that the copy engine, another warp or the tensor
  * cores complete) gives up after a fixed number of SM clock cycles, sets JP_ERR_TIMEOUT in a

@@ -26,6 +26,7 @@ JP_NORM_RMS = 1
 JP_W4_MAX_TOKENS = 32
 JP_VERIFY_MAX_DRAFT = 32
 JP_PREFERENCE_AVERAGE = 1
+JP_I8_MAX_K = 65536
 
 EXPORTS = (
     "jp_create", "jp_destroy", "jp_set_stream", "jp_obrs_workspace_bytes", "jp_reserve",
@@ -37,6 +38,7 @@ EXPORTS = (
     "jp_verify_workspace_bytes", "jp_verify_draft",
     "jp_policy_workspace_bytes", "jp_policy_loss", "jp_preference_workspace_bytes", "jp_preference_loss",
     "jp_block_norm_forward", "jp_block_norm_workspace_bytes", "jp_block_norm_backward",
+    "jp_i8_packed_bytes", "jp_i8_pack", "jp_i8_token_bytes", "jp_i8_quantize", "jp_i8_linear",
 )
 
 
@@ -134,6 +136,10 @@ class jp_block_norm_desc(ctypes.Structure):
     ]
 
 
+class jp_i8_desc(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("K", ctypes.c_int64), ("ld_q", ctypes.c_int64)]
+
+
 STATS_BYTES = ctypes.sizeof(jp_stats)
 _lib = None
 
@@ -214,6 +220,13 @@ def load():
     lib.jp_block_norm_workspace_bytes.argtypes = [vp, i64, i64, i32]
     lib.jp_block_norm_workspace_bytes.restype = ctypes.c_size_t
     lib.jp_block_norm_backward.argtypes = [vp, ctypes.POINTER(jp_block_norm_desc)] + [vp] * 22 + [ctypes.c_size_t]
+    lib.jp_i8_packed_bytes.argtypes = [i64, i64]
+    lib.jp_i8_packed_bytes.restype = ctypes.c_size_t
+    lib.jp_i8_pack.argtypes = [vp, ctypes.POINTER(jp_i8_desc), vp, vp, vp]
+    lib.jp_i8_token_bytes.argtypes = [i64, i64]
+    lib.jp_i8_token_bytes.restype = ctypes.c_size_t
+    lib.jp_i8_quantize.argtypes = [vp, vp, i64, i64, i64, vp, ctypes.c_size_t]
+    lib.jp_i8_linear.argtypes = [vp, ctypes.POINTER(jp_i8_desc), vp, vp, i64, i64, vp, ctypes.c_size_t, vp, i64, i32, vp]
     for name in EXPORTS:
         getattr(lib, name)          # raises AttributeError if the library lacks an entry point
     _lib = lib
@@ -612,6 +625,30 @@ def jp_block_norm_backward(ctx: Context, desc: jp_block_norm_desc, dy, dsum, x, 
                                            post_mean, post_rstd, dx, dresidual, dweight, dbias, dpost_weight, dpost_bias, dgate,
                                            dtoken_gate, workspace),
                                0 if workspace is None else workspace.numel())
+
+
+def jp_i8_packed_bytes(N: int, K: int) -> int:
+    return int(load().jp_i8_packed_bytes(N, K))
+
+
+def jp_i8_pack(ctx: Context, desc: jp_i8_desc, q, scales, packed):
+    ctx.call_on_current_stream(ctx.lib.jp_i8_pack, ctypes.byref(desc), *_on_device(ctx, q, scales, packed))
+
+
+def jp_i8_token_bytes(M: int, K: int) -> int:
+    return int(load().jp_i8_token_bytes(M, K))
+
+
+def jp_i8_quantize(ctx: Context, x, ld_x: int, M: int, K: int, tokens):
+    xa, ta = _on_device(ctx, x, tokens)
+    ctx.call_on_current_stream(ctx.lib.jp_i8_quantize, xa, ld_x, M, K, ta, 0 if tokens is None else tokens.numel())
+
+
+def jp_i8_linear(ctx: Context, desc: jp_i8_desc, packed, x, ld_x: int, M: int, tokens, out, ld_out: int, out_dtype: int, out_status=None):
+    """``tokens``: a uint8 CUDA tensor of at least jp_i8_token_bytes bytes, or None when M is 0."""
+    p, xa, ta, oa, sa = _on_device(ctx, packed, x, tokens, out, out_status)
+    ctx.call_on_current_stream(ctx.lib.jp_i8_linear, ctypes.byref(desc), p, xa, ld_x, M, ta, 0 if tokens is None else tokens.numel(),
+                               oa, ld_out, out_dtype, sa)
 
 
 def jp_enable_kernel_timing(ctx: Context, on: bool):

@@ -1247,6 +1247,109 @@ jp_status jp_block_norm_backward(jp_ctx* c, const jp_block_norm_desc* d, const v
   return JP_OK;
 }
 
+namespace {
+
+jp_status i8_shape(jp_ctx* c, const jp_i8_desc* d) {
+  if (!d) return fail(c, JP_ERR_INVALID_ARG, "desc is NULL");
+  if (d->N < 1 || d->N > (int64_t)0x7fffffff) return fail(c, JP_ERR_INVALID_ARG, "N out of range");
+  if (d->K < 1 || d->K > JP_I8_MAX_K) return fail(c, JP_ERR_INVALID_ARG, "K out of range (1 .. JP_I8_MAX_K)");
+  return JP_OK;
+}
+
+jp_status i8_quantize(jp_ctx* c, const void* x, int64_t ld_x, int64_t M, int64_t K, void* tokens) {
+  I8QuantArgs a{};
+  a.x = x; a.tokens = tokens; a.M = M; a.K = K; a.ld_x = ld_x;
+  const cudaError_t e = launch_i8_quantize(a, c->stream);
+  if (e != cudaSuccess) return cuda_fail(c, e, "8-bit quantisation launch");
+  c->launches += 1;
+  return JP_OK;
+}
+
+jp_status i8_tokens(jp_ctx* c, const void* x, int64_t ld_x, int64_t M, int64_t K, const void* tokens, size_t token_bytes) {
+  if (M < 0) return fail(c, JP_ERR_INVALID_ARG, "M < 0");
+  if (M >= (1 << 24)) return fail(c, JP_ERR_TOO_LARGE, "2^24 tokens or more");
+  if (ld_x < K || ld_x > (int64_t)1 << 38) return fail(c, JP_ERR_INVALID_ARG, "a leading dimension is smaller than a row or out of range");
+  if (M == 0) return JP_OK;
+  if (!tokens || token_bytes < i8_token_bytes(M, K)) return fail(c, JP_ERR_WORKSPACE, "tokens is NULL or smaller than jp_i8_token_bytes");
+  if (!aligned16(tokens)) return fail(c, JP_ERR_ALIGNMENT, "tokens must be 16-byte aligned");
+  if ((uintptr_t)x & 1u) return fail(c, JP_ERR_ALIGNMENT, "x must be aligned to its elements");
+  return JP_OK;
+}
+
+}  // namespace
+
+size_t jp_i8_packed_bytes(int64_t N, int64_t K) {
+  return N < 1 || N > (int64_t)0x7fffffff || K < 1 || K > JP_I8_MAX_K ? 0 : i8_packed_bytes(N, K);
+}
+
+size_t jp_i8_token_bytes(int64_t M, int64_t K) { return M < 1 || M >= (1 << 24) || K < 1 || K > JP_I8_MAX_K ? 0 : i8_token_bytes(M, K); }
+
+jp_status jp_i8_pack(jp_ctx* c, const jp_i8_desc* d, const int8_t* q, const float* scales, void* packed) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  const jp_status st = i8_shape(c, d);
+  if (st != JP_OK) return st;
+  if (!q || !scales || !packed) return fail(c, JP_ERR_INVALID_ARG, "q, scales or packed is NULL");
+  if (!aligned16(packed)) return fail(c, JP_ERR_ALIGNMENT, "packed must be 16-byte aligned");
+  if (!aligned4(scales)) return fail(c, JP_ERR_ALIGNMENT, "scales must be aligned to their elements");
+  I8PackArgs a{};
+  a.q = q; a.scales = scales; a.packed = packed; a.N = d->N; a.K = d->K; a.ld_q = d->ld_q ? d->ld_q : d->K;
+  if (a.ld_q < d->K || a.ld_q > (int64_t)1 << 31) return fail(c, JP_ERR_INVALID_ARG, "a leading dimension is smaller than a row or out of range");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  const cudaError_t e = launch_i8_pack(a, c->stream, c->sms);
+  if (e != cudaSuccess) return cuda_fail(c, e, "8-bit layout launch");
+  c->launches += 1;
+  return JP_OK;
+}
+
+jp_status jp_i8_quantize(jp_ctx* c, const void* x, int64_t ld_x, int64_t M, int64_t K, void* tokens, size_t token_bytes) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  if (K < 1 || K > JP_I8_MAX_K) return fail(c, JP_ERR_INVALID_ARG, "K out of range (1 .. JP_I8_MAX_K)");
+  if (ld_x == 0) ld_x = K;
+  const jp_status st = i8_tokens(c, x, ld_x, M, K, tokens, token_bytes);
+  if (st != JP_OK || M == 0) return st;
+  if (!x) return fail(c, JP_ERR_INVALID_ARG, "x is NULL");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  return i8_quantize(c, x, ld_x, M, K, tokens);
+}
+
+jp_status jp_i8_linear(jp_ctx* c, const jp_i8_desc* d, const void* packed, const void* x, int64_t ld_x, int64_t M, void* tokens,
+                       size_t token_bytes, void* out, int64_t ld_out, int32_t out_dtype, int32_t* out_status) {
+  if (!c) return JP_ERR_INVALID_ARG;
+  jp_status st = i8_shape(c, d);
+  if (st != JP_OK) return st;
+  if (out_dtype != JP_BF16 && out_dtype != JP_F32) return fail(c, JP_ERR_INVALID_ARG, "out must be JP_BF16 or JP_F32");
+  if (ld_x == 0) ld_x = d->K;
+  if (ld_out == 0) ld_out = d->N;
+  if (ld_out < d->N || ld_out > (int64_t)1 << 38) return fail(c, JP_ERR_INVALID_ARG, "a leading dimension is smaller than a row or out of range");
+  st = i8_tokens(c, x, ld_x, M, d->K, tokens, token_bytes);
+  if (st != JP_OK) return st;
+  if (!aligned4(out_status)) return fail(c, JP_ERR_ALIGNMENT, "out_status must be aligned to its element");
+  DeviceScope dev(c->device);
+  if (!dev.ok) return fail(c, JP_ERR_CUDA, "cannot select the context's device");
+  if (M > 0) {
+    if (!packed || !out) return fail(c, JP_ERR_INVALID_ARG, "packed or out is NULL");
+    if (!aligned16(packed)) return fail(c, JP_ERR_ALIGNMENT, "packed must be 16-byte aligned");
+    if (!element_aligned(out, out_dtype)) return fail(c, JP_ERR_ALIGNMENT, "out must be aligned to its elements");
+  }
+  if (out_status) {
+    const cudaError_t e = cudaMemsetAsync(out_status, 0, sizeof(int32_t), c->stream);
+    if (e != cudaSuccess) return cuda_fail(c, e, "cudaMemsetAsync");
+  }
+  if (M == 0) return JP_OK;
+  if (x) {
+    st = i8_quantize(c, x, ld_x, M, d->K, tokens);
+    if (st != JP_OK) return st;
+  }
+  I8Args a{};
+  a.out = out; a.status = out_status; a.M = M; a.N = d->N; a.ld_out = ld_out; a.early = x != nullptr;
+  const cudaError_t e = launch_i8_linear(a, packed, tokens, d->K, out_dtype == JP_BF16, c->stream, c->sms);
+  if (e != cudaSuccess) return cuda_fail(c, e, "8-bit linear layer launch");
+  c->launches += 1;
+  return JP_OK;
+}
+
 jp_status jp_selftest_bounded_wait(jp_ctx* c, int64_t limit_cycles, int32_t* out_status) {
   if (!c) return JP_ERR_INVALID_ARG;
   if (limit_cycles < 1 || limit_cycles > 2000000000ll) return fail(c, JP_ERR_INVALID_ARG, "limit_cycles must lie in [1, 2e9] (about a second at most)");

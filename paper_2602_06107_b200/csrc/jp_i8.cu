@@ -1,0 +1,466 @@
+// Linear layers in 8-bit integers: out[m, n] = sx[m] sw[n] sum_k xq[m, k] q[n, k], with a scale a token (sx = max |x| / 127, xq = x / sx
+// rounded to the nearest integer) and a scale an output channel.  Products and sums are exact in int32; out is rounded once.
+//
+// The weights are the A operand of tcgen05.mma (kind::i8, 128 channels an instruction) and the tokens the B operand (16 to 256 of them),
+// so that few tokens waste no rows of an instruction: a decode step reads the weights once at HBM's rate, a prompt keeps the tensor cores busy.  Both
+// operands lie in memory as the instruction wants them in shared memory: atoms of 8 rows x 128 bytes in the 128-byte swizzle (16-byte chunk c
+// of row r at chunk c ^ (r & 7)), padded with zeros to whole atoms.  So a stage of the ring is two plain bulk copies, of one run of memory each,
+// with no tensor map and no edge cases:
+//   weights  [N / 128 tiles][K / 128 blocks][128 rows x 128 bytes], laid out once;  scales [N]
+//   tokens   [K / 128 blocks][M / 8 groups][8 rows x 128 bytes], written by the quantisation;  scales [M]
+// A CTA (one an SM): warp 0 copies, warp 1 issues the instructions into one of two accumulators in tensor memory, warps 2 to 5 scale and
+// store the other one.  Where the tiles do not fill the GPU, the CTAs of a cluster share a tile's K and add their integers through
+// distributed shared memory (any order gives the same bits).
+#include "jp_common.cuh"
+#include "jp_internal.h"
+
+namespace jp {
+namespace {
+
+constexpr int kRows = 128;                    // channels of a tile
+constexpr int kBlock = 128;                   // k of a stage: one row of the swizzle
+constexpr int kTileBytes = kRows * kBlock;
+constexpr int kThreads = 192;
+constexpr int kMaxStages = 12;
+constexpr int kRingBytes = 200 * 1024;
+constexpr long long kSpin = 4000000000ll;     // clock cycles after which a wait gives up
+
+struct Control {                              // behind the ring in shared memory
+  unsigned long long full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
+  float sx[4][256];
+  uint32_t tmem;
+  int abort;
+};
+constexpr int kSharedBytes = 1024 + kRingBytes + (int)sizeof(Control);
+static_assert(kSharedBytes <= 232448, "beyond the 227 KB a CTA can have");
+
+__device__ __forceinline__ uint32_t s32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(unsigned long long* b, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s32(b)), "r"(n) : "memory"); }
+__device__ __forceinline__ void bar_arrive(unsigned long long* b) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(s32(b)) : "memory"); }
+__device__ __forceinline__ void bar_expect(unsigned long long* b, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(s32(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(unsigned long long* b, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(s32(b)), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __noinline__ bool bar_wait(unsigned long long* b, uint32_t parity, volatile int* abort) {      // false: gave up, or another role did
+  long long t0 = 0;
+  for (uint32_t i = 0;; ++i) {
+    if (bar_try(b, parity)) return true;
+    if ((i & 63u) == 0u) {
+      if (*abort) return false;
+      const long long now = clock64();
+      if (i == 0u) t0 = now;
+      else if (now - t0 > kSpin) { *abort = 1; return false; }
+    }
+  }
+}
+__device__ __forceinline__ void copy(void* to, const void* from, uint32_t bytes, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(s32(to)), "l"(from), "r"(bytes), "r"(s32(bar)) : "memory");
+}
+// Shared-memory descriptor of a K-major operand in the 128-byte swizzle: address / 16, 1024 bytes between groups of 8 rows, version 1.
+__device__ __forceinline__ uint64_t operand(uint32_t address) {
+  return (uint64_t)((address & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void commit(unsigned long long* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(s32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, int (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+template <bool BF16> __device__ __forceinline__ void put(void* out, int64_t i, float v) {
+  if constexpr (BF16) ((__nv_bfloat16*)out)[i] = __float2bfloat16_rn(v);
+  else ((float*)out)[i] = v;
+}
+
+template <bool BF16, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
+  extern __shared__ unsigned char raw[];
+  unsigned char* const ring = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+  Control& sm = *(Control*)(ring + kRingBytes);
+  uint32_t rank = 0;
+  if (SPLIT) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int TN = A.tokens_tile, stages = A.stages, ranks = SPLIT ? A.split : 1;
+  const uint32_t stage_bytes = kTileBytes + (uint32_t)TN * kBlock;
+  const int k0 = SPLIT ? (int)(A.kblocks * rank / ranks) : 0, k1 = SPLIT ? (int)(A.kblocks * (rank + 1) / ranks) : (int)A.kblocks;
+  const int64_t first = blockIdx.x / ranks, step = gridDim.x / ranks;       // tiles of this CTA (with a split: one)
+
+  if (tid == 0) {
+    for (int s = 0; s < stages; ++s) { bar_init(&sm.full[s], 1); bar_init(&sm.empty[s], 1); }
+    for (int b = 0; b < 2; ++b) { bar_init(&sm.acc_full[b], 1); bar_init(&sm.acc_empty[b], 4); }
+    sm.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s32(&sm.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    fence_before();
+  }
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *(volatile uint32_t*)&sm.tmem;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  if (warp == 0) {
+    // ---- copies of the next stage of both operands, tile after tile
+    if (lane == 0) {
+      // The weights do not depend on the quantisation in front of this kernel: with A.early their first stages are fetched before it is done.
+      uint32_t armed = 0;
+      bool ok = true, waited = false;
+      auto tokens = [&](int64_t tile, int kb, uint32_t s) {
+        const int64_t m0 = tile % A.tiles_m * TN, rows = A.padded_m - m0 < TN ? A.padded_m - m0 : TN;
+        copy(ring + s * stage_bytes + kTileBytes, A.xq + ((int64_t)kb * (A.padded_m / 8) + m0 / 8) * 1024, (uint32_t)rows * kBlock, &sm.full[s]);
+      };
+      auto arm = [&](int64_t tile, int kb, uint32_t s) {
+        const int64_t m0 = tile % A.tiles_m * TN, rows = A.padded_m - m0 < TN ? A.padded_m - m0 : TN;
+        bar_expect(&sm.full[s], kTileBytes + (uint32_t)rows * kBlock);
+        copy(ring + s * stage_bytes, A.weights + (tile / A.tiles_m * A.kblocks + kb) * kTileBytes, kTileBytes, &sm.full[s]);
+      };
+      if (A.early && first < A.tiles) {
+        const int n = k1 - k0 < stages ? k1 - k0 : stages;
+        for (int i = 0; i < n; ++i) arm(first, k0 + i, i);
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        waited = true;
+        for (int i = 0; i < n; ++i) tokens(first, k0 + i, i);
+        armed = n;
+      }
+      if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+      uint32_t n = 0;                          // stages passed
+      for (int64_t tile = first; tile < A.tiles && ok; tile += step)
+        for (int kb = k0; kb < k1; ++kb, ++n) {
+          if (n < armed) continue;
+          const uint32_t s = n % stages, use = n / stages;
+          if (!bar_wait(&sm.empty[s], (use & 1u) ^ 1u, &sm.abort)) { ok = false; break; }
+          arm(tile, kb, s);
+          tokens(tile, kb, s);
+        }
+      if (!ok) {                               // leave no copy in flight: wait (bounded) for the last one of every stage
+        if (A.status) atomicExch(A.status, (int)JP_ERR_TIMEOUT);
+        for (uint32_t i = n < (uint32_t)stages ? 0 : n - stages; i < n; ++i) {
+          const long long t0 = clock64();
+          while (!bar_try(&sm.full[i % stages], (i / stages) & 1u))
+            if (clock64() - t0 > kSpin) break;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---- instructions: 32 k each, four a stage
+    if (lane == 0) {
+      // int32 accumulator, signed 8-bit operands, both K-major, TN columns, 128 rows
+      const uint32_t shape = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+      uint32_t n = 0;
+      bool ok = true;
+      int t = 0;
+      for (int64_t tile = first; tile < A.tiles && ok; tile += step, ++t) {
+        const uint32_t buf = t & 1, use = t >> 1;
+        if (!bar_wait(&sm.acc_empty[buf], (use & 1u) ^ 1u, &sm.abort)) { ok = false; break; }
+        fence_after();
+        for (int kb = k0; kb < k1; ++kb, ++n) {
+          const uint32_t s = n % stages;
+          if (!bar_wait(&sm.full[s], (n / stages) & 1u, &sm.abort)) { ok = false; break; }
+          fence_after();
+          const uint32_t at = s32(ring) + s * stage_bytes;
+          const uint64_t a = operand(at), b = operand(at + kTileBytes);
+#pragma unroll
+          for (int q = 0; q < kBlock / 32; ++q)      // 32 bytes further inside the swizzled row: start address + 2
+            mma_i8(tmem + buf * 256, a + q * 2, b + q * 2, shape, kb != k0 || q != 0);
+          commit(&sm.empty[s]);
+        }
+        if (ok) commit(&sm.acc_full[buf]);
+      }
+      if (!ok && A.status) atomicExch(A.status, (int)JP_ERR_TIMEOUT);
+    }
+  } else {
+    // ---- results: a thread has one channel, columns are tokens
+    const int q = warp & 3;                    // the quarter of tensor memory's lanes this warp may read
+    const int row = q * 32 + lane;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    int t = 0;
+    for (int64_t tile = first; tile < A.tiles; tile += step, ++t) {
+      const uint32_t buf = t & 1, use = t >> 1;
+      const int64_t m0 = tile % A.tiles_m * TN, n = tile / A.tiles_m * kRows + row;
+      const int cols = (int)(A.M - m0 < TN ? A.M - m0 : TN);
+      const float sw = n < A.N ? A.weight_scales[n] : 0.f;
+      if (!SPLIT) {
+        __syncwarp();
+        for (int c = lane; c < cols; c += 32) sm.sx[q][c] = __ldcg(A.token_scales + m0 + c);
+        __syncwarp();
+      }
+      if (!bar_wait(&sm.acc_full[buf], use & 1u, &sm.abort)) {
+        if (lane == 0 && A.status) atomicExch(A.status, (int)JP_ERR_TIMEOUT);
+        break;
+      }
+      fence_after();
+      const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + buf * 256;
+#pragma unroll 1
+      for (int c0 = 0; c0 < cols; c0 += 16) {
+        int r[16];
+        tmem_ld16(from + c0, r);
+        if (SPLIT) {                           // (the ring is free: all of its stages have been read)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) ((int*)ring)[(c0 + j) * kRows + row] = r[j];
+        } else if (n < A.N) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (c0 + j < cols) put<BF16>(A.out, (m0 + c0 + j) * A.ld_out + n, (float)r[j] * (sm.sx[q][c0 + j] * sw));
+        }
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(&sm.acc_empty[buf]);
+    }
+  }
+  if (SPLIT) {                                 // the ranks' sums of every rank-th token
+    __syncwarp();
+    cluster_sync();
+    const int64_t tile = first;
+    if (warp >= 2 && !*(volatile int*)&sm.abort) {
+      const int row = (warp & 3) * 32 + lane;
+      const int64_t m0 = tile % A.tiles_m * TN, n = tile / A.tiles_m * kRows + row;
+      const int cols = (int)(A.M - m0 < TN ? A.M - m0 : TN);
+      if (n < A.N) {
+        const float sw = A.weight_scales[n];
+        for (int c = rank; c < cols; c += ranks) {
+          int sum = 0;
+          for (int r = 0; r < ranks; ++r) {
+            uint32_t from;
+            int v;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(s32((int*)ring + c * kRows + row)), "r"(r));
+            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(from) : "memory");
+            sum += v;
+          }
+          put<BF16>(A.out, (m0 + c) * A.ld_out + n, (float)sum * (__ldcg(A.token_scales + m0 + c) * sw));
+        }
+      }
+    }
+    __syncwarp();
+    cluster_sync();                            // nobody leaves while its sums are read
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// ---- layouts ------------------------------------------------------------------------------------------------------------------------
+
+__global__ void __launch_bounds__(256) i8_pack_kernel(I8PackArgs A) {
+  const int64_t chunks = A.tiles_n * A.kblocks * (kTileBytes / 16);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
+    const int row = (int)(i / 8 % kRows), at = (int)(i % 8);
+    const int64_t kb = i / (kTileBytes / 16) % A.kblocks, n = i / (kTileBytes / 16) / A.kblocks * kRows + row;
+    const int64_t k0 = kb * kBlock + (at ^ (row & 7)) * 16;
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if (n < A.N)
+      for (int e = 0; e < 16; ++e)
+        if (k0 + e < A.K) w[e / 4] |= (uint32_t)(uint8_t)A.q[n * A.ld_q + k0 + e] << (8 * (e & 3));
+    ((uint4*)A.packed)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  float* scales = (float*)((char*)A.packed + A.tiles_n * A.kblocks * kTileBytes);
+  for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < A.tiles_n * kRows; n += (int64_t)gridDim.x * 256) scales[n] = n < A.N ? A.scales[n] : 0.f;
+}
+
+// Quantisation of a token's row: q = 127 x / max |x| rounded to the nearest integer, halves to the even one, as exact arithmetic has it.  x
+// and the maximum have 8 significant bits, so 127 x and (2 q + 1) max / 2 are exact in fp32, and 127 x / max is either a half or at least 1/512 (of numbers up
+// to 254) away from one: the product with a rounded reciprocal (off by 2^-15 at most) picks the right integer, or one of the two of a
+// half, and the remainder of the product tells a half.  max is scaled to 1 .. 2 first, by a power of two, so that nothing overflows or leaves the normal numbers.
+constexpr int kQuantThreads = 256;
+constexpr int kHeld = 4;                       // chunks of 16 a thread keeps between the maximum and the rounding
+
+struct Chunk { uint4 a, b; };                  // 16 bf16
+__device__ __forceinline__ Chunk load_chunk(const I8QuantArgs& A, const char* row, int64_t k0) {
+  Chunk c{make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+  if (A.vectors && k0 + 16 <= A.K) {
+    c.a = ((const uint4*)(row + k0 * 2))[0];
+    c.b = ((const uint4*)(row + k0 * 2))[1];
+  } else if (k0 < A.K) {
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t lo = k0 + 2 * e < A.K ? ((const uint16_t*)row)[k0 + 2 * e] : 0u, hi = k0 + 2 * e + 1 < A.K ? ((const uint16_t*)row)[k0 + 2 * e + 1] : 0u;
+      w[e] = lo | hi << 16;
+    }
+    c.a = make_uint4(w[0], w[1], w[2], w[3]);
+    c.b = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+  return c;
+}
+__device__ __forceinline__ uint32_t word_of(const Chunk& c, int i) {
+  return i == 0 ? c.a.x : i == 1 ? c.a.y : i == 2 ? c.a.z : i == 3 ? c.a.w : i == 4 ? c.b.x : i == 5 ? c.b.y : i == 6 ? c.b.z : c.b.w;
+}
+// The largest magnitude, as the bits of a bf16: ordered like integers, infinity and NaN above all numbers.
+__device__ __forceinline__ uint32_t largest(const Chunk& c, uint32_t m) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = __vmaxu2(m, word_of(c, i) & 0x7fff7fffu);
+  return m;
+}
+__device__ __forceinline__ int quantized(float x, float scale, float m, float inv) {
+  const float xs = x * scale, x127 = xs * 127.f;
+  const float n = rintf(x127 * inv);
+  const float rest = fmaf(-n, m, x127);        // exact wherever it matters
+  int q = (int)n;
+  if (fabsf(rest) * 2.f == m && (q & 1)) q += rest > 0.f ? 1 : -1;
+  return q;
+}
+__device__ __forceinline__ uint4 quantized_chunk(const Chunk& c, float scale, float m, float inv) {
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[i] = 0u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t w = word_of(c, (4 * i + e) / 2);
+      o[i] |= ((uint32_t)quantized(__uint_as_float((e & 1) ? w & 0xffff0000u : w << 16), scale, m, inv) & 0xffu) << (8 * e);
+    }
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+__global__ void __launch_bounds__(kQuantThreads) i8_quantize_kernel(I8QuantArgs A) {
+  __shared__ uint32_t sh[kQuantThreads / 32];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int64_t m = blockIdx.x, chunks = A.kblocks * (kBlock / 16);
+  const char* row = (const char*)A.x + m * A.ld_x * 2;
+  Chunk held[kHeld];
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int64_t c = (int64_t)i * blockDim.x + threadIdx.x;
+    held[i] = load_chunk(A, row, c < chunks ? c * 16 : A.K);
+    top = largest(held[i], top);
+  }
+  for (int64_t c = (int64_t)kHeld * blockDim.x + threadIdx.x; c < chunks; c += blockDim.x) top = largest(load_chunk(A, row, c * 16), top);
+  top = (top & 0xffffu) > top >> 16 ? top & 0xffffu : top >> 16;
+  top = __reduce_max_sync(0xffffffffu, top);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = top;
+  __syncthreads();
+  for (int w = 0; w < (int)blockDim.x / 32; ++w) top = sh[w] > top ? sh[w] : top;
+  const float most = __uint_as_float(top << 16);
+  // a power of two that takes the largest magnitude to 1 .. 2 (subnormal ones come out below 1, still with all of their bits)
+  const uint32_t exponent = top >> 7;
+  const float scale = exponent == 0u ? __uint_as_float(253u << 23) : exponent == 254u ? __uint_as_float(1u << 22) : __uint_as_float((254u - exponent) << 23);
+  const float scaled = most * scale, inv = scaled > 0.f ? 1.f / scaled : 0.f;
+  const bool usable = exponent < 255u;         // else a NaN or an infinity: the token's outputs are NaN
+  char* out = (char*)A.tokens + (m / 8) * 1024 + (m & 7) * 128;
+  auto place = [&](int64_t c) { return (uint4*)(out + c / 8 * (A.padded_m / 8) * 1024 + (((int)(c & 7) ^ (int)(m & 7)) * 16)); };
+  const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int64_t c = (int64_t)i * blockDim.x + threadIdx.x;
+    if (c < chunks) *place(c) = usable ? quantized_chunk(held[i], scale, scaled, inv) : none;
+  }
+  for (int64_t c = (int64_t)kHeld * blockDim.x + threadIdx.x; c < chunks; c += blockDim.x)
+    *place(c) = usable ? quantized_chunk(load_chunk(A, row, c * 16), scale, scaled, inv) : none;
+  if (threadIdx.x == 0)
+    ((float*)((char*)A.tokens + A.padded_m * A.kblocks * kBlock))[m] = usable ? most / 127.f : __uint_as_float(0x7fc00000u);
+}
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// Tokens a tile takes and CTAs that share a tile's K.  A tile of c tokens takes about c + 64 (its instructions, and the copy of its channels
+// beside them); the least rounds over the SMs times that, of the token counts that share M evenly.
+struct Plan { int tokens, split; int64_t tiles_m; };
+Plan plan_for(int64_t M, int64_t N, int64_t kblocks, int sms) {
+  const int64_t tiles_n = (N + kRows - 1) / kRows, least = (M + 255) / 256;
+  Plan p{};
+  double best = 0;
+  for (int64_t tm = least; tm <= least * 3 && tm <= (M + 15) / 16; ++tm) {
+    const int64_t c = up((M + tm - 1) / tm, 16), rounds = (tiles_n * tm + sms - 1) / sms;
+    const double cost = (double)rounds * (double)(c + 64);
+    if (p.tokens == 0 || cost < best) best = cost, p.tokens = (int)c, p.tiles_m = (M + c - 1) / c;
+  }
+  p.split = 1;
+  const int64_t tiles = tiles_n * p.tiles_m;
+  while (p.split < 8 && tiles * p.split * 2 <= sms && kblocks >= p.split * 2) p.split *= 2;
+  return p;
+}
+
+}  // namespace
+
+size_t i8_packed_bytes(int64_t N, int64_t K) {
+  const int64_t tiles = (N + kRows - 1) / kRows;
+  return (size_t)(tiles * ((K + kBlock - 1) / kBlock) * kTileBytes + tiles * kRows * 4);
+}
+size_t i8_token_bytes(int64_t M, int64_t K) { return (size_t)(up(M, 8) * up(K, kBlock) + up(M, 8) * 4); }
+
+cudaError_t launch_i8_pack(I8PackArgs a, cudaStream_t s, int sms) {
+  a.tiles_n = (a.N + kRows - 1) / kRows;
+  a.kblocks = (a.K + kBlock - 1) / kBlock;
+  const int64_t need = (a.tiles_n * a.kblocks * (kTileBytes / 16) + 255) / 256, most = (int64_t)sms * 8;
+  i8_pack_kernel<<<(unsigned)(need < most ? need : most), 256, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_i8_quantize(I8QuantArgs a, cudaStream_t s) {
+  a.padded_m = up(a.M, 8);
+  a.kblocks = (a.K + kBlock - 1) / kBlock;
+  a.vectors = ((uintptr_t)a.x & 15) == 0 && a.ld_x % 8 == 0;
+  const int64_t threads = up(a.kblocks * (kBlock / 16), 32);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)a.M);
+  cfg.blockDim = dim3((unsigned)(threads < kQuantThreads ? threads : kQuantThreads));
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, i8_quantize_kernel, a);
+}
+
+template <bool BF16, bool SPLIT> static cudaError_t launch_linear(const I8Args& a, cudaStream_t s, int sms) {
+  const cudaError_t e = cudaFuncSetAttribute(i8_linear_kernel<BF16, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(SPLIT ? a.tiles * a.split : a.tiles < sms ? a.tiles : sms));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSharedBytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)a.split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = SPLIT ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, i8_linear_kernel<BF16, SPLIT>, a);
+}
+
+cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, int64_t K, bool out_bf16, cudaStream_t s, int sms) {
+  a.kblocks = (K + kBlock - 1) / kBlock;
+  a.padded_m = up(a.M, 8);
+  const Plan p = plan_for(a.M, a.N, a.kblocks, sms);
+  const int64_t tiles_n = (a.N + kRows - 1) / kRows;
+  a.tokens_tile = p.tokens;
+  a.tiles_m = p.tiles_m;
+  a.tiles = tiles_n * p.tiles_m;
+  a.split = p.split;
+  const int fit = kRingBytes / (kTileBytes + p.tokens * kBlock);
+  a.stages = fit < kMaxStages ? fit : kMaxStages;
+  a.weights = (const uint8_t*)packed;
+  a.weight_scales = (const float*)((const char*)packed + tiles_n * a.kblocks * kTileBytes);
+  a.xq = (const uint8_t*)tokens;
+  a.token_scales = (const float*)((const char*)tokens + a.padded_m * a.kblocks * kBlock);
+  if (out_bf16) return p.split > 1 ? launch_linear<true, true>(a, s, sms) : launch_linear<true, false>(a, s, sms);
+  return p.split > 1 ? launch_linear<false, true>(a, s, sms) : launch_linear<false, false>(a, s, sms);
+}
+
+}  // namespace jp

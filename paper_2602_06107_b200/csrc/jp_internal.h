@@ -420,4 +420,38 @@ cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms);
 size_t block_workspace_bytes(int64_t T, int64_t H, int dtype, int sms);
 cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms);
 
+// Linear layers in 8-bit integers (jp_i8.cu).
+struct I8PackArgs {
+  const int8_t* q;         // [N, ld_q]
+  const float* scales;     // [N]
+  void* packed;
+  int64_t N, K, ld_q;
+  int64_t tiles_n, kblocks;    // set by the launch
+};
+struct I8QuantArgs {
+  const void* x;           // [M, ld_x] bf16
+  void* tokens;
+  int64_t M, K, ld_x;
+  int64_t padded_m, kblocks;   // set by the launch
+  bool vectors;            // set by the launch: rows start on 16 bytes
+};
+struct I8Args {
+  void* out;               // [M, ld_out]
+  int32_t* status;         // or null
+  int64_t M, N, ld_out;
+  bool early;              // the kernel in front is the quantisation: weights may be fetched before it is done
+  // set by the launch
+  const uint8_t* weights;
+  const float* weight_scales;  // [N]
+  const uint8_t* xq;
+  const float* token_scales;   // [M]
+  int64_t kblocks, padded_m, tiles, tiles_m;
+  int32_t tokens_tile, stages, split;
+};
+size_t i8_packed_bytes(int64_t N, int64_t K);
+size_t i8_token_bytes(int64_t M, int64_t K);
+cudaError_t launch_i8_pack(I8PackArgs a, cudaStream_t s, int sms);
+cudaError_t launch_i8_quantize(I8QuantArgs a, cudaStream_t s);
+cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, int64_t K, bool out_bf16, cudaStream_t s, int sms);
+
 }  // namespace jp

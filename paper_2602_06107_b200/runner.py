@@ -503,3 +503,78 @@ def block_norm_backward(ctx: B.Context, dy, dsum, x, sum, weight, mean, rstd, *,
                              post_mean if post and not rms else None, post_rstd if post else None, dx, dresidual, out["dweight"],
                              out["dbias"], out["dpost_weight"], out["dpost_bias"], out["dgate"], out["dtoken_gate"], ws)
     return out
+
+
+class I8Weight:
+    """8-bit weights laid out by jp_i8_pack: what jp_i8_linear takes."""
+
+    def __init__(self, packed, N, K):
+        self.packed = packed
+        self.desc = B.jp_i8_desc(N=N, K=K)
+        self.N, self.K = N, K
+
+
+class I8Tokens:
+    """Tokens quantised by jp_i8_quantize, for the layers that read them."""
+
+    def __init__(self, data, M, K):
+        self.data, self.M, self.K = data, M, K
+
+
+def quantize_i8(weight):
+    """Rounds a [N, K] weight to 8 bits, each row by its own largest magnitude: ``(q [N, K] int8, scales [N] fp32)`` for :func:`pack_i8`."""
+    w = weight.float()
+    scales = w.abs().amax(1) / 127.0
+    q = torch.where(scales[:, None] > 0, w / scales[:, None], torch.zeros_like(w)).round().clamp(-127, 127)
+    return q.to(torch.int8), scales
+
+
+def pack_i8(ctx: B.Context, q, scales):
+    """One jp_i8_pack call on torch's current stream: lays ``q`` [N, K] int8 and ``scales`` [N] fp32 out once."""
+    if q.dim() != 2 or q.dtype != torch.int8:
+        raise B.JackpotError("q must be an int8 matrix")
+    N, K = q.shape
+    _dense(scales, (N,), torch.float32, "scales")
+    need = B.jp_i8_packed_bytes(N, K)
+    if need == 0:
+        raise B.JackpotError(f"no layout for N = {N}, K = {K} (1 <= K <= {B.JP_I8_MAX_K})")
+    packed = torch.empty(need, dtype=torch.uint8, device=q.device)
+    B.jp_i8_pack(ctx, B.jp_i8_desc(N=N, K=K, ld_q=_rows(q, "q")), q, scales, packed)
+    return I8Weight(packed, N, K)
+
+
+def _token_buffer(x):
+    if x.dtype != torch.bfloat16:
+        raise B.JackpotError(f"x must be bfloat16, got {x.dtype}")
+    ld_x = _rows(x, "x")
+    M, K = x.shape
+    if K < 1 or K > B.JP_I8_MAX_K:
+        raise B.JackpotError(f"x has {K} columns (1 .. {B.JP_I8_MAX_K})")
+    need = (M + 7) // 8 * 8 * ((K + 127) // 128 * 128 + 4)   # jp_i8_token_bytes, without a call
+    return x.new_empty(need, dtype=torch.uint8) if M else None, ld_x
+
+
+def quantize_tokens_i8(ctx: B.Context, x):
+    """One jp_i8_quantize call on torch's current stream: x [M, K] bf16 in 8 bits with a scale a token, for several :func:`linear_i8`."""
+    data, ld_x = _token_buffer(x)
+    M, K = x.shape
+    B.jp_i8_quantize(ctx, x, ld_x, M, K, data)
+    return I8Tokens(data, M, K)
+
+
+def linear_i8(ctx: B.Context, x, w: I8Weight, *, out_dtype=torch.bfloat16, out=None):
+    """One jp_i8_linear call on torch's current stream: x [M, K] bf16 (or what :func:`quantize_tokens_i8` made of it) times the packed
+    weight: [M, N], contiguous or in ``out``."""
+    if isinstance(x, I8Tokens):
+        M, K, data, src, ld_x = x.M, x.K, x.data, None, 0
+    else:
+        data, ld_x = _token_buffer(x)
+        (M, K), src = x.shape, x
+    if K != w.K:
+        raise B.JackpotError(f"x has {K} columns, the weight {w.K}")
+    if out is None:
+        out = w.packed.new_empty((M, w.N), dtype=out_dtype)
+    elif out.shape != (M, w.N):
+        raise B.JackpotError(f"out must be [{M}, {w.N}]")
+    B.jp_i8_linear(ctx, w.desc, w.packed, src, ld_x, M, data, out, _rows(out, "out"), B._dtype_code(out, "out"))
+    return out
