@@ -7,9 +7,14 @@
 //   dgc = sum_t a gt u gs,  dgt = sum_h a gc u gs,  dw1 = sum_t du xhat1,  db1 = sum_t du,  dw2 = sum_t dy xhat2,  db2 = sum_t dy
 //
 // Bound by HBM: forward reads x and the residual and writes s and y, backward reads dy, ds, s and x and writes dresidual and dx, each
-// once.  A row stays in the registers of one block of threads through all of its sums; the next row is fetched meanwhile.  A thread owns
-// fixed columns, so the sums over rows add up in its registers; blocks leave a line each in the workspace, which a second kernel
-// adds in a fixed order: no atomics, the same bits every time.
+// once.  A row belongs to one group of threads through all of its sums, 8 elements a thread, so that the parameters of a thread's columns
+// stay in registers; the next rows come through asynchronous copies into shared memory meanwhile.  Two rows at a time share their sums'
+// barriers.  The sums over rows add up in registers too, and there are fewer of them than gradients: with Q1 = sum_t gt gs xhat1 and
+// Q0 = sum_t gt gs,  dw1 = a gc Q1,  db1 = a gc Q0,  dgc = a (w1 Q1 + b1 Q0),  and dgt is what dx's sum has anyway.  The groups of a block add
+// theirs in their order, the blocks leave a line each in the workspace, which a second kernel adds in a fixed order: no atomics, the
+// same bits every time.
+// Rows on 16 bytes: each thread copies what it will read itself, no barrier for the data.  Other rows: the group copies the vectors that cover a
+// row and reads elements.
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -17,51 +22,11 @@ namespace jp {
 namespace {
 
 constexpr int kMaxWarps = 32;
+constexpr int kMaxValues = 6;                  // sums that share a barrier
 
 __device__ __forceinline__ float param(const void* p, int64_t i, bool bf16) {
   return bf16 ? __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16) : ((const float*)p)[i];
 }
-
-// W consecutive elements: a 16-byte vector, or one element where rows do not start on 16 bytes.
-template <int DT, int W> struct Item;
-template <int DT> struct Item<DT, Vec<DT>::N> {
-  uint4 v;
-  __device__ __forceinline__ void load(const void* p) {
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
-  }
-  __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
-  __device__ __forceinline__ float get(int e) const { return Vec<DT>::get(v, e); }
-  __device__ __forceinline__ void set(const float* f) {     // rounds
-    if constexpr (DT == JP_BF16) {
-      uint32_t o[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
-        o[e] = *(const uint32_t*)&h;
-      }
-      v = make_uint4(o[0], o[1], o[2], o[3]);
-    } else {
-      v = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-    }
-  }
-  __device__ __forceinline__ void store(void* p) const { stg_stream((uint4*)p, v); }
-};
-template <int DT> struct Item<DT, 1> {
-  uint32_t v;                                               // as fp32
-  __device__ __forceinline__ void load(const void* p) {
-    if constexpr (DT == JP_BF16) v = (uint32_t)(*(const volatile uint16_t*)p) << 16;
-    else v = *(const volatile uint32_t*)p;
-  }
-  __device__ __forceinline__ void zero() { v = 0u; }
-  __device__ __forceinline__ float get(int) const { return __uint_as_float(v); }
-  __device__ __forceinline__ void set(const float* f) {
-    v = DT == JP_BF16 ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(f[0])) << 16 : __float_as_uint(f[0]);
-  }
-  __device__ __forceinline__ void store(void* p) const {
-    if constexpr (DT == JP_BF16) *(uint16_t*)p = (uint16_t)(v >> 16);
-    else *(uint32_t*)p = v;
-  }
-};
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -69,169 +34,357 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// N sums over the block, in all of its threads.  `slot` alternates between uses, so that one barrier each is enough.
-template <int N> __device__ __forceinline__ void block_sums(float (&v)[N], float (*sh)[3][kMaxWarps], int& slot) {
+// Groups are the rows of threadIdx.x; a warp that is a group of its own needs no barrier.  SOLE: the block is one group (barriers by number
+// would reserve all 16 of them, and an SM has 64).
+template <bool SOLE> __device__ __forceinline__ void group_sync() {
+  if (blockDim.x == 32) __syncwarp();
+  else if (SOLE) __syncthreads();
+  else asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.y + 1), "r"(blockDim.x) : "memory");
+}
+
+// N sums over the group, in all of its threads.  `slot` alternates between uses, so that one barrier each is enough.
+template <bool SOLE, int N> __device__ __forceinline__ void group_sums(float (&v)[N], float (*sh)[kMaxValues][kMaxWarps], int& slot) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
   if (blockDim.x == 32) return;
-  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31, first = threadIdx.y * warps;
   float (*part)[kMaxWarps] = sh[slot];
   slot ^= 1;
   if (lane == 0)
 #pragma unroll
-    for (int i = 0; i < N; ++i) part[i][threadIdx.x >> 5] = v[i];
-  __syncthreads();
+    for (int i = 0; i < N; ++i) part[i][first + (threadIdx.x >> 5)] = v[i];
+  group_sync<SOLE>();
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? part[i][lane] : 0.f);
+  for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? part[i][first + lane] : 0.f);
 }
 
-template <int W> __device__ __forceinline__ int64_t column(int i) { return (int64_t)(threadIdx.x + i * (int)blockDim.x) * W; }
-
-// W parameters from column c on (through L1: every row reads them again), 1 or 0 where there are none
-template <int W> __device__ __forceinline__ void params(const void* p, int64_t c, bool bf16, float none, float* f) {
-  if (!p) {
+// What a thread has of a row: NU units.  A unit is a 16-byte vector, or two elements a group's width apart where rows do not start on 16 bytes.
+template <int DT, bool VEC> struct Unit {
+  static constexpr int W = VEC ? Vec<DT>::N : 1;            // consecutive elements
+  static constexpr int E = VEC ? W : 2, P = E / 2;          // elements and pairs of a unit
+  static constexpr int ES = Vec<DT>::ESIZE;
+  __device__ static __forceinline__ int64_t column(int u, int half = 0) {
+    return VEC ? (int64_t)(threadIdx.x + u * (int)blockDim.x) * W : threadIdx.x + (2 * u + half) * (int64_t)blockDim.x;
+  }
+  __device__ static __forceinline__ bool have(int u, int64_t H, int half = 0) { return column(u, half) < H; }
+  // a unit in its type
+  struct Raw { uint32_t w[VEC ? 4 : ES == 2 ? 1 : 2]; };
+  __device__ static __forceinline__ void unpack(const Raw& r, float2 (&f)[P]) {
+    if constexpr (ES == 2) {
 #pragma unroll
-    for (int e = 0; e < W; ++e) f[e] = none;
-  } else if constexpr (W == 1) {
-    f[0] = param(p, c, bf16);
-  } else if (bf16) {
-    if constexpr (W == 8) {
-      const uint4 v = __ldg((const uint4*)((const uint16_t*)p + c));
-#pragma unroll
-      for (int e = 0; e < W; ++e) f[e] = Vec<JP_BF16>::get(v, e);
+      for (int p = 0; p < P; ++p) f[p] = make_float2(__uint_as_float(r.w[p] << 16), __uint_as_float(r.w[p] & 0xffff0000u));
     } else {
-      const uint2 v = __ldg((const uint2*)((const uint16_t*)p + c));
-      f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
-      f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
-    }
-  } else {
 #pragma unroll
-    for (int q = 0; q < W; q += 4) {
-      const float4 v = __ldg((const float4*)((const float*)p + c + q));
-      f[q] = v.x; f[q + 1] = v.y; f[q + 2] = v.z; f[q + 3] = v.w;
+      for (int p = 0; p < P; ++p) f[p] = make_float2(__uint_as_float(r.w[2 * p]), __uint_as_float(r.w[2 * p + 1]));
     }
   }
+  __device__ static __forceinline__ Raw pack(const float2 (&f)[P]) {      // rounds
+    Raw r;
+    if constexpr (ES == 2) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(f[p].x, f[p].y);
+        r.w[p] = *(const uint32_t*)&h;
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < P; ++p) r.w[2 * p] = __float_as_uint(f[p].x), r.w[2 * p + 1] = __float_as_uint(f[p].y);
+    }
+    return r;
+  }
+  __device__ static __forceinline__ void store(void* row, int u, int64_t H, const Raw& r) {
+    if constexpr (VEC) {
+      if (have(u, H)) stg_stream((uint4*)((char*)row + column(u) * ES), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+    } else {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        if (have(u, H, half)) {
+          if constexpr (ES == 2) ((uint16_t*)row)[column(u, half)] = (uint16_t)(r.w[0] >> (16 * half));
+          else ((uint32_t*)row)[column(u, half)] = r.w[half];
+        }
+    }
+  }
+  // parameters at the unit's columns; `none` where there are none, 0 past the end
+  __device__ static __forceinline__ void params(const void* p, int u, int64_t H, bool bf16, float none, float2 (&f)[P]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int64_t c = VEC ? column(u) + e : column(u, e);
+      const float v = c >= H ? 0.f : p ? param(p, c, bf16) : none;
+      if (e & 1) f[e / 2].y = v;
+      else f[e / 2].x = v;
+    }
+  }
+};
+
+// Bytes of a row's place in shared memory: the vectors of all threads, or the vectors that cover a row wherever it starts.
+__host__ __device__ inline int place_bytes(bool vec, int threads, int units, int64_t H, int es) {
+  return vec ? threads * units * 16 : (int)((H * es + 15) / 16 + 1) * 16;
 }
 
-// Mean (0 for RMS norm) and 1 / sqrt(mean of squares + eps) of a row held in registers; squares are taken of x - mu.
-template <int DT, int W, int NV>
-__device__ __forceinline__ void row_stats(const BlockArgs& A, const Item<DT, W> (&x)[NV], float (*sh)[3][kMaxWarps], int& slot, float& mean, float& rstd) {
-  const float inv_h = 1.f / (float)A.H;
-  mean = 0.f;
-  if (!A.rms) {
-    float s[1] = {0.f};
+// The group's rows of NT matrices: row `first`, then every `step`-th, STAGES of them under way.
+template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
+  using Un = Unit<DT, VEC>;
+  static constexpr int ES = Vec<DT>::ESIZE;
+  const char* base[NT];                                     // null: a matrix that there is not, which reads 0
+  int64_t ld[NT], H, T, next, step;
+  char* mem;
+  int place, in, out;
+  __device__ __forceinline__ void fetch() {
+    if (next < T) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int t = 0; t < NT; ++t)
+        if (base[t]) {
+          const char* row = base[t] + next * ld[t];
+          char* to = mem + (in * NT + t) * place;
+          if constexpr (VEC) {
 #pragma unroll
-      for (int e = 0; e < W; ++e) s[0] += x[i].get(e);      // (0 past the end)
-    block_sums<1>(s, sh, slot);
-    mean = s[0] * inv_h;
+            for (int u = 0; u < NU; ++u)
+              if (Un::have(u, H))
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + (u * (int)blockDim.x + threadIdx.x) * 16)),
+                             "l"(row + Un::column(u) * ES) : "memory");
+          } else {                                          // vectors that reach beyond the matrix, in its first and last row, element by element
+            const char* const end = row + H * ES;
+            const char* const last = base[t] + (T - 1) * ld[t] + H * ES;
+            const int head = (int)((uintptr_t)row & 15);
+            for (int i = threadIdx.x * 16; i < head + (int)(H * ES); i += blockDim.x * 16) {
+              const char* from = row - head + i;
+              if (from >= base[t] && from + 16 <= last) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + i)), "l"(from) : "memory");
+              } else {
+                for (int q = 0; q < 16; q += ES)
+                  if (from + q >= row && from + q < end) {
+                    if constexpr (ES == 2) *(uint16_t*)(to + i + q) = *(const volatile uint16_t*)(from + q);
+                    else *(uint32_t*)(to + i + q) = *(const volatile uint32_t*)(from + q);
+                  }
+              }
+            }
+          }
+        }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    next += step;
+    in = in == STAGES - 1 ? 0 : in + 1;
   }
-  float q[1] = {0.f};
+  __device__ __forceinline__ void start(const void* const (&b)[NT], const int64_t (&l)[NT], int64_t first, int64_t step_, int64_t T_, int64_t H_, char* mem_, int place_) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (column<W>(i) < A.H) {
+    for (int t = 0; t < NT; ++t) base[t] = (const char*)b[t], ld[t] = l[t] * ES;
+    H = H_; T = T_; next = first; step = step_; mem = mem_; place = place_;
+    in = out = 0;
+#pragma unroll 1
+    for (int s = 0; s < STAGES; ++s) fetch();
+  }
+  template <int R> __device__ __forceinline__ void wait() {   // for the oldest R rows
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - R) : "memory");
+    if (!VEC) group_sync<SOLE>();
+  }
+  // unit u of matrix t of the r-th oldest row, which is `row`
+  __device__ __forceinline__ void get(int t, int u, int r_, int64_t row, float2 (&f)[Un::P]) const {
+    const int place_of = out + r_ >= STAGES ? out + r_ - STAGES : out + r_;
+    typename Un::Raw r;
 #pragma unroll
-      for (int e = 0; e < W; ++e) {
-        const float d = x[i].get(e) - mean;
-        q[0] = fmaf(d, d, q[0]);
+    for (int i = 0; i < (int)(sizeof(r) / 4); ++i) r.w[i] = 0u;
+    if (base[t]) {
+      const char* from = mem + (place_of * NT + t) * place;
+      if constexpr (VEC) {
+        if (Un::have(u, H)) {
+          const uint4 v = *(const uint4*)(from + (u * (int)blockDim.x + threadIdx.x) * 16);
+          r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+        }
+      } else {
+        from += (uintptr_t)(base[t] + row * ld[t]) & 15;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          if (Un::have(u, H, half)) {
+            if constexpr (ES == 2) r.w[0] |= (uint32_t)((const uint16_t*)from)[Un::column(u, half)] << (16 * half);
+            else r.w[half] = ((const uint32_t*)from)[Un::column(u, half)];
+          }
       }
     }
-  block_sums<1>(q, sh, slot);
-  rstd = 1.f / sqrtf(q[0] * inv_h + A.eps);
+    Un::unpack(r, f);
+  }
+  template <int R> __device__ __forceinline__ void done() {   // the oldest R rows' places are free
+    if (!VEC) group_sync<SOLE>();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      out = out == STAGES - 1 ? 0 : out + 1;
+      fetch();
+    }
+  }
+};
+
+// x - mu where there is a column, 0 past the end (a pair's columns lie apart without vectors)
+template <int DT, bool VEC> __device__ __forceinline__ float2 centred(float2 x, float mu, int u, int64_t H) {
+  const float2 d = add2(x, make_float2(-mu, -mu));
+  if (VEC) return Unit<DT, VEC>::have(u, H) ? d : make_float2(0.f, 0.f);
+  return make_float2(Unit<DT, VEC>::have(u, H, 0) ? d.x : 0.f, Unit<DT, VEC>::have(u, H, 1) ? d.y : 0.f);
 }
 
-template <int DT, int W, int NV>
-__global__ void __launch_bounds__(1024) block_fwd_kernel(BlockArgs A) {
-  constexpr int ES = Vec<DT>::ESIZE;
-  using It = Item<DT, W>;
-  __shared__ float sh[2][3][kMaxWarps];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+// Mean (0 for RMS norm) and 1 / sqrt(mean of squares + eps) of R rows; squares are taken of x - mu.  get(r, u, f): unit u of row r.
+template <int DT, bool VEC, int NU, int R, bool FULL, class Get>
+__device__ __forceinline__ void row_stats(const BlockArgs& A, Get get, float (*sh)[kMaxValues][kMaxWarps], int& slot, float (&mean)[R], float (&rstd)[R]) {
+  using Un = Unit<DT, VEC>;
+  const float inv_h = 1.f / (float)A.H;
+  const bool center = FULL && !A.rms;
+  float v[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) mean[r] = 0.f;
+  if (center) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        float2 x[Un::P];
+        get(r, u, x);                                       // (0 past the end)
+#pragma unroll
+        for (int p = 0; p < Un::P; ++p) t = add2(t, x[p]);
+      }
+      v[r] = t.x + t.y;
+    }
+    group_sums<true, R>(v, sh, slot);
+#pragma unroll
+    for (int r = 0; r < R; ++r) mean[r] = v[r] * inv_h;
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      float2 x[Un::P];
+      get(r, u, x);
+#pragma unroll
+      for (int p = 0; p < Un::P; ++p) {
+        if (center) x[p] = centred<DT, VEC>(x[p], mean[r], u, A.H);
+        t = fma2(x[p], x[p], t);
+      }
+    }
+    v[r] = t.x + t.y;
+  }
+  group_sums<true, R>(v, sh, slot);
+#pragma unroll
+  for (int r = 0; r < R; ++r) rstd[r] = 1.f / sqrtf(v[r] * inv_h + A.eps);
+}
+
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// R rows at a time.  FULL: layer norm, biases, a gate a token; without it those instructions and registers are left out.
+template <int DT, bool VEC, int NU, int R, int STAGES, bool FULL, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) block_fwd_kernel(BlockArgs A, int place) {
+  using Un = Unit<DT, VEC>;
+  constexpr int ES = Vec<DT>::ESIZE, P = Un::P;
+  extern __shared__ uint4 places[];
+  __shared__ float sh[2][kMaxValues][kMaxWarps];
+  asm volatile("griddepcontrol.wait;" ::: "memory");        // launched as a programmatic dependent of whatever is before it
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int slot = 0;
-  It nx[NV], nr[NV];
-  auto fetch = [&](int64_t row) {
+  const int64_t step = gridDim.x;
+  const bool center = FULL && !A.rms, post = A.post_weight != nullptr;
+  Ring<DT, VEC, NU, 2, STAGES, true> in;
+  in.start({A.x, A.residual}, {A.ld_x, A.ld_residual}, blockIdx.x, step, A.T, A.H, (char*)places, place);
+  // s = residual + gt (xhat1 fw + fb),  y = xhat2 w2 + b2
+  float2 fw[NU][P], fb[FULL ? NU : 1][P], w2[NU][P], b2[FULL ? NU : 1][P];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      nx[i].zero();
-      nr[i].zero();
-      if (row < A.T && c < A.H) {
-        nx[i].load((const char*)A.x + (row * A.ld_x + c) * ES);
-        nr[i].load((const char*)A.residual + (row * A.ld_residual + c) * ES);
+  for (int u = 0; u < NU; ++u) {
+    float2 g[P];
+    Un::params(A.post_weight, u, A.H, A.param_bf16, 1.f, fw[u]);
+    Un::params(A.gate, u, A.H, A.param_bf16, 1.f, g);
+    Un::params(A.weight, u, A.H, A.param_bf16, 1.f, w2[u]);
+#pragma unroll
+    for (int p = 0; p < P; ++p) g[p] = mul2(g[p], both(A.scale));
+    if (FULL) {
+      Un::params(A.post_bias, u, A.H, A.param_bf16, 0.f, fb[u]);
+      Un::params(A.bias, u, A.H, A.param_bf16, 0.f, b2[u]);
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      fw[u][p] = mul2(fw[u][p], g[p]);
+      if (FULL) fb[u][p] = mul2(fb[u][p], g[p]);
+    }
+  }
+  for (int64_t row = blockIdx.x; row < A.T; row += R * step) {
+    float m1[R], r1[R], m2[R], r2[R];
+    in.template wait<R>();
+    if (post) {
+      row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { in.get(0, u, r, row + r * step, f); }, sh, slot, m1, r1);
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r) m1[r] = 0.f, r1[r] = 1.f;
+    }
+    typename Un::Raw s[R][NU];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t t = row + r * step;
+      if (r > 0 && t >= A.T) break;
+      const float gt = FULL && A.token_gate ? A.token_gate[t] : 1.f;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        float2 x[P], o[P];
+        in.get(0, u, r, t, x);
+        in.get(1, u, r, t, o);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          if (center) x[p] = add2(x[p], both(-m1[r]));
+          x[p] = mul2(x[p], both(r1[r]));
+          o[p] = FULL ? fma2(fma2(x[p], fw[u][p], fb[u][p]), both(gt), o[p]) : fma2(x[p], fw[u][p], o[p]);
+        }
+        s[r][u] = Un::pack(o);
+        Un::store((char*)A.sum + t * A.ld_sum * ES, u, A.H, s[r][u]);
+      }
+      if (threadIdx.x == 0 && post) {
+        if (A.out_post_mean) A.out_post_mean[t] = m1[r];
+        if (A.out_post_rstd) A.out_post_rstd[t] = r1[r];
       }
     }
-  };
-  fetch(blockIdx.x);
-  for (int64_t row = blockIdx.x; row < A.T; row += gridDim.x) {
-    It x[NV], s[NV];
+    in.template done<R>();
+    row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { Un::unpack(s[r][u], f); }, sh, slot, m2, r2);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      x[i] = nx[i];
-      s[i] = nr[i];
-    }
-    fetch(row + gridDim.x);
-    float scale = A.scale;
-    if (A.token_gate) scale *= A.token_gate[row];
-    float m1 = 0.f, r1 = 1.f, m2, r2;
-    if (A.post_weight) {
-      row_stats<DT, W, NV>(A, x, sh, slot, m1, r1);
+    for (int r = 0; r < R; ++r) {
+      const int64_t t = row + r * step;
+      if (r > 0 && t >= A.T) break;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        float2 x[P];
+        Un::unpack(s[r][u], x);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          if (center) x[p] = add2(x[p], both(-m2[r]));
+          x[p] = mul2(x[p], both(r2[r]));
+          x[p] = FULL ? fma2(x[p], w2[u][p], b2[u][p]) : mul2(x[p], w2[u][p]);
+        }
+        Un::store((char*)A.y + t * A.ld_y * ES, u, A.H, Un::pack(x));
+      }
       if (threadIdx.x == 0) {
-        if (A.out_post_mean) A.out_post_mean[row] = m1;
-        if (A.out_post_rstd) A.out_post_rstd[row] = r1;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      if (c < A.H) {
-        float w[W], b[W], g[W], o[W];
-        params<W>(A.post_weight, c, A.param_bf16, 1.f, w);
-        params<W>(A.post_bias, c, A.param_bf16, 0.f, b);
-        params<W>(A.gate, c, A.param_bf16, 1.f, g);
-#pragma unroll
-        for (int e = 0; e < W; ++e) o[e] = fmaf(fmaf((x[i].get(e) - m1) * r1, w[e], b[e]), scale * g[e], s[i].get(e));
-        s[i].set(o);
-        s[i].store((char*)A.sum + (row * A.ld_sum + c) * ES);
-      }
-    }
-    row_stats<DT, W, NV>(A, s, sh, slot, m2, r2);
-    if (threadIdx.x == 0) {
-      if (A.out_mean) A.out_mean[row] = m2;
-      if (A.out_rstd) A.out_rstd[row] = r2;
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      if (c < A.H) {
-        float w[W], b[W], o[W];
-        params<W>(A.weight, c, A.param_bf16, 1.f, w);
-        params<W>(A.bias, c, A.param_bf16, 0.f, b);
-#pragma unroll
-        for (int e = 0; e < W; ++e) o[e] = fmaf((s[i].get(e) - m2) * r2, w[e], b[e]);
-        It y;
-        y.set(o);
-        y.store((char*)A.y + (row * A.ld_y + c) * ES);
+        if (A.out_mean) A.out_mean[t] = m2[r];
+        if (A.out_rstd) A.out_rstd[t] = r2[r];
       }
     }
   }
 }
+
+// One element, for rows of any width.
+template <int DT> __device__ __forceinline__ float element(const void* p, int64_t i) {
+  if constexpr (DT == JP_BF16) return __uint_as_float((uint32_t)((const volatile uint16_t*)p)[i] << 16);
+  else return ((const volatile float*)p)[i];
+}
+template <int DT> __device__ __forceinline__ void put(void* p, int64_t i, float v) {
+  if constexpr (DT == JP_BF16) ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(v);
+  else ((float*)p)[i] = v;
+}
+__device__ __forceinline__ float param_or(const void* p, int64_t i, bool bf16, float none) { return p ? param(p, i, bf16) : none; }
 
 // Any width: the rows are read again for each of their sums (from L2).
 template <int DT>
 __global__ void __launch_bounds__(1024) block_fwd_wide_kernel(BlockArgs A) {
-  constexpr int ES = Vec<DT>::ESIZE;
-  using It = Item<DT, 1>;
-  __shared__ float sh[2][3][kMaxWarps];
+  __shared__ float sh[2][kMaxValues][kMaxWarps];
   int slot = 0;
   const float inv_h = 1.f / (float)A.H;
-  auto at = [&](const void* p, int64_t i) { It t; t.load((const char*)p + i * ES); return t.get(0); };
+  auto at = [](const void* p, int64_t i) { return element<DT>(p, i); };
   auto stats = [&](const void* p, int64_t first, float& mean, float& rstd) {
     mean = 0.f;
     if (!A.rms) {
       float s[1] = {0.f};
       for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x) s[0] += at(p, first + c);
-      block_sums<1>(s, sh, slot);
+      group_sums<true, 1>(s, sh, slot);
       mean = s[0] * inv_h;
     }
     float q[1] = {0.f};
@@ -239,7 +392,7 @@ __global__ void __launch_bounds__(1024) block_fwd_wide_kernel(BlockArgs A) {
       const float d = at(p, first + c) - mean;
       q[0] = fmaf(d, d, q[0]);
     }
-    block_sums<1>(q, sh, slot);
+    group_sums<true, 1>(q, sh, slot);
     rstd = 1.f / sqrtf(q[0] * inv_h + A.eps);
   };
   for (int64_t row = blockIdx.x; row < A.T; row += gridDim.x) {
@@ -254,13 +407,11 @@ __global__ void __launch_bounds__(1024) block_fwd_wide_kernel(BlockArgs A) {
     }
     for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x) {
       float w, b, g;
-      params<1>(A.post_weight, c, A.param_bf16, 1.f, &w);
-      params<1>(A.post_bias, c, A.param_bf16, 0.f, &b);
-      params<1>(A.gate, c, A.param_bf16, 1.f, &g);
+      w = param_or(A.post_weight, c, A.param_bf16, 1.f);
+      b = param_or(A.post_bias, c, A.param_bf16, 0.f);
+      g = param_or(A.gate, c, A.param_bf16, 1.f);
       const float o = fmaf(fmaf((at(A.x, row * A.ld_x + c) - m1) * r1, w, b), scale * g, at(A.residual, row * A.ld_residual + c));
-      It s;
-      s.set(&o);
-      s.store((char*)A.sum + (row * A.ld_sum + c) * ES);
+      put<DT>(A.sum, row * A.ld_sum + c, o);
     }
     stats(A.sum, row * A.ld_sum, m2, r2);                   // (each thread reads what it wrote itself)
     if (threadIdx.x == 0) {
@@ -269,174 +420,210 @@ __global__ void __launch_bounds__(1024) block_fwd_wide_kernel(BlockArgs A) {
     }
     for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x) {
       float w, b;
-      params<1>(A.weight, c, A.param_bf16, 1.f, &w);
-      params<1>(A.bias, c, A.param_bf16, 0.f, &b);
+      w = param_or(A.weight, c, A.param_bf16, 1.f);
+      b = param_or(A.bias, c, A.param_bf16, 0.f);
       const float o = fmaf((at(A.sum, row * A.ld_sum + c) - m2) * r2, w, b);
-      It y;
-      y.set(&o);
-      y.store((char*)A.y + (row * A.ld_y + c) * ES);
+      put<DT>(A.y, row * A.ld_y + c, o);
     }
   }
 }
 
-// Sums over rows: dw2, then db2 (BIAS), dw1 (POST), db1 (POST and BIAS), dgate (GATE), each a line of H.
-__host__ __device__ constexpr int n_sums(bool post, bool gate, bool bias) { return 1 + bias + post + (post && bias) + gate; }
-constexpr int kMaxSums = 5;
+// Lines of sums over rows: dw2, Q1 and, with FULL, db2 and Q0.
+constexpr int kMaxSums = 4;
 
-template <int DT, int W, int NV, bool POST, bool GATE, bool BIAS>
-__global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A) {
-  constexpr int ES = Vec<DT>::ESIZE, N = n_sums(POST, GATE, BIAS);
-  constexpr int B2 = 1, W1 = 1 + BIAS, B1 = W1 + 1, G = W1 + POST + (POST && BIAS);
-  using It = Item<DT, W>;
-  __shared__ float sh[2][3][kMaxWarps];
+template <int DT, bool VEC, int NU, int R, int STAGES, bool POST, bool FULL>
+__global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) {
+  using Un = Unit<DT, VEC>;
+  constexpr int ES = Vec<DT>::ESIZE, P = Un::P, N = FULL ? 4 : 2, V1 = FULL ? 2 * R : R, V2 = FULL ? 3 * R : R;
+  static_assert(V2 <= kMaxValues, "");
+  extern __shared__ uint4 places[];
+  __shared__ float sh[2][kMaxValues][kMaxWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   int slot = 0;
   const float inv_h = 1.f / (float)A.H;
-  const bool use_x = POST || GATE || A.token_gate;
-  float acc[N][NV][W];
+  const bool token = FULL && A.token_gate != nullptr, center = FULL && !A.rms, use_x = POST || A.gate || token;
+  float2 acc[N][NU][P];
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int e = 0; e < W; ++e) acc[n][i][e] = 0.f;
-  It ndy[NV], nds[NV], ns[NV], nx[NV];
-  auto fetch = [&](int64_t row) {
+      for (int p = 0; p < P; ++p) acc[n][u][p] = both(0.f);
+  const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
+  Ring<DT, VEC, NU, 4, STAGES, false> in;
+  in.start({A.dy, A.sum, A.dsum, use_x ? A.x : nullptr}, {A.ld_dy, A.ld_sum, A.ld_dsum, A.ld_x}, first, step, A.T, A.H,
+           (char*)places + threadIdx.y * STAGES * 4 * place, place);
+  float2 w2[NU][P], fw[NU][P], fb[FULL ? NU : 1][P];        // fw = a gc w1, fb = a gc b1
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      ndy[i].zero(); nds[i].zero(); ns[i].zero(); nx[i].zero();
-      if (row < A.T && c < A.H) {
-        ndy[i].load((const char*)A.dy + (row * A.ld_dy + c) * ES);
-        if (A.dsum) nds[i].load((const char*)A.dsum + (row * A.ld_dsum + c) * ES);
-        ns[i].load((const char*)A.sum + (row * A.ld_sum + c) * ES);
-        if (use_x) nx[i].load((const char*)A.x + (row * A.ld_x + c) * ES);
-      }
-    }
-  };
-  fetch(blockIdx.x);
-  for (int64_t row = blockIdx.x; row < A.T; row += gridDim.x) {
-    It dy[NV], ds[NV], s[NV], x[NV];
+  for (int u = 0; u < NU; ++u) {
+    float2 g[P];
+    Un::params(A.weight, u, A.H, A.param_bf16, 1.f, w2[u]);
+    Un::params(POST ? A.post_weight : nullptr, u, A.H, A.param_bf16, 1.f, fw[u]);
+    Un::params(A.gate, u, A.H, A.param_bf16, 1.f, g);
+    if (FULL) Un::params(A.post_bias, u, A.H, A.param_bf16, 0.f, fb[u]);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      dy[i] = ndy[i]; ds[i] = nds[i]; s[i] = ns[i]; x[i] = nx[i];
-    }
-    const float m2 = A.rms ? 0.f : A.mean[row], r2 = A.rstd[row];
-    const float m1 = POST && !A.rms ? A.post_mean[row] : 0.f, r1 = POST ? A.post_rstd[row] : 1.f;
-    const float gt = A.token_gate ? A.token_gate[row] : 1.f;
-    fetch(row + gridDim.x);
-    float v[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      if (c < A.H) {
-        float w[W];
-        params<W>(A.weight, c, A.param_bf16, 1.f, w);
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-          const float d = dy[i].get(e), xh = (s[i].get(e) - m2) * r2, g = d * w[e];
-          v[0] += g;
-          v[1] = fmaf(g, xh, v[1]);
-          acc[0][i][e] = fmaf(d, xh, acc[0][i][e]);
-          if (BIAS) acc[B2][i][e] += d;
-        }
-      }
-    }
-    block_sums<3>(v, sh, slot);
-    const float a1 = A.rms ? 0.f : v[0] * inv_h, a2 = v[1] * inv_h;
-    float gs[NV][W], t[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      if (c < A.H) {
-        float w2[W], w1[W], b1[W], gc[W];
-        params<W>(A.weight, c, A.param_bf16, 1.f, w2);
-        params<W>(POST ? A.post_weight : nullptr, c, A.param_bf16, 1.f, w1);
-        params<W>(POST ? A.post_bias : nullptr, c, A.param_bf16, 0.f, b1);
-        params<W>(GATE ? A.gate : nullptr, c, A.param_bf16, 1.f, gc);
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-          const float xh2 = (s[i].get(e) - m2) * r2;
-          const float g = fmaf(r2, fmaf(-xh2, a2, fmaf(dy[i].get(e), w2[e], -a1)), ds[i].get(e));
-          const float xh1 = (x[i].get(e) - m1) * r1, u = POST ? fmaf(xh1, w1[e], b1[e]) : x[i].get(e);
-          const float gu = A.scale * g * u, du = A.scale * gt * gc[e] * g;
-          gs[i][e] = g;
-          if (GATE) acc[G][i][e] = fmaf(gt, gu, acc[G][i][e]);
-          t[2] = fmaf(gc[e], gu, t[2]);
-          if (POST) {
-            const float g1 = du * w1[e];
-            t[0] += g1;
-            t[1] = fmaf(g1, xh1, t[1]);
-            acc[W1][i][e] = fmaf(du, xh1, acc[W1][i][e]);
-            if (BIAS) acc[B1][i][e] += du;
-          }
-        }
-        It o;
-        o.set(gs[i]);
-        o.store((char*)A.dresidual + (row * A.ld_dresidual + c) * ES);
-      }
-    }
-    if (POST || A.token_gate) block_sums<3>(t, sh, slot);
-    if (A.token_gate && threadIdx.x == 0) A.dtoken_gate[row] = t[2];
-    const float c1 = A.rms ? 0.f : t[0] * inv_h, c2 = t[1] * inv_h;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = column<W>(i);
-      if (c < A.H) {
-        float w1[W], gc[W], o[W];
-        params<W>(POST ? A.post_weight : nullptr, c, A.param_bf16, 1.f, w1);
-        params<W>(GATE ? A.gate : nullptr, c, A.param_bf16, 1.f, gc);
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-          const float du = A.scale * gt * gc[e] * gs[i][e];
-          o[e] = POST ? r1 * fmaf(-(x[i].get(e) - m1) * r1, c2, fmaf(du, w1[e], -c1)) : du;
-        }
-        It d;
-        d.set(o);
-        d.store((char*)A.dx + (row * A.ld_dx + c) * ES);
-      }
+    for (int p = 0; p < P; ++p) {
+      g[p] = mul2(g[p], both(A.scale));
+      fw[u][p] = mul2(fw[u][p], g[p]);
+      if (FULL) fb[u][p] = mul2(fb[u][p], g[p]);
     }
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the kernel that adds the lines may set up
-  float* line = A.partial + (int64_t)blockIdx.x * N * A.H;
+  for (int64_t row = first; row < A.T; row += R * step) {
+    float m1[R], r1[R], m2[R], r2[R], gt[R], v[V1], t[V2];
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+    for (int r = 0; r < R; ++r) {
+      const int64_t at = row + r * step;
+      const bool have = r == 0 || at < A.T;                 // (a row behind the last one reads 0 throughout)
+      m2[r] = center && have ? A.mean[at] : 0.f;
+      r2[r] = have ? A.rstd[at] : 0.f;
+      m1[r] = POST && center && have ? A.post_mean[at] : 0.f;
+      r1[r] = !POST ? 1.f : have ? A.post_rstd[at] : 0.f;
+      gt[r] = token && have ? A.token_gate[at] : have ? 1.f : 0.f;
+    }
+    in.template wait<R>();
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (column<W>(i) < A.H) {
+    for (int r = 0; r < R; ++r) {
+      float2 v1 = both(0.f), v2 = v1;
+      if (r == 0 || row + r * step < A.T) {
 #pragma unroll
-        for (int e = 0; e < W; ++e) line[n * A.H + column<W>(i) + e] = acc[n][i][e];
+        for (int u = 0; u < NU; ++u) {
+          float2 d[P], s[P];
+          in.get(0, u, r, row + r * step, d);
+          in.get(1, u, r, row + r * step, s);
+#pragma unroll
+          for (int p = 0; p < P; ++p) {
+            if (center) s[p] = add2(s[p], both(-m2[r]));
+            const float2 xh = mul2(s[p], both(r2[r])), g = mul2(d[p], w2[u][p]);
+            if (center) v1 = add2(v1, g);
+            v2 = fma2(g, xh, v2);
+            acc[0][u][p] = fma2(d[p], xh, acc[0][u][p]);
+            if (FULL) acc[2][u][p] = add2(acc[2][u][p], d[p]);
+          }
+        }
       }
+      v[r] = v2.x + v2.y;
+      if (FULL) v[R + r] = v1.x + v1.y;
+    }
+    group_sums<false, V1>(v, sh, slot);
+    // gs = r2 (dy w2 - a1 - xhat2 a2) + ds, kept; x is read once more behind its sums
+    float2 gs[R][NU][P];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t at = row + r * step;
+      const float a1 = center ? v[V1 - R + r] * inv_h : 0.f, k2 = -r2[r] * (r2[r] * (v[r] * inv_h));      // (r r alone may leave fp32)
+      float2 t0 = both(0.f), t1 = t0, tb = t0;
+      if (r == 0 || at < A.T) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          float2 d[P], s[P], e[P], x[P];
+          in.get(0, u, r, at, d);
+          in.get(1, u, r, at, s);
+          in.get(2, u, r, at, e);
+          in.get(3, u, r, at, x);
+#pragma unroll
+          for (int p = 0; p < P; ++p) {
+            if (center) s[p] = add2(s[p], both(-m2[r]));
+            float2 g = mul2(d[p], w2[u][p]);
+            if (center) g = add2(g, both(-a1));
+            g = fma2(g, both(r2[r]), fma2(s[p], both(k2), e[p]));
+            gs[r][u][p] = g;
+            if (center) x[p] = add2(x[p], both(-m1[r]));
+            const float2 xh = POST ? mul2(x[p], both(r1[r])) : x[p], g1 = mul2(g, fw[u][p]), gg = FULL ? mul2(g, both(gt[r])) : g;
+            t1 = fma2(g1, xh, t1);
+            acc[1][u][p] = fma2(gg, xh, acc[1][u][p]);
+            if (FULL) {
+              t0 = add2(t0, g1);
+              tb = fma2(g, fb[u][p], tb);
+              acc[3][u][p] = add2(acc[3][u][p], gg);
+            }
+          }
+          Un::store((char*)A.dresidual + at * A.ld_dresidual * ES, u, A.H, Un::pack(gs[r][u]));
+        }
+      }
+      t[r] = t1.x + t1.y;
+      if (FULL) {
+        t[R + r] = t0.x + t0.y;
+        t[2 * R + r] = tb.x + tb.y;
+      }
+    }
+    if (POST || token) group_sums<false, V2>(t, sh, slot);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t at = row + r * step;
+      if (r > 0 && at >= A.T) break;
+      if (token && threadIdx.x == 0) A.dtoken_gate[at] = t[r] + t[V2 - R + r];
+      // dx = r1 (gt g1 - c1 - xhat1 c2)
+      const float c0 = center ? -r1[r] * (gt[r] * (t[V2 > R ? R + r : r] * inv_h)) : 0.f, c2 = -r1[r] * (r1[r] * (gt[r] * (t[r] * inv_h))), rg = r1[r] * gt[r];
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        float2 o[P], x[P];
+        if (POST) in.get(3, u, r, at, x);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          o[p] = mul2(gs[r][u][p], fw[u][p]);
+          if (POST) {
+            if (center) x[p] = add2(x[p], both(-m1[r]));
+            o[p] = fma2(o[p], both(rg), fma2(x[p], both(c2), both(c0)));
+          } else if (FULL) {
+            o[p] = mul2(o[p], both(gt[r]));
+          }
+        }
+        Un::store((char*)A.dx + at * A.ld_dx * ES, u, A.H, Un::pack(o));
+      }
+    }
+    in.template done<R>();
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the kernel that adds the lines may set up
+  // the block's groups one after the other, in shared memory; the last one writes the block's line
+  float* const all = (float*)places;                        // [N][H]
+  for (int g = 0; g < (int)blockDim.y; ++g) {
+    __syncthreads();
+    if ((int)threadIdx.y == g) {
+      float* to = g + 1 == (int)blockDim.y ? A.partial + (int64_t)blockIdx.x * N * A.H : all;
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const int64_t c = VEC ? Un::column(u) + 2 * p + half : Un::column(u, half);
+              if (c < A.H) {
+                float sum = half ? acc[n][u][p].y : acc[n][u][p].x;
+                if (g > 0) sum += all[n * A.H + c];
+                to[n * A.H + c] = sum;
+              }
+            }
+    }
+  }
 }
 
 // Any width: rows are read again for each sum, and the sums over rows stay in the block's line of the workspace (each thread its columns).
 template <int DT>
-__global__ void __launch_bounds__(1024) block_bwd_wide_kernel(BlockArgs A, int n_lines) {
-  constexpr int ES = Vec<DT>::ESIZE;
-  using It = Item<DT, 1>;
-  __shared__ float sh[2][3][kMaxWarps];
+__global__ void __launch_bounds__(1024) block_bwd_wide_kernel(BlockArgs A) {
+  __shared__ float sh[2][kMaxValues][kMaxWarps];
   int slot = 0;
   const float inv_h = 1.f / (float)A.H;
-  const bool post = A.post_weight != nullptr, use_x = post || A.gate || A.token_gate, bias = A.with_bias;
-  float* line = A.partial + (int64_t)blockIdx.x * n_lines * A.H;
-  float* const l_w2 = line, * const l_b2 = line + A.H, * const l_w1 = line + (1 + bias) * A.H, * const l_b1 = l_w1 + A.H,
-       * const l_g = line + (1 + bias + post + (post && bias)) * A.H;
+  const bool post = A.post_weight != nullptr, use_x = post || A.gate || A.token_gate;
+  float* const line = A.partial + (int64_t)blockIdx.x * kMaxSums * A.H;
   for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x)
-    for (int n = 0; n < n_lines; ++n) line[n * A.H + c] = 0.f;
-  auto at = [&](const void* p, int64_t i) { It t; t.load((const char*)p + i * ES); return t.get(0); };
+    for (int n = 0; n < kMaxSums; ++n) line[n * A.H + c] = 0.f;
+  auto at = [](const void* p, int64_t i) { return element<DT>(p, i); };
   for (int64_t row = blockIdx.x; row < A.T; row += gridDim.x) {
     const float m2 = A.rms ? 0.f : A.mean[row], r2 = A.rstd[row];
     const float m1 = post && !A.rms ? A.post_mean[row] : 0.f, r1 = post ? A.post_rstd[row] : 1.f;
     const float gt = A.token_gate ? A.token_gate[row] : 1.f;
-    float v[3] = {0.f, 0.f, 0.f}, t[3] = {0.f, 0.f, 0.f};
+    float v[2] = {0.f, 0.f}, t[3] = {0.f, 0.f, 0.f};
     for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x) {
       const float d = at(A.dy, row * A.ld_dy + c), xh = (at(A.sum, row * A.ld_sum + c) - m2) * r2, g = d * param(A.weight, c, A.param_bf16);
       v[0] += g;
       v[1] = fmaf(g, xh, v[1]);
-      l_w2[c] = fmaf(d, xh, l_w2[c]);
-      if (bias) l_b2[c] += d;
+      line[c] = fmaf(d, xh, line[c]);
+      line[2 * A.H + c] += d;
     }
-    block_sums<3>(v, sh, slot);
+    group_sums<true, 2>(v, sh, slot);
     const float a1 = A.rms ? 0.f : v[0] * inv_h, a2 = v[1] * inv_h;
     // gs of a column; dresidual and dx may lie where dy, dsum, x or sum do, so both are written in the last pass only
     auto gs_at = [&](int64_t c) {
@@ -444,69 +631,71 @@ __global__ void __launch_bounds__(1024) block_bwd_wide_kernel(BlockArgs A, int n
       return fmaf(r2, fmaf(-xh, a2, fmaf(at(A.dy, row * A.ld_dy + c), param(A.weight, c, A.param_bf16), -a1)),
                   A.dsum ? at(A.dsum, row * A.ld_dsum + c) : 0.f);
     };
+    auto factor = [&](int64_t c) { return A.scale * param_or(A.gate, c, A.param_bf16, 1.f); };
     if (use_x) {
       for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x) {
-        const float g = gs_at(c), xv = at(A.x, row * A.ld_x + c), xh1 = (xv - m1) * r1;
-        float w1, b1, gc;
-        params<1>(A.post_weight, c, A.param_bf16, 1.f, &w1);
-        params<1>(A.post_bias, c, A.param_bf16, 0.f, &b1);
-        params<1>(A.gate, c, A.param_bf16, 1.f, &gc);
-        const float u = post ? fmaf(xh1, w1, b1) : xv, gu = A.scale * g * u, du = A.scale * gt * gc * g;
-        if (A.gate) l_g[c] = fmaf(gt, gu, l_g[c]);
-        t[2] = fmaf(gc, gu, t[2]);
-        if (post) {
-          t[0] += du * w1;
-          t[1] = fmaf(du * w1, xh1, t[1]);
-          l_w1[c] = fmaf(du, xh1, l_w1[c]);
-          if (bias) l_b1[c] += du;
-        }
+        const float g = gs_at(c), xh = (at(A.x, row * A.ld_x + c) - m1) * r1, f = factor(c);
+        const float g1 = g * f * param_or(A.post_weight, c, A.param_bf16, 1.f);
+        t[0] += g1;
+        t[1] = fmaf(g1, xh, t[1]);
+        t[2] = fmaf(g, f * param_or(A.post_bias, c, A.param_bf16, 0.f), t[2]);
+        line[A.H + c] = fmaf(g * gt, xh, line[A.H + c]);
+        line[3 * A.H + c] += g * gt;
       }
-      block_sums<3>(t, sh, slot);
-      if (A.token_gate && threadIdx.x == 0) A.dtoken_gate[row] = t[2];
+      group_sums<true, 3>(t, sh, slot);
+      if (A.token_gate && threadIdx.x == 0) A.dtoken_gate[row] = t[1] + t[2];
     }
-    const float c1 = A.rms ? 0.f : t[0] * inv_h, c2 = t[1] * inv_h;
+    const float c1 = A.rms ? 0.f : gt * (t[0] * inv_h), c2 = gt * (t[1] * inv_h);
     for (int64_t c = threadIdx.x; c < A.H; c += blockDim.x) {
-      const float g = gs_at(c);
-      float w1, gc;
-      params<1>(A.post_weight, c, A.param_bf16, 1.f, &w1);
-      params<1>(A.gate, c, A.param_bf16, 1.f, &gc);
-      const float du = A.scale * gt * gc * g;
-      const float o = post ? r1 * fmaf(-(at(A.x, row * A.ld_x + c) - m1) * r1, c2, fmaf(du, w1, -c1)) : du;
-      It d;
-      d.set(&g);
-      d.store((char*)A.dresidual + (row * A.ld_dresidual + c) * ES);
-      d.set(&o);
-      d.store((char*)A.dx + (row * A.ld_dx + c) * ES);
+      const float g = gs_at(c), g1 = gt * g * factor(c);
+      const float o = post ? r1 * (fmaf(g1, param(A.post_weight, c, A.param_bf16), -c1) - (at(A.x, row * A.ld_x + c) - m1) * r1 * c2) : g1;
+      put<DT>(A.dresidual, row * A.ld_dresidual + c, g);
+      put<DT>(A.dx, row * A.ld_dx + c, o);
     }
   }
 }
 
-struct Outputs { float* p[kMaxSums]; };
-
-// Column sums of the blocks' lines, in a fixed order: 32 threads a column, each every 32nd line, then their sums.
-__global__ void __launch_bounds__(1024) block_lines_kernel(const float* partial, int64_t lines, int64_t H, int n, Outputs out) {
-  __shared__ float sh[32][33];
+// Column sums of the blocks' lines in a fixed order, 32 threads a column, each every 32nd line, then their sums; and the gradients that
+// are made of them.  Blocks with y = 0: of dw2 and db2; y = 1: of Q1 and Q0.
+__global__ void __launch_bounds__(1024) block_lines_kernel(BlockArgs A, int lines, int n) {
+  __shared__ float sh[2][32][33];
   const int which = blockIdx.y;
-  const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
+  const int64_t H = A.H, c = (int64_t)blockIdx.x * 32 + threadIdx.x;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  float s = 0.f;
+  float a = 0.f, b = 0.f;
   if (c < H) {
-    const float* p = partial + ((int64_t)threadIdx.y * n + which) * H + c;
+    const float* p = A.partial + ((int64_t)threadIdx.y * n + which) * H + c;
 #pragma unroll 8
-    for (int64_t g = threadIdx.y; g < lines; g += 32, p += 32 * n * H) s += *p;
+    for (int g = threadIdx.y; g < lines; g += 32, p += 32 * n * H) {
+      a += p[0];
+      if (n > 2) b += p[2 * H];
+    }
   }
-  sh[threadIdx.y][threadIdx.x] = s;
+  sh[0][threadIdx.y][threadIdx.x] = a;
+  sh[1][threadIdx.y][threadIdx.x] = b;
   __syncthreads();
-  const float v = warp_sum(sh[threadIdx.x][threadIdx.y]);   // warp y has column y of the block
+  a = warp_sum(sh[0][threadIdx.x][threadIdx.y]);            // warp y has column y of the block
+  b = warp_sum(sh[1][threadIdx.x][threadIdx.y]);
   const int64_t o = (int64_t)blockIdx.x * 32 + threadIdx.y;
-  if (threadIdx.x == 0 && o < H) out.p[which][o] = v;
+  if (threadIdx.x != 0 || o >= H) return;
+  if (which == 0) {
+    A.dweight[o] = a;
+    if (A.with_bias) A.dbias[o] = b;
+  } else {
+    const float f = A.scale * param_or(A.gate, o, A.param_bf16, 1.f);
+    if (A.post_weight) {
+      A.dpost_weight[o] = f * a;
+      if (A.with_bias) A.dpost_bias[o] = f * b;
+    }
+    if (A.gate) A.dgate[o] = A.scale * (param_or(A.post_weight, o, A.param_bf16, 1.f) * a + param_or(A.post_bias, o, A.param_bf16, 0.f) * b);
+  }
 }
 
-// Threads a row (a block) and accesses a thread.
+// Threads a row (a group), rows at a time and under way, groups a block.
 struct Plan {
-  int w;          // elements an access: a 16-byte vector, or 1
-  int nv;         // accesses a thread; 0: the kernels for any width
-  int threads;
+  bool vec, twice;         // twice: 16 elements a thread instead of 8
+  int rows, stages;        // rows 0: the kernels for any width
+  int threads, groups, place, smem;
 };
 
 bool vectors(const BlockArgs& a, bool backward) {
@@ -523,36 +712,45 @@ bool vectors(const BlockArgs& a, bool backward) {
   return a.H * es % 16 == 0 && pitch * es % 16 == 0 && (bits & 15) == 0;
 }
 
-Plan plan_for(int64_t H, int dtype, bool vec, bool backward) {
+constexpr int kShared = 225 * 1024;           // of an SM, for rows
+constexpr int stages_of(int rows, bool twice, int dt) { return rows == 2 ? 6 : twice && dt == JP_F32 ? 1 : 3; }
+
+Plan plan_for(int64_t T, int64_t H, int dtype, bool vec, int matrices, int most_threads, int sms) {
+  const int es = dtype == JP_BF16 ? 2 : 4;
   Plan p{};
-  const int vw = dtype == JP_BF16 ? 8 : 4, most = backward ? 512 : 1024;
-  p.w = vec ? vw : 1;
-  const int64_t n = (H + p.w - 1) / p.w;
-  p.nv = 0;
-  if (vec) {
-    for (int nv = 1; nv <= 16 / vw; nv *= 2)
-      if (n <= (int64_t)nv * most) { p.nv = nv; break; }
-  } else {
-    p.nv = n <= 8 * most ? 8 : n <= 16 * most ? 16 : 0;
+  p.vec = vec;
+  const int64_t per = (H + 7) / 8;
+  p.twice = per > most_threads;
+  const int64_t threads = ((p.twice ? (H + 15) / 16 : per) + 31) / 32 * 32;
+  if (threads > most_threads) return p;
+  p.threads = (int)threads;
+  p.groups = most_threads / p.threads;
+  p.place = place_bytes(vec, p.threads, (p.twice ? 2 : 1) * es / 2, H, es);
+  // two rows at a time where every group has several and their places fit
+  for (p.rows = p.twice || T < 4 * (int64_t)sms * p.groups ? 1 : 2; p.rows >= 1; --p.rows) {
+    p.stages = stages_of(p.rows, p.twice, dtype);
+    p.smem = p.stages * matrices * p.place;
+    if ((int64_t)p.smem * p.groups <= kShared) return p;
+    if (p.rows == 1) {
+      p.groups = kShared / p.smem;
+      if (p.groups > 0) return p;
+    }
   }
-  if (p.nv == 0) return {1, 0, 1024};
-  p.threads = (int)(((n + p.nv - 1) / p.nv + 31) / 32 * 32);
+  p.rows = 0;
   return p;
 }
 
-// Blocks: what an SM holds of 1024 threads (backward 512), at most 16 of them; fewer where rows are.
-int grid_for(int64_t T, const Plan& p, int sms, bool backward) {
-  int per = (backward && p.nv ? 512 : 1024) / p.threads;
-  per = per > 16 ? 16 : per;
-  const int64_t cap = (int64_t)sms * per;
-  return (int)(T < cap ? T : cap);
-}
-
 template <class... P, class... Q>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t s, Q... args) {
+cudaError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, int smem, cudaStream_t s, Q... args) {
+  // (the limit belongs to the kernel on the device, for all threads of the host: always the same amount)
+  cudaError_t e = cudaSuccess;
+  if (smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (e == cudaSuccess && smem > 40 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -562,73 +760,68 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t s, 
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <int DT> cudaError_t forward(const BlockArgs& a, cudaStream_t s, int sms) {
-  constexpr int VW = Vec<DT>::N;
-  const Plan p = plan_for(a.H, a.dtype, vectors(a, false), false);
-  const dim3 g(grid_for(a.T, p, sms, false)), b(p.threads);
-  if (p.nv == 0) {
-    block_fwd_wide_kernel<DT><<<g, b, 0, s>>>(a);
+// Forward: a block a group, 1024 threads an SM.
+template <int DT, bool FULL> cudaError_t forward(const BlockArgs& a, cudaStream_t s, int sms) {
+  const Plan p = plan_for(a.T, a.H, a.dtype, vectors(a, false), 2, 1024, sms);
+  if (p.rows == 0) {
+    block_fwd_wide_kernel<DT><<<(unsigned)(a.T < sms ? a.T : sms), 1024, 0, s>>>(a);
     return cudaGetLastError();
   }
-  if (p.w == 1) return p.nv == 8 ? launch(block_fwd_kernel<DT, 1, 8>, g, b, s, a) : launch(block_fwd_kernel<DT, 1, 16>, g, b, s, a);
-  if (p.nv == 1) return launch(block_fwd_kernel<DT, VW, 1>, g, b, s, a);
-  if (p.nv == 2) return launch(block_fwd_kernel<DT, VW, 2>, g, b, s, a);
-  if constexpr (DT == JP_F32) return launch(block_fwd_kernel<DT, VW, 4>, g, b, s, a);
-  return cudaErrorInvalidConfiguration;
+  const int64_t most = (int64_t)sms * (p.groups < 24 ? p.groups : 24), need = (a.T + p.rows - 1) / p.rows;
+  const dim3 g((unsigned)(need < most ? need : most)), b(p.threads);
+  constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
+#define JP_FORWARD(VEC, NU, R, TWICE) (p.threads <= 256 ? launch(block_fwd_kernel<DT, VEC, NU, R, stages_of(R, TWICE, DT), FULL, 256>, g, b, p.smem, s, a, p.place) \
+                                       : p.threads <= 512 ? launch(block_fwd_kernel<DT, VEC, NU, R, stages_of(R, TWICE, DT), FULL, 512>, g, b, p.smem, s, a, p.place) \
+                                                          : launch(block_fwd_kernel<DT, VEC, NU, R, stages_of(R, TWICE, DT), FULL, 1024>, g, b, p.smem, s, a, p.place))
+#define JP_FORWARD_TWICE(VEC, NU) launch(block_fwd_kernel<DT, VEC, NU, 1, stages_of(1, true, DT), FULL, 1024>, g, b, p.smem, s, a, p.place)
+  if (p.twice) return p.vec ? JP_FORWARD_TWICE(true, 2 * V) : JP_FORWARD_TWICE(false, 2 * E);
+  if (p.rows == 2) return p.vec ? JP_FORWARD(true, V, 2, false) : JP_FORWARD(false, E, 2, false);
+  return p.vec ? JP_FORWARD(true, V, 1, false) : JP_FORWARD(false, E, 1, false);
+#undef JP_FORWARD
+#undef JP_FORWARD_TWICE
 }
 
-template <int DT, bool POST, bool GATE, bool BIAS> cudaError_t backward(const BlockArgs& a, const Plan& p, dim3 g, cudaStream_t s) {
-  constexpr int VW = Vec<DT>::N;
-  const dim3 b(p.threads);
-  if (p.w == 1) return p.nv == 8 ? launch(block_bwd_kernel<DT, 1, 8, POST, GATE, BIAS>, g, b, s, a) : launch(block_bwd_kernel<DT, 1, 16, POST, GATE, BIAS>, g, b, s, a);
-  if (p.nv == 1) return launch(block_bwd_kernel<DT, VW, 1, POST, GATE, BIAS>, g, b, s, a);
-  if (p.nv == 2) return launch(block_bwd_kernel<DT, VW, 2, POST, GATE, BIAS>, g, b, s, a);
-  if constexpr (DT == JP_F32) return launch(block_bwd_kernel<DT, VW, 4, POST, GATE, BIAS>, g, b, s, a);
-  return cudaErrorInvalidConfiguration;
+// Backward: the groups of an SM in one block, of 512 threads.
+template <int DT, bool POST, bool FULL> cudaError_t backward(const BlockArgs& a, const Plan& p, dim3 g, cudaStream_t s) {
+  constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
+  const dim3 b(p.threads, p.groups);
+  const int sums = p.groups > 1 ? (FULL ? 4 : 2) * (int)a.H * 4 : 0, rows = p.smem * p.groups, smem = rows > sums ? rows : sums;
+#define JP_BACKWARD(VEC, NU, R, TWICE) launch(block_bwd_kernel<DT, VEC, NU, R, stages_of(R, TWICE, DT), POST, FULL>, g, b, smem, s, a, p.place)
+  if (p.twice) return p.vec ? JP_BACKWARD(true, 2 * V, 1, true) : JP_BACKWARD(false, 2 * E, 1, true);
+  if (p.rows == 2) return p.vec ? JP_BACKWARD(true, V, 2, false) : JP_BACKWARD(false, E, 2, false);
+  return p.vec ? JP_BACKWARD(true, V, 1, false) : JP_BACKWARD(false, E, 1, false);
+#undef JP_BACKWARD
 }
-template <int DT, bool POST, bool GATE> cudaError_t backward(const BlockArgs& a, const Plan& p, dim3 g, cudaStream_t s) {
-  return a.with_bias ? backward<DT, POST, GATE, true>(a, p, g, s) : backward<DT, POST, GATE, false>(a, p, g, s);
-}
-template <int DT> cudaError_t backward(const BlockArgs& a, const Plan& p, dim3 g, int n_lines, cudaStream_t s) {
-  if (p.nv == 0) {
-    block_bwd_wide_kernel<DT><<<g, p.threads, 0, s>>>(a, n_lines);
+template <int DT> cudaError_t backward(const BlockArgs& a, const Plan& p, int grid, bool full, cudaStream_t s) {
+  if (p.rows == 0) {
+    block_bwd_wide_kernel<DT><<<grid, 1024, 0, s>>>(a);
     return cudaGetLastError();
   }
-  if (a.post_weight) return a.gate ? backward<DT, true, true>(a, p, g, s) : backward<DT, true, false>(a, p, g, s);
-  return a.gate ? backward<DT, false, true>(a, p, g, s) : backward<DT, false, false>(a, p, g, s);
+  const dim3 g(grid);
+  if (a.post_weight) return full ? backward<DT, true, true>(a, p, g, s) : backward<DT, true, false>(a, p, g, s);
+  return full ? backward<DT, false, true>(a, p, g, s) : backward<DT, false, false>(a, p, g, s);
 }
+
+bool full(const BlockArgs& a, bool backward) { return !a.rms || a.token_gate || a.post_bias || (backward ? a.with_bias : a.bias != nullptr); }
 
 }  // namespace
 
 cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms) {
-  return a.dtype == JP_BF16 ? forward<JP_BF16>(a, s, sms) : forward<JP_F32>(a, s, sms);
+  if (a.dtype == JP_BF16) return full(a, false) ? forward<JP_BF16, true>(a, s, sms) : forward<JP_BF16, false>(a, s, sms);
+  return full(a, false) ? forward<JP_F32, true>(a, s, sms) : forward<JP_F32, false>(a, s, sms);
 }
 
-// The lines a backward call can need, whatever the alignment of its pointers.
-size_t block_workspace_bytes(int64_t T, int64_t H, int dtype, int sms) {
-  int most = 0;
-  for (const bool vec : {false, true}) {
-    const int g = grid_for(T, plan_for(H, dtype, vec, true), sms, true);
-    most = g > most ? g : most;
-  }
-  return (size_t)most * kMaxSums * (size_t)H * sizeof(float);
-}
+// At most a line a block and SM, whatever the kernel.
+size_t block_workspace_bytes(int64_t T, int64_t H, int, int sms) { return (size_t)(T < sms ? T : sms) * kMaxSums * (size_t)H * sizeof(float); }
 
 cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a.H, a.dtype, vectors(a, true), true);
-  const int grid = grid_for(a.T, p, sms, true);
-  const bool post = a.post_weight != nullptr, gate = a.gate != nullptr;
-  const int n = n_sums(post, gate, a.with_bias);
-  const cudaError_t e = a.dtype == JP_BF16 ? backward<JP_BF16>(a, p, dim3(grid), n, s) : backward<JP_F32>(a, p, dim3(grid), n, s);
+  const Plan p = plan_for(a.T, a.H, a.dtype, vectors(a, true), 4, 512, sms);
+  const int64_t need = p.rows ? (a.T + p.groups - 1) / p.groups : a.T;
+  const int grid = (int)(need < sms ? need : sms), n = p.rows == 0 || full(a, true) ? 4 : 2;
+  const cudaError_t e = a.dtype == JP_BF16 ? backward<JP_BF16>(a, p, grid, n == 4, s) : backward<JP_F32>(a, p, grid, n == 4, s);
   if (e != cudaSuccess) return e;
-  Outputs out{};
-  int k = 0;
-  out.p[k++] = a.dweight;
-  if (a.with_bias) out.p[k++] = a.dbias;
-  if (post) out.p[k++] = a.dpost_weight;
-  if (post && a.with_bias) out.p[k++] = a.dpost_bias;
-  if (gate) out.p[k++] = a.dgate;
-  return launch(block_lines_kernel, dim3((unsigned)((a.H + 31) / 32), n), dim3(32, 32), s, (const float*)a.partial, (int64_t)grid, a.H, n, out);
+  const unsigned y = a.post_weight || a.gate ? 2 : 1;
+  return launch(block_lines_kernel, dim3((unsigned)((a.H + 31) / 32), y), dim3(32, 32), 0, s, a, grid, n);
 }
 
 }  // namespace jp
