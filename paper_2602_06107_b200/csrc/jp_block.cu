@@ -42,20 +42,44 @@ template <bool SOLE> __device__ __forceinline__ void group_sync() {
   else asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.y + 1), "r"(blockDim.x) : "memory");
 }
 
-// N sums over the group, in all of its threads.  `slot` alternates between uses, so that one barrier each is enough.
+// N sums over the group, in all of its threads, at once: at each step of a warp's sum half of the values go to the other half of the lanes
+// (N - 1 + log2(32 / N) shuffles for N a power of two, instead of 5 N), and so when each warp adds the warps' sums.  `slot` alternates
+// between uses, so that one barrier each is enough.
 template <bool SOLE, int N> __device__ __forceinline__ void group_sums(float (&v)[N], float (*sh)[kMaxValues][kMaxWarps], int& slot) {
+  constexpr int M = N == 1 ? 1 : N == 2 ? 2 : N <= 4 ? 4 : 8, kLanes = 32 / M;      // lanes a value has
+  const int lane = threadIdx.x & 31;
+  float t[M];
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-  if (blockDim.x == 32) return;
-  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31, first = threadIdx.y * warps;
-  float (*part)[kMaxWarps] = sh[slot];
-  slot ^= 1;
-  if (lane == 0)
+  for (int i = 0; i < M; ++i) t[i] = i < N ? v[i] : 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) part[i][first + (threadIdx.x >> 5)] = v[i];
-  group_sync<SOLE>();
+  for (int n = M, o = 16; o > 0; o >>= 1) {
+    if (n > 1) {
+      n /= 2;
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? part[i][first + lane] : 0.f);
+      for (int i = 0; i < M / 2; ++i)
+        if (i < n) {
+          const float keep = (lane & o) ? t[i + n] : t[i], send = (lane & o) ? t[i] : t[i + n];
+          t[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        }
+    } else {
+      t[0] += __shfl_xor_sync(0xffffffffu, t[0], o);
+    }
+  }
+  float s = t[0];                                           // of value lane / kLanes
+  if (blockDim.x > 32) {
+    const int warps = blockDim.x >> 5, first = threadIdx.y * warps, mine = lane / kLanes;
+    float (*part)[kMaxWarps] = sh[slot];
+    slot ^= 1;
+    if (lane % kLanes == 0 && mine < N) part[mine][first + (threadIdx.x >> 5)] = s;
+    group_sync<SOLE>();
+    s = 0.f;
+    if (mine < N)
+      for (int w = lane % kLanes; w < warps; w += kLanes) s += part[mine][first + w];
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, s, i * kLanes);
 }
 
 // What a thread has of a row: NU units.  A unit is a 16-byte vector, or two elements a group's width apart where rows do not start on 16 bytes.
@@ -92,15 +116,17 @@ template <int DT, bool VEC> struct Unit {
     }
     return r;
   }
-  __device__ static __forceinline__ void store(void* row, int u, int64_t H, const Raw& r) {
+  // `at`: the thread's first element of the row
+  __device__ static __forceinline__ void store(char* at, int u, int64_t H, const Raw& r) {
     if constexpr (VEC) {
-      if (have(u, H)) stg_stream((uint4*)((char*)row + column(u) * ES), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+      if (have(u, H)) stg_stream((uint4*)(at + u * (int)blockDim.x * 16), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
     } else {
 #pragma unroll
       for (int half = 0; half < 2; ++half)
         if (have(u, H, half)) {
-          if constexpr (ES == 2) ((uint16_t*)row)[column(u, half)] = (uint16_t)(r.w[0] >> (16 * half));
-          else ((uint32_t*)row)[column(u, half)] = r.w[half];
+          char* const to = at + (2 * u + half) * (int)blockDim.x * ES;
+          if constexpr (ES == 2) *(uint16_t*)to = (uint16_t)(r.w[0] >> (16 * half));
+          else *(uint32_t*)to = r.w[half];
         }
     }
   }
@@ -121,38 +147,49 @@ __host__ __device__ inline int place_bytes(bool vec, int threads, int units, int
   return vec ? threads * units * 16 : (int)((H * es + 15) / 16 + 1) * 16;
 }
 
+// A matrix's rows of a group, for the thread that writes them: row `first`, then every `step`-th.
+template <int DT, bool VEC> struct Out {
+  char* at;
+  int64_t stride;
+  __device__ __forceinline__ Out(void* base, int64_t ld, int64_t first, int64_t step)
+      : at((char*)base + (first * ld + Unit<DT, VEC>::column(0)) * Vec<DT>::ESIZE), stride(step * ld * Vec<DT>::ESIZE) {}
+};
+
 // The group's rows of NT matrices: row `first`, then every `step`-th, STAGES of them under way.
 template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
   using Un = Unit<DT, VEC>;
   static constexpr int ES = Vec<DT>::ESIZE;
-  const char* base[NT];                                     // null: a matrix that there is not, which reads 0
-  int64_t ld[NT], H, T, next, step;
-  char* mem;
-  int place, in, out;
+  const char* next[NT];                                     // the next row to fetch (VEC: from the thread's first column on)
+  int64_t stride[NT], left;                                 // rows not fetched yet
+  char* mem;                                                // (VEC: the thread's own places)
+  int place, in, out;                                       // in, out: bytes, of the place to fill and of the oldest row's
+  unsigned have, there;                                     // bits: the unit is within the row; there is such a matrix (else it reads 0)
+  // without VEC
+  int64_t H;
+  unsigned taken[NT];                                       // low bits of the oldest row's address: a place begins at its row's offset to 16
+  const char* first_byte[NT];
+  const char* last_byte[NT];
   __device__ __forceinline__ void fetch() {
-    if (next < T) {
+    if (left > 0) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
-        if (base[t]) {
-          const char* row = base[t] + next * ld[t];
-          char* to = mem + (in * NT + t) * place;
+        if (there >> t & 1u) {
+          char* const to = mem + in + t * place;
           if constexpr (VEC) {
 #pragma unroll
             for (int u = 0; u < NU; ++u)
-              if (Un::have(u, H))
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + (u * (int)blockDim.x + threadIdx.x) * 16)),
-                             "l"(row + Un::column(u) * ES) : "memory");
+              if (have >> u & 1u)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + u * (int)blockDim.x * 16)), "l"(next[t] + u * (int)blockDim.x * 16) : "memory");
           } else {                                          // vectors that reach beyond the matrix, in its first and last row, element by element
-            const char* const end = row + H * ES;
-            const char* const last = base[t] + (T - 1) * ld[t] + H * ES;
-            const int head = (int)((uintptr_t)row & 15);
-            for (int i = threadIdx.x * 16; i < head + (int)(H * ES); i += blockDim.x * 16) {
-              const char* from = row - head + i;
-              if (from >= base[t] && from + 16 <= last) {
+            const char* const row = next[t];
+            const int skip = (int)((uintptr_t)row & 15), bytes = (int)(H * ES);
+            for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) {
+              const char* from = row - skip + i;
+              if (from >= first_byte[t] && from + 16 <= last_byte[t]) {
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + i)), "l"(from) : "memory");
               } else {
                 for (int q = 0; q < 16; q += ES)
-                  if (from + q >= row && from + q < end) {
+                  if (from + q >= row && from + q < row + bytes) {
                     if constexpr (ES == 2) *(uint16_t*)(to + i + q) = *(const volatile uint16_t*)(from + q);
                     else *(uint32_t*)(to + i + q) = *(const volatile uint32_t*)(from + q);
                   }
@@ -160,54 +197,74 @@ template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
             }
           }
         }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) next[t] += stride[t];
+      --left;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    next += step;
-    in = in == STAGES - 1 ? 0 : in + 1;
+    in = in == (STAGES - 1) * NT * place ? 0 : in + NT * place;
   }
-  __device__ __forceinline__ void start(const void* const (&b)[NT], const int64_t (&l)[NT], int64_t first, int64_t step_, int64_t T_, int64_t H_, char* mem_, int place_) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) base[t] = (const char*)b[t], ld[t] = l[t] * ES;
-    H = H_; T = T_; next = first; step = step_; mem = mem_; place = place_;
+  __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T, int64_t H_, char* mem_, int place_) {
+    H = H_;
+    place = place_;
+    mem = mem_ + (VEC ? threadIdx.x * 16 : 0);
     in = out = 0;
-#pragma unroll 1
+    have = there = 0u;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) have |= (unsigned)Un::have(u, H) << u;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      there |= (base[t] ? 1u : 0u) << t;
+      next[t] = (const char*)base[t] + (first * ld[t] + (VEC ? Un::column(0) : 0)) * ES;
+      taken[t] = (unsigned)(uintptr_t)next[t];
+      stride[t] = step * ld[t] * ES;
+      first_byte[t] = (const char*)base[t];
+      last_byte[t] = (const char*)base[t] + ((T - 1) * ld[t] + H) * ES;
+    }
+    left = first < T ? (T - first + step - 1) / step : 0;
+#pragma unroll
     for (int s = 0; s < STAGES; ++s) fetch();
   }
   template <int R> __device__ __forceinline__ void wait() {   // for the oldest R rows
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - R) : "memory");
     if (!VEC) group_sync<SOLE>();
   }
-  // unit u of matrix t of the r-th oldest row, which is `row`
-  __device__ __forceinline__ void get(int t, int u, int r_, int64_t row, float2 (&f)[Un::P]) const {
-    const int place_of = out + r_ >= STAGES ? out + r_ - STAGES : out + r_;
-    typename Un::Raw r;
+  // unit u of matrix t of the r-th oldest row
+  __device__ __forceinline__ void get(int t, int u, int r, float2 (&f)[Un::P]) const {
+    int at = out + r * NT * place;
+    if (r > 0) at = at >= STAGES * NT * place ? at - STAGES * NT * place : at;
+    typename Un::Raw w;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(r) / 4); ++i) r.w[i] = 0u;
-    if (base[t]) {
-      const char* from = mem + (place_of * NT + t) * place;
+    for (int i = 0; i < (int)(sizeof(w) / 4); ++i) w.w[i] = 0u;
+    if (there >> t & 1u) {
+      const char* from = mem + at + t * place;
       if constexpr (VEC) {
-        if (Un::have(u, H)) {
-          const uint4 v = *(const uint4*)(from + (u * (int)blockDim.x + threadIdx.x) * 16);
-          r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+        if (have >> u & 1u) {
+          const uint4 v = *(const uint4*)(from + u * (int)blockDim.x * 16);
+          w.w[0] = v.x; w.w[1] = v.y; w.w[2] = v.z; w.w[3] = v.w;
         }
       } else {
-        from += (uintptr_t)(base[t] + row * ld[t]) & 15;
+        from += (taken[t] + (unsigned)r * (unsigned)stride[t]) & 15u;
 #pragma unroll
         for (int half = 0; half < 2; ++half)
           if (Un::have(u, H, half)) {
-            if constexpr (ES == 2) r.w[0] |= (uint32_t)((const uint16_t*)from)[Un::column(u, half)] << (16 * half);
-            else r.w[half] = ((const uint32_t*)from)[Un::column(u, half)];
+            if constexpr (ES == 2) w.w[0] |= (uint32_t)((const uint16_t*)from)[Un::column(u, half)] << (16 * half);
+            else w.w[half] = ((const uint32_t*)from)[Un::column(u, half)];
           }
       }
     }
-    Un::unpack(r, f);
+    Un::unpack(w, f);
   }
   template <int R> __device__ __forceinline__ void done() {   // the oldest R rows' places are free
     if (!VEC) group_sync<SOLE>();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      out = out == STAGES - 1 ? 0 : out + 1;
+      out = out == (STAGES - 1) * NT * place ? 0 : out + NT * place;
       fetch();
+    }
+    if (!VEC) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) taken[t] += R * (unsigned)stride[t];
     }
   }
 };
@@ -262,7 +319,7 @@ __device__ __forceinline__ void row_stats(const BlockArgs& A, Get get, float (*s
   }
   group_sums<true, R>(v, sh, slot);
 #pragma unroll
-  for (int r = 0; r < R; ++r) rstd[r] = 1.f / sqrtf(v[r] * inv_h + A.eps);
+  for (int r = 0; r < R; ++r) rstd[r] = rsqrtf(v[r] * inv_h + A.eps);     // (2 units in the last place at most)
 }
 
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
@@ -271,7 +328,7 @@ __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 template <int DT, bool VEC, int NU, int R, int STAGES, bool FULL, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) block_fwd_kernel(BlockArgs A, int place) {
   using Un = Unit<DT, VEC>;
-  constexpr int ES = Vec<DT>::ESIZE, P = Un::P;
+  constexpr int P = Un::P;
   extern __shared__ uint4 places[];
   __shared__ float sh[2][kMaxValues][kMaxWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");        // launched as a programmatic dependent of whatever is before it
@@ -281,6 +338,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
   const bool center = FULL && !A.rms, post = A.post_weight != nullptr;
   Ring<DT, VEC, NU, 2, STAGES, true> in;
   in.start({A.x, A.residual}, {A.ld_x, A.ld_residual}, blockIdx.x, step, A.T, A.H, (char*)places, place);
+  Out<DT, VEC> sum(A.sum, A.ld_sum, blockIdx.x, step), y(A.y, A.ld_y, blockIdx.x, step);
   // s = residual + gt (xhat1 fw + fb),  y = xhat2 w2 + b2
   float2 fw[NU][P], fb[FULL ? NU : 1][P], w2[NU][P], b2[FULL ? NU : 1][P];
 #pragma unroll
@@ -305,7 +363,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
     float m1[R], r1[R], m2[R], r2[R];
     in.template wait<R>();
     if (post) {
-      row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { in.get(0, u, r, row + r * step, f); }, sh, slot, m1, r1);
+      row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { in.get(0, u, r, f); }, sh, slot, m1, r1);
     } else {
 #pragma unroll
       for (int r = 0; r < R; ++r) m1[r] = 0.f, r1[r] = 1.f;
@@ -319,8 +377,8 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         float2 x[P], o[P];
-        in.get(0, u, r, t, x);
-        in.get(1, u, r, t, o);
+        in.get(0, u, r, x);
+        in.get(1, u, r, o);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           if (center) x[p] = add2(x[p], both(-m1[r]));
@@ -328,7 +386,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
           o[p] = FULL ? fma2(fma2(x[p], fw[u][p], fb[u][p]), both(gt), o[p]) : fma2(x[p], fw[u][p], o[p]);
         }
         s[r][u] = Un::pack(o);
-        Un::store((char*)A.sum + t * A.ld_sum * ES, u, A.H, s[r][u]);
+        Un::store(sum.at + r * sum.stride, u, A.H, s[r][u]);
       }
       if (threadIdx.x == 0 && post) {
         if (A.out_post_mean) A.out_post_mean[t] = m1[r];
@@ -351,13 +409,15 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
           x[p] = mul2(x[p], both(r2[r]));
           x[p] = FULL ? fma2(x[p], w2[u][p], b2[u][p]) : mul2(x[p], w2[u][p]);
         }
-        Un::store((char*)A.y + t * A.ld_y * ES, u, A.H, Un::pack(x));
+        Un::store(y.at + r * y.stride, u, A.H, Un::pack(x));
       }
       if (threadIdx.x == 0) {
         if (A.out_mean) A.out_mean[t] = m2[r];
         if (A.out_rstd) A.out_rstd[t] = r2[r];
       }
     }
+    sum.at += R * sum.stride;
+    y.at += R * y.stride;
   }
 }
 
@@ -434,7 +494,7 @@ constexpr int kMaxSums = 4;
 template <int DT, bool VEC, int NU, int R, int STAGES, bool POST, bool FULL>
 __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) {
   using Un = Unit<DT, VEC>;
-  constexpr int ES = Vec<DT>::ESIZE, P = Un::P, N = FULL ? 4 : 2, V1 = FULL ? 2 * R : R, V2 = FULL ? 3 * R : R;
+  constexpr int P = Un::P, N = FULL ? 4 : 2, V1 = FULL ? 2 * R : R, V2 = FULL ? 3 * R : R;
   static_assert(V2 <= kMaxValues, "");
   extern __shared__ uint4 places[];
   __shared__ float sh[2][kMaxValues][kMaxWarps];
@@ -468,18 +528,27 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
       if (FULL) fb[u][p] = mul2(fb[u][p], g[p]);
     }
   }
-  for (int64_t row = first; row < A.T; row += R * step) {
-    float m1[R], r1[R], m2[R], r2[R], gt[R], v[V1], t[V2];
+  // the rows' scalars, fetched a turn ahead (a row behind the last one reads 0 throughout)
+  float next[R][5];
+  auto scalars = [&](int64_t row) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t at = row + r * step;
-      const bool have = r == 0 || at < A.T;                 // (a row behind the last one reads 0 throughout)
-      m2[r] = center && have ? A.mean[at] : 0.f;
-      r2[r] = have ? A.rstd[at] : 0.f;
-      m1[r] = POST && center && have ? A.post_mean[at] : 0.f;
-      r1[r] = !POST ? 1.f : have ? A.post_rstd[at] : 0.f;
-      gt[r] = token && have ? A.token_gate[at] : have ? 1.f : 0.f;
+      const bool have = at < A.T;
+      next[r][0] = POST && center && have ? A.post_mean[at] : 0.f;
+      next[r][1] = !POST ? 1.f : have ? A.post_rstd[at] : 0.f;
+      next[r][2] = center && have ? A.mean[at] : 0.f;
+      next[r][3] = have ? A.rstd[at] : 0.f;
+      next[r][4] = token && have ? A.token_gate[at] : have ? 1.f : 0.f;
     }
+  };
+  scalars(first);
+  Out<DT, VEC> dres(A.dresidual, A.ld_dresidual, first, step), dx(A.dx, A.ld_dx, first, step);
+  for (int64_t row = first; row < A.T; row += R * step) {
+    float m1[R], r1[R], m2[R], r2[R], gt[R], v[V1], t[V2];
+#pragma unroll
+    for (int r = 0; r < R; ++r) m1[r] = next[r][0], r1[r] = next[r][1], m2[r] = next[r][2], r2[r] = next[r][3], gt[r] = next[r][4];
+    scalars(row + R * step);
     in.template wait<R>();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -488,8 +557,8 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
           float2 d[P], s[P];
-          in.get(0, u, r, row + r * step, d);
-          in.get(1, u, r, row + r * step, s);
+          in.get(0, u, r, d);
+          in.get(1, u, r, s);
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             if (center) s[p] = add2(s[p], both(-m2[r]));
@@ -516,10 +585,10 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
           float2 d[P], s[P], e[P], x[P];
-          in.get(0, u, r, at, d);
-          in.get(1, u, r, at, s);
-          in.get(2, u, r, at, e);
-          in.get(3, u, r, at, x);
+          in.get(0, u, r, d);
+          in.get(1, u, r, s);
+          in.get(2, u, r, e);
+          in.get(3, u, r, x);
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             if (center) s[p] = add2(s[p], both(-m2[r]));
@@ -537,7 +606,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
               acc[3][u][p] = add2(acc[3][u][p], gg);
             }
           }
-          Un::store((char*)A.dresidual + at * A.ld_dresidual * ES, u, A.H, Un::pack(gs[r][u]));
+          Un::store(dres.at + r * dres.stride, u, A.H, Un::pack(gs[r][u]));
         }
       }
       t[r] = t1.x + t1.y;
@@ -557,7 +626,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         float2 o[P], x[P];
-        if (POST) in.get(3, u, r, at, x);
+        if (POST) in.get(3, u, r, x);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           o[p] = mul2(gs[r][u][p], fw[u][p]);
@@ -568,10 +637,12 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
             o[p] = mul2(o[p], both(gt[r]));
           }
         }
-        Un::store((char*)A.dx + at * A.ld_dx * ES, u, A.H, Un::pack(o));
+        Un::store(dx.at + r * dx.stride, u, A.H, Un::pack(o));
       }
     }
     in.template done<R>();
+    dres.at += R * dres.stride;
+    dx.at += R * dx.stride;
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the kernel that adds the lines may set up
