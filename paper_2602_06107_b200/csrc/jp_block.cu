@@ -102,6 +102,11 @@ template <int DT, bool VEC> struct Unit {
       for (int p = 0; p < P; ++p) f[p] = make_float2(__uint_as_float(r.w[2 * p]), __uint_as_float(r.w[2 * p + 1]));
     }
   }
+  // (unpacked again behind a sum instead of being kept over it: as fp32 a row takes twice the registers)
+  __device__ static __forceinline__ void keep(Raw& r) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Raw) / 4); ++i) asm volatile("" : "+r"(r.w[i]));
+  }
   __device__ static __forceinline__ Raw pack(const float2 (&f)[P]) {      // rounds
     Raw r;
     if constexpr (ES == 2) {
@@ -155,15 +160,40 @@ template <int DT, bool VEC> struct Out {
       : at((char*)base + (first * ld + Unit<DT, VEC>::column(0)) * Vec<DT>::ESIZE), stride(step * ld * Vec<DT>::ESIZE) {}
 };
 
+// Shared memory by its own addresses (32 bits, no generic loads).
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+template <int ES> __device__ __forceinline__ uint32_t lds_one(uint32_t at) {
+  uint32_t v;
+  if constexpr (ES == 2) {
+    uint16_t h;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at) : "memory");
+    v = h;
+  } else {
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  }
+  return v;
+}
+template <int ES> __device__ __forceinline__ void sts_one(uint32_t at, const char* from) {
+  if constexpr (ES == 2) asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(*(const volatile uint16_t*)from) : "memory");
+  else asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(*(const volatile uint32_t*)from) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t to, const char* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
 // The group's rows of NT matrices: row `first`, then every `step`-th, STAGES of them under way.
 template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
   using Un = Unit<DT, VEC>;
   static constexpr int ES = Vec<DT>::ESIZE;
   const char* next[NT];                                     // the next row to fetch (VEC: from the thread's first column on)
   int64_t stride[NT], left;                                 // rows not fetched yet
-  char* mem;                                                // (VEC: the thread's own places)
-  int place, in, out;                                       // in, out: bytes, of the place to fill and of the oldest row's
-  unsigned have, there;                                     // bits: the unit is within the row; there is such a matrix (else it reads 0)
+  uint32_t mem, in, out, end;                               // places (VEC: the thread's own): all, to fill, the oldest row's
+  int place;
+  unsigned have, there;                                     // bits: the unit is within the row; there is such a matrix
   // without VEC
   int64_t H;
   unsigned taken[NT];                                       // low bits of the oldest row's address: a place begins at its row's offset to 16
@@ -174,25 +204,21 @@ template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
         if (there >> t & 1u) {
-          char* const to = mem + in + t * place;
+          const uint32_t to = in + t * place;
           if constexpr (VEC) {
 #pragma unroll
             for (int u = 0; u < NU; ++u)
-              if (have >> u & 1u)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + u * (int)blockDim.x * 16)), "l"(next[t] + u * (int)blockDim.x * 16) : "memory");
+              if (have >> u & 1u) copy16(to + u * blockDim.x * 16, next[t] + u * (int)blockDim.x * 16);
           } else {                                          // vectors that reach beyond the matrix, in its first and last row, element by element
             const char* const row = next[t];
             const int skip = (int)((uintptr_t)row & 15), bytes = (int)(H * ES);
             for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) {
               const char* from = row - skip + i;
               if (from >= first_byte[t] && from + 16 <= last_byte[t]) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + i)), "l"(from) : "memory");
+                copy16(to + i, from);
               } else {
                 for (int q = 0; q < 16; q += ES)
-                  if (from + q >= row && from + q < row + bytes) {
-                    if constexpr (ES == 2) *(uint16_t*)(to + i + q) = *(const volatile uint16_t*)(from + q);
-                    else *(uint32_t*)(to + i + q) = *(const volatile uint32_t*)(from + q);
-                  }
+                  if (from + q >= row && from + q < row + bytes) sts_one<ES>(to + i + q, from + q);
               }
             }
           }
@@ -202,13 +228,15 @@ template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
       --left;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    in = in == (STAGES - 1) * NT * place ? 0 : in + NT * place;
+    in += NT * place;
+    if (in == end) in = mem;
   }
-  __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T, int64_t H_, char* mem_, int place_) {
+  __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T, int64_t H_, const void* mem_, int place_) {
     H = H_;
     place = place_;
-    mem = mem_ + (VEC ? threadIdx.x * 16 : 0);
-    in = out = 0;
+    mem = (uint32_t)__cvta_generic_to_shared(mem_) + (VEC ? threadIdx.x * 16 : 0);
+    in = out = mem;
+    end = mem + STAGES * NT * place;
     have = there = 0u;
 #pragma unroll
     for (int u = 0; u < NU; ++u) have |= (unsigned)Un::have(u, H) << u;
@@ -222,44 +250,52 @@ template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
       last_byte[t] = (const char*)base[t] + ((T - 1) * ld[t] + H) * ES;
     }
     left = first < T ? (T - first + step - 1) / step : 0;
+    if constexpr (VEC) {                                    // what is never fetched reads 0
+      if (have != (1u << NU) - 1u || there != (1u << NT) - 1u || left < STAGES)
+        for (uint32_t at = mem; at != end; at += place)
 #pragma unroll
+          for (int u = 0; u < NU; ++u)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at + u * blockDim.x * 16), "r"(0u) : "memory");
+    }
+#pragma unroll 1
     for (int s = 0; s < STAGES; ++s) fetch();
   }
   template <int R> __device__ __forceinline__ void wait() {   // for the oldest R rows
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - R) : "memory");
     if (!VEC) group_sync<SOLE>();
   }
-  // unit u of matrix t of the r-th oldest row
-  __device__ __forceinline__ void get(int t, int u, int r, float2 (&f)[Un::P]) const {
-    int at = out + r * NT * place;
-    if (r > 0) at = at >= STAGES * NT * place ? at - STAGES * NT * place : at;
+  __device__ __forceinline__ uint32_t row(int r) const {      // the r-th oldest row's places
+    const uint32_t at = out + r * NT * place;
+    return r > 0 && at >= end ? at - STAGES * NT * place : at;
+  }
+  // unit u of matrix t of the r-th oldest row, whose places are `at`
+  __device__ __forceinline__ typename Un::Raw get(uint32_t at, int t, int u, int r) const {
     typename Un::Raw w;
+    if constexpr (VEC) {
+      const uint4 v = lds16(at + t * place + u * blockDim.x * 16);
+      w.w[0] = v.x; w.w[1] = v.y; w.w[2] = v.z; w.w[3] = v.w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(w) / 4); ++i) w.w[i] = 0u;
-    if (there >> t & 1u) {
-      const char* from = mem + at + t * place;
-      if constexpr (VEC) {
-        if (have >> u & 1u) {
-          const uint4 v = *(const uint4*)(from + u * (int)blockDim.x * 16);
-          w.w[0] = v.x; w.w[1] = v.y; w.w[2] = v.z; w.w[3] = v.w;
-        }
-      } else {
-        from += (taken[t] + (unsigned)r * (unsigned)stride[t]) & 15u;
+      for (int i = 0; i < (int)(sizeof(w) / 4); ++i) w.w[i] = 0u;
+      if (there >> t & 1u) {
+        const uint32_t from = at + t * place + ((taken[t] + (unsigned)r * (unsigned)stride[t]) & 15u) + threadIdx.x * ES;
 #pragma unroll
         for (int half = 0; half < 2; ++half)
           if (Un::have(u, H, half)) {
-            if constexpr (ES == 2) w.w[0] |= (uint32_t)((const uint16_t*)from)[Un::column(u, half)] << (16 * half);
-            else w.w[half] = ((const uint32_t*)from)[Un::column(u, half)];
+            const uint32_t v = lds_one<ES>(from + (2 * u + half) * blockDim.x * ES);
+            if constexpr (ES == 2) w.w[0] |= v << (16 * half);
+            else w.w[half] = v;
           }
       }
     }
-    Un::unpack(w, f);
+    return w;
   }
   template <int R> __device__ __forceinline__ void done() {   // the oldest R rows' places are free
     if (!VEC) group_sync<SOLE>();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      out = out == (STAGES - 1) * NT * place ? 0 : out + NT * place;
+      out += NT * place;
+      if (out == end) out = mem;
       fetch();
     }
     if (!VEC) {
@@ -337,7 +373,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
   const int64_t step = gridDim.x;
   const bool center = FULL && !A.rms, post = A.post_weight != nullptr;
   Ring<DT, VEC, NU, 2, STAGES, true> in;
-  in.start({A.x, A.residual}, {A.ld_x, A.ld_residual}, blockIdx.x, step, A.T, A.H, (char*)places, place);
+  in.start({A.x, A.residual}, {A.ld_x, A.ld_residual}, blockIdx.x, step, A.T, A.H, places, place);
   Out<DT, VEC> sum(A.sum, A.ld_sum, blockIdx.x, step), y(A.y, A.ld_y, blockIdx.x, step);
   // s = residual + gt (xhat1 fw + fb),  y = xhat2 w2 + b2
   float2 fw[NU][P], fb[FULL ? NU : 1][P], w2[NU][P], b2[FULL ? NU : 1][P];
@@ -362,13 +398,22 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
   for (int64_t row = blockIdx.x; row < A.T; row += R * step) {
     float m1[R], r1[R], m2[R], r2[R];
     in.template wait<R>();
+    typename Un::Raw rx[R][NU], s[R][NU];                   // s: the residual, then the sum
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint32_t at = in.row(r);
+#pragma unroll
+      for (int u = 0; u < NU; ++u) rx[r][u] = in.get(at, 0, u, r);
+#pragma unroll
+      for (int u = 0; u < NU; ++u) s[r][u] = in.get(at, 1, u, r);
+    }
+    in.template done<R>();
     if (post) {
-      row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { in.get(0, u, r, f); }, sh, slot, m1, r1);
+      row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { Un::unpack(rx[r][u], f); }, sh, slot, m1, r1);
     } else {
 #pragma unroll
       for (int r = 0; r < R; ++r) m1[r] = 0.f, r1[r] = 1.f;
     }
-    typename Un::Raw s[R][NU];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t t = row + r * step;
@@ -377,8 +422,8 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         float2 x[P], o[P];
-        in.get(0, u, r, x);
-        in.get(1, u, r, o);
+        Un::unpack(rx[r][u], x);
+        Un::unpack(s[r][u], o);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           if (center) x[p] = add2(x[p], both(-m1[r]));
@@ -393,7 +438,6 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
         if (A.out_post_rstd) A.out_post_rstd[t] = r1[r];
       }
     }
-    in.template done<R>();
     row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { Un::unpack(s[r][u], f); }, sh, slot, m2, r2);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -550,6 +594,16 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
     for (int r = 0; r < R; ++r) m1[r] = next[r][0], r1[r] = next[r][1], m2[r] = next[r][2], r2[r] = next[r][3], gt[r] = next[r][4];
     scalars(row + R * step);
     in.template wait<R>();
+    typename Un::Raw rd[R][NU], rs[R][NU], re[R][NU], rx[R][NU];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint32_t at = in.row(r);
+#pragma unroll
+      for (int u = 0; u < NU; ++u) rd[r][u] = in.get(at, 0, u, r), rs[r][u] = in.get(at, 1, u, r);
+#pragma unroll
+      for (int u = 0; u < NU; ++u) re[r][u] = in.get(at, 2, u, r), rx[r][u] = in.get(at, 3, u, r);
+    }
+    in.template done<R>();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float2 v1 = both(0.f), v2 = v1;
@@ -557,8 +611,8 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
           float2 d[P], s[P];
-          in.get(0, u, r, d);
-          in.get(1, u, r, s);
+          Un::unpack(rd[r][u], d);
+          Un::unpack(rs[r][u], s);
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             if (center) s[p] = add2(s[p], both(-m2[r]));
@@ -574,7 +628,11 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
       if (FULL) v[R + r] = v1.x + v1.y;
     }
     group_sums<false, V1>(v, sh, slot);
-    // gs = r2 (dy w2 - a1 - xhat2 a2) + ds, kept; x is read once more behind its sums
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int u = 0; u < NU; ++u) Un::keep(rd[r][u]), Un::keep(rs[r][u]);
+    // gs = r2 (dy w2 - a1 - xhat2 a2) + ds
     float2 gs[R][NU][P];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -585,10 +643,10 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
           float2 d[P], s[P], e[P], x[P];
-          in.get(0, u, r, d);
-          in.get(1, u, r, s);
-          in.get(2, u, r, e);
-          in.get(3, u, r, x);
+          Un::unpack(rd[r][u], d);
+          Un::unpack(rs[r][u], s);
+          Un::unpack(re[r][u], e);
+          Un::unpack(rx[r][u], x);
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             if (center) s[p] = add2(s[p], both(-m2[r]));
@@ -617,6 +675,10 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
     }
     if (POST || token) group_sums<false, V2>(t, sh, slot);
 #pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int u = 0; u < NU; ++u) Un::keep(rx[r][u]);
+#pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t at = row + r * step;
       if (r > 0 && at >= A.T) break;
@@ -626,7 +688,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         float2 o[P], x[P];
-        if (POST) in.get(3, u, r, x);
+        if (POST) Un::unpack(rx[r][u], x);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           o[p] = mul2(gs[r][u][p], fw[u][p]);
@@ -640,7 +702,6 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
         Un::store(dx.at + r * dx.stride, u, A.H, Un::pack(o));
       }
     }
-    in.template done<R>();
     dres.at += R * dres.stride;
     dx.at += R * dx.stride;
   }
@@ -786,12 +847,12 @@ bool vectors(const BlockArgs& a, bool backward) {
 constexpr int kShared = 225 * 1024;           // of an SM, for rows
 constexpr int stages_of(int rows, bool twice, int dt) { return rows == 2 ? 6 : twice && dt == JP_F32 ? 1 : 3; }
 
-Plan plan_for(int64_t T, int64_t H, int dtype, bool vec, int matrices, int most_threads, int sms) {
+Plan plan_for(int64_t T, int64_t H, int dtype, bool vec, bool prefer_twice, int matrices, int most_threads, int sms) {
   const int es = dtype == JP_BF16 ? 2 : 4;
   Plan p{};
   p.vec = vec;
   const int64_t per = (H + 7) / 8;
-  p.twice = per > most_threads;
+  p.twice = per > most_threads || prefer_twice;
   const int64_t threads = ((p.twice ? (H + 15) / 16 : per) + 31) / 32 * 32;
   if (threads > most_threads) return p;
   p.threads = (int)threads;
@@ -833,7 +894,7 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, int smem, cudaSt
 
 // Forward: a block a group, 1024 threads an SM.
 template <int DT, bool FULL> cudaError_t forward(const BlockArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a.T, a.H, a.dtype, vectors(a, false), 2, 1024, sms);
+  const Plan p = plan_for(a.T, a.H, a.dtype, vectors(a, false), false, 2, 1024, sms);
   if (p.rows == 0) {
     block_fwd_wide_kernel<DT><<<(unsigned)(a.T < sms ? a.T : sms), 1024, 0, s>>>(a);
     return cudaGetLastError();
@@ -886,7 +947,8 @@ cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms) {
 size_t block_workspace_bytes(int64_t T, int64_t H, int, int sms) { return (size_t)(T < sms ? T : sms) * kMaxSums * (size_t)H * sizeof(float); }
 
 cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a.T, a.H, a.dtype, vectors(a, true), 4, 512, sms);
+  const bool vec = vectors(a, true);
+  const Plan p = plan_for(a.T, a.H, a.dtype, vec, false, 4, 512, sms);
   const int64_t need = p.rows ? (a.T + p.groups - 1) / p.groups : a.T;
   const int grid = (int)(need < sms ? need : sms), n = p.rows == 0 || full(a, true) ? 4 : 2;
   const cudaError_t e = a.dtype == JP_BF16 ? backward<JP_BF16>(a, p, grid, n == 4, s) : backward<JP_F32>(a, p, grid, n == 4, s);
