@@ -13,8 +13,10 @@
 // Q0 = sum_t gt gs,  dw1 = a gc Q1,  db1 = a gc Q0,  dgc = a (w1 Q1 + b1 Q0),  and dgt is what dx's sum has anyway.  The groups of a block add
 // theirs in their order, the blocks leave a line each in the workspace, which a second kernel adds in a fixed order: no atomics, the
 // same bits every time.
-// Rows on 16 bytes: each thread copies what it will read itself, no barrier for the data.  Other rows: the group copies the vectors that cover a
-// row and reads elements.
+// A thread reads what it copied itself, 16 bytes at a time, no barrier for the data.  Rows that start anywhere, all matrices at the same offset to
+// 16 bytes (packed ones of odd width): the vectors that cover the row, with what belongs to other rows masked in the first and the
+// last one; a group's rows are a multiple of the period apart after which offsets repeat, so a thread keeps its columns.  Matrices at
+// different offsets: the group copies the covering vectors together and reads elements.
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -82,15 +84,35 @@ template <bool SOLE, int N> __device__ __forceinline__ void group_sums(float (&v
   for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, s, i * kLanes);
 }
 
-// What a thread has of a row: NU units.  A unit is a 16-byte vector, or two elements a group's width apart where rows do not start on 16 bytes.
-template <int DT, bool VEC> struct Unit {
+enum Kind { kAligned, kShared, kElements };                 // rows on 16 bytes; all matrices' rows at the same offsets to 16 bytes; neither
+
+// What a thread has of a row: NU units.  A unit is a 16-byte vector, or (kElements) two elements a group's width apart.
+template <int DT, int KIND> struct Unit {
+  static constexpr bool VEC = KIND != kElements;
   static constexpr int W = VEC ? Vec<DT>::N : 1;            // consecutive elements
   static constexpr int E = VEC ? W : 2, P = E / 2;          // elements and pairs of a unit
   static constexpr int ES = Vec<DT>::ESIZE;
-  __device__ static __forceinline__ int64_t column(int u, int half = 0) {
-    return VEC ? (int64_t)(threadIdx.x + u * (int)blockDim.x) * W : threadIdx.x + (2 * u + half) * (int64_t)blockDim.x;
+  int64_t H;
+  int first;                                                // column of the first unit (kShared: of its vector, from -W + 1 on)
+  unsigned have, part;                                      // bits: some of the unit's columns are in the row; not all of them
+  // `row`: where a row of the group starts
+  template <int NU> __device__ __forceinline__ void start(const void* row, int64_t H_) {
+    H = H_;
+    first = VEC ? (int)threadIdx.x * W - (KIND == kShared ? (int)((uintptr_t)row & 15) / ES : 0) : threadIdx.x;
+    have = part = 0u;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      int n = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) n += inside(column(u, e));
+      have |= (n > 0 ? 1u : 0u) << u;
+      part |= (n > 0 && n < E ? 1u : 0u) << u;
+    }
   }
-  __device__ static __forceinline__ bool have(int u, int64_t H, int half = 0) { return column(u, half) < H; }
+  __device__ __forceinline__ int64_t column(int u, int e) const {
+    return VEC ? first + (int64_t)u * (int)blockDim.x * W + e : first + (2 * u + e) * (int64_t)blockDim.x;
+  }
+  __device__ __forceinline__ bool inside(int64_t c) const { return c >= 0 && c < H; }
   // a unit in its type
   struct Raw { uint32_t w[VEC ? 4 : ES == 2 ? 1 : 2]; };
   __device__ static __forceinline__ void unpack(const Raw& r, float2 (&f)[P]) {
@@ -121,26 +143,47 @@ template <int DT, bool VEC> struct Unit {
     }
     return r;
   }
-  // `at`: the thread's first element of the row
-  __device__ static __forceinline__ void store(char* at, int u, int64_t H, const Raw& r) {
-    if constexpr (VEC) {
-      if (have(u, H)) stg_stream((uint4*)(at + u * (int)blockDim.x * 16), make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
-    } else {
+  // what belongs to other rows reads 0
+  __device__ __forceinline__ void mask(Raw& r, int u) const {
+    if (KIND == kShared && (part >> u & 1u)) {
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
-        if (have(u, H, half)) {
-          char* const to = at + (2 * u + half) * (int)blockDim.x * ES;
-          if constexpr (ES == 2) *(uint16_t*)to = (uint16_t)(r.w[0] >> (16 * half));
-          else *(uint32_t*)to = r.w[half];
+      for (int e = 0; e < E; ++e)
+        if (!inside(column(u, e))) {
+          if (ES == 2) r.w[e / 2] &= (e & 1) ? 0xffffu : 0xffff0000u;
+          else r.w[e] = 0u;
         }
     }
   }
-  // parameters at the unit's columns; `none` where there are none, 0 past the end
-  __device__ static __forceinline__ void params(const void* p, int u, int64_t H, bool bf16, float none, float2 (&f)[P]) {
+  // `at`: the thread's first unit of the row
+  __device__ __forceinline__ void store(char* at, int u, const Raw& r) const {
+    if constexpr (VEC) {
+      at += u * (int)blockDim.x * 16;
+      if (KIND == kShared && (part >> u & 1u)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (inside(column(u, e))) {
+            if constexpr (ES == 2) ((uint16_t*)at)[e] = (uint16_t)(r.w[e / 2] >> (16 * (e & 1)));
+            else ((uint32_t*)at)[e] = r.w[e];
+          }
+      } else if (have >> u & 1u) {
+        stg_stream((uint4*)at, make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (inside(column(u, e))) {
+          char* const to = at + (2 * u + e) * (int)blockDim.x * ES;
+          if constexpr (ES == 2) *(uint16_t*)to = (uint16_t)(r.w[0] >> (16 * e));
+          else *(uint32_t*)to = r.w[e];
+        }
+    }
+  }
+  // parameters at the unit's columns; `none` where there are none, 0 outside the row
+  __device__ __forceinline__ void params(const void* p, int u, bool bf16, float none, float2 (&f)[P]) const {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int64_t c = VEC ? column(u) + e : column(u, e);
-      const float v = c >= H ? 0.f : p ? param(p, c, bf16) : none;
+      const int64_t c = column(u, e);
+      const float v = !inside(c) ? 0.f : p ? param(p, c, bf16) : none;
       if (e & 1) f[e / 2].y = v;
       else f[e / 2].x = v;
     }
@@ -148,16 +191,16 @@ template <int DT, bool VEC> struct Unit {
 };
 
 // Bytes of a row's place in shared memory: the vectors of all threads, or the vectors that cover a row wherever it starts.
-__host__ __device__ inline int place_bytes(bool vec, int threads, int units, int64_t H, int es) {
+inline int place_bytes(bool vec, int threads, int units, int64_t H, int es) {
   return vec ? threads * units * 16 : (int)((H * es + 15) / 16 + 1) * 16;
 }
 
 // A matrix's rows of a group, for the thread that writes them: row `first`, then every `step`-th.
-template <int DT, bool VEC> struct Out {
+template <int ES> struct Out {
   char* at;
   int64_t stride;
-  __device__ __forceinline__ Out(void* base, int64_t ld, int64_t first, int64_t step)
-      : at((char*)base + (first * ld + Unit<DT, VEC>::column(0)) * Vec<DT>::ESIZE), stride(step * ld * Vec<DT>::ESIZE) {}
+  __device__ __forceinline__ Out(void* base, int64_t ld, int64_t first, int64_t step, int column)
+      : at((char*)base + (first * ld + column) * ES), stride(step * ld * ES) {}
 };
 
 // Shared memory by its own addresses (32 bits, no generic loads).
@@ -186,20 +229,28 @@ __device__ __forceinline__ void copy16(uint32_t to, const char* from) {
 }
 
 // The group's rows of NT matrices: row `first`, then every `step`-th, STAGES of them under way.
-template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
-  using Un = Unit<DT, VEC>;
+template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
+  using Un = Unit<DT, KIND>;
   static constexpr int ES = Vec<DT>::ESIZE;
-  const char* next[NT];                                     // the next row to fetch (VEC: from the thread's first column on)
+  static constexpr bool VEC = Un::VEC;
+  const char* next[NT];                                     // the next row to fetch (VEC: from the thread's first unit on)
   int64_t stride[NT], left;                                 // rows not fetched yet
   uint32_t mem, in, out, end;                               // places (VEC: the thread's own): all, to fill, the oldest row's
   int place;
-  unsigned have, there;                                     // bits: the unit is within the row; there is such a matrix
-  // without VEC
-  int64_t H;
-  unsigned taken[NT];                                       // low bits of the oldest row's address: a place begins at its row's offset to 16
+  unsigned there;                                           // bits: there is such a matrix
+  // kShared, kElements: vectors that reach beyond the matrix, in its first and last row, are copied element by element
   const char* first_byte[NT];
   const char* last_byte[NT];
-  __device__ __forceinline__ void fetch() {
+  unsigned taken[NT];                                       // kElements: low bits of the oldest row's address; a place begins at its row's offset to 16
+  __device__ __forceinline__ void copy(uint32_t to, const char* from, int t, const char* row, int64_t bytes) const {
+    if (from >= first_byte[t] && from + 16 <= last_byte[t]) {
+      copy16(to, from);
+    } else {
+      for (int q = 0; q < 16; q += ES)
+        if (from + q >= row && from + q < row + bytes) sts_one<ES>(to + q, from + q);
+    }
+  }
+  __device__ __forceinline__ void fetch(const Un& un) {
     if (left > 0) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -208,19 +259,15 @@ template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
           if constexpr (VEC) {
 #pragma unroll
             for (int u = 0; u < NU; ++u)
-              if (have >> u & 1u) copy16(to + u * blockDim.x * 16, next[t] + u * (int)blockDim.x * 16);
-          } else {                                          // vectors that reach beyond the matrix, in its first and last row, element by element
-            const char* const row = next[t];
-            const int skip = (int)((uintptr_t)row & 15), bytes = (int)(H * ES);
-            for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) {
-              const char* from = row - skip + i;
-              if (from >= first_byte[t] && from + 16 <= last_byte[t]) {
-                copy16(to + i, from);
-              } else {
-                for (int q = 0; q < 16; q += ES)
-                  if (from + q >= row && from + q < row + bytes) sts_one<ES>(to + i + q, from + q);
+              if (un.have >> u & 1u) {
+                const char* const from = next[t] + u * (int)blockDim.x * 16;
+                if (KIND == kShared && (un.part >> u & 1u)) copy(to + u * blockDim.x * 16, from, t, next[t] - un.first * ES, un.H * ES);
+                else copy16(to + u * blockDim.x * 16, from);
               }
-            }
+          } else {
+            const char* const row = next[t];
+            const int skip = (int)((uintptr_t)row & 15), bytes = (int)(un.H * ES);
+            for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) copy(to + i, row - skip + i, t, row, bytes);
           }
         }
 #pragma unroll
@@ -231,34 +278,31 @@ template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
     in += NT * place;
     if (in == end) in = mem;
   }
-  __device__ __forceinline__ void start(const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T, int64_t H_, const void* mem_, int place_) {
-    H = H_;
+  __device__ __forceinline__ void start(const Un& un, const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T, const void* mem_, int place_) {
     place = place_;
     mem = (uint32_t)__cvta_generic_to_shared(mem_) + (VEC ? threadIdx.x * 16 : 0);
     in = out = mem;
     end = mem + STAGES * NT * place;
-    have = there = 0u;
-#pragma unroll
-    for (int u = 0; u < NU; ++u) have |= (unsigned)Un::have(u, H) << u;
+    there = 0u;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       there |= (base[t] ? 1u : 0u) << t;
-      next[t] = (const char*)base[t] + (first * ld[t] + (VEC ? Un::column(0) : 0)) * ES;
+      next[t] = (const char*)base[t] + (first * ld[t] + (VEC ? un.first : 0)) * ES;
       taken[t] = (unsigned)(uintptr_t)next[t];
       stride[t] = step * ld[t] * ES;
       first_byte[t] = (const char*)base[t];
-      last_byte[t] = (const char*)base[t] + ((T - 1) * ld[t] + H) * ES;
+      last_byte[t] = (const char*)base[t] + ((T - 1) * ld[t] + un.H) * ES;
     }
     left = first < T ? (T - first + step - 1) / step : 0;
     if constexpr (VEC) {                                    // what is never fetched reads 0
-      if (have != (1u << NU) - 1u || there != (1u << NT) - 1u || left < STAGES)
+      if (un.have != (1u << NU) - 1u || there != (1u << NT) - 1u || left < STAGES)
         for (uint32_t at = mem; at != end; at += place)
 #pragma unroll
           for (int u = 0; u < NU; ++u)
             asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at + u * blockDim.x * 16), "r"(0u) : "memory");
     }
 #pragma unroll 1
-    for (int s = 0; s < STAGES; ++s) fetch();
+    for (int s = 0; s < STAGES; ++s) fetch(un);
   }
   template <int R> __device__ __forceinline__ void wait() {   // for the oldest R rows
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - R) : "memory");
@@ -269,34 +313,35 @@ template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
     return r > 0 && at >= end ? at - STAGES * NT * place : at;
   }
   // unit u of matrix t of the r-th oldest row, whose places are `at`
-  __device__ __forceinline__ typename Un::Raw get(uint32_t at, int t, int u, int r) const {
+  __device__ __forceinline__ typename Un::Raw get(const Un& un, uint32_t at, int t, int u, int r) const {
     typename Un::Raw w;
     if constexpr (VEC) {
       const uint4 v = lds16(at + t * place + u * blockDim.x * 16);
       w.w[0] = v.x; w.w[1] = v.y; w.w[2] = v.z; w.w[3] = v.w;
+      un.mask(w, u);
     } else {
 #pragma unroll
       for (int i = 0; i < (int)(sizeof(w) / 4); ++i) w.w[i] = 0u;
       if (there >> t & 1u) {
         const uint32_t from = at + t * place + ((taken[t] + (unsigned)r * (unsigned)stride[t]) & 15u) + threadIdx.x * ES;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-          if (Un::have(u, H, half)) {
-            const uint32_t v = lds_one<ES>(from + (2 * u + half) * blockDim.x * ES);
-            if constexpr (ES == 2) w.w[0] |= v << (16 * half);
-            else w.w[half] = v;
+        for (int e = 0; e < 2; ++e)
+          if (un.inside(un.column(u, e))) {
+            const uint32_t v = lds_one<ES>(from + (2 * u + e) * blockDim.x * ES);
+            if constexpr (ES == 2) w.w[0] |= v << (16 * e);
+            else w.w[e] = v;
           }
       }
     }
     return w;
   }
-  template <int R> __device__ __forceinline__ void done() {   // the oldest R rows' places are free
+  template <int R> __device__ __forceinline__ void done(const Un& un) {   // the oldest R rows' places are free
     if (!VEC) group_sync<SOLE>();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       out += NT * place;
       if (out == end) out = mem;
-      fetch();
+      fetch(un);
     }
     if (!VEC) {
 #pragma unroll
@@ -305,17 +350,16 @@ template <int DT, bool VEC, int NU, int NT, int STAGES, bool SOLE> struct Ring {
   }
 };
 
-// x - mu where there is a column, 0 past the end (a pair's columns lie apart without vectors)
-template <int DT, bool VEC> __device__ __forceinline__ float2 centred(float2 x, float mu, int u, int64_t H) {
+// x - mu of a unit's pair p where there are columns, 0 outside the row
+template <class Un> __device__ __forceinline__ float2 centred(const Un& un, float2 x, float mu, int u, int p) {
   const float2 d = add2(x, make_float2(-mu, -mu));
-  if (VEC) return Unit<DT, VEC>::have(u, H) ? d : make_float2(0.f, 0.f);
-  return make_float2(Unit<DT, VEC>::have(u, H, 0) ? d.x : 0.f, Unit<DT, VEC>::have(u, H, 1) ? d.y : 0.f);
+  if (Un::VEC && !(un.part >> u & 1u)) return (un.have >> u & 1u) ? d : make_float2(0.f, 0.f);
+  return make_float2(un.inside(un.column(u, 2 * p)) ? d.x : 0.f, un.inside(un.column(u, 2 * p + 1)) ? d.y : 0.f);
 }
 
 // Mean (0 for RMS norm) and 1 / sqrt(mean of squares + eps) of R rows; squares are taken of x - mu.  get(r, u, f): unit u of row r.
-template <int DT, bool VEC, int NU, int R, bool FULL, class Get>
-__device__ __forceinline__ void row_stats(const BlockArgs& A, Get get, float (*sh)[kMaxValues][kMaxWarps], int& slot, float (&mean)[R], float (&rstd)[R]) {
-  using Un = Unit<DT, VEC>;
+template <class Un, int NU, int R, bool FULL, class Get>
+__device__ __forceinline__ void row_stats(const BlockArgs& A, const Un& un, Get get, float (*sh)[kMaxValues][kMaxWarps], int& slot, float (&mean)[R], float (&rstd)[R]) {
   const float inv_h = 1.f / (float)A.H;
   const bool center = FULL && !A.rms;
   float v[R];
@@ -347,7 +391,7 @@ __device__ __forceinline__ void row_stats(const BlockArgs& A, Get get, float (*s
       get(r, u, x);
 #pragma unroll
       for (int p = 0; p < Un::P; ++p) {
-        if (center) x[p] = centred<DT, VEC>(x[p], mean[r], u, A.H);
+        if (center) x[p] = centred(un, x[p], mean[r], u, p);
         t = fma2(x[p], x[p], t);
       }
     }
@@ -361,10 +405,10 @@ __device__ __forceinline__ void row_stats(const BlockArgs& A, Get get, float (*s
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 // R rows at a time.  FULL: layer norm, biases, a gate a token; without it those instructions and registers are left out.
-template <int DT, bool VEC, int NU, int R, int STAGES, bool FULL, int THREADS>
+template <int DT, int KIND, int NU, int R, int STAGES, bool FULL, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) block_fwd_kernel(BlockArgs A, int place) {
-  using Un = Unit<DT, VEC>;
-  constexpr int P = Un::P;
+  using Un = Unit<DT, KIND>;
+  constexpr int ES = Vec<DT>::ESIZE, P = Un::P;
   extern __shared__ uint4 places[];
   __shared__ float sh[2][kMaxValues][kMaxWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");        // launched as a programmatic dependent of whatever is before it
@@ -372,22 +416,24 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
   int slot = 0;
   const int64_t step = gridDim.x;
   const bool center = FULL && !A.rms, post = A.post_weight != nullptr;
-  Ring<DT, VEC, NU, 2, STAGES, true> in;
-  in.start({A.x, A.residual}, {A.ld_x, A.ld_residual}, blockIdx.x, step, A.T, A.H, places, place);
-  Out<DT, VEC> sum(A.sum, A.ld_sum, blockIdx.x, step), y(A.y, A.ld_y, blockIdx.x, step);
+  Un un;
+  un.template start<NU>((const char*)A.x + blockIdx.x * A.ld_x * ES, A.H);
+  Ring<DT, KIND, NU, 2, STAGES, true> in;
+  in.start(un, {A.x, A.residual}, {A.ld_x, A.ld_residual}, blockIdx.x, step, A.T, places, place);
+  Out<ES> sum(A.sum, A.ld_sum, blockIdx.x, step, un.first), y(A.y, A.ld_y, blockIdx.x, step, un.first);
   // s = residual + gt (xhat1 fw + fb),  y = xhat2 w2 + b2
   float2 fw[NU][P], fb[FULL ? NU : 1][P], w2[NU][P], b2[FULL ? NU : 1][P];
 #pragma unroll
   for (int u = 0; u < NU; ++u) {
     float2 g[P];
-    Un::params(A.post_weight, u, A.H, A.param_bf16, 1.f, fw[u]);
-    Un::params(A.gate, u, A.H, A.param_bf16, 1.f, g);
-    Un::params(A.weight, u, A.H, A.param_bf16, 1.f, w2[u]);
+    un.params(A.post_weight, u, A.param_bf16, 1.f, fw[u]);
+    un.params(A.gate, u, A.param_bf16, 1.f, g);
+    un.params(A.weight, u, A.param_bf16, 1.f, w2[u]);
 #pragma unroll
     for (int p = 0; p < P; ++p) g[p] = mul2(g[p], both(A.scale));
     if (FULL) {
-      Un::params(A.post_bias, u, A.H, A.param_bf16, 0.f, fb[u]);
-      Un::params(A.bias, u, A.H, A.param_bf16, 0.f, b2[u]);
+      un.params(A.post_bias, u, A.param_bf16, 0.f, fb[u]);
+      un.params(A.bias, u, A.param_bf16, 0.f, b2[u]);
     }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -403,13 +449,13 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
     for (int r = 0; r < R; ++r) {
       const uint32_t at = in.row(r);
 #pragma unroll
-      for (int u = 0; u < NU; ++u) rx[r][u] = in.get(at, 0, u, r);
+      for (int u = 0; u < NU; ++u) rx[r][u] = in.get(un, at, 0, u, r);
 #pragma unroll
-      for (int u = 0; u < NU; ++u) s[r][u] = in.get(at, 1, u, r);
+      for (int u = 0; u < NU; ++u) s[r][u] = in.get(un, at, 1, u, r);
     }
-    in.template done<R>();
+    in.template done<R>(un);
     if (post) {
-      row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { Un::unpack(rx[r][u], f); }, sh, slot, m1, r1);
+      row_stats<Un, NU, R, FULL>(A, un, [&](int r, int u, float2 (&f)[P]) { Un::unpack(rx[r][u], f); }, sh, slot, m1, r1);
     } else {
 #pragma unroll
       for (int r = 0; r < R; ++r) m1[r] = 0.f, r1[r] = 1.f;
@@ -431,14 +477,14 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
           o[p] = FULL ? fma2(fma2(x[p], fw[u][p], fb[u][p]), both(gt), o[p]) : fma2(x[p], fw[u][p], o[p]);
         }
         s[r][u] = Un::pack(o);
-        Un::store(sum.at + r * sum.stride, u, A.H, s[r][u]);
+        un.store(sum.at + r * sum.stride, u, s[r][u]);
       }
       if (threadIdx.x == 0 && post) {
         if (A.out_post_mean) A.out_post_mean[t] = m1[r];
         if (A.out_post_rstd) A.out_post_rstd[t] = r1[r];
       }
     }
-    row_stats<DT, VEC, NU, R, FULL>(A, [&](int r, int u, float2 (&f)[P]) { Un::unpack(s[r][u], f); }, sh, slot, m2, r2);
+    row_stats<Un, NU, R, FULL>(A, un, [&](int r, int u, float2 (&f)[P]) { Un::unpack(s[r][u], f); }, sh, slot, m2, r2);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t t = row + r * step;
@@ -453,7 +499,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
           x[p] = mul2(x[p], both(r2[r]));
           x[p] = FULL ? fma2(x[p], w2[u][p], b2[u][p]) : mul2(x[p], w2[u][p]);
         }
-        Un::store(y.at + r * y.stride, u, A.H, Un::pack(x));
+        un.store(y.at + r * y.stride, u, Un::pack(x));
       }
       if (threadIdx.x == 0) {
         if (A.out_mean) A.out_mean[t] = m2[r];
@@ -535,10 +581,10 @@ __global__ void __launch_bounds__(1024) block_fwd_wide_kernel(BlockArgs A) {
 // Lines of sums over rows: dw2, Q1 and, with FULL, db2 and Q0.
 constexpr int kMaxSums = 4;
 
-template <int DT, bool VEC, int NU, int R, int STAGES, bool POST, bool FULL>
+template <int DT, int KIND, int NU, int R, int STAGES, bool POST, bool FULL>
 __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) {
-  using Un = Unit<DT, VEC>;
-  constexpr int P = Un::P, N = FULL ? 4 : 2, V1 = FULL ? 2 * R : R, V2 = FULL ? 3 * R : R;
+  using Un = Unit<DT, KIND>;
+  constexpr int ES = Vec<DT>::ESIZE, P = Un::P, N = FULL ? 4 : 2, V1 = FULL ? 2 * R : R, V2 = FULL ? 3 * R : R;
   static_assert(V2 <= kMaxValues, "");
   extern __shared__ uint4 places[];
   __shared__ float sh[2][kMaxValues][kMaxWarps];
@@ -554,17 +600,19 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
       for (int p = 0; p < P; ++p) acc[n][u][p] = both(0.f);
   const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
-  Ring<DT, VEC, NU, 4, STAGES, false> in;
-  in.start({A.dy, A.sum, A.dsum, use_x ? A.x : nullptr}, {A.ld_dy, A.ld_sum, A.ld_dsum, A.ld_x}, first, step, A.T, A.H,
+  Un un;
+  un.template start<NU>((const char*)A.dy + first * A.ld_dy * ES, A.H);
+  Ring<DT, KIND, NU, 4, STAGES, false> in;
+  in.start(un, {A.dy, A.sum, A.dsum, use_x ? A.x : nullptr}, {A.ld_dy, A.ld_sum, A.ld_dsum, A.ld_x}, first, step, A.T,
            (char*)places + threadIdx.y * STAGES * 4 * place, place);
   float2 w2[NU][P], fw[NU][P], fb[FULL ? NU : 1][P];        // fw = a gc w1, fb = a gc b1
 #pragma unroll
   for (int u = 0; u < NU; ++u) {
     float2 g[P];
-    Un::params(A.weight, u, A.H, A.param_bf16, 1.f, w2[u]);
-    Un::params(POST ? A.post_weight : nullptr, u, A.H, A.param_bf16, 1.f, fw[u]);
-    Un::params(A.gate, u, A.H, A.param_bf16, 1.f, g);
-    if (FULL) Un::params(A.post_bias, u, A.H, A.param_bf16, 0.f, fb[u]);
+    un.params(A.weight, u, A.param_bf16, 1.f, w2[u]);
+    un.params(POST ? A.post_weight : nullptr, u, A.param_bf16, 1.f, fw[u]);
+    un.params(A.gate, u, A.param_bf16, 1.f, g);
+    if (FULL) un.params(A.post_bias, u, A.param_bf16, 0.f, fb[u]);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       g[p] = mul2(g[p], both(A.scale));
@@ -587,7 +635,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
     }
   };
   scalars(first);
-  Out<DT, VEC> dres(A.dresidual, A.ld_dresidual, first, step), dx(A.dx, A.ld_dx, first, step);
+  Out<ES> dres(A.dresidual, A.ld_dresidual, first, step, un.first), dx(A.dx, A.ld_dx, first, step, un.first);
   for (int64_t row = first; row < A.T; row += R * step) {
     float m1[R], r1[R], m2[R], r2[R], gt[R], v[V1], t[V2];
 #pragma unroll
@@ -599,11 +647,11 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
     for (int r = 0; r < R; ++r) {
       const uint32_t at = in.row(r);
 #pragma unroll
-      for (int u = 0; u < NU; ++u) rd[r][u] = in.get(at, 0, u, r), rs[r][u] = in.get(at, 1, u, r);
+      for (int u = 0; u < NU; ++u) rd[r][u] = in.get(un, at, 0, u, r), rs[r][u] = in.get(un, at, 1, u, r);
 #pragma unroll
-      for (int u = 0; u < NU; ++u) re[r][u] = in.get(at, 2, u, r), rx[r][u] = in.get(at, 3, u, r);
+      for (int u = 0; u < NU; ++u) re[r][u] = in.get(un, at, 2, u, r), rx[r][u] = in.get(un, at, 3, u, r);
     }
-    in.template done<R>();
+    in.template done<R>(un);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float2 v1 = both(0.f), v2 = v1;
@@ -664,7 +712,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
               acc[3][u][p] = add2(acc[3][u][p], gg);
             }
           }
-          Un::store(dres.at + r * dres.stride, u, A.H, Un::pack(gs[r][u]));
+          un.store(dres.at + r * dres.stride, u, Un::pack(gs[r][u]));
         }
       }
       t[r] = t1.x + t1.y;
@@ -699,7 +747,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
             o[p] = mul2(o[p], both(gt[r]));
           }
         }
-        Un::store(dx.at + r * dx.stride, u, A.H, Un::pack(o));
+        un.store(dx.at + r * dx.stride, u, Un::pack(o));
       }
     }
     dres.at += R * dres.stride;
@@ -721,8 +769,8 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
           for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              const int64_t c = VEC ? Un::column(u) + 2 * p + half : Un::column(u, half);
-              if (c < A.H) {
+              const int64_t c = un.column(u, 2 * p + half);
+              if (un.inside(c)) {
                 float sum = half ? acc[n][u][p].y : acc[n][u][p].x;
                 if (g > 0) sum += all[n * A.H + c];
                 to[n * A.H + c] = sum;
@@ -825,46 +873,51 @@ __global__ void __launch_bounds__(1024) block_lines_kernel(BlockArgs A, int line
 
 // Threads a row (a group), rows at a time and under way, groups a block.
 struct Plan {
-  bool vec, twice;         // twice: 16 elements a thread instead of 8
+  Kind kind;
+  int period;              // rows after which offsets to 16 bytes repeat
+  bool twice;              // 16 elements a thread instead of 8
   int rows, stages;        // rows 0: the kernels for any width
   int threads, groups, place, smem;
 };
 
-bool vectors(const BlockArgs& a, bool backward) {
+void kind_of(const BlockArgs& a, bool backward, Plan* p) {
   const int64_t es = a.dtype == JP_BF16 ? 2 : 4;
-  uintptr_t bits = (uintptr_t)a.x | (uintptr_t)a.sum | (uintptr_t)a.post_weight | (uintptr_t)a.post_bias | (uintptr_t)a.gate | (uintptr_t)a.weight | (uintptr_t)a.bias;
-  int64_t pitch = (a.x ? a.ld_x : 0) | a.ld_sum;
-  if (backward) {
-    bits |= (uintptr_t)a.dy | (uintptr_t)a.dsum | (uintptr_t)a.dx | (uintptr_t)a.dresidual;
-    pitch |= a.ld_dy | (a.dsum ? a.ld_dsum : 0) | a.ld_dx | a.ld_dresidual;
-  } else {
-    bits |= (uintptr_t)a.residual | (uintptr_t)a.y;
-    pitch |= a.ld_residual | a.ld_y;
+  const void* at[6] = {a.sum, a.x, backward ? a.dy : a.residual, backward ? a.dsum : a.y, a.dx, a.dresidual};
+  const int64_t ld[6] = {a.ld_sum, a.ld_x, backward ? a.ld_dy : a.ld_residual, backward ? a.ld_dsum : a.ld_y, a.ld_dx, a.ld_dresidual};
+  p->kind = a.H * es % 16 == 0 ? kAligned : kShared;
+  for (int i = 0; i < 6; ++i) {
+    if (!at[i]) continue;
+    if ((((uintptr_t)at[i] ^ (uintptr_t)a.sum) & 15) != 0 || (ld[i] - a.ld_sum) * es % 16 != 0) { p->kind = kElements; break; }
+    if (((uintptr_t)at[i] & 15) != 0 || ld[i] * es % 16 != 0) p->kind = kShared;
   }
-  return a.H * es % 16 == 0 && pitch * es % 16 == 0 && (bits & 15) == 0;
+  p->period = 1;
+  while (p->kind == kShared && a.ld_sum * es * p->period % 16 != 0) p->period *= 2;
 }
 
-constexpr int kShared = 225 * 1024;           // of an SM, for rows
+constexpr int kSharedBytes = 225 * 1024;      // of an SM, for rows
 constexpr int stages_of(int rows, bool twice, int dt) { return rows == 2 ? 6 : twice && dt == JP_F32 ? 1 : 3; }
 
-Plan plan_for(int64_t T, int64_t H, int dtype, bool vec, bool prefer_twice, int matrices, int most_threads, int sms) {
-  const int es = dtype == JP_BF16 ? 2 : 4;
+Plan plan_for(const BlockArgs& a, bool backward, bool one_row, int matrices, int most_threads, int sms) {
+  const int dtype = a.dtype, es = dtype == JP_BF16 ? 2 : 4, w = 16 / es;
+  const int64_t T = a.T;
   Plan p{};
-  p.vec = vec;
+  kind_of(a, backward, &p);
+  const bool vec = p.kind != kElements;
+  const int64_t H = p.kind == kShared ? (a.H + 2 * w - 2) / w * w : a.H;     // the columns that covering vectors have
   const int64_t per = (H + 7) / 8;
-  p.twice = per > most_threads || prefer_twice;
+  p.twice = per > most_threads;
   const int64_t threads = ((p.twice ? (H + 15) / 16 : per) + 31) / 32 * 32;
   if (threads > most_threads) return p;
   p.threads = (int)threads;
   p.groups = most_threads / p.threads;
   p.place = place_bytes(vec, p.threads, (p.twice ? 2 : 1) * es / 2, H, es);
   // two rows at a time where every group has several and their places fit
-  for (p.rows = p.twice || T < 4 * (int64_t)sms * p.groups ? 1 : 2; p.rows >= 1; --p.rows) {
+  for (p.rows = p.twice || one_row || T < 4 * (int64_t)sms * p.groups ? 1 : 2; p.rows >= 1; --p.rows) {
     p.stages = stages_of(p.rows, p.twice, dtype);
     p.smem = p.stages * matrices * p.place;
-    if ((int64_t)p.smem * p.groups <= kShared) return p;
+    if ((int64_t)p.smem * p.groups <= kSharedBytes) return p;
     if (p.rows == 1) {
-      p.groups = kShared / p.smem;
+      p.groups = kSharedBytes / p.smem;
       if (p.groups > 0) return p;
     }
   }
@@ -872,12 +925,21 @@ Plan plan_for(int64_t T, int64_t H, int dtype, bool vec, bool prefer_twice, int 
   return p;
 }
 
+// Blocks: one for each group's rows, or what fits the GPU; then a multiple of the period.
+int grid_for(int64_t T, const Plan& p, int groups_a_block, int64_t most) {
+  const int64_t each = (int64_t)groups_a_block * p.rows, need = (T + each - 1) / each;
+  if (need <= most && T <= need * groups_a_block) return (int)need;
+  int64_t g = need < most ? need : most;
+  while (g > 1 && g * groups_a_block % p.period != 0) --g;
+  return g * groups_a_block % p.period == 0 ? (int)g : p.period;
+}
+
 template <class... P, class... Q>
 cudaError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, int smem, cudaStream_t s, Q... args) {
   // (the limit belongs to the kernel on the device, for all threads of the host: always the same amount)
   cudaError_t e = cudaSuccess;
   if (smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-  if (e == cudaSuccess && smem > 40 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+  if (e == cudaSuccess && smem > 40 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
@@ -894,21 +956,20 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, int smem, cudaSt
 
 // Forward: a block a group, 1024 threads an SM.
 template <int DT, bool FULL> cudaError_t forward(const BlockArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a.T, a.H, a.dtype, vectors(a, false), false, 2, 1024, sms);
+  const Plan p = plan_for(a, false, false, 2, 1024, sms);
   if (p.rows == 0) {
     block_fwd_wide_kernel<DT><<<(unsigned)(a.T < sms ? a.T : sms), 1024, 0, s>>>(a);
     return cudaGetLastError();
   }
-  const int64_t most = (int64_t)sms * (p.groups < 24 ? p.groups : 24), need = (a.T + p.rows - 1) / p.rows;
-  const dim3 g((unsigned)(need < most ? need : most)), b(p.threads);
+  const dim3 g((unsigned)grid_for(a.T, p, 1, (int64_t)sms * (p.groups < 24 ? p.groups : 24))), b(p.threads);
   constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
-#define JP_FORWARD(VEC, NU, R, TWICE) (p.threads <= 256 ? launch(block_fwd_kernel<DT, VEC, NU, R, stages_of(R, TWICE, DT), FULL, 256>, g, b, p.smem, s, a, p.place) \
-                                       : p.threads <= 512 ? launch(block_fwd_kernel<DT, VEC, NU, R, stages_of(R, TWICE, DT), FULL, 512>, g, b, p.smem, s, a, p.place) \
-                                                          : launch(block_fwd_kernel<DT, VEC, NU, R, stages_of(R, TWICE, DT), FULL, 1024>, g, b, p.smem, s, a, p.place))
-#define JP_FORWARD_TWICE(VEC, NU) launch(block_fwd_kernel<DT, VEC, NU, 1, stages_of(1, true, DT), FULL, 1024>, g, b, p.smem, s, a, p.place)
-  if (p.twice) return p.vec ? JP_FORWARD_TWICE(true, 2 * V) : JP_FORWARD_TWICE(false, 2 * E);
-  if (p.rows == 2) return p.vec ? JP_FORWARD(true, V, 2, false) : JP_FORWARD(false, E, 2, false);
-  return p.vec ? JP_FORWARD(true, V, 1, false) : JP_FORWARD(false, E, 1, false);
+#define JP_FORWARD(KIND, NU, R, TWICE) (p.threads <= 256 ? launch(block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 256>, g, b, p.smem, s, a, p.place) \
+                                       : p.threads <= 512 ? launch(block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 512>, g, b, p.smem, s, a, p.place) \
+                                                          : launch(block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 1024>, g, b, p.smem, s, a, p.place))
+#define JP_FORWARD_TWICE(KIND, NU) launch(block_fwd_kernel<DT, KIND, NU, 1, stages_of(1, true, DT), FULL, 1024>, g, b, p.smem, s, a, p.place)
+  if (p.twice) return p.kind == kAligned ? JP_FORWARD_TWICE(kAligned, 2 * V) : p.kind == kShared ? JP_FORWARD_TWICE(kShared, 2 * V) : JP_FORWARD_TWICE(kElements, 2 * E);
+  if (p.rows == 2) return p.kind == kAligned ? JP_FORWARD(kAligned, V, 2, false) : p.kind == kShared ? JP_FORWARD(kShared, V, 2, false) : JP_FORWARD(kElements, E, 2, false);
+  return p.kind == kAligned ? JP_FORWARD(kAligned, V, 1, false) : p.kind == kShared ? JP_FORWARD(kShared, V, 1, false) : JP_FORWARD(kElements, E, 1, false);
 #undef JP_FORWARD
 #undef JP_FORWARD_TWICE
 }
@@ -918,10 +979,11 @@ template <int DT, bool POST, bool FULL> cudaError_t backward(const BlockArgs& a,
   constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
   const dim3 b(p.threads, p.groups);
   const int sums = p.groups > 1 ? (FULL ? 4 : 2) * (int)a.H * 4 : 0, rows = p.smem * p.groups, smem = rows > sums ? rows : sums;
-#define JP_BACKWARD(VEC, NU, R, TWICE) launch(block_bwd_kernel<DT, VEC, NU, R, stages_of(R, TWICE, DT), POST, FULL>, g, b, smem, s, a, p.place)
-  if (p.twice) return p.vec ? JP_BACKWARD(true, 2 * V, 1, true) : JP_BACKWARD(false, 2 * E, 1, true);
-  if (p.rows == 2) return p.vec ? JP_BACKWARD(true, V, 2, false) : JP_BACKWARD(false, E, 2, false);
-  return p.vec ? JP_BACKWARD(true, V, 1, false) : JP_BACKWARD(false, E, 1, false);
+#define JP_BACKWARD(KIND, NU, R, TWICE) launch(block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL>, g, b, smem, s, a, p.place)
+  if (p.twice) return p.kind == kAligned ? JP_BACKWARD(kAligned, 2 * V, 1, true) : p.kind == kShared ? JP_BACKWARD(kShared, 2 * V, 1, true) : JP_BACKWARD(kElements, 2 * E, 1, true);
+  if constexpr (!FULL)
+    if (p.rows == 2) return p.kind == kAligned ? JP_BACKWARD(kAligned, V, 2, false) : p.kind == kShared ? JP_BACKWARD(kShared, V, 2, false) : JP_BACKWARD(kElements, E, 2, false);
+  return p.kind == kAligned ? JP_BACKWARD(kAligned, V, 1, false) : p.kind == kShared ? JP_BACKWARD(kShared, V, 1, false) : JP_BACKWARD(kElements, E, 1, false);
 #undef JP_BACKWARD
 }
 template <int DT> cudaError_t backward(const BlockArgs& a, const Plan& p, int grid, bool full, cudaStream_t s) {
@@ -947,10 +1009,8 @@ cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms) {
 size_t block_workspace_bytes(int64_t T, int64_t H, int, int sms) { return (size_t)(T < sms ? T : sms) * kMaxSums * (size_t)H * sizeof(float); }
 
 cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms) {
-  const bool vec = vectors(a, true);
-  const Plan p = plan_for(a.T, a.H, a.dtype, vec, false, 4, 512, sms);
-  const int64_t need = p.rows ? (a.T + p.groups - 1) / p.groups : a.T;
-  const int grid = (int)(need < sms ? need : sms), n = p.rows == 0 || full(a, true) ? 4 : 2;
+  const Plan p = plan_for(a, true, full(a, true), 4, 512, sms);      // (FULL: two rows do not fit the registers)
+  const int grid = p.rows ? grid_for(a.T, p, p.groups, sms) : (int)(a.T < sms ? a.T : sms), n = p.rows == 0 || full(a, true) ? 4 : 2;
   const cudaError_t e = a.dtype == JP_BF16 ? backward<JP_BF16>(a, p, grid, n == 4, s) : backward<JP_F32>(a, p, grid, n == 4, s);
   if (e != cudaSuccess) return e;
   const unsigned y = a.post_weight || a.gate ? 2 : 1;
