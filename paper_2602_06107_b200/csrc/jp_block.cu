@@ -84,6 +84,31 @@ template <bool SOLE, int N> __device__ __forceinline__ void group_sums(float (&v
   for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, s, i * kLanes);
 }
 
+// Shared memory by its own addresses (32 bits, no generic loads).
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+template <int ES> __device__ __forceinline__ uint32_t lds_one(uint32_t at) {
+  uint32_t v;
+  if constexpr (ES == 2) {
+    uint16_t h;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at) : "memory");
+    v = h;
+  } else {
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  }
+  return v;
+}
+template <int ES> __device__ __forceinline__ void sts_one(uint32_t at, const char* from) {
+  if constexpr (ES == 2) asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(*(const volatile uint16_t*)from) : "memory");
+  else asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(*(const volatile uint32_t*)from) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t to, const char* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
 enum Kind { kAligned, kShared, kElements };                 // rows on 16 bytes; all matrices' rows at the same offsets to 16 bytes; neither
 
 // What a thread has of a row: NU units.  A unit is a 16-byte vector, or (kElements) two elements a group's width apart.
@@ -92,12 +117,12 @@ template <int DT, int KIND> struct Unit {
   static constexpr int W = VEC ? Vec<DT>::N : 1;            // consecutive elements
   static constexpr int E = VEC ? W : 2, P = E / 2;          // elements and pairs of a unit
   static constexpr int ES = Vec<DT>::ESIZE;
-  int64_t H;
+  int H;                                                    // (widths that fit the registers: far below 31 bits)
   int first;                                                // column of the first unit (kShared: of its vector, from -W + 1 on)
   unsigned have, part;                                      // bits: some of the unit's columns are in the row; not all of them
   // `row`: where a row of the group starts
   template <int NU> __device__ __forceinline__ void start(const void* row, int64_t H_) {
-    H = H_;
+    H = (int)H_;
     first = VEC ? (int)threadIdx.x * W - (KIND == kShared ? (int)((uintptr_t)row & 15) / ES : 0) : threadIdx.x;
     have = part = 0u;
 #pragma unroll
@@ -109,10 +134,9 @@ template <int DT, int KIND> struct Unit {
       part |= (n > 0 && n < E ? 1u : 0u) << u;
     }
   }
-  __device__ __forceinline__ int64_t column(int u, int e) const {
-    return VEC ? first + (int64_t)u * (int)blockDim.x * W + e : first + (2 * u + e) * (int64_t)blockDim.x;
-  }
-  __device__ __forceinline__ bool inside(int64_t c) const { return c >= 0 && c < H; }
+  __device__ __forceinline__ int column(int u, int e) const { return VEC ? first + u * (int)blockDim.x * W + e : first + (2 * u + e) * (int)blockDim.x; }
+  __device__ __forceinline__ bool inside(int c) const { return (unsigned)c < (unsigned)H; }
+  __device__ __forceinline__ bool inside(int u, int e) const { return KIND == kAligned ? (have >> u & 1u) != 0u : inside(column(u, e)); }
   // a unit in its type
   struct Raw { uint32_t w[VEC ? 4 : ES == 2 ? 1 : 2]; };
   __device__ static __forceinline__ void unpack(const Raw& r, float2 (&f)[P]) {
@@ -143,15 +167,18 @@ template <int DT, int KIND> struct Unit {
     }
     return r;
   }
-  // what belongs to other rows reads 0
-  __device__ __forceinline__ void mask(Raw& r, int u) const {
-    if (KIND == kShared && (part >> u & 1u)) {
+  // what belongs to other rows, in the places `at` of NT matrices, reads 0 from here on
+  template <int NT> __device__ __forceinline__ void mask(uint32_t at, int place, int u) const {
+    uint32_t keep[4];
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (!inside(column(u, e))) {
-          if (ES == 2) r.w[e / 2] &= (e & 1) ? 0xffffu : 0xffff0000u;
-          else r.w[e] = 0u;
-        }
+    for (int i = 0; i < 4; ++i) {
+      if (ES == 2) keep[i] = (inside(u, 2 * i) ? 0xffffu : 0u) | (inside(u, 2 * i + 1) ? 0xffff0000u : 0u);
+      else keep[i] = inside(u, i) ? 0xffffffffu : 0u;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t, at += place) {
+      const uint4 v = lds16(at);
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x & keep[0]), "r"(v.y & keep[1]), "r"(v.z & keep[2]), "r"(v.w & keep[3]) : "memory");
     }
   }
   // `at`: the thread's first unit of the row
@@ -160,18 +187,18 @@ template <int DT, int KIND> struct Unit {
       at += u * (int)blockDim.x * 16;
       if (KIND == kShared && (part >> u & 1u)) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (inside(column(u, e))) {
-            if constexpr (ES == 2) ((uint16_t*)at)[e] = (uint16_t)(r.w[e / 2] >> (16 * (e & 1)));
-            else ((uint32_t*)at)[e] = r.w[e];
-          }
+        for (int i = 0; i < 4; ++i) {
+          const bool lo = inside(u, ES == 2 ? 2 * i : i), hi = ES == 2 ? inside(u, 2 * i + 1) : lo;
+          if (lo && hi) ((uint32_t*)at)[i] = r.w[i];
+          else if (lo || hi) ((uint16_t*)at)[2 * i + hi] = (uint16_t)(r.w[i] >> (hi ? 16 : 0));
+        }
       } else if (have >> u & 1u) {
         stg_stream((uint4*)at, make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
       }
     } else {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        if (inside(column(u, e))) {
+        if (inside(u, e)) {
           char* const to = at + (2 * u + e) * (int)blockDim.x * ES;
           if constexpr (ES == 2) *(uint16_t*)to = (uint16_t)(r.w[0] >> (16 * e));
           else *(uint32_t*)to = r.w[e];
@@ -180,13 +207,24 @@ template <int DT, int KIND> struct Unit {
   }
   // parameters at the unit's columns; `none` where there are none, 0 outside the row
   __device__ __forceinline__ void params(const void* p, int u, bool bf16, float none, float2 (&f)[P]) const {
+    const char* const at = (const char*)p + (int64_t)column(u, 0) * (bf16 ? 2 : 4);
+    const int next = (VEC ? 1 : (int)blockDim.x) * (bf16 ? 2 : 4);
+    float v[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int64_t c = column(u, e);
-      const float v = !inside(c) ? 0.f : p ? param(p, c, bf16) : none;
-      if (e & 1) f[e / 2].y = v;
-      else f[e / 2].x = v;
+    for (int e = 0; e < E; ++e) v[e] = inside(u, e) ? none : 0.f;
+    if (p) {
+      if (bf16) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (inside(u, e)) v[e] = __uint_as_float((uint32_t)*(const uint16_t*)(at + e * next) << 16);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (inside(u, e)) v[e] = *(const float*)(at + e * next);
+      }
     }
+#pragma unroll
+    for (int q = 0; q < P; ++q) f[q] = make_float2(v[2 * q], v[2 * q + 1]);
   }
 };
 
@@ -203,31 +241,6 @@ template <int ES> struct Out {
       : at((char*)base + (first * ld + column) * ES), stride(step * ld * ES) {}
 };
 
-// Shared memory by its own addresses (32 bits, no generic loads).
-__device__ __forceinline__ uint4 lds16(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-  return v;
-}
-template <int ES> __device__ __forceinline__ uint32_t lds_one(uint32_t at) {
-  uint32_t v;
-  if constexpr (ES == 2) {
-    uint16_t h;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at) : "memory");
-    v = h;
-  } else {
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-  }
-  return v;
-}
-template <int ES> __device__ __forceinline__ void sts_one(uint32_t at, const char* from) {
-  if constexpr (ES == 2) asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(*(const volatile uint16_t*)from) : "memory");
-  else asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(*(const volatile uint32_t*)from) : "memory");
-}
-__device__ __forceinline__ void copy16(uint32_t to, const char* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-
 // The group's rows of NT matrices: row `first`, then every `step`-th, STAGES of them under way.
 template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
   using Un = Unit<DT, KIND>;
@@ -238,16 +251,16 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
   uint32_t mem, in, out, end;                               // places (VEC: the thread's own): all, to fill, the oldest row's
   int place;
   unsigned there;                                           // bits: there is such a matrix
-  // kShared, kElements: vectors that reach beyond the matrix, in its first and last row, are copied element by element
-  const char* first_byte[NT];
-  const char* last_byte[NT];
+  bool at_start, at_end;                                    // the next row is the matrices' first one; the group's last row is their last one
   unsigned taken[NT];                                       // kElements: low bits of the oldest row's address; a place begins at its row's offset to 16
-  __device__ __forceinline__ void copy(uint32_t to, const char* from, int t, const char* row, int64_t bytes) const {
-    if (from >= first_byte[t] && from + 16 <= last_byte[t]) {
-      copy16(to, from);
-    } else {
+  // 16 bytes of a row's covering vectors; those that reach beyond the matrix, in its first and last row, element by element
+  __device__ __forceinline__ void copy(uint32_t to, const char* from, const char* row, int bytes) const {
+    if ((at_start || (at_end && left == 1)) && (from < row || from + 16 > row + bytes)) {
+#pragma unroll 1
       for (int q = 0; q < 16; q += ES)
         if (from + q >= row && from + q < row + bytes) sts_one<ES>(to + q, from + q);
+    } else {
+      copy16(to, from);
     }
   }
   __device__ __forceinline__ void fetch(const Un& un) {
@@ -261,18 +274,19 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
             for (int u = 0; u < NU; ++u)
               if (un.have >> u & 1u) {
                 const char* const from = next[t] + u * (int)blockDim.x * 16;
-                if (KIND == kShared && (un.part >> u & 1u)) copy(to + u * blockDim.x * 16, from, t, next[t] - un.first * ES, un.H * ES);
+                if (KIND == kShared && (un.part >> u & 1u)) copy(to + u * blockDim.x * 16, from, next[t] - un.first * ES, un.H * ES);
                 else copy16(to + u * blockDim.x * 16, from);
               }
           } else {
             const char* const row = next[t];
-            const int skip = (int)((uintptr_t)row & 15), bytes = (int)(un.H * ES);
-            for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) copy(to + i, row - skip + i, t, row, bytes);
+            const int skip = (int)((uintptr_t)row & 15), bytes = un.H * ES;
+            for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) copy(to + i, row - skip + i, row, bytes);
           }
         }
 #pragma unroll
       for (int t = 0; t < NT; ++t) next[t] += stride[t];
       --left;
+      at_start = false;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     in += NT * place;
@@ -290,10 +304,10 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
       next[t] = (const char*)base[t] + (first * ld[t] + (VEC ? un.first : 0)) * ES;
       taken[t] = (unsigned)(uintptr_t)next[t];
       stride[t] = step * ld[t] * ES;
-      first_byte[t] = (const char*)base[t];
-      last_byte[t] = (const char*)base[t] + ((T - 1) * ld[t] + un.H) * ES;
     }
     left = first < T ? (T - first + step - 1) / step : 0;
+    at_start = KIND != kAligned && first == 0;
+    at_end = KIND != kAligned && left > 0 && first + (left - 1) * step == T - 1;
     if constexpr (VEC) {                                    // what is never fetched reads 0
       if (un.have != (1u << NU) - 1u || there != (1u << NT) - 1u || left < STAGES)
         for (uint32_t at = mem; at != end; at += place)
@@ -304,9 +318,16 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
 #pragma unroll 1
     for (int s = 0; s < STAGES; ++s) fetch(un);
   }
-  template <int R> __device__ __forceinline__ void wait() {   // for the oldest R rows
+  template <int R> __device__ __forceinline__ void wait(const Un& un) {   // for the oldest R rows
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - R) : "memory");
     if (!VEC) group_sync<SOLE>();
+    if (KIND == kShared && un.part != 0u) {                 // (a place is the thread's own)
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+          if (un.part >> u & 1u) un.template mask<NT>(row(r) + u * blockDim.x * 16, place, u);
+    }
   }
   __device__ __forceinline__ uint32_t row(int r) const {      // the r-th oldest row's places
     const uint32_t at = out + r * NT * place;
@@ -318,7 +339,6 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
     if constexpr (VEC) {
       const uint4 v = lds16(at + t * place + u * blockDim.x * 16);
       w.w[0] = v.x; w.w[1] = v.y; w.w[2] = v.z; w.w[3] = v.w;
-      un.mask(w, u);
     } else {
 #pragma unroll
       for (int i = 0; i < (int)(sizeof(w) / 4); ++i) w.w[i] = 0u;
@@ -326,7 +346,7 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
         const uint32_t from = at + t * place + ((taken[t] + (unsigned)r * (unsigned)stride[t]) & 15u) + threadIdx.x * ES;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          if (un.inside(un.column(u, e))) {
+          if (un.inside(u, e)) {
             const uint32_t v = lds_one<ES>(from + (2 * u + e) * blockDim.x * ES);
             if constexpr (ES == 2) w.w[0] |= v << (16 * e);
             else w.w[e] = v;
@@ -354,7 +374,7 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
 template <class Un> __device__ __forceinline__ float2 centred(const Un& un, float2 x, float mu, int u, int p) {
   const float2 d = add2(x, make_float2(-mu, -mu));
   if (Un::VEC && !(un.part >> u & 1u)) return (un.have >> u & 1u) ? d : make_float2(0.f, 0.f);
-  return make_float2(un.inside(un.column(u, 2 * p)) ? d.x : 0.f, un.inside(un.column(u, 2 * p + 1)) ? d.y : 0.f);
+  return make_float2(un.inside(u, 2 * p) ? d.x : 0.f, un.inside(u, 2 * p + 1) ? d.y : 0.f);
 }
 
 // Mean (0 for RMS norm) and 1 / sqrt(mean of squares + eps) of R rows; squares are taken of x - mu.  get(r, u, f): unit u of row r.
@@ -443,7 +463,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
   }
   for (int64_t row = blockIdx.x; row < A.T; row += R * step) {
     float m1[R], r1[R], m2[R], r2[R];
-    in.template wait<R>();
+    in.template wait<R>(un);
     typename Un::Raw rx[R][NU], s[R][NU];                   // s: the residual, then the sum
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -585,6 +605,10 @@ template <int DT, int KIND, int NU, int R, int STAGES, bool POST, bool FULL>
 __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) {
   using Un = Unit<DT, KIND>;
   constexpr int ES = Vec<DT>::ESIZE, P = Un::P, N = FULL ? 4 : 2, V1 = FULL ? 2 * R : R, V2 = FULL ? 3 * R : R;
+  // Where they fit the registers, a row's values are held as they were stored from its first sum on and its places are free at once; else
+  // they are read again behind each sum.
+  constexpr bool HOLD = KIND == kAligned && !FULL && NU * Un::E == 8;
+  constexpr int HR = HOLD ? R : 1, HU = HOLD ? NU : 1;
   static_assert(V2 <= kMaxValues, "");
   extern __shared__ uint4 places[];
   __shared__ float sh[2][kMaxValues][kMaxWarps];
@@ -641,17 +665,21 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
     for (int r = 0; r < R; ++r) m1[r] = next[r][0], r1[r] = next[r][1], m2[r] = next[r][2], r2[r] = next[r][3], gt[r] = next[r][4];
     scalars(row + R * step);
-    in.template wait<R>();
-    typename Un::Raw rd[R][NU], rs[R][NU], re[R][NU], rx[R][NU];
+    in.template wait<R>(un);
+    typename Un::Raw held[4][HR][HU];
+    if constexpr (HOLD) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const uint32_t at = in.row(r);
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int u = 0; u < NU; ++u) rd[r][u] = in.get(un, at, 0, u, r), rs[r][u] = in.get(un, at, 1, u, r);
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int u = 0; u < NU; ++u) re[r][u] = in.get(un, at, 2, u, r), rx[r][u] = in.get(un, at, 3, u, r);
+          for (int t = 0; t < 4; ++t) held[t][r][u] = in.get(un, in.row(r), t, u, r);
+      in.template done<R>(un);
     }
-    in.template done<R>(un);
+    auto read = [&](int t, int r, int u, float2 (&f)[P]) {  // unit u of dy, sum, dsum or x
+      if constexpr (HOLD) Un::unpack(held[t][r][u], f);
+      else Un::unpack(in.get(un, in.row(r), t, u, r), f);
+    };
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float2 v1 = both(0.f), v2 = v1;
@@ -659,8 +687,8 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
           float2 d[P], s[P];
-          Un::unpack(rd[r][u], d);
-          Un::unpack(rs[r][u], s);
+          read(0, r, u, d);
+          read(1, r, u, s);
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             if (center) s[p] = add2(s[p], both(-m2[r]));
@@ -676,10 +704,12 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
       if (FULL) v[R + r] = v1.x + v1.y;
     }
     group_sums<false, V1>(v, sh, slot);
+    if constexpr (HOLD) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int u = 0; u < NU; ++u) Un::keep(rd[r][u]), Un::keep(rs[r][u]);
+        for (int u = 0; u < NU; ++u) Un::keep(held[0][r][u]), Un::keep(held[1][r][u]);
+    }
     // gs = r2 (dy w2 - a1 - xhat2 a2) + ds
     float2 gs[R][NU][P];
 #pragma unroll
@@ -691,10 +721,10 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
           float2 d[P], s[P], e[P], x[P];
-          Un::unpack(rd[r][u], d);
-          Un::unpack(rs[r][u], s);
-          Un::unpack(re[r][u], e);
-          Un::unpack(rx[r][u], x);
+          read(0, r, u, d);
+          read(1, r, u, s);
+          read(2, r, u, e);
+          read(3, r, u, x);
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             if (center) s[p] = add2(s[p], both(-m2[r]));
@@ -722,10 +752,12 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
       }
     }
     if (POST || token) group_sums<false, V2>(t, sh, slot);
+    if constexpr (HOLD) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int u = 0; u < NU; ++u) Un::keep(rx[r][u]);
+        for (int u = 0; u < NU; ++u) Un::keep(held[3][r][u]);
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t at = row + r * step;
@@ -736,7 +768,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         float2 o[P], x[P];
-        if (POST) Un::unpack(rx[r][u], x);
+        if (POST) read(3, r, u, x);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           o[p] = mul2(gs[r][u][p], fw[u][p]);
@@ -750,6 +782,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
         un.store(dx.at + r * dx.stride, u, Un::pack(o));
       }
     }
+    if constexpr (!HOLD) in.template done<R>(un);
     dres.at += R * dres.stride;
     dx.at += R * dx.stride;
   }
@@ -769,11 +802,11 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
           for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              const int64_t c = un.column(u, 2 * p + half);
-              if (un.inside(c)) {
+              const int c = n * un.H + un.column(u, 2 * p + half);
+              if (un.inside(u, 2 * p + half)) {
                 float sum = half ? acc[n][u][p].y : acc[n][u][p].x;
-                if (g > 0) sum += all[n * A.H + c];
-                to[n * A.H + c] = sum;
+                if (g > 0) sum += all[c];
+                to[c] = sum;
               }
             }
     }
@@ -981,7 +1014,7 @@ template <int DT, bool POST, bool FULL> cudaError_t backward(const BlockArgs& a,
   const int sums = p.groups > 1 ? (FULL ? 4 : 2) * (int)a.H * 4 : 0, rows = p.smem * p.groups, smem = rows > sums ? rows : sums;
 #define JP_BACKWARD(KIND, NU, R, TWICE) launch(block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL>, g, b, smem, s, a, p.place)
   if (p.twice) return p.kind == kAligned ? JP_BACKWARD(kAligned, 2 * V, 1, true) : p.kind == kShared ? JP_BACKWARD(kShared, 2 * V, 1, true) : JP_BACKWARD(kElements, 2 * E, 1, true);
-  if constexpr (!FULL)
+  if constexpr (!FULL || DT == JP_F32)
     if (p.rows == 2) return p.kind == kAligned ? JP_BACKWARD(kAligned, V, 2, false) : p.kind == kShared ? JP_BACKWARD(kShared, V, 2, false) : JP_BACKWARD(kElements, E, 2, false);
   return p.kind == kAligned ? JP_BACKWARD(kAligned, V, 1, false) : p.kind == kShared ? JP_BACKWARD(kShared, V, 1, false) : JP_BACKWARD(kElements, E, 1, false);
 #undef JP_BACKWARD
@@ -1009,7 +1042,7 @@ cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms) {
 size_t block_workspace_bytes(int64_t T, int64_t H, int, int sms) { return (size_t)(T < sms ? T : sms) * kMaxSums * (size_t)H * sizeof(float); }
 
 cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a, true, full(a, true), 4, 512, sms);      // (FULL: two rows do not fit the registers)
+  const Plan p = plan_for(a, true, a.dtype == JP_BF16 && full(a, true), 4, 512, sms);      // (8192 x 4096 layer norms with gates: one row at a time 140 us, two 167)
   const int grid = p.rows ? grid_for(a.T, p, p.groups, sms) : (int)(a.T < sms ? a.T : sms), n = p.rows == 0 || full(a, true) ? 4 : 2;
   const cudaError_t e = a.dtype == JP_BF16 ? backward<JP_BF16>(a, p, grid, n == 4, s) : backward<JP_F32>(a, p, grid, n == 4, s);
   if (e != cudaSuccess) return e;
