@@ -7,11 +7,16 @@
 //   preference  S = sum or mean of a sequence's lp, h = beta ((S - R)_chosen - (S - R)_rejected) - margin:
 //               L = mean over pairs of -(1 - e) log sigma(h) - e log sigma(-h),  k = +-(beta / P) (e sigma(h) - (1 - e) sigma(-h))
 //
-// Bound by HBM.  The policy loss has a row's k as soon as the row's sum is known, so sum and gradient are one launch: the row is read
-// twice, the second time from L2, and HBM sees one read and one write.  The preference loss needs both sequences of a pair first: a pass
-// for the sums, one for the gradients.  A row is shared by the blocks of a cluster; their (maximum, sum) pairs meet in shared memory.
+// Bound by HBM.  The policy loss has a row's k as soon as the row's sum is known, so sum and gradient are one launch, and the row stays in
+// shared memory in between, spread over the blocks of a cluster: HBM and L2 see one read and one write.  The preference loss needs both
+// sequences of a pair first: a pass for the sums, one for the gradients, each a stream through a ring of places.  Each thread copies its own
+// vectors (asynchronously, no barriers) and fetches the next row's into a place as soon as it has read it for the last time; two blocks
+// an SM, so that one loads and stores while the other waits for its sum.  One warp makes a row's scalars of the warps' sums.
+// Rows that no cluster can hold are read twice.
 // Sums of exponentials are fp32 of at most a few hundred terms a thread (in 2^x of z log2(e) / tau, relative to a running maximum), the row's
 // scalars fp64: the clip is a decision, and exp(d) - d - 1 cancels.
+#include <atomic>
+
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -49,45 +54,129 @@ template <int DT> __device__ __forceinline__ void store_one(void* row, int64_t i
   else ((float*)row)[i] = f;
 }
 
-// (maximum, sum of 2^(y - maximum)) of two parts
-__device__ __forceinline__ float2 merge(float2 a, float2 b) {
-  const float m = fmaxf(a.x, b.x);
-  return make_float2(m, a.y * ex2_approx(a.x - m) + b.y * ex2_approx(b.x - m));
+struct Shared {
+  float2 warp[2][kThreads / 32];              // by the parity of the row's number, like what follows
+  float2 part[2][kMaxCluster];                // of the cluster's blocks
+  unsigned long long arrived[2];              // barriers that count the parts' bytes
+  float top, k_over_s, coef;
+  int count[kThreads / 32];
+};
+constexpr long long kSpin = 4000000000ll;     // clock cycles after which a wait gives up
+
+// (maximum, sum) over a warp
+__device__ __forceinline__ float2 warp_merge(float2 v) {
+  float m = v.x;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float s = v.y * ex2_approx(v.x - m);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return make_float2(m, s);
 }
 
-struct Shared {
-  float2 warp[kThreads / 32];
-  float2 part[2][kMaxCluster];                // of the cluster's blocks, by the parity of the row's number
-  float k_over_s, coef;
-  int count[kThreads / 32];
-  double inv_n;
-};
-
-// The row's (maximum, sum) in all threads of all blocks of the cluster.
-__device__ __forceinline__ float2 cluster_total(Shared& sh, float2 v, int rank, int ranks, int& parity) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = merge(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
-  if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = sh.warp[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) v = merge(v, sh.warp[w]);
+// By one warp: the row's (maximum, sum) over the block's warps, then over the cluster's blocks, each of which sends its part to every other one's
+// shared memory (and gets the same total: the parts are merged in the same order).  A wait that gives up returns a sum below 0.
+__device__ __forceinline__ float2 row_total(Shared& sh, int rank, int ranks, int64_t count) {
+  const int p = (int)(count & 1), lane = threadIdx.x & 31;
+  float2 v = warp_merge(lane < kThreads / 32 ? sh.warp[p][lane] : make_float2(kFloor, 0.f));
   if (ranks == 1) return v;
-  if ((int)threadIdx.x < ranks) {             // to the place of this block in every block of the cluster
-    uint32_t to;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&sh.part[parity][rank])), "r"((uint32_t)threadIdx.x));
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.x), "f"(v.y) : "memory");
+  const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&sh.arrived[p]), at = (uint32_t)__cvta_generic_to_shared(&sh.part[p][rank]);
+  if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ranks * 8) : "memory");
+  if (lane < ranks) {
+    uint32_t to, theirs;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(at), "r"(lane));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(theirs) : "r"(bar), "r"(lane));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to), "f"(v.x), "f"(v.y), "r"(theirs) : "memory");
   }
-  // (the places of the next row are others, and nobody is two rows ahead: one barrier a row)
-  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-  v = sh.part[parity][0];
-  for (int r = 1; r < ranks; ++r) v = merge(v, sh.part[parity][r]);
-  parity ^= 1;
+  const uint32_t phase = (uint32_t)(count >> 1) & 1u;
+  long long t0 = 0;
+  for (uint32_t i = 0;; ++i) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 1000;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(phase) : "memory");
+    if (ok) break;
+    if ((i & 63u) == 0u) {
+      const long long now = clock64();
+      if (i == 0u) t0 = now;
+      else if (now - t0 > kSpin) return make_float2(0.f, -1.f);
+    }
+  }
+  v = warp_merge(lane < ranks ? sh.part[p][lane] : make_float2(kFloor, 0.f));
   return v;
 }
 
-template <int DT> __device__ __forceinline__ float2 row_sums(const char* z, int64_t v0, int64_t v1, int64_t tail0, int64_t V, float c) {
+// The largest of a vector's values (NaN aside)
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+  uint32_t m;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+  return m;
+}
+template <int DT> __device__ __forceinline__ float largest(uint4 v) {
+  if constexpr (DT == JP_BF16) {
+    const uint32_t m = max_pair(max_pair(v.x, v.y), max_pair(v.z, v.w));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  } else {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
+}
+// Values 2 q and 2 q + 1
+template <int DT> __device__ __forceinline__ float2 value_pair(uint4 v, int q) {
+  if constexpr (DT == JP_BF16) {
+    const uint32_t w = q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w;
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  } else {
+    return q == 0 ? make_float2(__uint_as_float(v.x), __uint_as_float(v.y)) : make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
+  }
+}
+// A vector's part of the running (maximum, sum); exponents and sums two at a time.
+template <int DT> __device__ __forceinline__ void add_vector(uint4 v, float c, float& m, float& s) {
   constexpr int W = Vec<DT>::N;
+  const float top = largest<DT>(v) * c;
+  if (top > m) {
+    s *= ex2_approx(m - top);
+    m = top;
+  }
+  float2 e[W / 2];
+#pragma unroll
+  for (int q = 0; q < W / 2; ++q) {
+    const float2 y = fma2(value_pair<DT>(v, q), make_float2(c, c), make_float2(-m, -m));
+    e[q] = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+  }
+#pragma unroll
+  for (int o = 1; o < W / 2; o *= 2)
+#pragma unroll
+    for (int q = 0; q + o < W / 2; q += 2 * o) e[q] = add2(e[q], e[q + o]);
+  s += e[0].x + e[0].y;
+}
+// The row's last elements, less than a vector
+template <int DT> __device__ __forceinline__ void add_tail(const char* z, int64_t i, float c, float& m, float& s) {
+  const float v = Vec<DT>::load_scalar(z, i), top = fmaxf(v * c, m);
+  s = s * ex2_approx(m - top) + ex2_approx(fmaf(v, c, -top));
+  m = top;
+}
+// Gradient of a vector, the i-th of the row: coef 1[v = x] - k 2^(z c - m), k = coef / s.  (The token's place is written once more: as an index into
+// the vector it would go through local memory.)
+template <int DT> __device__ __forceinline__ void put_gradient(char* dz, uint4 v, float c, float m, float k, float coef, int64_t i, int64_t x) {
+  constexpr int W = Vec<DT>::N;
+  auto at = [&](int q) {
+    const float2 y = fma2(value_pair<DT>(v, q), make_float2(c, c), make_float2(-m, -m));
+    return mul2(make_float2(ex2_approx(y.x), ex2_approx(y.y)), make_float2(-k, -k));
+  };
+  float g[W];
+#pragma unroll
+  for (int q = 0; q < W / 2; ++q) {
+    const float2 t = at(q);
+    g[2 * q] = t.x;
+    g[2 * q + 1] = t.y;
+  }
+  stg_stream((uint4*)dz + i, pack<DT>(g));
+  if (i == x / W) {
+    const float2 t = at((int)(x % W) / 2);
+    store_one<DT>(dz, x, coef + ((x & 1) ? t.y : t.x));
+  }
+}
+
+// A block's part of a row straight from memory, kUnroll vectors of a thread at a time.
+template <int DT> __device__ __forceinline__ float2 row_sums(const char* z, int64_t v0, int64_t v1, float c) {
   float m = kFloor, s = 0.f;
   for (int64_t i0 = v0; i0 < v1; i0 += kThreads * kUnroll) {
     uint4 v[kUnroll];
@@ -97,34 +186,11 @@ template <int DT> __device__ __forceinline__ float2 row_sums(const char* z, int6
       v[j] = i < v1 ? ld_row((const uint4*)z + i) : Vec<DT>::neg_inf();
     }
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      const float top = Vec<DT>::vmax(v[j]) * c;
-      if (top > m) {
-        s *= ex2_approx(m - top);
-        m = top;
-      }
-      float e[W];
-#pragma unroll
-      for (int q = 0; q < W; ++q) e[q] = ex2_approx(fmaf(Vec<DT>::get(v[j], q), c, -m));
-#pragma unroll
-      for (int o = 1; o < W; o *= 2)
-#pragma unroll
-        for (int q = 0; q + o < W; q += 2 * o) e[q] += e[q + o];
-      s += e[0];
-    }
-  }
-  if (tail0 + threadIdx.x < V) {              // the row's last elements, less than a vector
-    const float y = Vec<DT>::load_scalar(z, tail0 + threadIdx.x) * c, top = fmaxf(y, m);
-    s = s * ex2_approx(m - top) + ex2_approx(fmaf(Vec<DT>::load_scalar(z, tail0 + threadIdx.x), c, -top));
-    m = top;
+    for (int j = 0; j < kUnroll; ++j) add_vector<DT>(v[j], c, m, s);
   }
   return make_float2(m, s);
 }
-
-// Gradient of the block's part of a row: coef (1[v = x] - p_v), p_v = 2^(z c - m) / s, k = coef / s.
-template <int DT> __device__ __forceinline__ void row_gradient(const char* z, char* dz, int64_t v0, int64_t v1, int64_t tail0, int64_t V, float c,
-                                                               float m, float k, float coef, int64_t x) {
-  constexpr int W = Vec<DT>::N;
+template <int DT> __device__ __forceinline__ void row_gradient(const char* z, char* dz, int64_t v0, int64_t v1, float c, float m, float k, float coef, int64_t x) {
   for (int64_t i0 = v0; i0 < v1; i0 += kThreads * kUnroll) {
     uint4 v[kUnroll];
 #pragma unroll
@@ -135,19 +201,12 @@ template <int DT> __device__ __forceinline__ void row_gradient(const char* z, ch
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
       const int64_t i = i0 + j * kThreads + threadIdx.x;
-      if (i < v1) {
-        float g[W];
-#pragma unroll
-        for (int q = 0; q < W; ++q) {
-          g[q] = -k * ex2_approx(fmaf(Vec<DT>::get(v[j], q), c, -m));
-          if (i * W + q == x) g[q] += coef;
-        }
-        stg_stream((uint4*)dz + i, pack<DT>(g));
-      }
+      if (i < v1) put_gradient<DT>(dz, v[j], c, m, k, coef, i, x);
     }
   }
-  const int64_t t = tail0 + threadIdx.x;
-  if (t < V) store_one<DT>(dz, t, (t == x ? coef : 0.f) - k * ex2_approx(fmaf(Vec<DT>::load_scalar(z, t), c, -m)));
+}
+template <int DT> __device__ __forceinline__ void tail_gradient(const char* z, char* dz, int64_t t, float c, float m, float k, float coef, int64_t x) {
+  store_one<DT>(dz, t, (t == x ? coef : 0.f) - k * ex2_approx(fmaf(Vec<DT>::load_scalar(z, t), c, -m)));
 }
 
 template <int DT> __device__ __forceinline__ void row_zeros(char* dz, int64_t v0, int64_t v1, int64_t tail0, int64_t V) {
@@ -178,113 +237,259 @@ __device__ __forceinline__ double inverse_count(Shared& sh, const uint8_t* mask,
   return all > 0 ? 1.0 / (double)all : 0.0;
 }
 
-template <int DT, int MODE>
+// Until at most n groups of copies are under way; n is a constant where it is called (the instruction takes no other).
+__device__ __forceinline__ void wait_copies(int n) {
+  switch (n) {
+#define JP_WAIT(N) case N: asm volatile("cp.async.wait_group " #N ";" ::: "memory"); break;
+    JP_WAIT(1) JP_WAIT(2) JP_WAIT(3) JP_WAIT(4) JP_WAIT(5) JP_WAIT(6) JP_WAIT(7) JP_WAIT(8) JP_WAIT(9) JP_WAIT(10) JP_WAIT(11) JP_WAIT(12) JP_WAIT(13)
+#undef JP_WAIT
+    default: asm volatile("cp.async.wait_group 0;" ::: "memory");
+  }
+}
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+// A row's inputs beside its logits, read before its sum: their time covers the loads (and nobody has written the row yet).
+struct RowInputs { float zx, adv, old, ref, weight; };
+
+// What becomes of a row's (maximum, sum), by one warp: two of its lanes take the two exponentials at the same time.
+template <int MODE>
+__device__ __forceinline__ void row_scalars(const LossArgs& A, Shared& sh, int64_t row, bool writes, float2 t, const RowInputs& in, double inv_n) {
+  const int lane = threadIdx.x & 31;
+  const double none = __longlong_as_double(0x7ff8000000000000ll);
+  if (t.y < 0.f) {                            // the blocks' parts did not arrive: NaN in the loss and in the gradient
+    if (lane == 0) {
+      sh.coef = sh.k_over_s = (float)none;
+      if (MODE == kPrefSums) {
+        if (writes) A.row_lp[row] = none, A.row_used[row] = 1, A.row_sum[row] = t;
+      } else if (writes) {
+        A.term[row] = A.kl_term[row] = none;
+      }
+    }
+    return;
+  }
+  // in log2 first: c is log2(e) / tau in fp32, and so are m and the exponents behind the sum; c_to_nat takes its rounding back
+  const double lp = ((double)in.zx * (double)A.c - (double)t.x - log2((double)t.y)) * A.c_to_nat;
+  const bool usable = t.x > kFloor && t.x < 3.4e38f && t.y < 3.4e38f;        // (NaN and infinities end in the sum)
+  if (MODE == kPrefSums) {
+    const bool fine = usable && lp > -3.0e38;
+    if (writes && lane == 0) {
+      A.row_lp[row] = fine ? lp : 0.0;
+      A.row_used[row] = fine;
+      A.row_sum[row] = t;
+      if (A.out_logp) A.out_logp[row] = fine ? (float)lp : 0.f;
+      if (A.out_state) A.out_state[row] = fine ? 1 : 3;
+    }
+    return;
+  }
+  const double d = (double)in.ref - lp, e = exp(lane == 1 ? d : lp - (double)in.old);
+  const double r = usable ? __shfl_sync(0xffffffffu, e, 0) : none, e1 = __shfl_sync(0xffffffffu, e, 1) - 1.0;
+  const double a = in.adv, plain = -a * r;
+  double loss = plain, slope = plain, kl = 0.0;
+  bool live = true;
+  if (A.clip) {
+    const double clipped = -a * fmin(fmax(r, 1.0 - (double)A.eps_lo), 1.0 + (double)A.eps_hi);
+    live = !(plain < clipped);
+    if (!live) loss = clipped, slope = 0.0;
+  }
+  if (A.logp_ref) {                           // (e - 1 loses 2^-53: of k = d^2 / 2 what lp's own error loses sooner)
+    kl = e1 - d;
+    slope -= (double)A.kl_coef * e1;
+  }
+  const double wt = (double)in.weight * inv_n;
+  const float co = (float)(wt * slope * A.grad_scale);
+  const bool fine = isfinite(wt * loss) && isfinite((float)kl) && isfinite(co) && !isnan(r);
+  if (lane == 0) {
+    sh.coef = fine ? co : 0.f;
+    sh.k_over_s = fine ? co / t.y : 0.f;
+    if (writes) {
+      if (A.out_logp) A.out_logp[row] = fine ? (float)lp : 0.f;
+      if (A.out_kl) A.out_kl[row] = fine ? (float)kl : 0.f;
+      if (A.out_state) A.out_state[row] = fine ? (live ? 1 : 2) : 3;
+      A.term[row] = fine ? wt * loss : 0.0;
+      A.kl_term[row] = fine ? wt * kl : 0.0;
+    }
+  }
+}
+
+// A row that takes no part: what is written of it beside its gradient.
+template <int MODE> __device__ __forceinline__ void row_without(const LossArgs& A, int64_t row) {
+  if (MODE == kPrefGrad) return;
+  if (A.out_logp) A.out_logp[row] = 0.f;
+  if (A.out_state) A.out_state[row] = 0;
+  if (MODE == kPrefSums) {
+    A.row_lp[row] = 0.0;
+    A.row_used[row] = 0;
+  } else {
+    if (A.out_kl) A.out_kl[row] = 0.f;
+    A.term[row] = 0.0;
+    A.kl_term[row] = 0.0;
+  }
+}
+
+// kPolicy: NV vectors a thread hold a block's part of a row; NV = 0: any row, straight from memory, twice.
+// The others: a ring of NV vectors a thread; rows of any length, in whole turns of the ring.
+template <int DT, int MODE, int NV>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) loss_rows_kernel(LossArgs A) {
+  extern __shared__ uint4 places[];           // [NV][threads]: each thread its own
   __shared__ Shared sh;
   constexpr int W = Vec<DT>::N, ES = Vec<DT>::ESIZE;
+  constexpr bool STREAM = MODE != kPolicy, GRAD = MODE == kPolicy || MODE == kPrefGrad;
+  const int ranks = A.cluster, rank = blockIdx.x % ranks, clusters = gridDim.x / ranks;
+  if (ranks > 1) {
+    if (threadIdx.x < 2) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&sh.arrived[threadIdx.x])) : "memory");
+    if (threadIdx.x == 0) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int ranks = A.cluster, rank = blockIdx.x % ranks, clusters = gridDim.x / ranks;
   const int64_t vecs = A.V / W, each = (vecs + ranks - 1) / ranks;
   const int64_t v0 = each * rank < vecs ? each * rank : vecs, v1 = v0 + each < vecs ? v0 + each : vecs;
   const int64_t tail0 = rank == ranks - 1 ? vecs * W : A.V;       // the last block has what is left behind the vectors
+  const int64_t mine = v1 - v0 - threadIdx.x;                     // vector i is there if i * kThreads < mine
+  const int turns = NV > 0 ? (int)((v1 - v0 + NV * kThreads - 1) / (NV * kThreads > 0 ? NV * kThreads : 1)) : 0;       // of the ring, a row
+  const uint32_t place = (uint32_t)__cvta_generic_to_shared(places) + threadIdx.x * 16;
+  const int64_t first = (v0 + threadIdx.x) * 16;                  // bytes from a row's start to the thread's first vector
+  int64_t lo = 0, hi = A.T;
+  if (MODE == kPrefSums) {
+    lo = A.seq_start[0];
+    hi = A.seq_start[2 * A.P];
+  }
+  // the n-th row of all; gradients of pairs from the last row on: the end of the logits is what L2 still has from their sums
+  auto nth = [&](int64_t n) { return MODE == kPrefGrad ? A.T - 1 - n : n; };
+  // the token of the n-th row, -1 if it takes no part
+  auto token_of = [&](int64_t n) {
+    if (n >= A.T) return -1;
+    const int64_t row = nth(n);
+    int32_t x = A.tokens[row];
+    if (MODE == kPrefGrad) return A.row_coef[row] != 0.f ? x : -1;
+    if (A.mask != nullptr && A.mask[row] == 0) x = -1;
+    if (MODE == kPrefSums && (row < lo || row >= hi)) x = -1;
+    return x < A.V ? x : -1;
+  };
+  // vector i of the n-th row, or an empty group of copies
+  auto fetch = [&](int64_t n, int slot, int64_t i) {
+    if (n < A.T && i * kThreads < mine)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place + slot * kThreads * 16), "l"((const char*)A.z + nth(n) * A.ld * ES + first + i * (kThreads * 16)) : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // `next`: the next of this cluster's rows that takes part, with its token; `ahead`: the token of the row behind it, read a row's time before
+  // it is needed
+  int64_t n = blockIdx.x / ranks, next = n;
+  int32_t token, ahead = token_of(next);
+  auto advance = [&]() {
+    while (ahead < 0 && next < A.T) {
+      next += clusters;
+      ahead = token_of(next);
+    }
+    if (next > A.T) next = A.T;
+    token = ahead;
+    ahead = token_of(next + clusters);
+  };
+  advance();
+#pragma unroll
+  for (int i = 0; i < NV; ++i) fetch(next, i, i);
   const double inv_n = MODE == kPolicy || MODE == kPolicyNoGrad ? inverse_count(sh, A.mask, A.T, A.n_valid) : 0.0;
-  int parity = 0;
-  for (int64_t n = blockIdx.x / ranks; n < A.T; n += clusters) {
-    // (gradients of pairs from the last row on: the end of the logits is what L2 still has from their sums)
-    const int64_t row = MODE == kPrefGrad ? A.T - 1 - n : n;
+  for (int64_t count = 0;; ++count) {
+    for (; n < next; n += clusters) {         // rows that take no part
+      if (threadIdx.x == 0 && rank == 0) row_without<MODE>(A, nth(n));
+      if (GRAD) row_zeros<DT>((char*)A.dz + nth(n) * A.ld_d * ES, v0, v1, tail0, A.V);
+    }
+    if (next >= A.T) break;
+    const int64_t row = nth(next), x = token;
+    next += clusters;
+    advance();
     const char* z = (const char*)A.z + row * A.ld * ES;
     char* dz = (char*)A.dz + row * A.ld_d * ES;
-    const int64_t x = A.tokens[row];
-    bool on = (A.mask == nullptr || A.mask[row] != 0) && x >= 0 && x < A.V;
     float m = 0.f, k = 0.f, coef = 0.f;
     if (MODE == kPrefGrad) {
       coef = A.row_coef[row];
-      if (coef != 0.f) {
-        const float2 r = A.row_sum[row];
-        m = r.x;
-        k = coef / r.y;
-      }
+      const float2 r = A.row_sum[row];
+      m = r.x;
+      k = coef / r.y;
     } else {
-      if (MODE == kPrefSums) on = on && row >= A.seq_start[0] && row < A.seq_start[2 * A.P];
-      if (!on) {
-        if (threadIdx.x == 0 && rank == 0) {
-          if (A.out_logp) A.out_logp[row] = 0.f;
-          if (A.out_state) A.out_state[row] = 0;
-          if (MODE == kPrefSums) A.row_lp[row] = 0.0, A.row_used[row] = 0;
-          else {
-            if (A.out_kl) A.out_kl[row] = 0.f;
-            A.term[row] = 0.0;
-            A.kl_term[row] = 0.0;
-          }
-        }
-      } else {
-        float zx = 0.f, adv = 0.f, old = 0.f, ref = 0.f, weight = 1.f;
-        if (threadIdx.x == 0) {               // (read before the sums: their time covers the loads; nobody has written the row yet)
-          zx = Vec<DT>::load_scalar(z, x);
-          if (MODE != kPrefSums) {
-            adv = A.advantages[row];
-            old = A.logp_old[row];
-            if (A.logp_ref) ref = A.logp_ref[row];
-            if (A.token_weight) weight = A.token_weight[row];
-          }
-        }
-        const float2 t = cluster_total(sh, row_sums<DT>(z, v0, v1, tail0, A.V, A.c), rank, ranks, parity);
-        m = t.x;
-        if (threadIdx.x == 0) {
-          // in log2 first: c is log2(e) / tau in fp32, and so are m and the exponents behind the sum; c_to_nat takes its rounding back
-          const double lp = ((double)zx * (double)A.c - (double)t.x - log2((double)t.y)) * A.c_to_nat;
-          const bool usable = t.x > kFloor && t.x < 3.4e38f && t.y < 3.4e38f;        // (NaN and infinities end in the sum)
-          const double none = __longlong_as_double(0x7ff8000000000000ll);
-          if (MODE == kPrefSums) {
-            const bool fine = usable && lp > -3.0e38;
-            if (rank == 0) {
-              A.row_lp[row] = fine ? lp : 0.0;
-              A.row_used[row] = fine;
-              A.row_sum[row] = t;
-              if (A.out_logp) A.out_logp[row] = fine ? (float)lp : 0.f;
-              if (A.out_state) A.out_state[row] = fine ? 1 : 3;
-            }
-          } else {
-            const double a = adv, r = usable ? exp(lp - (double)old) : none, plain = -a * r;
-            double loss = plain, slope = plain, kl = 0.0;
-            bool live = true;
-            if (A.clip) {
-              const double clipped = -a * fmin(fmax(r, 1.0 - (double)A.eps_lo), 1.0 + (double)A.eps_hi);
-              live = !(plain < clipped);
-              if (!live) loss = clipped, slope = 0.0;
-            }
-            if (A.logp_ref) {
-              const double d = (double)ref - lp, e1 = expm1(d);
-              kl = e1 - d;
-              slope -= (double)A.kl_coef * e1;
-            }
-            const double wt = (double)weight * inv_n;
-            const float co = (float)(wt * slope * A.grad_scale);
-            const bool fine = isfinite(wt * loss) && isfinite((float)kl) && isfinite(co) && !isnan(r);
-            sh.coef = fine ? co : 0.f;
-            sh.k_over_s = fine ? co / t.y : 0.f;
-            if (rank == 0) {
-              if (A.out_logp) A.out_logp[row] = fine ? (float)lp : 0.f;
-              if (A.out_kl) A.out_kl[row] = fine ? (float)kl : 0.f;
-              if (A.out_state) A.out_state[row] = fine ? (live ? 1 : 2) : 3;
-              A.term[row] = fine ? wt * loss : 0.0;
-              A.kl_term[row] = fine ? wt * kl : 0.0;
-            }
-          }
-        }
-        if (MODE == kPolicy) {
-          __syncthreads();
-          coef = sh.coef;
-          k = sh.k_over_s;
+      RowInputs in{0.f, 0.f, 0.f, 0.f, 1.f};
+      if (threadIdx.x < 32) {
+        in.zx = Vec<DT>::load_scalar(z, x);
+        if (MODE != kPrefSums) {
+          in.adv = A.advantages[row];
+          in.old = A.logp_old[row];
+          if (A.logp_ref) in.ref = A.logp_ref[row];
+          if (A.token_weight) in.weight = A.token_weight[row];
         }
       }
+      float top = kFloor, sum = 0.f;
+      if constexpr (NV == 0) {
+        const float2 t = row_sums<DT>(z, v0, v1, A.c);
+        top = t.x;
+        sum = t.y;
+      } else {
+        for (int turn = 0; turn < (STREAM ? turns : 1); ++turn) {
+#pragma unroll
+          for (int u = 0; u < NV; ++u) {
+            const int64_t i = turn * NV + u;
+            wait_copies(STREAM ? NV - 1 : NV - 1 - u);
+            uint4 v;
+            const bool have = i * kThreads < mine;
+            if (have) v = lds16(place + u * kThreads * 16);
+            if (STREAM) {
+              if (turn + 1 < turns) fetch(n, u, i + NV);
+              else fetch(next, u, u);
+            }
+            if (have) add_vector<DT>(v, A.c, top, sum);
+          }
+        }
+      }
+      if (tail0 + threadIdx.x < A.V) add_tail<DT>(z, tail0 + threadIdx.x, A.c, top, sum);
+      const float2 t = warp_merge(make_float2(top, sum));
+      if ((threadIdx.x & 31) == 0) sh.warp[count & 1][threadIdx.x >> 5] = t;
+      __syncthreads();
+      if (threadIdx.x < 32) {                 // (without a gradient the others go on with the next row)
+        // the token's logit has arrived before the other blocks hear of this one: they may write the gradient over it
+        if (MODE == kPolicy) asm volatile("{.reg .f32 t;\n\tmov.f32 t, %0;}" ::"f"(in.zx) : "memory");
+        const float2 all = row_total(sh, rank, ranks, count);
+        if (MODE == kPolicy && threadIdx.x == 0) sh.top = all.x;
+        row_scalars<MODE>(A, sh, row, rank == 0, all, in, inv_n);
+      }
+      if (MODE == kPolicy) {
+        __syncthreads();
+        m = sh.top;
+        coef = sh.coef;
+        k = sh.k_over_s;
+      }
     }
-    if (MODE == kPolicy || MODE == kPrefGrad) {
-      if (coef != 0.f) row_gradient<DT>(z, dz, v0, v1, tail0, A.V, A.c, m, k, coef, x);
-      else row_zeros<DT>(dz, v0, v1, tail0, A.V);
+    if (GRAD) {
+      if constexpr (NV == 0) {
+        if (coef != 0.f) row_gradient<DT>(z, dz, v0, v1, A.c, m, k, coef, x);
+        else row_zeros<DT>(dz, v0, v1, A.V, A.V);
+      } else {
+        for (int turn = 0; turn < (STREAM ? turns : 1); ++turn) {
+#pragma unroll
+          for (int u = 0; u < NV; ++u) {
+            const int64_t i = turn * NV + u;
+            if (STREAM) wait_copies(NV - 1);
+            uint4 v;
+            const bool have = i * kThreads < mine;
+            if (have) v = lds16(place + u * kThreads * 16);
+            if (STREAM && turn + 1 < turns) fetch(n, u, i + NV);
+            else fetch(next, u, u);
+            if (have) {
+              const int64_t at = v0 + threadIdx.x + i * kThreads;
+              if (coef != 0.f) put_gradient<DT>(dz, v, A.c, m, k, coef, at, x);
+              else stg_stream((uint4*)dz + at, make_uint4(0u, 0u, 0u, 0u));
+            }
+          }
+        }
+      }
+      if (tail0 + threadIdx.x < A.V) {
+        if (coef != 0.f) tail_gradient<DT>(z, dz, tail0 + threadIdx.x, A.c, m, k, coef, x);
+        else store_one<DT>(dz, tail0 + threadIdx.x, 0.f);
+      }
     }
-    if (MODE != kPrefGrad && on) __syncthreads();           // (the next row writes what this one reads of sh)
+    n += clusters;
   }
 }
 
@@ -381,11 +586,14 @@ __global__ void __launch_bounds__(1024) preference_pairs_kernel(LossArgs A) {
   }
 }
 
+constexpr int kMostVectors = 14;              // a thread: 112 KB a block, two blocks an SM
+
 template <class K>
-cudaError_t launch(K kernel, const LossArgs& a, unsigned grid, unsigned threads, int cluster, cudaStream_t s) {
+cudaError_t launch(K kernel, const LossArgs& a, unsigned grid, unsigned threads, int cluster, int smem, cudaStream_t s) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -398,16 +606,65 @@ cudaError_t launch(K kernel, const LossArgs& a, unsigned grid, unsigned threads,
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <int MODE> cudaError_t rows(LossArgs a, cudaStream_t s, int sms) {
-  // Blocks that share a row: enough that all SMs have work where rows are few, and that the rows in flight (48 MB of logits) stay in L2
-  // until they are read again; not more than leave every thread a vector.
-  const int64_t bytes = a.V * (a.dtype == JP_BF16 ? 2 : 4), blocks = (int64_t)sms * kBlocksPerSm;
+// Clusters of c blocks that the GPU holds at once (fewer than its SMs would, where c does not divide what shares their memory); asked once for
+// each kernel and size, since the answer is always the same.
+template <auto kernel> int clusters_at_once(int c, int smem, int sms) {
+  static std::atomic<int> known[kMaxCluster + 1];
+  if (c == 1) return sms * kBlocksPerSm;
+  int n = known[c].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(sms * kBlocksPerSm / c * c));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = c;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return sms * kBlocksPerSm / c;
+  }
+  known[c].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+template <int NV, int DT, int MODE> cudaError_t rows_of(const LossArgs& a, cudaStream_t s, int sms) {
+  constexpr auto kernel = loss_rows_kernel<DT, MODE, NV>;
+  constexpr int smem = NV * kThreads * 16;
+  if (smem > 0) {                             // (always the same limit: it belongs to the kernel on the device, for all threads of the host)
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e != cudaSuccess) return e;
+  }
+  const int64_t most = clusters_at_once<kernel>(a.cluster, smem, sms), clusters = most < a.T ? most : a.T;
+  return launch(kernel, a, (unsigned)(clusters * a.cluster), kThreads, a.cluster, smem, s);
+}
+
+template <int DT, int MODE> cudaError_t rows(LossArgs a, cudaStream_t s, int sms) {
+  // Blocks that share a row: enough that all SMs have work where rows are few, and (policy loss with its gradient) that the row fits
+  // their shared memory; not more than leave every thread a vector.
+  const int64_t vecs = (a.V + Vec<DT>::N - 1) / Vec<DT>::N, blocks = (int64_t)sms * kBlocksPerSm;
   int c = 1;
-  while (c < kMaxCluster && (a.T * c * 2 <= blocks || blocks / c * bytes > (48 << 20)) && bytes / (2 * c) >= 8 * 1024) c *= 2;
+  while (c < kMaxCluster && (a.T * c * 2 <= blocks || (MODE == kPolicy && vecs > (int64_t)c * kThreads * kMostVectors)) && vecs >= 2 * c * kThreads) c *= 2;
   a.cluster = c;
-  const int64_t clusters = blocks / c < a.T ? blocks / c : a.T;
-  if (a.dtype == JP_BF16) return launch(loss_rows_kernel<JP_BF16, MODE>, a, (unsigned)(clusters * c), kThreads, c, s);
-  return launch(loss_rows_kernel<JP_F32, MODE>, a, (unsigned)(clusters * c), kThreads, c, s);
+  const int64_t per = (vecs + c - 1) / c;
+  if constexpr (MODE != kPolicy) {
+    return per <= 2 * kThreads ? rows_of<2, DT, MODE>(a, s, sms) : rows_of<8, DT, MODE>(a, s, sms);
+  } else {
+    if (per <= 1 * kThreads) return rows_of<1, DT, MODE>(a, s, sms);
+    if (per <= 2 * kThreads) return rows_of<2, DT, MODE>(a, s, sms);
+    if (per <= 4 * kThreads) return rows_of<4, DT, MODE>(a, s, sms);
+    if (per <= 7 * kThreads) return rows_of<7, DT, MODE>(a, s, sms);
+    if (per <= 10 * kThreads) return rows_of<10, DT, MODE>(a, s, sms);
+    if (per <= kMostVectors * kThreads) return rows_of<kMostVectors, DT, MODE>(a, s, sms);
+    return rows_of<0, DT, MODE>(a, s, sms);
+  }
+}
+template <int MODE> cudaError_t rows(const LossArgs& a, cudaStream_t s, int sms) {
+  return a.dtype == JP_BF16 ? rows<JP_BF16, MODE>(a, s, sms) : rows<JP_F32, MODE>(a, s, sms);
 }
 
 }  // namespace
@@ -422,7 +679,7 @@ cudaError_t launch_policy(LossArgs a, void* workspace, cudaStream_t s, int sms) 
   a.term = (double*)workspace;
   a.kl_term = (double*)((char*)workspace + up256((size_t)a.T * 8));
   const cudaError_t e = a.dz ? rows<kPolicy>(a, s, sms) : rows<kPolicyNoGrad>(a, s, sms);
-  return e != cudaSuccess ? e : launch(policy_sum_kernel, a, 1, 1024, 1, s);
+  return e != cudaSuccess ? e : launch(policy_sum_kernel, a, 1, 1024, 1, 0, s);
 }
 
 size_t preference_workspace_bytes(int64_t T, int64_t P) {
@@ -440,7 +697,7 @@ cudaError_t launch_preference(LossArgs a, void* workspace, cudaStream_t s, int s
   a.seq_per = (double*)take((size_t)a.P * 16);
   *n_launch = 0;
   cudaError_t e = rows<kPrefSums>(a, s, sms);
-  if (e == cudaSuccess) { *n_launch = 1; e = launch(preference_pairs_kernel, a, 1, 1024, 1, s); }
+  if (e == cudaSuccess) { *n_launch = 1; e = launch(preference_pairs_kernel, a, 1, 1024, 1, 0, s); }
   if (e == cudaSuccess) { *n_launch = 2; if (a.dz) e = rows<kPrefGrad>(a, s, sms); }
   if (e == cudaSuccess && a.dz) *n_launch = 3;
   return e;
