@@ -23,8 +23,7 @@
 namespace jp {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kBlocksPerSm = 2;
+constexpr int kMostThreads = 512;             // of a block; an SM has 1024, whatever the block
 constexpr int kMaxCluster = 8;
 constexpr int kUnroll = 4;
 constexpr float kFloor = -1.0e38f;            // below any row's maximum (in units of log2) that counts as one
@@ -55,11 +54,11 @@ template <int DT> __device__ __forceinline__ void store_one(void* row, int64_t i
 }
 
 struct Shared {
-  float2 warp[2][kThreads / 32];              // by the parity of the row's number, like what follows
+  float2 warp[2][kMostThreads / 32];              // by the parity of the row's number, like what follows
   float2 part[2][kMaxCluster];                // of the cluster's blocks
   unsigned long long arrived[2];              // barriers that count the parts' bytes
   float top, k_over_s, coef;
-  int count[kThreads / 32];
+  int count[kMostThreads / 32];
 };
 constexpr long long kSpin = 4000000000ll;     // clock cycles after which a wait gives up
 
@@ -78,7 +77,7 @@ __device__ __forceinline__ float2 warp_merge(float2 v) {
 // shared memory (and gets the same total: the parts are merged in the same order).  A wait that gives up returns a sum below 0.
 __device__ __forceinline__ float2 row_total(Shared& sh, int rank, int ranks, int64_t count) {
   const int p = (int)(count & 1), lane = threadIdx.x & 31;
-  float2 v = warp_merge(lane < kThreads / 32 ? sh.warp[p][lane] : make_float2(kFloor, 0.f));
+  float2 v = warp_merge(lane < (int)blockDim.x / 32 ? sh.warp[p][lane] : make_float2(kFloor, 0.f));
   if (ranks == 1) return v;
   const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&sh.arrived[p]), at = (uint32_t)__cvta_generic_to_shared(&sh.part[p][rank]);
   if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ranks * 8) : "memory");
@@ -178,11 +177,11 @@ template <int DT> __device__ __forceinline__ void put_gradient(char* dz, uint4 v
 // A block's part of a row straight from memory, kUnroll vectors of a thread at a time.
 template <int DT> __device__ __forceinline__ float2 row_sums(const char* z, int64_t v0, int64_t v1, float c) {
   float m = kFloor, s = 0.f;
-  for (int64_t i0 = v0; i0 < v1; i0 += kThreads * kUnroll) {
+  for (int64_t i0 = v0; i0 < v1; i0 += (int)blockDim.x * kUnroll) {
     uint4 v[kUnroll];
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
-      const int64_t i = i0 + j * kThreads + threadIdx.x;
+      const int64_t i = i0 + j * (int)blockDim.x + threadIdx.x;
       v[j] = i < v1 ? ld_row((const uint4*)z + i) : Vec<DT>::neg_inf();
     }
 #pragma unroll
@@ -191,16 +190,16 @@ template <int DT> __device__ __forceinline__ float2 row_sums(const char* z, int6
   return make_float2(m, s);
 }
 template <int DT> __device__ __forceinline__ void row_gradient(const char* z, char* dz, int64_t v0, int64_t v1, float c, float m, float k, float coef, int64_t x) {
-  for (int64_t i0 = v0; i0 < v1; i0 += kThreads * kUnroll) {
+  for (int64_t i0 = v0; i0 < v1; i0 += (int)blockDim.x * kUnroll) {
     uint4 v[kUnroll];
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
-      const int64_t i = i0 + j * kThreads + threadIdx.x;
+      const int64_t i = i0 + j * (int)blockDim.x + threadIdx.x;
       if (i < v1) v[j] = ld_row((const uint4*)z + i);
     }
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
-      const int64_t i = i0 + j * kThreads + threadIdx.x;
+      const int64_t i = i0 + j * (int)blockDim.x + threadIdx.x;
       if (i < v1) put_gradient<DT>(dz, v[j], c, m, k, coef, i, x);
     }
   }
@@ -210,7 +209,7 @@ template <int DT> __device__ __forceinline__ void tail_gradient(const char* z, c
 }
 
 template <int DT> __device__ __forceinline__ void row_zeros(char* dz, int64_t v0, int64_t v1, int64_t tail0, int64_t V) {
-  for (int64_t i = v0 + threadIdx.x; i < v1; i += kThreads) stg_stream((uint4*)dz + i, make_uint4(0u, 0u, 0u, 0u));
+  for (int64_t i = v0 + threadIdx.x; i < v1; i += (int)blockDim.x) stg_stream((uint4*)dz + i, make_uint4(0u, 0u, 0u, 0u));
   if (tail0 + threadIdx.x < V) store_one<DT>(dz, tail0 + threadIdx.x, 0.f);
 }
 
@@ -222,7 +221,7 @@ __device__ __forceinline__ double inverse_count(Shared& sh, const uint8_t* mask,
   const int64_t head = (16 - ((uintptr_t)mask & 15)) & 15;
   const int64_t first = head < T ? head : T, vecs = (T - first) / 16;
   const uint4* m = (const uint4*)(mask + first);
-  for (int64_t i = threadIdx.x; i < vecs; i += kThreads) {
+  for (int64_t i = threadIdx.x; i < vecs; i += (int)blockDim.x) {
     const uint4 v = m[i];
     n += __popc(__vcmpne4(v.x, 0u) & 0x01010101u) + __popc(__vcmpne4(v.y, 0u) & 0x01010101u) +
          __popc(__vcmpne4(v.z, 0u) & 0x01010101u) + __popc(__vcmpne4(v.w, 0u) & 0x01010101u);
@@ -233,7 +232,7 @@ __device__ __forceinline__ double inverse_count(Shared& sh, const uint8_t* mask,
   if ((threadIdx.x & 31) == 0) sh.count[threadIdx.x >> 5] = n;
   __syncthreads();
   int64_t all = 0;
-  for (int w = 0; w < kThreads / 32; ++w) all += sh.count[w];
+  for (int w = 0; w < (int)blockDim.x / 32; ++w) all += sh.count[w];
   return all > 0 ? 1.0 / (double)all : 0.0;
 }
 
@@ -332,8 +331,8 @@ template <int MODE> __device__ __forceinline__ void row_without(const LossArgs& 
 
 // kPolicy: NV vectors a thread hold a block's part of a row; NV = 0: any row, straight from memory, twice.
 // The others: a ring of NV vectors a thread; rows of any length, in whole turns of the ring.
-template <int DT, int MODE, int NV>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) loss_rows_kernel(LossArgs A) {
+template <int DT, int MODE, int NV, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(LossArgs A) {
   extern __shared__ uint4 places[];           // [NV][threads]: each thread its own
   __shared__ Shared sh;
   constexpr int W = Vec<DT>::N, ES = Vec<DT>::ESIZE;
@@ -608,13 +607,13 @@ cudaError_t launch(K kernel, const LossArgs& a, unsigned grid, unsigned threads,
 
 // Clusters of c blocks that the GPU holds at once (fewer than its SMs would, where c does not divide what shares their memory); asked once for
 // each kernel and size, since the answer is always the same.
-template <auto kernel> int clusters_at_once(int c, int smem, int sms) {
+template <auto kernel, int kThreads> int clusters_at_once(int c, int smem, int sms) {
   static std::atomic<int> known[kMaxCluster + 1];
-  if (c == 1) return sms * kBlocksPerSm;
+  if (c == 1) return sms * (1024 / kThreads);
   int n = known[c].load(std::memory_order_relaxed);
   if (n > 0) return n;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(sms * kBlocksPerSm / c * c));
+  cfg.gridDim = dim3((unsigned)(sms * (1024 / kThreads) / c * c));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cudaLaunchAttribute attr{};
@@ -625,42 +624,58 @@ template <auto kernel> int clusters_at_once(int c, int smem, int sms) {
   cfg.numAttrs = 1;
   if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
     cudaGetLastError();
-    return sms * kBlocksPerSm / c;
+    return sms * (1024 / kThreads) / c;
   }
   known[c].store(n, std::memory_order_relaxed);
   return n;
 }
 
-template <int NV, int DT, int MODE> cudaError_t rows_of(const LossArgs& a, cudaStream_t s, int sms) {
-  constexpr auto kernel = loss_rows_kernel<DT, MODE, NV>;
+template <int NV, int kThreads, int DT, int MODE> cudaError_t rows_of(const LossArgs& a, cudaStream_t s, int sms) {
+  constexpr auto kernel = loss_rows_kernel<DT, MODE, NV, kThreads>;
   constexpr int smem = NV * kThreads * 16;
   if (smem > 0) {                             // (always the same limit: it belongs to the kernel on the device, for all threads of the host)
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
   }
-  const int64_t most = clusters_at_once<kernel>(a.cluster, smem, sms), clusters = most < a.T ? most : a.T;
+  const int64_t most = clusters_at_once<kernel, kThreads>(a.cluster, smem, sms), clusters = most < a.T ? most : a.T;
   return launch(kernel, a, (unsigned)(clusters * a.cluster), kThreads, a.cluster, smem, s);
 }
 
-template <int DT, int MODE> cudaError_t rows(LossArgs a, cudaStream_t s, int sms) {
-  // Blocks that share a row: enough that all SMs have work where rows are few, and (policy loss with its gradient) that the row fits
-  // their shared memory; not more than leave every thread a vector.
-  const int64_t vecs = (a.V + Vec<DT>::N - 1) / Vec<DT>::N, blocks = (int64_t)sms * kBlocksPerSm;
+// Blocks that share a row: enough that all SMs have work where rows are few, and `most` vectors a thread (0: any number) hold it; not more than
+// leave every thread a vector.
+int cluster_for(int64_t T, int64_t vecs, int threads, int most, int sms) {
   int c = 1;
-  while (c < kMaxCluster && (a.T * c * 2 <= blocks || (MODE == kPolicy && vecs > (int64_t)c * kThreads * kMostVectors)) && vecs >= 2 * c * kThreads) c *= 2;
-  a.cluster = c;
-  const int64_t per = (vecs + c - 1) / c;
+  while (c < kMaxCluster && (T * c * 2 <= (int64_t)sms * (1024 / threads) || (most > 0 && vecs > (int64_t)c * threads * most)) && vecs >= 2 * c * threads) c *= 2;
+  return c;
+}
+
+template <int DT, int MODE, int kThreads> cudaError_t resident(LossArgs a, int64_t vecs, cudaStream_t s, int sms) {
+  const int64_t per = (vecs + a.cluster - 1) / a.cluster;
+  if constexpr (kThreads == 256) {            // (blocks of 512 start where those end)
+    if (per <= 1 * kThreads) return rows_of<1, kThreads, DT, MODE>(a, s, sms);
+    if (per <= 2 * kThreads) return rows_of<2, kThreads, DT, MODE>(a, s, sms);
+    if (per <= 4 * kThreads) return rows_of<4, kThreads, DT, MODE>(a, s, sms);
+    if (per <= 7 * kThreads) return rows_of<7, kThreads, DT, MODE>(a, s, sms);
+  }
+  if (per <= 10 * kThreads) return rows_of<10, kThreads, DT, MODE>(a, s, sms);
+  return rows_of<kMostVectors, kThreads, DT, MODE>(a, s, sms);
+}
+
+template <int DT, int MODE> cudaError_t rows(LossArgs a, cudaStream_t s, int sms) {
+  const int64_t vecs = (a.V + Vec<DT>::N - 1) / Vec<DT>::N;
   if constexpr (MODE != kPolicy) {
-    return per <= 2 * kThreads ? rows_of<2, DT, MODE>(a, s, sms) : rows_of<8, DT, MODE>(a, s, sms);
+    a.cluster = cluster_for(a.T, vecs, 512, 0, sms);
+    return vecs <= (int64_t)a.cluster * 2 * 512 ? rows_of<2, 512, DT, MODE>(a, s, sms) : rows_of<8, 512, DT, MODE>(a, s, sms);
   } else {
-    if (per <= 1 * kThreads) return rows_of<1, DT, MODE>(a, s, sms);
-    if (per <= 2 * kThreads) return rows_of<2, DT, MODE>(a, s, sms);
-    if (per <= 4 * kThreads) return rows_of<4, DT, MODE>(a, s, sms);
-    if (per <= 7 * kThreads) return rows_of<7, DT, MODE>(a, s, sms);
-    if (per <= 10 * kThreads) return rows_of<10, DT, MODE>(a, s, sms);
-    if (per <= kMostVectors * kThreads) return rows_of<kMostVectors, DT, MODE>(a, s, sms);
-    return rows_of<0, DT, MODE>(a, s, sms);
+    // four rows' blocks an SM where eight blocks of 256 threads hold a row, two where it takes eight of 512
+    if (vecs <= (int64_t)kMaxCluster * 256 * kMostVectors) {
+      a.cluster = cluster_for(a.T, vecs, 256, kMostVectors, sms);
+      return resident<DT, MODE, 256>(a, vecs, s, sms);
+    }
+    a.cluster = kMaxCluster;
+    if (vecs <= (int64_t)kMaxCluster * 512 * kMostVectors) return resident<DT, MODE, 512>(a, vecs, s, sms);
+    return rows_of<0, 512, DT, MODE>(a, s, sms);
   }
 }
 template <int MODE> cudaError_t rows(const LossArgs& a, cudaStream_t s, int sms) {
