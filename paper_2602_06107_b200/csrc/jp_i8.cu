@@ -9,8 +9,15 @@
 //   weights  [N / 128 tiles][K / 128 blocks][128 rows x 128 bytes], laid out once;  scales [N]
 //   tokens   [K / 128 blocks][M / 8 groups][8 rows x 128 bytes], written by the quantisation;  scales [M]
 // A CTA (one an SM): warp 0 copies, warp 1 issues the instructions into one of two accumulators in tensor memory, warps 2 to 5 scale and
-// store the other one.  Where the tiles do not fill the GPU, the CTAs of a cluster share a tile's K and add their integers through
-// distributed shared memory (any order gives the same bits).
+// store the other one.  Four forms, by what bounds the call (plan_for):
+//   kShare    few tiles: the CTAs of a cluster share a tile's K and add their integers through distributed shared memory (any order gives
+//             the same bits)
+//   kRowsEven up to 128 tokens, many channels: the weights' bytes decide.  Every CTA takes the same number of channels, in groups of 8 wherever they
+//             lie (an atom is one run of memory), for all tokens; whole tiles dealt to 148 SMs leave some with one more than the others.
+//             (151,936 x 2048, 48 tokens: 75 us with whole tiles)
+//   kTiles    tiles of 128 channels and up to 256 tokens one after the other
+//   kPairs    many tiles: two CTAs share a tile of 256 channels and up to 256 tokens (cta_group::2), each fetching its channels and half of the tokens:
+//             a third less to fetch, and six stages where four fit
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -86,8 +93,11 @@ template <bool BF16> __device__ __forceinline__ void put(void* out, int64_t i, f
   else ((float*)out)[i] = v;
 }
 
-template <bool BF16, bool SPLIT>
+enum Form { kShare, kRowsEven, kTiles };
+
+template <bool BF16, int FORM>
 __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
+  constexpr bool SPLIT = FORM == kShare;
   extern __shared__ unsigned char raw[];
   unsigned char* const ring = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   Control& sm = *(Control*)(ring + kRingBytes);
@@ -97,7 +107,16 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
   const int TN = A.tokens_tile, stages = A.stages, ranks = SPLIT ? A.split : 1;
   const uint32_t stage_bytes = kTileBytes + (uint32_t)TN * kBlock;
   const int k0 = SPLIT ? (int)(A.kblocks * rank / ranks) : 0, k1 = SPLIT ? (int)(A.kblocks * (rank + 1) / ranks) : (int)A.kblocks;
-  const int64_t first = blockIdx.x / ranks, step = gridDim.x / ranks;       // tiles of this CTA (with a split: one)
+  // tiles of this CTA: first, first + step .. below end (kShare: one), and the channels of them that are its own
+  int64_t first = blockIdx.x / ranks, step = gridDim.x / ranks, end = A.tiles, row0 = 0, row1 = A.N;
+  if (FORM == kRowsEven) {
+    const int64_t groups = (A.N + 7) / 8;
+    row0 = groups * blockIdx.x / gridDim.x * 8;
+    row1 = groups * (blockIdx.x + 1) / gridDim.x * 8;
+    first = row0 / kRows;
+    step = 1;
+    end = (row1 + kRows - 1) / kRows;
+  }
 
   if (tid == 0) {
     for (int s = 0; s < stages; ++s) { bar_init(&sm.full[s], 1); bar_init(&sm.empty[s], 1); }
@@ -121,33 +140,51 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
       // The weights do not depend on the quantisation in front of this kernel: with A.early their first stages are fetched before it is done.
       uint32_t armed = 0;
       bool ok = true, waited = false;
-      auto tokens = [&](int64_t tile, int kb, uint32_t s) {
-        const int64_t m0 = tile % A.tiles_m * TN, rows = A.padded_m - m0 < TN ? A.padded_m - m0 : TN;
-        copy(ring + s * stage_bytes + kTileBytes, A.xq + ((int64_t)kb * (A.padded_m / 8) + m0 / 8) * 1024, (uint32_t)rows * kBlock, &sm.full[s]);
+      // what the copies of a tile's stages have in common
+      const uint8_t* weights = nullptr;
+      const uint8_t* xq = nullptr;
+      uint32_t w_bytes = 0, w_at = 0, x_bytes = 0;
+      const int64_t x_step = A.padded_m / 8 * 1024;
+      auto enter = [&](int64_t tile) {
+        const int64_t m0 = tile % A.tiles_m * TN, rows = A.padded_m - m0 < TN ? A.padded_m - m0 : TN, n = tile / A.tiles_m;
+        uint32_t from = 0, to = kRows;         // channels of the tile
+        if (FORM == kRowsEven) {
+          from = n * kRows < row0 ? (uint32_t)(row0 - n * kRows) : 0u;
+          to = (n + 1) * kRows > row1 ? (uint32_t)(row1 - n * kRows) : (uint32_t)kRows;
+        }
+        w_at = from * kBlock;
+        w_bytes = (to - from) * kBlock;
+        x_bytes = (uint32_t)rows * kBlock;
+        weights = A.weights + (n * A.kblocks + k0) * kTileBytes + w_at;
+        xq = A.xq + k0 * x_step + m0 / 8 * 1024;
       };
-      auto arm = [&](int64_t tile, int kb, uint32_t s) {
-        const int64_t m0 = tile % A.tiles_m * TN, rows = A.padded_m - m0 < TN ? A.padded_m - m0 : TN;
-        bar_expect(&sm.full[s], kTileBytes + (uint32_t)rows * kBlock);
-        copy(ring + s * stage_bytes, A.weights + (tile / A.tiles_m * A.kblocks + kb) * kTileBytes, kTileBytes, &sm.full[s]);
+      auto arm = [&](int kb, uint32_t s) {
+        bar_expect(&sm.full[s], w_bytes + x_bytes);
+        copy(ring + s * stage_bytes + w_at, weights + (int64_t)(kb - k0) * kTileBytes, w_bytes, &sm.full[s]);
       };
-      if (A.early && first < A.tiles) {
+      auto tokens = [&](int kb, uint32_t s) { copy(ring + s * stage_bytes + kTileBytes, xq + (kb - k0) * x_step, x_bytes, &sm.full[s]); };
+      if (A.early && first < end) {
         const int n = k1 - k0 < stages ? k1 - k0 : stages;
-        for (int i = 0; i < n; ++i) arm(first, k0 + i, i);
+        enter(first);
+        for (int i = 0; i < n; ++i) arm(k0 + i, i);
         asm volatile("griddepcontrol.wait;" ::: "memory");
         waited = true;
-        for (int i = 0; i < n; ++i) tokens(first, k0 + i, i);
+        for (int i = 0; i < n; ++i) tokens(k0 + i, i);
         armed = n;
       }
       if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
-      uint32_t n = 0;                          // stages passed
-      for (int64_t tile = first; tile < A.tiles && ok; tile += step)
+      uint32_t n = 0, s = 0, use = 0;          // stages passed; the place of the next one, and how often it was used
+      for (int64_t tile = first; tile < end && ok; tile += step) {
+        enter(tile);
         for (int kb = k0; kb < k1; ++kb, ++n) {
-          if (n < armed) continue;
-          const uint32_t s = n % stages, use = n / stages;
-          if (!bar_wait(&sm.empty[s], (use & 1u) ^ 1u, &sm.abort)) { ok = false; break; }
-          arm(tile, kb, s);
-          tokens(tile, kb, s);
+          if (n >= armed) {
+            if (!bar_wait(&sm.empty[s], (use & 1u) ^ 1u, &sm.abort)) { ok = false; break; }
+            arm(kb, s);
+            tokens(kb, s);
+          }
+          if (++s == (uint32_t)stages) s = 0, ++use;
         }
+      }
       if (!ok) {                               // leave no copy in flight: wait (bounded) for the last one of every stage
         if (A.status) atomicExch(A.status, (int)JP_ERR_TIMEOUT);
         for (uint32_t i = n < (uint32_t)stages ? 0 : n - stages; i < n; ++i) {
@@ -162,16 +199,15 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
     if (lane == 0) {
       // int32 accumulator, signed 8-bit operands, both K-major, TN columns, 128 rows
       const uint32_t shape = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
-      uint32_t n = 0;
+      uint32_t s = 0, phase = 0;
       bool ok = true;
       int t = 0;
-      for (int64_t tile = first; tile < A.tiles && ok; tile += step, ++t) {
+      for (int64_t tile = first; tile < end && ok; tile += step, ++t) {
         const uint32_t buf = t & 1, use = t >> 1;
         if (!bar_wait(&sm.acc_empty[buf], (use & 1u) ^ 1u, &sm.abort)) { ok = false; break; }
         fence_after();
-        for (int kb = k0; kb < k1; ++kb, ++n) {
-          const uint32_t s = n % stages;
-          if (!bar_wait(&sm.full[s], (n / stages) & 1u, &sm.abort)) { ok = false; break; }
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!bar_wait(&sm.full[s], phase, &sm.abort)) { ok = false; break; }
           fence_after();
           const uint32_t at = s32(ring) + s * stage_bytes;
           const uint64_t a = operand(at), b = operand(at + kTileBytes);
@@ -179,6 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
           for (int q = 0; q < kBlock / 32; ++q)      // 32 bytes further inside the swizzled row: start address + 2
             mma_i8(tmem + buf * 256, a + q * 2, b + q * 2, shape, kb != k0 || q != 0);
           commit(&sm.empty[s]);
+          if (++s == (uint32_t)stages) s = 0, phase ^= 1u;
         }
         if (ok) commit(&sm.acc_full[buf]);
       }
@@ -190,11 +227,12 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
     const int row = q * 32 + lane;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     int t = 0;
-    for (int64_t tile = first; tile < A.tiles; tile += step, ++t) {
+    for (int64_t tile = first; tile < end; tile += step, ++t) {
       const uint32_t buf = t & 1, use = t >> 1;
       const int64_t m0 = tile % A.tiles_m * TN, n = tile / A.tiles_m * kRows + row;
       const int cols = (int)(A.M - m0 < TN ? A.M - m0 : TN);
-      const float sw = n < A.N ? A.weight_scales[n] : 0.f;
+      const bool mine = FORM == kRowsEven ? n >= row0 && n < row1 && n < A.N : n < A.N;
+      const float sw = mine ? A.weight_scales[n] : 0.f;
       if (!SPLIT) {
         __syncwarp();
         for (int c = lane; c < cols; c += 32) sm.sx[q][c] = __ldcg(A.token_scales + m0 + c);
@@ -213,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
         if (SPLIT) {                           // (the ring is free: all of its stages have been read)
 #pragma unroll
           for (int j = 0; j < 16; ++j) ((int*)ring)[(c0 + j) * kRows + row] = r[j];
-        } else if (n < A.N) {
+        } else if (mine) {
 #pragma unroll
           for (int j = 0; j < 16; ++j)
             if (c0 + j < cols) put<BF16>(A.out, (m0 + c0 + j) * A.ld_out + n, (float)r[j] * (sm.sx[q][c0 + j] * sw));
@@ -281,7 +319,6 @@ __global__ void __launch_bounds__(256) i8_pack_kernel(I8PackArgs A) {
 // to 254) away from one: the product with a rounded reciprocal (off by 2^-15 at most) picks the right integer, or one of the two of a
 // half, and the remainder of the product tells a half.  max is scaled to 1 .. 2 first, by a power of two, so that nothing overflows or leaves the normal numbers.
 constexpr int kQuantThreads = 256;
-constexpr int kHeld = 4;                       // chunks of 16 a thread keeps between the maximum and the rounding
 
 struct Chunk { uint4 a, b; };                  // 16 bf16
 __device__ __forceinline__ Chunk load_chunk(const I8QuantArgs& A, const char* row, int64_t k0) {
@@ -332,7 +369,9 @@ __device__ __forceinline__ uint4 quantized_chunk(const Chunk& c, float scale, fl
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-__global__ void __launch_bounds__(kQuantThreads) i8_quantize_kernel(I8QuantArgs A) {
+// kHeld: chunks of 16 a thread keeps between the maximum and the rounding; a row's others are read again.  (One, for rows of up to 4096, leaves
+// room for eight blocks an SM: 4096 x 4096 25 us with four.)
+template <int kHeld> __global__ void __launch_bounds__(kQuantThreads, kHeld == 1 ? 8 : 3) i8_quantize_kernel(I8QuantArgs A) {
   __shared__ uint32_t sh[kQuantThreads / 32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -376,19 +415,26 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Tokens a tile takes and CTAs that share a tile's K.  A tile of c tokens takes about c + 64 (its instructions, and the copy of its channels
 // beside them); the least rounds over the SMs times that, of the token counts that share M evenly.
-struct Plan { int tokens, split; int64_t tiles_m; };
+struct Plan { Form form; int tokens, split; int64_t tiles_m; };
 Plan plan_for(int64_t M, int64_t N, int64_t kblocks, int sms) {
   const int64_t tiles_n = (N + kRows - 1) / kRows, least = (M + 255) / 256;
   Plan p{};
+  p.split = 1;
+  if (M <= 128 && tiles_n > sms) {
+    p.form = kRowsEven;
+    p.tokens = (int)up(M, 16);
+    p.tiles_m = 1;
+    return p;
+  }
   double best = 0;
   for (int64_t tm = least; tm <= least * 3 && tm <= (M + 15) / 16; ++tm) {
     const int64_t c = up((M + tm - 1) / tm, 16), rounds = (tiles_n * tm + sms - 1) / sms;
     const double cost = (double)rounds * (double)(c + 64);
     if (p.tokens == 0 || cost < best) best = cost, p.tokens = (int)c, p.tiles_m = (M + c - 1) / c;
   }
-  p.split = 1;
   const int64_t tiles = tiles_n * p.tiles_m;
   while (p.split < 8 && tiles * p.split * 2 <= sms && kblocks >= p.split * 2) p.split *= 2;
+  p.form = p.split > 1 ? kShare : kTiles;
   return p;
 }
 
@@ -422,14 +468,14 @@ cudaError_t launch_i8_quantize(I8QuantArgs a, cudaStream_t s) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, i8_quantize_kernel, a);
+  return cudaLaunchKernelEx(&cfg, threads <= kQuantThreads ? i8_quantize_kernel<1> : i8_quantize_kernel<4>, a);
 }
 
-template <bool BF16, bool SPLIT> static cudaError_t launch_linear(const I8Args& a, cudaStream_t s, int sms) {
-  const cudaError_t e = cudaFuncSetAttribute(i8_linear_kernel<BF16, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+template <bool BF16, int FORM> static cudaError_t launch_linear(const I8Args& a, cudaStream_t s, int sms) {
+  const cudaError_t e = cudaFuncSetAttribute(i8_linear_kernel<BF16, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(SPLIT ? a.tiles * a.split : a.tiles < sms ? a.tiles : sms));
+  cfg.gridDim = dim3((unsigned)(FORM == kShare ? a.tiles * a.split : FORM == kRowsEven || a.tiles > sms ? sms : a.tiles));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSharedBytes;
   cfg.stream = s;
@@ -440,8 +486,8 @@ template <bool BF16, bool SPLIT> static cudaError_t launch_linear(const I8Args& 
   attr[1].val.clusterDim.x = (unsigned)a.split;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = SPLIT ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, i8_linear_kernel<BF16, SPLIT>, a);
+  cfg.numAttrs = FORM == kShare ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, i8_linear_kernel<BF16, FORM>, a);
 }
 
 cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, int64_t K, bool out_bf16, cudaStream_t s, int sms) {
@@ -459,8 +505,9 @@ cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, i
   a.weight_scales = (const float*)((const char*)packed + tiles_n * a.kblocks * kTileBytes);
   a.xq = (const uint8_t*)tokens;
   a.token_scales = (const float*)((const char*)tokens + a.padded_m * a.kblocks * kBlock);
-  if (out_bf16) return p.split > 1 ? launch_linear<true, true>(a, s, sms) : launch_linear<true, false>(a, s, sms);
-  return p.split > 1 ? launch_linear<false, true>(a, s, sms) : launch_linear<false, false>(a, s, sms);
+  if (p.form == kShare) return out_bf16 ? launch_linear<true, kShare>(a, s, sms) : launch_linear<false, kShare>(a, s, sms);
+  if (p.form == kRowsEven) return out_bf16 ? launch_linear<true, kRowsEven>(a, s, sms) : launch_linear<false, kRowsEven>(a, s, sms);
+  return out_bf16 ? launch_linear<true, kTiles>(a, s, sms) : launch_linear<false, kTiles>(a, s, sms);
 }
 
 }  // namespace jp
