@@ -8,7 +8,7 @@
 // with no tensor map and no edge cases:
 //   weights  [N / 128 tiles][K / 128 blocks][128 rows x 128 bytes], laid out once;  scales [N]
 //   tokens   [K / 128 blocks][M / 8 groups][8 rows x 128 bytes], written by the quantisation;  scales [M]
-// A CTA (one an SM): warp 0 copies, warp 1 issues the instructions into one of two accumulators in tensor memory, warps 2 to 5 scale and
+// A CTA (one an SM): warp 0 copies, warp 1 issues the instructions into one of two accumulators in tensor memory, warps 2 to 9 scale and
 // store the other one.  Four forms, by what bounds the call (plan_for):
 //   kShare    few tiles: the CTAs of a cluster share a tile's K and add their integers through distributed shared memory (any order gives
 //             the same bits)
@@ -27,14 +27,15 @@ namespace {
 constexpr int kRows = 128;                    // channels of a tile
 constexpr int kBlock = 128;                   // k of a stage: one row of the swizzle
 constexpr int kTileBytes = kRows * kBlock;
-constexpr int kThreads = 192;
+constexpr int kResultWarps = 8;               // two for each quarter of tensor memory's lanes, half of the tokens each
+constexpr int kThreads = 64 + 32 * kResultWarps;
 constexpr int kMaxStages = 12;
 constexpr int kRingBytes = 200 * 1024;
 constexpr long long kSpin = 4000000000ll;     // clock cycles after which a wait gives up
 
 struct Control {                              // behind the ring in shared memory
   unsigned long long full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2];
-  float sx[4][256];
+  float sx[kResultWarps][256];
   uint32_t tmem;
   int abort;
 };
@@ -81,11 +82,16 @@ __device__ __forceinline__ void commit(unsigned long long* bar) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory"); }
+// 16 columns of a warp's lanes: the load, and the wait for loads before their registers are used
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, int (&r)[16]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
                  "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait(int (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(r[i]));
 }
 
 template <bool BF16> __device__ __forceinline__ void put(void* out, int64_t i, float v) {
@@ -120,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
 
   if (tid == 0) {
     for (int s = 0; s < stages; ++s) { bar_init(&sm.full[s], 1); bar_init(&sm.empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { bar_init(&sm.acc_full[b], 1); bar_init(&sm.acc_empty[b], 4); }
+    for (int b = 0; b < 2; ++b) { bar_init(&sm.acc_full[b], 1); bar_init(&sm.acc_empty[b], kResultWarps); }
     sm.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -223,19 +229,22 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
     }
   } else {
     // ---- results: a thread has one channel, columns are tokens
-    const int q = warp & 3;                    // the quarter of tensor memory's lanes this warp may read
+    const int q = warp & 3, w = warp - 2;      // the quarter of tensor memory's lanes this warp may read
     const int row = q * 32 + lane;
+    constexpr int ES = BF16 ? 2 : 4;
+    // pairs of channels in one word, where words are aligned: two lanes swap halves of two tokens, and each stores one of them
+    const bool words = BF16 && ((uintptr_t)A.out & 3) == 0 && A.ld_out % 2 == 0 && A.N % 2 == 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     int t = 0;
     for (int64_t tile = first; tile < end; tile += step, ++t) {
       const uint32_t buf = t & 1, use = t >> 1;
       const int64_t m0 = tile % A.tiles_m * TN, n = tile / A.tiles_m * kRows + row;
-      const int cols = (int)(A.M - m0 < TN ? A.M - m0 : TN);
+      const int cols = (int)(A.M - m0 < TN ? A.M - m0 : TN), half = (cols + 31) / 32 * 16, c_first = w < 4 ? 0 : half, c_end = w < 4 ? (half < cols ? half : cols) : cols;
       const bool mine = FORM == kRowsEven ? n >= row0 && n < row1 && n < A.N : n < A.N;
       const float sw = mine ? A.weight_scales[n] : 0.f;
       if (!SPLIT) {
         __syncwarp();
-        for (int c = lane; c < cols; c += 32) sm.sx[q][c] = __ldcg(A.token_scales + m0 + c);
+        for (int c = c_first + lane; c < c_end; c += 32) sm.sx[w][c] = __ldcg(A.token_scales + m0 + c);
         __syncwarp();
       }
       if (!bar_wait(&sm.acc_full[buf], use & 1u, &sm.abort)) {
@@ -244,17 +253,37 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
       }
       fence_after();
       const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + buf * 256;
+      int r[2][16];
+      if (c_first < c_end) tmem_ld16(from + c_first, r[0]);
+      char* out = (char*)A.out + ((m0 + c_first) * A.ld_out + n) * ES;
+      const int64_t ld = A.ld_out * ES;
 #pragma unroll 1
-      for (int c0 = 0; c0 < cols; c0 += 16) {
-        int r[16];
-        tmem_ld16(from + c0, r);
-        if (SPLIT) {                           // (the ring is free: all of its stages have been read)
+      for (int c0 = c_first; c0 < c_end; c0 += 32) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) ((int*)ring)[(c0 + j) * kRows + row] = r[j];
-        } else if (mine) {
+        for (int h = 0; h < 2; ++h) {          // (the next 16 columns are under way while these are stored)
+          const int c = c0 + 16 * h;
+          if (c >= c_end) break;
+          tmem_wait(r[h]);
+          if (c + 16 < c_end) tmem_ld16(from + c + 16, r[h ^ 1]);
+          if (SPLIT) {                         // (the ring is free: all of its stages have been read)
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (c0 + j < cols) put<BF16>(A.out, (m0 + c0 + j) * A.ld_out + n, (float)r[j] * (sm.sx[q][c0 + j] * sw));
+            for (int j = 0; j < 16; ++j) ((int*)ring)[(c + j) * kRows + row] = r[h][j];
+          } else if (words) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+              const float a = (float)r[h][j] * (sm.sx[w][c + j] * sw), b = (float)r[h][j + 1] * (sm.sx[w][c + j + 1] * sw);
+              const float other = __shfl_xor_sync(0xffffffffu, (lane & 1) ? a : b, 1);
+              const __nv_bfloat162 v = (lane & 1) ? __floats2bfloat162_rn(other, b) : __floats2bfloat162_rn(a, other);
+              if (mine && c + j + (lane & 1) < c_end) *(uint32_t*)(out + ((lane & 1) ? ld - 2 : 0)) = *(const uint32_t*)&v;
+              out += 2 * ld;
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              if (mine && c + j < c_end) put<BF16>(out, 0, (float)r[h][j] * (sm.sx[w][c + j] * sw));
+              out += ld;
+            }
+          }
         }
       }
       fence_before();
@@ -272,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
       const int cols = (int)(A.M - m0 < TN ? A.M - m0 : TN);
       if (n < A.N) {
         const float sw = A.weight_scales[n];
-        for (int c = rank; c < cols; c += ranks) {
+        for (int c = rank * 2 + (warp - 2) / 4; c < cols; c += ranks * 2) {
           int sum = 0;
           for (int r = 0; r < ranks; ++r) {
             uint32_t from;
