@@ -18,6 +18,8 @@
 //   kTiles    tiles of 128 channels and up to 256 tokens one after the other
 //   kPairs    many tiles: two CTAs share a tile of 256 channels and up to 256 tokens (cta_group::2), each fetching its channels and half of the tokens:
 //             a third less to fetch, and six stages where four fit
+#include <cuda.h>
+
 #include "jp_common.cuh"
 #include "jp_internal.h"
 
@@ -79,6 +81,21 @@ __device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint3
 __device__ __forceinline__ void commit(unsigned long long* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(s32(bar)) : "memory");
 }
+// The same for a pair of CTAs: copies that are counted on the even CTA's barrier (bit 24 of a shared::cluster address is the CTA's rank), instructions
+// over both CTAs' shared and tensor memory, and arrivals on the same barrier of both.
+__device__ __forceinline__ void copy_pair(uint32_t to, const CUtensorMap* map, int row, unsigned long long* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to), "l"(map), "r"(0), "r"(row),
+               "r"(s32(bar) & 0xFEFFFFFFu) : "memory");
+}
+__device__ __forceinline__ void mma_i8_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void commit_pair(unsigned long long* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(s32(bar)), "h"((unsigned short)3) : "memory");
+}
+__device__ __forceinline__ void arrive_even(unsigned long long* bar) {
+  asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %0, 0;\n\tmbarrier.arrive.shared::cluster.b64 _, [ra];\n\t}" ::"r"(s32(bar)) : "memory");
+}
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory"); }
@@ -99,19 +116,19 @@ template <bool BF16> __device__ __forceinline__ void put(void* out, int64_t i, f
   else ((float*)out)[i] = v;
 }
 
-enum Form { kShare, kRowsEven, kTiles };
+enum Form { kShare, kRowsEven, kTiles, kPairs };
 
 template <bool BF16, int FORM>
-__global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
-  constexpr bool SPLIT = FORM == kShare;
+__global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x) {
+  constexpr bool SPLIT = FORM == kShare, PAIR = FORM == kPairs;
   extern __shared__ unsigned char raw[];
   unsigned char* const ring = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
   Control& sm = *(Control*)(ring + kRingBytes);
   uint32_t rank = 0;
-  if (SPLIT) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  if (SPLIT || PAIR) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int TN = A.tokens_tile, stages = A.stages, ranks = SPLIT ? A.split : 1;
-  const uint32_t stage_bytes = kTileBytes + (uint32_t)TN * kBlock;
+  const int TN = A.tokens_tile, stages = A.stages, ranks = SPLIT ? A.split : PAIR ? 2 : 1;
+  const uint32_t stage_bytes = kTileBytes + (uint32_t)(PAIR ? TN / 2 : TN) * kBlock;
   const int k0 = SPLIT ? (int)(A.kblocks * rank / ranks) : 0, k1 = SPLIT ? (int)(A.kblocks * (rank + 1) / ranks) : (int)A.kblocks;
   // tiles of this CTA: first, first + step .. below end (kShare: one), and the channels of them that are its own
   int64_t first = blockIdx.x / ranks, step = gridDim.x / ranks, end = A.tiles, row0 = 0, row1 = A.N;
@@ -126,23 +143,54 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
 
   if (tid == 0) {
     for (int s = 0; s < stages; ++s) { bar_init(&sm.full[s], 1); bar_init(&sm.empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { bar_init(&sm.acc_full[b], 1); bar_init(&sm.acc_empty[b], kResultWarps); }
+    for (int b = 0; b < 2; ++b) { bar_init(&sm.acc_full[b], 1); bar_init(&sm.acc_empty[b], PAIR ? 2 * kResultWarps : kResultWarps); }
     sm.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s32(&sm.tmem)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s32(&sm.tmem)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s32(&sm.tmem)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
     fence_before();
   }
   __syncthreads();
+  if (PAIR) cluster_sync();                    // the partner's barriers exist before anything is sent to them
   fence_after();
   const uint32_t tmem = *(volatile uint32_t*)&sm.tmem;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   if (warp == 0) {
     // ---- copies of the next stage of both operands, tile after tile
-    if (lane == 0) {
+    if (PAIR) {
+      if (lane == 0) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        uint32_t n = 0, s = 0, use = 0;
+        bool ok = true;
+        for (int64_t tile = first; tile < end && ok; tile += step) {
+          // (channels behind the last tile and tokens behind the last group read zeros, or tokens that are not stored)
+          const int w_row = (int)((tile / A.tiles_m * 2 + rank) * A.kblocks * kRows), x_row = (int)(tile % A.tiles_m * TN + rank * (TN / 2));
+          for (int kb = 0; kb < (int)A.kblocks; ++kb, ++n) {
+            if (!bar_wait(&sm.empty[s], (use & 1u) ^ 1u, &sm.abort)) { ok = false; break; }
+            if (rank == 0) bar_expect(&sm.full[s], 2u * stage_bytes);
+            copy_pair(s32(ring) + s * stage_bytes, &map_w, w_row + kb * kRows, &sm.full[s]);
+            copy_pair(s32(ring) + s * stage_bytes + kTileBytes, &map_x, x_row + kb * (int)A.padded_m, &sm.full[s]);
+            if (++s == (uint32_t)stages) s = 0, ++use;
+          }
+        }
+        if (!ok) {                             // as below; the even CTA's barriers count both CTAs' copies
+          if (A.status) atomicExch(A.status, (int)JP_ERR_TIMEOUT);
+          for (uint32_t i = n < (uint32_t)stages ? 0 : n - stages; rank == 0 && i < n; ++i) {
+            const long long t0 = clock64();
+            while (!bar_try(&sm.full[i % stages], (i / stages) & 1u))
+              if (clock64() - t0 > kSpin) break;
+          }
+        }
+      }
+    } else if (lane == 0) {
       // The weights do not depend on the quantisation in front of this kernel: with A.early their first stages are fetched before it is done.
       uint32_t armed = 0;
       bool ok = true, waited = false;
@@ -202,9 +250,9 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
     }
   } else if (warp == 1) {
     // ---- instructions: 32 k each, four a stage
-    if (lane == 0) {
-      // int32 accumulator, signed 8-bit operands, both K-major, TN columns, 128 rows
-      const uint32_t shape = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+    if (lane == 0 && (!PAIR || rank == 0)) {
+      // int32 accumulator, signed 8-bit operands, both K-major, TN columns, 128 rows (256 of a pair)
+      const uint32_t shape = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)((PAIR ? 2 * kRows : kRows) >> 4) << 24);
       uint32_t s = 0, phase = 0;
       bool ok = true;
       int t = 0;
@@ -218,12 +266,18 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
           const uint32_t at = s32(ring) + s * stage_bytes;
           const uint64_t a = operand(at), b = operand(at + kTileBytes);
 #pragma unroll
-          for (int q = 0; q < kBlock / 32; ++q)      // 32 bytes further inside the swizzled row: start address + 2
-            mma_i8(tmem + buf * 256, a + q * 2, b + q * 2, shape, kb != k0 || q != 0);
-          commit(&sm.empty[s]);
+          for (int q = 0; q < kBlock / 32; ++q) {    // 32 bytes further inside the swizzled row: start address + 2
+            if (PAIR) mma_i8_pair(tmem + buf * 256, a + q * 2, b + q * 2, shape, kb != k0 || q != 0);
+            else mma_i8(tmem + buf * 256, a + q * 2, b + q * 2, shape, kb != k0 || q != 0);
+          }
+          if (PAIR) commit_pair(&sm.empty[s]);
+          else commit(&sm.empty[s]);
           if (++s == (uint32_t)stages) s = 0, phase ^= 1u;
         }
-        if (ok) commit(&sm.acc_full[buf]);
+        if (ok) {
+          if (PAIR) commit_pair(&sm.acc_full[buf]);
+          else commit(&sm.acc_full[buf]);
+        }
       }
       if (!ok && A.status) atomicExch(A.status, (int)JP_ERR_TIMEOUT);
     }
@@ -238,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
     int t = 0;
     for (int64_t tile = first; tile < end; tile += step, ++t) {
       const uint32_t buf = t & 1, use = t >> 1;
-      const int64_t m0 = tile % A.tiles_m * TN, n = tile / A.tiles_m * kRows + row;
+      const int64_t m0 = tile % A.tiles_m * TN, n = (PAIR ? tile / A.tiles_m * 2 + rank : tile / A.tiles_m) * kRows + row;
       const int cols = (int)(A.M - m0 < TN ? A.M - m0 : TN), half = (cols + 31) / 32 * 16, c_first = w < 4 ? 0 : half, c_end = w < 4 ? (half < cols ? half : cols) : cols;
       const bool mine = FORM == kRowsEven ? n >= row0 && n < row1 && n < A.N : n < A.N;
       const float sw = mine ? A.weight_scales[n] : 0.f;
@@ -288,7 +342,10 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
       }
       fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive(&sm.acc_empty[buf]);
+      if (lane == 0) {
+        if (PAIR) arrive_even(&sm.acc_empty[buf]);
+        else bar_arrive(&sm.acc_empty[buf]);
+      }
     }
   }
   if (SPLIT) {                                 // the ranks' sums of every rank-th token
@@ -319,7 +376,11 @@ __global__ void __launch_bounds__(kThreads, 1) i8_linear_kernel(I8Args A) {
   }
   fence_before();
   __syncthreads();
-  if (warp == 1) {
+  if (PAIR) cluster_sync();                    // neither CTA leaves while the other may still use its memory
+  if (warp == 1 && PAIR) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  } else if (warp == 1) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
@@ -461,6 +522,14 @@ Plan plan_for(int64_t M, int64_t N, int64_t kblocks, int sms) {
     const double cost = (double)rounds * (double)(c + 64);
     if (p.tokens == 0 || cost < best) best = cost, p.tokens = (int)c, p.tiles_m = (M + c - 1) / c;
   }
+  // pairs of CTAs where they have two rounds of tiles at least
+  const int64_t pairs = (tiles_n + 1) / 2 * least;
+  if (M > 128 && pairs >= sms && N * kblocks < (int64_t)1 << 30 && up(M, 8) * kblocks < (int64_t)1 << 30) {
+    p.form = kPairs;
+    p.tokens = (int)up((M + least - 1) / least, 32);
+    p.tiles_m = (M + p.tokens - 1) / p.tokens;
+    return p;
+  }
   const int64_t tiles = tiles_n * p.tiles_m;
   while (p.split < 8 && tiles * p.split * 2 <= sms && kblocks >= p.split * 2) p.split *= 2;
   p.form = p.split > 1 ? kShare : kTiles;
@@ -500,11 +569,38 @@ cudaError_t launch_i8_quantize(I8QuantArgs a, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, threads <= kQuantThreads ? i8_quantize_kernel<1> : i8_quantize_kernel<4>, a);
 }
 
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encode_tiled() {
+  static EncodeTiled fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found);
+    return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? (EncodeTiled)f : nullptr;
+  }();
+  return fn;
+}
+// Rows of 128 bytes as they lie (they are swizzled already), fetched `box` at a time; rows behind the last one read zeros.
+static bool map_rows(CUtensorMap* map, const void* base, int64_t rows, uint32_t box) {
+  const cuuint64_t dims[2] = {(cuuint64_t)kBlock, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)kBlock};
+  const cuuint32_t boxes[2] = {(cuuint32_t)kBlock, box}, steps[2] = {1, 1};
+  return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool BF16, int FORM> static cudaError_t launch_linear(const I8Args& a, cudaStream_t s, int sms) {
   const cudaError_t e = cudaFuncSetAttribute(i8_linear_kernel<BF16, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
   if (e != cudaSuccess) return e;
+  CUtensorMap map_w{}, map_x{};
+  if (FORM == kPairs) {
+    if (!encode_tiled()) return cudaErrorNotSupported;
+    const int64_t tiles_n = (a.N + kRows - 1) / kRows;
+    if (!map_rows(&map_w, a.weights, tiles_n * a.kblocks * kRows, kRows) || !map_rows(&map_x, a.xq, a.kblocks * a.padded_m, (uint32_t)a.tokens_tile / 2))
+      return cudaErrorInvalidValue;
+  }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(FORM == kShare ? a.tiles * a.split : FORM == kRowsEven || a.tiles > sms ? sms : a.tiles));
+  const int64_t pairs = a.tiles < sms / 2 ? a.tiles : sms / 2;
+  cfg.gridDim = dim3((unsigned)(FORM == kShare ? a.tiles * a.split : FORM == kPairs ? 2 * pairs : FORM == kRowsEven || a.tiles > sms ? sms : a.tiles));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSharedBytes;
   cfg.stream = s;
@@ -512,11 +608,11 @@ template <bool BF16, int FORM> static cudaError_t launch_linear(const I8Args& a,
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)a.split;
+  attr[1].val.clusterDim.x = FORM == kPairs ? 2u : (unsigned)a.split;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = FORM == kShare ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, i8_linear_kernel<BF16, FORM>, a);
+  cfg.numAttrs = FORM == kShare || FORM == kPairs ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, i8_linear_kernel<BF16, FORM>, a, map_w, map_x);
 }
 
 cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, int64_t K, bool out_bf16, cudaStream_t s, int sms) {
@@ -526,9 +622,9 @@ cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, i
   const int64_t tiles_n = (a.N + kRows - 1) / kRows;
   a.tokens_tile = p.tokens;
   a.tiles_m = p.tiles_m;
-  a.tiles = tiles_n * p.tiles_m;
+  a.tiles = (p.form == kPairs ? (tiles_n + 1) / 2 : tiles_n) * p.tiles_m;
   a.split = p.split;
-  const int fit = kRingBytes / (kTileBytes + p.tokens * kBlock);
+  const int fit = kRingBytes / (kTileBytes + (p.form == kPairs ? p.tokens / 2 : p.tokens) * kBlock);
   a.stages = fit < kMaxStages ? fit : kMaxStages;
   a.weights = (const uint8_t*)packed;
   a.weight_scales = (const float*)((const char*)packed + tiles_n * a.kblocks * kTileBytes);
@@ -536,6 +632,7 @@ cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, i
   a.token_scales = (const float*)((const char*)tokens + a.padded_m * a.kblocks * kBlock);
   if (p.form == kShare) return out_bf16 ? launch_linear<true, kShare>(a, s, sms) : launch_linear<false, kShare>(a, s, sms);
   if (p.form == kRowsEven) return out_bf16 ? launch_linear<true, kRowsEven>(a, s, sms) : launch_linear<false, kRowsEven>(a, s, sms);
+  if (p.form == kPairs) return out_bf16 ? launch_linear<true, kPairs>(a, s, sms) : launch_linear<false, kPairs>(a, s, sms);
   return out_bf16 ? launch_linear<true, kTiles>(a, s, sms) : launch_linear<false, kTiles>(a, s, sms);
 }
 

@@ -64,7 +64,8 @@ def test_sizes(ctx, M, N, K):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 300, 65536), (40, 130, 65536), (300, 256, 16384), (3, 151936, 256), (48, 30000, 1024), (4100, 1300, 520), (70, 19000, 384),
-                                   (600, 20000, 300), (1, 128, 8192), (20, 2048, 5120), (2500, 2500, 2500)])
+                                   (600, 20000, 300), (1, 128, 8192), (20, 2048, 5120), (2500, 2500, 2500), (257, 37900, 129), (1000, 12801, 256), (129, 38000, 90),
+                                   (513, 19999, 640), (4096, 4096, 384), (7777, 1500, 1111)])
 def test_large_sizes(ctx, M, N, K):
     x, q, scales = make(M, N, K, M + N + K)
     w = runner.pack_i8(ctx, q, scales)
