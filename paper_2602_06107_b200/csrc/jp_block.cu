@@ -967,13 +967,11 @@ int grid_for(int64_t T, const Plan& p, int groups_a_block, int64_t most) {
   return g * groups_a_block % p.period == 0 ? (int)g : p.period;
 }
 
-template <class... P, class... Q>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, int smem, cudaStream_t s, Q... args) {
-  // (the limit belongs to the kernel on the device, for all threads of the host: always the same amount)
-  cudaError_t e = cudaSuccess;
-  if (smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-  if (e == cudaSuccess && smem > 40 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
-  if (e != cudaSuccess) return e;
+template <auto kernel, class... Q> cudaError_t launch(dim3 grid, dim3 block, int smem, cudaStream_t s, Q... args) {
+  if (smem > 0) {
+    const cudaError_t e = allow_shared_memory<kernel>(kSharedBytes);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -996,10 +994,10 @@ template <int DT, bool FULL> cudaError_t forward(const BlockArgs& a, cudaStream_
   }
   const dim3 g((unsigned)grid_for(a.T, p, 1, (int64_t)sms * (p.groups < 24 ? p.groups : 24))), b(p.threads);
   constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
-#define JP_FORWARD(KIND, NU, R, TWICE) (p.threads <= 256 ? launch(block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 256>, g, b, p.smem, s, a, p.place) \
-                                       : p.threads <= 512 ? launch(block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 512>, g, b, p.smem, s, a, p.place) \
-                                                          : launch(block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 1024>, g, b, p.smem, s, a, p.place))
-#define JP_FORWARD_TWICE(KIND, NU) launch(block_fwd_kernel<DT, KIND, NU, 1, stages_of(1, true, DT), FULL, 1024>, g, b, p.smem, s, a, p.place)
+#define JP_FORWARD(KIND, NU, R, TWICE) (p.threads <= 256 ? launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 256>>(g, b, p.smem, s, a, p.place) \
+                                       : p.threads <= 512 ? launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 512>>(g, b, p.smem, s, a, p.place) \
+                                                          : launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 1024>>(g, b, p.smem, s, a, p.place))
+#define JP_FORWARD_TWICE(KIND, NU) launch<block_fwd_kernel<DT, KIND, NU, 1, stages_of(1, true, DT), FULL, 1024>>(g, b, p.smem, s, a, p.place)
   if (p.twice) return p.kind == kAligned ? JP_FORWARD_TWICE(kAligned, 2 * V) : p.kind == kShared ? JP_FORWARD_TWICE(kShared, 2 * V) : JP_FORWARD_TWICE(kElements, 2 * E);
   if (p.rows == 2) return p.kind == kAligned ? JP_FORWARD(kAligned, V, 2, false) : p.kind == kShared ? JP_FORWARD(kShared, V, 2, false) : JP_FORWARD(kElements, E, 2, false);
   return p.kind == kAligned ? JP_FORWARD(kAligned, V, 1, false) : p.kind == kShared ? JP_FORWARD(kShared, V, 1, false) : JP_FORWARD(kElements, E, 1, false);
@@ -1012,7 +1010,7 @@ template <int DT, bool POST, bool FULL> cudaError_t backward(const BlockArgs& a,
   constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
   const dim3 b(p.threads, p.groups);
   const int sums = p.groups > 1 ? (FULL ? 4 : 2) * (int)a.H * 4 : 0, rows = p.smem * p.groups, smem = rows > sums ? rows : sums;
-#define JP_BACKWARD(KIND, NU, R, TWICE) launch(block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL>, g, b, smem, s, a, p.place)
+#define JP_BACKWARD(KIND, NU, R, TWICE) launch<block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL>>(g, b, smem, s, a, p.place)
   if (p.twice) return p.kind == kAligned ? JP_BACKWARD(kAligned, 2 * V, 1, true) : p.kind == kShared ? JP_BACKWARD(kShared, 2 * V, 1, true) : JP_BACKWARD(kElements, 2 * E, 1, true);
   if constexpr (!FULL || DT == JP_F32)
     if (p.rows == 2) return p.kind == kAligned ? JP_BACKWARD(kAligned, V, 2, false) : p.kind == kShared ? JP_BACKWARD(kShared, V, 2, false) : JP_BACKWARD(kElements, E, 2, false);
@@ -1047,7 +1045,7 @@ cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms) {
   const cudaError_t e = a.dtype == JP_BF16 ? backward<JP_BF16>(a, p, grid, n == 4, s) : backward<JP_F32>(a, p, grid, n == 4, s);
   if (e != cudaSuccess) return e;
   const unsigned y = a.post_weight || a.gate ? 2 : 1;
-  return launch(block_lines_kernel, dim3((unsigned)((a.H + 31) / 32), y), dim3(32, 32), 0, s, a, grid, n);
+  return launch<block_lines_kernel>(dim3((unsigned)((a.H + 31) / 32), y), dim3(32, 32), 0, s, a, grid, n);
 }
 
 }  // namespace jp

@@ -589,7 +589,7 @@ static bool map_rows(CUtensorMap* map, const void* base, int64_t rows, uint32_t 
 }
 
 template <bool BF16, int FORM> static cudaError_t launch_linear(const I8Args& a, cudaStream_t s, int sms) {
-  const cudaError_t e = cudaFuncSetAttribute(i8_linear_kernel<BF16, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes);
+  const cudaError_t e = allow_shared_memory<i8_linear_kernel<BF16, FORM>>(kSharedBytes);
   if (e != cudaSuccess) return e;
   CUtensorMap map_w{}, map_x{};
   if (FORM == kPairs) {

@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "jackpot.h"
 
 namespace jp {
@@ -332,6 +334,21 @@ struct VerifyArgs {
 };
 cudaError_t launch_verify(VerifyArgs a, int dtype, cudaStream_t s);
 
+
+// Sets what a kernel needs before its launch (the most dynamic shared memory of a block, and the carveout for it) on the current device, the first
+// time only: the amounts belong to the kernel on the device and are always the same, whatever the call.
+template <auto kernel> cudaError_t allow_shared_memory(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (device & 63);
+  if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (e == cudaSuccess && device < 64) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 
 // Policy and preference losses over the logits of one model (jp_loss.cu).
 struct LossArgs {

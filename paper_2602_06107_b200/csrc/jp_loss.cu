@@ -633,9 +633,8 @@ template <auto kernel, int kThreads> int clusters_at_once(int c, int smem, int s
 template <int NV, int kThreads, int DT, int MODE> cudaError_t rows_of(const LossArgs& a, cudaStream_t s, int sms) {
   constexpr auto kernel = loss_rows_kernel<DT, MODE, NV, kThreads>;
   constexpr int smem = NV * kThreads * 16;
-  if (smem > 0) {                             // (always the same limit: it belongs to the kernel on the device, for all threads of the host)
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (smem > 0) {
+    const cudaError_t e = allow_shared_memory<kernel>(smem);
     if (e != cudaSuccess) return e;
   }
   const int64_t most = clusters_at_once<kernel, kThreads>(a.cluster, smem, sms), clusters = most < a.T ? most : a.T;

@@ -381,7 +381,7 @@ def _loss_rows(logits, tokens, mask, grad, d_logits):
     if not grad:
         return shape[0], shape[1], ld, 0, None
     if d_logits is None:
-        d_logits = logits.new_empty((shape[0], (shape[1] + 7) // 8 * 8))[:, :shape[1]]
+        d_logits = torch.empty_strided(shape, ((shape[1] + 7) // 8 * 8, 1), dtype=logits.dtype, device=logits.device)
     elif d_logits.dtype is not logits.dtype:
         raise B.JackpotError("d_logits must have logits' dtype")
     return shape[0], shape[1], ld, _logit_pitch(d_logits, shape, "d_logits"), d_logits
