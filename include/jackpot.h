@@ -699,8 +699,8 @@ jp_status jp_i8_pack(jp_ctx* ctx, const jp_i8_desc* desc, const int8_t* q, const
 size_t jp_i8_token_bytes(int64_t M, int64_t K);
 /* Quantises x [M, ld_x] bf16 (0 = K, aligned to its elements) into tokens (16-byte aligned), for several layers that read the same x. */
 jp_status jp_i8_quantize(jp_ctx* ctx, const void* x, int64_t ld_x, int64_t M, int64_t K, void* tokens, size_t token_bytes);
-/* out [M, ld_out] of out_dtype (JP_BF16 or JP_F32, 0 = N).  x [M, ld_x] bf16 is quantised into tokens first; x NULL: tokens are as
- * jp_i8_quantize left them.  out_status: one int32 in DEVICE memory or NULL: 0, or JP_ERR_TIMEOUT if a wait inside the kernel
+/* out [M, ld_out] of out_dtype (JP_BF16 or JP_F32, 0 = N).  x [M, ld_x] bf16 is quantised first (tokens is then a workspace, its content of no meaning
+ * afterwards); x NULL: tokens are as jp_i8_quantize left them.  out_status: one int32 in DEVICE memory or NULL: 0, or JP_ERR_TIMEOUT if a wait inside the kernel
  * ran out (out is then unspecified). */
 jp_status jp_i8_linear(jp_ctx* ctx, const jp_i8_desc* desc, const void* packed, const void* x, int64_t ld_x, int64_t M,
                        void* tokens, size_t token_bytes, void* out, int64_t ld_out, int32_t out_dtype, int32_t* out_status);

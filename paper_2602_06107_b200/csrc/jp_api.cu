@@ -1338,12 +1338,20 @@ jp_status jp_i8_linear(jp_ctx* c, const jp_i8_desc* d, const void* packed, const
     if (e != cudaSuccess) return cuda_fail(c, e, "cudaMemsetAsync");
   }
   if (M == 0) return JP_OK;
+  I8Args a{};
+  a.out = out; a.status = out_status; a.M = M; a.N = d->N; a.ld_out = ld_out; a.early = x != nullptr;
+  if (x && i8_one_token(M, d->N, d->K, c->sms)) {
+    I8QuantArgs q{};
+    q.x = x; q.M = M; q.K = d->K; q.ld_x = ld_x;
+    const cudaError_t e = launch_i8_one_token(q, a, packed, out_dtype == JP_BF16, c->stream);
+    if (e != cudaSuccess) return cuda_fail(c, e, "8-bit linear layer launch");
+    c->launches += 1;
+    return JP_OK;
+  }
   if (x) {
     st = i8_quantize(c, x, ld_x, M, d->K, tokens);
     if (st != JP_OK) return st;
   }
-  I8Args a{};
-  a.out = out; a.status = out_status; a.M = M; a.N = d->N; a.ld_out = ld_out; a.early = x != nullptr;
   const cudaError_t e = launch_i8_linear(a, packed, tokens, d->K, out_dtype == JP_BF16, c->stream, c->sms);
   if (e != cudaSuccess) return cuda_fail(c, e, "8-bit linear layer launch");
   c->launches += 1;

@@ -9,7 +9,8 @@
 //   weights  [N / 128 tiles][K / 128 blocks][128 rows x 128 bytes], laid out once;  scales [N]
 //   tokens   [K / 128 blocks][M / 8 groups][8 rows x 128 bytes], written by the quantisation;  scales [M]
 // A CTA (one an SM): warp 0 copies, warp 1 issues the instructions into one of two accumulators in tensor memory, warps 2 to 9 scale and
-// store the other one.  Four forms, by what bounds the call (plan_for):
+// store the other one.  Four forms, by what bounds the call (plan_for), and a kernel of its own for one token of a small layer
+// (i8_one_token_kernel):
 //   kShare    few tiles: the CTAs of a cluster share a tile's K and add their integers through distributed shared memory (any order gives
 //             the same bits)
 //   kRowsEven up to 128 tokens, many channels: the weights' bytes decide.  Every CTA takes the same number of channels, in groups of 8 wherever they
@@ -459,6 +460,22 @@ __device__ __forceinline__ uint4 quantized_chunk(const Chunk& c, float scale, fl
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+// What a token's largest magnitude (the bits of a bf16) makes of it.
+struct TokenScale {
+  float most, scale, scaled, inv;
+  bool usable;
+  __device__ __forceinline__ explicit TokenScale(uint32_t top) {
+    most = __uint_as_float(top << 16);
+    // a power of two that takes the largest magnitude to 1 .. 2 (subnormal ones come out below 1, still with all of their bits)
+    const uint32_t exponent = top >> 7;
+    scale = exponent == 0u ? __uint_as_float(253u << 23) : exponent == 254u ? __uint_as_float(1u << 22) : __uint_as_float((254u - exponent) << 23);
+    scaled = most * scale;
+    inv = scaled > 0.f ? 1.f / scaled : 0.f;
+    usable = exponent < 255u;                  // else a NaN or an infinity: the token's outputs are NaN
+  }
+  __device__ __forceinline__ float step() const { return usable ? most / 127.f : __uint_as_float(0x7fc00000u); }
+};
+
 // kHeld: chunks of 16 a thread keeps between the maximum and the rounding; a row's others are read again.  (One, for rows of up to 4096, leaves
 // room for eight blocks an SM: 4096 x 4096 25 us with four.)
 template <int kHeld> __global__ void __launch_bounds__(kQuantThreads, kHeld == 1 ? 8 : 3) i8_quantize_kernel(I8QuantArgs A) {
@@ -481,12 +498,9 @@ template <int kHeld> __global__ void __launch_bounds__(kQuantThreads, kHeld == 1
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = top;
   __syncthreads();
   for (int w = 0; w < (int)blockDim.x / 32; ++w) top = sh[w] > top ? sh[w] : top;
-  const float most = __uint_as_float(top << 16);
-  // a power of two that takes the largest magnitude to 1 .. 2 (subnormal ones come out below 1, still with all of their bits)
-  const uint32_t exponent = top >> 7;
-  const float scale = exponent == 0u ? __uint_as_float(253u << 23) : exponent == 254u ? __uint_as_float(1u << 22) : __uint_as_float((254u - exponent) << 23);
-  const float scaled = most * scale, inv = scaled > 0.f ? 1.f / scaled : 0.f;
-  const bool usable = exponent < 255u;         // else a NaN or an infinity: the token's outputs are NaN
+  const TokenScale t(top);
+  const float scale = t.scale, scaled = t.scaled, inv = t.inv;
+  const bool usable = t.usable;
   char* out = (char*)A.tokens + (m / 8) * 1024 + (m & 7) * 128;
   auto place = [&](int64_t c) { return (uint4*)(out + c / 8 * (A.padded_m / 8) * 1024 + (((int)(c & 7) ^ (int)(m & 7)) * 16)); };
   const uint4 none = make_uint4(0u, 0u, 0u, 0u);
@@ -498,7 +512,73 @@ template <int kHeld> __global__ void __launch_bounds__(kQuantThreads, kHeld == 1
   for (int64_t c = (int64_t)kHeld * blockDim.x + threadIdx.x; c < chunks; c += blockDim.x)
     *place(c) = usable ? quantized_chunk(load_chunk(A, row, c * 16), scale, scaled, inv) : none;
   if (threadIdx.x == 0)
-    ((float*)((char*)A.tokens + A.padded_m * A.kblocks * kBlock))[m] = usable ? most / 127.f : __uint_as_float(0x7fc00000u);
+    ((float*)((char*)A.tokens + A.padded_m * A.kblocks * kBlock))[m] = t.step();
+}
+
+// One token of a small layer, in one launch: a CTA quantises the token by itself into shared memory (it is short, so that this costs less than a
+// kernel in front) and takes 8 channels, its warps a part of K each; four products an instruction (dp4a), as a tensor-core tile would be 1/128 full.
+// Latency bounds such a call.
+constexpr int kOneBatch = 4;                   // 1 KB lines of weights a warp has on the way at once
+constexpr int64_t kOneK = 16384, kOneWeights = 48 << 20;
+template <bool BF16> __global__ void __launch_bounds__(256) i8_one_token_kernel(I8QuantArgs X, I8Args A) {
+  extern __shared__ uint4 xs[];                // [K / 16]
+  __shared__ uint32_t top;
+  __shared__ int sums[8][8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kblocks = (int)A.kblocks, chunks = kblocks * (kBlock / 16);
+  if (threadIdx.x == 0) top = 0u;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  __syncthreads();
+  const int64_t group = blockIdx.x;            // of 8 channels: 1024 contiguous bytes of a block of K
+  const uint4* const w = (const uint4*)(A.weights + group / 16 * A.kblocks * kTileBytes + group % 16 * 1024) + lane;
+  uint4 held[kOneBatch][2];                    // chunks lane and lane + 32 of the line: channels lane / 8 and 4 + lane / 8
+  const auto load = [&](int kb) {
+#pragma unroll
+    for (int i = 0; i < kOneBatch; ++i) {
+      const bool has = kb + 8 * i < kblocks;
+      const uint4* const from = w + (int64_t)(kb + 8 * i) * (kTileBytes / 16);
+      held[i][0] = has ? __ldg(from) : make_uint4(0u, 0u, 0u, 0u);
+      held[i][1] = has ? __ldg(from + 32) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  };
+  load(warp);
+  uint32_t t = 0u;
+  for (int c = threadIdx.x; c < chunks; c += 256) t = largest(load_chunk(X, (const char*)X.x, c * 16), t);
+  t = (t & 0xffffu) > t >> 16 ? t & 0xffffu : t >> 16;
+  t = __reduce_max_sync(0xffffffffu, t);
+  if (lane == 0) atomicMax(&top, t);           // (integers: any order)
+  __syncthreads();
+  const TokenScale token(top);
+  for (int c = threadIdx.x; c < chunks; c += 256)
+    xs[c] = token.usable ? quantized_chunk(load_chunk(X, (const char*)X.x, c * 16), token.scale, token.scaled, token.inv) : make_uint4(0u, 0u, 0u, 0u);
+  __syncthreads();
+  int acc[2] = {0, 0};
+  const int at[2] = {(lane & 7) ^ (lane >> 3), (lane & 7) ^ (4 + (lane >> 3))};          // where in the row's 128 bytes the chunks belong
+  for (int kb = warp; kb < kblocks; kb += 8 * kOneBatch) {
+    if (kb != warp) load(kb);
+#pragma unroll
+    for (int i = 0; i < kOneBatch; ++i)
+      if (kb + 8 * i < kblocks)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint4 p = xs[(kb + 8 * i) * 8 + at[h]], q = held[i][h];
+          acc[h] = __dp4a((int)q.x, (int)p.x, __dp4a((int)q.y, (int)p.y, __dp4a((int)q.z, (int)p.z, __dp4a((int)q.w, (int)p.w, acc[h]))));
+        }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) acc[h] += __shfl_xor_sync(0xffffffffu, acc[h], o);
+    if ((lane & 7) == 0) sums[warp][4 * h + (lane >> 3)] = acc[h];
+  }
+  __syncthreads();
+  const int64_t n = group * 8 + threadIdx.x;
+  if (threadIdx.x < 8 && n < A.N) {
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += sums[i][threadIdx.x];
+    put<BF16>(A.out, n, (float)sum * (token.step() * A.weight_scales[n]));
+  }
 }
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -613,6 +693,29 @@ template <bool BF16, int FORM> static cudaError_t launch_linear(const I8Args& a,
   cfg.attrs = attr;
   cfg.numAttrs = FORM == kShare || FORM == kPairs ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, i8_linear_kernel<BF16, FORM>, a, map_w, map_x);
+}
+
+// Measured in us, one token to bf16, N x K (two launches with the kernels above in brackets): 512 x 512 2.3 (5.0), 2048 x 2048 3.3 (9.9), 9472 x 4096
+// 10.8 (13.1), 11,008 x 4096 12.4 (15.4), 2048 x 16,384 12.0 (20.8); more weights or channels: 9472 x 8192 17.8 (18.2), 18,944 x 2048 13.6 (11.7),
+// 40,960 x 1024 23.6 (15.9), 151,936 x 2048 90 (56), where every CTA's own quantisation adds up.
+bool i8_one_token(int64_t M, int64_t N, int64_t K, int sms) { return M == 1 && K <= kOneK && N <= 80 * (int64_t)sms && N * K <= kOneWeights; }
+
+cudaError_t launch_i8_one_token(I8QuantArgs x, I8Args a, const void* packed, bool out_bf16, cudaStream_t s) {
+  a.kblocks = (x.K + kBlock - 1) / kBlock;
+  x.vectors = ((uintptr_t)x.x & 15) == 0;
+  a.weights = (const uint8_t*)packed;
+  a.weight_scales = (const float*)((const char*)packed + (a.N + kRows - 1) / kRows * a.kblocks * kTileBytes);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)((a.N + 7) / 8));
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = (size_t)(a.kblocks * kBlock);
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return out_bf16 ? cudaLaunchKernelEx(&cfg, i8_one_token_kernel<true>, x, a) : cudaLaunchKernelEx(&cfg, i8_one_token_kernel<false>, x, a);
 }
 
 cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, int64_t K, bool out_bf16, cudaStream_t s, int sms) {

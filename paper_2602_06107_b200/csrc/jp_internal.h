@@ -469,6 +469,8 @@ size_t i8_packed_bytes(int64_t N, int64_t K);
 size_t i8_token_bytes(int64_t M, int64_t K);
 cudaError_t launch_i8_pack(I8PackArgs a, cudaStream_t s, int sms);
 cudaError_t launch_i8_quantize(I8QuantArgs a, cudaStream_t s);
+bool i8_one_token(int64_t M, int64_t N, int64_t K, int sms);     // one token of a small layer, in one launch
+cudaError_t launch_i8_one_token(I8QuantArgs x, I8Args a, const void* packed, bool out_bf16, cudaStream_t s);
 cudaError_t launch_i8_linear(I8Args a, const void* packed, const void* tokens, int64_t K, bool out_bf16, cudaStream_t s, int sms);
 
 }  // namespace jp

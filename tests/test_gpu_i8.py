@@ -129,6 +129,23 @@ def test_pitches_and_places(ctx, M, N, K, ld_x, ld_q):
     assert torch.equal(runner.linear_i8(ctx, xo, w, out_dtype=F32), runner.linear_i8(ctx, x, w, out_dtype=F32))
 
 
+@pytest.mark.parametrize("N,K", [(7, 16384), (2048, 16384), (2048, 16385), (11840, 4096), (11848, 4096), (9001, 5009), (1024, 4096), (1025, 4097)])
+def test_one_token(ctx, N, K):
+    """One token, quantised in the same kernel up to some size: the same bits as in two steps, from any place of x."""
+    x, q, scales = make(6, N, K, N + K, K + 3)
+    x[3] = 0
+    x[4, K - 1], x[5, 0] = float("nan"), float("-inf")
+    w = runner.pack_i8(ctx, q, scales)
+    for i in range(6):
+        row = x[i:i + 1]
+        out = runner.linear_i8(ctx, row, w, out_dtype=F32)
+        two = runner.linear_i8(ctx, runner.quantize_tokens_i8(ctx, row), w, out_dtype=F32)
+        assert torch.equal(out.view(torch.int32), two.view(torch.int32)) or (i > 3 and out.isnan().all() and two.isnan().all())
+        if i < 4:
+            check(out, row, q, scales)
+            check(runner.linear_i8(ctx, row, w), row, q, scales)
+
+
 def test_no_tokens(ctx):
     x, q, scales = make(4, 100, 64, 1)
     w = runner.pack_i8(ctx, q, scales)
