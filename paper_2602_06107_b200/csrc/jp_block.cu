@@ -233,29 +233,38 @@ inline int place_bytes(bool vec, int threads, int units, int64_t H, int es) {
   return vec ? threads * units * 16 : (int)((H * es + 15) / 16 + 1) * 16;
 }
 
-// A matrix's rows of a group, for the thread that writes them: row `first`, then every `step`-th.
-template <int ES> struct Out {
-  char* at;
-  int64_t stride;
-  __device__ __forceinline__ Out(void* base, int64_t ld, int64_t first, int64_t step, int column)
-      : at((char*)base + (first * ld + column) * ES), stride(step * ld * ES) {}
+// Where column `column` of a row is.  (From the row's number each time: the pitches lie in the constant bank, and pointers that move along would
+// take registers, which the sums over rows need.)
+template <int ES> __device__ __forceinline__ char* row_at(const void* base, int64_t ld, unsigned row, int column) {
+  return (char*)base + ((int64_t)((uint64_t)row * (uint32_t)ld) + column) * ES;
+}
+
+// The matrices that the forward and the backward read.
+struct ForwardIn {
+  static constexpr int N = 2;
+  __device__ static __forceinline__ const void* base(const BlockArgs& A, int t) { return t == 0 ? A.x : A.residual; }
+  __device__ static __forceinline__ int64_t ld(const BlockArgs& A, int t) { return t == 0 ? A.ld_x : A.ld_residual; }
+};
+struct BackwardIn {
+  static constexpr int N = 4;
+  __device__ static __forceinline__ const void* base(const BlockArgs& A, int t) { return t == 0 ? A.dy : t == 1 ? A.sum : t == 2 ? A.dsum : A.x; }
+  __device__ static __forceinline__ int64_t ld(const BlockArgs& A, int t) { return t == 0 ? A.ld_dy : t == 1 ? A.ld_sum : t == 2 ? A.ld_dsum : A.ld_x; }
 };
 
-// The group's rows of NT matrices: row `first`, then every `step`-th, STAGES of them under way.
-template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
+// The group's rows of the matrices IN: row `first`, then every `step`-th, STAGES of them under way.
+template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring {
   using Un = Unit<DT, KIND>;
-  static constexpr int ES = Vec<DT>::ESIZE;
+  static constexpr int ES = Vec<DT>::ESIZE, NT = IN::N;
   static constexpr bool VEC = Un::VEC;
-  const char* next[NT];                                     // the next row to fetch (VEC: from the thread's first unit on)
-  int64_t stride[NT], left;                                 // rows not fetched yet
+  const BlockArgs& A;
+  unsigned next, step;                                      // the next row to fetch (below 2^32: T, and so step, are below 2^31)
   uint32_t mem, in, out, end;                               // places (VEC: the thread's own): all, to fill, the oldest row's
   int place;
   unsigned there;                                           // bits: there is such a matrix
-  bool at_start, at_end;                                    // the next row is the matrices' first one; the group's last row is their last one
-  unsigned taken[NT];                                       // kElements: low bits of the oldest row's address; a place begins at its row's offset to 16
+  __device__ __forceinline__ Ring(const BlockArgs& A_) : A(A_) {}
   // 16 bytes of a row's covering vectors; those that reach beyond the matrix, in its first and last row, element by element
   __device__ __forceinline__ void copy(uint32_t to, const char* from, const char* row, int bytes) const {
-    if ((at_start || (at_end && left == 1)) && (from < row || from + 16 > row + bytes)) {
+    if ((next == 0u || next == (unsigned)A.T - 1u) && (from < row || from + 16 > row + bytes)) {
 #pragma unroll 1
       for (int q = 0; q < 16; q += ES)
         if (from + q >= row && from + q < row + bytes) sts_one<ES>(to + q, from + q);
@@ -264,52 +273,42 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
     }
   }
   __device__ __forceinline__ void fetch(const Un& un) {
-    if (left > 0) {
+    if (next < (unsigned)A.T) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
         if (there >> t & 1u) {
           const uint32_t to = in + t * place;
           if constexpr (VEC) {
+            const char* const at = row_at<ES>(IN::base(A, t), IN::ld(A, t), next, un.first);
 #pragma unroll
             for (int u = 0; u < NU; ++u)
               if (un.have >> u & 1u) {
-                const char* const from = next[t] + u * (int)blockDim.x * 16;
-                if (KIND == kShared && (un.part >> u & 1u)) copy(to + u * blockDim.x * 16, from, next[t] - un.first * ES, un.H * ES);
+                const char* const from = at + u * (int)blockDim.x * 16;
+                if (KIND == kShared && (un.part >> u & 1u)) copy(to + u * blockDim.x * 16, from, at - un.first * ES, un.H * ES);
                 else copy16(to + u * blockDim.x * 16, from);
               }
           } else {
-            const char* const row = next[t];
+            const char* const row = row_at<ES>(IN::base(A, t), IN::ld(A, t), next, 0);
             const int skip = (int)((uintptr_t)row & 15), bytes = un.H * ES;
             for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) copy(to + i, row - skip + i, row, bytes);
           }
         }
-#pragma unroll
-      for (int t = 0; t < NT; ++t) next[t] += stride[t];
-      --left;
-      at_start = false;
+      next += step;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     in += NT * place;
     if (in == end) in = mem;
   }
-  __device__ __forceinline__ void start(const Un& un, const void* const (&base)[NT], const int64_t (&ld)[NT], int64_t first, int64_t step, int64_t T, const void* mem_, int place_) {
+  __device__ __forceinline__ void start(const Un& un, unsigned there_, unsigned first, unsigned step_, const void* mem_, int place_) {
     place = place_;
     mem = (uint32_t)__cvta_generic_to_shared(mem_) + (VEC ? threadIdx.x * 16 : 0);
     in = out = mem;
     end = mem + STAGES * NT * place;
-    there = 0u;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      there |= (base[t] ? 1u : 0u) << t;
-      next[t] = (const char*)base[t] + (first * ld[t] + (VEC ? un.first : 0)) * ES;
-      taken[t] = (unsigned)(uintptr_t)next[t];
-      stride[t] = step * ld[t] * ES;
-    }
-    left = first < T ? (T - first + step - 1) / step : 0;
-    at_start = KIND != kAligned && first == 0;
-    at_end = KIND != kAligned && left > 0 && first + (left - 1) * step == T - 1;
+    there = there_;
+    next = first;
+    step = step_;
     if constexpr (VEC) {                                    // what is never fetched reads 0
-      if (un.have != (1u << NU) - 1u || there != (1u << NT) - 1u || left < STAGES)
+      if (un.have != (1u << NU) - 1u || there != (1u << NT) - 1u || (int64_t)first + (int64_t)(STAGES - 1) * step >= A.T)
         for (uint32_t at = mem; at != end; at += place)
 #pragma unroll
           for (int u = 0; u < NU; ++u)
@@ -333,8 +332,8 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
     const uint32_t at = out + r * NT * place;
     return r > 0 && at >= end ? at - STAGES * NT * place : at;
   }
-  // unit u of matrix t of the r-th oldest row, whose places are `at`
-  __device__ __forceinline__ typename Un::Raw get(const Un& un, uint32_t at, int t, int u, int r) const {
+  // unit u of matrix t of a row, whose places are `at` (kElements: a place begins at its row's offset to 16)
+  __device__ __forceinline__ typename Un::Raw get(const Un& un, uint32_t at, int t, int u, unsigned number) const {
     typename Un::Raw w;
     if constexpr (VEC) {
       const uint4 v = lds16(at + t * place + u * blockDim.x * 16);
@@ -343,7 +342,7 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
 #pragma unroll
       for (int i = 0; i < (int)(sizeof(w) / 4); ++i) w.w[i] = 0u;
       if (there >> t & 1u) {
-        const uint32_t from = at + t * place + ((taken[t] + (unsigned)r * (unsigned)stride[t]) & 15u) + threadIdx.x * ES;
+        const uint32_t from = at + t * place + ((unsigned)(uintptr_t)row_at<ES>(IN::base(A, t), IN::ld(A, t), number, 0) & 15u) + threadIdx.x * ES;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
           if (un.inside(u, e)) {
@@ -362,10 +361,6 @@ template <int DT, int KIND, int NU, int NT, int STAGES, bool SOLE> struct Ring {
       out += NT * place;
       if (out == end) out = mem;
       fetch(un);
-    }
-    if (!VEC) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t) taken[t] += R * (unsigned)stride[t];
     }
   }
 };
@@ -426,7 +421,7 @@ __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 // R rows at a time.  FULL: layer norm, biases, a gate a token; without it those instructions and registers are left out.
 template <int DT, int KIND, int NU, int R, int STAGES, bool FULL, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) block_fwd_kernel(BlockArgs A, int place) {
+__global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) block_fwd_kernel(const __grid_constant__ BlockArgs A, int place) {
   using Un = Unit<DT, KIND>;
   constexpr int ES = Vec<DT>::ESIZE, P = Un::P;
   extern __shared__ uint4 places[];
@@ -434,13 +429,12 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
   asm volatile("griddepcontrol.wait;" ::: "memory");        // launched as a programmatic dependent of whatever is before it
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int slot = 0;
-  const int64_t step = gridDim.x;
+  const unsigned step = gridDim.x;
   const bool center = FULL && !A.rms, post = A.post_weight != nullptr;
   Un un;
-  un.template start<NU>((const char*)A.x + blockIdx.x * A.ld_x * ES, A.H);
-  Ring<DT, KIND, NU, 2, STAGES, true> in;
-  in.start(un, {A.x, A.residual}, {A.ld_x, A.ld_residual}, blockIdx.x, step, A.T, places, place);
-  Out<ES> sum(A.sum, A.ld_sum, blockIdx.x, step, un.first), y(A.y, A.ld_y, blockIdx.x, step, un.first);
+  un.template start<NU>(row_at<ES>(A.x, A.ld_x, blockIdx.x, 0), A.H);
+  Ring<DT, KIND, NU, ForwardIn, STAGES, true> in(A);
+  in.start(un, 3u, blockIdx.x, step, places, place);
   // s = residual + gt (xhat1 fw + fb),  y = xhat2 w2 + b2
   float2 fw[NU][P], fb[FULL ? NU : 1][P], w2[NU][P], b2[FULL ? NU : 1][P];
 #pragma unroll
@@ -461,7 +455,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
       if (FULL) fb[u][p] = mul2(fb[u][p], g[p]);
     }
   }
-  for (int64_t row = blockIdx.x; row < A.T; row += R * step) {
+  for (unsigned row = blockIdx.x; row < (unsigned)A.T; row += R * step) {
     float m1[R], r1[R], m2[R], r2[R];
     in.template wait<R>(un);
     typename Un::Raw rx[R][NU], s[R][NU];                   // s: the residual, then the sum
@@ -469,9 +463,9 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
     for (int r = 0; r < R; ++r) {
       const uint32_t at = in.row(r);
 #pragma unroll
-      for (int u = 0; u < NU; ++u) rx[r][u] = in.get(un, at, 0, u, r);
+      for (int u = 0; u < NU; ++u) rx[r][u] = in.get(un, at, 0, u, row + r * step);
 #pragma unroll
-      for (int u = 0; u < NU; ++u) s[r][u] = in.get(un, at, 1, u, r);
+      for (int u = 0; u < NU; ++u) s[r][u] = in.get(un, at, 1, u, row + r * step);
     }
     in.template done<R>(un);
     if (post) {
@@ -482,8 +476,9 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t t = row + r * step;
-      if (r > 0 && t >= A.T) break;
+      const unsigned t = row + r * step;
+      if (r > 0 && t >= (unsigned)A.T) break;
+      char* const to = row_at<ES>(A.sum, A.ld_sum, t, un.first);
       const float gt = FULL && A.token_gate ? A.token_gate[t] : 1.f;
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
@@ -497,7 +492,7 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
           o[p] = FULL ? fma2(fma2(x[p], fw[u][p], fb[u][p]), both(gt), o[p]) : fma2(x[p], fw[u][p], o[p]);
         }
         s[r][u] = Un::pack(o);
-        un.store(sum.at + r * sum.stride, u, s[r][u]);
+        un.store(to, u, s[r][u]);
       }
       if (threadIdx.x == 0 && post) {
         if (A.out_post_mean) A.out_post_mean[t] = m1[r];
@@ -507,8 +502,9 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
     row_stats<Un, NU, R, FULL>(A, un, [&](int r, int u, float2 (&f)[P]) { Un::unpack(s[r][u], f); }, sh, slot, m2, r2);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t t = row + r * step;
-      if (r > 0 && t >= A.T) break;
+      const unsigned t = row + r * step;
+      if (r > 0 && t >= (unsigned)A.T) break;
+      char* const to = row_at<ES>(A.y, A.ld_y, t, un.first);
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         float2 x[P];
@@ -519,15 +515,13 @@ __global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) b
           x[p] = mul2(x[p], both(r2[r]));
           x[p] = FULL ? fma2(x[p], w2[u][p], b2[u][p]) : mul2(x[p], w2[u][p]);
         }
-        un.store(y.at + r * y.stride, u, Un::pack(x));
+        un.store(to, u, Un::pack(x));
       }
       if (threadIdx.x == 0) {
         if (A.out_mean) A.out_mean[t] = m2[r];
         if (A.out_rstd) A.out_rstd[t] = r2[r];
       }
     }
-    sum.at += R * sum.stride;
-    y.at += R * y.stride;
   }
 }
 
@@ -602,7 +596,7 @@ __global__ void __launch_bounds__(1024) block_fwd_wide_kernel(BlockArgs A) {
 constexpr int kMaxSums = 4;
 
 template <int DT, int KIND, int NU, int R, int STAGES, bool POST, bool FULL>
-__global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) {
+__global__ void __launch_bounds__(512) block_bwd_kernel(const __grid_constant__ BlockArgs A, int place) {
   using Un = Unit<DT, KIND>;
   constexpr int ES = Vec<DT>::ESIZE, P = Un::P, N = FULL ? 4 : 2, V1 = FULL ? 2 * R : R, V2 = FULL ? 3 * R : R;
   // Where they fit the registers, a row's values are held as they were stored from its first sum on and its places are free at once; else
@@ -623,12 +617,11 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
     for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int p = 0; p < P; ++p) acc[n][u][p] = both(0.f);
-  const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
+  const unsigned first = blockIdx.x * blockDim.y + threadIdx.y, step = gridDim.x * blockDim.y;
   Un un;
-  un.template start<NU>((const char*)A.dy + first * A.ld_dy * ES, A.H);
-  Ring<DT, KIND, NU, 4, STAGES, false> in;
-  in.start(un, {A.dy, A.sum, A.dsum, use_x ? A.x : nullptr}, {A.ld_dy, A.ld_sum, A.ld_dsum, A.ld_x}, first, step, A.T,
-           (char*)places + threadIdx.y * STAGES * 4 * place, place);
+  un.template start<NU>(row_at<ES>(A.dy, A.ld_dy, first, 0), A.H);
+  Ring<DT, KIND, NU, BackwardIn, STAGES, false> in(A);
+  in.start(un, 3u | (A.dsum ? 4u : 0u) | (use_x ? 8u : 0u), first, step, (char*)places + threadIdx.y * STAGES * 4 * place, place);
   float2 w2[NU][P], fw[NU][P], fb[FULL ? NU : 1][P];        // fw = a gc w1, fb = a gc b1
 #pragma unroll
   for (int u = 0; u < NU; ++u) {
@@ -646,11 +639,11 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
   }
   // the rows' scalars, fetched a turn ahead (a row behind the last one reads 0 throughout)
   float next[R][5];
-  auto scalars = [&](int64_t row) {
+  auto scalars = [&](unsigned row) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t at = row + r * step;
-      const bool have = at < A.T;
+      const unsigned at = row + r * step;
+      const bool have = at < (unsigned)A.T;
       next[r][0] = POST && center && have ? A.post_mean[at] : 0.f;
       next[r][1] = !POST ? 1.f : have ? A.post_rstd[at] : 0.f;
       next[r][2] = center && have ? A.mean[at] : 0.f;
@@ -659,8 +652,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
     }
   };
   scalars(first);
-  Out<ES> dres(A.dresidual, A.ld_dresidual, first, step, un.first), dx(A.dx, A.ld_dx, first, step, un.first);
-  for (int64_t row = first; row < A.T; row += R * step) {
+  for (unsigned row = first; row < (unsigned)A.T; row += R * step) {
     float m1[R], r1[R], m2[R], r2[R], gt[R], v[V1], t[V2];
 #pragma unroll
     for (int r = 0; r < R; ++r) m1[r] = next[r][0], r1[r] = next[r][1], m2[r] = next[r][2], r2[r] = next[r][3], gt[r] = next[r][4];
@@ -673,17 +665,17 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
 #pragma unroll
         for (int u = 0; u < NU; ++u)
 #pragma unroll
-          for (int t = 0; t < 4; ++t) held[t][r][u] = in.get(un, in.row(r), t, u, r);
+          for (int t = 0; t < 4; ++t) held[t][r][u] = in.get(un, in.row(r), t, u, row + r * step);
       in.template done<R>(un);
     }
     auto read = [&](int t, int r, int u, float2 (&f)[P]) {  // unit u of dy, sum, dsum or x
       if constexpr (HOLD) Un::unpack(held[t][r][u], f);
-      else Un::unpack(in.get(un, in.row(r), t, u, r), f);
+      else Un::unpack(in.get(un, in.row(r), t, u, row + r * step), f);
     };
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float2 v1 = both(0.f), v2 = v1;
-      if (r == 0 || row + r * step < A.T) {
+      if (r == 0 || row + r * step < (unsigned)A.T) {
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
           float2 d[P], s[P];
@@ -714,10 +706,11 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
     float2 gs[R][NU][P];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t at = row + r * step;
+      const unsigned at = row + r * step;
+      char* const to = row_at<ES>(A.dresidual, A.ld_dresidual, at, un.first);
       const float a1 = center ? v[V1 - R + r] * inv_h : 0.f, k2 = -r2[r] * (r2[r] * (v[r] * inv_h));      // (r r alone may leave fp32)
       float2 t0 = both(0.f), t1 = t0, tb = t0;
-      if (r == 0 || at < A.T) {
+      if (r == 0 || at < (unsigned)A.T) {
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
           float2 d[P], s[P], e[P], x[P];
@@ -742,7 +735,7 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
               acc[3][u][p] = add2(acc[3][u][p], gg);
             }
           }
-          un.store(dres.at + r * dres.stride, u, Un::pack(gs[r][u]));
+          un.store(to, u, Un::pack(gs[r][u]));
         }
       }
       t[r] = t1.x + t1.y;
@@ -760,8 +753,9 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t at = row + r * step;
-      if (r > 0 && at >= A.T) break;
+      const unsigned at = row + r * step;
+      if (r > 0 && at >= (unsigned)A.T) break;
+      char* const to = row_at<ES>(A.dx, A.ld_dx, at, un.first);
       if (token && threadIdx.x == 0) A.dtoken_gate[at] = t[r] + t[V2 - R + r];
       // dx = r1 (gt g1 - c1 - xhat1 c2)
       const float c0 = center ? -r1[r] * (gt[r] * (t[V2 > R ? R + r : r] * inv_h)) : 0.f, c2 = -r1[r] * (r1[r] * (gt[r] * (t[r] * inv_h))), rg = r1[r] * gt[r];
@@ -779,12 +773,10 @@ __global__ void __launch_bounds__(512) block_bwd_kernel(BlockArgs A, int place) 
             o[p] = mul2(o[p], both(gt[r]));
           }
         }
-        un.store(dx.at + r * dx.stride, u, Un::pack(o));
+        un.store(to, u, Un::pack(o));
       }
     }
     if constexpr (!HOLD) in.template done<R>(un);
-    dres.at += R * dres.stride;
-    dx.at += R * dx.stride;
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the kernel that adds the lines may set up
