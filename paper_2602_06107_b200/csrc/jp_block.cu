@@ -595,13 +595,13 @@ __global__ void __launch_bounds__(1024) block_fwd_wide_kernel(BlockArgs A) {
 // Lines of sums over rows: dw2, Q1 and, with FULL, db2 and Q0.
 constexpr int kMaxSums = 4;
 
-template <int DT, int KIND, int NU, int R, int STAGES, bool POST, bool FULL>
-__global__ void __launch_bounds__(512) block_bwd_kernel(const __grid_constant__ BlockArgs A, int place) {
+template <int DT, int KIND, int NU, int R, int STAGES, bool POST, bool FULL, int THREADS>
+__global__ void __launch_bounds__(THREADS) block_bwd_kernel(const __grid_constant__ BlockArgs A, int place) {
   using Un = Unit<DT, KIND>;
   constexpr int ES = Vec<DT>::ESIZE, P = Un::P, N = FULL ? 4 : 2, V1 = FULL ? 2 * R : R, V2 = FULL ? 3 * R : R;
   // Where they fit the registers, a row's values are held as they were stored from its first sum on and its places are free at once; else
   // they are read again behind each sum.
-  constexpr bool HOLD = KIND == kAligned && !FULL && NU * Un::E == 8;
+  constexpr bool HOLD = KIND == kAligned && !FULL && NU * Un::E == 8 && THREADS == 512;     // (8192 x 4096 in 96 registers: 362 us instead of 82)
   constexpr int HR = HOLD ? R : 1, HU = HOLD ? NU : 1;
   static_assert(V2 <= kMaxValues, "");
   extern __shared__ uint4 places[];
@@ -922,7 +922,8 @@ void kind_of(const BlockArgs& a, bool backward, Plan* p) {
 constexpr int kSharedBytes = 225 * 1024;      // of an SM, for rows
 constexpr int stages_of(int rows, bool twice, int dt) { return rows == 2 ? 6 : twice && dt == JP_F32 ? 1 : 3; }
 
-Plan plan_for(const BlockArgs& a, bool backward, bool one_row, int matrices, int most_threads, int sms) {
+// Threads a block may have: usual, or most where it has one group more of 8 elements a thread then (one instead of none, two instead of one)
+Plan plan_for(const BlockArgs& a, bool backward, bool one_row, int matrices, int usual, int most, int sms) {
   const int dtype = a.dtype, es = dtype == JP_BF16 ? 2 : 4, w = 16 / es;
   const int64_t T = a.T;
   Plan p{};
@@ -930,11 +931,12 @@ Plan plan_for(const BlockArgs& a, bool backward, bool one_row, int matrices, int
   const bool vec = p.kind != kElements;
   const int64_t H = p.kind == kShared ? (a.H + 2 * w - 2) / w * w : a.H;     // the columns that covering vectors have
   const int64_t per = (H + 7) / 8;
-  p.twice = per > most_threads;
+  p.twice = per > most;
   const int64_t threads = ((p.twice ? (H + 15) / 16 : per) + 31) / 32 * 32;
-  if (threads > most_threads) return p;
+  if (threads > (p.twice ? usual : most)) return p;
   p.threads = (int)threads;
-  p.groups = most_threads / p.threads;
+  p.groups = usual / p.threads;
+  if (p.groups < 2 && !p.twice && most / p.threads > p.groups) p.groups = most / p.threads;
   p.place = place_bytes(vec, p.threads, (p.twice ? 2 : 1) * es / 2, H, es);
   // two rows at a time where every group has several and their places fit
   for (p.rows = p.twice || one_row || T < 4 * (int64_t)sms * p.groups ? 1 : 2; p.rows >= 1; --p.rows) {
@@ -979,7 +981,7 @@ template <auto kernel, class... Q> cudaError_t launch(dim3 grid, dim3 block, int
 
 // Forward: a block a group, 1024 threads an SM.
 template <int DT, bool FULL> cudaError_t forward(const BlockArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a, false, false, 2, 1024, sms);
+  const Plan p = plan_for(a, false, false, 2, 1024, 1024, sms);
   if (p.rows == 0) {
     block_fwd_wide_kernel<DT><<<(unsigned)(a.T < sms ? a.T : sms), 1024, 0, s>>>(a);
     return cudaGetLastError();
@@ -997,12 +999,15 @@ template <int DT, bool FULL> cudaError_t forward(const BlockArgs& a, cudaStream_
 #undef JP_FORWARD_TWICE
 }
 
-// Backward: the groups of an SM in one block, of 512 threads.
+// Backward: the groups of an SM in one block, of 512 threads, or of 640 with 96 registers each where that makes room for a row more (bf16, 8192 rows:
+// 4095 columns 184 us with 16 elements a thread, 144 with 640 threads; 2047 107 and 74, 2560 68 and 57; with gates and layer norms 4095 358 and
+// 254, 2560 106 and 98; not for a third row: 24,496 x 1283 fp32 222 and 236).
 template <int DT, bool POST, bool FULL> cudaError_t backward(const BlockArgs& a, const Plan& p, dim3 g, cudaStream_t s) {
   constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
   const dim3 b(p.threads, p.groups);
   const int sums = p.groups > 1 ? (FULL ? 4 : 2) * (int)a.H * 4 : 0, rows = p.smem * p.groups, smem = rows > sums ? rows : sums;
-#define JP_BACKWARD(KIND, NU, R, TWICE) launch<block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL>>(g, b, smem, s, a, p.place)
+#define JP_BACKWARD(KIND, NU, R, TWICE) (TWICE || p.threads * p.groups <= 512 ? launch<block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL, 512>>(g, b, smem, s, a, p.place) \
+                                                                                : launch<block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL, 640>>(g, b, smem, s, a, p.place))
   if (p.twice) return p.kind == kAligned ? JP_BACKWARD(kAligned, 2 * V, 1, true) : p.kind == kShared ? JP_BACKWARD(kShared, 2 * V, 1, true) : JP_BACKWARD(kElements, 2 * E, 1, true);
   if constexpr (!FULL || DT == JP_F32)
     if (p.rows == 2) return p.kind == kAligned ? JP_BACKWARD(kAligned, V, 2, false) : p.kind == kShared ? JP_BACKWARD(kShared, V, 2, false) : JP_BACKWARD(kElements, E, 2, false);
@@ -1032,7 +1037,7 @@ cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms) {
 size_t block_workspace_bytes(int64_t T, int64_t H, int, int sms) { return (size_t)(T < sms ? T : sms) * kMaxSums * (size_t)H * sizeof(float); }
 
 cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms) {
-  const Plan p = plan_for(a, true, a.dtype == JP_BF16 && full(a, true), 4, 512, sms);      // (8192 x 4096 layer norms with gates: one row at a time 140 us, two 167)
+  const Plan p = plan_for(a, true, a.dtype == JP_BF16 && full(a, true), 4, 512, 640, sms);      // (8192 x 4096 layer norms with gates: one row at a time 140 us, two 167)
   const int grid = p.rows ? grid_for(a.T, p, p.groups, sms) : (int)(a.T < sms ? a.T : sms), n = p.rows == 0 || full(a, true) ? 4 : 2;
   const cudaError_t e = a.dtype == JP_BF16 ? backward<JP_BF16>(a, p, grid, n == 4, s) : backward<JP_F32>(a, p, grid, n == 4, s);
   if (e != cudaSuccess) return e;
