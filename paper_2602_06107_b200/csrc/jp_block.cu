@@ -108,6 +108,12 @@ template <int ES> __device__ __forceinline__ void sts_one(uint32_t at, const cha
 __device__ __forceinline__ void copy16(uint32_t to, const char* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void copy16(uint32_t to, const char* from, int bytes) {      // zeros behind the first `bytes`, which alone are read
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const char* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
 
 enum Kind { kAligned, kShared, kElements };                 // rows on 16 bytes; all matrices' rows at the same offsets to 16 bytes; neither
 
@@ -167,19 +173,17 @@ template <int DT, int KIND> struct Unit {
     }
     return r;
   }
-  // what belongs to other rows, in the places `at` of NT matrices, reads 0 from here on
-  template <int NT> __device__ __forceinline__ void mask(uint32_t at, int place, int u) const {
+  // kShared: the row's first vector, in the places `at` of NT matrices: what belongs to the row before reads 0 from here on
+  template <int NT> __device__ __forceinline__ void mask(uint32_t at, int place) const {
+    uint4 v[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) v[t] = lds16(at + t * place);
     uint32_t keep[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (ES == 2) keep[i] = (inside(u, 2 * i) ? 0xffffu : 0u) | (inside(u, 2 * i + 1) ? 0xffff0000u : 0u);
-      else keep[i] = inside(u, i) ? 0xffffffffu : 0u;
-    }
+    for (int i = 0; i < 4; ++i) keep[i] = (first + 2 * i >= 0 ? 0xffffu : 0u) | (first + 2 * i + 1 >= 0 ? 0xffff0000u : 0u);
 #pragma unroll
-    for (int t = 0; t < NT; ++t, at += place) {
-      const uint4 v = lds16(at);
-      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x & keep[0]), "r"(v.y & keep[1]), "r"(v.z & keep[2]), "r"(v.w & keep[3]) : "memory");
-    }
+    for (int t = 0; t < NT; ++t)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + t * place), "r"(v[t].x & keep[0]), "r"(v[t].y & keep[1]), "r"(v[t].z & keep[2]), "r"(v[t].w & keep[3]) : "memory");
   }
   // `at`: the thread's first unit of the row
   __device__ __forceinline__ void store(char* at, int u, const Raw& r) const {
@@ -262,7 +266,7 @@ template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring
   int place;
   unsigned there;                                           // bits: there is such a matrix
   __device__ __forceinline__ Ring(const BlockArgs& A_) : A(A_) {}
-  // 16 bytes of a row's covering vectors; those that reach beyond the matrix, in its first and last row, element by element
+  // kElements: 16 bytes of a row's covering vectors; those that reach beyond the matrix, in its first and last row, element by element
   __device__ __forceinline__ void copy(uint32_t to, const char* from, const char* row, int bytes) const {
     if ((next == 0u || next == (unsigned)A.T - 1u) && (from < row || from + 16 > row + bytes)) {
 #pragma unroll 1
@@ -270,6 +274,20 @@ template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring
         if (from + q >= row && from + q < row + bytes) sts_one<ES>(to + q, from + q);
     } else {
       copy16(to, from);
+    }
+  }
+  // kShared: the row's first vector, which begins in front of the row.  fp32: the row's words of it (the others are never written); bf16: all of it,
+  // to be masked, but for a first row its elements.  `bytes`: up to the row's end
+  __device__ __forceinline__ void copy_first(const Un& un, uint32_t to, const char* from, int bytes) const {
+    if (ES == 2 && next != 0u) {
+      copy16(to, from, bytes);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 16; q += ES)
+        if (q >= -un.first * ES && q < bytes) {
+          if (ES == 4) copy4(to + q, from + q);
+          else sts_one<ES>(to + q, from + q);
+        }
     }
   }
   __device__ __forceinline__ void fetch(const Un& un) {
@@ -284,8 +302,10 @@ template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring
             for (int u = 0; u < NU; ++u)
               if (un.have >> u & 1u) {
                 const char* const from = at + u * (int)blockDim.x * 16;
-                if (KIND == kShared && (un.part >> u & 1u)) copy(to + u * blockDim.x * 16, from, at - un.first * ES, un.H * ES);
-                else copy16(to + u * blockDim.x * 16, from);
+                const int left = (un.H - un.column(u, 0)) * ES, bytes = left < 16 ? left : 16;
+                if (KIND != kShared) copy16(to + u * blockDim.x * 16, from);
+                else if (u == 0 && un.first < 0) copy_first(un, to, from, bytes);
+                else copy16(to + u * blockDim.x * 16, from, bytes);
               }
           } else {
             const char* const row = row_at<ES>(IN::base(A, t), IN::ld(A, t), next, 0);
@@ -308,7 +328,7 @@ template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring
     next = first;
     step = step_;
     if constexpr (VEC) {                                    // what is never fetched reads 0
-      if (un.have != (1u << NU) - 1u || there != (1u << NT) - 1u || (int64_t)first + (int64_t)(STAGES - 1) * step >= A.T)
+      if (un.have != (1u << NU) - 1u || un.first < 0 || there != (1u << NT) - 1u || (int64_t)first + (int64_t)(STAGES - 1) * step >= A.T)
         for (uint32_t at = mem; at != end; at += place)
 #pragma unroll
           for (int u = 0; u < NU; ++u)
@@ -320,12 +340,9 @@ template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring
   template <int R> __device__ __forceinline__ void wait(const Un& un) {   // for the oldest R rows
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - R) : "memory");
     if (!VEC) group_sync<SOLE>();
-    if (KIND == kShared && un.part != 0u) {                 // (a place is the thread's own)
+    if (KIND == kShared && ES == 2 && un.first < 0) {        // (a place is the thread's own)
 #pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-          if (un.part >> u & 1u) un.template mask<NT>(row(r) + u * blockDim.x * 16, place, u);
+      for (int r = 0; r < R; ++r) un.template mask<NT>(row(r), place);
     }
   }
   __device__ __forceinline__ uint32_t row(int r) const {      // the r-th oldest row's places
@@ -1006,12 +1023,17 @@ template <int DT, bool POST, bool FULL> cudaError_t backward(const BlockArgs& a,
   constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
   const dim3 b(p.threads, p.groups);
   const int sums = p.groups > 1 ? (FULL ? 4 : 2) * (int)a.H * 4 : 0, rows = p.smem * p.groups, smem = rows > sums ? rows : sums;
-#define JP_BACKWARD(KIND, NU, R, TWICE) (TWICE || p.threads * p.groups <= 512 ? launch<block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL, 512>>(g, b, smem, s, a, p.place) \
-                                                                                : launch<block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL, 640>>(g, b, smem, s, a, p.place))
-  if (p.twice) return p.kind == kAligned ? JP_BACKWARD(kAligned, 2 * V, 1, true) : p.kind == kShared ? JP_BACKWARD(kShared, 2 * V, 1, true) : JP_BACKWARD(kElements, 2 * E, 1, true);
+#define JP_BACKWARD(THREADS, KIND, NU, R, TWICE) launch<block_bwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), POST, FULL, THREADS>>(g, b, smem, s, a, p.place)
+#define JP_KINDS(THREADS, VECTORS, ELEMENTS, R, TWICE) (p.kind == kAligned ? JP_BACKWARD(THREADS, kAligned, VECTORS, R, TWICE) : p.kind == kShared ? JP_BACKWARD(THREADS, kShared, VECTORS, R, TWICE) \
+                                                                                             : JP_BACKWARD(THREADS, kElements, ELEMENTS, R, TWICE))
+  if (p.twice) return JP_KINDS(512, 2 * V, 2 * E, 1, true);
+  const bool many = p.threads * p.groups > 512;
+  if constexpr (!FULL && DT == JP_BF16)
+    if (many && p.rows == 2) return JP_KINDS(640, V, E, 2, false);
   if constexpr (!FULL || DT == JP_F32)
-    if (p.rows == 2) return p.kind == kAligned ? JP_BACKWARD(kAligned, V, 2, false) : p.kind == kShared ? JP_BACKWARD(kShared, V, 2, false) : JP_BACKWARD(kElements, E, 2, false);
-  return p.kind == kAligned ? JP_BACKWARD(kAligned, V, 1, false) : p.kind == kShared ? JP_BACKWARD(kShared, V, 1, false) : JP_BACKWARD(kElements, E, 1, false);
+    if (p.rows == 2) return JP_KINDS(512, V, E, 2, false);      // (with 640 threads in fp32 their places do not fit)
+  return many ? JP_KINDS(640, V, E, 1, false) : JP_KINDS(512, V, E, 1, false);
+#undef JP_KINDS
 #undef JP_BACKWARD
 }
 template <int DT> cudaError_t backward(const BlockArgs& a, const Plan& p, int grid, bool full, cudaStream_t s) {
