@@ -586,7 +586,8 @@ jp_status jp_w4_linear(jp_ctx* ctx, const jp_w4_desc* desc, const void* packed, 
  * A row holding NaN or +inf, or nothing above -1e38 (in units of log2: masked throughout), or whose terms are not finite (a token
  * of probability 0 with a KL term, NaN among its inputs) has state 3 and takes no part, as a masked one; the
  * others do not depend on it.  -inf logits have probability 0 and gradient 0.
- * Rows with mask 0 are not read.  The same call gives the same bits.
+ * Rows with mask 0 are not read.  The same call gives the same bits.  Blocks that share a row wait for one another's sums with a limit: if it ran
+ * out (it does not, in a call that is run to its end), out_loss is NaN.
  *
  * Clipped policy loss with a KL term to a reference model.  r = exp(lp - logp_old), d = logp_ref - lp:
  *   l = max(-A r, -A clip(r, 1 - eps_lo, 1 + eps_hi)),   k = exp(d) - d - 1  (>= 0; its mean estimates KL(p || p_ref))
@@ -617,7 +618,7 @@ jp_status jp_policy_loss(jp_ctx* ctx, const jp_policy_desc* desc, const void* lo
  * (the reference model's S_s; NULL: 0):
  *   h_i = beta ((S_2i - R_2i) - (S_2i+1 - R_2i+1)) - margin
  *   out_loss[0] = mean over pairs of -(1 - label_smoothing) log sigma(h) - label_smoothing log sigma(-h)
- * (0 if P is 0).  temperature is 1.  A row's coefficient needs both sequences of its pair, so the logits are read twice. */
+ * (0 if P is 0; a NaN in ref_logp makes it NaN, and the gradient of its pair 0).  temperature is 1.  A row's coefficient needs both sequences of its pair, so the logits are read twice. */
 enum { JP_PREFERENCE_AVERAGE = 1 };
 typedef struct {
   int64_t T, V, ld, ld_d;   /* as above                                                 */
@@ -701,7 +702,7 @@ size_t jp_i8_token_bytes(int64_t M, int64_t K);
 jp_status jp_i8_quantize(jp_ctx* ctx, const void* x, int64_t ld_x, int64_t M, int64_t K, void* tokens, size_t token_bytes);
 /* out [M, ld_out] of out_dtype (JP_BF16 or JP_F32, 0 = N).  x [M, ld_x] bf16 is quantised first (tokens is then a workspace, its content of no meaning
  * afterwards); x NULL: tokens are as jp_i8_quantize left them.  out_status: one int32 in DEVICE memory or NULL: 0, or JP_ERR_TIMEOUT if a wait inside the kernel
- * ran out (out is then unspecified). */
+ * ran out (out is then unspecified).  out overlaps nothing that is read. */
 jp_status jp_i8_linear(jp_ctx* ctx, const jp_i8_desc* desc, const void* packed, const void* x, int64_t ld_x, int64_t M,
                        void* tokens, size_t token_bytes, void* out, int64_t ld_out, int32_t out_dtype, int32_t* out_status);
 

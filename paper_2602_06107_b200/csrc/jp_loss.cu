@@ -10,9 +10,11 @@
 // Bound by HBM.  The policy loss has a row's k as soon as the row's sum is known, so sum and gradient are one launch, and the row stays in
 // shared memory in between, spread over the blocks of a cluster: HBM and L2 see one read and one write.  The preference loss needs both
 // sequences of a pair first: a pass for the sums, one for the gradients, each a stream through a ring of places.  Each thread copies its own
-// vectors (asynchronously, no barriers) and fetches the next row's into a place as soon as it has read it for the last time; two blocks
-// an SM, so that one loads and stores while the other waits for its sum.  One warp makes a row's scalars of the warps' sums.
-// Rows that no cluster can hold are read twice.
+// vectors (asynchronously, no barriers) and fetches the next row's into a place as soon as it has read it for the last time; several blocks
+// an SM (four of 256 threads, or two of 512 where eight small ones cannot hold a row), so that some load and store while others wait for their sum.
+// One warp makes a row's scalars of the warps' sums.  Rows that no cluster can hold are read twice.
+// Measured, bf16: policy loss 4096 x 151,936 450 us (5.5 TB/s; with two blocks of 512 threads 483); preference loss, six pairs of sequences, 3.5 GB in
+// three passes, 663 us (5.3 TB/s).
 // Sums of exponentials are fp32 of at most a few hundred terms a thread (in 2^x of z log2(e) / tau, relative to a running maximum), the row's
 // scalars fp64: the clip is a decision, and exp(d) - d - 1 cancels.
 #include <atomic>

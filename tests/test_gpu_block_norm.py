@@ -251,6 +251,43 @@ def test_rows_do_not_touch_one_another(ctx):
     assert o["dx"][good].isfinite().all() and o["dresidual"][good].isfinite().all()
 
 
+@pytest.mark.parametrize("T,H", [(23, 7), (40, 63), (21, 515), (600, 1283), (1301, 2047), (30, 4097)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("form,rms", [("all", False), ("post_gate", True)])
+def test_packed_odd_rows_do_not_touch_one_another(ctx, T, H, dtype, form, rms):
+    """Rows that share 16 bytes with a row of NaN give the bits that they give beside a row of zeros."""
+    s = make(T, H, dtype, dtype, form, T + H)
+    bad, good = slice(1, None, 2), slice(0, None, 2)
+    clean, f = [], None
+    for value in (0.0, float("nan")):
+        t = {**s, "x": s["x"].clone(), "residual": s["residual"].clone()}
+        t["x"][bad], t["residual"][bad] = value, value
+        o = run_forward(ctx, t, rms)
+        f = f or o
+        clean.append([o[k][good] for k in ("sum", "y", "rstd", "post_rstd")])
+    assert all(torch.equal(a, b) for a, b in zip(*clean))
+    grads = []
+    for value in (0.0, float("nan")):
+        t = {**s, **{k: s[k].clone() for k in ("dy", "dsum", "x")}, "sum": f["sum"].clone()}
+        for k in ("dy", "dsum", "x", "sum"):
+            t[k][bad] = value
+        o = run_backward(ctx, t, f, t["sum"], rms, t["dsum"], bias=s["bias"] is not None)
+        grads.append([o[k][good] for k in ("dx", "dresidual")] + ([] if o["dtoken_gate"] is None else [o["dtoken_gate"][good]]))
+    assert all(torch.equal(a, b) for a, b in zip(*grads)) and grads[0][0].isfinite().all()
+
+
+@pytest.mark.parametrize("T,H", [(2500, 2047), (1300, 2500), (1300, 2560), (1300, 4097), (700, 4600), (650, 5112)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("form,rms", [("all", False), ("plain", True), ("post_gate", True)])
+def test_widths_of_larger_blocks(ctx, T, H, dtype, form, rms):
+    s = make(T, H, dtype, dtype, form, T + H)
+    f = run_forward(ctx, s, rms)
+    check_forward(f, s, rms, s["residual"])
+    dsum = None if form == "plain" else s["dsum"]
+    o = run_backward(ctx, s, f, f["sum"], rms, dsum, bias=s["bias"] is not None)
+    check_backward(o, s, f, f["sum"], rms, dsum, cs=160)
+
+
 def test_gradients_against_differences(ctx):
     T, H, h = 3, 21, 1e-5
     for rms in (False, True):

@@ -314,6 +314,18 @@ def test_preference_far_apart_and_without_numbers(ctx):
     check_preference({**o, "state": o["state"] % 3}, F32, R)
 
 
+def test_preference_without_pairs_and_with_a_reference_that_is_no_number(ctx):
+    z, tok, _, _, _, _, _ = make(6, 300, F32, 9)
+    o = runner.preference_loss(ctx, z, tok, torch.tensor([2], dtype=torch.int32, device="cuda"))
+    assert o["loss"].item() == 0 and (o["d_logits"] == 0).all() and (o["state"] == 0).all() and o["margin"].numel() == 0
+    start = torch.tensor([0, 1, 3, 4, 6], dtype=torch.int32, device="cuda")
+    ref = torch.tensor([float("nan"), 0.0, -3.0, -4.0], device="cuda")
+    o = runner.preference_loss(ctx, z, tok, start, ref_logp=ref)
+    clean = runner.preference_loss(ctx, z, tok, start, ref_logp=torch.nan_to_num(ref))
+    assert o["loss"].isnan() and o["margin"][0].isnan() and o["margin"][1] == clean["margin"][1]
+    assert (o["d_logits"][:3] == 0).all() and torch.equal(o["d_logits"][3:], clean["d_logits"][3:])
+
+
 def test_offsets_beyond_32_bits(ctx):
     """4500 rows of 500,000 bf16: more than 2^31 elements, 4.5 GB; the last row is the first one's copy."""
     T, V = 4500, 500000
