@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libjackpot.so")
 SOURCES = ["jp_api.cu", "jp_stream.cu", "jp_epilogue.cu", "jp_grad.cu", "jp_noalloc.cu", "jp_probe.cu", "jp_rowlambda.cu", "jp_vshard.cu", "jp_sparse.cu", "jp_lmhead.cu", "jp_norm.cu", "jp_w4.cu", "jp_verify.cu", "jp_loss.cu", "jp_block.cu", "jp_i8.cu"]
-HEADERS = ["jp_common.cuh", "jp_internal.h"]
+HEADERS = ["jp_common.cuh", "jp_internal.h", "jp_pairs.cuh"]
 
 
 def _newest_source() -> float:

@@ -21,6 +21,7 @@
 // with layer norms, biases and a gate a token, backward, 126 and 245 us.
 #include "jp_common.cuh"
 #include "jp_internal.h"
+#include "jp_pairs.cuh"
 
 namespace jp {
 namespace {

@@ -145,9 +145,4 @@ __device__ __forceinline__ void stg_stream(uint4* p, const uint4& v) {
                : "memory");
 }
 
-// ---- two fp32 operations in one instruction --------------------------------
-__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
-
 }  // namespace jp

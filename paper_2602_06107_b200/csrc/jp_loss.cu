@@ -21,6 +21,7 @@
 
 #include "jp_common.cuh"
 #include "jp_internal.h"
+#include "jp_pairs.cuh"
 
 namespace jp {
 namespace {

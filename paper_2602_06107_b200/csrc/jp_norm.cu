@@ -76,9 +76,23 @@ template <int DT> struct Access<DT, 1> {
   }
 };
 
-// Two fp32 operations in one instruction (add2, mul2, fma2): at 8192 x 4096 both passes are as much bound by issue as by HBM (forward with bias 31 us
+// Two fp32 operations in one instruction: at 8192 x 4096 both passes are as much bound by issue as by HBM (forward with bias 31 us
 // without, 28.9; backward of RMS norm 41, 39.4).  xhat is (x - mu) r in two of them, not x r + (-mu r) in one: rounding mu r would leave
 // 2^-24 |mu| r in every xhat, a thousand times its own rounding in a row whose mean is a thousand standard deviations.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  asm("{.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;}" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
+  return a;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  asm("{.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;}" : "+f"(a.x), "+f"(a.y) : "f"(b.x), "f"(b.y));
+  return a;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  asm("{.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%0, %1};\n\tfma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;}"
+      : "+f"(c.x), "+f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
