@@ -1332,6 +1332,7 @@ jp_status jp_i8_linear(jp_ctx* c, const jp_i8_desc* d, const void* packed, const
     if (!packed || !out) return fail(c, JP_ERR_INVALID_ARG, "packed or out is NULL");
     if (!aligned16(packed)) return fail(c, JP_ERR_ALIGNMENT, "packed must be 16-byte aligned");
     if (!element_aligned(out, out_dtype)) return fail(c, JP_ERR_ALIGNMENT, "out must be aligned to its elements");
+    if (out == x) return fail(c, JP_ERR_INVALID_ARG, "out and x are the same matrix");
   }
   if (out_status) {
     const cudaError_t e = cudaMemsetAsync(out_status, 0, sizeof(int32_t), c->stream);

@@ -253,3 +253,10 @@ def test_status_and_refusals(ctx):
     call()
     assert status.item() == 0
     check(out, x, q, scales)
+
+
+@pytest.mark.parametrize("M", [1, 5])
+def test_out_in_the_place_of_x_is_refused(ctx, M):
+    x, q, scales = make(M, 64, 64, 2)
+    with pytest.raises(B.JackpotError, match="the same matrix"):
+        runner.linear_i8(ctx, x, runner.pack_i8(ctx, q, scales), out=x)
