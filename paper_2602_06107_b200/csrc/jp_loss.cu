@@ -13,8 +13,9 @@
 // vectors (asynchronously, no barriers) and fetches the next row's into a place as soon as it has read it for the last time; several blocks
 // an SM (four of 256 threads, or two of 512 where eight small ones cannot hold a row), so that some load and store while others wait for their sum.
 // One warp makes a row's scalars of the warps' sums.  Rows that no cluster can hold are read twice.
-// Measured, bf16: policy loss 4096 x 151,936 450 us (5.5 TB/s; with two blocks of 512 threads 483); preference loss, six pairs of sequences, 3.5 GB in
-// three passes, 663 us (5.3 TB/s).
+// Measured, bf16, V = 151,936: policy loss, 4096 rows of which some are masked, 2.2 GB, 444 us (5.0 TB/s; with two blocks of 512 threads 483 instead
+// of 450, with five of 192 474); preference loss, six pairs of sequences, 3.5 GB in three passes, 646 us (5.4 TB/s).  Vectors are counted in
+// 32 bits: their addresses in 64 cost 1 to 3 %.
 // Sums of exponentials are fp32 of at most a few hundred terms a thread (in 2^x of z log2(e) / tau, relative to a running maximum), the row's
 // scalars fp64: the clip is a decision, and exp(d) - d - 1 cancels.
 #include <atomic>
@@ -155,9 +156,9 @@ template <int DT> __device__ __forceinline__ void add_tail(const char* z, int64_
   s = s * ex2_approx(m - top) + ex2_approx(fmaf(v, c, -top));
   m = top;
 }
-// Gradient of a vector, the i-th of the row: coef 1[v = x] - k 2^(z c - m), k = coef / s.  (The token's place is written once more: as an index into
+// Gradient of a vector: coef 1[v = x] - k 2^(z c - m), k = coef / s; `hit`: it holds the token.  (The token's place is written once more: as an index into
 // the vector it would go through local memory.)
-template <int DT> __device__ __forceinline__ void put_gradient(char* dz, uint4 v, float c, float m, float k, float coef, int64_t i, int64_t x) {
+template <int DT> __device__ __forceinline__ void put_gradient(char* to, uint4 v, float c, float m, float k, float coef, bool hit, int x) {
   constexpr int W = Vec<DT>::N;
   auto at = [&](int q) {
     const float2 y = fma2(value_pair<DT>(v, q), make_float2(c, c), make_float2(-m, -m));
@@ -170,10 +171,10 @@ template <int DT> __device__ __forceinline__ void put_gradient(char* dz, uint4 v
     g[2 * q] = t.x;
     g[2 * q + 1] = t.y;
   }
-  stg_stream((uint4*)dz + i, pack<DT>(g));
-  if (i == x / W) {
-    const float2 t = at((int)(x % W) / 2);
-    store_one<DT>(dz, x, coef + ((x & 1) ? t.y : t.x));
+  stg_stream((uint4*)to, pack<DT>(g));
+  if (hit) {
+    const float2 t = at(x % W / 2);
+    store_one<DT>(to, x % W, coef + ((x & 1) ? t.y : t.x));
   }
 }
 
@@ -203,7 +204,7 @@ template <int DT> __device__ __forceinline__ void row_gradient(const char* z, ch
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
       const int64_t i = i0 + j * (int)blockDim.x + threadIdx.x;
-      if (i < v1) put_gradient<DT>(dz, v[j], c, m, k, coef, i, x);
+      if (i < v1) put_gradient<DT>(dz + i * 16, v[j], c, m, k, coef, i == x / Vec<DT>::N, (int)x);
     }
   }
 }
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
   const int64_t vecs = A.V / W, each = (vecs + ranks - 1) / ranks;
   const int64_t v0 = each * rank < vecs ? each * rank : vecs, v1 = v0 + each < vecs ? v0 + each : vecs;
   const int64_t tail0 = rank == ranks - 1 ? vecs * W : A.V;       // the last block has what is left behind the vectors
-  const int64_t mine = v1 - v0 - threadIdx.x;                     // vector i is there if i * kThreads < mine
+  const int mine = (int)(v1 - v0) - (int)threadIdx.x;             // vector i is there if i * kThreads < mine (a row has less than 2^29)
   const int turns = NV > 0 ? (int)((v1 - v0 + NV * kThreads - 1) / (NV * kThreads > 0 ? NV * kThreads : 1)) : 0;       // of the ring, a row
   const uint32_t place = (uint32_t)__cvta_generic_to_shared(places) + threadIdx.x * 16;
   const int64_t first = (v0 + threadIdx.x) * 16;                  // bytes from a row's start to the thread's first vector
@@ -372,10 +373,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
     if (MODE == kPrefSums && (row < lo || row >= hi)) x = -1;
     return x < A.V ? x : -1;
   };
-  // vector i of the n-th row, or an empty group of copies
-  auto fetch = [&](int64_t n, int slot, int64_t i) {
-    if (n < A.T && i * kThreads < mine)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place + slot * kThreads * 16), "l"((const char*)A.z + nth(n) * A.ld * ES + first + i * (kThreads * 16)) : "memory");
+  // where the thread's first vector of the n-th row is, and `mine` of it (0 behind the last row)
+  auto source = [&](int64_t n) { return (const char*)A.z + (n < A.T ? nth(n) : 0) * A.ld * ES + first; };
+  auto mine_of = [&](int64_t n) { return n < A.T ? mine : 0; };
+  // vector i of a row, or an empty group of copies
+  auto fetch = [&](const char* row, int have, int slot, int i) {
+    if (i * kThreads < have)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place + slot * kThreads * 16), "l"(row + (int64_t)i * (kThreads * 16)) : "memory");
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   // `next`: the next of this cluster's rows that takes part, with its token; `ahead`: the token of the row behind it, read a row's time before
@@ -393,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
   };
   advance();
 #pragma unroll
-  for (int i = 0; i < NV; ++i) fetch(next, i, i);
+  for (int i = 0; i < NV; ++i) fetch(source(next), mine_of(next), i, i);
   const double inv_n = MODE == kPolicy || MODE == kPolicyNoGrad ? inverse_count(sh, A.mask, A.T, A.n_valid) : 0.0;
   for (int64_t count = 0;; ++count) {
     for (; n < next; n += clusters) {         // rows that take no part
@@ -406,6 +410,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
     advance();
     const char* z = (const char*)A.z + row * A.ld * ES;
     char* dz = (char*)A.dz + row * A.ld_d * ES;
+    const char* const next_row = source(next);
+    const int next_mine = mine_of(next);
     float m = 0.f, k = 0.f, coef = 0.f;
     if (MODE == kPrefGrad) {
       coef = A.row_coef[row];
@@ -432,14 +438,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
         for (int turn = 0; turn < (STREAM ? turns : 1); ++turn) {
 #pragma unroll
           for (int u = 0; u < NV; ++u) {
-            const int64_t i = turn * NV + u;
+            const int i = turn * NV + u;
             wait_copies(STREAM ? NV - 1 : NV - 1 - u);
             uint4 v;
             const bool have = i * kThreads < mine;
             if (have) v = lds16(place + u * kThreads * 16);
             if (STREAM) {
-              if (turn + 1 < turns) fetch(n, u, i + NV);
-              else fetch(next, u, u);
+              if (turn + 1 < turns) fetch(z + first, mine, u, i + NV);
+              else fetch(next_row, next_mine, u, u);
             }
             if (have) add_vector<DT>(v, A.c, top, sum);
           }
@@ -468,20 +474,21 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
         if (coef != 0.f) row_gradient<DT>(z, dz, v0, v1, A.c, m, k, coef, x);
         else row_zeros<DT>(dz, v0, v1, A.V, A.V);
       } else {
+        const int token_at = (int)(x / W - v0) - (int)threadIdx.x;
         for (int turn = 0; turn < (STREAM ? turns : 1); ++turn) {
 #pragma unroll
           for (int u = 0; u < NV; ++u) {
-            const int64_t i = turn * NV + u;
+            const int i = turn * NV + u;
             if (STREAM) wait_copies(NV - 1);
             uint4 v;
             const bool have = i * kThreads < mine;
             if (have) v = lds16(place + u * kThreads * 16);
-            if (STREAM && turn + 1 < turns) fetch(n, u, i + NV);
-            else fetch(next, u, u);
+            if (STREAM && turn + 1 < turns) fetch(z + first, mine, u, i + NV);
+            else fetch(next_row, next_mine, u, u);
             if (have) {
-              const int64_t at = v0 + threadIdx.x + i * kThreads;
-              if (coef != 0.f) put_gradient<DT>(dz, v, A.c, m, k, coef, at, x);
-              else stg_stream((uint4*)dz + at, make_uint4(0u, 0u, 0u, 0u));
+              char* const to = dz + first + (int64_t)i * (kThreads * 16);
+              if (coef != 0.f) put_gradient<DT>(to, v, A.c, m, k, coef, i * kThreads == token_at, (int)x);
+              else stg_stream((uint4*)to, make_uint4(0u, 0u, 0u, 0u));
             }
           }
         }
