@@ -673,10 +673,20 @@ template <int DT, int MODE, int kThreads> cudaError_t resident(LossArgs a, int64
 
 template <int DT, int MODE> cudaError_t rows(LossArgs a, cudaStream_t s, int sms) {
   const int64_t vecs = (a.V + Vec<DT>::N - 1) / Vec<DT>::N;
+  // Many short rows: a row's latency (barriers, its scalars) decides, so more of them at a time in smaller blocks, where four rows an SM are not
+  // all of them.  bf16, us, with blocks of 256 and 512 threads in brackets: policy loss 65,536 x 1000 144 (242), 65,536 x 2000 173 (264), 30,000 x
+  // 5003 151 (190); preference loss, 64 pairs of up to 512 rows, V = 1000 151 (449), 32 of 256, V = 5003 97 (161).
+  const bool narrow = a.T > (int64_t)sms * 4;
+  a.cluster = 1;
   if constexpr (MODE != kPolicy) {
+    if (narrow && vecs <= 64 * 4) return rows_of<2, 64, DT, MODE>(a, s, sms);
+    if (narrow && vecs <= 128 * 8) return rows_of<8, 128, DT, MODE>(a, s, sms);
     a.cluster = cluster_for(a.T, vecs, 512, 0, sms);
     return vecs <= (int64_t)a.cluster * 2 * 512 ? rows_of<2, 512, DT, MODE>(a, s, sms) : rows_of<8, 512, DT, MODE>(a, s, sms);
   } else {
+    if (narrow && vecs <= 64 * 2) return rows_of<2, 64, DT, MODE>(a, s, sms);
+    if (narrow && vecs <= 64 * 4) return rows_of<4, 64, DT, MODE>(a, s, sms);
+    if (narrow && vecs <= 128 * 7) return rows_of<7, 128, DT, MODE>(a, s, sms);
     // four rows' blocks an SM where eight blocks of 256 threads hold a row, two where it takes eight of 512
     if (vecs <= (int64_t)kMaxCluster * 256 * kMostVectors) {
       a.cluster = cluster_for(a.T, vecs, 256, kMostVectors, sms);

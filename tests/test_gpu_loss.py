@@ -294,6 +294,16 @@ def test_preference_matches_the_formula(ctx, P, most, V, dtype, average, eps):
     assert torch.equal(z, o["d_logits"]) and torch.equal(inside["loss"], o["loss"])
 
 
+@pytest.mark.parametrize("V", [5, 513, 1030, 2049, 4100, 7167, 7180, 8200])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_many_short_rows(ctx, V, dtype):
+    """More rows than four an SM, by length."""
+    for form in ("all", "bare"):
+        test_policy_matches_the_formula(ctx, 1311, V, dtype, form)
+    for average, eps in ((False, 0.0), (True, 0.1)):
+        test_preference_matches_the_formula(ctx, 40, 60, V, dtype, average, eps)
+
+
 def test_preference_far_apart_and_without_numbers(ctx):
     """Pairs far apart on either side keep the small sigma; a row without numbers leaves its sequence's others."""
     T, V = 8, 300
