@@ -587,7 +587,7 @@ jp_status jp_w4_linear(jp_ctx* ctx, const jp_w4_desc* desc, const void* packed, 
  * of probability 0 with a KL term, NaN among its inputs) has state 3 and takes no part, as a masked one; the
  * others do not depend on it.  -inf logits have probability 0 and gradient 0.
  * Rows with mask 0 are not read.  The same call gives the same bits.  Blocks that share a row wait for one another's sums with a limit: if it ran
- * out (it does not, in a call that is run to its end), out_loss is NaN.
+ * out in any of them (it does not, in a call that is run to its end), out_loss is NaN.
  *
  * Clipped policy loss with a KL term to a reference model.  r = exp(lp - logp_old), d = logp_ref - lp:
  *   l = max(-A r, -A clip(r, 1 - eps_lo, 1 + eps_hi)),   k = exp(d) - d - 1  (>= 0; its mean estimates KL(p || p_ref))
@@ -711,7 +711,9 @@ jp_status jp_i8_linear(jp_ctx* ctx, const jp_i8_desc* desc, const void* packed, 
  * cores complete) gives up after a fixed number of SM clock cycles, sets JP_ERR_TIMEOUT in a
  * device status word and lets the kernel end instead of trapping or hanging.  This call runs
  * that routine against a barrier nobody completes, with a limit of limit_cycles (1 .. 2e9:
- * about a second at most): out_status (one int32, DEVICE) must read JP_ERR_TIMEOUT afterwards
+ * about a second at most), then the losses' exchange between two blocks, one of which sends
+ * its part only after the other has given up: the part must still find the other one's memory
+ * (else JP_ERR_CUDA).  out_status (one int32, DEVICE) must read JP_ERR_TIMEOUT afterwards
  * and the context must work as before.  Enqueued on the context's stream; does not wait. */
 jp_status jp_selftest_bounded_wait(jp_ctx* ctx, int64_t limit_cycles, int32_t* out_status);
 

@@ -1366,8 +1366,9 @@ jp_status jp_selftest_bounded_wait(jp_ctx* c, int64_t limit_cycles, int32_t* out
   cudaSetDevice(c->device);
   cudaError_t e = cudaMemsetAsync(out_status, 0, sizeof(int32_t), c->stream);
   if (e == cudaSuccess) e = launch_wait_selftest((long long)limit_cycles, out_status, c->stream);
+  if (e == cudaSuccess) e = launch_exchange_selftest((long long)limit_cycles, out_status, c->stream);
   if (e != cudaSuccess) return cuda_fail(c, e, "self-test launch");
-  c->launches += 1;
+  c->launches += 2;
   return JP_OK;
 }
 

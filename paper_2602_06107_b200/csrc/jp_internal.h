@@ -393,6 +393,7 @@ struct LossArgs {
 };
 size_t policy_workspace_bytes(int64_t T);
 cudaError_t launch_policy(LossArgs a, void* workspace, cudaStream_t s, int sms);
+cudaError_t launch_exchange_selftest(long long limit_cycles, int32_t* status, cudaStream_t s);   // status: left alone, or JP_ERR_CUDA
 size_t preference_workspace_bytes(int64_t T, int64_t P);
 cudaError_t launch_preference(LossArgs a, void* workspace, cudaStream_t s, int sms, int* n_launch);
 

@@ -57,12 +57,14 @@ template <int DT> __device__ __forceinline__ void store_one(void* row, int64_t i
   else ((float*)row)[i] = f;
 }
 
-struct Shared {
+// (Whole lines of 128 bytes, so that the places behind it start on one: 16 bytes off 32, every copy's line is split, which costs 4 to 8 %.)
+struct alignas(128) Shared {
   float2 warp[2][kMostThreads / 32];              // by the parity of the row's number, like what follows
   float2 part[2][kMaxCluster];                // of the cluster's blocks
   unsigned long long arrived[2];              // barriers that count the parts' bytes
   float top, k_over_s, coef;
   int count[kMostThreads / 32];
+  long long lost_row, lost_count;             // the row whose exchange gave up (-1: none did), and its number among the block's
 };
 constexpr long long kSpin = 4000000000ll;     // clock cycles after which a wait gives up
 
@@ -77,12 +79,28 @@ __device__ __forceinline__ float2 warp_merge(float2 v) {
   return make_float2(m, s);
 }
 
+__device__ __forceinline__ bool parts_are_here(uint32_t bar, uint32_t phase) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 1000;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(phase) : "memory");
+  return ok != 0u;
+}
+
+// By all threads of a cluster's blocks, before the first exchange.
+__device__ __forceinline__ void exchange_start(Shared& sh) {
+  if (threadIdx.x < 2) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&sh.arrived[threadIdx.x])) : "memory");
+  if (threadIdx.x == 0) sh.lost_row = -1;
+  if (threadIdx.x == 0) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
 // By one warp: the row's (maximum, sum) over the block's warps, then over the cluster's blocks, each of which sends its part to every other one's
-// shared memory (and gets the same total: the parts are merged in the same order).  A wait that gives up returns a sum below 0.
-__device__ __forceinline__ float2 row_total(Shared& sh, int rank, int ranks, int64_t count) {
+// shared memory (and gets the same total: the parts are merged in the same order).  A wait that gives up returns a sum below 0, and so does every row
+// of this block behind it: its barrier's phase is open still, and the others no longer hear of this block and give up in their turn.
+__device__ __forceinline__ float2 row_total(Shared& sh, int rank, int ranks, int64_t count, int64_t row, long long limit = kSpin) {
   const int p = (int)(count & 1), lane = threadIdx.x & 31;
   float2 v = warp_merge(lane < (int)blockDim.x / 32 ? sh.warp[p][lane] : make_float2(kFloor, 0.f));
   if (ranks == 1) return v;
+  if (sh.lost_row >= 0) return make_float2(0.f, -1.f);
   const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&sh.arrived[p]), at = (uint32_t)__cvta_generic_to_shared(&sh.part[p][rank]);
   if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ranks * 8) : "memory");
   if (lane < ranks) {
@@ -92,19 +110,38 @@ __device__ __forceinline__ float2 row_total(Shared& sh, int rank, int ranks, int
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to), "f"(v.x), "f"(v.y), "r"(theirs) : "memory");
   }
   const uint32_t phase = (uint32_t)(count >> 1) & 1u;
+  bool here = false;
   long long t0 = 0;
-  for (uint32_t i = 0;; ++i) {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 1000;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(phase) : "memory");
-    if (ok) break;
-    if ((i & 63u) == 0u) {
+  for (uint32_t i = 0; !here; ++i) {
+    here = parts_are_here(bar, phase);
+    if (!here && (i & 63u) == 0u) {
       const long long now = clock64();
       if (i == 0u) t0 = now;
-      else if (now - t0 > kSpin) return make_float2(0.f, -1.f);
+      else if (now - t0 > limit) break;
     }
+  }
+  if (__any_sync(0xffffffffu, !here)) {       // (for all lanes alike)
+    if (lane == 0) sh.lost_row = row, sh.lost_count = count;
+    __syncwarp();
+    return make_float2(0.f, -1.f);
   }
   v = warp_merge(lane < ranks ? sh.part[p][lane] : make_float2(kFloor, 0.f));
   return v;
+}
+
+// By all threads of a cluster's blocks, behind the last exchange.  A block leaves at once: it has all parts of its last row, so nothing is on its way
+// to it.  Not so one that gave up, and its shared memory has to stay until the others send no more: it waits until their threads have come here, then
+// (with a limit) for what they sent last, and long enough that their stores have arrived too.  True in that case, for its first warp.
+// (Arrivals that release those stores instead would cost every call 0.2 us.)
+__device__ __forceinline__ bool exchange_end(Shared& sh) {
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+  if (threadIdx.x >= 32 || sh.lost_row < 0) return false;
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&sh.arrived[sh.lost_count & 1]), phase = (uint32_t)(sh.lost_count >> 1) & 1u;
+  const long long t0 = clock64();
+  while (!parts_are_here(bar, phase) && clock64() - t0 < 1000000ll) {}
+  while (clock64() - t0 < 200000ll) {}
+  return true;
 }
 
 // The largest of a vector's values (NaN aside)
@@ -342,11 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
   constexpr int W = Vec<DT>::N, ES = Vec<DT>::ESIZE;
   constexpr bool STREAM = MODE != kPolicy, GRAD = MODE == kPolicy || MODE == kPrefGrad;
   const int ranks = A.cluster, rank = blockIdx.x % ranks, clusters = gridDim.x / ranks;
-  if (ranks > 1) {
-    if (threadIdx.x < 2) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&sh.arrived[threadIdx.x])) : "memory");
-    if (threadIdx.x == 0) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-  }
+  if (ranks > 1) exchange_start(sh);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int64_t vecs = A.V / W, each = (vecs + ranks - 1) / ranks;
@@ -458,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
       if (threadIdx.x < 32) {                 // (without a gradient the others go on with the next row)
         // the token's logit has arrived before the other blocks hear of this one: they may write the gradient over it
         if (MODE == kPolicy) asm volatile("{.reg .f32 t;\n\tmov.f32 t, %0;}" ::"f"(in.zx) : "memory");
-        const float2 all = row_total(sh, rank, ranks, count);
+        const float2 all = row_total(sh, rank, ranks, count, row);
         if (MODE == kPolicy && threadIdx.x == 0) sh.top = all.x;
         row_scalars<MODE>(A, sh, row, rank == 0, all, in, inv_n);
       }
@@ -500,6 +533,28 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) loss_rows_kernel(Lo
     }
     n += clusters;
   }
+  // a block that gave up: NaN in the loss, whatever the row's first block made of it
+  if (MODE != kPrefGrad && ranks > 1 && exchange_end(sh) && threadIdx.x == 0) {
+    const double none = __longlong_as_double(0x7ff8000000000000ll);
+    if (MODE == kPrefSums) A.row_lp[sh.lost_row] = none, A.row_used[sh.lost_row] = 1;
+    else A.term[sh.lost_row] = none;
+  }
+}
+
+// Two blocks, the second of which sends its part only after the first one has given up: the part has to find the first one's memory, and both end.
+__global__ void __launch_bounds__(64) exchange_selftest_kernel(long long limit, int32_t* status) {
+  __shared__ Shared sh;
+  const int rank = blockIdx.x;
+  exchange_start(sh);
+  if (threadIdx.x < 32) {
+    if (threadIdx.x < 2) sh.warp[0][threadIdx.x] = make_float2(3.f + rank, 1.f);
+    __syncwarp();
+    const long long t0 = clock64(), late = limit / 4 * 5 + 4000000ll;
+    while (rank == 1 && clock64() - t0 < late) {}
+    const float2 t = row_total(sh, rank, 2, 0, 0, limit);
+    if (threadIdx.x == 0 && (rank == 0 ? t.y >= 0.f : t.x != 4.f || t.y != 3.f)) atomicExch(status, (int)JP_ERR_CUDA);
+  }
+  if (exchange_end(sh) && threadIdx.x == 0 && (sh.part[0][1].x != 4.f || sh.part[0][1].y != 2.f)) atomicExch(status, (int)JP_ERR_CUDA);
 }
 
 __device__ __forceinline__ double warp_add(double v) {
@@ -702,6 +757,20 @@ template <int MODE> cudaError_t rows(const LossArgs& a, cudaStream_t s, int sms)
 }
 
 }  // namespace
+
+cudaError_t launch_exchange_selftest(long long limit_cycles, int32_t* status, cudaStream_t s) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(2);
+  cfg.blockDim = dim3(64);
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 2;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, exchange_selftest_kernel, limit_cycles, status);
+}
 
 namespace {
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
