@@ -269,9 +269,10 @@ template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring
   int place;
   unsigned there;                                           // bits: there is such a matrix
   __device__ __forceinline__ Ring(const BlockArgs& A_) : A(A_) {}
-  // kElements: 16 bytes of a row's covering vectors; those that reach beyond the matrix, in its first and last row, element by element
-  __device__ __forceinline__ void copy(uint32_t to, const char* from, const char* row, int bytes) const {
-    if ((next == 0u || next == (unsigned)A.T - 1u) && (from < row || from + 16 > row + bytes)) {
+  // kElements: 16 bytes of a row's covering vectors; in the rows whose vectors may reach beyond the matrix (`edge`), those that lie in part outside
+  // the row element by element
+  __device__ __forceinline__ void copy(uint32_t to, const char* from, const char* row, int bytes, bool edge) const {
+    if (edge && (from < row || from + 16 > row + bytes)) {
 #pragma unroll 1
       for (int q = 0; q < 16; q += ES)
         if (from + q >= row && from + q < row + bytes) sts_one<ES>(to + q, from + q);
@@ -280,9 +281,9 @@ template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring
     }
   }
   // kShared: the row's first vector, which begins in front of the row.  fp32: the row's words of it (the others are never written); bf16: all of it,
-  // to be masked, but for a first row its elements.  `bytes`: up to the row's end
+  // to be masked, but for a row that it could reach beyond the matrix of, its elements.  `bytes`: up to the row's end
   __device__ __forceinline__ void copy_first(const Un& un, uint32_t to, const char* from, int bytes) const {
-    if (ES == 2 && next != 0u) {
+    if (ES == 2 && next >= A.edge_rows) {
       copy16(to, from, bytes);
     } else {
 #pragma unroll
@@ -313,7 +314,8 @@ template <int DT, int KIND, int NU, class IN, int STAGES, bool SOLE> struct Ring
           } else {
             const char* const row = row_at<ES>(IN::base(A, t), IN::ld(A, t), next, 0);
             const int skip = (int)((uintptr_t)row & 15), bytes = un.H * ES;
-            for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) copy(to + i, row - skip + i, row, bytes);
+            const bool edge = next < A.edge_rows || next + A.edge_rows >= (unsigned)A.T;
+            for (int i = threadIdx.x * 16; i < skip + bytes; i += blockDim.x * 16) copy(to + i, row - skip + i, row, bytes, edge);
           }
         }
       next += step;
@@ -1054,7 +1056,15 @@ bool full(const BlockArgs& a, bool backward) { return !a.rms || a.token_gate || 
 
 }  // namespace
 
-cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms) {
+static uint32_t edge_rows(const BlockArgs& a, bool backward) {
+  const int64_t es = a.dtype == JP_BF16 ? 2 : 4, ld[4] = {a.ld_x, a.ld_sum, backward ? a.ld_dy : a.ld_residual, backward ? a.ld_dsum : a.ld_sum};
+  uint32_t n = 1;
+  for (int64_t v : ld) n = rows_near_an_end(v * es) > n ? rows_near_an_end(v * es) : n;
+  return n;
+}
+
+cudaError_t launch_block_forward(BlockArgs a, cudaStream_t s, int sms) {
+  a.edge_rows = edge_rows(a, false);
   if (a.dtype == JP_BF16) return full(a, false) ? forward<JP_BF16, true>(a, s, sms) : forward<JP_BF16, false>(a, s, sms);
   return full(a, false) ? forward<JP_F32, true>(a, s, sms) : forward<JP_F32, false>(a, s, sms);
 }
@@ -1062,7 +1072,8 @@ cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms) {
 // At most a line a block and SM, whatever the kernel.
 size_t block_workspace_bytes(int64_t T, int64_t H, int, int sms) { return (size_t)(T < sms ? T : sms) * kMaxSums * (size_t)H * sizeof(float); }
 
-cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms) {
+cudaError_t launch_block_backward(BlockArgs a, cudaStream_t s, int sms) {
+  a.edge_rows = edge_rows(a, true);
   const Plan p = plan_for(a, true, a.dtype == JP_BF16 && full(a, true), 4, 512, 640, sms);      // (8192 x 4096 layer norms with gates: one row at a time 127 us, two 130)
   const int grid = p.rows ? grid_for(a.T, p, p.groups, sms) : (int)(a.T < sms ? a.T : sms), n = p.rows == 0 || full(a, true) ? 4 : 2;
   const cudaError_t e = a.dtype == JP_BF16 ? backward<JP_BF16>(a, p, grid, n == 4, s) : backward<JP_F32>(a, p, grid, n == 4, s);

@@ -398,6 +398,8 @@ size_t preference_workspace_bytes(int64_t T, int64_t P);
 cudaError_t launch_preference(LossArgs a, void* workspace, cudaStream_t s, int sms, int* n_launch);
 
 // The norms around a block with gate and residual (jp_block.cu).
+// The rows at each end of a matrix whose covering 16-byte vectors may reach beyond it (pitches under 16 bytes: more than one).
+constexpr uint32_t rows_near_an_end(int64_t pitch_bytes) { return pitch_bytes < 16 ? (uint32_t)((15 + pitch_bytes) / pitch_bytes) : 1u; }
 struct BlockArgs {
   const void* x;           // [T, ld_x] the block's output
   const void* residual;    // forward: [T, ld_residual]
@@ -433,10 +435,11 @@ struct BlockArgs {
   float* dgate;
   float* dtoken_gate;      // [T]
   float* partial;          // backward: [blocks, sums, H] workspace
+  uint32_t edge_rows;      // set by the launch: rows_near_an_end of the smallest pitch
 };
-cudaError_t launch_block_forward(const BlockArgs& a, cudaStream_t s, int sms);
+cudaError_t launch_block_forward(BlockArgs a, cudaStream_t s, int sms);
 size_t block_workspace_bytes(int64_t T, int64_t H, int dtype, int sms);
-cudaError_t launch_block_backward(const BlockArgs& a, cudaStream_t s, int sms);
+cudaError_t launch_block_backward(BlockArgs a, cudaStream_t s, int sms);
 
 // Linear layers in 8-bit integers (jp_i8.cu).
 struct I8PackArgs {
