@@ -335,9 +335,11 @@ __device__ __forceinline__ void row_scalars(const LossArgs& A, Shared& sh, int64
     live = !(plain < clipped);
     if (!live) loss = clipped, slope = 0.0;
   }
-  if (A.logp_ref) {                           // (e - 1 loses 2^-53: of k = d^2 / 2 what lp's own error loses sooner)
-    kl = e1 - d;
-    slope -= (double)A.kl_coef * e1;
+  if (A.logp_ref) {
+    // e - 1 is off by 2^-53, of which d^2 / 2 next to 0 would be nothing: there, the series, off by 2^-48 of itself at most, and never below 0
+    const bool near = fabs(d) < 0x1p-10;
+    kl = near ? d * d * fma(d, fma(d, fma(d, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5) : e1 - d;
+    slope -= (double)A.kl_coef * (near ? kl + d : e1);
   }
   const double wt = (double)in.weight * inv_n;
   const float co = (float)(wt * slope * A.grad_scale);
