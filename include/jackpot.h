@@ -683,7 +683,8 @@ jp_status jp_block_norm_backward(jp_ctx* ctx, const jp_block_norm_desc* desc, co
  * quantised model over a prompt, or while it decodes more tokens than jp_w4_linear takes (nothing is kept in the context, as above):
  *   sx[m] = max_k |x[m, k]| / 127,  xq[m, k] = 127 x[m, k] / max_k |x[m, k]| rounded to the nearest integer (halves to even, exactly; 0 in a row of zeros)
  *   out[m, n] = sx[m] scales[n] sum_k xq[m, k] q[n, k]
- * Sums are exact (int32), out is rounded from fp32 once.  A token that holds NaN or an infinity gives NaN, the others do not depend on it.
+ * Sums are exact (int32); out is off by 2^-22 of itself at most, with any finite scales, and rounded to its type (sx is held in fp32: a token whose
+ * max |x| is below 127 2^-126 has 2^-150 / sx in addition).  A token that holds NaN or an infinity gives NaN, the others do not depend on it.
  *
  * jp_i8_pack lays the weights out once: q [N, ld_q] int8 (DEVICE, any value), scales [N] fp32, packed of jp_i8_packed_bytes(N, K)
  * bytes (16-byte aligned).  jp_i8_linear takes the same N and K. */
