@@ -672,28 +672,36 @@ cudaError_t launch(K kernel, const LossArgs& a, unsigned grid, unsigned threads,
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-// Clusters of c blocks that the GPU holds at once (fewer than its SMs would, where c does not divide what shares their memory); asked once for
-// each kernel and size, since the answer is always the same.
+// Clusters of c blocks that the GPU holds at once (fewer than its SMs' threads would, where c does not divide what shares their memory, or the memory of a
+// block does not go so often into an SM's); asked once for each kernel, size and device, since the answer is always the same.
 template <auto kernel, int kThreads> int clusters_at_once(int c, int smem, int sms) {
-  static std::atomic<int> known[kMaxCluster + 1];
-  if (c == 1) return sms * (1024 / kThreads);
-  int n = known[c].load(std::memory_order_relaxed);
-  if (n > 0) return n;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(sms * (1024 / kThreads) / c * c));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = c;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices][kMaxCluster + 1];
+  int device = 0, n = 0;
+  const bool keep = cudaGetDevice(&device) == cudaSuccess && device < kDevices;
+  if (keep && (n = known[device][c].load(std::memory_order_relaxed)) > 0) return n;
+  cudaError_t e;
+  if (c == 1) {
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kThreads, smem);
+    n *= sms;
+  } else {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(sms * (1024 / kThreads) / c * c));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = c;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+  }
+  if (e != cudaSuccess || n < 1) {
     cudaGetLastError();
     return sms * (1024 / kThreads) / c;
   }
-  known[c].store(n, std::memory_order_relaxed);
+  if (keep) known[device][c].store(n, std::memory_order_relaxed);
   return n;
 }
 
