@@ -11,7 +11,7 @@
 // shared memory in between, spread over the blocks of a cluster: HBM and L2 see one read and one write.  The preference loss needs both
 // sequences of a pair first: a pass for the sums, one for the gradients, each a stream through a ring of places.  Each thread copies its own
 // vectors (asynchronously, no barriers) and fetches the next row's into a place as soon as it has read it for the last time; several blocks
-// an SM (four of 256 threads, or two of 512 where eight small ones cannot hold a row), so that some load and store while others wait for their sum.
+// an SM (four of 256 threads where 13 vectors a thread hold a row, or two of 512 where eight small ones cannot), so that some load and store while others wait for their sum.
 // One warp makes a row's scalars of the warps' sums.  Rows that no cluster can hold are read twice.
 // Measured, bf16, V = 151,936: policy loss, 4096 rows of which some are masked, 2.2 GB, 444 us (5.0 TB/s; with two blocks of 512 threads 483 instead
 // of 450, with five of 192 474); preference loss, six pairs of sequences, 3.5 GB in three passes, 646 us (5.4 TB/s).  Vectors are counted in
@@ -652,7 +652,7 @@ __global__ void __launch_bounds__(1024) preference_pairs_kernel(LossArgs A) {
   }
 }
 
-constexpr int kMostVectors = 14;              // a thread: 112 KB a block, two blocks an SM
+constexpr int kMostVectors = 14;              // a thread: of blocks of 512 threads two fit an SM (112 KB each), of 256 threads three
 
 template <class K>
 cudaError_t launch(K kernel, const LossArgs& a, unsigned grid, unsigned threads, int cluster, int smem, cudaStream_t s) {
@@ -733,6 +733,11 @@ template <int DT, int MODE, int kThreads> cudaError_t resident(LossArgs a, int64
     if (per <= 7 * kThreads) return rows_of<7, kThreads, DT, MODE>(a, s, sms);
   }
   if (per <= 10 * kThreads) return rows_of<10, kThreads, DT, MODE>(a, s, sms);
+  // With 13 vectors four blocks of 256 threads fit an SM (bf16, us, three in brackets: 4096 x 24,000 83 (87), 4096 x 100,277 345 (397), 2048 x 200,064 337
+  // (397); fp32 2048 x 50,257 150 (177)); three are better for fp32 rows of one block (8192 x 12,000 136, four 143),
+  // and for what 14 vectors hold and 13 do not (bf16 4096 x 28,000 98, as two blocks of 7 vectors 106; 4096 x 56,000 192 and 211).
+  if constexpr (kThreads == 256)
+    if (per <= 13 * kThreads && (DT == JP_BF16 || a.cluster > 1)) return rows_of<13, kThreads, DT, MODE>(a, s, sms);
   return rows_of<kMostVectors, kThreads, DT, MODE>(a, s, sms);
 }
 
@@ -752,7 +757,7 @@ template <int DT, int MODE> cudaError_t rows(LossArgs a, cudaStream_t s, int sms
     if (narrow && vecs <= 64 * 2) return rows_of<2, 64, DT, MODE>(a, s, sms);
     if (narrow && vecs <= 64 * 4) return rows_of<4, 64, DT, MODE>(a, s, sms);
     if (narrow && vecs <= 128 * 7) return rows_of<7, 128, DT, MODE>(a, s, sms);
-    // four rows' blocks an SM where eight blocks of 256 threads hold a row, two where it takes eight of 512
+    // four rows' blocks an SM (three with 14 vectors a thread) where eight blocks of 256 threads hold a row, two where it takes eight of 512
     if (vecs <= (int64_t)kMaxCluster * 256 * kMostVectors) {
       a.cluster = cluster_for(a.T, vecs, 256, kMostVectors, sms);
       return resident<DT, MODE, 256>(a, vecs, s, sms);

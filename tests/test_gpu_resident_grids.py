@@ -78,3 +78,11 @@ LOSSES = [(700, 20011, BF), (700, 24000, BF), (700, 27000, BF), (700, 12000, F32
 def test_rows_of_logits(ctx, T, V, dtype, grad):
     for blocks, fit, each, threads in launches(loss_call(ctx, T, V, dtype, grad), "loss_rows_kernel"):
         assert blocks <= fit, (blocks, fit, each, threads)
+
+
+@pytest.mark.parametrize("T,V,dtype", [(700, 20011, BF), (700, 24000, BF), (700, 26624, BF), (700, 32000, BF), (700, 50257, BF), (700, 25000, F32), (700, 50257, F32),
+                                       (400, 100277, BF), (300, 151936, BF), (300, 200064, BF), (300, 212992, BF), (300, 106496, F32)])
+def test_four_blocks_an_sm(ctx, T, V, dtype):
+    """Rows that 13 vectors a thread of up to eight blocks of 256 threads hold (fp32: of two blocks or more)."""
+    for blocks, fit, each, threads in launches(loss_call(ctx, T, V, dtype, True), "loss_rows_kernel"):
+        assert threads == 256 and each == 4 and blocks <= fit, (blocks, fit, each, threads)
