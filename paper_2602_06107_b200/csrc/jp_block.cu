@@ -1002,14 +1002,16 @@ template <auto kernel, class... Q> cudaError_t launch(dim3 grid, dim3 block, int
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Forward: a block a group, 1024 threads an SM.
+// Forward: a block a group, 1024 threads an SM, or what an SM's memory holds of such blocks with what each has beside its rows' places (64 threads: 15).
+constexpr int kSmBytes = 228 * 1024, kOwnBytes = 1024 + 2 * kMaxValues * kMaxWarps * (int)sizeof(float);
 template <int DT, bool FULL> cudaError_t forward(const BlockArgs& a, cudaStream_t s, int sms) {
   const Plan p = plan_for(a, false, false, 2, 1024, 1024, sms);
   if (p.rows == 0) {
     block_fwd_wide_kernel<DT><<<(unsigned)(a.T < sms ? a.T : sms), 1024, 0, s>>>(a);
     return cudaGetLastError();
   }
-  const dim3 g((unsigned)grid_for(a.T, p, 1, (int64_t)sms * (p.groups < 24 ? p.groups : 24))), b(p.threads);
+  const int fit = kSmBytes / (p.smem + kOwnBytes), most = p.groups < 24 ? p.groups : 24;
+  const dim3 g((unsigned)grid_for(a.T, p, 1, (int64_t)sms * (fit < most ? fit : most))), b(p.threads);
   constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
 #define JP_FORWARD(KIND, NU, R, TWICE) (p.threads <= 256 ? launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 256>>(g, b, p.smem, s, a, p.place) \
                                        : p.threads <= 512 ? launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 512>>(g, b, p.smem, s, a, p.place) \

@@ -86,3 +86,27 @@ def test_four_blocks_an_sm(ctx, T, V, dtype):
     """Rows that 13 vectors a thread of up to eight blocks of 256 threads hold (fp32: of two blocks or more)."""
     for blocks, fit, each, threads in launches(loss_call(ctx, T, V, dtype, True), "loss_rows_kernel"):
         assert threads == 256 and each == 4 and blocks <= fit, (blocks, fit, each, threads)
+
+
+def block_call(ctx, T, H, dtype, full, ld):
+    m = lambda: torch.zeros((T, ld), device="cuda", dtype=dtype)[:, :H]
+    x, r, y, total = m(), m(), m(), m()
+    w = torch.ones(H, device="cuda")
+    extra = dict(post_weight=w, gate=w, token_gate=torch.ones(T, device="cuda")) if full else dict(post_weight=w)
+
+    def call():
+        f = runner.block_norm(ctx, x, r, w, eps=1e-6, rms=not full, out=y, out_sum=total, **extra)
+        runner.block_norm_backward(ctx, y, None, x, total, w, f["mean"], f["rstd"], post_mean=f["post_mean"], post_rstd=f["post_rstd"], rms=not full, bias=full, **extra)
+    return call
+
+
+# every number of threads a row from 32 to 1024, with 8 and 16 elements each; rows on 16 bytes and off them
+@pytest.mark.parametrize("H", [8, 64, 256, 264, 500, 512, 520, 768, 1000, 1024, 1283, 1536, 2047, 2048, 2560, 4095, 4096, 5120, 8191, 8192, 16384])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("full", [True, False])
+def test_rows_of_block_norms(ctx, H, dtype, full):
+    for T in (300, 9600, 40000 if H <= 2048 else 9601):
+        call = block_call(ctx, T, H, dtype, full, H)
+        for name in ("block_fwd_kernel", "block_bwd_kernel") if H <= 5120 else ("block_fwd",):
+            for blocks, fit, each, threads in launches(call, name):
+                assert blocks <= fit, (name, T, blocks, fit, each, threads)
