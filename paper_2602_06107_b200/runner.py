@@ -1,6 +1,8 @@
 """Output allocation around the libjackpot calls (no arithmetic of the method here)."""
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
 from . import binding as B
@@ -387,11 +389,17 @@ def _loss_rows(logits, tokens, mask, grad, d_logits):
     return shape[0], shape[1], ld, _logit_pitch(d_logits, shape, "d_logits"), d_logits
 
 
+def _no_gradient(grad, grad_out):
+    """A gradient times 0: the entries take a 0 in their descriptor for 1, so they are called without a gradient and it is set to 0."""
+    return grad and ctypes.c_float(float(grad_out)).value == 0.0
+
+
 def policy_loss(ctx: B.Context, logits, tokens, advantages, logp_old, *, logp_ref=None, mask=None, token_weight=None, n_valid=0,
                 eps_lo=0.2, eps_hi=0.2, kl_coef=0.0, temperature=1.0, grad_out=1.0, grad=True, d_logits=None):
     """One jp_policy_loss call on torch's current stream: the clipped policy loss of one model's logits [T, V] with a KL term to a
     reference model, and its gradient.  tokens [T] int32, advantages, logp_old, logp_ref, token_weight [T] fp32, mask [T] uint8.
-    ``n_valid``: the tokens of the whole batch, where this call holds a part of it (0: counted from the mask).  ``d_logits``: where the
+    ``n_valid``: the tokens of the whole batch, where this call holds a part of it (0: counted from the mask).  ``eps_lo`` = ``eps_hi`` = 0
+    switches the clip off; ``temperature`` 0 is taken for 1; ``grad_out`` 0 gives a gradient of 0.  ``d_logits``: where the
     gradient goes (may be ``logits``).  Returns ``loss`` [3] (whole, clipped term, KL term), ``logp``, ``kl``, ``state`` [T] and
     ``d_logits`` (None without ``grad``).  Rows are a multiple of 16 bytes apart: those of an odd vocabulary are a slice of wider rows."""
     T, V, ld, ld_d, d_logits = _loss_rows(logits, tokens, mask, grad, d_logits)
@@ -404,8 +412,11 @@ def policy_loss(ctx: B.Context, logits, tokens, advantages, logp_old, *, logp_re
                state=torch.empty_like(advantages, dtype=torch.uint8), d_logits=d_logits)
     need = B.jp_policy_workspace_bytes(ctx, T)
     ws = advantages.new_empty(need, dtype=torch.uint8) if need else None
+    zero = _no_gradient(grad, grad_out)
     B.jp_policy_loss(ctx, d, logits, tokens, mask, advantages, logp_old, logp_ref, token_weight, out["loss"], out["logp"],
-                     out["kl"], out["state"], d_logits, ws)
+                     out["kl"], out["state"], None if zero else d_logits, ws)
+    if zero:
+        d_logits.zero_()
     return out
 
 
@@ -413,7 +424,7 @@ def preference_loss(ctx: B.Context, logits, tokens, seq_start, *, ref_logp=None,
                     margin=0.0, average=False, grad_out=1.0, grad=True, d_logits=None):
     """One jp_preference_loss call on torch's current stream: the loss of P pairs of sequences packed in logits [T, V], and its
     gradient.  seq_start [2 P + 1] int32: sequence 2 i (chosen) and 2 i + 1 (rejected) are pair i; ref_logp [2 P] fp32: the reference
-    model's sums (means with ``average``).  Returns ``loss`` [1], ``margin`` [P], ``seq_logp`` [2 P], ``logp``, ``state`` [T] and
+    model's sums (means with ``average``).  ``grad_out`` 0 gives a gradient of 0.  Returns ``loss`` [1], ``margin`` [P], ``seq_logp`` [2 P], ``logp``, ``state`` [T] and
     ``d_logits`` (None without ``grad``; may be ``logits``)."""
     T, V, ld, ld_d, d_logits = _loss_rows(logits, tokens, mask, grad, d_logits)
     if seq_start.dim() != 1 or seq_start.shape[0] % 2 == 0:
@@ -430,8 +441,11 @@ def preference_loss(ctx: B.Context, logits, tokens, seq_start, *, ref_logp=None,
                state=torch.empty_like(tokens, dtype=torch.uint8), d_logits=d_logits)
     need = B.jp_preference_workspace_bytes(ctx, T, n // 2)
     ws = seq_start.new_empty(need, dtype=torch.uint8) if need else None
+    zero = _no_gradient(grad, grad_out)
     B.jp_preference_loss(ctx, d, logits, tokens, mask, seq_start, ref_logp, out["loss"], out["margin"], out["seq_logp"],
-                         out["logp"], out["state"], d_logits, ws)
+                         out["logp"], out["state"], None if zero else d_logits, ws)
+    if zero:
+        d_logits.zero_()
     return out
 
 
