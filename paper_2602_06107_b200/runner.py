@@ -576,9 +576,10 @@ def quantize_tokens_i8(ctx: B.Context, x):
     return I8Tokens(data, M, K)
 
 
-def linear_i8(ctx: B.Context, x, w: I8Weight, *, out_dtype=torch.bfloat16, out=None):
+def linear_i8(ctx: B.Context, x, w: I8Weight, *, out_dtype=torch.bfloat16, out=None, status=None):
     """One jp_i8_linear call on torch's current stream: x [M, K] bf16 (or what :func:`quantize_tokens_i8` made of it) times the packed
-    weight: [M, N], contiguous or in ``out``."""
+    weight: [M, N], contiguous or in ``out``.  ``status``: an int32 CUDA tensor of one element, written by the call: 0, or JP_ERR_TIMEOUT
+    (-6) if a wait inside the kernel gave up, in which case the result is unspecified."""
     if isinstance(x, I8Tokens):
         M, K, data, src, ld_x = x.M, x.K, x.data, None, 0
     else:
@@ -590,5 +591,7 @@ def linear_i8(ctx: B.Context, x, w: I8Weight, *, out_dtype=torch.bfloat16, out=N
         out = w.packed.new_empty((M, w.N), dtype=out_dtype)
     elif out.shape != (M, w.N):
         raise B.JackpotError(f"out must be [{M}, {w.N}]")
-    B.jp_i8_linear(ctx, w.desc, w.packed, src, ld_x, M, data, out, _rows(out, "out"), B._dtype_code(out, "out"))
+    if status is not None:
+        _dense(status, (1,), torch.int32, "status")
+    B.jp_i8_linear(ctx, w.desc, w.packed, src, ld_x, M, data, out, _rows(out, "out"), B._dtype_code(out, "out"), status)
     return out
