@@ -619,7 +619,8 @@ jp_status jp_policy_loss(jp_ctx* ctx, const jp_policy_desc* desc, const void* lo
  * (the reference model's S_s; NULL: 0):
  *   h_i = beta ((S_2i - R_2i) - (S_2i+1 - R_2i+1)) - margin
  *   out_loss[0] = mean over pairs of -(1 - label_smoothing) log sigma(h) - label_smoothing log sigma(-h)
- * (0 if P is 0; a NaN in ref_logp makes it NaN, and the gradient of its pair 0).  temperature is 1.  A row's coefficient needs both sequences of its pair, so the logits are read twice. */
+ * (0 if P is 0; a NaN in ref_logp makes it NaN, and the gradient of its pair 0; an infinite one its pair's h infinite: a loss of 0 on the one side, where
+ * label_smoothing is 0, infinity on the other).  temperature is 1.  A row's coefficient needs both sequences of its pair, so the logits are read twice. */
 enum { JP_PREFERENCE_AVERAGE = 1 };
 typedef struct {
   int64_t T, V, ld, ld_d;   /* as above                                                 */

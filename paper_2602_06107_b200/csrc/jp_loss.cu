@@ -626,7 +626,8 @@ __global__ void __launch_bounds__(1024) preference_pairs_kernel(LossArgs A) {
     if (A.ref_logp) gap -= (double)A.ref_logp[2 * p] - (double)A.ref_logp[2 * p + 1];
     const double h = (double)A.beta * gap - (double)A.margin, e = A.label_smoothing;
     const double up = log1p(exp(-fabs(h)));
-    loss += (1.0 - e) * (up + fmax(-h, 0.0)) + e * (up + fmax(h, 0.0));
+    // (a side without weight adds nothing, also where h is infinite)
+    loss += (e < 1.0 ? (1.0 - e) * (up + fmax(-h, 0.0)) : 0.0) + (e > 0.0 ? e * (up + fmax(h, 0.0)) : 0.0);
     // (sigma of either sign without taking 1 - sigma, which would lose the small one)
     const double small = exp(-fabs(h)) / (1.0 + exp(-fabs(h))), large = 1.0 / (1.0 + exp(-fabs(h)));
     const double slope = (double)A.beta * A.grad_scale / (double)A.P * (e * (h > 0.0 ? large : small) - (1.0 - e) * (h > 0.0 ? small : large));
