@@ -290,6 +290,7 @@ jp_status jp_create(jp_ctx** out_ctx, int device, void* cuda_stream) {
   c->device = device;
   c->stream = (cudaStream_t)cuda_stream;
   c->sms = stream_grid_size(device);
+  if (device < kKnownDevices) device_epoch[device].fetch_add(1, std::memory_order_acq_rel);
   *out_ctx = c;
   return JP_OK;
 }

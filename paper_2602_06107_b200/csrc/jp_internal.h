@@ -336,17 +336,21 @@ cudaError_t launch_verify(VerifyArgs a, int dtype, cudaStream_t s);
 
 
 // Sets what a kernel needs before its launch (the most dynamic shared memory of a block, and the carveout for it) on the current device, the first
-// time only: the amounts belong to the kernel on the device and are always the same, whatever the call.
+// time only: the amounts belong to the kernel on the device and are always the same, whatever the call.  First, that is, since a context was last
+// created for the device: it may have been reset in between, which takes the amounts back.
+constexpr int kKnownDevices = 64;
+inline std::atomic<uint32_t> device_epoch[kKnownDevices];           // contexts created so far
 template <auto kernel> cudaError_t allow_shared_memory(int bytes) {
-  static std::atomic<uint64_t> done{0};
+  static std::atomic<uint32_t> done[kKnownDevices];
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
-  const uint64_t bit = 1ull << (device & 63);
-  if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  const bool known = device < kKnownDevices;
+  const uint32_t epoch = known ? device_epoch[device].load(std::memory_order_acquire) : 0u;
+  if (known && done[device].load(std::memory_order_acquire) == epoch) return cudaSuccess;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-  if (e == cudaSuccess && device < 64) done.fetch_or(bit, std::memory_order_release);
+  if (e == cudaSuccess && known) done[device].store(epoch, std::memory_order_release);
   return e;
 }
 
