@@ -441,9 +441,10 @@ __device__ __forceinline__ void row_stats(const BlockArgs& A, const Un& un, Get 
 
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
-// R rows at a time.  FULL: layer norm, biases, a gate a token; without it those instructions and registers are left out.
-template <int DT, int KIND, int NU, int R, int STAGES, bool FULL, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS > 512 ? 1 : 1024 / THREADS) block_fwd_kernel(const __grid_constant__ BlockArgs A, int place) {
+// R rows at a time.  FULL: layer norm, biases, a gate a token; without it those instructions and registers are left out.  (64 registers, whatever the block:
+// an SM has 1024 threads of it.)
+template <int DT, int KIND, int NU, int R, int STAGES, bool FULL>
+__global__ void __launch_bounds__(1024, 1) block_fwd_kernel(const __grid_constant__ BlockArgs A, int place) {
   using Un = Unit<DT, KIND>;
   constexpr int ES = Vec<DT>::ESIZE, P = Un::P;
   extern __shared__ uint4 places[];
@@ -1013,15 +1014,11 @@ template <int DT, bool FULL> cudaError_t forward(const BlockArgs& a, cudaStream_
   const int fit = kSmBytes / (p.smem + kOwnBytes), most = p.groups < 24 ? p.groups : 24;
   const dim3 g((unsigned)grid_for(a.T, p, 1, (int64_t)sms * (fit < most ? fit : most))), b(p.threads);
   constexpr int V = DT == JP_BF16 ? 1 : 2, E = 4;
-#define JP_FORWARD(KIND, NU, R, TWICE) (p.threads <= 256 ? launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 256>>(g, b, p.smem, s, a, p.place) \
-                                       : p.threads <= 512 ? launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 512>>(g, b, p.smem, s, a, p.place) \
-                                                          : launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL, 1024>>(g, b, p.smem, s, a, p.place))
-#define JP_FORWARD_TWICE(KIND, NU) launch<block_fwd_kernel<DT, KIND, NU, 1, stages_of(1, true, DT), FULL, 1024>>(g, b, p.smem, s, a, p.place)
-  if (p.twice) return p.kind == kAligned ? JP_FORWARD_TWICE(kAligned, 2 * V) : p.kind == kShared ? JP_FORWARD_TWICE(kShared, 2 * V) : JP_FORWARD_TWICE(kElements, 2 * E);
+#define JP_FORWARD(KIND, NU, R, TWICE) launch<block_fwd_kernel<DT, KIND, NU, R, stages_of(R, TWICE, DT), FULL>>(g, b, p.smem, s, a, p.place)
+  if (p.twice) return p.kind == kAligned ? JP_FORWARD(kAligned, 2 * V, 1, true) : p.kind == kShared ? JP_FORWARD(kShared, 2 * V, 1, true) : JP_FORWARD(kElements, 2 * E, 1, true);
   if (p.rows == 2) return p.kind == kAligned ? JP_FORWARD(kAligned, V, 2, false) : p.kind == kShared ? JP_FORWARD(kShared, V, 2, false) : JP_FORWARD(kElements, E, 2, false);
   return p.kind == kAligned ? JP_FORWARD(kAligned, V, 1, false) : p.kind == kShared ? JP_FORWARD(kShared, V, 1, false) : JP_FORWARD(kElements, E, 1, false);
 #undef JP_FORWARD
-#undef JP_FORWARD_TWICE
 }
 
 // Backward: the groups of an SM in one block, of 512 threads, or of 640 with 96 registers each where that makes room for a row more (bf16, 8192 rows:
