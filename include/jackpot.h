@@ -583,7 +583,8 @@ jp_status jp_w4_linear(jp_ctx* ctx, const jp_w4_desc* desc, const void* packed, 
  *   lp = log p_x,   d_logits[v] = grad_out dL/dlp (1[v = x] - p_v) / temperature, rounded once; 0 in all V places of a row that takes no part.
  *   out_logp [T] fp32 or NULL: lp;  out_state [T] uint8 or NULL: 0 a row with mask 0 or a token outside [0, V), 1 a row that
  *     takes part, 2 (policy loss) one whose ratio sits on the clipped branch, 3 a row without usable numbers
- * A row holding NaN or +inf, or nothing above -1e38 (in units of log2: masked throughout), or whose terms are not finite (a token
+ * A row holding NaN or +inf (or, as the kernels take it, a logit whose z log2(e) / temperature is beyond fp32), or nothing above -1e38 there (masked
+ * throughout), or whose terms are not finite (a token
  * of probability 0 with a KL term, NaN among its inputs) has state 3 and takes no part, as a masked one; the
  * others do not depend on it.  -inf logits have probability 0 and gradient 0.
  * lp is off by 2^-17 + 2^-25 n at most, n the additions of a thread to its part of the row's sum (fp32): V / 4096 where a row has one block, V / 2048 of fp32 logits.

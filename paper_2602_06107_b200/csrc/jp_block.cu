@@ -17,8 +17,8 @@
 // 16 bytes (packed ones of odd width): the vectors that cover the row; what belongs to other rows is masked in the first one and cut from the
 // last one's copy, and a group's rows are a multiple of the period apart after which offsets repeat, so a thread keeps its columns.  Matrices at
 // different offsets: the group copies the covering vectors together and reads elements.
-// Measured, 8192 rows of bf16, RMS norms with gate: forward 4096 columns 48 us (5.6 TB/s), 4095 94 us; backward 4096 82 us (4.9 TB/s), 4095 143 us;
-// with layer norms, biases and a gate a token, backward, 126 and 245 us.
+// Measured, 8192 rows of bf16, RMS norms with gate: forward 4096 columns 48 us (5.6 TB/s), 4095 97 us; backward 4096 82 us (4.9 TB/s), 4095 145 us;
+// with layer norms, biases and a gate a token, forward 82 and 204 us, backward 127 and 248 us.
 #include "jp_common.cuh"
 #include "jp_internal.h"
 #include "jp_pairs.cuh"

@@ -11,10 +11,11 @@
 // shared memory in between, spread over the blocks of a cluster: HBM and L2 see one read and one write.  The preference loss needs both
 // sequences of a pair first: a pass for the sums, one for the gradients, each a stream through a ring of places.  Each thread copies its own
 // vectors (asynchronously, no barriers) and fetches the next row's into a place as soon as it has read it for the last time; several blocks
-// an SM (four of 256 threads where 13 vectors a thread hold a row, or two of 512 where eight small ones cannot), so that some load and store while others wait for their sum.
+// an SM (four of 256 threads where 13 vectors a thread hold a row, or two of 512 where eight small ones cannot), so that some load and store while
+// others wait for their sum.
 // One warp makes a row's scalars of the warps' sums.  Rows that no cluster can hold are read twice.
 // Measured, bf16, V = 151,936: policy loss, 4096 rows of which some are masked, 2.2 GB, 444 us (5.0 TB/s; with two blocks of 512 threads 483 instead
-// of 450, with five of 192 474); preference loss, six pairs of sequences, 3.5 GB in three passes, 646 us (5.4 TB/s).  Vectors are counted in
+// of 450, with five of 192 474); preference loss, six pairs of sequences, 3.5 GB in three passes, 642 us (5.5 TB/s).  Vectors are counted in
 // 32 bits: their addresses in 64 cost 1 to 3 %.
 // Sums of exponentials are fp32 (in 2^x of z log2(e) / tau, relative to a running maximum): a thread adds a vector's 8 (bf16) or 4 (fp32) terms as a tree
 // and the result to its sum, one addition a vector, each off by 2^-24 of the sum so far.  That is V / (8 or 4) / (threads of the blocks that share a
